@@ -382,6 +382,70 @@ ffsplit_status ffsplit_quant_unpack(ffsplit_ctx* ctx, const void* blob, int32_t 
  * eight at a time, one launch each; meant for decode, T <= 8).  X, Y dev bf16 [T, d].  Uses the workspace. */
 ffsplit_status ffsplit_quant_forward(ffsplit_ctx* ctx, const void* blob, const void* X, int64_t T, void* Y, void* stream);
 
+/* ---- Training a layer: forward and backward of the whole (unsplit) FFN, gradient norm and clipping ---------
+ * For fine-tuning a layer before it is scored and split.  The weights are the row-major tensors of
+ * ffsplit_weights, read where they are (they change with every optimiser step: nothing is packed or kept).
+ *   SWIGLU:  G = X W1, U = X W1u, H = SiLU(G) * U, Y = H W2 (+ b2)
+ *   GELU:    Z = X W1 + b1, H = act(Z), Y = H W2 + b2
+ * T >= 1 tokens.  Products of bf16 layers are accumulated in fp32; what one product hands to the next (H and the
+ * gradients of G, U or Z) is rounded to bf16 once, G, U and Z themselves are kept with at least 12 significant
+ * bits.  FFSPLIT_F32 layers keep fp32 accuracy throughout.  An infinity or NaN among the inputs makes the outputs
+ * it reaches non-finite (NaN where the formula may give an infinity). */
+
+/* Bytes of `saved` (what the backward pass keeps of the forward pass) and of the workspace that
+ * ffsplit_train_forward() and ffsplit_train_backward() need for T tokens of this layer. */
+ffsplit_status ffsplit_train_sizes(const ffsplit_shape* shape, int64_t T, size_t* saved_bytes, size_t* workspace_bytes);
+
+/* Y dev [T, d] from X dev [T, d], in the layer's dtype.
+ *   saved  dev, 256-byte aligned, saved_bytes >= what ffsplit_train_sizes() says: written for the backward pass
+ *          of the same layer, weights and X.  NULL: no backward pass will follow, nothing is kept.
+ * X and Y may not overlap.  Uses the workspace. */
+ffsplit_status ffsplit_train_forward(ffsplit_ctx* ctx, const ffsplit_shape* shape, const ffsplit_weights* weights,
+                                     const void* X, int64_t T, void* saved, size_t saved_bytes, void* Y, void* stream);
+
+/* Gradients of a loss with respect to the layer's inputs and weights, dev, in the layer's dtype and in the layouts
+ * of what they belong to; overwritten.  NULL: not wanted (its product is left out). */
+typedef struct {
+  void* dX;    /* [T, d] */
+  void* dW1;   /* [d, m] */
+  void* dW1u;  /* [d, m], SWIGLU only */
+  void* db1;   /* [m], GELU only      */
+  void* dW2;   /* [m, d] */
+  void* db2;   /* [d]    */
+} ffsplit_train_grads;
+
+/* dY dev [T, d] is the gradient of the loss with respect to Y; saved is what ffsplit_train_forward() wrote for the
+ * same weights and X (it is read only and may be used again).  The biases are not read.  At least one gradient must
+ * be asked for; no gradient may overlap another or an input.  Sums over tokens are taken in a fixed order. */
+ffsplit_status ffsplit_train_backward(ffsplit_ctx* ctx, const ffsplit_shape* shape, const ffsplit_weights* weights,
+                                      const void* X, int64_t T, const void* saved, size_t saved_bytes, const void* dY,
+                                      const ffsplit_train_grads* grads, void* stream);
+
+/* One of the tensors whose gradients are clipped together.  n elements, contiguous, aligned to their own size (no
+ * 16-byte rule: views into a flat buffer are fine).  out may be in (in place) or a tensor that overlaps none. */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t n;       /* >= 0; pointers of an empty tensor are not looked at */
+  int32_t dtype;   /* ffsplit_dtype of in and out */
+} ffsplit_grad_tensor;
+
+/* Workspace that the two calls below need for a list of `count` tensors. */
+ffsplit_status ffsplit_grad_workspace_size(int32_t count, size_t* bytes);
+
+/* norm dev float[1] = the 2-norm of all elements of all tensors (out is not used).  Squares are summed in fp32 over
+ * runs of at most 16 bytes (in fp64 where those would leave fp32's range) and in fp64 from there on, in a fixed order.
+ * `tensors` is a host array, read before the call returns; count may be 0 (norm 0).
+ * A non-finite norm is written as it is and reported as FFSPLIT_ERR_NONFINITE through ffsplit_poll(). */
+ffsplit_status ffsplit_grad_norm(ffsplit_ctx* ctx, const ffsplit_grad_tensor* tensors, int32_t count, float* norm,
+                                 void* stream);
+
+/* The norm as above, then out = in * min(1, max_norm / (norm + 1e-6)) for every tensor, the product taken in fp32 and
+ * rounded to the tensor's type.  max_norm >= 0 (an infinity clips nothing).  Where the norm is not finite the
+ * gradients are left as they are (copied, where out is another tensor), and ffsplit_poll() reports it. */
+ffsplit_status ffsplit_grad_clip(ffsplit_ctx* ctx, const ffsplit_grad_tensor* tensors, int32_t count, float max_norm,
+                                 float* norm, void* stream);
+
 /* Synchronise `stream`, then return and clear the first device-side condition found in the workspace's
  * status word or in that of the built-in scratch of ffsplit_forward_noalloc() on the context's device
  * (FFSPLIT_OK if no kernel recorded one).  Works on a context without a workspace. */

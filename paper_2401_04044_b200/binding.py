@@ -38,6 +38,8 @@ EXPORTS = [
     "ffsplit_debug_wait_timeout", "ffsplit_quant_pack_size", "ffsplit_quant_workspace_size", "ffsplit_quant_pack",
     "ffsplit_quant_blob_open", "ffsplit_quant_unpack", "ffsplit_quant_forward",
     "ffsplit_factor_workspace_size", "ffsplit_factor_light", "ffsplit_encoder_workspace_size", "ffsplit_encoder_forward",
+    "ffsplit_train_sizes", "ffsplit_train_forward", "ffsplit_train_backward",
+    "ffsplit_grad_workspace_size", "ffsplit_grad_norm", "ffsplit_grad_clip",
 ]
 
 
@@ -58,6 +60,15 @@ class Weights(C.Structure):
 class Factors(C.Structure):
     _fields_ = [("A1", C.c_void_p), ("B1", C.c_void_p), ("A1u", C.c_void_p), ("B1u", C.c_void_p),
                 ("A2", C.c_void_p), ("B2", C.c_void_p), ("r", C.c_int32)]
+
+
+class TrainGrads(C.Structure):
+    _fields_ = [("dX", C.c_void_p), ("dW1", C.c_void_p), ("dW1u", C.c_void_p), ("db1", C.c_void_p), ("dW2", C.c_void_p),
+                ("db2", C.c_void_p)]
+
+
+class GradTensor(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
 class FFSplitError(RuntimeError):
@@ -113,6 +124,12 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.ffsplit_forward.argtypes = [vp, vp, vp, i64, vp, vp]
     lib.ffsplit_forward_host.argtypes = [vp, vp, vp, i64, vp, vp]
     lib.ffsplit_forward_noalloc.argtypes = [vp, vp, vp, i64, vp, vp]
+    lib.ffsplit_train_sizes.argtypes = [P(Shape), i64, P(sz), P(sz)]
+    lib.ffsplit_train_forward.argtypes = [vp, P(Shape), P(Weights), vp, i64, vp, sz, vp, vp]
+    lib.ffsplit_train_backward.argtypes = [vp, P(Shape), P(Weights), vp, i64, vp, sz, vp, P(TrainGrads), vp]
+    lib.ffsplit_grad_workspace_size.argtypes = [i32, P(sz)]
+    lib.ffsplit_grad_norm.argtypes = [vp, vp, i32, vp, vp]
+    lib.ffsplit_grad_clip.argtypes = [vp, vp, i32, C.c_float, vp, vp]
     lib.ffsplit_poll.argtypes = [vp, vp]
     lib.ffsplit_profile_begin.argtypes = [vp]
     lib.ffsplit_profile_end.argtypes = [vp, vp, i32, P(i32), P(C.c_double), P(C.c_double)]
@@ -138,6 +155,28 @@ def _ptr(t: Optional[torch.Tensor]):
 def _stream_ptr(stream=None):
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.c_void_p(s.cuda_stream)
+
+
+class GradList:
+    """The tensors whose gradients are clipped together, as the array ffsplit_grad_norm() / ffsplit_grad_clip() take.
+    `out` holds where the clipped gradients go, tensor by tensor; without it they replace the gradients.  The list
+    keeps the tensors alive and names their memory: make a new one when a gradient moves to another buffer."""
+
+    def __init__(self, device: int, grads, out=None):
+        self.grads, self.out = list(grads), list(grads) if out is None else list(out)
+        if len(self.grads) != len(self.out):
+            raise FFSplitError(2, "grad_list", "as many outputs as gradients are needed")
+        for g, o in zip(self.grads, self.out):
+            for t in (g, o):
+                if t.dtype not in DTYPE_IDS or t.dtype != g.dtype:
+                    raise FFSplitError(4, "grad_list", "gradients are float32 or bfloat16, and outputs of the same type")
+                if t.numel() != g.numel() or not t.is_contiguous():
+                    raise FFSplitError(2, "grad_list", "tensors must be contiguous, and outputs as long as the gradients")
+                if t.device.type != "cuda" or t.device.index != device:
+                    raise FFSplitError(1, "grad_list", f"tensors must be on cuda:{device}")
+        self.count = len(self.grads)
+        self.array = (GradTensor * max(1, self.count))(*[
+            GradTensor(g.data_ptr(), o.data_ptr(), g.numel(), DTYPE_IDS[g.dtype]) for g, o in zip(self.grads, self.out)])
 
 
 def make_shape(d: int, m: int, act, dtype) -> Shape:
@@ -344,6 +383,82 @@ class Context:
     def quant_forward(self, blob, X, Y, stream=None):
         self._check(self.lib.ffsplit_quant_forward(self.h, _ptr(blob), _ptr(X), X.shape[0], _ptr(Y), _stream_ptr(stream)),
                     "ffsplit_quant_forward")
+
+    # ------------------------------------------------------------------ training
+    def _operand(self, where: str, name: str, t, shape: Shape, dims, optional: bool = True):
+        """Pointer of one tensor of a training call, checked against what the layer says it has to be."""
+        if t is None:
+            if optional:
+                return None
+            raise FFSplitError(1, where, f"{name} is missing")
+        if DTYPE_IDS.get(t.dtype) != shape.dtype:
+            raise FFSplitError(4, where, f"{name} is {t.dtype}, which is not the layer's type")
+        if tuple(t.shape) != tuple(dims) or not t.is_contiguous():
+            raise FFSplitError(2, where, f"{name} must be contiguous and of shape {tuple(dims)}")
+        if t.device.type != "cuda" or t.device.index != self.device:
+            raise FFSplitError(1, where, f"{name} must be on cuda:{self.device}")
+        return t.data_ptr()
+
+    def _train_weights(self, where, shape, W1, W1u, b1, W2, b2):
+        d, m, op = shape.d, shape.m, self._operand
+        return Weights(op(where, "W1", W1, shape, (d, m), False), op(where, "W1u", W1u, shape, (d, m)),
+                       op(where, "b1", b1, shape, (m,)), op(where, "W2", W2, shape, (m, d), False),
+                       op(where, "b2", b2, shape, (d,)))
+
+    def train_sizes(self, shape: Shape, T: int):
+        """-> (bytes of `saved`, bytes of workspace) that train_forward / train_backward need for T tokens."""
+        a, b = C.c_size_t(), C.c_size_t()
+        rc = self.lib.ffsplit_train_sizes(C.byref(shape), T, C.byref(a), C.byref(b))
+        if rc != OK:
+            raise FFSplitError(rc, "ffsplit_train_sizes")
+        return a.value, b.value
+
+    def train_forward(self, shape: Shape, W1, b1, W2, b2, X, Y, saved=None, W1u=None, stream=None):
+        """ffsplit_train_forward: Y from the row-major weights; `saved` (a byte tensor) is written for train_backward()."""
+        where, T = "ffsplit_train_forward", X.shape[0]
+        w = self._train_weights(where, shape, W1, W1u, b1, W2, b2)
+        rc = self.lib.ffsplit_train_forward(
+            self.h, C.byref(shape), C.byref(w), self._operand(where, "X", X, shape, (T, shape.d), False), T, _ptr(saved),
+            0 if saved is None else saved.numel() * saved.element_size(),
+            self._operand(where, "Y", Y, shape, (T, shape.d), False), _stream_ptr(stream))
+        self._check(rc, where)
+
+    def train_backward(self, shape: Shape, W1, b1, W2, X, saved, dY, dX=None, dW1=None, db1=None, dW2=None, db2=None,
+                       W1u=None, dW1u=None, stream=None):
+        """ffsplit_train_backward: writes the gradients that are given (None: not wanted)."""
+        where, T, d, m, op = "ffsplit_train_backward", X.shape[0], shape.d, shape.m, self._operand
+        w = self._train_weights(where, shape, W1, W1u, b1, W2, None)
+        g = TrainGrads(op(where, "dX", dX, shape, (T, d)), op(where, "dW1", dW1, shape, (d, m)),
+                       op(where, "dW1u", dW1u, shape, (d, m)), op(where, "db1", db1, shape, (m,)),
+                       op(where, "dW2", dW2, shape, (m, d)), op(where, "db2", db2, shape, (d,)))
+        rc = self.lib.ffsplit_train_backward(
+            self.h, C.byref(shape), C.byref(w), op(where, "X", X, shape, (T, d), False), T, _ptr(saved),
+            0 if saved is None else saved.numel() * saved.element_size(), op(where, "dY", dY, shape, (T, d), False),
+            C.byref(g), _stream_ptr(stream))
+        self._check(rc, where)
+
+    def grad_list(self, grads, out=None) -> "GradList":
+        return GradList(self.device, grads, out)
+
+    def grad_workspace_size(self, count: int) -> int:
+        n = C.c_size_t()
+        self._check(self.lib.ffsplit_grad_workspace_size(count, C.byref(n)), "ffsplit_grad_workspace_size")
+        return n.value
+
+    def _norm_ptr(self, where, norm):
+        if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device.type != "cuda" or norm.device.index != self.device:
+            raise FFSplitError(2, where, f"norm must be one float32 on cuda:{self.device}")
+        return _ptr(norm)
+
+    def grad_norm(self, grads: "GradList", norm, stream=None):
+        """ffsplit_grad_norm: norm[0] = the 2-norm of all gradients of the list."""
+        self._check(self.lib.ffsplit_grad_norm(self.h, C.byref(grads.array), grads.count, self._norm_ptr("ffsplit_grad_norm", norm),
+                                               _stream_ptr(stream)), "ffsplit_grad_norm")
+
+    def clip_grads(self, grads: "GradList", max_norm: float, norm, stream=None):
+        """ffsplit_grad_clip: the norm, then every gradient times min(1, max_norm / (norm + 1e-6))."""
+        self._check(self.lib.ffsplit_grad_clip(self.h, C.byref(grads.array), grads.count, max_norm,
+                                               self._norm_ptr("ffsplit_grad_clip", norm), _stream_ptr(stream)), "ffsplit_grad_clip")
 
     def debug_wait_timeout(self, limit_cycles: int, stream=None):
         self._check(self.lib.ffsplit_debug_wait_timeout(self.h, int(limit_cycles), _stream_ptr(stream)),

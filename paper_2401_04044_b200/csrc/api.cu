@@ -43,6 +43,30 @@ bool decode_path_applies(const ffsplit_ctx* ctx, const BlobHeader& h, long long 
 char* noalloc_control_block(int device);   // nullptr until ffsplit_forward_noalloc has run on that device
 size_t decode_scratch_bytes(int dtype, long long T);
 
+ffsplit_status check_shape(ffsplit_ctx* ctx, const ffsplit_shape* s) {
+  if (!s) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "shape is NULL");
+  if (s->d < 1 || s->m < 1) return fail(ctx, FFSPLIT_ERR_SHAPE, "d and m must be >= 1");
+  if (s->act < 0 || s->act > 2) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "unknown activation");
+  if (s->dtype != FFSPLIT_F32 && s->dtype != FFSPLIT_BF16) return fail(ctx, FFSPLIT_ERR_DTYPE, "unknown dtype");
+  if (s->dtype == FFSPLIT_BF16 && s->d % 8 != 0)
+    return fail(ctx, FFSPLIT_ERR_SHAPE, "bf16 layers need d to be a multiple of 8");
+  return FFSPLIT_OK;
+}
+
+ffsplit_status check_ctx(ffsplit_ctx* ctx, bool need_ws) {
+  if (!ctx) return FFSPLIT_ERR_INVALID_ARG;
+  ctx->err.clear();
+  ctx->prep_active = false;   // a batch left open by a call that failed half-way is dropped
+  ctx->prep.n = 0;
+  int dev = -1;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaGetDevice");
+  if (dev != ctx->device) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "the context's device is not the current device");
+  if (need_ws && (!ctx->ws || ctx->ws_bytes < kCtrlBytes))
+    return fail(ctx, FFSPLIT_ERR_BUFFER_TOO_SMALL, "no workspace set (ffsplit_set_workspace)");
+  return FFSPLIT_OK;
+}
+
 namespace {
 
 constexpr size_t kAlign = 256;
@@ -64,16 +88,6 @@ SplitDims make_dims(const ffsplit_shape& s, int k, int r) {
   if (o.k_pad + o.r_pad == 0) o.k_pad = 16;  // keeps the last GEMM non-empty: Y = b2
   o.kp_rp = o.k_pad + o.r_pad;
   return o;
-}
-
-ffsplit_status check_shape(ffsplit_ctx* ctx, const ffsplit_shape* s) {
-  if (!s) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "shape is NULL");
-  if (s->d < 1 || s->m < 1) return fail(ctx, FFSPLIT_ERR_SHAPE, "d and m must be >= 1");
-  if (s->act < 0 || s->act > 2) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "unknown activation");
-  if (s->dtype != FFSPLIT_F32 && s->dtype != FFSPLIT_BF16) return fail(ctx, FFSPLIT_ERR_DTYPE, "unknown dtype");
-  if (s->dtype == FFSPLIT_BF16 && s->d % 8 != 0)
-    return fail(ctx, FFSPLIT_ERR_SHAPE, "bf16 layers need d to be a multiple of 8");
-  return FFSPLIT_OK;
 }
 
 ffsplit_status check_split(ffsplit_ctx* ctx, const ffsplit_shape* s, int k, int r) {
@@ -172,20 +186,6 @@ ScoreLayout score_layout(const ffsplit_shape& s, long long T) {
   L.partial = off; off = align_up(off + (size_t)L.groups * s.m * 4);
   L.end = off;
   return L;
-}
-
-ffsplit_status check_ctx(ffsplit_ctx* ctx, bool need_ws) {
-  if (!ctx) return FFSPLIT_ERR_INVALID_ARG;
-  ctx->err.clear();
-  ctx->prep_active = false;   // a batch left open by a call that failed half-way is dropped
-  ctx->prep.n = 0;
-  int dev = -1;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaGetDevice");
-  if (dev != ctx->device) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "the context's device is not the current device");
-  if (need_ws && (!ctx->ws || ctx->ws_bytes < kCtrlBytes))
-    return fail(ctx, FFSPLIT_ERR_BUFFER_TOO_SMALL, "no workspace set (ffsplit_set_workspace)");
-  return FFSPLIT_OK;
 }
 
 // A blob is known to a context once ffsplit_pack() wrote it or ffsplit_blob_open() registered it there;
