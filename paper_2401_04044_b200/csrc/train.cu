@@ -5,135 +5,127 @@
 //           dW1 = X^T dG, dW1u = X^T dU, dW2 = H^T dY, db2 = sum_t dY
 //   GELU:   Z = X W1 + b1, H = act(Z), Y = H W2 + b2; dZ = (dY W2^T) act'(Z), the rest likewise, db1 = sum_t dZ
 //
-// First form: one plain fp32 kernel for all products (64 x 64 tiles, any strides), with the activation or its
-// derivative in its epilogue.
+// The products run on the tensor cores from the tensors where they lie (train_gemm.cu): two launches forward, two
+// backward (dH with the activation's derivative; then every gradient that was asked for, as one launch).
+// fp32 layers are first split into bf16 planes here; bf16 layers whose m is no multiple of 8 get W1 (W1u) copied to
+// rows of 16 bytes, which TMA asks for.
 #include <cstring>
 
 #include "epilogue.cuh"
-#include "internal.h"
+#include "train_gemm.h"
 
 namespace ffsp {
 namespace train {
 
-__device__ __forceinline__ void act_and_slope(float z, int act, float* value, float* slope) {
-  if (act == FFSPLIT_SWIGLU) {
-    const float s = 1.0f / (1.0f + expf(-z));
-    *value = z * s;
-    *slope = s * (1.0f + z * (1.0f - s));
-  } else if (act == FFSPLIT_GELU_ERF) {
-    const float phi = 0.5f * erfcf(-z * 0.70710678118654752f);
-    *value = z * phi;
-    *slope = phi + z * (0.3989422804014327f * expf(-0.5f * z * z));
-  } else {
-    const float c = 0.79788456080286536f, a = 0.044715f;
-    const float t = tanhf(c * (z + a * z * z * z));
-    *value = 0.5f * z * (1.0f + t);
-    *slope = 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * (c * (1.0f + 3.0f * a * z * z));
+constexpr int MAX_JOBS = 5;
+struct PrepJob {
+  const void* in;          // [rows, cols], pitch cols
+  __nv_bfloat16* out;      // pitch ld; fp32: three planes
+  long long rows, ld, plane_stride;
+  int cols, quads;         // quads of columns in a row
+  int block0;              // first block
+};
+struct PrepArgs {
+  PrepJob job[MAX_JOBS];
+  int n;
+};
+constexpr int PREP_THREADS = 256, PREP_UNROLL = 4;
+
+// fp32 -> three bf16 planes (F32), or a copy of a bf16 matrix to another pitch.  One thread per four columns.
+template <bool F32>
+__global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_constant__ PrepArgs a) {
+  pdl_wait();
+  int j = 0;
+  while (j + 1 < a.n && static_cast<int>(blockIdx.x) >= a.job[j + 1].block0) ++j;
+  const PrepJob& job = a.job[j];
+  const long long first = static_cast<long long>(blockIdx.x - job.block0) * (PREP_THREADS * PREP_UNROLL) + threadIdx.x;
+  const long long all = job.rows * job.quads;
+#pragma unroll
+  for (int u = 0; u < PREP_UNROLL; ++u) {
+    const long long i = first + u * PREP_THREADS;
+    if (i >= all) break;
+    const long long row = i / job.quads;
+    const int c = static_cast<int>(i - row * job.quads) * 4;
+    __nv_bfloat16* out = job.out + row * job.ld + c;      // 8-byte aligned: the pitch is a multiple of 64
+    if (F32) {
+      const float* in = static_cast<const float*>(job.in) + row * job.cols + c;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      if (c + 4 <= job.cols && (reinterpret_cast<uintptr_t>(in) & 15u) == 0) {
+        const float4 t = __ldg(reinterpret_cast<const float4*>(in));
+        v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (c + k < job.cols) v[k] = __ldg(in + k);
+      }
+      float w[4][3];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) tg::split3(v[k], w[k]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        *reinterpret_cast<uint2*>(out + k * job.plane_stride) = make_uint2(pack_bf16x2(w[0][k], w[1][k]), pack_bf16x2(w[2][k], w[3][k]));
+    } else {
+      const unsigned short* in = static_cast<const unsigned short*>(job.in) + row * job.cols + c;
+      unsigned short v[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (c + k < job.cols) v[k] = __ldg(in + k);
+      *reinterpret_cast<uint2*>(out) = make_uint2(v[0] | static_cast<uint32_t>(v[1]) << 16, v[2] | static_cast<uint32_t>(v[3]) << 16);
+    }
   }
 }
 
-// An operand element (i, k) at p[i * si + k * sk].
-template <typename E> struct Operand { const E* p; long long si, sk; };
-
-enum Mode : int { PLAIN = 0, FORWARD = 1, BACKWARD = 2 };
-
-template <typename E>
-struct SimpleArgs {
-  Operand<E> a[2], b[2];
-  int pairs;            // PLAIN: products added up
-  int gated, act, mode;
-  long long M; int N; long long K;
-  const E* bias;        // [N] or nullptr
-  E* C;                 // PLAIN: output, FORWARD: H; BACKWARD: H
-  E *dG, *dU;           // BACKWARD
-  float *G, *U;         // FORWARD: written when not nullptr, BACKWARD: read
-  long long ldc, ldm;
+// Bias gradients: out[c] = sum over rows of in[r, c], in fp32 and in a fixed order (eight interleaved row sets, four
+// partial sums in each).  A block takes 64 columns.  `planes` bf16 planes that add up, or 0: fp32 values.
+struct SumJob {
+  const void* in;
+  void* out;               // bf16, or fp32 with f32_out
+  long long rows, ld, plane_stride;
+  int cols, planes, f32_out;
 };
-
-constexpr int TM = 64, TN = 64, TK = 16;
-
-template <typename E>
-__global__ void __launch_bounds__(256) simple_kernel(const SimpleArgs<E> p) {
-  __shared__ float As[TK][TM + 1], Bs[2][TK][TN + 1];
-  pdl_wait();
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const long long row0 = static_cast<long long>(blockIdx.y) * TM;
-  const int col0 = blockIdx.x * TN;
-  const bool two = p.mode == FORWARD && p.gated;
-  float acc[2][4][4] = {};
-  for (int pair = 0; pair < p.pairs; ++pair)
-    for (long long k0 = 0; k0 < p.K; k0 += TK) {
-      for (int i = tid; i < TM * TK; i += 256) {
-        const Operand<E>& a = p.a[pair];
-        const bool along_k = a.sk == 1;
-        const int kk = along_k ? i % TK : i / TM, r = along_k ? i / TK : i % TM;
-        const bool in = row0 + r < p.M && k0 + kk < p.K;
-        As[kk][r] = in ? to_float<E>(a.p[(row0 + r) * a.si + (k0 + kk) * a.sk]) : 0.f;
-      }
-      for (int w = 0; w < (two ? 2 : 1); ++w)
-        for (int i = tid; i < TN * TK; i += 256) {
-          const Operand<E>& b = p.b[two ? w : pair];
-          const bool along_k = b.sk == 1;
-          const int kk = along_k ? i % TK : i / TN, c = along_k ? i / TK : i % TN;
-          const bool in = col0 + c < p.N && k0 + kk < p.K;
-          Bs[w][kk][c] = in ? to_float<E>(b.p[(col0 + c) * b.si + (k0 + kk) * b.sk]) : 0.f;
-        }
-      __syncthreads();
-      for (int kk = 0; kk < TK; ++kk)
-        for (int i = 0; i < 4; ++i)
-          for (int j = 0; j < 4; ++j) {
-            acc[0][i][j] = fmaf(As[kk][ty * 4 + i], Bs[0][kk][tx + 16 * j], acc[0][i][j]);
-            if (two) acc[1][i][j] = fmaf(As[kk][ty * 4 + i], Bs[1][kk][tx + 16 * j], acc[1][i][j]);
-          }
-      __syncthreads();
-    }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const long long row = row0 + ty * 4 + i;
-      const int col = col0 + tx + 16 * j;
-      if (row >= p.M || col >= p.N) continue;
-      const float v = acc[0][i][j] + (p.bias ? to_float<E>(p.bias[col]) : 0.f);
-      if (p.mode == PLAIN) {
-        p.C[row * p.ldc + col] = from_float<E>(v);
-        continue;
-      }
-      const long long at = row * p.ldm + col;
-      float a, s;
-      if (p.mode == FORWARD) {
-        act_and_slope(v, p.act, &a, &s);
-        if (p.G) p.G[at] = v;
-        if (p.gated) {
-          if (p.U) p.U[at] = acc[1][i][j];
-          a *= acc[1][i][j];
-        }
-        p.C[at] = from_float<E>(a);
-      } else {
-        act_and_slope(p.G[at], p.act, &a, &s);
-        if (p.gated) {
-          const float u = p.U[at];
-          p.dG[at] = from_float<E>(v * u * s);
-          p.dU[at] = from_float<E>(v * a);
-          p.C[at] = from_float<E>(a * u);
-        } else {
-          p.dG[at] = from_float<E>(v * s);
-          p.C[at] = from_float<E>(a);
-        }
-      }
-    }
+struct SumArgs {
+  SumJob job[2];
+};
+__device__ __forceinline__ float2 load2(const SumJob& j, long long row, int c) {
+  if (j.planes == 0) {
+    const float* p = static_cast<const float*>(j.in) + row * j.ld + c;
+    return make_float2(p[0], c + 1 < j.cols ? p[1] : 0.f);
+  }
+  float2 r = make_float2(0.f, 0.f);
+  for (int k = 0; k < j.planes; ++k) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(j.in) + k * j.plane_stride + row * j.ld + c);
+    r.x += __uint_as_float(w << 16);
+    r.y += __uint_as_float(w & 0xffff0000u);
+  }
+  return r;
 }
-
-template <typename E>
-__global__ void __launch_bounds__(256) column_sum_kernel(const E* in, long long rows, int cols, long long ld, E* out) {
-  __shared__ float red[8][33];
+__global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ SumArgs a) {
+  __shared__ float2 red[8][32];
   pdl_wait();
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
-  float s = 0.f;
-  if (c < cols) for (long long r = w; r < rows; r += 8) s += to_float<E>(in[r * ld + c]);
-  red[w][threadIdx.x & 31] = s;
+  const SumJob& j = a.job[blockIdx.y];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 64 + lane * 2;
+  if (blockIdx.x * 64 >= j.cols) return;
+  float2 s[4] = {};
+  if (c < j.cols)
+    for (long long r = w; r < j.rows; r += 32) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (r + 8 * k < j.rows) {
+          const float2 v = load2(j, r + 8 * k, c);
+          s[k].x += v.x;
+          s[k].y += v.y;
+        }
+    }
+  red[w][lane] = make_float2((s[0].x + s[1].x) + (s[2].x + s[3].x), (s[0].y + s[1].y) + (s[2].y + s[3].y));
   __syncthreads();
-  if (w == 0 && c < cols) {
-    for (int i = 1; i < 8; ++i) s += red[i][threadIdx.x];
-    out[c] = from_float<E>(s);
+  if (w == 0 && c < j.cols) {
+    float2 t = red[0][lane];
+    for (int k = 1; k < 8; ++k) { t.x += red[k][lane].x; t.y += red[k][lane].y; }
+    if (j.f32_out) {
+      static_cast<float*>(j.out)[c] = t.x;
+      if (c + 1 < j.cols) static_cast<float*>(j.out)[c + 1] = t.y;
+    } else {
+      static_cast<__nv_bfloat16*>(j.out)[c] = __float2bfloat16_rn(t.x);
+      if (c + 1 < j.cols) static_cast<__nv_bfloat16*>(j.out)[c + 1] = __float2bfloat16_rn(t.y);
+    }
   }
 }
 
@@ -143,18 +135,39 @@ namespace {
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-struct TrainLayout { size_t g, u, saved; size_t h, dg, du, end; };
+// Offsets of what the forward pass keeps, and of the workspace's buffers.  The rows of both are padded to a multiple
+// of 64 elements (ldm for m, ldd for d), so that every row starts on 128 bytes; the pads are neither written to by
+// whole chunks that matter nor read (the tensor maps end at m and d).
+struct TrainLayout {
+  long long ldm, ldd;
+  size_t hi, hi2, lo, saved;
+  size_t H, dG, dU, W1, W1u, W2, X, dY, end;
+};
 TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   TrainLayout L;
-  const bool gated = s.act == FFSPLIT_SWIGLU;
-  const size_t es = elem_size(s.dtype), n = static_cast<size_t>(T) * s.m;
-  L.g = 0;
-  L.u = up256(n * 4);
-  L.saved = L.u + (gated ? up256(n * 4) : 0);
-  L.h = 0;
-  L.dg = up256(n * es);
-  L.du = L.dg + up256(n * es);
-  L.end = L.du + (gated ? up256(n * es) : 0);
+  const bool gated = s.act == FFSPLIT_SWIGLU, f32 = s.dtype == FFSPLIT_F32;
+  L.ldm = round_up_ll(s.m, 64);
+  L.ldd = round_up_ll(s.d, 64);
+  const size_t hidden = static_cast<size_t>(T) * L.ldm;
+  size_t off = 0;
+  L.hi = off;  off = up256(off + hidden * (f32 ? 4 : 2));
+  L.hi2 = off; off = up256(off + (gated ? hidden * (f32 ? 4 : 2) : 0));
+  L.lo = off;  off = up256(off + (f32 ? 0 : hidden));
+  L.saved = off;
+  const size_t planes = f32 ? 3 : 1;
+  off = 0;
+  L.H = off;  off = up256(off + hidden * 2 * planes);
+  L.dG = off; off = up256(off + hidden * 2 * planes);
+  L.dU = off; off = up256(off + (gated ? hidden * 2 * planes : 0));
+  const bool copy_w1 = f32 || s.m % 8 != 0;
+  const size_t w1 = copy_w1 ? static_cast<size_t>(s.d) * L.ldm * 2 * planes : 0;
+  L.W1 = off;  off = up256(off + w1);
+  L.W1u = off; off = up256(off + (gated ? w1 : 0));
+  L.W2 = off;  off = up256(off + (f32 ? static_cast<size_t>(s.m) * L.ldd * 6 : 0));
+  const size_t tokens = f32 ? static_cast<size_t>(T) * L.ldd * 6 : 0;
+  L.X = off;  off = up256(off + tokens);
+  L.dY = off; off = up256(off + tokens);
+  L.end = off;
   return L;
 }
 
@@ -180,90 +193,140 @@ ffsplit_status check_saved(ffsplit_ctx* ctx, const ffsplit_shape& s, int64_t T, 
   return FFSPLIT_OK;
 }
 
-template <typename E>
-ffsplit_status simple_launch(ffsplit_ctx* ctx, const train::SimpleArgs<E>& a, cudaStream_t st) {
-  const cudaError_t e = launch_pdl(train::simple_kernel<E>, dim3((a.N + 63) / 64, static_cast<unsigned>((a.M + 63) / 64)), dim3(256), 0, st, a);
-  ctx->launches++;
-  return check_cuda(ctx, e, "train::simple_kernel launch");
+// The operands of a pass: the caller's tensors, or their planes (or padded copies) in the workspace.
+struct Pass {
+  ffsplit_ctx* ctx;
+  ffsplit_shape s;
+  TrainLayout L;
+  long long T;
+  char* ws;
+  cudaStream_t st;
+  train::PrepArgs prep;
+  int prep_blocks = 0;
+
+  Pass(ffsplit_ctx* c, const ffsplit_shape& shape, long long tokens, cudaStream_t stream)
+      : ctx(c), s(shape), L(train_layout(shape, tokens)), T(tokens), ws(c->ws + kCtrlBytes), st(stream) {
+    std::memset(&prep, 0, sizeof(prep));
+    ctx->score_prep.valid = false;   // the scoring buffers share the workspace
+  }
+  bool f32() const { return s.dtype == FFSPLIT_F32; }
+  bool gated() const { return s.act == FFSPLIT_SWIGLU; }
+
+  // A caller's tensor [rows, cols]: as it is, or as copied to `at` by the preparation launch.
+  tg::Matrix tensor(const void* p, long long rows, int cols, long long ld, size_t at) {
+    if (!f32() && cols % 8 == 0) return {p, rows, cols, cols, rows * cols, 1};
+    train::PrepJob& j = prep.job[prep.n++];
+    j.in = p;
+    j.out = reinterpret_cast<__nv_bfloat16*>(ws + at);
+    j.rows = rows; j.cols = cols; j.ld = ld; j.plane_stride = rows * ld;
+    j.quads = (cols + 3) / 4;
+    j.block0 = prep_blocks;
+    constexpr int per = train::PREP_THREADS * train::PREP_UNROLL;
+    prep_blocks += static_cast<int>((rows * j.quads + per - 1) / per);
+    return {j.out, rows, cols, ld, j.plane_stride, f32() ? 3 : 1};
+  }
+  tg::Matrix hidden(size_t at) const {
+    return {ws + at, T, s.m, L.ldm, T * L.ldm, f32() ? 3 : 1};
+  }
+  tg::Hidden buffers(char* saved) const {
+    tg::Hidden h;
+    h.hi = saved ? saved + L.hi : nullptr;
+    h.hi2 = saved ? saved + L.hi2 : nullptr;
+    h.lo = saved ? reinterpret_cast<unsigned char*>(saved + L.lo) : nullptr;
+    h.H = reinterpret_cast<__nv_bfloat16*>(ws + L.H);
+    h.dG = reinterpret_cast<__nv_bfloat16*>(ws + L.dG);
+    h.dU = reinterpret_cast<__nv_bfloat16*>(ws + L.dU);
+    h.ldm = L.ldm;
+    h.plane_stride = T * L.ldm;
+    return h;
+  }
+  ffsplit_status prepare() {
+    if (prep.n == 0) return FFSPLIT_OK;
+    const cudaError_t e = f32() ? launch_pdl(train::prepare_kernel<true>, dim3(prep_blocks), dim3(train::PREP_THREADS), 0, st, prep)
+                                : launch_pdl(train::prepare_kernel<false>, dim3(prep_blocks), dim3(train::PREP_THREADS), 0, st, prep);
+    ctx->launches++;
+    return check_cuda(ctx, e, "train::prepare_kernel launch");
+  }
+};
+
+tg::Product product(const tg::Matrix& a, int a_mn, const tg::Matrix& b, int b_mn, long long M, int N, long long K) {
+  tg::Product g;
+  std::memset(&g, 0, sizeof(g));
+  g.a[0] = a; g.b[0] = b;
+  g.pairs = 1;
+  g.a_mn = a_mn; g.b_mn = b_mn;
+  g.M = M; g.N = N; g.K = K;
+  return g;
 }
 
-template <typename E>
 ffsplit_status run_train_forward(ffsplit_ctx* ctx, const ffsplit_shape& s, const ffsplit_weights& w, const void* X, long long T,
                                  char* saved, void* Y, cudaStream_t st) {
-  const TrainLayout L = train_layout(s, T);
+  Pass p(ctx, s, T, st);
   const int d = s.d, m = s.m;
-  E* H = reinterpret_cast<E*>(ctx->ws + kCtrlBytes + L.h);
-  train::SimpleArgs<E> a;
-  std::memset(&a, 0, sizeof(a));
-  a.pairs = 1; a.mode = train::FORWARD; a.gated = s.act == FFSPLIT_SWIGLU; a.act = s.act;
-  a.a[0] = {static_cast<const E*>(X), d, 1};
-  a.b[0] = {static_cast<const E*>(w.W1), 1, m};
-  a.b[1] = {static_cast<const E*>(w.W1u), 1, m};
-  a.M = T; a.N = m; a.K = d; a.bias = static_cast<const E*>(w.b1);
-  a.C = H; a.ldm = m;
-  if (saved) { a.G = reinterpret_cast<float*>(saved + L.g); a.U = reinterpret_cast<float*>(saved + L.u); }
-  ffsplit_status r = simple_launch(ctx, a, st);
-  if (r != FFSPLIT_OK) return r;
-  std::memset(&a, 0, sizeof(a));
-  a.pairs = 1;
-  a.a[0] = {H, m, 1};
-  a.b[0] = {static_cast<const E*>(w.W2), 1, d};
-  a.M = T; a.N = d; a.K = m; a.bias = static_cast<const E*>(w.b2);
-  a.C = static_cast<E*>(Y); a.ldc = d;
-  return simple_launch(ctx, a, st);
+  const tg::Matrix x = p.tensor(X, T, d, p.L.ldd, p.L.X), w1 = p.tensor(w.W1, d, m, p.L.ldm, p.L.W1),
+                   w2 = p.tensor(w.W2, m, d, p.L.ldd, p.L.W2);
+  tg::Product g = product(x, 0, w1, 1, T, m, d);
+  if (p.gated()) g.b[1] = p.tensor(w.W1u, d, m, p.L.ldm, p.L.W1u);
+  g.bias = w.b1;
+  ffsplit_status r;
+  if ((r = p.prepare()) != FFSPLIT_OK) return r;
+  const tg::Hidden h = p.buffers(saved);
+  if ((r = tg::launch(ctx, p.gated() ? tg::FORWARD_GATED : tg::FORWARD_ACT, s.act, p.f32(), &g, 1, h, st)) != FFSPLIT_OK) return r;
+  g = product(p.hidden(p.L.H), 0, w2, 1, T, d, m);
+  g.C = Y; g.ldc = d; g.bias = w.b2;
+  return tg::launch(ctx, tg::PLAIN, s.act, p.f32(), &g, 1, h, st);
 }
 
-template <typename E>
 ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, const ffsplit_weights& w, const void* X, long long T,
-                                  const char* saved, const void* dY, const ffsplit_train_grads& g, cudaStream_t st) {
-  const TrainLayout L = train_layout(s, T);
+                                  const char* saved, const void* dY, const ffsplit_train_grads& grads, cudaStream_t st) {
+  Pass p(ctx, s, T, st);
   const int d = s.d, m = s.m;
-  const bool gated = s.act == FFSPLIT_SWIGLU;
-  char* base = ctx->ws + kCtrlBytes;
-  E *H = reinterpret_cast<E*>(base + L.h), *dG = reinterpret_cast<E*>(base + L.dg), *dU = reinterpret_cast<E*>(base + L.du);
-  const E *x = static_cast<const E*>(X), *dy = static_cast<const E*>(dY);
-  train::SimpleArgs<E> a;
-  ffsplit_status r = FFSPLIT_OK;
-  if (g.dX || g.dW1 || g.dW1u || g.db1 || g.dW2) {
-    std::memset(&a, 0, sizeof(a));
-    a.pairs = 1; a.mode = train::BACKWARD; a.gated = gated; a.act = s.act;
-    a.a[0] = {dy, d, 1};
-    a.b[0] = {static_cast<const E*>(w.W2), d, 1};
-    a.M = T; a.N = m; a.K = d;
-    a.C = H; a.dG = dG; a.dU = dU; a.ldm = m;
-    a.G = reinterpret_cast<float*>(const_cast<char*>(saved) + L.g);
-    a.U = reinterpret_cast<float*>(const_cast<char*>(saved) + L.u);
-    if ((r = simple_launch(ctx, a, st)) != FFSPLIT_OK) return r;
+  const bool inner = grads.dX || grads.dW1 || grads.dW1u || grads.db1 || grads.dW2;   // anything that needs dH or H
+  const tg::Hidden h = p.buffers(const_cast<char*>(saved));
+  const tg::Matrix H = p.hidden(p.L.H), dG = p.hidden(p.L.dG), dU = p.hidden(p.L.dU);
+  tg::Product out[4];
+  int n = 0;
+  ffsplit_status r;
+  if (inner) {
+    const tg::Matrix dy = p.tensor(dY, T, d, p.L.ldd, p.L.dY), w2 = p.tensor(w.W2, m, d, p.L.ldd, p.L.W2);
+    if (grads.dX) {
+      tg::Product& g = out[n++] = product(dG, 0, p.tensor(w.W1, d, m, p.L.ldm, p.L.W1), 0, T, d, m);
+      if (p.gated()) {
+        g.pairs = 2;
+        g.a[1] = dU;
+        g.b[1] = p.tensor(w.W1u, d, m, p.L.ldm, p.L.W1u);
+      }
+      g.C = grads.dX; g.ldc = d;
+    }
+    tg::Matrix x;
+    if (grads.dW1 || grads.dW1u) x = p.tensor(X, T, d, p.L.ldd, p.L.X);
+    if (grads.dW1) {
+      tg::Product& g = out[n++] = product(x, 1, dG, 1, d, m, T);
+      g.C = grads.dW1; g.ldc = m;
+    }
+    if (grads.dW1u) {
+      tg::Product& g = out[n++] = product(x, 1, dU, 1, d, m, T);
+      g.C = grads.dW1u; g.ldc = m;
+    }
+    if (grads.dW2) {
+      tg::Product& g = out[n++] = product(H, 1, dy, 1, m, d, T);
+      g.C = grads.dW2; g.ldc = d;
+    }
+    if ((r = p.prepare()) != FFSPLIT_OK) return r;
+    const tg::Product g = product(dy, 0, w2, 0, T, m, d);
+    if ((r = tg::launch(ctx, p.gated() ? tg::BACKWARD_GATED : tg::BACKWARD_ACT, s.act, p.f32(), &g, 1, h, st)) != FFSPLIT_OK) return r;
+    if (n > 0 && (r = tg::launch(ctx, tg::PLAIN, s.act, p.f32(), out, n, h, st)) != FFSPLIT_OK) return r;
   }
-  if (g.dX) {
+  if (grads.db1 || grads.db2) {
+    train::SumArgs a;
     std::memset(&a, 0, sizeof(a));
-    a.pairs = gated ? 2 : 1;
-    a.a[0] = {dG, m, 1}; a.b[0] = {static_cast<const E*>(w.W1), m, 1};
-    a.a[1] = {dU, m, 1}; a.b[1] = {static_cast<const E*>(w.W1u), m, 1};
-    a.M = T; a.N = d; a.K = m; a.C = static_cast<E*>(g.dX); a.ldc = d;
-    if ((r = simple_launch(ctx, a, st)) != FFSPLIT_OK) return r;
-  }
-  const E* left[3] = {x, x, H};
-  const E* right[3] = {dG, dU, dy};
-  void* out[3] = {g.dW1, g.dW1u, g.dW2};
-  for (int i = 0; i < 3; ++i) {
-    if (!out[i]) continue;
-    const int M = i < 2 ? d : m, N = i < 2 ? m : d;
-    std::memset(&a, 0, sizeof(a));
-    a.pairs = 1;
-    a.a[0] = {left[i], 1, M}; a.b[0] = {right[i], 1, N};
-    a.M = M; a.N = N; a.K = T; a.C = static_cast<E*>(out[i]); a.ldc = N;
-    if ((r = simple_launch(ctx, a, st)) != FFSPLIT_OK) return r;
-  }
-  const E* sums[2] = {dG, dy};
-  void* bias[2] = {g.db1, g.db2};
-  for (int i = 0; i < 2; ++i) {
-    if (!bias[i]) continue;
-    const int cols = i == 0 ? m : d;
-    const cudaError_t e = launch_pdl(train::column_sum_kernel<E>, dim3((cols + 31) / 32), dim3(256), 0, st, sums[i], T, cols,
-                                     static_cast<long long>(cols), static_cast<E*>(bias[i]));
+    int k = 0, cols = 0;
+    const int f32 = p.f32() ? 1 : 0;
+    if (grads.db1) { a.job[k++] = {h.dG, grads.db1, T, p.L.ldm, T * p.L.ldm, m, f32 ? 3 : 1, f32}; cols = m; }
+    if (grads.db2) { a.job[k++] = {dY, grads.db2, T, d, 0, d, f32 ? 0 : 1, f32}; cols = cols > d ? cols : d; }
+    const cudaError_t e = launch_pdl(train::column_sum_kernel, dim3((cols + 63) / 64, k), dim3(256), 0, st, a);
     ctx->launches++;
-    if (e != cudaSuccess) return check_cuda(ctx, e, "column_sum_kernel launch");
+    return check_cuda(ctx, e, "column_sum_kernel launch");
   }
   return FFSPLIT_OK;
 }
@@ -292,11 +355,7 @@ ffsplit_status ffsplit_train_forward(ffsplit_ctx* ctx, const ffsplit_shape* shap
   if (!Y) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "NULL tensor");
   if (!aligned16(Y)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
   if (saved && (s = check_saved(ctx, *shape, T, saved, saved_bytes)) != FFSPLIT_OK) return s;
-  ctx->score_prep.valid = false;   // the scoring buffers share the workspace
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return shape->dtype == FFSPLIT_BF16
-             ? run_train_forward<__nv_bfloat16>(ctx, *shape, *weights, X, T, static_cast<char*>(saved), Y, st)
-             : run_train_forward<float>(ctx, *shape, *weights, X, T, static_cast<char*>(saved), Y, st);
+  return run_train_forward(ctx, *shape, *weights, X, T, static_cast<char*>(saved), Y, static_cast<cudaStream_t>(stream));
 }
 
 ffsplit_status ffsplit_train_backward(ffsplit_ctx* ctx, const ffsplit_shape* shape, const ffsplit_weights* weights, const void* X,
@@ -318,11 +377,7 @@ ffsplit_status ffsplit_train_backward(ffsplit_ctx* ctx, const ffsplit_shape* sha
   if (!any) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "no gradient asked for");
   if (!aligned16(dY)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
   if ((s = check_saved(ctx, *shape, T, saved, saved_bytes)) != FFSPLIT_OK) return s;
-  ctx->score_prep.valid = false;   // the scoring buffers share the workspace
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const char* sv = static_cast<const char*>(saved);
-  return shape->dtype == FFSPLIT_BF16 ? run_train_backward<__nv_bfloat16>(ctx, *shape, *weights, X, T, sv, dY, *grads, st)
-                                      : run_train_backward<float>(ctx, *shape, *weights, X, T, sv, dY, *grads, st);
+  return run_train_backward(ctx, *shape, *weights, X, T, static_cast<const char*>(saved), dY, *grads, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

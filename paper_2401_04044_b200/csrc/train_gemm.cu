@@ -1,0 +1,683 @@
+// The matrix products of a training pass on the tensor cores, weights and activations where they lie.
+//
+//   C [M, N] = sum over pairs, k of A_i[m, k] B_i[k, n]
+//
+// A training pass multiplies the same row-major tensors along either of their axes (X W1, but X^T dG; H W2, but
+// dY W2^T), and the weights change with every step, so nothing is transposed or packed beforehand: an operand whose
+// contraction runs along memory goes to the tensor cores as a K-major tile, any other as an MN-major one.  Which of
+// the two it is, is a bit of the instruction descriptor and the shape of the TMA box, both chosen at run time.
+//
+// One persistent pair of CTAs (two SMs, cta_group::2) per 256 x 256 tile: each CTA stages 128 rows of A and 128 rows
+// of B per 64-deep k-block (32 KB) by TMA in a ring of six, rank 0 issues the MMAs for both, and each CTA finishes the
+// 128 accumulator rows in its own tensor memory.  Two accumulators of 256 columns: a tile's epilogue runs under the
+// next tile's MMAs.  A gated tile is 256 x 128: rank 0 stages the 128 columns of W1, rank 1 those of W1u, so that
+// every accumulator row holds G next to U and the product H leaves from the same registers.
+//
+// fp32 layers: every fp32 matrix is split into three bf16 planes (x0 = bf16(x), x1 = bf16(x - x0), ...: 24 significant
+// bits), and the six products of planes (i, j), i + j <= 2, are accumulated as six runs over K, the smallest first.
+// What is dropped is below 2^-24 of a term.
+//
+// Warp roles: 0 TMA producer (both CTAs), 1 MMA issuer (rank 0), 2-9 epilogue (four lane quarters x two column halves).
+// Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
+#include <cstring>
+
+#include "epilogue.cuh"
+#include "ptx.cuh"
+#include "train_gemm.h"
+
+namespace ffsp {
+namespace tg {
+
+constexpr int CTA_M = 128, TILE_M = 256, TILE_N = 256, BLOCK_K = 64;
+constexpr int STAGES = 6;
+constexpr int HALF_BYTES = CTA_M * BLOCK_K * 2;      // one operand of one CTA and stage
+constexpr int STAGE_BYTES = 2 * HALF_BYTES;
+constexpr int BLOCK64_BYTES = 64 * BLOCK_K * 2;      // 64 x 64 elements: MN-major tiles are staged in two of these
+constexpr int EPI_WARPS = 8;
+constexpr int THREADS = 32 * (EPI_WARPS + 2);
+constexpr int TMEM_COLS = 512;
+constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 256 + 1024;
+constexpr int MAX_PRODUCTS = 4;
+
+struct Unit {
+  int prod, m_blk, n_blk;
+};
+
+struct DevProduct {
+  CUtensorMap a[2], b[2];
+  long long M;
+  int N, kb;             // k-blocks per run
+  int runs, pairs;       // runs over K: pairs x (1, or the 6 products of planes)
+  int a_mn, b_mn;
+  int tiles_m, tiles_n, panel_m;
+  int unit0;             // first unit of this product
+  void* C;
+  long long ldc;
+  const void* bias;
+};
+
+struct Params {
+  DevProduct prod[MAX_PRODUCTS];
+  int n_prod;
+  int units;             // tiles of all products, the products with the longer runs first
+  // Units are dealt to the clusters in turn.  The first `heavy` ones (the product with the longest tiles) may leave the
+  // clusters from `short_from` on one tile short: `extra` of the following units go to those clusters first.
+  int heavy, short_from, extra;
+  int act;
+  Hidden hid;
+  int* status;
+};
+
+// Units of one cluster in order.
+struct Walk {
+  int c, C, next, phase, given;
+  __device__ __forceinline__ Walk() : c(blockIdx.x >> 1), C(gridDim.x >> 1), next(blockIdx.x >> 1), phase(0), given(0) {}
+  // next unit, or -1
+  __device__ __forceinline__ int take(const Params& p) {
+    if (phase == 0) {
+      if (next < p.heavy) {
+        const int u = next;
+        next += C;
+        return u;
+      }
+      phase = 1;
+    }
+    const int narrow = C - p.short_from;       // clusters that are one heavy tile short
+    if (phase == 1) {
+      if (c >= p.short_from && given < p.extra) {
+        const int u = p.heavy + (c - p.short_from) + given * narrow;
+        ++given;
+        return u;                              // extra * narrow <= units - heavy, by construction
+      }
+      phase = 2;
+      int turn = c - p.short_from;             // the short clusters first again
+      if (turn < 0) turn += C;
+      next = p.heavy + p.extra * narrow + turn;
+    }
+    if (next >= p.units) return -1;
+    const int u = next;
+    next += C;
+    return u;
+  }
+};
+
+__device__ __forceinline__ Unit find_unit(const Params& p, int u) {
+  Unit r;
+  r.prod = 0;
+  while (r.prod + 1 < p.n_prod && u >= p.prod[r.prod + 1].unit0) ++r.prod;
+  const DevProduct& d = p.prod[r.prod];
+  const int tile = u - d.unit0;
+  const int per_panel = d.panel_m * d.tiles_n;
+  const int panel = tile / per_panel, in_panel = tile - panel * per_panel, m0 = panel * d.panel_m;
+  const int h = d.tiles_m - m0 < d.panel_m ? d.tiles_m - m0 : d.panel_m;
+  r.n_blk = in_panel / h;
+  r.m_blk = m0 + (in_panel - r.n_blk * h);
+  return r;
+}
+
+// Planes of run r: the pairs of one product of planes one after the other, small products first.
+template <bool F32>
+__device__ __forceinline__ void run_planes(const DevProduct& d, int run, int* pair, int* pa, int* pb) {
+  if (!F32) {
+    *pair = run; *pa = 0; *pb = 0;
+    return;
+  }
+  const int combo = run / d.pairs;
+  *pair = run - combo * d.pairs;
+  // (0,2) (1,1) (2,0) (0,1) (1,0) (0,0)
+  *pa = (0x012010 >> (4 * (5 - combo))) & 0xF;
+  *pb = (0x001012 >> (4 * combo)) & 0xF;
+}
+
+// ---------------------------------------------------------------------------------------------- number formats
+// What is kept of G (Z) and U between forward and backward.  Their own rounding would be a third one on the way to dX
+// and dW1 besides those of dG and of the result; with four more bits it is not seen (2^-13).  Gated: 16 + 4 bits each, the
+// two nibbles in one byte (5 bytes a pair); ungated: 16 + 8 bits (3 bytes).  Rounded half up in magnitude, except that
+// infinities and NaN are cut (their low bits are not needed).
+__device__ __forceinline__ uint32_t round_bits(float v, uint32_t half) {
+  const uint32_t b = __float_as_uint(v);
+  return (b & 0x7f800000u) == 0x7f800000u ? b : b + half;
+}
+template <bool F32>
+__device__ __forceinline__ float sigmoid_of(float z) {
+  // one reciprocal and one exponential either way; the fast forms are good to a few 2^-22, far below bf16's 2^-9
+  return F32 ? 1.0f / (1.0f + expf(-z)) : __fdividef(1.0f, 1.0f + __expf(-z));
+}
+// GELU and its slope; both from the same exponential (tanh u = 1 - 2 / (1 + exp(2 u)); Phi from erfc).
+template <bool F32>
+__device__ __forceinline__ void gelu_and_slope(float z, int act, float* value, float* slope) {
+  if (act == FFSPLIT_GELU_ERF) {
+    float below;
+    const float density = 0.3989422804014327f * (F32 ? expf(-0.5f * z * z) : __expf(-0.5f * z * z));
+    if (F32) {
+      below = 0.5f * erfcf(-0.70710678118654752f * z);
+    } else {
+      // Abramowitz and Stegun 7.1.26 (1.5e-7 absolute) on the exponential that the density needs anyway
+      const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
+      float q = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+      q = fmaf(q, t, 0.5f * 1.421413741f);
+      q = fmaf(q, t, 0.5f * -0.284496736f);
+      q = fmaf(q, t, 0.5f * 0.254829592f);
+      q *= t * (density * 2.5066282746310002f);
+      below = z >= 0.f ? 1.0f - q : q;
+    }
+    *value = z * below;
+    *slope = fmaf(z, density, below);
+  } else {
+    const float c = 0.79788456080286536f, a = 0.044715f;
+    const float z2 = z * z;
+    const float s = sigmoid_of<F32>(2.0f * c * z * fmaf(a, z2, 1.0f));     // (1 + tanh u) / 2
+    *value = z * s;
+    *slope = fmaf(z * s * (1.0f - s), 2.0f * c * fmaf(3.0f * a, z2, 1.0f), s);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- epilogue pieces
+__device__ __forceinline__ void store16_bf16(__nv_bfloat16* base, const float* v) {   // 32-byte aligned
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(base), "r"(pack_bf16x2(v[0], v[1])),
+               "r"(pack_bf16x2(v[2], v[3])), "r"(pack_bf16x2(v[4], v[5])), "r"(pack_bf16x2(v[6], v[7])), "r"(pack_bf16x2(v[8], v[9])),
+               "r"(pack_bf16x2(v[10], v[11])), "r"(pack_bf16x2(v[12], v[13])), "r"(pack_bf16x2(v[14], v[15]))
+               : "memory");
+}
+// 16 values into the library's own buffers (pitch a multiple of 64 elements): one bf16 plane, or three.
+template <bool F32>
+__device__ __forceinline__ void store16_planes(__nv_bfloat16* base, long long plane_stride, const float* v) {
+  if (!F32) {
+    store16_bf16(base, v);
+    return;
+  }
+  float w[3][16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float o[3];
+    split3(v[i], o);
+    w[0][i] = o[0]; w[1][i] = o[1]; w[2][i] = o[2];
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) store16_bf16(base + k * plane_stride, w[k]);
+}
+__device__ __forceinline__ void store16_f32(float* base, const float* v) {   // 16-byte aligned
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(base)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+// 16 values of a caller's tensor, of which `valid` lie inside; any alignment.
+template <bool F32>
+__device__ __forceinline__ void store16_user(void* C, long long at, int valid, const float* v) {
+  if (F32) {
+    float* base = static_cast<float*>(C) + at;
+    if (valid >= 16 && (reinterpret_cast<uintptr_t>(base) & 15u) == 0) {
+      store16_f32(base, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) if (i < valid) base[i] = v[i];
+    }
+  } else {
+    __nv_bfloat16* base = static_cast<__nv_bfloat16*>(C) + at;
+    if (valid >= 16 && (reinterpret_cast<uintptr_t>(base) & 31u) == 0) {
+      store16_bf16(base, v);
+    } else if (valid >= 8 && (reinterpret_cast<uintptr_t>(base) & 15u) == 0) {
+      reinterpret_cast<uint4*>(base)[0] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+      if (valid >= 16) {
+        reinterpret_cast<uint4*>(base)[1] =
+            make_uint4(pack_bf16x2(v[8], v[9]), pack_bf16x2(v[10], v[11]), pack_bf16x2(v[12], v[13]), pack_bf16x2(v[14], v[15]));
+      } else {
+#pragma unroll
+        for (int i = 8; i < 16; ++i) if (i < valid) base[i] = __float2bfloat16_rn(v[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) if (i < valid) base[i] = __float2bfloat16_rn(v[i]);
+    }
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void add_bias(const void* bias, int n0, int N, float* v) {
+  if (F32) {
+    const float* b = static_cast<const float*>(bias) + n0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) if (n0 + i < N) v[i] += __ldg(b + i);
+  } else {
+    const __nv_bfloat16* b = static_cast<const __nv_bfloat16*>(bias) + n0;
+    if (n0 + 16 <= N) {
+      const uint4 q[2] = {__ldg(reinterpret_cast<const uint4*>(b)), __ldg(reinterpret_cast<const uint4*>(b) + 1)};
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[2 * i] += __uint_as_float(w[i] << 16);
+        v[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) if (n0 + i < N) v[i] += __bfloat162float(b[i]);
+    }
+  }
+}
+
+// What is kept of 16 columns of one row, as loaded; of the pair (G, U), or of Z alone.
+template <bool F32, bool GATED>
+struct Kept {
+  uint4 a[F32 ? 4 : 2];
+  uint4 b[GATED ? (F32 ? 4 : 2) : 1];
+  uint4 lo;
+  __device__ __forceinline__ void load(const Hidden& h, long long at) {
+    constexpr int Q = F32 ? 4 : 2;
+    const char* pa = static_cast<const char*>(h.hi) + at * (F32 ? 4 : 2);
+    const char* pb = static_cast<const char*>(h.hi2) + at * (F32 ? 4 : 2);
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      a[i] = __ldcs(reinterpret_cast<const uint4*>(pa) + i);
+      if (GATED) b[i] = __ldcs(reinterpret_cast<const uint4*>(pb) + i);
+    }
+    if (!F32) lo = __ldcs(reinterpret_cast<const uint4*>(h.lo + at));
+  }
+  __device__ __forceinline__ float first(int i) const {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(a);
+    if (F32) return __uint_as_float(w[i]);
+    const uint32_t top = (i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16);
+    const uint32_t byte = (reinterpret_cast<const uint32_t*>(&lo)[i >> 2] >> (8 * (i & 3))) & 0xffu;
+    return __uint_as_float(top | (GATED ? (byte & 0xfu) << 12 : byte << 8));
+  }
+  __device__ __forceinline__ float second(int i) const {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(b);
+    if (F32) return __uint_as_float(w[i]);
+    const uint32_t top = (i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16);
+    const uint32_t byte = (reinterpret_cast<const uint32_t*>(&lo)[i >> 2] >> (8 * (i & 3))) & 0xffu;
+    return __uint_as_float(top | (byte >> 4) << 12);
+  }
+};
+
+// Keeps 16 columns of one row.
+template <bool F32, bool GATED>
+__device__ __forceinline__ void keep16(const Hidden& h, long long at, const float* g, const float* u) {
+  if (F32) {
+    store16_f32(static_cast<float*>(h.hi) + at, g);
+    if (GATED) store16_f32(static_cast<float*>(h.hi2) + at, u);
+    return;
+  }
+  uint32_t a[8], b[8], lo[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t x = round_bits(g[i], GATED ? 0x800u : 0x80u);
+    uint32_t byte;
+    if (GATED) {
+      const uint32_t y = round_bits(u[i], 0x800u);
+      b[i >> 1] = (i & 1) ? (b[i >> 1] | (y & 0xffff0000u)) : (y >> 16);
+      byte = ((x >> 12) & 0xfu) | ((y >> 8) & 0xf0u);
+    } else {
+      byte = (x >> 8) & 0xffu;
+    }
+    a[i >> 1] = (i & 1) ? (a[i >> 1] | (x & 0xffff0000u)) : (x >> 16);
+    lo[i >> 2] |= byte << (8 * (i & 3));
+  }
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(static_cast<__nv_bfloat16*>(h.hi) + at), "r"(a[0]),
+               "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(a[4]), "r"(a[5]), "r"(a[6]), "r"(a[7])
+               : "memory");
+  if (GATED)
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(static_cast<__nv_bfloat16*>(h.hi2) + at), "r"(b[0]),
+                 "r"(b[1]), "r"(b[2]), "r"(b[3]), "r"(b[4]), "r"(b[5]), "r"(b[6]), "r"(b[7])
+                 : "memory");
+  *reinterpret_cast<uint4*>(h.lo + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
+// ---------------------------------------------------------------------------------------------- the kernel
+template <int MODE, bool F32>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_gemm_kernel(const __grid_constant__ Params p) {
+  constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
+  constexpr int OUT_N = MODE == FORWARD_GATED ? TILE_N / 2 : TILE_N;     // output columns of a tile
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES);
+  uint64_t* full = bars;                  // [STAGES] TMA of both CTAs -> MMA (rank 0's are used)
+  uint64_t* empty = full + STAGES;        // [STAGES] MMA -> TMA, one set in each CTA
+  uint64_t* tfull = empty + STAGES;       // [2] MMA -> epilogue, one set in each CTA
+  uint64_t* tempty = tfull + 2;           // [2] epilogue warps of both CTAs -> MMA (rank 0's are used)
+  uint64_t* drain = tempty + 2;           // used only when giving up
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = ptx::cluster_rank();
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(&tfull[a], 1);
+      ptx::mbar_init(&tempty[a], 2 * EPI_WARPS);
+    }
+    ptx::mbar_init(drain, 1);
+    *abort_flag = 0;
+    ptx::mbar_fence_init();
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(tmem_holder, TMEM_COLS);
+    ptx::tmem_relinquish_pair();
+  }
+  ptx::tc_fence_before();
+  ptx::cluster_sync_all();     // also: the other CTA's barriers are set up
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_holder;
+  // Launched with programmatic stream serialisation: all of the above ran under the tail of the kernel before.  The one
+  // after may be set up only now that this CTA holds its tensor memory (see gemm_tc.cu).
+  pdl_wait();
+
+  if (warp == 0) {
+    if (ptx::elect_one()) {
+      // ------------------------------------------------------------ TMA producer
+      Walk walk;
+      uint32_t it = 0, ph = 0;
+      int s = 0;
+      bool ok = true;
+      const uint32_t smem0 = ptx::smem_u32(smem), full0 = ptx::map_to_cta(ptx::smem_u32(full), 0);
+      for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
+        const Unit t = find_unit(p, u);
+        const DevProduct& d = p.prod[t.prod];
+        const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M;
+        const int n0 = MODE == FORWARD_GATED ? t.n_blk * OUT_N : t.n_blk * OUT_N + static_cast<int>(rank) * CTA_M;
+        for (int run = 0; run < d.runs && ok; ++run) {
+          int pair, pa, pb;
+          run_planes<F32>(d, run, &pair, &pa, &pb);
+          const CUtensorMap* ta = &d.a[pair];
+          const CUtensorMap* tb = &d.b[MODE == FORWARD_GATED ? static_cast<int>(rank) : pair];
+          for (int kb = 0; kb < d.kb; ++kb, ++it) {
+            if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+            if (rank == 0) ptx::mbar_expect_tx(&full[s], 2 * STAGE_BYTES);
+            const uint32_t bar = full0 + s * 8;
+            const uint32_t da = smem0 + s * STAGE_BYTES, db = da + HALF_BYTES;
+            const int k0 = kb * BLOCK_K;
+            if (d.a_mn) {
+              ptx::tma_load_3d_pair(ta, da, bar, m0, k0, pa);
+              ptx::tma_load_3d_pair(ta, da + BLOCK64_BYTES, bar, m0 + 64, k0, pa);
+            } else {
+              ptx::tma_load_3d_pair(ta, da, bar, k0, m0, pa);
+            }
+            if (d.b_mn) {
+              ptx::tma_load_3d_pair(tb, db, bar, n0, k0, pb);
+              ptx::tma_load_3d_pair(tb, db + BLOCK64_BYTES, bar, n0 + 64, k0, pb);
+            } else {
+              ptx::tma_load_3d_pair(tb, db, bar, k0, n0, pb);
+            }
+            if (++s == STAGES) { s = 0; ph ^= 1u; }
+          }
+        }
+      }
+      // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
+      for (int i = 0; i < STAGES && ok; ++i) {
+        ok = ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag);
+        if (++s == STAGES) { s = 0; ph ^= 1u; }
+      }
+      if (!ok) {
+        // Copies into this CTA's shared memory are counted on rank 0's barriers: give what is in flight a bounded time
+        // to land before the CTA exits.
+        const long long t0 = clock64();
+        while (clock64() - t0 < ptx::kWaitLimitCycles / 64) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      // ------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
+      const uint32_t idesc0 = ptx::umma_idesc_bf16(TILE_M, TILE_N);
+      Walk walk;
+      uint32_t tl = 0, ph = 0;
+      int s = 0;
+      bool ok = true;
+      const uint32_t smem0 = ptx::smem_u32(smem);
+      for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p), ++tl) {
+        const Unit t = find_unit(p, u);
+        const DevProduct& d = p.prod[t.prod];
+        const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
+        ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aph ^ 1, abort_flag) ? 1 : 0, 0) != 0;
+        if (!ok) break;
+        ptx::tc_fence_after();
+        // bits 15, 16: the operand's rows run along memory
+        const uint32_t idesc = idesc0 | (d.a_mn ? 1u << 15 : 0u) | (d.b_mn ? 1u << 16 : 0u);
+        const uint64_t a_desc0 = d.a_mn ? ptx::umma_desc_mn128(smem0, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0);
+        const uint64_t b_desc0 = d.b_mn ? ptx::umma_desc_mn128(smem0 + HALF_BYTES, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0 + HALF_BYTES);
+        // 16 further along K: 32 bytes inside the swizzled row, or 16 rows of 128 bytes (addresses count 16 bytes)
+        const uint32_t a_step = d.a_mn ? 2048 >> 4 : 32 >> 4, b_step = d.b_mn ? 2048 >> 4 : 32 >> 4;
+        const uint32_t d_tmem = tmem_base + acc * TILE_N;
+        const int total = d.runs * d.kb;
+        for (int kb = 0; kb < total; ++kb) {
+          ok = ptx::mbar_wait_warp(&full[s], ph, abort_flag);
+          if (!ok) break;
+          ptx::tc_fence_after();
+          const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(s) * (STAGE_BYTES >> 4);
+          const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (STAGE_BYTES >> 4);
+          if (ptx::elect_one()) {
+#pragma unroll
+            for (int k = 0; k < BLOCK_K / 16; ++k)
+              ptx::umma_bf16_pair(d_tmem, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb | k) != 0 ? 1u : 0u);
+            ptx::umma_commit_pair(&empty[s]);
+          }
+          __syncwarp();
+          if (++s == STAGES) { s = 0; ph ^= 1u; }
+        }
+        if (ok) {
+          if (ptx::elect_one()) ptx::umma_commit_pair(&tfull[acc]);
+          __syncwarp();
+        }
+      }
+      if (!ok) {
+        // wait (bounded) until the MMAs issued so far have retired before tensor memory is freed
+        if (ptx::elect_one()) {
+          ptx::umma_commit_pair(drain);
+          const long long t0 = clock64();
+          while (!ptx::mbar_try_wait(drain, 0) && clock64() - t0 < ptx::kWaitLimitCycles / 8) {}
+        }
+        __syncwarp();
+      }
+    }
+  } else {
+    // -------------------------------------------------------------- epilogue warps
+    const int q = warp & 3;              // tensor-memory lane quarter
+    const int half = (warp - 2) >> 2;    // column half
+    constexpr int HALF_N = OUT_N / 2, CHUNKS = HALF_N / 16;
+    Walk walk;
+    uint32_t tl = 0;
+    for (int u = walk.take(p); u >= 0; u = walk.take(p), ++tl) {
+      const Unit t = find_unit(p, u);
+      const DevProduct& d = p.prod[t.prod];
+      const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
+      const long long row = static_cast<long long>(t.m_blk) * TILE_M + rank * CTA_M + q * 32 + lane;
+      const bool in = row < d.M;
+      const int c0 = t.n_blk * OUT_N + half * HALF_N;
+      if (!ptx::mbar_wait(&tfull[acc], aph, abort_flag)) break;
+      ptx::tc_fence_after();
+      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * TILE_N + half * HALF_N;
+#pragma unroll 1
+      for (int c = 0; c < CHUNKS; ++c) {
+        const int n0 = c0 + c * 16;
+        if (n0 >= d.N) break;
+        const long long at = row * p.hid.ldm + n0;
+        float v[16];
+        if (MODE == PLAIN) {
+          ptx::tmem_ld16(t_row + c * 16, v);
+          ptx::tmem_ld_wait();
+          if (d.bias) add_bias<F32>(d.bias, n0, d.N, v);
+          if (in) store16_user<F32>(d.C, row * d.ldc + n0, d.N - n0, v);
+        } else if (MODE == FORWARD_GATED) {
+          float w[16];
+          ptx::tmem_ld16(t_row + c * 16, v);
+          ptx::tmem_ld16(t_row + TILE_N / 2 + c * 16, w);
+          ptx::tmem_ld_wait();
+          if (in) {
+            if (p.hid.hi) keep16<F32, true>(p.hid, at, v, w);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = v[i] * sigmoid_of<F32>(v[i]) * w[i];
+            store16_planes<F32>(p.hid.H + at, p.hid.plane_stride, v);
+          }
+        } else if (MODE == FORWARD_ACT) {
+          ptx::tmem_ld16(t_row + c * 16, v);
+          ptx::tmem_ld_wait();
+          if (d.bias) add_bias<F32>(d.bias, n0, d.N, v);
+          if (in) {
+            if (p.hid.hi) keep16<F32, false>(p.hid, at, v, nullptr);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float slope;
+              gelu_and_slope<F32>(v[i], p.act, &v[i], &slope);
+            }
+            store16_planes<F32>(p.hid.H + at, p.hid.plane_stride, v);
+          }
+        } else {
+          Kept<F32, GATED> kept;
+          if (in) kept.load(p.hid, at);
+          ptx::tmem_ld16(t_row + c * 16, v);
+          ptx::tmem_ld_wait();
+          if (in) {
+            float h[16], w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float g = kept.first(i);
+              if (GATED) {
+                const float up = kept.second(i), s = sigmoid_of<F32>(g), a = g * s;
+                h[i] = a * up;
+                w[i] = v[i] * a;
+                v[i] = v[i] * up * (s * fmaf(g, 1.0f - s, 1.0f));
+              } else {
+                float a, slope;
+                gelu_and_slope<F32>(g, p.act, &a, &slope);
+                h[i] = a;
+                v[i] *= slope;
+              }
+            }
+            store16_planes<F32>(p.hid.H + at, p.hid.plane_stride, h);
+            store16_planes<F32>(p.hid.dG + at, p.hid.plane_stride, v);
+            if (GATED) store16_planes<F32>(p.hid.dU + at, p.hid.plane_stride, w);
+          }
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(&tempty[acc]), 0));
+    }
+  }
+
+  ptx::tc_fence_before();
+  ptx::cluster_sync_all();     // neither CTA leaves while the other may still signal it or read its shared memory
+  if (threadIdx.x == 0 && *abort_flag) record_status(p.status, FFSPLIT_ERR_TIMEOUT, blockIdx.x, KID_TRAIN);
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc_pair(tmem_base, TMEM_COLS);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// Tensor map over [planes][rows][cols]; box of 64 columns by box_rows rows, 128-byte swizzle, zeros outside.  Made anew
+// for every launch: it costs the host well under a microsecond.
+ffsplit_status encode(ffsplit_ctx* ctx, const Matrix& m, int box_rows, CUtensorMap* out) {
+  if (!ctx->encode_fn) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+    if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn)
+      return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    ctx->encode_fn = fn;
+  }
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows), static_cast<cuuint64_t>(m.planes)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(m.ld) * 2, static_cast<cuuint64_t>(m.plane_stride) * 2};
+  cuuint32_t box[3] = {BLOCK_K, static_cast<cuuint32_t>(box_rows), 1}, estr[3] = {1, 1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_fn)(
+      out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(m.p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
+  return FFSPLIT_OK;
+}
+
+template <int MODE, bool F32>
+ffsplit_status launch_mode(ffsplit_ctx* ctx, const Params& p, int clusters, cudaStream_t st) {
+  // (set on every launch: a host-side lookup, and the attribute belongs to the device, not to the context)
+  cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(train_gemm_kernel)");
+  e = launch_pdl(train_gemm_kernel<MODE, F32>, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, p);
+  ctx->launches++;
+  return check_cuda(ctx, e, "train_gemm_kernel launch");
+}
+
+}  // namespace
+
+ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, cudaStream_t st) {
+  Params p;
+  std::memset(&p, 0, sizeof(p));
+  const int clusters_max = ctx->num_sms / 2;
+  // longest tiles first
+  int order[MAX_PRODUCTS];
+  long long length[MAX_PRODUCTS];
+  const int planes6 = f32 ? 6 : 1;
+  for (int i = 0; i < n; ++i) {
+    length[i] = static_cast<long long>(products[i].pairs) * planes6 * ((products[i].K + BLOCK_K - 1) / BLOCK_K);
+    int at = i;
+    for (; at > 0 && length[order[at - 1]] < length[i]; --at) order[at] = order[at - 1];
+    order[at] = i;
+  }
+  const int out_n = mode == FORWARD_GATED ? TILE_N / 2 : TILE_N;
+  long long units = 0;
+  for (int i = 0; i < n; ++i) {
+    const Product& g = products[order[i]];
+    DevProduct& d = p.prod[i];
+    const int maps_b = mode == FORWARD_GATED ? 2 : g.pairs;
+    ffsplit_status s;
+    for (int j = 0; j < g.pairs; ++j)
+      if ((s = encode(ctx, g.a[j], g.a_mn ? BLOCK_K : CTA_M, &d.a[j])) != FFSPLIT_OK) return s;
+    for (int j = 0; j < maps_b; ++j)
+      if ((s = encode(ctx, g.b[j], g.b_mn ? BLOCK_K : CTA_M, &d.b[j])) != FFSPLIT_OK) return s;
+    d.M = g.M; d.N = g.N;
+    d.kb = static_cast<int>((g.K + BLOCK_K - 1) / BLOCK_K);
+    d.pairs = g.pairs; d.runs = g.pairs * planes6;
+    d.a_mn = g.a_mn; d.b_mn = g.b_mn;
+    d.tiles_m = static_cast<int>((g.M + TILE_M - 1) / TILE_M);
+    d.tiles_n = (g.N + out_n - 1) / out_n;
+    d.unit0 = static_cast<int>(units);
+    d.C = g.C; d.ldc = g.ldc; d.bias = g.bias;
+    // panel height: the tiles in flight form a block whose two sides carry about the same operand bytes (both 256 wide)
+    int best = 1;
+    double best_cost = 1e300;
+    for (int h = 1; h <= d.tiles_m && h <= clusters_max; ++h) {
+      const double w = static_cast<double>(clusters_max) / h;
+      const double cost = h + (w < d.tiles_n ? w : d.tiles_n);
+      if (cost < best_cost - 1e-9) { best_cost = cost; best = h; }
+    }
+    d.panel_m = best;
+    units += static_cast<long long>(d.tiles_m) * d.tiles_n;
+    if (units > 0x3fffffffll) return fail(ctx, FFSPLIT_ERR_SHAPE, "more than 2^30 tiles in one product");
+  }
+  p.n_prod = n;
+  p.units = static_cast<int>(units);
+  const int clusters = units < clusters_max ? static_cast<int>(units) : clusters_max;
+  // The product with the longest tiles is dealt first; where its last round does not reach every cluster and shorter
+  // tiles follow, the clusters left out get as many of those as fit into the length of one long tile.
+  p.heavy = 0; p.short_from = 0; p.extra = 0;
+  if (n > 1 && length[order[0]] > length[order[1]]) {
+    p.heavy = p.prod[1].unit0;
+    const int left = p.heavy % clusters;
+    if (left) {
+      constexpr int EPILOGUE_BLOCKS = 4;    // a tile's set-up and tail, in k-blocks
+      p.short_from = left;
+      long long extra = (length[order[0]] + EPILOGUE_BLOCKS) / (length[order[1]] + EPILOGUE_BLOCKS);
+      const long long most = (units - p.heavy) / (clusters - left);
+      p.extra = static_cast<int>(extra < most ? extra : most);
+    }
+  }
+  p.act = act;
+  p.hid = hidden;
+  p.status = ctx->status();
+  switch (mode) {
+    case PLAIN: return f32 ? launch_mode<PLAIN, true>(ctx, p, clusters, st) : launch_mode<PLAIN, false>(ctx, p, clusters, st);
+    case FORWARD_GATED: return f32 ? launch_mode<FORWARD_GATED, true>(ctx, p, clusters, st) : launch_mode<FORWARD_GATED, false>(ctx, p, clusters, st);
+    case FORWARD_ACT: return f32 ? launch_mode<FORWARD_ACT, true>(ctx, p, clusters, st) : launch_mode<FORWARD_ACT, false>(ctx, p, clusters, st);
+    case BACKWARD_GATED: return f32 ? launch_mode<BACKWARD_GATED, true>(ctx, p, clusters, st) : launch_mode<BACKWARD_GATED, false>(ctx, p, clusters, st);
+    default: return f32 ? launch_mode<BACKWARD_ACT, true>(ctx, p, clusters, st) : launch_mode<BACKWARD_ACT, false>(ctx, p, clusters, st);
+  }
+}
+
+}  // namespace tg
+}  // namespace ffsp

@@ -1,0 +1,72 @@
+// The products of a training pass, as train_gemm.cu runs them.  Not part of the public ABI.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "internal.h"
+
+namespace ffsp {
+namespace tg {
+
+// One operand of a product: `planes` bf16 matrices [rows, cols] with pitch ld, plane_stride elements apart.  A bf16
+// tensor is one plane; an fp32 tensor is three, whose sum it is to fp32 accuracy (split3() below).
+struct Matrix {
+  const void* p;
+  long long rows, cols, ld, plane_stride;
+  int planes;
+};
+
+enum Mode : int {
+  PLAIN = 0,            // C = sum of the pairs' products (+ bias)
+  FORWARD_GATED = 1,    // G = A0 B0, U = A0 B1: keeps G, U; H = silu(G) U
+  FORWARD_ACT = 2,      // Z = A0 B0 + bias: keeps Z; H = act(Z)
+  BACKWARD_GATED = 3,   // dH = A0 B0: dU = dH silu(G), dG = dH U silu'(G), H = silu(G) U
+  BACKWARD_ACT = 4      // dH = A0 B0: dZ = dH act'(Z), H = act(Z)
+};
+
+// C [M, N] = sum over pairs of A_i [M, K] B_i [K, N].  a_mn: A lies in memory as [K, M] rows (M runs along memory),
+// else as [M, K]; b_mn: B as [K, N], else as [N, K].
+struct Product {
+  Matrix a[2], b[2];
+  int pairs;
+  int a_mn, b_mn;
+  long long M, K;
+  int N;
+  void* C;               // PLAIN: bf16 or fp32 output
+  long long ldc;
+  const void* bias;      // [N], the layer's type, or nullptr
+};
+
+// What the activation's epilogue reads and writes, all [T, ldm]: what the forward pass keeps (hi, hi2: the upper 16 bits
+// of G or Z and of U; lo: what follows them, see pack20; fp32 layers: hi, hi2 are fp32 and lo is unused) and the bf16
+// planes of H, dG (dZ) and dU.
+struct Hidden {
+  void *hi, *hi2;
+  unsigned char* lo;
+  __nv_bfloat16 *H, *dG, *dU;
+  long long ldm, plane_stride;
+};
+
+#ifdef __CUDACC__
+// x = x0 + x1 + x2 with bf16 terms; non-finite values stay in x0 alone, and a finite x0 does not round to infinity.
+__device__ __forceinline__ void split3(float x, float* o) {
+  float a = __bfloat162float(__float2bfloat16_rn(x));
+  if ((__float_as_uint(a) & 0x7f800000u) == 0x7f800000u) {
+    const bool finite = (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
+    if (!finite) {
+      o[0] = a; o[1] = 0.f; o[2] = 0.f;
+      return;
+    }
+    a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  }
+  const float r = x - a, b = __bfloat162float(__float2bfloat16_rn(r));
+  o[0] = a; o[1] = b; o[2] = r - b;
+}
+#endif
+
+// Up to four PLAIN products (or one of the other modes) as one launch.  f32: three-plane operands and fp32 outputs.
+ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, cudaStream_t st);
+
+}  // namespace tg
+}  // namespace ffsp
