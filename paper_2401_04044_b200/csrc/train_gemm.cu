@@ -15,7 +15,10 @@
 //
 // fp32 layers: every fp32 matrix is split into three bf16 planes (x0 = bf16(x), x1 = bf16(x - x0), ...: 24 significant
 // bits), and the six products of planes (i, j), i + j <= 2, are accumulated as six runs over K, the smallest first.
-// What is dropped is below 2^-24 of a term.
+// What is dropped is below 2^-24 of a term.  The tensor cores cut their running sums to 24 bits instead of rounding them
+// (measured: a bias of about 3e-8 of the sum per MMA, 8e-6 in all at K = 2752), so the sum is taken out of tensor memory
+// every PROMOTE k-blocks of the largest product and added up in registers; the five small products before it (2^-8 of
+// the sum and less) need no such care.
 //
 // Warp roles: 0 TMA producer (both CTAs), 1 MMA issuer (rank 0), 2-9 epilogue (four lane quarters x two column halves).
 // Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
@@ -38,6 +41,7 @@ constexpr int THREADS = 32 * (EPI_WARPS + 2);
 constexpr int TMEM_COLS = 512;
 constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 256 + 1024;
 constexpr int MAX_PRODUCTS = 4;
+constexpr int PROMOTE = 2;   // k-blocks: 8 MMAs, 2.5e-7
 
 struct Unit {
   int prod, m_blk, n_blk;
@@ -127,6 +131,13 @@ __device__ __forceinline__ void run_planes(const DevProduct& d, int run, int* pa
   // (0,2) (1,1) (2,0) (0,1) (1,0) (0,0)
   *pa = (0x012010 >> (4 * (5 - combo))) & 0xF;
   *pb = (0x001012 >> (4 * combo)) & 0xF;
+}
+
+// fp32 layers: end of the part of a tile's sum that begins at k-block `begin` (counted over all runs).
+__device__ __forceinline__ int part_end(const DevProduct& d, int begin) {
+  const int total = d.runs * d.kb, large = total - d.pairs * d.kb;   // the last `pairs` runs are the largest product
+  const int end = (begin > large ? begin : large) + PROMOTE;
+  return end < total ? end : total;
 }
 
 // ---------------------------------------------------------------------------------------------- number formats
@@ -425,39 +436,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
       int s = 0;
       bool ok = true;
       const uint32_t smem0 = ptx::smem_u32(smem);
-      for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p), ++tl) {
+      for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
         const Unit t = find_unit(p, u);
         const DevProduct& d = p.prod[t.prod];
-        const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
-        ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aph ^ 1, abort_flag) ? 1 : 0, 0) != 0;
-        if (!ok) break;
-        ptx::tc_fence_after();
         // bits 15, 16: the operand's rows run along memory
         const uint32_t idesc = idesc0 | (d.a_mn ? 1u << 15 : 0u) | (d.b_mn ? 1u << 16 : 0u);
         const uint64_t a_desc0 = d.a_mn ? ptx::umma_desc_mn128(smem0, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0);
         const uint64_t b_desc0 = d.b_mn ? ptx::umma_desc_mn128(smem0 + HALF_BYTES, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0 + HALF_BYTES);
         // 16 further along K: 32 bytes inside the swizzled row, or 16 rows of 128 bytes (addresses count 16 bytes)
         const uint32_t a_step = d.a_mn ? 2048 >> 4 : 32 >> 4, b_step = d.b_mn ? 2048 >> 4 : 32 >> 4;
-        const uint32_t d_tmem = tmem_base + acc * TILE_N;
         const int total = d.runs * d.kb;
-        for (int kb = 0; kb < total; ++kb) {
-          ok = ptx::mbar_wait_warp(&full[s], ph, abort_flag);
+        // fp32: the tile is summed in parts, each through an accumulator of its own
+        for (int begin = 0; begin < total && ok; ++tl) {
+          const int end = F32 ? part_end(d, begin) : total;
+          const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
+          ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aph ^ 1, abort_flag) ? 1 : 0, 0) != 0;
           if (!ok) break;
           ptx::tc_fence_after();
-          const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(s) * (STAGE_BYTES >> 4);
-          const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (STAGE_BYTES >> 4);
-          if (ptx::elect_one()) {
+          const uint32_t d_tmem = tmem_base + acc * TILE_N;
+          for (int kb = begin; kb < end; ++kb) {
+            ok = ptx::mbar_wait_warp(&full[s], ph, abort_flag);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(s) * (STAGE_BYTES >> 4);
+            const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (STAGE_BYTES >> 4);
+            if (ptx::elect_one()) {
 #pragma unroll
-            for (int k = 0; k < BLOCK_K / 16; ++k)
-              ptx::umma_bf16_pair(d_tmem, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb | k) != 0 ? 1u : 0u);
-            ptx::umma_commit_pair(&empty[s]);
+              for (int k = 0; k < BLOCK_K / 16; ++k)
+                ptx::umma_bf16_pair(d_tmem, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb > begin || k > 0) ? 1u : 0u);
+              ptx::umma_commit_pair(&empty[s]);
+            }
+            __syncwarp();
+            if (++s == STAGES) { s = 0; ph ^= 1u; }
           }
-          __syncwarp();
-          if (++s == STAGES) { s = 0; ph ^= 1u; }
-        }
-        if (ok) {
-          if (ptx::elect_one()) ptx::umma_commit_pair(&tfull[acc]);
-          __syncwarp();
+          if (ok) {
+            if (ptx::elect_one()) ptx::umma_commit_pair(&tfull[acc]);
+            __syncwarp();
+          }
+          begin = end;
         }
       }
       if (!ok) {
@@ -477,16 +493,53 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
     constexpr int HALF_N = OUT_N / 2, CHUNKS = HALF_N / 16;
     Walk walk;
     uint32_t tl = 0;
-    for (int u = walk.take(p); u >= 0; u = walk.take(p), ++tl) {
+    bool live = true;
+    for (int u = walk.take(p); u >= 0 && live; u = walk.take(p), ++tl) {
       const Unit t = find_unit(p, u);
       const DevProduct& d = p.prod[t.prod];
-      const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
       const long long row = static_cast<long long>(t.m_blk) * TILE_M + rank * CTA_M + q * 32 + lane;
       const bool in = row < d.M;
       const int c0 = t.n_blk * OUT_N + half * HALF_N;
+      const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * HALF_N;
+      if (F32) {
+        // All parts of the sum but the last are added up in registers (a gated tile's two halves lie 128 columns
+        // apart); then it goes back to where the last part lies, and on as for bf16.
+        constexpr int BLOCKS = 8, SKIP = MODE == FORWARD_GATED ? TILE_N / 2 - HALF_N : 0;
+        float sum[BLOCKS][16];
+        bool first = true;
+        for (int begin = 0;; ++tl) {
+          const int end = part_end(d, begin);
+          const bool last = end == d.runs * d.kb;
+          if (first && last) break;      // one part: nothing to add
+          if (!ptx::mbar_wait(&tfull[tl & 1], (tl >> 1) & 1, abort_flag)) { live = false; break; }
+          ptx::tc_fence_after();
+          const uint32_t t_part = t_quarter + (tl & 1) * TILE_N;
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b) {
+            const uint32_t at = t_part + b * 16 + (b >= BLOCKS / 2 ? SKIP : 0);
+            float v[16];
+            ptx::tmem_ld16(at, v);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[b][i] = first ? v[i] : sum[b][i] + v[i];
+            if (last) ptx::tmem_st16(at, sum[b]);
+          }
+          first = false;
+          if (last) {
+            ptx::tmem_st_wait();
+            break;
+          }
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(&tempty[tl & 1]), 0));
+          begin = end;
+        }
+        if (!live) break;
+      }
+      const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
       if (!ptx::mbar_wait(&tfull[acc], aph, abort_flag)) break;
       ptx::tc_fence_after();
-      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * TILE_N + half * HALF_N;
+      const uint32_t t_row = t_quarter + acc * TILE_N;
 #pragma unroll 1
       for (int c = 0; c < CHUNKS; ++c) {
         const int n0 = c0 + c * 16;
