@@ -73,60 +73,76 @@ __global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_cons
   }
 }
 
-// Bias gradients: out[c] = sum over rows of in[r, c], in fp32 and in a fixed order (eight interleaved row sets, four
-// partial sums in each).  A block takes 64 columns.  `planes` bf16 planes that add up, or 0: fp32 values.
+// Bias gradients: out[c] = sum over rows of in[r, c], in fp32 and in a fixed order.  Bound by reading dZ and dY once.  A
+// block sums `rows_per` rows of 256 columns (a warp reads 512 contiguous bytes of every eighth row) and leaves a partial;
+// a second launch adds the partials.  (One block per 64 columns over all rows, without the second launch, had too few
+// loads in flight: 307 us for 4096 rows of 20480 + 5120 columns.)
 struct SumJob {
-  const void* in;
+  const void* in;          // `planes` bf16 planes that add up, or (planes = 0) fp32 values
   void* out;               // bf16, or fp32 with f32_out
-  long long rows, ld, plane_stride;
-  int cols, planes, f32_out;
+  float* partial;          // [splits][cols]
+  long long rows, ld, plane_stride, rows_per;
+  int cols, planes, f32_out, splits, col_blocks, block0;
 };
 struct SumArgs {
   SumJob job[2];
+  int n;
 };
-__device__ __forceinline__ float2 load2(const SumJob& j, long long row, int c) {
+constexpr int SUM_COLS = 256;
+// Eight columns of one row: 8 lane + (0 .. 7) of bf16 planes, lane + 32 (0 .. 7) of fp32 values (whose rows may start
+// anywhere).
+__device__ __forceinline__ void add8(const SumJob& j, long long row, int c0, int lane, float* s) {
   if (j.planes == 0) {
-    const float* p = static_cast<const float*>(j.in) + row * j.ld + c;
-    return make_float2(p[0], c + 1 < j.cols ? p[1] : 0.f);
+    const float* p = static_cast<const float*>(j.in) + row * j.ld + c0 + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (c0 + lane + 32 * i < j.cols) s[i] += __ldg(p + 32 * i);
+    return;
   }
-  float2 r = make_float2(0.f, 0.f);
+  if (c0 + lane * 8 >= j.cols) return;      // (a last group of eight ends inside the row's padding)
   for (int k = 0; k < j.planes; ++k) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(j.in) + k * j.plane_stride + row * j.ld + c);
-    r.x += __uint_as_float(w << 16);
-    r.y += __uint_as_float(w & 0xffff0000u);
+    const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(j.in) + k * j.plane_stride + row * j.ld + c0 + lane * 8));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[2 * i] += __uint_as_float(w[i] << 16);
+      s[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
+    }
   }
-  return r;
 }
 __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ SumArgs a) {
-  __shared__ float2 red[8][32];
+  __shared__ float red[8][SUM_COLS];
+  pdl_wait();
+  const SumJob& j = a.job[a.n > 1 && static_cast<int>(blockIdx.x) >= a.job[1].block0 ? 1 : 0];
+  const int b = blockIdx.x - j.block0, split = b / j.col_blocks, c0 = (b - split * j.col_blocks) * SUM_COLS;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const long long begin = split * j.rows_per, end = begin + j.rows_per < j.rows ? begin + j.rows_per : j.rows;
+  float s[8] = {};
+  long long r = begin + w;
+  for (; r + 56 < end; r += 64) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add8(j, r + 8 * k, c0, lane, s);
+  }
+  for (; r < end; r += 8) add8(j, r, c0, lane, s);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) red[w][j.planes == 0 ? lane + 32 * i : lane * 8 + i] = s[i];
+  __syncthreads();
+  const int c = threadIdx.x;
+  if (c0 + c < j.cols) {
+    float t = red[0][c];
+    for (int k = 1; k < 8; ++k) t += red[k][c];
+    j.partial[static_cast<long long>(split) * j.cols + c0 + c] = t;
+  }
+}
+__global__ void __launch_bounds__(256) column_sum_finish_kernel(const __grid_constant__ SumArgs a) {
   pdl_wait();
   const SumJob& j = a.job[blockIdx.y];
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 64 + lane * 2;
-  if (blockIdx.x * 64 >= j.cols) return;
-  float2 s[4] = {};
-  if (c < j.cols)
-    for (long long r = w; r < j.rows; r += 32) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (r + 8 * k < j.rows) {
-          const float2 v = load2(j, r + 8 * k, c);
-          s[k].x += v.x;
-          s[k].y += v.y;
-        }
-    }
-  red[w][lane] = make_float2((s[0].x + s[1].x) + (s[2].x + s[3].x), (s[0].y + s[1].y) + (s[2].y + s[3].y));
-  __syncthreads();
-  if (w == 0 && c < j.cols) {
-    float2 t = red[0][lane];
-    for (int k = 1; k < 8; ++k) { t.x += red[k][lane].x; t.y += red[k][lane].y; }
-    if (j.f32_out) {
-      static_cast<float*>(j.out)[c] = t.x;
-      if (c + 1 < j.cols) static_cast<float*>(j.out)[c + 1] = t.y;
-    } else {
-      static_cast<__nv_bfloat16*>(j.out)[c] = __float2bfloat16_rn(t.x);
-      if (c + 1 < j.cols) static_cast<__nv_bfloat16*>(j.out)[c + 1] = __float2bfloat16_rn(t.y);
-    }
-  }
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= j.cols) return;
+  float t = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < j.splits; ++k) t += __ldcg(j.partial + static_cast<long long>(k) * j.cols + c);
+  if (j.f32_out) static_cast<float*>(j.out)[c] = t;
+  else static_cast<__nv_bfloat16*>(j.out)[c] = __float2bfloat16_rn(t);
 }
 
 }  // namespace train
@@ -135,13 +151,21 @@ namespace {
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Offsets of what the forward pass keeps, and of the workspace's buffers.  The rows of both are padded to a multiple
+// Row ranges of a column sum: about four blocks of 256 columns to an SM, but no fewer than 64 rows (eight to a warp).
+int sum_splits(long long rows, int cols) {
+  const long long col_blocks = (cols + train::SUM_COLS - 1) / train::SUM_COLS;
+  long long n = (4 * 148 + col_blocks - 1) / col_blocks;
+  if (n > (rows + 63) / 64) n = (rows + 63) / 64;
+  return static_cast<int>(n < 1 ? 1 : n);
+}
+
+// Size of what the forward pass keeps, and offsets of the workspace's buffers.  The rows of both are padded to a multiple
 // of 64 elements (ldm for m, ldd for d), so that every row starts on 128 bytes; the pads are neither written to by
 // whole chunks that matter nor read (the tensor maps end at m and d).
 struct TrainLayout {
   long long ldm, ldd;
-  size_t hi, hi2, lo, saved;
-  size_t H, dG, dU, W1, W1u, W2, X, dY, end;
+  size_t saved;
+  size_t H, dG, dU, W1, W1u, W2, X, dY, sums, end;
 };
 TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   TrainLayout L;
@@ -149,13 +173,9 @@ TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   L.ldm = round_up_ll(s.m, 64);
   L.ldd = round_up_ll(s.d, 64);
   const size_t hidden = static_cast<size_t>(T) * L.ldm;
-  size_t off = 0;
-  L.hi = off;  off = up256(off + hidden * (f32 ? 4 : 2));
-  L.hi2 = off; off = up256(off + (gated ? hidden * (f32 ? 4 : 2) : 0));
-  L.lo = off;  off = up256(off + (f32 ? 0 : hidden));
-  L.saved = off;
+  L.saved = up256(tg::kept_bytes(T, L.ldm, gated, f32));
   const size_t planes = f32 ? 3 : 1;
-  off = 0;
+  size_t off = 0;
   L.H = off;  off = up256(off + hidden * 2 * planes);
   L.dG = off; off = up256(off + hidden * 2 * planes);
   L.dU = off; off = up256(off + (gated ? hidden * 2 * planes : 0));
@@ -167,6 +187,7 @@ TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   const size_t tokens = f32 ? static_cast<size_t>(T) * L.ldd * 6 : 0;
   L.X = off;  off = up256(off + tokens);
   L.dY = off; off = up256(off + tokens);
+  L.sums = off; off = up256(off + 4 * (static_cast<size_t>(sum_splits(T, s.m)) * s.m + static_cast<size_t>(sum_splits(T, s.d)) * s.d));
   L.end = off;
   return L;
 }
@@ -230,9 +251,7 @@ struct Pass {
   }
   tg::Hidden buffers(char* saved) const {
     tg::Hidden h;
-    h.hi = saved ? saved + L.hi : nullptr;
-    h.hi2 = saved ? saved + L.hi2 : nullptr;
-    h.lo = saved ? reinterpret_cast<unsigned char*>(saved + L.lo) : nullptr;
+    h.kept = saved;
     h.H = reinterpret_cast<__nv_bfloat16*>(ws + L.H);
     h.dG = reinterpret_cast<__nv_bfloat16*>(ws + L.dG);
     h.dU = reinterpret_cast<__nv_bfloat16*>(ws + L.dU);
@@ -320,13 +339,29 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
   if (grads.db1 || grads.db2) {
     train::SumArgs a;
     std::memset(&a, 0, sizeof(a));
-    int k = 0, cols = 0;
-    const int f32 = p.f32() ? 1 : 0;
-    if (grads.db1) { a.job[k++] = {h.dG, grads.db1, T, p.L.ldm, T * p.L.ldm, m, f32 ? 3 : 1, f32}; cols = m; }
-    if (grads.db2) { a.job[k++] = {dY, grads.db2, T, d, 0, d, f32 ? 0 : 1, f32}; cols = cols > d ? cols : d; }
-    const cudaError_t e = launch_pdl(train::column_sum_kernel, dim3((cols + 63) / 64, k), dim3(256), 0, st, a);
+    int blocks = 0, cols = 0;
+    float* partial = reinterpret_cast<float*>(p.ws + p.L.sums);
+    const auto add = [&](const void* in, void* to, long long ld, long long plane_stride, int n_cols, int planes) {
+      train::SumJob& j = a.job[a.n++];
+      j.in = in; j.out = to; j.partial = partial;
+      j.rows = T; j.ld = ld; j.plane_stride = plane_stride;
+      j.cols = n_cols; j.planes = planes; j.f32_out = p.f32() ? 1 : 0;
+      j.col_blocks = (n_cols + train::SUM_COLS - 1) / train::SUM_COLS;
+      j.splits = sum_splits(T, n_cols);
+      j.rows_per = (T + j.splits - 1) / j.splits;
+      j.block0 = blocks;
+      blocks += j.splits * j.col_blocks;
+      partial += static_cast<size_t>(j.splits) * n_cols;
+      cols = cols > n_cols ? cols : n_cols;
+    };
+    if (grads.db1) add(h.dG, grads.db1, p.L.ldm, T * p.L.ldm, m, p.f32() ? 3 : 1);
+    if (grads.db2) add(dY, grads.db2, d, 0, d, p.f32() ? 0 : 1);
+    cudaError_t e = launch_pdl(train::column_sum_kernel, dim3(blocks), dim3(256), 0, st, a);
     ctx->launches++;
-    return check_cuda(ctx, e, "column_sum_kernel launch");
+    if (e != cudaSuccess) return check_cuda(ctx, e, "column_sum_kernel launch");
+    e = launch_pdl(train::column_sum_finish_kernel, dim3((cols + 255) / 256, a.n), dim3(256), 0, st, a);
+    ctx->launches++;
+    return check_cuda(ctx, e, "column_sum_finish_kernel launch");
   }
   return FFSPLIT_OK;
 }

@@ -39,7 +39,8 @@ constexpr int BLOCK64_BYTES = 64 * BLOCK_K * 2;      // 64 x 64 elements: MN-maj
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 32 * (EPI_WARPS + 2);
 constexpr int TMEM_COLS = 512;
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 256 + 1024;
+constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 256 + EPI_WARPS * 32 * 33 * 4 + 1024;
+static_assert(SMEM_BYTES <= 232448, "shared memory of one CTA");
 constexpr int MAX_PRODUCTS = 4;
 constexpr int PROMOTE = 2;   // k-blocks: 8 MMAs, 2.5e-7
 
@@ -58,6 +59,7 @@ struct DevProduct {
   void* C;
   long long ldc;
   const void* bias;
+  int ragged;            // rows of C do not all start on 16 bytes
 };
 
 struct Params {
@@ -193,19 +195,19 @@ __device__ __forceinline__ void store16_bf16(__nv_bfloat16* base, const float* v
 // 16 values into the library's own buffers (pitch a multiple of 64 elements): one bf16 plane, or three.
 template <bool F32>
 __device__ __forceinline__ void store16_planes(__nv_bfloat16* base, long long plane_stride, const float* v) {
-  if (!F32) {
+  if constexpr (!F32) {
     store16_bf16(base, v);
-    return;
-  }
-  float w[3][16];
+  } else {
+    float w[3][16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float o[3];
-    split3(v[i], o);
-    w[0][i] = o[0]; w[1][i] = o[1]; w[2][i] = o[2];
-  }
+    for (int i = 0; i < 16; ++i) {
+      float o[3];
+      split3(v[i], o);
+      w[0][i] = o[0]; w[1][i] = o[1]; w[2][i] = o[2];
+    }
 #pragma unroll
-  for (int k = 0; k < 3; ++k) store16_bf16(base + k * plane_stride, w[k]);
+    for (int k = 0; k < 3; ++k) store16_bf16(base + k * plane_stride, w[k]);
+  }
 }
 __device__ __forceinline__ void store16_f32(float* base, const float* v) {   // 16-byte aligned
 #pragma unroll
@@ -264,70 +266,151 @@ __device__ __forceinline__ void add_bias(const void* bias, int n0, int N, float*
   }
 }
 
-// What is kept of 16 columns of one row, as loaded; of the pair (G, U), or of Z alone.
+// What is kept lies in blocks of 32 rows x 16 columns, which is what a warp of either pass handles at once (a lane to a
+// row): 16-byte pieces, each 512 contiguous bytes of the warp.  (Row by row, every lane's piece was a line of its own.)
 template <bool F32, bool GATED>
 struct Kept {
-  uint4 a[F32 ? 4 : 2];
-  uint4 b[GATED ? (F32 ? 4 : 2) : 1];
-  uint4 lo;
-  __device__ __forceinline__ void load(const Hidden& h, long long at) {
-    constexpr int Q = F32 ? 4 : 2;
-    const char* pa = static_cast<const char*>(h.hi) + at * (F32 ? 4 : 2);
-    const char* pb = static_cast<const char*>(h.hi2) + at * (F32 ? 4 : 2);
+  static constexpr int Q = F32 ? 4 : 2;                                    // pieces of 16 values of one of G, U, Z
+  static constexpr int PIECES = (GATED ? 2 * Q : Q) + (F32 ? 0 : 1);       // and one for the low bits
+  uint4 a[Q], b[GATED ? Q : 1], lo;
+  __device__ __forceinline__ static uint4* block(const Hidden& h, long long row, int n0) {
+    return static_cast<uint4*>(h.kept) + ((row >> 5) * (h.ldm >> 4) + (n0 >> 4)) * (PIECES * 32) + (row & 31);
+  }
+  __device__ __forceinline__ void load(const uint4* p) {
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
-      a[i] = __ldcs(reinterpret_cast<const uint4*>(pa) + i);
-      if (GATED) b[i] = __ldcs(reinterpret_cast<const uint4*>(pb) + i);
+      a[i] = __ldcs(p + i * 32);
+      if (GATED) b[i] = __ldcs(p + (Q + i) * 32);
     }
-    if (!F32) lo = __ldcs(reinterpret_cast<const uint4*>(h.lo + at));
+    if (!F32) lo = __ldcs(p + (PIECES - 1) * 32);
   }
-  __device__ __forceinline__ float first(int i) const {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(a);
-    if (F32) return __uint_as_float(w[i]);
-    const uint32_t top = (i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16);
-    const uint32_t byte = (reinterpret_cast<const uint32_t*>(&lo)[i >> 2] >> (8 * (i & 3))) & 0xffu;
-    return __uint_as_float(top | (GATED ? (byte & 0xfu) << 12 : byte << 8));
+  __device__ __forceinline__ void store(uint4* p) const {
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      p[i * 32] = a[i];
+      if (GATED) p[(Q + i) * 32] = b[i];
+    }
+    if (!F32) p[(PIECES - 1) * 32] = lo;
   }
-  __device__ __forceinline__ float second(int i) const {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(b);
+  __device__ __forceinline__ float value(const uint4* q, int i, bool upper_nibble) const {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
     if (F32) return __uint_as_float(w[i]);
-    const uint32_t top = (i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16);
-    const uint32_t byte = (reinterpret_cast<const uint32_t*>(&lo)[i >> 2] >> (8 * (i & 3))) & 0xffu;
-    return __uint_as_float(top | (byte >> 4) << 12);
+    const uint32_t top = (i & 1) ? (w[(i >> 1) & 7] & 0xffff0000u) : (w[(i >> 1) & 7] << 16);
+    const uint32_t byte = reinterpret_cast<const uint32_t*>(&lo)[i >> 2] >> (8 * (i & 3));
+    return __uint_as_float(top | (GATED ? (upper_nibble ? (byte & 0xf0u) << 8 : (byte & 0xfu) << 12) : (byte & 0xffu) << 8));
+  }
+  __device__ __forceinline__ float first(int i) const { return value(a, i, false); }
+  __device__ __forceinline__ float second(int i) const { return value(b, i, true); }
+  __device__ __forceinline__ void set(const float* g, const float* u) {
+    uint32_t *wa = reinterpret_cast<uint32_t*>(a), *wb = reinterpret_cast<uint32_t*>(b), *wl = reinterpret_cast<uint32_t*>(&lo);
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        wa[i] = __float_as_uint(g[i]);
+        if (GATED) wb[i] = __float_as_uint(u[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t x = round_bits(g[i], GATED ? 0x800u : 0x80u);
+        uint32_t byte;
+        if (GATED) {
+          const uint32_t y = round_bits(u[i], 0x800u);
+          wb[i >> 1] = (i & 1) ? (wb[i >> 1] | (y & 0xffff0000u)) : (y >> 16);
+          byte = ((x >> 12) & 0xfu) | ((y >> 8) & 0xf0u);
+        } else {
+          byte = (x >> 8) & 0xffu;
+        }
+        wa[i >> 1] = (i & 1) ? (wa[i >> 1] | (x & 0xffff0000u)) : (x >> 16);
+        wl[i >> 2] = (i & 3) ? (wl[i >> 2] | byte << (8 * (i & 3))) : byte;
+      }
+    }
   }
 };
 
-// Keeps 16 columns of one row.
-template <bool F32, bool GATED>
-__device__ __forceinline__ void keep16(const Hidden& h, long long at, const float* g, const float* u) {
-  if (F32) {
-    store16_f32(static_cast<float*>(h.hi) + at, g);
-    if (GATED) store16_f32(static_cast<float*>(h.hi2) + at, u);
-    return;
-  }
-  uint32_t a[8], b[8], lo[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const uint32_t x = round_bits(g[i], GATED ? 0x800u : 0x80u);
-    uint32_t byte;
-    if (GATED) {
-      const uint32_t y = round_bits(u[i], 0x800u);
-      b[i >> 1] = (i & 1) ? (b[i >> 1] | (y & 0xffff0000u)) : (y >> 16);
-      byte = ((x >> 12) & 0xfu) | ((y >> 8) & 0xf0u);
-    } else {
-      byte = (x >> 8) & 0xffu;
+// The activation's part of a pass for 16 columns of one row: v holds the accumulators (FORWARD_GATED: G, with U in w).
+template <int MODE, bool F32>
+__device__ __forceinline__ void finish16(const Hidden& h, int act, const void* bias, int N, long long row, int n0, float* v, float* w,
+                                         const Kept<F32, MODE == FORWARD_GATED || MODE == BACKWARD_GATED>& loaded) {
+  constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
+  const long long at = row * h.ldm + n0;
+  if (MODE == FORWARD_GATED || MODE == FORWARD_ACT) {
+    if (MODE == FORWARD_ACT && bias) add_bias<F32>(bias, n0, N, v);
+    if (h.kept) {
+      Kept<F32, GATED> k;
+      k.set(v, w);
+      k.store(Kept<F32, GATED>::block(h, row, n0));
     }
-    a[i >> 1] = (i & 1) ? (a[i >> 1] | (x & 0xffff0000u)) : (x >> 16);
-    lo[i >> 2] |= byte << (8 * (i & 3));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (GATED) {
+        v[i] = v[i] * sigmoid_of<F32>(v[i]) * w[i];
+      } else {
+        float slope;
+        gelu_and_slope<F32>(v[i], act, &v[i], &slope);
+      }
+    }
+    store16_planes<F32>(h.H + at, h.plane_stride, v);
+  } else {
+    float hid[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float g = loaded.first(i);
+      if (GATED) {
+        const float up = loaded.second(i), s = sigmoid_of<F32>(g), a = g * s;
+        hid[i] = a * up;
+        w[i] = v[i] * a;
+        v[i] = v[i] * up * (s * fmaf(g, 1.0f - s, 1.0f));
+      } else {
+        float slope;
+        gelu_and_slope<F32>(g, act, &hid[i], &slope);
+        v[i] *= slope;
+      }
+    }
+    store16_planes<F32>(h.H + at, h.plane_stride, hid);
+    store16_planes<F32>(h.dG + at, h.plane_stride, v);
+    if (GATED) store16_planes<F32>(h.dU + at, h.plane_stride, w);
   }
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(static_cast<__nv_bfloat16*>(h.hi) + at), "r"(a[0]),
-               "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(a[4]), "r"(a[5]), "r"(a[6]), "r"(a[7])
-               : "memory");
-  if (GATED)
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(static_cast<__nv_bfloat16*>(h.hi2) + at), "r"(b[0]),
-                 "r"(b[1]), "r"(b[2]), "r"(b[3]), "r"(b[4]), "r"(b[5]), "r"(b[6]), "r"(b[7])
-                 : "memory");
-  *reinterpret_cast<uint4*>(h.lo + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
+// Rows that do not start on 16 bytes (m odd, or fp32 widths that are no multiple of 4) leave through shared memory, so
+// that a warp writes along one row at a time: SPAN columns of 32 rows, one word a lane and row.  (One lane to a row wrote
+// two bytes into each of 32 lines per instruction: 88 us for the gradients of a 1000 x 2731 gated layer.)
+constexpr int STAGE_WORDS = 32 * 33;
+template <bool F32> constexpr int SPAN_COLS = F32 ? 32 : 64;
+template <bool F32>
+__device__ __forceinline__ void stage16(uint32_t* buf, int lane, int col, const float* v) {
+  uint32_t* row = buf + lane * 33;
+  if (F32) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) row[col + i] = __float_as_uint(v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) row[(col >> 1) + i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+  }
+}
+// The staged columns n .. n + valid - 1 of rows row0 .. of C.
+template <bool F32>
+__device__ __forceinline__ void write_staged(const uint32_t* buf, int lane, void* C, long long ldc, long long row0, int rows, int n, int valid) {
+  for (int r = 0; r < rows; ++r) {
+    const uint32_t* w = buf + r * 33;
+    const long long at = (row0 + r) * ldc + n;
+    if (F32) {
+      if (lane < valid) reinterpret_cast<uint32_t*>(C)[at + lane] = w[lane];
+    } else {
+      unsigned short* out = static_cast<unsigned short*>(C) + at;
+      if ((reinterpret_cast<uintptr_t>(out) & 3u) == 0) {
+        if (2 * lane + 1 < valid) *reinterpret_cast<uint32_t*>(out + 2 * lane) = w[lane];
+        else if (2 * lane < valid) out[2 * lane] = static_cast<unsigned short>(w[lane]);
+      } else {
+        // words start at the odd columns; column 0 is left over, and the last one where valid is even
+        const uint32_t word = w[lane] >> 16 | (lane < 31 ? w[lane + 1] << 16 : 0u);
+        if (lane < 31 && 2 * lane + 2 < valid) *reinterpret_cast<uint32_t*>(out + 2 * lane + 1) = word;
+        else if (2 * lane + 1 < valid) out[2 * lane + 1] = static_cast<unsigned short>(word);
+        if (lane == 0) out[0] = static_cast<unsigned short>(w[0]);
+      }
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------------------------- the kernel
@@ -345,6 +428,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
   uint64_t* drain = tempty + 2;           // used only when giving up
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  uint32_t* stage = reinterpret_cast<uint32_t*>(smem + STAGES * STAGE_BYTES + 256);     // one buffer to an epilogue warp
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_rank();
@@ -500,6 +584,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
       const long long row = static_cast<long long>(t.m_blk) * TILE_M + rank * CTA_M + q * 32 + lane;
       const bool in = row < d.M;
       const int c0 = t.n_blk * OUT_N + half * HALF_N;
+      Kept<F32, GATED> kept;
+      constexpr bool LOADS = MODE == BACKWARD_GATED || MODE == BACKWARD_ACT;
+      if (LOADS && !F32 && in && c0 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, c0));
       const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * HALF_N;
       if (F32) {
         // All parts of the sum but the last are added up in registers (a gated tile's two halves lie 128 columns
@@ -536,71 +623,61 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
         }
         if (!live) break;
       }
+      if (LOADS && F32 && in && c0 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, c0));
       const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
       if (!ptx::mbar_wait(&tfull[acc], aph, abort_flag)) break;
       ptx::tc_fence_after();
       const uint32_t t_row = t_quarter + acc * TILE_N;
+      if (MODE == PLAIN) {
+        uint32_t* buf = stage + (warp - 2) * STAGE_WORDS;
+        const long long row0 = row - lane;
+        const int rows = d.M - row0 >= 32 ? 32 : static_cast<int>(d.M - row0);      // (may be negative)
 #pragma unroll 1
-      for (int c = 0; c < CHUNKS; ++c) {
-        const int n0 = c0 + c * 16;
-        if (n0 >= d.N) break;
-        const long long at = row * p.hid.ldm + n0;
-        float v[16];
-        if (MODE == PLAIN) {
+        for (int c = 0; c < CHUNKS; ++c) {
+          const int n0 = c0 + c * 16;
+          if (n0 >= d.N) break;
+          float v[16];
           ptx::tmem_ld16(t_row + c * 16, v);
           ptx::tmem_ld_wait();
           if (d.bias) add_bias<F32>(d.bias, n0, d.N, v);
-          if (in) store16_user<F32>(d.C, row * d.ldc + n0, d.N - n0, v);
-        } else if (MODE == FORWARD_GATED) {
-          float w[16];
-          ptx::tmem_ld16(t_row + c * 16, v);
-          ptx::tmem_ld16(t_row + TILE_N / 2 + c * 16, w);
-          ptx::tmem_ld_wait();
-          if (in) {
-            if (p.hid.hi) keep16<F32, true>(p.hid, at, v, w);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = v[i] * sigmoid_of<F32>(v[i]) * w[i];
-            store16_planes<F32>(p.hid.H + at, p.hid.plane_stride, v);
-          }
-        } else if (MODE == FORWARD_ACT) {
-          ptx::tmem_ld16(t_row + c * 16, v);
-          ptx::tmem_ld_wait();
-          if (d.bias) add_bias<F32>(d.bias, n0, d.N, v);
-          if (in) {
-            if (p.hid.hi) keep16<F32, false>(p.hid, at, v, nullptr);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float slope;
-              gelu_and_slope<F32>(v[i], p.act, &v[i], &slope);
+          if (!d.ragged) {
+            if (in) store16_user<F32>(d.C, row * d.ldc + n0, d.N - n0, v);
+          } else {
+            constexpr int SPAN = SPAN_COLS<F32>;
+            const int col = (c * 16) % SPAN;
+            stage16<F32>(buf, lane, col, v);
+            if (col + 16 == SPAN || n0 + 16 >= d.N) {
+              __syncwarp();
+              const int n = n0 - col, valid = d.N - n < SPAN ? d.N - n : SPAN;
+              write_staged<F32>(buf, lane, d.C, d.ldc, row0, rows, n, valid);
+              __syncwarp();
             }
-            store16_planes<F32>(p.hid.H + at, p.hid.plane_stride, v);
           }
-        } else {
-          Kept<F32, GATED> kept;
-          if (in) kept.load(p.hid, at);
+        }
+      } else if (MODE == FORWARD_GATED || MODE == FORWARD_ACT) {
+        Kept<F32, GATED> none;
+#pragma unroll 1
+        for (int c = 0; c < CHUNKS; ++c) {
+          const int n0 = c0 + c * 16;
+          if (n0 >= d.N) break;
+          float v[16], w[16];
+          ptx::tmem_ld16(t_row + c * 16, v);
+          if (GATED) ptx::tmem_ld16(t_row + TILE_N / 2 + c * 16, w);
+          ptx::tmem_ld_wait();
+          if (in) finish16<MODE, F32>(p.hid, p.act, d.bias, d.N, row, n0, v, w, none);
+        }
+      } else {
+        // what was kept of the next chunk is on its way while this one is computed
+#pragma unroll 2
+        for (int c = 0; c < CHUNKS; ++c) {
+          const int n0 = c0 + c * 16;
+          if (n0 >= d.N) break;
+          const Kept<F32, GATED> now = kept;
+          if (in && c + 1 < CHUNKS && n0 + 16 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, n0 + 16));
+          float v[16], w[16];
           ptx::tmem_ld16(t_row + c * 16, v);
           ptx::tmem_ld_wait();
-          if (in) {
-            float h[16], w[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float g = kept.first(i);
-              if (GATED) {
-                const float up = kept.second(i), s = sigmoid_of<F32>(g), a = g * s;
-                h[i] = a * up;
-                w[i] = v[i] * a;
-                v[i] = v[i] * up * (s * fmaf(g, 1.0f - s, 1.0f));
-              } else {
-                float a, slope;
-                gelu_and_slope<F32>(g, p.act, &a, &slope);
-                h[i] = a;
-                v[i] *= slope;
-              }
-            }
-            store16_planes<F32>(p.hid.H + at, p.hid.plane_stride, h);
-            store16_planes<F32>(p.hid.dG + at, p.hid.plane_stride, v);
-            if (GATED) store16_planes<F32>(p.hid.dU + at, p.hid.plane_stride, w);
-          }
+          if (in) finish16<MODE, F32>(p.hid, p.act, nullptr, d.N, row, n0, v, w, now);
         }
       }
       ptx::tc_fence_before();
@@ -691,6 +768,7 @@ ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Prod
     d.tiles_n = (g.N + out_n - 1) / out_n;
     d.unit0 = static_cast<int>(units);
     d.C = g.C; d.ldc = g.ldc; d.bias = g.bias;
+    d.ragged = (g.ldc * (f32 ? 4 : 2)) % 16 != 0 ? 1 : 0;     // (the tensors themselves do)
     // panel height: the tiles in flight form a block whose two sides carry about the same operand bytes (both 256 wide)
     int best = 1;
     double best_cost = 1e300;

@@ -38,15 +38,17 @@ struct Product {
   const void* bias;      // [N], the layer's type, or nullptr
 };
 
-// What the activation's epilogue reads and writes, all [T, ldm]: what the forward pass keeps (hi, hi2: the upper 16 bits
-// of G or Z and of U; lo: what follows them, see pack20; fp32 layers: hi, hi2 are fp32 and lo is unused) and the bf16
-// planes of H, dG (dZ) and dU.
+// What the activation's epilogue reads and writes: what the forward pass keeps (see Kept in train_gemm.cu; nullptr:
+// nothing) and the bf16 planes of H, dG (dZ) and dU, [T, ldm] each.
 struct Hidden {
-  void *hi, *hi2;
-  unsigned char* lo;
+  void* kept;
   __nv_bfloat16 *H, *dG, *dU;
   long long ldm, plane_stride;
 };
+// Bytes of what is kept: 20 bits of G and U each, 24 of Z, all 32 in fp32 layers; whole blocks of 32 rows.
+inline size_t kept_bytes(long long T, long long ldm, bool gated, bool f32) {
+  return static_cast<size_t>((T + 31) / 32 * 32) * ldm * (f32 ? (gated ? 8 : 4) : (gated ? 5 : 3));
+}
 
 #ifdef __CUDACC__
 // x = x0 + x1 + x2 with bf16 terms; non-finite values stay in x0 alone, and a finite x0 does not round to infinity.
