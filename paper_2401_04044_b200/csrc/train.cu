@@ -165,7 +165,7 @@ int sum_splits(long long rows, int cols) {
 struct TrainLayout {
   long long ldm, ldd;
   size_t saved;
-  size_t H, dG, dU, W1, W1u, W2, X, dY, sums, end;
+  size_t H, dG, dU, W1, W1u, W2, X, dY, sums, parts, parts_bytes, end;
 };
 TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   TrainLayout L;
@@ -188,6 +188,11 @@ TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   L.X = off;  off = up256(off + tokens);
   L.dY = off; off = up256(off + tokens);
   L.sums = off; off = up256(off + 4 * (static_cast<size_t>(sum_splits(T, s.m)) * s.m + static_cast<size_t>(sum_splits(T, s.d)) * s.d));
+  // partials of products that are cut along K: that pays where their outputs are small, and is bounded at 32 MB
+  const size_t a = static_cast<size_t>(T) * (2 * L.ldm > L.ldd ? 2 * L.ldm : L.ldd), b = static_cast<size_t>(L.ldm) * L.ldd;
+  const size_t want = 64 * (a > b ? a : b);
+  L.parts_bytes = up256(want < (32u << 20) ? want : (32u << 20));
+  L.parts = off; off += L.parts_bytes;
   L.end = off;
   return L;
 }
@@ -290,10 +295,10 @@ ffsplit_status run_train_forward(ffsplit_ctx* ctx, const ffsplit_shape& s, const
   ffsplit_status r;
   if ((r = p.prepare()) != FFSPLIT_OK) return r;
   const tg::Hidden h = p.buffers(saved);
-  if ((r = tg::launch(ctx, p.gated() ? tg::FORWARD_GATED : tg::FORWARD_ACT, s.act, p.f32(), &g, 1, h, st)) != FFSPLIT_OK) return r;
+  if ((r = tg::launch(ctx, p.gated() ? tg::FORWARD_GATED : tg::FORWARD_ACT, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st)) != FFSPLIT_OK) return r;
   g = product(p.hidden(p.L.H), 0, w2, 1, T, d, m);
   g.C = Y; g.ldc = d; g.bias = w.b2;
-  return tg::launch(ctx, tg::PLAIN, s.act, p.f32(), &g, 1, h, st);
+  return tg::launch(ctx, tg::PLAIN, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st);
 }
 
 ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, const ffsplit_weights& w, const void* X, long long T,
@@ -308,33 +313,32 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
   ffsplit_status r;
   if (inner) {
     const tg::Matrix dy = p.tensor(dY, T, d, p.L.ldd, p.L.dY), w2 = p.tensor(w.W2, m, d, p.L.ldd, p.L.W2);
-    if (grads.dX) {
-      tg::Product& g = out[n++] = product(dG, 0, p.tensor(w.W1, d, m, p.L.ldm, p.L.W1), 0, T, d, m);
+    {
+      tg::Product& g = out[n++] = product(dG, 0, grads.dX ? p.tensor(w.W1, d, m, p.L.ldm, p.L.W1) : tg::Matrix{}, 0, T, d, m);
       if (p.gated()) {
         g.pairs = 2;
         g.a[1] = dU;
-        g.b[1] = p.tensor(w.W1u, d, m, p.L.ldm, p.L.W1u);
+        if (grads.dX) g.b[1] = p.tensor(w.W1u, d, m, p.L.ldm, p.L.W1u);
       }
       g.C = grads.dX; g.ldc = d;
     }
-    tg::Matrix x;
-    if (grads.dW1 || grads.dW1u) x = p.tensor(X, T, d, p.L.ldd, p.L.X);
-    if (grads.dW1) {
+    const tg::Matrix x = grads.dW1 || grads.dW1u ? p.tensor(X, T, d, p.L.ldd, p.L.X) : tg::Matrix{};
+    {
       tg::Product& g = out[n++] = product(x, 1, dG, 1, d, m, T);
       g.C = grads.dW1; g.ldc = m;
     }
-    if (grads.dW1u) {
+    if (p.gated()) {
       tg::Product& g = out[n++] = product(x, 1, dU, 1, d, m, T);
       g.C = grads.dW1u; g.ldc = m;
     }
-    if (grads.dW2) {
+    {
       tg::Product& g = out[n++] = product(H, 1, dy, 1, m, d, T);
       g.C = grads.dW2; g.ldc = d;
     }
     if ((r = p.prepare()) != FFSPLIT_OK) return r;
     const tg::Product g = product(dy, 0, w2, 0, T, m, d);
-    if ((r = tg::launch(ctx, p.gated() ? tg::BACKWARD_GATED : tg::BACKWARD_ACT, s.act, p.f32(), &g, 1, h, st)) != FFSPLIT_OK) return r;
-    if (n > 0 && (r = tg::launch(ctx, tg::PLAIN, s.act, p.f32(), out, n, h, st)) != FFSPLIT_OK) return r;
+    if ((r = tg::launch(ctx, p.gated() ? tg::BACKWARD_GATED : tg::BACKWARD_ACT, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st)) != FFSPLIT_OK) return r;
+    if ((grads.dX || grads.dW1 || grads.dW1u || grads.dW2) && (r = tg::launch(ctx, tg::PLAIN, s.act, p.f32(), out, n, h, p.ws + p.L.parts, p.L.parts_bytes, st)) != FFSPLIT_OK) return r;
   }
   if (grads.db1 || grads.db2) {
     train::SumArgs a;

@@ -20,6 +20,10 @@
 // every PROMOTE k-blocks of the largest product and added up in registers; the five small products before it (2^-8 of
 // the sum and less) need no such care.
 //
+// Few tiles, long sums (few tokens, small layers): a tile's K range is cut into `split` units that leave fp32 partials, and
+// a second launch (join_kernel) adds them in order and does what the epilogue would have done; or the tile is halved to
+// 256 x 128.  plan() weighs both.
+//
 // Warp roles: 0 TMA producer (both CTAs), 1 MMA issuer (rank 0), 2-9 epilogue (four lane quarters x two column halves).
 // Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
 #include <cstring>
@@ -39,23 +43,29 @@ constexpr int BLOCK64_BYTES = 64 * BLOCK_K * 2;      // 64 x 64 elements: MN-maj
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 32 * (EPI_WARPS + 2);
 constexpr int TMEM_COLS = 512;
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 256 + EPI_WARPS * 32 * 33 * 4 + 1024;
+constexpr int OUT_BYTES = 4096;                       // output staging of one epilogue warp: 32 rows x 128 bytes
+constexpr int BAR_BYTES = 256;
+constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES + BAR_BYTES + 1024;
 static_assert(SMEM_BYTES <= 232448, "shared memory of one CTA");
 constexpr int MAX_PRODUCTS = 4;
 constexpr int PROMOTE = 2;   // k-blocks: 8 MMAs, 2.5e-7
 
 struct Unit {
   int prod, m_blk, n_blk;
+  int split, k0, k1;     // k-blocks [k0, k1), counted over all runs
 };
 
 struct DevProduct {
-  CUtensorMap a[2], b[2];
+  CUtensorMap a[2], b[2], c;
   long long M;
   int N, kb;             // k-blocks per run
   int runs, pairs;       // runs over K: pairs x (1, or the 6 products of planes)
   int a_mn, b_mn;
   int tiles_m, tiles_n, panel_m;
   int unit0;             // first unit of this product
+  int splits, per;       // ranges of K, and k-blocks in each (the last one may be shorter)
+  float* partial;        // splits > 1: [splits][M][ldp] fp32; the gated forward pass keeps U at column ldp / 2
+  long long ldp;
   void* C;
   long long ldc;
   const void* bias;
@@ -65,7 +75,8 @@ struct DevProduct {
 struct Params {
   DevProduct prod[MAX_PRODUCTS];
   int n_prod;
-  int units;             // tiles of all products, the products with the longer runs first
+  int tile_n;            // accumulator columns of a tile, 256 or 128
+  int units;             // work units of all products, the products with the longer runs first
   // Units are dealt to the clusters in turn.  The first `heavy` ones (the product with the longest tiles) may leave the
   // clusters from `short_from` on one tile short: `extra` of the following units go to those clusters first.
   int heavy, short_from, extra;
@@ -112,7 +123,11 @@ __device__ __forceinline__ Unit find_unit(const Params& p, int u) {
   r.prod = 0;
   while (r.prod + 1 < p.n_prod && u >= p.prod[r.prod + 1].unit0) ++r.prod;
   const DevProduct& d = p.prod[r.prod];
-  const int tile = u - d.unit0;
+  const int tiles = d.tiles_m * d.tiles_n;
+  r.split = (u - d.unit0) / tiles;
+  r.k0 = r.split * d.per;
+  r.k1 = r.k0 + d.per < d.runs * d.kb ? r.k0 + d.per : d.runs * d.kb;
+  const int tile = u - d.unit0 - r.split * tiles;
   const int per_panel = d.panel_m * d.tiles_n;
   const int panel = tile / per_panel, in_panel = tile - panel * per_panel, m0 = panel * d.panel_m;
   const int h = d.tiles_m - m0 < d.panel_m ? d.tiles_m - m0 : d.panel_m;
@@ -135,11 +150,11 @@ __device__ __forceinline__ void run_planes(const DevProduct& d, int run, int* pa
   *pb = (0x001012 >> (4 * combo)) & 0xF;
 }
 
-// fp32 layers: end of the part of a tile's sum that begins at k-block `begin` (counted over all runs).
-__device__ __forceinline__ int part_end(const DevProduct& d, int begin) {
-  const int total = d.runs * d.kb, large = total - d.pairs * d.kb;   // the last `pairs` runs are the largest product
+// fp32 layers: end of the part of a unit's sum that begins at k-block `begin`.
+__device__ __forceinline__ int part_end(const DevProduct& d, const Unit& t, int begin) {
+  const int large = (d.runs - d.pairs) * d.kb;       // the last `pairs` runs are the largest product
   const int end = (begin > large ? begin : large) + PROMOTE;
-  return end < total ? end : total;
+  return end < t.k1 ? end : t.k1;
 }
 
 // ---------------------------------------------------------------------------------------------- number formats
@@ -376,38 +391,52 @@ __device__ __forceinline__ void finish16(const Hidden& h, int act, const void* b
 // Rows that do not start on 16 bytes (m odd, or fp32 widths that are no multiple of 4) leave through shared memory, so
 // that a warp writes along one row at a time: SPAN columns of 32 rows, one word a lane and row.  (One lane to a row wrote
 // two bytes into each of 32 lines per instruction: 88 us for the gradients of a 1000 x 2731 gated layer.)
-constexpr int STAGE_WORDS = 32 * 33;
 template <bool F32> constexpr int SPAN_COLS = F32 ? 32 : 64;
 template <bool F32>
-__device__ __forceinline__ void stage16(uint32_t* buf, int lane, int col, const float* v) {
-  uint32_t* row = buf + lane * 33;
-  if (F32) {
+__device__ __forceinline__ void stage16(uint32_t* buf, int lane, int col, const float* v) {   // word w of row r at w ^ r
+  uint32_t* row = buf + lane * 32;
+  if constexpr (F32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) row[col + i] = __float_as_uint(v[i]);
+    for (int i = 0; i < 16; ++i) row[(col + i) ^ lane] = __float_as_uint(v[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) row[(col >> 1) + i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 8; ++i) row[((col >> 1) + i) ^ lane] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+  }
+}
+// The same for a TMA store with 128-byte swizzle: 16-byte piece j of row r at j ^ (r % 8).
+template <bool F32>
+__device__ __forceinline__ void stage16_swizzled(uint32_t* buf, int lane, int col, const float* v) {
+  uint4* row = reinterpret_cast<uint4*>(buf) + lane * 8;
+  if constexpr (F32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      row[((col >> 2) + i) ^ (lane & 7)] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      row[((col >> 3) + i) ^ (lane & 7)] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
+                                                      pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
   }
 }
 // The staged columns n .. n + valid - 1 of rows row0 .. of C.
 template <bool F32>
 __device__ __forceinline__ void write_staged(const uint32_t* buf, int lane, void* C, long long ldc, long long row0, int rows, int n, int valid) {
   for (int r = 0; r < rows; ++r) {
-    const uint32_t* w = buf + r * 33;
+    const uint32_t mine = buf[r * 32 + (lane ^ r)], next = buf[r * 32 + (((lane + 1) & 31) ^ r)];
     const long long at = (row0 + r) * ldc + n;
-    if (F32) {
-      if (lane < valid) reinterpret_cast<uint32_t*>(C)[at + lane] = w[lane];
+    if constexpr (F32) {
+      if (lane < valid) static_cast<uint32_t*>(C)[at + lane] = mine;
     } else {
       unsigned short* out = static_cast<unsigned short*>(C) + at;
       if ((reinterpret_cast<uintptr_t>(out) & 3u) == 0) {
-        if (2 * lane + 1 < valid) *reinterpret_cast<uint32_t*>(out + 2 * lane) = w[lane];
-        else if (2 * lane < valid) out[2 * lane] = static_cast<unsigned short>(w[lane]);
+        if (2 * lane + 1 < valid) *reinterpret_cast<uint32_t*>(out + 2 * lane) = mine;
+        else if (2 * lane < valid) out[2 * lane] = static_cast<unsigned short>(mine);
       } else {
         // words start at the odd columns; column 0 is left over, and the last one where valid is even
-        const uint32_t word = w[lane] >> 16 | (lane < 31 ? w[lane + 1] << 16 : 0u);
+        const uint32_t word = mine >> 16 | next << 16;
         if (lane < 31 && 2 * lane + 2 < valid) *reinterpret_cast<uint32_t*>(out + 2 * lane + 1) = word;
         else if (2 * lane + 1 < valid) out[2 * lane + 1] = static_cast<unsigned short>(word);
-        if (lane == 0) out[0] = static_cast<unsigned short>(w[0]);
+        if (lane == 0) out[0] = static_cast<unsigned short>(mine);
       }
     }
   }
@@ -417,10 +446,12 @@ __device__ __forceinline__ void write_staged(const uint32_t* buf, int lane, void
 template <int MODE, bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_gemm_kernel(const __grid_constant__ Params p) {
   constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
-  constexpr int OUT_N = MODE == FORWARD_GATED ? TILE_N / 2 : TILE_N;     // output columns of a tile
+  const int out_n = MODE == FORWARD_GATED ? p.tile_n / 2 : p.tile_n;     // output columns of a tile
+  const int half_n = p.tile_n / 2;                                       // rows of B that one CTA stages
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES);
+  uint8_t* out_stage = smem + STAGES * STAGE_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(out_stage + EPI_WARPS * OUT_BYTES);
   uint64_t* full = bars;                  // [STAGES] TMA of both CTAs -> MMA (rank 0's are used)
   uint64_t* empty = full + STAGES;        // [STAGES] MMA -> TMA, one set in each CTA
   uint64_t* tfull = empty + STAGES;       // [2] MMA -> epilogue, one set in each CTA
@@ -428,7 +459,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
   uint64_t* drain = tempty + 2;           // used only when giving up
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
-  uint32_t* stage = reinterpret_cast<uint32_t*>(smem + STAGES * STAGE_BYTES + 256);     // one buffer to an epilogue warp
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_rank();
@@ -462,23 +492,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
     if (ptx::elect_one()) {
       // ------------------------------------------------------------ TMA producer
       Walk walk;
-      uint32_t it = 0, ph = 0;
+      uint32_t ph = 0;
       int s = 0;
       bool ok = true;
       const uint32_t smem0 = ptx::smem_u32(smem), full0 = ptx::map_to_cta(ptx::smem_u32(full), 0);
+      const uint32_t tx = 2 * (HALF_BYTES + half_n * BLOCK_K * 2);
       for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
         const Unit t = find_unit(p, u);
         const DevProduct& d = p.prod[t.prod];
         const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M;
-        const int n0 = MODE == FORWARD_GATED ? t.n_blk * OUT_N : t.n_blk * OUT_N + static_cast<int>(rank) * CTA_M;
-        for (int run = 0; run < d.runs && ok; ++run) {
+        const int n0 = t.n_blk * out_n + (MODE == FORWARD_GATED ? 0 : static_cast<int>(rank) * half_n);
+        int run = t.k0 / d.kb, kb = t.k0 - run * d.kb;
+        while (run < d.runs && run * d.kb < t.k1 && ok) {
           int pair, pa, pb;
           run_planes<F32>(d, run, &pair, &pa, &pb);
           const CUtensorMap* ta = &d.a[pair];
           const CUtensorMap* tb = &d.b[MODE == FORWARD_GATED ? static_cast<int>(rank) : pair];
-          for (int kb = 0; kb < d.kb; ++kb, ++it) {
+          const int kb_end = t.k1 - run * d.kb < d.kb ? t.k1 - run * d.kb : d.kb;
+          for (; kb < kb_end; ++kb) {
             if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-            if (rank == 0) ptx::mbar_expect_tx(&full[s], 2 * STAGE_BYTES);
+            if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);
             const uint32_t bar = full0 + s * 8;
             const uint32_t da = smem0 + s * STAGE_BYTES, db = da + HALF_BYTES;
             const int k0 = kb * BLOCK_K;
@@ -490,12 +523,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
             }
             if (d.b_mn) {
               ptx::tma_load_3d_pair(tb, db, bar, n0, k0, pb);
-              ptx::tma_load_3d_pair(tb, db + BLOCK64_BYTES, bar, n0 + 64, k0, pb);
+              if (half_n > 64) ptx::tma_load_3d_pair(tb, db + BLOCK64_BYTES, bar, n0 + 64, k0, pb);
             } else {
               ptx::tma_load_3d_pair(tb, db, bar, k0, n0, pb);
             }
             if (++s == STAGES) { s = 0; ph ^= 1u; }
           }
+          ++run;
+          kb = 0;
         }
       }
       // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
@@ -514,7 +549,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
   } else if (warp == 1) {
     if (rank == 0) {
       // ------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
-      const uint32_t idesc0 = ptx::umma_idesc_bf16(TILE_M, TILE_N);
+      const uint32_t idesc0 = ptx::umma_idesc_bf16(TILE_M, p.tile_n);
       Walk walk;
       uint32_t tl = 0, ph = 0;
       int s = 0;
@@ -529,10 +564,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
         const uint64_t b_desc0 = d.b_mn ? ptx::umma_desc_mn128(smem0 + HALF_BYTES, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0 + HALF_BYTES);
         // 16 further along K: 32 bytes inside the swizzled row, or 16 rows of 128 bytes (addresses count 16 bytes)
         const uint32_t a_step = d.a_mn ? 2048 >> 4 : 32 >> 4, b_step = d.b_mn ? 2048 >> 4 : 32 >> 4;
-        const int total = d.runs * d.kb;
-        // fp32: the tile is summed in parts, each through an accumulator of its own
-        for (int begin = 0; begin < total && ok; ++tl) {
-          const int end = F32 ? part_end(d, begin) : total;
+        // fp32: the unit is summed in parts, each through an accumulator of its own
+        for (int begin = t.k0; begin < t.k1 && ok; ++tl) {
+          const int end = F32 ? part_end(d, t, begin) : t.k1;
           const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
           ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aph ^ 1, abort_flag) ? 1 : 0, 0) != 0;
           if (!ok) break;
@@ -572,31 +606,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
     }
   } else {
     // -------------------------------------------------------------- epilogue warps
-    const int q = warp & 3;              // tensor-memory lane quarter
-    const int half = (warp - 2) >> 2;    // column half
-    constexpr int HALF_N = OUT_N / 2, CHUNKS = HALF_N / 16;
+    constexpr bool LOADS = MODE == BACKWARD_GATED || MODE == BACKWARD_ACT;
+    const int q = warp & 3;                             // tensor-memory lane quarter
+    const int cols = out_n / 2;                         // output columns of this warp's half of the tile
+    const int col0 = ((warp - 2) >> 2) * cols;
+    const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + col0;
+    uint32_t* buf = reinterpret_cast<uint32_t*>(out_stage + (warp - 2) * OUT_BYTES);
     Walk walk;
     uint32_t tl = 0;
     bool live = true;
     for (int u = walk.take(p); u >= 0 && live; u = walk.take(p), ++tl) {
       const Unit t = find_unit(p, u);
       const DevProduct& d = p.prod[t.prod];
+      const bool parts = d.splits > 1;                  // this unit leaves a partial
       const long long row = static_cast<long long>(t.m_blk) * TILE_M + rank * CTA_M + q * 32 + lane;
       const bool in = row < d.M;
-      const int c0 = t.n_blk * OUT_N + half * HALF_N;
+      const int c0 = t.n_blk * out_n + col0;
       Kept<F32, GATED> kept;
-      constexpr bool LOADS = MODE == BACKWARD_GATED || MODE == BACKWARD_ACT;
-      if (LOADS && !F32 && in && c0 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, c0));
-      const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * HALF_N;
-      if (F32) {
+      if (LOADS && !F32 && !parts && in && c0 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, c0));
+      if constexpr (F32) {
         // All parts of the sum but the last are added up in registers (a gated tile's two halves lie 128 columns
         // apart); then it goes back to where the last part lies, and on as for bf16.
-        constexpr int BLOCKS = 8, SKIP = MODE == FORWARD_GATED ? TILE_N / 2 - HALF_N : 0;
+        constexpr int BLOCKS = 8, SKIP = MODE == FORWARD_GATED ? TILE_N / 4 : 0;     // (fp32 tiles are 256 wide)
         float sum[BLOCKS][16];
         bool first = true;
-        for (int begin = 0;; ++tl) {
-          const int end = part_end(d, begin);
-          const bool last = end == d.runs * d.kb;
+        for (int begin = t.k0;; ++tl) {
+          const int end = part_end(d, t, begin);
+          const bool last = end == t.k1;
           if (first && last) break;      // one part: nothing to add
           if (!ptx::mbar_wait(&tfull[tl & 1], (tl >> 1) & 1, abort_flag)) { live = false; break; }
           ptx::tc_fence_after();
@@ -622,31 +658,53 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
           begin = end;
         }
         if (!live) break;
+        if (LOADS && !parts && in && c0 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, c0));
       }
-      if (LOADS && F32 && in && c0 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, c0));
       const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
       if (!ptx::mbar_wait(&tfull[acc], aph, abort_flag)) break;
       ptx::tc_fence_after();
       const uint32_t t_row = t_quarter + acc * TILE_N;
-      if (MODE == PLAIN) {
-        uint32_t* buf = stage + (warp - 2) * STAGE_WORDS;
+      const int width = d.N - c0 < cols ? d.N - c0 : cols;       // (may be negative)
+      if (parts) {
+        float* base = d.partial + (t.split * d.M + row) * d.ldp + c0;
+#pragma unroll 1
+        for (int c = 0; c < width; c += 16) {
+          float v[16];
+          ptx::tmem_ld16(t_row + c, v);
+          ptx::tmem_ld_wait();
+          if (in) store16_f32(base + c, v);
+          if (MODE == FORWARD_GATED) {
+            ptx::tmem_ld16(t_row + half_n + c, v);
+            ptx::tmem_ld_wait();
+            if (in) store16_f32(base + d.ldp / 2 + c, v);
+          }
+        }
+      } else if (MODE == PLAIN) {
+        constexpr int SPAN = SPAN_COLS<F32>;
         const long long row0 = row - lane;
         const int rows = d.M - row0 >= 32 ? 32 : static_cast<int>(d.M - row0);      // (may be negative)
 #pragma unroll 1
-        for (int c = 0; c < CHUNKS; ++c) {
-          const int n0 = c0 + c * 16;
-          if (n0 >= d.N) break;
+        for (int c = 0; c < width; c += 16) {
+          const int n0 = c0 + c, col = c % SPAN;
           float v[16];
-          ptx::tmem_ld16(t_row + c * 16, v);
+          ptx::tmem_ld16(t_row + c, v);
           ptx::tmem_ld_wait();
           if (d.bias) add_bias<F32>(d.bias, n0, d.N, v);
           if (!d.ragged) {
-            if (in) store16_user<F32>(d.C, row * d.ldc + n0, d.N - n0, v);
+            if (col == 0) {
+              // the store before must have read the buffer
+              if (lane == 0) ptx::tma_store_wait_read();
+              __syncwarp();
+            }
+            stage16_swizzled<F32>(buf, lane, col, v);
+            if (col + 16 == SPAN || c + 16 >= width) {
+              ptx::fence_proxy_async();
+              __syncwarp();
+              if (lane == 0 && rows > 0) ptx::tma_store_2d(&d.c, ptx::smem_u32(buf), n0 - col, static_cast<int>(row0));
+            }
           } else {
-            constexpr int SPAN = SPAN_COLS<F32>;
-            const int col = (c * 16) % SPAN;
             stage16<F32>(buf, lane, col, v);
-            if (col + 16 == SPAN || n0 + 16 >= d.N) {
+            if (col + 16 == SPAN || c + 16 >= width) {
               __syncwarp();
               const int n = n0 - col, valid = d.N - n < SPAN ? d.N - n : SPAN;
               write_staged<F32>(buf, lane, d.C, d.ldc, row0, rows, n, valid);
@@ -654,36 +712,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
             }
           }
         }
-      } else if (MODE == FORWARD_GATED || MODE == FORWARD_ACT) {
-        Kept<F32, GATED> none;
-#pragma unroll 1
-        for (int c = 0; c < CHUNKS; ++c) {
-          const int n0 = c0 + c * 16;
-          if (n0 >= d.N) break;
-          float v[16], w[16];
-          ptx::tmem_ld16(t_row + c * 16, v);
-          if (GATED) ptx::tmem_ld16(t_row + TILE_N / 2 + c * 16, w);
-          ptx::tmem_ld_wait();
-          if (in) finish16<MODE, F32>(p.hid, p.act, d.bias, d.N, row, n0, v, w, none);
-        }
       } else {
         // what was kept of the next chunk is on its way while this one is computed
 #pragma unroll 2
-        for (int c = 0; c < CHUNKS; ++c) {
-          const int n0 = c0 + c * 16;
-          if (n0 >= d.N) break;
+        for (int c = 0; c < width; c += 16) {
+          const int n0 = c0 + c;
           const Kept<F32, GATED> now = kept;
-          if (in && c + 1 < CHUNKS && n0 + 16 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, n0 + 16));
+          if (LOADS && in && c + 16 < width) kept.load(Kept<F32, GATED>::block(p.hid, row, n0 + 16));
           float v[16], w[16];
-          ptx::tmem_ld16(t_row + c * 16, v);
+          ptx::tmem_ld16(t_row + c, v);
+          if (MODE == FORWARD_GATED) ptx::tmem_ld16(t_row + half_n + c, w);
           ptx::tmem_ld_wait();
-          if (in) finish16<MODE, F32>(p.hid, p.act, nullptr, d.N, row, n0, v, w, now);
+          if (in) finish16<MODE, F32>(p.hid, p.act, d.bias, d.N, row, n0, v, w, now);
         }
       }
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(&tempty[acc]), 0));
     }
+    if (MODE == PLAIN && lane == 0) ptx::tma_store_wait();
   }
 
   ptx::tc_fence_before();
@@ -692,6 +739,61 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc_pair(tmem_base, TMEM_COLS);
+  }
+}
+
+// Adds the partials of every product that was cut along K, in order, and finishes it.  One thread per row and 16 columns.
+struct JoinProduct {
+  const float* partial;
+  long long M, ldp, ldc;
+  int N, chunks, splits;
+  void* C;
+  const void* bias;
+  long long thread0;     // first thread
+};
+struct JoinParams {
+  JoinProduct prod[MAX_PRODUCTS];
+  int n;
+  long long threads;
+  int act;
+  Hidden hid;
+};
+template <int MODE, bool F32>
+__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ JoinParams p) {
+  constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
+  pdl_wait();
+  const long long t = static_cast<long long>(blockIdx.x) * 128 + threadIdx.x;
+  if (t >= p.threads) return;
+  int i = 0;
+  while (i + 1 < p.n && t >= p.prod[i + 1].thread0) ++i;
+  const JoinProduct& d = p.prod[i];
+  const long long row = (t - d.thread0) / d.chunks;
+  const int n0 = static_cast<int>(t - d.thread0 - row * d.chunks) * 16;
+  Kept<F32, GATED> kept;
+  if (MODE == BACKWARD_GATED || MODE == BACKWARD_ACT) kept.load(Kept<F32, GATED>::block(p.hid, row, n0));
+  float v[16] = {}, w[16] = {};
+#pragma unroll 2
+  for (int k = 0; k < d.splits; ++k) {
+    const float4* a = reinterpret_cast<const float4*>(d.partial + (k * d.M + row) * d.ldp + n0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 x = __ldcg(a + j);
+      v[4 * j] += x.x; v[4 * j + 1] += x.y; v[4 * j + 2] += x.z; v[4 * j + 3] += x.w;
+    }
+    if (MODE == FORWARD_GATED) {
+      const float4* b = a + (d.ldp / 2) / 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 x = __ldcg(b + j);
+        w[4 * j] += x.x; w[4 * j + 1] += x.y; w[4 * j + 2] += x.z; w[4 * j + 3] += x.w;
+      }
+    }
+  }
+  if (MODE == PLAIN) {
+    if (d.bias) add_bias<F32>(d.bias, n0, d.N, v);
+    store16_user<F32>(d.C, row * d.ldc + n0, d.N - n0, v);
+  } else {
+    finish16<MODE, F32>(p.hid, p.act, d.bias, d.N, row, n0, v, w, kept);
   }
 }
 
@@ -723,33 +825,127 @@ ffsplit_status encode(ffsplit_ctx* ctx, const Matrix& m, int box_rows, CUtensorM
   return FFSPLIT_OK;
 }
 
+// Row-major output [rows, cols]: tiles of 32 rows x 128 bytes.
+ffsplit_status encode_out(ffsplit_ctx* ctx, bool f32, void* p, long long rows, int cols, long long ld, CUtensorMap* out) {
+  const cuuint64_t es = f32 ? 4 : 2;
+  cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(ld) * es};
+  cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), 32}, estr[2] = {1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_fn)(
+      out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, dims, strides, box, estr,
+      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
+  return FFSPLIT_OK;
+}
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// How a launch is cut: the width of its tiles, and the ranges of K of each product.
+struct Plan {
+  int tile_n;
+  int splits[MAX_PRODUCTS], per[MAX_PRODUCTS];
+  size_t partial_bytes[MAX_PRODUCTS];
+  double cost;
+};
+
+// Estimated time of a plan in microseconds.  A k-block takes 0.27 us in a 256-wide tile (the tensor cores' rate) and
+// 0.17 us in a 128-wide one (shared memory's); where a block's operands come from HBM (few rows), 74 clusters share
+// 6.5 TB/s.  A tile's epilogue, 2.5 us at full width, runs under the next tile; the last one's does not.
+void estimate(Plan* plan, Mode mode, bool f32, const Product* products, int n, int clusters) {
+  const double wide = plan->tile_n / 256.0;
+  double work = 0.0, longest = 0.0, join = 0.0;
+  long long units = 0;
+  for (int i = 0; i < n; ++i) {
+    const Product& g = products[i];
+    const int out_n = mode == FORWARD_GATED ? plan->tile_n / 2 : plan->tile_n;
+    const long long u = ceil_div(g.M, TILE_M) * ceil_div(g.N, out_n) * plan->splits[i];
+    const double rows = static_cast<double>(g.M < TILE_M ? g.M : TILE_M);
+    const double bytes = rows * 128.0 + plan->tile_n * 128.0;      // of one k-block
+    const double from_hbm = g.M <= TILE_M ? bytes / 88e3 : 0.0;    // (larger outputs read their operands from L2 mostly)
+    double block = plan->tile_n == 256 ? 0.27 : 0.17;
+    if (block < from_hbm) block = from_hbm;
+    const double epilogue = 2.5 * wide * (f32 ? 1.5 : 1.0);
+    const double len = plan->per[i] * block;
+    const double unit = len > epilogue ? len : epilogue;
+    work += u * unit;
+    units += u;
+    if (len + epilogue > longest) longest = len + epilogue;
+    if (n == 1) work = static_cast<double>(ceil_div(u, clusters)) * unit * clusters;
+    if (plan->splits[i] > 1) join += 2.0 * plan->partial_bytes[i] / 5e6;
+  }
+  double t = work / clusters + 2.5 * wide;
+  if (t < longest) t = longest;
+  if (join > 0.0) t += join + 3.0;
+  plan->cost = t;
+}
+
+Plan make_plan(Mode mode, bool f32, const Product* products, int n, int clusters, size_t room) {
+  Plan best;
+  best.cost = 1e300;
+  long long total[MAX_PRODUCTS];
+  for (int i = 0; i < n; ++i) total[i] = static_cast<long long>(products[i].pairs) * (f32 ? 6 : 1) * ceil_div(products[i].K, BLOCK_K);
+  for (int tile_n = 256; tile_n >= (f32 ? 256 : 128); tile_n /= 2) {      // (the fp32 epilogue is written for full tiles)
+    // candidates: units of at most `len` k-blocks
+    long long last_len = -1;
+    for (int cut = 1; cut <= 16; ++cut) {
+      long long longest = 0;
+      for (int i = 0; i < n; ++i) longest = total[i] > longest ? total[i] : longest;
+      const long long len = ceil_div(longest, cut);
+      if (len == last_len || (cut > 1 && len < 4)) break;
+      last_len = len;
+      Plan p;
+      p.tile_n = tile_n;
+      size_t bytes = 0;
+      for (int i = 0; i < n; ++i) {
+        const Product& g = products[i];
+        const int s = static_cast<int>(ceil_div(total[i], len));
+        p.per[i] = static_cast<int>(ceil_div(total[i], s));
+        p.splits[i] = static_cast<int>(ceil_div(total[i], p.per[i]));
+        const long long ldp = (mode == FORWARD_GATED ? 2 : 1) * round_up_ll(g.N, 64);
+        p.partial_bytes[i] = p.splits[i] > 1 ? static_cast<size_t>(p.splits[i]) * g.M * ldp * 4 : 0;
+        bytes += p.partial_bytes[i];
+      }
+      if (cut > 1 && bytes > room) break;
+      estimate(&p, mode, f32, products, n, clusters);
+      if (p.cost < best.cost) best = p;
+    }
+  }
+  return best;
+}
+
 template <int MODE, bool F32>
-ffsplit_status launch_mode(ffsplit_ctx* ctx, const Params& p, int clusters, cudaStream_t st) {
+ffsplit_status launch_mode(ffsplit_ctx* ctx, const Params& p, const JoinParams& join, int clusters, cudaStream_t st) {
   // (set on every launch: a host-side lookup, and the attribute belongs to the device, not to the context)
   cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(train_gemm_kernel)");
   e = launch_pdl(train_gemm_kernel<MODE, F32>, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, p);
   ctx->launches++;
-  return check_cuda(ctx, e, "train_gemm_kernel launch");
+  if (e != cudaSuccess || join.n == 0) return check_cuda(ctx, e, "train_gemm_kernel launch");
+  e = launch_pdl(join_kernel<MODE, F32>, dim3(static_cast<unsigned>(ceil_div(join.threads, 128))), dim3(128), 0, st, join);
+  ctx->launches++;
+  return check_cuda(ctx, e, "join_kernel launch");
 }
 
 }  // namespace
 
-ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, cudaStream_t st) {
+ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, char* partials,
+                      size_t partial_room, cudaStream_t st) {
   Params p;
+  JoinParams join;
   std::memset(&p, 0, sizeof(p));
+  std::memset(&join, 0, sizeof(join));
   const int clusters_max = ctx->num_sms / 2;
-  // longest tiles first
-  int order[MAX_PRODUCTS];
-  long long length[MAX_PRODUCTS];
-  const int planes6 = f32 ? 6 : 1;
+  const Plan plan = make_plan(mode, f32, products, n, clusters_max, partial_room);
+  // longest units first
+  int order[MAX_PRODUCTS], wanted = 0;
   for (int i = 0; i < n; ++i) {
-    length[i] = static_cast<long long>(products[i].pairs) * planes6 * ((products[i].K + BLOCK_K - 1) / BLOCK_K);
-    int at = i;
-    for (; at > 0 && length[order[at - 1]] < length[i]; --at) order[at] = order[at - 1];
+    if (mode == PLAIN && !products[i].C) continue;
+    int at = wanted++;
+    for (; at > 0 && plan.per[order[at - 1]] < plan.per[i]; --at) order[at] = order[at - 1];
     order[at] = i;
   }
-  const int out_n = mode == FORWARD_GATED ? TILE_N / 2 : TILE_N;
+  n = wanted;
+  const int out_n = mode == FORWARD_GATED ? plan.tile_n / 2 : plan.tile_n;
+  const int planes6 = f32 ? 6 : 1;
   long long units = 0;
   for (int i = 0; i < n; ++i) {
     const Product& g = products[order[i]];
@@ -759,41 +955,56 @@ ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Prod
     for (int j = 0; j < g.pairs; ++j)
       if ((s = encode(ctx, g.a[j], g.a_mn ? BLOCK_K : CTA_M, &d.a[j])) != FFSPLIT_OK) return s;
     for (int j = 0; j < maps_b; ++j)
-      if ((s = encode(ctx, g.b[j], g.b_mn ? BLOCK_K : CTA_M, &d.b[j])) != FFSPLIT_OK) return s;
+      if ((s = encode(ctx, g.b[j], g.b_mn ? BLOCK_K : plan.tile_n / 2, &d.b[j])) != FFSPLIT_OK) return s;
     d.M = g.M; d.N = g.N;
-    d.kb = static_cast<int>((g.K + BLOCK_K - 1) / BLOCK_K);
+    d.kb = static_cast<int>(ceil_div(g.K, BLOCK_K));
     d.pairs = g.pairs; d.runs = g.pairs * planes6;
     d.a_mn = g.a_mn; d.b_mn = g.b_mn;
-    d.tiles_m = static_cast<int>((g.M + TILE_M - 1) / TILE_M);
-    d.tiles_n = (g.N + out_n - 1) / out_n;
+    d.tiles_m = static_cast<int>(ceil_div(g.M, TILE_M));
+    d.tiles_n = static_cast<int>(ceil_div(g.N, out_n));
     d.unit0 = static_cast<int>(units);
+    d.splits = plan.splits[order[i]];
+    d.per = plan.per[order[i]];
     d.C = g.C; d.ldc = g.ldc; d.bias = g.bias;
-    d.ragged = (g.ldc * (f32 ? 4 : 2)) % 16 != 0 ? 1 : 0;     // (the tensors themselves do)
-    // panel height: the tiles in flight form a block whose two sides carry about the same operand bytes (both 256 wide)
+    d.ragged = (g.ldc * (f32 ? 4 : 2)) % 16 != 0 ? 1 : 0;     // (the tensors themselves start on 16 bytes)
+    if (mode == PLAIN && d.splits == 1 && !d.ragged && (s = encode_out(ctx, f32, g.C, g.M, g.N, g.ldc, &d.c)) != FFSPLIT_OK) return s;
+    if (d.splits > 1) {
+      d.partial = reinterpret_cast<float*>(partials);
+      d.ldp = (mode == FORWARD_GATED ? 2 : 1) * round_up_ll(g.N, 64);
+      partials += plan.partial_bytes[order[i]];
+      JoinProduct& j = join.prod[join.n++];
+      j.partial = d.partial;
+      j.M = g.M; j.ldp = d.ldp; j.ldc = g.ldc; j.N = g.N; j.splits = d.splits;
+      j.chunks = (g.N + 15) / 16;
+      j.C = g.C; j.bias = g.bias;
+      j.thread0 = join.threads;
+      join.threads += g.M * j.chunks;
+    }
+    // panel height: the tiles in flight form a block whose two sides carry about the same operand bytes
     int best = 1;
     double best_cost = 1e300;
     for (int h = 1; h <= d.tiles_m && h <= clusters_max; ++h) {
       const double w = static_cast<double>(clusters_max) / h;
-      const double cost = h + (w < d.tiles_n ? w : d.tiles_n);
+      const double cost = h * 256.0 + (w < d.tiles_n ? w : d.tiles_n) * plan.tile_n;
       if (cost < best_cost - 1e-9) { best_cost = cost; best = h; }
     }
     d.panel_m = best;
-    units += static_cast<long long>(d.tiles_m) * d.tiles_n;
+    units += static_cast<long long>(d.tiles_m) * d.tiles_n * d.splits;
     if (units > 0x3fffffffll) return fail(ctx, FFSPLIT_ERR_SHAPE, "more than 2^30 tiles in one product");
   }
   p.n_prod = n;
+  p.tile_n = plan.tile_n;
   p.units = static_cast<int>(units);
   const int clusters = units < clusters_max ? static_cast<int>(units) : clusters_max;
-  // The product with the longest tiles is dealt first; where its last round does not reach every cluster and shorter
-  // tiles follow, the clusters left out get as many of those as fit into the length of one long tile.
-  p.heavy = 0; p.short_from = 0; p.extra = 0;
-  if (n > 1 && length[order[0]] > length[order[1]]) {
+  // The product with the longest units is dealt first; where its last round does not reach every cluster and shorter
+  // units follow, the clusters left out get as many of those as fit into the length of one long unit.
+  if (n > 1 && p.prod[0].per > p.prod[1].per) {
     p.heavy = p.prod[1].unit0;
     const int left = p.heavy % clusters;
     if (left) {
-      constexpr int EPILOGUE_BLOCKS = 4;    // a tile's set-up and tail, in k-blocks
+      constexpr int EPILOGUE_BLOCKS = 4;    // a unit's set-up and tail, in k-blocks
       p.short_from = left;
-      long long extra = (length[order[0]] + EPILOGUE_BLOCKS) / (length[order[1]] + EPILOGUE_BLOCKS);
+      const long long extra = (p.prod[0].per + EPILOGUE_BLOCKS) / (p.prod[1].per + EPILOGUE_BLOCKS);
       const long long most = (units - p.heavy) / (clusters - left);
       p.extra = static_cast<int>(extra < most ? extra : most);
     }
@@ -801,12 +1012,18 @@ ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Prod
   p.act = act;
   p.hid = hidden;
   p.status = ctx->status();
+  join.act = act;
+  join.hid = hidden;
   switch (mode) {
-    case PLAIN: return f32 ? launch_mode<PLAIN, true>(ctx, p, clusters, st) : launch_mode<PLAIN, false>(ctx, p, clusters, st);
-    case FORWARD_GATED: return f32 ? launch_mode<FORWARD_GATED, true>(ctx, p, clusters, st) : launch_mode<FORWARD_GATED, false>(ctx, p, clusters, st);
-    case FORWARD_ACT: return f32 ? launch_mode<FORWARD_ACT, true>(ctx, p, clusters, st) : launch_mode<FORWARD_ACT, false>(ctx, p, clusters, st);
-    case BACKWARD_GATED: return f32 ? launch_mode<BACKWARD_GATED, true>(ctx, p, clusters, st) : launch_mode<BACKWARD_GATED, false>(ctx, p, clusters, st);
-    default: return f32 ? launch_mode<BACKWARD_ACT, true>(ctx, p, clusters, st) : launch_mode<BACKWARD_ACT, false>(ctx, p, clusters, st);
+    case PLAIN: return f32 ? launch_mode<PLAIN, true>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false>(ctx, p, join, clusters, st);
+    case FORWARD_GATED:
+      return f32 ? launch_mode<FORWARD_GATED, true>(ctx, p, join, clusters, st) : launch_mode<FORWARD_GATED, false>(ctx, p, join, clusters, st);
+    case FORWARD_ACT:
+      return f32 ? launch_mode<FORWARD_ACT, true>(ctx, p, join, clusters, st) : launch_mode<FORWARD_ACT, false>(ctx, p, join, clusters, st);
+    case BACKWARD_GATED:
+      return f32 ? launch_mode<BACKWARD_GATED, true>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_GATED, false>(ctx, p, join, clusters, st);
+    default:
+      return f32 ? launch_mode<BACKWARD_ACT, true>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_ACT, false>(ctx, p, join, clusters, st);
   }
 }
 

@@ -33,7 +33,8 @@ struct Product {
   int a_mn, b_mn;
   long long M, K;
   int N;
-  void* C;               // PLAIN: bf16 or fp32 output
+  void* C;               // PLAIN: bf16 or fp32 output; nullptr: not wanted.  Such a product is not run, but counts when
+                         // the launch is planned: a gradient has the same bits whichever others are asked for
   long long ldc;
   const void* bias;      // [N], the layer's type, or nullptr
 };
@@ -67,8 +68,10 @@ __device__ __forceinline__ void split3(float x, float* o) {
 }
 #endif
 
-// Up to four PLAIN products (or one of the other modes) as one launch.  f32: three-plane operands and fp32 outputs.
-ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, cudaStream_t st);
+// Up to four PLAIN products (or one of the other modes) as one launch, or as two where K is cut.  f32: three-plane
+// operands and fp32 outputs.  partials: scratch for the fp32 partials of products that are cut along K.
+ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, char* partials,
+                      size_t partial_room, cudaStream_t st);
 
 }  // namespace tg
 }  // namespace ffsp
