@@ -75,8 +75,8 @@ __global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_cons
 
 // Bias gradients: out[c] = sum over rows of in[r, c], in fp32 and in a fixed order.  Bound by reading dZ and dY once.  A
 // block sums `rows_per` rows of 256 columns (a warp reads 512 contiguous bytes of every eighth row) and leaves a partial;
-// a second launch adds the partials.  (One block per 64 columns over all rows, without the second launch, had too few
-// loads in flight: 307 us for 4096 rows of 20480 + 5120 columns.)
+// the block that is the last of its columns to arrive (a ticket, zero again afterwards) adds the partials in order.  (One
+// block per 64 columns over all rows had too few loads in flight: 307 us for 4096 rows of 20480 + 5120 columns.)
 struct SumJob {
   const void* in;          // `planes` bf16 planes that add up, or (planes = 0) fp32 values
   void* out;               // bf16, or fp32 with f32_out
@@ -87,6 +87,7 @@ struct SumJob {
 struct SumArgs {
   SumJob job[2];
   int n;
+  int* tickets;            // one to a block of columns of either job
 };
 constexpr int SUM_COLS = 256;
 // Eight columns of one row: 8 lane + (0 .. 7) of bf16 planes, lane + 32 (0 .. 7) of fp32 values (whose rows may start
@@ -127,22 +128,28 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__
   for (int i = 0; i < 8; ++i) red[w][j.planes == 0 ? lane + 32 * i : lane * 8 + i] = s[i];
   __syncthreads();
   const int c = threadIdx.x;
-  if (c0 + c < j.cols) {
-    float t = red[0][c];
-    for (int k = 1; k < 8; ++k) t += red[k][c];
-    j.partial[static_cast<long long>(split) * j.cols + c0 + c] = t;
-  }
-}
-__global__ void __launch_bounds__(256) column_sum_finish_kernel(const __grid_constant__ SumArgs a) {
-  pdl_wait();
-  const SumJob& j = a.job[blockIdx.y];
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= j.cols) return;
-  float t = 0.f;
+  float t = red[0][c];
+  for (int k = 1; k < 8; ++k) t += red[k][c];
+  if (j.splits > 1) {
+    if (c0 + c < j.cols) j.partial[static_cast<long long>(split) * j.cols + c0 + c] = t;
+    __threadfence();
+    __syncthreads();
+    __shared__ int last;
+    int* ticket = a.tickets + (&j == &a.job[1] ? a.job[0].col_blocks : 0) + c0 / SUM_COLS;
+    if (c == 0) {
+      last = atomicAdd(ticket, 1) == j.splits - 1 ? 1 : 0;
+      if (last) *ticket = 0;
+    }
+    __syncthreads();
+    if (!last || c0 + c >= j.cols) return;
+    __threadfence();
+    t = 0.f;
 #pragma unroll 8
-  for (int k = 0; k < j.splits; ++k) t += __ldcg(j.partial + static_cast<long long>(k) * j.cols + c);
-  if (j.f32_out) static_cast<float*>(j.out)[c] = t;
-  else static_cast<__nv_bfloat16*>(j.out)[c] = __float2bfloat16_rn(t);
+    for (int k = 0; k < j.splits; ++k) t += __ldcg(j.partial + static_cast<long long>(k) * j.cols + c0 + c);
+  }
+  if (c0 + c >= j.cols) return;
+  if (j.f32_out) static_cast<float*>(j.out)[c0 + c] = t;
+  else static_cast<__nv_bfloat16*>(j.out)[c0 + c] = __float2bfloat16_rn(t);
 }
 
 }  // namespace train
@@ -343,7 +350,7 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
   if (grads.db1 || grads.db2) {
     train::SumArgs a;
     std::memset(&a, 0, sizeof(a));
-    int blocks = 0, cols = 0;
+    int blocks = 0;
     float* partial = reinterpret_cast<float*>(p.ws + p.L.sums);
     const auto add = [&](const void* in, void* to, long long ld, long long plane_stride, int n_cols, int planes) {
       train::SumJob& j = a.job[a.n++];
@@ -356,16 +363,13 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
       j.block0 = blocks;
       blocks += j.splits * j.col_blocks;
       partial += static_cast<size_t>(j.splits) * n_cols;
-      cols = cols > n_cols ? cols : n_cols;
     };
     if (grads.db1) add(h.dG, grads.db1, p.L.ldm, T * p.L.ldm, m, p.f32() ? 3 : 1);
     if (grads.db2) add(dY, grads.db2, d, 0, d, p.f32() ? 0 : 1);
-    cudaError_t e = launch_pdl(train::column_sum_kernel, dim3(blocks), dim3(256), 0, st, a);
+    a.tickets = ctx->tickets();     // (columns are only cut along the rows where there are fewer blocks of them than tickets)
+    const cudaError_t e = launch_pdl(train::column_sum_kernel, dim3(blocks), dim3(256), 0, st, a);
     ctx->launches++;
-    if (e != cudaSuccess) return check_cuda(ctx, e, "column_sum_kernel launch");
-    e = launch_pdl(train::column_sum_finish_kernel, dim3((cols + 255) / 256, a.n), dim3(256), 0, st, a);
-    ctx->launches++;
-    return check_cuda(ctx, e, "column_sum_finish_kernel launch");
+    return check_cuda(ctx, e, "column_sum_kernel launch");
   }
   return FFSPLIT_OK;
 }

@@ -61,6 +61,7 @@ struct DevProduct {
   int N, kb;             // k-blocks per run
   int runs, pairs;       // runs over K: pairs x (1, or the 6 products of planes)
   int a_mn, b_mn;
+  int a_rows;            // rows of A that a CTA's box holds: 128, or (K-major, one tile) what M needs
   int tiles_m, tiles_n, panel_m;
   int unit0;             // first unit of this product
   int splits, per;       // ranges of K, and k-blocks in each (the last one may be shorter)
@@ -157,72 +158,98 @@ __device__ __forceinline__ int part_end(const DevProduct& d, const Unit& t, int 
   return end < t.k1 ? end : t.k1;
 }
 
-// ---------------------------------------------------------------------------------------------- number formats
-// What is kept of G (Z) and U between forward and backward.  Their own rounding would be a third one on the way to dX
-// and dW1 besides those of dG and of the result; with four more bits it is not seen (2^-13).  Gated: 16 + 4 bits each, the
-// two nibbles in one byte (5 bytes a pair); ungated: 16 + 8 bits (3 bytes).  Rounded half up in magnitude, except that
-// infinities and NaN are cut (their low bits are not needed).
-__device__ __forceinline__ uint32_t round_bits(float v, uint32_t half) {
-  const uint32_t b = __float_as_uint(v);
-  return (b & 0x7f800000u) == 0x7f800000u ? b : b + half;
+// ---------------------------------------------------------------------------------------------- activations
+// Values go through in pairs (the packed fp32 instructions of sm_100): the epilogue of a 256 x 256 tile has 32768 values
+// per SM, and at one instruction issued per clock and scheduler every instruction per value costs 0.14 us.  bf16 layers
+// use the hardware's exponential and reciprocal (a few 2^-22, far below bf16's 2^-9), fp32 layers the library functions.
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 ex2(float2 x) {
+  float2 r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(x.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(x.y));
+  return r;
 }
-template <bool F32>
-__device__ __forceinline__ float sigmoid_of(float z) {
-  // one reciprocal and one exponential either way; the fast forms are good to a few 2^-22, far below bf16's 2^-9
-  return F32 ? 1.0f / (1.0f + expf(-z)) : __fdividef(1.0f, 1.0f + __expf(-z));
+__device__ __forceinline__ float2 rcp(float2 x) {
+  float2 r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(x.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(x.y));
+  return r;
 }
-// GELU and its slope; both from the same exponential (tanh u = 1 - 2 / (1 + exp(2 u)); Phi from erfc).
+// 1 / (1 + exp(-z))
 template <bool F32>
-__device__ __forceinline__ void gelu_and_slope(float z, int act, float* value, float* slope) {
-  if (act == FFSPLIT_GELU_ERF) {
-    float below;
-    const float density = 0.3989422804014327f * (F32 ? expf(-0.5f * z * z) : __expf(-0.5f * z * z));
-    if (F32) {
-      below = 0.5f * erfcf(-0.70710678118654752f * z);
-    } else {
-      // Abramowitz and Stegun 7.1.26 (1.5e-7 absolute) on the exponential that the density needs anyway
-      const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
-      float q = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
-      q = fmaf(q, t, 0.5f * 1.421413741f);
-      q = fmaf(q, t, 0.5f * -0.284496736f);
-      q = fmaf(q, t, 0.5f * 0.254829592f);
-      q *= t * (density * 2.5066282746310002f);
-      below = z >= 0.f ? 1.0f - q : q;
-    }
-    *value = z * below;
-    *slope = fmaf(z, density, below);
+__device__ __forceinline__ float2 sigmoid2(float2 z) {
+  if constexpr (F32) {
+    return make_float2(1.0f / (1.0f + expf(-z.x)), 1.0f / (1.0f + expf(-z.y)));
   } else {
+    return rcp(__fadd2_rn(ex2(__fmul2_rn(z, both(-1.4426950408889634f))), both(1.0f)));
+  }
+}
+// GELU and, where asked for, its slope.
+template <bool F32, bool SLOPE>
+__device__ __forceinline__ void gelu2(float2 z, int act, float2* value, float2* slope) {
+  if (act == FFSPLIT_GELU_ERF) {
+    // z Phi(z), Phi + z phi
+    float2 below, density;
+    if constexpr (F32) {
+      below = make_float2(0.5f * erfcf(-0.70710678118654752f * z.x), 0.5f * erfcf(-0.70710678118654752f * z.y));
+      if (SLOPE) density = make_float2(0.3989422804014327f * expf(-0.5f * z.x * z.x), 0.3989422804014327f * expf(-0.5f * z.y * z.y));
+    } else {
+      // Abramowitz and Stegun 7.1.26 (1.5e-7 absolute) for the tail of Phi, on the exponential that phi needs anyway
+      density = ex2(__fmul2_rn(__fmul2_rn(z, z), both(-0.72134752044448170f)));       // exp(-z^2 / 2)
+      const float2 t = rcp(__ffma2_rn(make_float2(fabsf(z.x), fabsf(z.y)), both(0.3275911f * 0.70710678118654752f), both(1.0f)));
+      float2 q = __ffma2_rn(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+      q = __ffma2_rn(q, t, both(0.5f * 1.421413741f));
+      q = __ffma2_rn(q, t, both(0.5f * -0.284496736f));
+      q = __ffma2_rn(q, t, both(0.5f * 0.254829592f));
+      q = __fmul2_rn(q, __fmul2_rn(t, density));
+      const float2 over = __ffma2_rn(q, both(-1.0f), both(1.0f));
+      below = make_float2(z.x >= 0.f ? over.x : q.x, z.y >= 0.f ? over.y : q.y);
+      if (SLOPE) density = __fmul2_rn(density, both(0.3989422804014327f));
+    }
+    *value = __fmul2_rn(z, below);
+    if (SLOPE) *slope = __ffma2_rn(z, density, below);
+  } else {
+    // tanh form: (1 + tanh u) / 2 = sigmoid(2 u), u = c (z + a z^3)
     const float c = 0.79788456080286536f, a = 0.044715f;
-    const float z2 = z * z;
-    const float s = sigmoid_of<F32>(2.0f * c * z * fmaf(a, z2, 1.0f));     // (1 + tanh u) / 2
-    *value = z * s;
-    *slope = fmaf(z * s * (1.0f - s), 2.0f * c * fmaf(3.0f * a, z2, 1.0f), s);
+    const float2 z2 = __fmul2_rn(z, z);
+    const float2 s = sigmoid2<F32>(__fmul2_rn(z, __ffma2_rn(z2, both(2.0f * c * a), both(2.0f * c))));
+    const float2 v = __fmul2_rn(z, s);
+    *value = v;
+    if (SLOPE) {
+      const float2 rest = __ffma2_rn(s, both(-1.0f), both(1.0f));
+      *slope = __ffma2_rn(__fmul2_rn(v, rest), __ffma2_rn(z2, both(6.0f * c * a), both(2.0f * c)), s);
+    }
   }
 }
 
 // ---------------------------------------------------------------------------------------------- epilogue pieces
-__device__ __forceinline__ void store16_bf16(__nv_bfloat16* base, const float* v) {   // 32-byte aligned
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(base), "r"(pack_bf16x2(v[0], v[1])),
-               "r"(pack_bf16x2(v[2], v[3])), "r"(pack_bf16x2(v[4], v[5])), "r"(pack_bf16x2(v[6], v[7])), "r"(pack_bf16x2(v[8], v[9])),
-               "r"(pack_bf16x2(v[10], v[11])), "r"(pack_bf16x2(v[12], v[13])), "r"(pack_bf16x2(v[14], v[15]))
+__device__ __forceinline__ void store32_bytes(void* base, const uint32_t* w) {   // 32-byte aligned
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(base), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+               "r"(w[5]), "r"(w[6]), "r"(w[7])
                : "memory");
+}
+__device__ __forceinline__ void pack16(const float* v, uint32_t* w) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
 }
 // 16 values into the library's own buffers (pitch a multiple of 64 elements): one bf16 plane, or three.
 template <bool F32>
-__device__ __forceinline__ void store16_planes(__nv_bfloat16* base, long long plane_stride, const float* v) {
-  if constexpr (!F32) {
-    store16_bf16(base, v);
-  } else {
-    float w[3][16];
+__device__ __forceinline__ void store16_planes(__nv_bfloat16* base, long long plane_stride, const float2* v) {
+  uint32_t w[F32 ? 3 : 1][8];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float o[3];
-      split3(v[i], o);
-      w[0][i] = o[0]; w[1][i] = o[1]; w[2][i] = o[2];
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (!F32) {
+      w[0][i] = pack_bf16x2(v[i].x, v[i].y);
+    } else {
+      float o[3], q[3];
+      split3(v[i].x, o);
+      split3(v[i].y, q);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) w[k][i] = pack_bf16x2(o[k], q[k]);
     }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) store16_bf16(base + k * plane_stride, w[k]);
   }
+#pragma unroll
+  for (int k = 0; k < (F32 ? 3 : 1); ++k) store32_bytes(base + k * plane_stride, w[k]);
 }
 __device__ __forceinline__ void store16_f32(float* base, const float* v) {   // 16-byte aligned
 #pragma unroll
@@ -242,7 +269,9 @@ __device__ __forceinline__ void store16_user(void* C, long long at, int valid, c
   } else {
     __nv_bfloat16* base = static_cast<__nv_bfloat16*>(C) + at;
     if (valid >= 16 && (reinterpret_cast<uintptr_t>(base) & 31u) == 0) {
-      store16_bf16(base, v);
+      uint32_t w[8];
+      pack16(v, w);
+      store32_bytes(base, w);
     } else if (valid >= 8 && (reinterpret_cast<uintptr_t>(base) & 15u) == 0) {
       reinterpret_cast<uint4*>(base)[0] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
       if (valid >= 16) {
@@ -281,7 +310,10 @@ __device__ __forceinline__ void add_bias(const void* bias, int n0, int N, float*
   }
 }
 
-// What is kept lies in blocks of 32 rows x 16 columns, which is what a warp of either pass handles at once (a lane to a
+// What is kept of G (Z) and U between forward and backward.  Their own rounding to bf16 would be a third one on the way
+// to dX and dW1 besides those of dG and of the result; with four more bits it is not seen.  Gated: 16 + 4 bits each, the
+// two nibbles in one byte (5 bytes a pair); ungated: 16 + 8 bits (3 bytes).
+// It lies in blocks of 32 rows x 16 columns, which is what a warp of either pass handles at once (a lane to a
 // row): 16-byte pieces, each 512 contiguous bytes of the warp.  (Row by row, every lane's piece was a line of its own.)
 template <bool F32, bool GATED>
 struct Kept {
@@ -307,37 +339,53 @@ struct Kept {
     }
     if (!F32) p[(PIECES - 1) * 32] = lo;
   }
-  __device__ __forceinline__ float value(const uint4* q, int i, bool upper_nibble) const {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
-    if (F32) return __uint_as_float(w[i]);
-    const uint32_t top = (i & 1) ? (w[(i >> 1) & 7] & 0xffff0000u) : (w[(i >> 1) & 7] << 16);
-    const uint32_t byte = reinterpret_cast<const uint32_t*>(&lo)[i >> 2] >> (8 * (i & 3));
-    return __uint_as_float(top | (GATED ? (upper_nibble ? (byte & 0xf0u) << 8 : (byte & 0xfu) << 12) : (byte & 0xffu) << 8));
+  // Values i and i + 1 (i even) of the first or the second of what is kept.  One byte permutation builds a value; the low
+  // byte, which is not kept, repeats the one above it.
+  __device__ __forceinline__ float2 pair(const uint4* q, int i, uint32_t low_bytes) const {
+    const uint32_t w = reinterpret_cast<const uint32_t*>(q)[F32 ? i : i >> 1];
+    if constexpr (F32) {
+      return make_float2(__uint_as_float(w), __uint_as_float(reinterpret_cast<const uint32_t*>(q)[i + 1]));
+    } else {
+      const uint32_t j = 4 + (i & 3), k = j + 1;
+      return make_float2(__uint_as_float(__byte_perm(w, low_bytes, 0x1000 | j << 4 | j)),
+                         __uint_as_float(__byte_perm(w, low_bytes, 0x3200 | k << 4 | k)));
+    }
   }
-  __device__ __forceinline__ float first(int i) const { return value(a, i, false); }
-  __device__ __forceinline__ float second(int i) const { return value(b, i, true); }
-  __device__ __forceinline__ void set(const float* g, const float* u) {
+  __device__ __forceinline__ uint32_t low_word(int i) const { return reinterpret_cast<const uint32_t*>(&lo)[(i >> 2) & 3]; }
+  __device__ __forceinline__ float2 first(int i) const { return pair(a, i, F32 ? 0u : GATED ? low_word(i) & 0xf0f0f0f0u : low_word(i)); }
+  __device__ __forceinline__ float2 second(int i) const { return pair(b, i, F32 ? 0u : low_word(i) << 4 & 0xf0f0f0f0u); }
+  // byte 1 of four words
+  __device__ __forceinline__ static uint32_t second_bytes(const uint32_t* x) {
+    return __byte_perm(__byte_perm(x[0], x[1], 0x0051), __byte_perm(x[2], x[3], 0x0051), 0x5410);
+  }
+  __device__ __forceinline__ void set(const float2* g, const float2* u) {
     uint32_t *wa = reinterpret_cast<uint32_t*>(a), *wb = reinterpret_cast<uint32_t*>(b), *wl = reinterpret_cast<uint32_t*>(&lo);
     if constexpr (F32) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        wa[i] = __float_as_uint(g[i]);
-        if (GATED) wb[i] = __float_as_uint(u[i]);
+      for (int i = 0; i < 8; ++i) {
+        wa[2 * i] = __float_as_uint(g[i].x);
+        wa[2 * i + 1] = __float_as_uint(g[i].y);
+        if (GATED) { wb[2 * i] = __float_as_uint(u[i].x); wb[2 * i + 1] = __float_as_uint(u[i].y); }
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t x = round_bits(g[i], GATED ? 0x800u : 0x80u);
-        uint32_t byte;
-        if (GATED) {
-          const uint32_t y = round_bits(u[i], 0x800u);
-          wb[i >> 1] = (i & 1) ? (wb[i >> 1] | (y & 0xffff0000u)) : (y >> 16);
-          byte = ((x >> 12) & 0xfu) | ((y >> 8) & 0xf0u);
-        } else {
-          byte = (x >> 8) & 0xffu;
+      for (int i = 0; i < 4; ++i) {      // four values at a time
+        uint32_t x[4], y[4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          // 20 bits are cut, not rounded; the factor 1 + 0.7 2^-12 moves the middle of what is cut off to zero
+          const float2 gx = GATED ? __fmul2_rn(g[2 * i + k], both(1.00017f)) : g[2 * i + k];
+          x[2 * k] = __float_as_uint(gx.x);
+          x[2 * k + 1] = __float_as_uint(gx.y);
+          wa[2 * i + k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x7632);
+          if (GATED) {
+            const float2 ux = __fmul2_rn(u[2 * i + k], both(1.00017f));
+            y[2 * k] = __float_as_uint(ux.x);
+            y[2 * k + 1] = __float_as_uint(ux.y);
+            wb[2 * i + k] = __byte_perm(y[2 * k], y[2 * k + 1], 0x7632);
+          }
         }
-        wa[i >> 1] = (i & 1) ? (wa[i >> 1] | (x & 0xffff0000u)) : (x >> 16);
-        wl[i >> 2] = (i & 3) ? (wl[i >> 2] | byte << (8 * (i & 3))) : byte;
+        wl[i] = GATED ? (second_bytes(x) & 0xf0f0f0f0u) | (second_bytes(y) >> 4 & 0x0f0f0f0fu) : second_bytes(x);
       }
     }
   }
@@ -349,42 +397,45 @@ __device__ __forceinline__ void finish16(const Hidden& h, int act, const void* b
                                          const Kept<F32, MODE == FORWARD_GATED || MODE == BACKWARD_GATED>& loaded) {
   constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
   const long long at = row * h.ldm + n0;
+  float2 x[8], y[8];
+  if (MODE == FORWARD_ACT && bias) add_bias<F32>(bias, n0, N, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] = make_float2(v[2 * i], v[2 * i + 1]);
+    if (MODE == FORWARD_GATED) y[i] = make_float2(w[2 * i], w[2 * i + 1]);
+  }
   if (MODE == FORWARD_GATED || MODE == FORWARD_ACT) {
-    if (MODE == FORWARD_ACT && bias) add_bias<F32>(bias, n0, N, v);
     if (h.kept) {
       Kept<F32, GATED> k;
-      k.set(v, w);
+      k.set(x, y);
       k.store(Kept<F32, GATED>::block(h, row, n0));
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (GATED) {
-        v[i] = v[i] * sigmoid_of<F32>(v[i]) * w[i];
-      } else {
-        float slope;
-        gelu_and_slope<F32>(v[i], act, &v[i], &slope);
-      }
+    for (int i = 0; i < 8; ++i) {
+      if (GATED) x[i] = __fmul2_rn(__fmul2_rn(x[i], sigmoid2<F32>(x[i])), y[i]);
+      else gelu2<F32, false>(x[i], act, &x[i], nullptr);
     }
-    store16_planes<F32>(h.H + at, h.plane_stride, v);
+    store16_planes<F32>(h.H + at, h.plane_stride, x);
   } else {
-    float hid[16];
+    float2 hid[8];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float g = loaded.first(i);
+    for (int i = 0; i < 8; ++i) {
+      const float2 g = loaded.first(2 * i);
       if (GATED) {
-        const float up = loaded.second(i), s = sigmoid_of<F32>(g), a = g * s;
-        hid[i] = a * up;
-        w[i] = v[i] * a;
-        v[i] = v[i] * up * (s * fmaf(g, 1.0f - s, 1.0f));
+        const float2 up = loaded.second(2 * i), s = sigmoid2<F32>(g), a = __fmul2_rn(g, s);
+        const float2 rest = __ffma2_rn(s, both(-1.0f), both(1.0f));
+        hid[i] = __fmul2_rn(a, up);
+        y[i] = __fmul2_rn(x[i], a);
+        x[i] = __fmul2_rn(__fmul2_rn(x[i], up), __fmul2_rn(s, __ffma2_rn(g, rest, both(1.0f))));
       } else {
-        float slope;
-        gelu_and_slope<F32>(g, act, &hid[i], &slope);
-        v[i] *= slope;
+        float2 slope;
+        gelu2<F32, true>(g, act, &hid[i], &slope);
+        x[i] = __fmul2_rn(x[i], slope);
       }
     }
     store16_planes<F32>(h.H + at, h.plane_stride, hid);
-    store16_planes<F32>(h.dG + at, h.plane_stride, v);
-    if (GATED) store16_planes<F32>(h.dU + at, h.plane_stride, w);
+    store16_planes<F32>(h.dG + at, h.plane_stride, x);
+    if (GATED) store16_planes<F32>(h.dU + at, h.plane_stride, y);
   }
 }
 
@@ -496,11 +547,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
       int s = 0;
       bool ok = true;
       const uint32_t smem0 = ptx::smem_u32(smem), full0 = ptx::map_to_cta(ptx::smem_u32(full), 0);
-      const uint32_t tx = 2 * (HALF_BYTES + half_n * BLOCK_K * 2);
       for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
         const Unit t = find_unit(p, u);
         const DevProduct& d = p.prod[t.prod];
         const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M;
+        // Few rows: what the box leaves out, and all of rank 1's half where M <= 128, is not staged at all.  Whatever lies
+        // in shared memory there only reaches accumulator rows behind M.  (One token: the empty rows cost as much of the
+        // copy engine as real ones, and the weights wait behind them.)
+        const bool load_a = rank == 0 || d.M > CTA_M;
+        const uint32_t tx = (d.M > CTA_M ? 2 : 1) * d.a_rows * BLOCK_K * 2 + 2 * half_n * BLOCK_K * 2;
         const int n0 = t.n_blk * out_n + (MODE == FORWARD_GATED ? 0 : static_cast<int>(rank) * half_n);
         int run = t.k0 / d.kb, kb = t.k0 - run * d.kb;
         while (run < d.runs && run * d.kb < t.k1 && ok) {
@@ -516,9 +571,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
             const uint32_t da = smem0 + s * STAGE_BYTES, db = da + HALF_BYTES;
             const int k0 = kb * BLOCK_K;
             if (d.a_mn) {
-              ptx::tma_load_3d_pair(ta, da, bar, m0, k0, pa);
-              ptx::tma_load_3d_pair(ta, da + BLOCK64_BYTES, bar, m0 + 64, k0, pa);
-            } else {
+              if (load_a) {
+                ptx::tma_load_3d_pair(ta, da, bar, m0, k0, pa);
+                if (d.a_rows > 64) ptx::tma_load_3d_pair(ta, da + BLOCK64_BYTES, bar, m0 + 64, k0, pa);
+              }
+            } else if (load_a) {
               ptx::tma_load_3d_pair(ta, da, bar, k0, m0, pa);
             }
             if (d.b_mn) {
@@ -951,9 +1008,10 @@ ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Prod
     const Product& g = products[order[i]];
     DevProduct& d = p.prod[i];
     const int maps_b = mode == FORWARD_GATED ? 2 : g.pairs;
+    d.a_rows = g.M >= CTA_M ? CTA_M : g.a_mn ? (g.M > 64 ? 128 : 64) : static_cast<int>(round_up_ll(g.M, 8));
     ffsplit_status s;
     for (int j = 0; j < g.pairs; ++j)
-      if ((s = encode(ctx, g.a[j], g.a_mn ? BLOCK_K : CTA_M, &d.a[j])) != FFSPLIT_OK) return s;
+      if ((s = encode(ctx, g.a[j], g.a_mn ? BLOCK_K : d.a_rows, &d.a[j])) != FFSPLIT_OK) return s;
     for (int j = 0; j < maps_b; ++j)
       if ((s = encode(ctx, g.b[j], g.b_mn ? BLOCK_K : plan.tile_n / 2, &d.b[j])) != FFSPLIT_OK) return s;
     d.M = g.M; d.N = g.N;
