@@ -26,6 +26,7 @@ GELU_ERF, GELU_TANH, SWIGLU = 0, 1, 2
 SCORE_EQ3, SCORE_ACT_ONLY, SCORE_SUM_NORM = 0, 1, 2
 ACT_IDS = {"gelu_erf": GELU_ERF, "gelu_tanh": GELU_TANH, "swiglu": SWIGLU}
 DTYPE_IDS = {torch.float32: F32, torch.bfloat16: BF16}
+DTYPES = {F32: torch.float32, BF16: torch.bfloat16}
 SCORE_IDS = {"eq3": SCORE_EQ3, "act_only": SCORE_ACT_ONLY, "sum_norm": SCORE_SUM_NORM}
 
 EXPORTS = [
@@ -385,25 +386,26 @@ class Context:
                     "ffsplit_quant_forward")
 
     # ------------------------------------------------------------------ training
-    def _operand(self, where: str, name: str, t, shape: Shape, dims, optional: bool = True):
-        """Pointer of one tensor of a training call, checked against what the layer says it has to be."""
+    # (These calls are made per layer and step, and a small layer takes the GPU no longer than the interpreter takes to
+    # get here: the checks below are written to cost little.)
+    def _operand(self, where: str, name: str, t, dtype, dims, optional: bool = True):
+        """Address of one tensor of a training call, checked against what the layer says it has to be."""
         if t is None:
             if optional:
                 return None
             raise FFSplitError(1, where, f"{name} is missing")
-        if DTYPE_IDS.get(t.dtype) != shape.dtype:
+        if t.dtype is not dtype:
             raise FFSplitError(4, where, f"{name} is {t.dtype}, which is not the layer's type")
-        if tuple(t.shape) != tuple(dims) or not t.is_contiguous():
-            raise FFSplitError(2, where, f"{name} must be contiguous and of shape {tuple(dims)}")
-        if t.device.type != "cuda" or t.device.index != self.device:
+        if t.shape != dims or not t.is_contiguous():
+            raise FFSplitError(2, where, f"{name} must be contiguous and of shape {dims}")
+        if t.get_device() != self.device:
             raise FFSplitError(1, where, f"{name} must be on cuda:{self.device}")
         return t.data_ptr()
 
     def _train_weights(self, where, shape, W1, W1u, b1, W2, b2):
-        d, m, op = shape.d, shape.m, self._operand
-        return Weights(op(where, "W1", W1, shape, (d, m), False), op(where, "W1u", W1u, shape, (d, m)),
-                       op(where, "b1", b1, shape, (m,)), op(where, "W2", W2, shape, (m, d), False),
-                       op(where, "b2", b2, shape, (d,)))
+        d, m, op, dt = shape.d, shape.m, self._operand, DTYPES[shape.dtype]
+        return Weights(op(where, "W1", W1, dt, (d, m), False), op(where, "W1u", W1u, dt, (d, m)), op(where, "b1", b1, dt, (m,)),
+                       op(where, "W2", W2, dt, (m, d), False), op(where, "b2", b2, dt, (d,)))
 
     def train_sizes(self, shape: Shape, T: int):
         """-> (bytes of `saved`, bytes of workspace) that train_forward / train_backward need for T tokens."""
@@ -415,27 +417,26 @@ class Context:
 
     def train_forward(self, shape: Shape, W1, b1, W2, b2, X, Y, saved=None, W1u=None, stream=None):
         """ffsplit_train_forward: Y from the row-major weights; `saved` (a byte tensor) is written for train_backward()."""
-        where, T = "ffsplit_train_forward", X.shape[0]
+        where, T, d, dt = "ffsplit_train_forward", X.shape[0], shape.d, DTYPES[shape.dtype]
         w = self._train_weights(where, shape, W1, W1u, b1, W2, b2)
         rc = self.lib.ffsplit_train_forward(
-            self.h, C.byref(shape), C.byref(w), self._operand(where, "X", X, shape, (T, shape.d), False), T, _ptr(saved),
-            0 if saved is None else saved.numel() * saved.element_size(),
-            self._operand(where, "Y", Y, shape, (T, shape.d), False), _stream_ptr(stream))
-        self._check(rc, where)
+            self.h, shape, w, self._operand(where, "X", X, dt, (T, d), False), T, None if saved is None else saved.data_ptr(),
+            0 if saved is None else saved.nbytes, self._operand(where, "Y", Y, dt, (T, d), False), _stream_ptr(stream))
+        if rc:
+            self._check(rc, where)
 
     def train_backward(self, shape: Shape, W1, b1, W2, X, saved, dY, dX=None, dW1=None, db1=None, dW2=None, db2=None,
                        W1u=None, dW1u=None, stream=None):
         """ffsplit_train_backward: writes the gradients that are given (None: not wanted)."""
-        where, T, d, m, op = "ffsplit_train_backward", X.shape[0], shape.d, shape.m, self._operand
-        w = self._train_weights(where, shape, W1, W1u, b1, W2, None)
-        g = TrainGrads(op(where, "dX", dX, shape, (T, d)), op(where, "dW1", dW1, shape, (d, m)),
-                       op(where, "dW1u", dW1u, shape, (d, m)), op(where, "db1", db1, shape, (m,)),
-                       op(where, "dW2", dW2, shape, (m, d)), op(where, "db2", db2, shape, (d,)))
+        where, T, d, m, op, dt = "ffsplit_train_backward", X.shape[0], shape.d, shape.m, self._operand, DTYPES[shape.dtype]
+        w = self._train_weights(where, shape, W1, W1u, None, W2, None)
+        g = TrainGrads(op(where, "dX", dX, dt, (T, d)), op(where, "dW1", dW1, dt, (d, m)), op(where, "dW1u", dW1u, dt, (d, m)),
+                       op(where, "db1", db1, dt, (m,)), op(where, "dW2", dW2, dt, (m, d)), op(where, "db2", db2, dt, (d,)))
         rc = self.lib.ffsplit_train_backward(
-            self.h, C.byref(shape), C.byref(w), op(where, "X", X, shape, (T, d), False), T, _ptr(saved),
-            0 if saved is None else saved.numel() * saved.element_size(), op(where, "dY", dY, shape, (T, d), False),
-            C.byref(g), _stream_ptr(stream))
-        self._check(rc, where)
+            self.h, shape, w, op(where, "X", X, dt, (T, d), False), T, None if saved is None else saved.data_ptr(),
+            0 if saved is None else saved.nbytes, op(where, "dY", dY, dt, (T, d), False), g, _stream_ptr(stream))
+        if rc:
+            self._check(rc, where)
 
     def grad_list(self, grads, out=None) -> "GradList":
         return GradList(self.device, grads, out)

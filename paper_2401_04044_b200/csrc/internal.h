@@ -211,6 +211,7 @@ struct ffsplit_ctx {
   bool attr_ares_set = false;
   bool attr_layer_set = false;
   bool attr_att_set = false;
+  unsigned attr_train_set = 0;   // one bit to an instance of the training products' kernel
   int* status() const { return reinterpret_cast<int*>(ws); }
   int* tickets() const { return reinterpret_cast<int*>(ws + ffsp::kStatusBytes); }
   int gemm_two_m = 1;          // tensor-core GEMM: 256-row tiles where they pay (FFSPLIT_GEMM_TWO_M=0: never, 2: wherever allowed)

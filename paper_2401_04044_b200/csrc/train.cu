@@ -171,7 +171,7 @@ int sum_splits(long long rows, int cols) {
 // whole chunks that matter nor read (the tensor maps end at m and d).
 struct TrainLayout {
   long long ldm, ldd;
-  size_t saved;
+  size_t savedH, saved;
   size_t H, dG, dU, W1, W1u, W2, X, dY, sums, parts, parts_bytes, end;
 };
 TrainLayout train_layout(const ffsplit_shape& s, long long T) {
@@ -180,10 +180,13 @@ TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   L.ldm = round_up_ll(s.m, 64);
   L.ldd = round_up_ll(s.d, 64);
   const size_t hidden = static_cast<size_t>(T) * L.ldm;
-  L.saved = up256(tg::kept_bytes(T, L.ldm, gated, f32));
   const size_t planes = f32 ? 3 : 1;
+  // H is kept as well: writing it a second time costs the backward pass more than reading it (an SM writes 18 bytes a
+  // nanosecond, and the epilogue of dH is bound by that)
+  L.savedH = up256(tg::kept_bytes(T, L.ldm, gated, f32));
+  L.saved = L.savedH + up256(hidden * 2 * planes);
   size_t off = 0;
-  L.H = off;  off = up256(off + hidden * 2 * planes);
+  L.H = off;                                   // (a forward pass that keeps nothing)
   L.dG = off; off = up256(off + hidden * 2 * planes);
   L.dU = off; off = up256(off + (gated ? hidden * 2 * planes : 0));
   const bool copy_w1 = f32 || s.m % 8 != 0;
@@ -258,13 +261,11 @@ struct Pass {
     prep_blocks += static_cast<int>((rows * j.quads + per - 1) / per);
     return {j.out, rows, cols, ld, j.plane_stride, f32() ? 3 : 1};
   }
-  tg::Matrix hidden(size_t at) const {
-    return {ws + at, T, s.m, L.ldm, T * L.ldm, f32() ? 3 : 1};
-  }
+  tg::Matrix hidden(const void* at) const { return {at, T, s.m, L.ldm, T * L.ldm, f32() ? 3 : 1}; }
   tg::Hidden buffers(char* saved) const {
     tg::Hidden h;
     h.kept = saved;
-    h.H = reinterpret_cast<__nv_bfloat16*>(ws + L.H);
+    h.H = reinterpret_cast<__nv_bfloat16*>(saved ? saved + L.savedH : ws + L.H);
     h.dG = reinterpret_cast<__nv_bfloat16*>(ws + L.dG);
     h.dU = reinterpret_cast<__nv_bfloat16*>(ws + L.dU);
     h.ldm = L.ldm;
@@ -303,7 +304,7 @@ ffsplit_status run_train_forward(ffsplit_ctx* ctx, const ffsplit_shape& s, const
   if ((r = p.prepare()) != FFSPLIT_OK) return r;
   const tg::Hidden h = p.buffers(saved);
   if ((r = tg::launch(ctx, p.gated() ? tg::FORWARD_GATED : tg::FORWARD_ACT, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st)) != FFSPLIT_OK) return r;
-  g = product(p.hidden(p.L.H), 0, w2, 1, T, d, m);
+  g = product(p.hidden(h.H), 0, w2, 1, T, d, m);
   g.C = Y; g.ldc = d; g.bias = w.b2;
   return tg::launch(ctx, tg::PLAIN, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st);
 }
@@ -314,7 +315,7 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
   const int d = s.d, m = s.m;
   const bool inner = grads.dX || grads.dW1 || grads.dW1u || grads.db1 || grads.dW2;   // anything that needs dH or H
   const tg::Hidden h = p.buffers(const_cast<char*>(saved));
-  const tg::Matrix H = p.hidden(p.L.H), dG = p.hidden(p.L.dG), dU = p.hidden(p.L.dU);
+  const tg::Matrix H = p.hidden(h.H), dG = p.hidden(h.dG), dU = p.hidden(h.dU);
   tg::Product out[4];
   int n = 0;
   ffsplit_status r;

@@ -73,8 +73,9 @@ struct DevProduct {
   int ragged;            // rows of C do not all start on 16 bytes
 };
 
+template <int CAP>
 struct Params {
-  DevProduct prod[MAX_PRODUCTS];
+  DevProduct prod[CAP];
   int n_prod;
   int tile_n;            // accumulator columns of a tile, 256 or 128
   int units;             // work units of all products, the products with the longer runs first
@@ -91,7 +92,8 @@ struct Walk {
   int c, C, next, phase, given;
   __device__ __forceinline__ Walk() : c(blockIdx.x >> 1), C(gridDim.x >> 1), next(blockIdx.x >> 1), phase(0), given(0) {}
   // next unit, or -1
-  __device__ __forceinline__ int take(const Params& p) {
+  template <int CAP>
+  __device__ __forceinline__ int take(const Params<CAP>& p) {
     if (phase == 0) {
       if (next < p.heavy) {
         const int u = next;
@@ -119,10 +121,11 @@ struct Walk {
   }
 };
 
-__device__ __forceinline__ Unit find_unit(const Params& p, int u) {
+template <int CAP>
+__device__ __forceinline__ Unit find_unit(const Params<CAP>& p, int u) {
   Unit r;
   r.prod = 0;
-  while (r.prod + 1 < p.n_prod && u >= p.prod[r.prod + 1].unit0) ++r.prod;
+  while (CAP > 1 && r.prod + 1 < p.n_prod && u >= p.prod[r.prod + 1].unit0) ++r.prod;
   const DevProduct& d = p.prod[r.prod];
   const int tiles = d.tiles_m * d.tiles_n;
   r.split = (u - d.unit0) / tiles;
@@ -311,55 +314,83 @@ __device__ __forceinline__ void add_bias(const void* bias, int n0, int N, float*
 }
 
 // What is kept of G (Z) and U between forward and backward.  Their own rounding to bf16 would be a third one on the way
-// to dX and dW1 besides those of dG and of the result; with four more bits it is not seen.  Gated: 16 + 4 bits each, the
-// two nibbles in one byte (5 bytes a pair); ungated: 16 + 8 bits (3 bytes).
-// It lies in blocks of 32 rows x 16 columns, which is what a warp of either pass handles at once (a lane to a
-// row): 16-byte pieces, each 512 contiguous bytes of the warp.  (Row by row, every lane's piece was a line of its own.)
+// to dX and dW1 besides those of dG and of the result; with four more bits it is not seen: 16 + 4 bits each, two values'
+// low nibbles in one byte (G's and U's, or those of the two halves of the 16 values of Z).
+// It lies in blocks of 32 rows x 16 columns, which is what a warp of either pass handles at once (a lane to a row): pieces
+// of 16 bytes a lane (the last 8, for Z), each contiguous over the warp.  (Row by row, every lane's piece was a line of
+// its own.)
 template <bool F32, bool GATED>
 struct Kept {
   static constexpr int Q = F32 ? 4 : 2;                                    // pieces of 16 values of one of G, U, Z
-  static constexpr int PIECES = (GATED ? 2 * Q : Q) + (F32 ? 0 : 1);       // and one for the low bits
-  uint4 a[Q], b[GATED ? Q : 1], lo;
-  __device__ __forceinline__ static uint4* block(const Hidden& h, long long row, int n0) {
-    return static_cast<uint4*>(h.kept) + ((row >> 5) * (h.ldm >> 4) + (n0 >> 4)) * (PIECES * 32) + (row & 31);
+  static constexpr int LOW = F32 ? 0 : GATED ? 16 : 8;                     // bytes of low nibbles
+  static constexpr int BLOCK = 32 * ((GATED ? 2 : 1) * Q * 16 + LOW);
+  uint4 a[Q], b[GATED ? Q : 1];
+  uint32_t lo[4];
+  __device__ __forceinline__ static char* block(const Hidden& h, long long row, int n0) {
+    return static_cast<char*>(h.kept) + ((row >> 5) * (h.ldm >> 4) + (n0 >> 4)) * BLOCK;
   }
-  __device__ __forceinline__ void load(const uint4* p) {
+  __device__ __forceinline__ void load(const Hidden& h, long long row, int n0) {
+    const char* at = block(h, row, n0);
+    const int lane = static_cast<int>(row & 31);
+    const uint4* p = reinterpret_cast<const uint4*>(at) + lane;
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
       a[i] = __ldcs(p + i * 32);
       if (GATED) b[i] = __ldcs(p + (Q + i) * 32);
     }
-    if (!F32) lo = __ldcs(p + (PIECES - 1) * 32);
+    if constexpr (LOW == 16) *reinterpret_cast<uint4*>(lo) = __ldcs(p + 2 * Q * 32);
+    if constexpr (LOW == 8) *reinterpret_cast<uint2*>(lo) = __ldcs(reinterpret_cast<const uint2*>(at + Q * 512) + lane);
   }
-  __device__ __forceinline__ void store(uint4* p) const {
+  __device__ __forceinline__ void store(const Hidden& h, long long row, int n0) const {
+    char* at = block(h, row, n0);
+    const int lane = static_cast<int>(row & 31);
+    uint4* p = reinterpret_cast<uint4*>(at) + lane;
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
       p[i * 32] = a[i];
       if (GATED) p[(Q + i) * 32] = b[i];
     }
-    if (!F32) p[(PIECES - 1) * 32] = lo;
+    if constexpr (LOW == 16) p[2 * Q * 32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    if constexpr (LOW == 8) reinterpret_cast<uint2*>(at + Q * 512)[lane] = make_uint2(lo[0], lo[1]);
   }
   // Values i and i + 1 (i even) of the first or the second of what is kept.  One byte permutation builds a value; the low
   // byte, which is not kept, repeats the one above it.
-  __device__ __forceinline__ float2 pair(const uint4* q, int i, uint32_t low_bytes) const {
-    const uint32_t w = reinterpret_cast<const uint32_t*>(q)[F32 ? i : i >> 1];
+  __device__ __forceinline__ static float2 pair(const uint4* q, int i, uint32_t low_bytes) {
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(q);
     if constexpr (F32) {
-      return make_float2(__uint_as_float(w), __uint_as_float(reinterpret_cast<const uint32_t*>(q)[i + 1]));
+      return make_float2(__uint_as_float(words[i]), __uint_as_float(words[i + 1]));
     } else {
-      const uint32_t j = 4 + (i & 3), k = j + 1;
+      const uint32_t w = words[i >> 1], j = 4 + (i & 3), k = j + 1;
       return make_float2(__uint_as_float(__byte_perm(w, low_bytes, 0x1000 | j << 4 | j)),
                          __uint_as_float(__byte_perm(w, low_bytes, 0x3200 | k << 4 | k)));
     }
   }
-  __device__ __forceinline__ uint32_t low_word(int i) const { return reinterpret_cast<const uint32_t*>(&lo)[(i >> 2) & 3]; }
-  __device__ __forceinline__ float2 first(int i) const { return pair(a, i, F32 ? 0u : GATED ? low_word(i) & 0xf0f0f0f0u : low_word(i)); }
-  __device__ __forceinline__ float2 second(int i) const { return pair(b, i, F32 ? 0u : low_word(i) << 4 & 0xf0f0f0f0u); }
+  __device__ __forceinline__ float2 first(int i) const {
+    if constexpr (F32) return pair(a, i, 0u);
+    if constexpr (GATED) return pair(a, i, lo[i >> 2] & 0xf0f0f0f0u);
+    return pair(a, i, i < 8 ? lo[i >> 2] & 0xf0f0f0f0u : lo[(i >> 2) & 1] << 4 & 0xf0f0f0f0u);
+  }
+  __device__ __forceinline__ float2 second(int i) const { return pair(b, i, F32 ? 0u : lo[i >> 2] << 4 & 0xf0f0f0f0u); }
+
   // byte 1 of four words
   __device__ __forceinline__ static uint32_t second_bytes(const uint32_t* x) {
     return __byte_perm(__byte_perm(x[0], x[1], 0x0051), __byte_perm(x[2], x[3], 0x0051), 0x5410);
   }
+  // Four values: their upper halves to `top`, returns their second bytes.  20 bits are cut, not rounded; the factor
+  // 1 + 0.7 2^-12 moves the middle of what is cut off to zero.
+  __device__ __forceinline__ static uint32_t cut4(const float2* v, uint32_t* top) {
+    uint32_t x[4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float2 s = __fmul2_rn(v[k], both(1.00017f));
+      x[2 * k] = __float_as_uint(s.x);
+      x[2 * k + 1] = __float_as_uint(s.y);
+      top[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x7632);
+    }
+    return second_bytes(x);
+  }
   __device__ __forceinline__ void set(const float2* g, const float2* u) {
-    uint32_t *wa = reinterpret_cast<uint32_t*>(a), *wb = reinterpret_cast<uint32_t*>(b), *wl = reinterpret_cast<uint32_t*>(&lo);
+    uint32_t *wa = reinterpret_cast<uint32_t*>(a), *wb = reinterpret_cast<uint32_t*>(b);
     if constexpr (F32) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -367,26 +398,12 @@ struct Kept {
         wa[2 * i + 1] = __float_as_uint(g[i].y);
         if (GATED) { wb[2 * i] = __float_as_uint(u[i].x); wb[2 * i + 1] = __float_as_uint(u[i].y); }
       }
+    } else if constexpr (GATED) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lo[i] = (cut4(g + 2 * i, wa + 2 * i) & 0xf0f0f0f0u) | (cut4(u + 2 * i, wb + 2 * i) >> 4 & 0x0f0f0f0fu);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {      // four values at a time
-        uint32_t x[4], y[4];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          // 20 bits are cut, not rounded; the factor 1 + 0.7 2^-12 moves the middle of what is cut off to zero
-          const float2 gx = GATED ? __fmul2_rn(g[2 * i + k], both(1.00017f)) : g[2 * i + k];
-          x[2 * k] = __float_as_uint(gx.x);
-          x[2 * k + 1] = __float_as_uint(gx.y);
-          wa[2 * i + k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x7632);
-          if (GATED) {
-            const float2 ux = __fmul2_rn(u[2 * i + k], both(1.00017f));
-            y[2 * k] = __float_as_uint(ux.x);
-            y[2 * k + 1] = __float_as_uint(ux.y);
-            wb[2 * i + k] = __byte_perm(y[2 * k], y[2 * k + 1], 0x7632);
-          }
-        }
-        wl[i] = GATED ? (second_bytes(x) & 0xf0f0f0f0u) | (second_bytes(y) >> 4 & 0x0f0f0f0fu) : second_bytes(x);
-      }
+      for (int i = 0; i < 2; ++i) lo[i] = (cut4(g + 2 * i, wa + 2 * i) & 0xf0f0f0f0u) | (cut4(g + 4 + 2 * i, wa + 4 + 2 * i) >> 4 & 0x0f0f0f0fu);
     }
   }
 };
@@ -408,7 +425,7 @@ __device__ __forceinline__ void finish16(const Hidden& h, int act, const void* b
     if (h.kept) {
       Kept<F32, GATED> k;
       k.set(x, y);
-      k.store(Kept<F32, GATED>::block(h, row, n0));
+      k.store(h, row, n0);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -417,23 +434,20 @@ __device__ __forceinline__ void finish16(const Hidden& h, int act, const void* b
     }
     store16_planes<F32>(h.H + at, h.plane_stride, x);
   } else {
-    float2 hid[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 g = loaded.first(2 * i);
       if (GATED) {
-        const float2 up = loaded.second(2 * i), s = sigmoid2<F32>(g), a = __fmul2_rn(g, s);
+        const float2 up = loaded.second(2 * i), s = sigmoid2<F32>(g);
         const float2 rest = __ffma2_rn(s, both(-1.0f), both(1.0f));
-        hid[i] = __fmul2_rn(a, up);
-        y[i] = __fmul2_rn(x[i], a);
+        y[i] = __fmul2_rn(x[i], __fmul2_rn(g, s));
         x[i] = __fmul2_rn(__fmul2_rn(x[i], up), __fmul2_rn(s, __ffma2_rn(g, rest, both(1.0f))));
       } else {
-        float2 slope;
-        gelu2<F32, true>(g, act, &hid[i], &slope);
+        float2 value, slope;
+        gelu2<F32, true>(g, act, &value, &slope);
         x[i] = __fmul2_rn(x[i], slope);
       }
     }
-    store16_planes<F32>(h.H + at, h.plane_stride, hid);
     store16_planes<F32>(h.dG + at, h.plane_stride, x);
     if (GATED) store16_planes<F32>(h.dU + at, h.plane_stride, y);
   }
@@ -494,8 +508,8 @@ __device__ __forceinline__ void write_staged(const uint32_t* buf, int lane, void
 }
 
 // ---------------------------------------------------------------------------------------------- the kernel
-template <int MODE, bool F32>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_gemm_kernel(const __grid_constant__ Params p) {
+template <int MODE, bool F32, int CAP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_gemm_kernel(const __grid_constant__ Params<CAP> p) {
   constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
   const int out_n = MODE == FORWARD_GATED ? p.tile_n / 2 : p.tile_n;     // output columns of a tile
   const int half_n = p.tile_n / 2;                                       // rows of B that one CTA stages
@@ -526,6 +540,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
     ptx::mbar_init(drain, 1);
     *abort_flag = 0;
     ptx::mbar_fence_init();
+  }
+  if (warp == 2 && lane < 2) {
+    ptx::prefetch_tmap(&p.prod[0].a[0]);
+    ptx::prefetch_tmap(&p.prod[0].b[MODE == FORWARD_GATED ? lane : 0]);
   }
   if (warp == 1) {
     ptx::tmem_alloc_pair(tmem_holder, TMEM_COLS);
@@ -680,7 +698,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
       const bool in = row < d.M;
       const int c0 = t.n_blk * out_n + col0;
       Kept<F32, GATED> kept;
-      if (LOADS && !F32 && !parts && in && c0 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, c0));
+      if (LOADS && !F32 && !parts && in && c0 < d.N) kept.load(p.hid, row, c0);
       if constexpr (F32) {
         // All parts of the sum but the last are added up in registers (a gated tile's two halves lie 128 columns
         // apart); then it goes back to where the last part lies, and on as for bf16.
@@ -715,7 +733,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
           begin = end;
         }
         if (!live) break;
-        if (LOADS && !parts && in && c0 < d.N) kept.load(Kept<F32, GATED>::block(p.hid, row, c0));
+        if (LOADS && !parts && in && c0 < d.N) kept.load(p.hid, row, c0);
       }
       const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
       if (!ptx::mbar_wait(&tfull[acc], aph, abort_flag)) break;
@@ -775,7 +793,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
         for (int c = 0; c < width; c += 16) {
           const int n0 = c0 + c;
           const Kept<F32, GATED> now = kept;
-          if (LOADS && in && c + 16 < width) kept.load(Kept<F32, GATED>::block(p.hid, row, n0 + 16));
+          if (LOADS && in && c + 16 < width) kept.load(p.hid, row, n0 + 16);
           float v[16], w[16];
           ptx::tmem_ld16(t_row + c, v);
           if (MODE == FORWARD_GATED) ptx::tmem_ld16(t_row + half_n + c, w);
@@ -827,7 +845,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ JoinP
   const long long row = (t - d.thread0) / d.chunks;
   const int n0 = static_cast<int>(t - d.thread0 - row * d.chunks) * 16;
   Kept<F32, GATED> kept;
-  if (MODE == BACKWARD_GATED || MODE == BACKWARD_ACT) kept.load(Kept<F32, GATED>::block(p.hid, row, n0));
+  if (MODE == BACKWARD_GATED || MODE == BACKWARD_ACT) kept.load(p.hid, row, n0);
   float v[16] = {}, w[16] = {};
 #pragma unroll 2
   for (int k = 0; k < d.splits; ++k) {
@@ -904,35 +922,45 @@ struct Plan {
   double cost;
 };
 
-// Estimated time of a plan in microseconds.  A k-block takes 0.27 us in a 256-wide tile (the tensor cores' rate) and
-// 0.17 us in a 128-wide one (shared memory's); where a block's operands come from HBM (few rows), 74 clusters share
-// 6.5 TB/s.  A tile's epilogue, 2.5 us at full width, runs under the next tile; the last one's does not.
+// Estimated time of a plan in microseconds, from these measurements:
+//  - from launch to the first operands in shared memory 2.8 us;
+//  - a k-block 0.27 us in a 256-wide tile (the tensor cores' rate), 0.165 us in a 128-wide one (shared memory's); where
+//    every weight is read once (one row of tiles) the clusters at work share 6.2 TB/s;
+//  - an epilogue is bound by what an SM can write, 18 bytes a nanosecond: the rows that exist times the bytes a column
+//    leaves (kept, H; dG, dU; the output; or fp32 partials).  It runs under the next unit's sum;
+//  - a join 3 us and its traffic.
 void estimate(Plan* plan, Mode mode, bool f32, const Product* products, int n, int clusters) {
-  const double wide = plan->tile_n / 256.0;
-  double work = 0.0, longest = 0.0, join = 0.0;
-  long long units = 0;
+  const int out_n = mode == FORWARD_GATED ? plan->tile_n / 2 : plan->tile_n;
+  double work = 0.0, longest = 0.0, join = 0.0, tail = 0.0;
   for (int i = 0; i < n; ++i) {
     const Product& g = products[i];
-    const int out_n = mode == FORWARD_GATED ? plan->tile_n / 2 : plan->tile_n;
     const long long u = ceil_div(g.M, TILE_M) * ceil_div(g.N, out_n) * plan->splits[i];
-    const double rows = static_cast<double>(g.M < TILE_M ? g.M : TILE_M);
-    const double bytes = rows * 128.0 + plan->tile_n * 128.0;      // of one k-block
-    const double from_hbm = g.M <= TILE_M ? bytes / 88e3 : 0.0;    // (larger outputs read their operands from L2 mostly)
-    double block = plan->tile_n == 256 ? 0.27 : 0.17;
-    if (block < from_hbm) block = from_hbm;
-    const double epilogue = 2.5 * wide * (f32 ? 1.5 : 1.0);
-    const double len = plan->per[i] * block;
-    const double unit = len > epilogue ? len : epilogue;
-    work += u * unit;
-    units += u;
+    const bool cut = plan->splits[i] > 1;
+    const double rows = g.M < CTA_M ? static_cast<double>(g.M) : CTA_M;
+    double column = f32 ? 4.0 : 2.0;                     // bytes written per row and column
+    if (mode == FORWARD_GATED) column = cut ? 8.0 : f32 ? 14.0 : 7.0;
+    else if (cut) column = 4.0;
+    else if (mode == FORWARD_ACT) column = f32 ? 10.0 : 4.5;
+    else if (mode == BACKWARD_GATED) column = f32 ? 12.0 : 4.0;
+    else if (mode == BACKWARD_ACT) column = f32 ? 6.0 : 2.0;
+    const double epilogue = 0.7 + rows * out_n * column / 18e3;
+    const double block = plan->tile_n == 256 ? 0.27 : 0.165, len = plan->per[i] * block;
+    const double hbm = g.M <= TILE_M ? plan->per[i] * plan->tile_n * 128.0 / 6.2e6 : 0.0;    // times the clusters at work
+    const auto round = [&](long long busy) {
+      const double t = len > hbm * busy ? len : hbm * busy;
+      return t > epilogue ? t : epilogue;
+    };
+    const long long rounds = u / clusters, left = u % clusters;
+    if (n == 1) work += rounds * round(clusters) + (left ? round(left) : 0.0);
+    else work += u * round(clusters) / clusters;
     if (len + epilogue > longest) longest = len + epilogue;
-    if (n == 1) work = static_cast<double>(ceil_div(u, clusters)) * unit * clusters;
-    if (plan->splits[i] > 1) join += 2.0 * plan->partial_bytes[i] / 5e6;
+    const double last = len < epilogue ? len : epilogue;
+    if (last > tail) tail = last;
+    if (cut) join += plan->partial_bytes[i] / 4e6;
   }
-  double t = work / clusters + 2.5 * wide;
+  double t = work + tail;
   if (t < longest) t = longest;
-  if (join > 0.0) t += join + 3.0;
-  plan->cost = t;
+  plan->cost = 2.8 + t + (join > 0.0 ? 3.0 + join : 0.0);
 }
 
 Plan make_plan(Mode mode, bool f32, const Product* products, int n, int clusters, size_t room) {
@@ -969,12 +997,15 @@ Plan make_plan(Mode mode, bool f32, const Product* products, int n, int clusters
   return best;
 }
 
-template <int MODE, bool F32>
-ffsplit_status launch_mode(ffsplit_ctx* ctx, const Params& p, const JoinParams& join, int clusters, cudaStream_t st) {
-  // (set on every launch: a host-side lookup, and the attribute belongs to the device, not to the context)
-  cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
-  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(train_gemm_kernel)");
-  e = launch_pdl(train_gemm_kernel<MODE, F32>, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, p);
+template <int MODE, bool F32, int CAP>
+ffsplit_status launch_mode(ffsplit_ctx* ctx, const Params<CAP>& p, const JoinParams& join, int clusters, cudaStream_t st) {
+  const unsigned bit = 1u << (MODE * 2 + (F32 ? 1 : 0) + (CAP > 1 ? 10 : 0));
+  if (!(ctx->attr_train_set & bit)) {
+    const cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(train_gemm_kernel)");
+    ctx->attr_train_set |= bit;
+  }
+  cudaError_t e = launch_pdl(train_gemm_kernel<MODE, F32, CAP>, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, p);
   ctx->launches++;
   if (e != cudaSuccess || join.n == 0) return check_cuda(ctx, e, "train_gemm_kernel launch");
   e = launch_pdl(join_kernel<MODE, F32>, dim3(static_cast<unsigned>(ceil_div(join.threads, 128))), dim3(128), 0, st, join);
@@ -982,11 +1013,11 @@ ffsplit_status launch_mode(ffsplit_ctx* ctx, const Params& p, const JoinParams& 
   return check_cuda(ctx, e, "join_kernel launch");
 }
 
-}  // namespace
-
-ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, char* partials,
-                      size_t partial_room, cudaStream_t st) {
-  Params p;
+// CAP: products that the argument block has room for (it is copied with every launch).
+template <int CAP>
+ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden,
+                               char* partials, size_t partial_room, cudaStream_t st) {
+  Params<CAP> p;
   JoinParams join;
   std::memset(&p, 0, sizeof(p));
   std::memset(&join, 0, sizeof(join));
@@ -1056,13 +1087,13 @@ ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Prod
   const int clusters = units < clusters_max ? static_cast<int>(units) : clusters_max;
   // The product with the longest units is dealt first; where its last round does not reach every cluster and shorter
   // units follow, the clusters left out get as many of those as fit into the length of one long unit.
-  if (n > 1 && p.prod[0].per > p.prod[1].per) {
-    p.heavy = p.prod[1].unit0;
+  if (CAP > 1 && n > 1 && p.prod[0].per > p.prod[CAP > 1 ? 1 : 0].per) {
+    p.heavy = p.prod[CAP > 1 ? 1 : 0].unit0;
     const int left = p.heavy % clusters;
     if (left) {
       constexpr int EPILOGUE_BLOCKS = 4;    // a unit's set-up and tail, in k-blocks
       p.short_from = left;
-      const long long extra = (p.prod[0].per + EPILOGUE_BLOCKS) / (p.prod[1].per + EPILOGUE_BLOCKS);
+      const long long extra = (p.prod[0].per + EPILOGUE_BLOCKS) / (p.prod[CAP > 1 ? 1 : 0].per + EPILOGUE_BLOCKS);
       const long long most = (units - p.heavy) / (clusters - left);
       p.extra = static_cast<int>(extra < most ? extra : most);
     }
@@ -1072,17 +1103,29 @@ ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Prod
   p.status = ctx->status();
   join.act = act;
   join.hid = hidden;
-  switch (mode) {
-    case PLAIN: return f32 ? launch_mode<PLAIN, true>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false>(ctx, p, join, clusters, st);
-    case FORWARD_GATED:
-      return f32 ? launch_mode<FORWARD_GATED, true>(ctx, p, join, clusters, st) : launch_mode<FORWARD_GATED, false>(ctx, p, join, clusters, st);
-    case FORWARD_ACT:
-      return f32 ? launch_mode<FORWARD_ACT, true>(ctx, p, join, clusters, st) : launch_mode<FORWARD_ACT, false>(ctx, p, join, clusters, st);
-    case BACKWARD_GATED:
-      return f32 ? launch_mode<BACKWARD_GATED, true>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_GATED, false>(ctx, p, join, clusters, st);
-    default:
-      return f32 ? launch_mode<BACKWARD_ACT, true>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_ACT, false>(ctx, p, join, clusters, st);
+  if constexpr (CAP > 1) {
+    return f32 ? launch_mode<PLAIN, true>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false>(ctx, p, join, clusters, st);
+  } else {
+    switch (mode) {
+      case PLAIN: return f32 ? launch_mode<PLAIN, true>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false>(ctx, p, join, clusters, st);
+      case FORWARD_GATED:
+        return f32 ? launch_mode<FORWARD_GATED, true>(ctx, p, join, clusters, st) : launch_mode<FORWARD_GATED, false>(ctx, p, join, clusters, st);
+      case FORWARD_ACT:
+        return f32 ? launch_mode<FORWARD_ACT, true>(ctx, p, join, clusters, st) : launch_mode<FORWARD_ACT, false>(ctx, p, join, clusters, st);
+      case BACKWARD_GATED:
+        return f32 ? launch_mode<BACKWARD_GATED, true>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_GATED, false>(ctx, p, join, clusters, st);
+      default:
+        return f32 ? launch_mode<BACKWARD_ACT, true>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_ACT, false>(ctx, p, join, clusters, st);
+    }
   }
+}
+
+}  // namespace
+
+ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, char* partials,
+                      size_t partial_room, cudaStream_t st) {
+  return n == 1 ? launch_products<1>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st)
+                : launch_products<MAX_PRODUCTS>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st);
 }
 
 }  // namespace tg

@@ -21,8 +21,8 @@ enum Mode : int {
   PLAIN = 0,            // C = sum of the pairs' products (+ bias)
   FORWARD_GATED = 1,    // G = A0 B0, U = A0 B1: keeps G, U; H = silu(G) U
   FORWARD_ACT = 2,      // Z = A0 B0 + bias: keeps Z; H = act(Z)
-  BACKWARD_GATED = 3,   // dH = A0 B0: dU = dH silu(G), dG = dH U silu'(G), H = silu(G) U
-  BACKWARD_ACT = 4      // dH = A0 B0: dZ = dH act'(Z), H = act(Z)
+  BACKWARD_GATED = 3,   // dH = A0 B0: dU = dH silu(G), dG = dH U silu'(G)
+  BACKWARD_ACT = 4      // dH = A0 B0: dZ = dH act'(Z)
 };
 
 // C [M, N] = sum over pairs of A_i [M, K] B_i [K, N].  a_mn: A lies in memory as [K, M] rows (M runs along memory),
@@ -46,9 +46,9 @@ struct Hidden {
   __nv_bfloat16 *H, *dG, *dU;
   long long ldm, plane_stride;
 };
-// Bytes of what is kept: 20 bits of G and U each, 24 of Z, all 32 in fp32 layers; whole blocks of 32 rows.
+// Bytes of what is kept of G and U, or of Z: 20 bits each, all 32 in fp32 layers; whole blocks of 32 rows.
 inline size_t kept_bytes(long long T, long long ldm, bool gated, bool f32) {
-  return static_cast<size_t>((T + 31) / 32 * 32) * ldm * (f32 ? (gated ? 8 : 4) : (gated ? 5 : 3));
+  return static_cast<size_t>((T + 31) / 32 * 32) * ldm * (gated ? 2 : 1) * (f32 ? 8 : 5) / 2;
 }
 
 #ifdef __CUDACC__
