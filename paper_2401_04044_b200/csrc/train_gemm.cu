@@ -8,7 +8,7 @@
 // the two it is, is a bit of the instruction descriptor and the shape of the TMA box, both chosen at run time.
 //
 // One persistent pair of CTAs (two SMs, cta_group::2) per 256 x 256 tile: each CTA stages 128 rows of A and 128 rows
-// of B per 64-deep k-block (32 KB) by TMA in a ring of six, rank 0 issues the MMAs for both, and each CTA finishes the
+// of B per 64-deep k-block (32 KB) by TMA in a ring of six (more where there are fewer rows or columns), rank 0 issues the MMAs for both, and each CTA finishes the
 // 128 accumulator rows in its own tensor memory.  Two accumulators of 256 columns: a tile's epilogue runs under the
 // next tile's MMAs.  A gated tile is 256 x 128: rank 0 stages the 128 columns of W1, rank 1 those of W1u, so that
 // every accumulator row holds G next to U and the product H leaves from the same registers.
@@ -24,7 +24,8 @@
 // a second launch (join_kernel) adds them in order and does what the epilogue would have done; or the tile is halved to
 // 256 x 128.  plan() weighs both.
 //
-// Warp roles: 0 TMA producer (both CTAs), 1 MMA issuer (rank 0), 2-9 epilogue (four lane quarters x two column halves).
+// Warp roles: 0 TMA producer (both CTAs), 1 MMA issuer (rank 0), from 2 on epilogue (four lane quarters x four groups of
+// columns; fp32 layers two).
 // Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
 #include <cstring>
 
@@ -36,17 +37,21 @@ namespace ffsp {
 namespace tg {
 
 constexpr int CTA_M = 128, TILE_M = 256, TILE_N = 256, BLOCK_K = 64;
-constexpr int STAGES = 6;
-constexpr int HALF_BYTES = CTA_M * BLOCK_K * 2;      // one operand of one CTA and stage
-constexpr int STAGE_BYTES = 2 * HALF_BYTES;
+constexpr int MAX_STAGES = 10;
 constexpr int BLOCK64_BYTES = 64 * BLOCK_K * 2;      // 64 x 64 elements: MN-major tiles are staged in two of these
-constexpr int EPI_WARPS = 8;
-constexpr int THREADS = 32 * (EPI_WARPS + 2);
 constexpr int TMEM_COLS = 512;
-constexpr int OUT_BYTES = 4096;                       // output staging of one epilogue warp: 32 rows x 128 bytes
 constexpr int BAR_BYTES = 256;
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES + BAR_BYTES + 1024;
-static_assert(SMEM_BYTES <= 232448, "shared memory of one CTA");
+constexpr int MAX_SMEM = 232448;
+// Epilogue warps and the output staging of each.  The activations' epilogues need many warps to hide their latencies (dH of
+// a 4096 x 11008 gated layer, 2048 tokens: 154 us with 8, 135 us with 16); plain outputs do not, and leave the tensor cores
+// more of the power and of the issue slots with 8 (the gradients of a 5120 x 20480 layer: 1.68 ms, 1.80 ms with 16); fp32
+// sums take 128 registers of a thread.
+template <int MODE, bool F32> constexpr int EPI_WARPS = F32 || MODE == PLAIN ? 8 : 16;
+template <int MODE, bool F32> constexpr int OUT_BYTES = F32 || MODE == PLAIN || MODE == BACKWARD_GATED ? 4096 : 2048;
+template <int MODE, bool F32> constexpr int THREADS = 32 * (EPI_WARPS<MODE, F32> + 2);
+// What is left for the ring of stages.  A stage holds a_rows rows of A and half a tile's columns of B, 128 bytes each.
+template <int MODE, bool F32>
+constexpr int RING_BYTES = (MAX_SMEM - 1024 - BAR_BYTES - EPI_WARPS<MODE, F32> * OUT_BYTES<MODE, F32>) / 1024 * 1024;
 constexpr int MAX_PRODUCTS = 4;
 constexpr int PROMOTE = 2;   // k-blocks: 8 MMAs, 2.5e-7
 
@@ -78,12 +83,15 @@ struct Params {
   DevProduct prod[CAP];
   int n_prod;
   int tile_n;            // accumulator columns of a tile, 256 or 128
+  int stages, a_bytes, stage_bytes;   // the ring
   int units;             // work units of all products, the products with the longer runs first
   // Units are dealt to the clusters in turn.  The first `heavy` ones (the product with the longest tiles) may leave the
   // clusters from `short_from` on one tile short: `extra` of the following units go to those clusters first.
   int heavy, short_from, extra;
   int act;
   Hidden hid;
+  CUtensorMap hid_map[2];  // bf16 layers: H, or dG (dZ) and dU, as outputs
+  int box_cols;            // columns of an output box
   int* status;
 };
 
@@ -325,7 +333,7 @@ struct Kept {
   static constexpr int LOW = F32 ? 0 : GATED ? 16 : 8;                     // bytes of low nibbles
   static constexpr int BLOCK = 32 * ((GATED ? 2 : 1) * Q * 16 + LOW);
   uint4 a[Q], b[GATED ? Q : 1];
-  uint32_t lo[4];
+  __align__(16) uint32_t lo[4];
   __device__ __forceinline__ static char* block(const Hidden& h, long long row, int n0) {
     return static_cast<char*>(h.kept) + ((row >> 5) * (h.ldm >> 4) + (n0 >> 4)) * BLOCK;
   }
@@ -408,31 +416,23 @@ struct Kept {
   }
 };
 
-// The activation's part of a pass for 16 columns of one row: v holds the accumulators (FORWARD_GATED: G, with U in w).
+// The activation's part of a pass for 16 columns of one row.  x holds the accumulators (FORWARD_GATED: G, with U in y) and
+// becomes H or dG (dZ), y becomes dU.
 template <int MODE, bool F32>
-__device__ __forceinline__ void finish16(const Hidden& h, int act, const void* bias, int N, long long row, int n0, float* v, float* w,
-                                         const Kept<F32, MODE == FORWARD_GATED || MODE == BACKWARD_GATED>& loaded) {
+__device__ __forceinline__ void activate16(const Hidden& h, int act, long long row, int n0, float2* x, float2* y,
+                                           const Kept<F32, MODE == FORWARD_GATED || MODE == BACKWARD_GATED>& loaded, bool in) {
   constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
-  const long long at = row * h.ldm + n0;
-  float2 x[8], y[8];
-  if (MODE == FORWARD_ACT && bias) add_bias<F32>(bias, n0, N, v);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x[i] = make_float2(v[2 * i], v[2 * i + 1]);
-    if (MODE == FORWARD_GATED) y[i] = make_float2(w[2 * i], w[2 * i + 1]);
-  }
   if (MODE == FORWARD_GATED || MODE == FORWARD_ACT) {
     if (h.kept) {
       Kept<F32, GATED> k;
       k.set(x, y);
-      k.store(h, row, n0);
+      if (in) k.store(h, row, n0);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (GATED) x[i] = __fmul2_rn(__fmul2_rn(x[i], sigmoid2<F32>(x[i])), y[i]);
       else gelu2<F32, false>(x[i], act, &x[i], nullptr);
     }
-    store16_planes<F32>(h.H + at, h.plane_stride, x);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -448,9 +448,22 @@ __device__ __forceinline__ void finish16(const Hidden& h, int act, const void* b
         x[i] = __fmul2_rn(x[i], slope);
       }
     }
-    store16_planes<F32>(h.dG + at, h.plane_stride, x);
-    if (GATED) store16_planes<F32>(h.dU + at, h.plane_stride, y);
   }
+}
+// What activate16() leaves, straight to memory.
+template <int MODE, bool F32>
+__device__ __forceinline__ void store_hidden16(const Hidden& h, long long row, int n0, const float2* x, const float2* y) {
+  const long long at = row * h.ldm + n0;
+  if (MODE == FORWARD_GATED || MODE == FORWARD_ACT) {
+    store16_planes<F32>(h.H + at, h.plane_stride, x);
+  } else {
+    store16_planes<F32>(h.dG + at, h.plane_stride, x);
+    if (MODE == BACKWARD_GATED) store16_planes<F32>(h.dU + at, h.plane_stride, y);
+  }
+}
+__device__ __forceinline__ void pairs16(const float* v, float2* x) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = make_float2(v[2 * i], v[2 * i + 1]);
 }
 
 // Rows that do not start on 16 bytes (m odd, or fp32 widths that are no multiple of 4) leave through shared memory, so
@@ -468,19 +481,17 @@ __device__ __forceinline__ void stage16(uint32_t* buf, int lane, int col, const 
     for (int i = 0; i < 8; ++i) row[((col >> 1) + i) ^ lane] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
   }
 }
-// The same for a TMA store with 128-byte swizzle: 16-byte piece j of row r at j ^ (r % 8).
+// The same for a TMA store of rows of 1 << row_shift bytes (32, 64 or 128) with the swizzle of that width: 16-byte piece
+// j of row r at j ^ (r % 8), j ^ (r / 2 % 4) or j ^ (r / 4 % 2).
 template <bool F32>
-__device__ __forceinline__ void stage16_swizzled(uint32_t* buf, int lane, int col, const float* v) {
-  uint4* row = reinterpret_cast<uint4*>(buf) + lane * 8;
-  if constexpr (F32) {
+__device__ __forceinline__ void stage16_swizzled(uint32_t* buf, int lane, int col, int row_shift, const uint32_t* w) {
+  char* row = reinterpret_cast<char*>(buf) + (lane << row_shift);
+  const int turn = (lane >> (7 - row_shift)) & ((1 << (row_shift - 4)) - 1);
+  constexpr int PIECES = F32 ? 4 : 2;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      row[((col >> 2) + i) ^ (lane & 7)] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      row[((col >> 3) + i) ^ (lane & 7)] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
-                                                      pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+  for (int i = 0; i < PIECES; ++i) {
+    const int j = (F32 ? col >> 2 : col >> 3) + i;
+    *reinterpret_cast<uint4*>(row + ((j ^ turn) << 4)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   }
 }
 // The staged columns n .. n + valid - 1 of rows row0 .. of C.
@@ -509,33 +520,34 @@ __device__ __forceinline__ void write_staged(const uint32_t* buf, int lane, void
 
 // ---------------------------------------------------------------------------------------------- the kernel
 template <int MODE, bool F32, int CAP>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_gemm_kernel(const __grid_constant__ Params<CAP> p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 1) train_gemm_kernel(const __grid_constant__ Params<CAP> p) {
   constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
   const int out_n = MODE == FORWARD_GATED ? p.tile_n / 2 : p.tile_n;     // output columns of a tile
   const int half_n = p.tile_n / 2;                                       // rows of B that one CTA stages
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* out_stage = smem + STAGES * STAGE_BYTES;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(out_stage + EPI_WARPS * OUT_BYTES);
-  uint64_t* full = bars;                  // [STAGES] TMA of both CTAs -> MMA (rank 0's are used)
-  uint64_t* empty = full + STAGES;        // [STAGES] MMA -> TMA, one set in each CTA
-  uint64_t* tfull = empty + STAGES;       // [2] MMA -> epilogue, one set in each CTA
+  uint8_t* out_stage = smem + RING_BYTES<MODE, F32>;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(out_stage + EPI_WARPS<MODE, F32> * OUT_BYTES<MODE, F32>);
+  uint64_t* full = bars;                  // [stages] TMA of both CTAs -> MMA (rank 0's are used)
+  uint64_t* empty = full + MAX_STAGES;    // [stages] MMA -> TMA, one set in each CTA
+  uint64_t* tfull = empty + MAX_STAGES;       // [2] MMA -> epilogue, one set in each CTA
   uint64_t* tempty = tfull + 2;           // [2] epilogue warps of both CTAs -> MMA (rank 0's are used)
   uint64_t* drain = tempty + 2;           // used only when giving up
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int stages = p.stages, stage_bytes = p.stage_bytes, a_bytes = p.a_bytes;
   const uint32_t rank = ptx::cluster_rank();
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < stages; ++s) {
       ptx::mbar_init(&full[s], 1);
       ptx::mbar_init(&empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&tfull[a], 1);
-      ptx::mbar_init(&tempty[a], 2 * EPI_WARPS);
+      ptx::mbar_init(&tempty[a], 2 * EPI_WARPS<MODE, F32>);
     }
     ptx::mbar_init(drain, 1);
     *abort_flag = 0;
@@ -586,7 +598,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
             if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
             if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);
             const uint32_t bar = full0 + s * 8;
-            const uint32_t da = smem0 + s * STAGE_BYTES, db = da + HALF_BYTES;
+            const uint32_t da = smem0 + s * stage_bytes, db = da + a_bytes;
             const int k0 = kb * BLOCK_K;
             if (d.a_mn) {
               if (load_a) {
@@ -602,16 +614,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
             } else {
               ptx::tma_load_3d_pair(tb, db, bar, k0, n0, pb);
             }
-            if (++s == STAGES) { s = 0; ph ^= 1u; }
+            if (++s == stages) { s = 0; ph ^= 1u; }
           }
           ++run;
           kb = 0;
         }
       }
       // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
-      for (int i = 0; i < STAGES && ok; ++i) {
+      for (int i = 0; i < stages && ok; ++i) {
         ok = ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag);
-        if (++s == STAGES) { s = 0; ph ^= 1u; }
+        if (++s == stages) { s = 0; ph ^= 1u; }
       }
       if (!ok) {
         // Copies into this CTA's shared memory are counted on rank 0's barriers: give what is in flight a bounded time
@@ -636,7 +648,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
         // bits 15, 16: the operand's rows run along memory
         const uint32_t idesc = idesc0 | (d.a_mn ? 1u << 15 : 0u) | (d.b_mn ? 1u << 16 : 0u);
         const uint64_t a_desc0 = d.a_mn ? ptx::umma_desc_mn128(smem0, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0);
-        const uint64_t b_desc0 = d.b_mn ? ptx::umma_desc_mn128(smem0 + HALF_BYTES, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0 + HALF_BYTES);
+        const uint64_t b_desc0 = d.b_mn ? ptx::umma_desc_mn128(smem0 + a_bytes, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0 + a_bytes);
         // 16 further along K: 32 bytes inside the swizzled row, or 16 rows of 128 bytes (addresses count 16 bytes)
         const uint32_t a_step = d.a_mn ? 2048 >> 4 : 32 >> 4, b_step = d.b_mn ? 2048 >> 4 : 32 >> 4;
         // fp32: the unit is summed in parts, each through an accumulator of its own
@@ -651,8 +663,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
             ok = ptx::mbar_wait_warp(&full[s], ph, abort_flag);
             if (!ok) break;
             ptx::tc_fence_after();
-            const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(s) * (STAGE_BYTES >> 4);
-            const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (STAGE_BYTES >> 4);
+            const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
+            const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
             if (ptx::elect_one()) {
 #pragma unroll
               for (int k = 0; k < BLOCK_K / 16; ++k)
@@ -660,7 +672,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
               ptx::umma_commit_pair(&empty[s]);
             }
             __syncwarp();
-            if (++s == STAGES) { s = 0; ph ^= 1u; }
+            if (++s == stages) { s = 0; ph ^= 1u; }
           }
           if (ok) {
             if (ptx::elect_one()) ptx::umma_commit_pair(&tfull[acc]);
@@ -683,10 +695,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
     // -------------------------------------------------------------- epilogue warps
     constexpr bool LOADS = MODE == BACKWARD_GATED || MODE == BACKWARD_ACT;
     const int q = warp & 3;                             // tensor-memory lane quarter
-    const int cols = out_n / 2;                         // output columns of this warp's half of the tile
+    constexpr int GROUPS = EPI_WARPS<MODE, F32> / 4;
+    const int cols = out_n / GROUPS;                    // output columns of this warp's part of the tile
     const int col0 = ((warp - 2) >> 2) * cols;
     const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + col0;
-    uint32_t* buf = reinterpret_cast<uint32_t*>(out_stage + (warp - 2) * OUT_BYTES);
+    uint32_t* buf = reinterpret_cast<uint32_t*>(out_stage + (warp - 2) * OUT_BYTES<MODE, F32>);
     Walk walk;
     uint32_t tl = 0;
     bool live = true;
@@ -699,6 +712,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
       const int c0 = t.n_blk * out_n + col0;
       Kept<F32, GATED> kept;
       if (LOADS && !F32 && !parts && in && c0 < d.N) kept.load(p.hid, row, c0);
+      if ((MODE == PLAIN || MODE == FORWARD_ACT) && d.bias && lane * 32 < cols && c0 + lane * 32 < d.N)
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(static_cast<const char*>(d.bias) + (c0 + lane * 32) * (F32 ? 4 : 2)));
       if constexpr (F32) {
         // All parts of the sum but the last are added up in registers (a gated tile's two halves lie 128 columns
         // apart); then it goes back to where the last part lies, and on as for bf16.
@@ -754,58 +769,85 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) train_ge
             if (in) store16_f32(base + d.ldp / 2 + c, v);
           }
         }
-      } else if (MODE == PLAIN) {
-        constexpr int SPAN = SPAN_COLS<F32>;
+      } else {
         const long long row0 = row - lane;
         const int rows = d.M - row0 >= 32 ? 32 : static_cast<int>(d.M - row0);      // (may be negative)
+        constexpr int SPAN = SPAN_COLS<F32>;
+        const int box = p.box_cols, row_shift = F32 ? 7 : box == 64 ? 7 : box == 32 ? 6 : 5;
+        uint32_t* buf2 = buf + 512;      // BACKWARD_GATED: dU, in the second half
 #pragma unroll 1
         for (int c = 0; c < width; c += 16) {
-          const int n0 = c0 + c, col = c % SPAN;
+          const int n0 = c0 + c;
           float v[16];
+          float2 x[8], y[8];
           ptx::tmem_ld16(t_row + c, v);
-          ptx::tmem_ld_wait();
-          if (d.bias) add_bias<F32>(d.bias, n0, d.N, v);
-          if (!d.ragged) {
-            if (col == 0) {
-              // the store before must have read the buffer
-              if (lane == 0) ptx::tma_store_wait_read();
-              __syncwarp();
-            }
-            stage16_swizzled<F32>(buf, lane, col, v);
-            if (col + 16 == SPAN || c + 16 >= width) {
-              ptx::fence_proxy_async();
-              __syncwarp();
-              if (lane == 0 && rows > 0) ptx::tma_store_2d(&d.c, ptx::smem_u32(buf), n0 - col, static_cast<int>(row0));
-            }
+          if (MODE == FORWARD_GATED) {
+            float w[16];
+            ptx::tmem_ld16(t_row + half_n + c, w);
+            ptx::tmem_ld_wait();
+            pairs16(w, y);
           } else {
+            ptx::tmem_ld_wait();
+          }
+          if ((MODE == PLAIN || MODE == FORWARD_ACT) && d.bias) add_bias<F32>(d.bias, n0, d.N, v);
+          if (MODE != PLAIN) {
+            pairs16(v, x);
+            activate16<MODE, F32>(p.hid, p.act, row, n0, x, y, kept, in);
+            // what was kept of the next columns is on its way while these leave
+            if (LOADS && in && c + 16 < width) kept.load(p.hid, row, n0 + 16);
+          }
+          if (MODE != PLAIN && F32) {
+            if (in) store_hidden16<MODE, F32>(p.hid, row, n0, x, y);
+          } else if (MODE == PLAIN && d.ragged) {
+            const int col = c % SPAN;
             stage16<F32>(buf, lane, col, v);
             if (col + 16 == SPAN || c + 16 >= width) {
               __syncwarp();
-              const int n = n0 - col, valid = d.N - n < SPAN ? d.N - n : SPAN;
+              const int n = n0 - col, valid = d.N - n < col + 16 ? d.N - n : col + 16;
               write_staged<F32>(buf, lane, d.C, d.ldc, row0, rows, n, valid);
               __syncwarp();
             }
+          } else {
+            const int col = c & (box - 1);
+            if (col == 0) {
+              // the stores before must have read the buffer
+              if (lane == 0) ptx::tma_store_wait_read();
+              __syncwarp();
+            }
+            uint32_t words[16];
+            if (MODE == PLAIN) {
+              if (F32) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) words[i] = __float_as_uint(v[i]);
+              } else {
+                pack16(v, words);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) words[i] = pack_bf16x2(x[i].x, x[i].y);
+            }
+            stage16_swizzled<F32>(buf, lane, col, row_shift, words);
+            if (MODE == BACKWARD_GATED) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) words[i] = pack_bf16x2(y[i].x, y[i].y);
+              stage16_swizzled<F32>(buf2, lane, col, row_shift, words);
+            }
+            if (col + 16 == box || c + 16 >= width) {
+              ptx::fence_proxy_async();
+              __syncwarp();
+              if (lane == 0 && rows > 0) {
+                ptx::tma_store_2d(MODE == PLAIN ? &d.c : &p.hid_map[0], ptx::smem_u32(buf), n0 - col, static_cast<int>(row0));
+                if (MODE == BACKWARD_GATED) ptx::tma_store_2d(&p.hid_map[1], ptx::smem_u32(buf2), n0 - col, static_cast<int>(row0));
+              }
+            }
           }
-        }
-      } else {
-        // what was kept of the next chunk is on its way while this one is computed
-#pragma unroll 2
-        for (int c = 0; c < width; c += 16) {
-          const int n0 = c0 + c;
-          const Kept<F32, GATED> now = kept;
-          if (LOADS && in && c + 16 < width) kept.load(p.hid, row, n0 + 16);
-          float v[16], w[16];
-          ptx::tmem_ld16(t_row + c, v);
-          if (MODE == FORWARD_GATED) ptx::tmem_ld16(t_row + half_n + c, w);
-          ptx::tmem_ld_wait();
-          if (in) finish16<MODE, F32>(p.hid, p.act, d.bias, d.N, row, n0, v, w, now);
         }
       }
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(&tempty[acc]), 0));
     }
-    if (MODE == PLAIN && lane == 0) ptx::tma_store_wait();
+    if (lane == 0) ptx::tma_store_wait();
   }
 
   ptx::tc_fence_before();
@@ -864,11 +906,15 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ JoinP
       }
     }
   }
+  if ((MODE == PLAIN || MODE == FORWARD_ACT) && d.bias) add_bias<F32>(d.bias, n0, d.N, v);
   if (MODE == PLAIN) {
-    if (d.bias) add_bias<F32>(d.bias, n0, d.N, v);
     store16_user<F32>(d.C, row * d.ldc + n0, d.N - n0, v);
   } else {
-    finish16<MODE, F32>(p.hid, p.act, d.bias, d.N, row, n0, v, w, kept);
+    float2 x[8], y[8];
+    pairs16(v, x);
+    pairs16(w, y);
+    activate16<MODE, F32>(p.hid, p.act, row, n0, x, y, kept, true);
+    store_hidden16<MODE, F32>(p.hid, row, n0, x, y);
   }
 }
 
@@ -900,14 +946,16 @@ ffsplit_status encode(ffsplit_ctx* ctx, const Matrix& m, int box_rows, CUtensorM
   return FFSPLIT_OK;
 }
 
-// Row-major output [rows, cols]: tiles of 32 rows x 128 bytes.
-ffsplit_status encode_out(ffsplit_ctx* ctx, bool f32, void* p, long long rows, int cols, long long ld, CUtensorMap* out) {
-  const cuuint64_t es = f32 ? 4 : 2;
+// Row-major output [rows, cols]: boxes of 32 rows x box_cols columns (32, 64 or 128 bytes), swizzled over that width.
+ffsplit_status encode_out(ffsplit_ctx* ctx, bool f32, void* p, long long rows, int cols, long long ld, int box_cols, CUtensorMap* out) {
+  const int es = f32 ? 4 : 2, bytes = box_cols * es;
   cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(ld) * es};
-  cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), 32}, estr[2] = {1, 1};
+  cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), 32}, estr[2] = {1, 1};
   const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_fn)(
       out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, dims, strides, box, estr,
-      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+      CU_TENSOR_MAP_INTERLEAVE_NONE,
+      bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
   return FFSPLIT_OK;
 }
@@ -924,7 +972,8 @@ struct Plan {
 
 // Estimated time of a plan in microseconds, from these measurements:
 //  - from launch to the first operands in shared memory 2.8 us;
-//  - a k-block 0.27 us in a 256-wide tile (the tensor cores' rate), 0.165 us in a 128-wide one (shared memory's); where
+//  - a k-block 0.27 us in a 256-wide tile (the tensor cores' rate), 0.2 us in a 128-wide one (shared memory's;
+//    0.26 us among the gradients, both of whose operands are MN-major); where
 //    every weight is read once (one row of tiles) the clusters at work share 6.2 TB/s;
 //  - an epilogue is bound by what an SM can write, 18 bytes a nanosecond: the rows that exist times the bytes a column
 //    leaves (kept, H; dG, dU; the output; or fp32 partials).  It runs under the next unit's sum;
@@ -944,7 +993,7 @@ void estimate(Plan* plan, Mode mode, bool f32, const Product* products, int n, i
     else if (mode == BACKWARD_GATED) column = f32 ? 12.0 : 4.0;
     else if (mode == BACKWARD_ACT) column = f32 ? 6.0 : 2.0;
     const double epilogue = 0.7 + rows * out_n * column / 18e3;
-    const double block = plan->tile_n == 256 ? 0.27 : 0.165, len = plan->per[i] * block;
+    const double block = plan->tile_n == 256 ? 0.27 : n == 1 ? 0.2 : 0.26, len = plan->per[i] * block;
     const double hbm = g.M <= TILE_M ? plan->per[i] * plan->tile_n * 128.0 / 6.2e6 : 0.0;    // times the clusters at work
     const auto round = [&](long long busy) {
       const double t = len > hbm * busy ? len : hbm * busy;
@@ -998,14 +1047,15 @@ Plan make_plan(Mode mode, bool f32, const Product* products, int n, int clusters
 }
 
 template <int MODE, bool F32, int CAP>
-ffsplit_status launch_mode(ffsplit_ctx* ctx, const Params<CAP>& p, const JoinParams& join, int clusters, cudaStream_t st) {
+ffsplit_status launch_mode(ffsplit_ctx* ctx, Params<CAP>& p, const JoinParams& join, int clusters, cudaStream_t st) {
   const unsigned bit = 1u << (MODE * 2 + (F32 ? 1 : 0) + (CAP > 1 ? 10 : 0));
   if (!(ctx->attr_train_set & bit)) {
-    const cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    const cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
     if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(train_gemm_kernel)");
     ctx->attr_train_set |= bit;
   }
-  cudaError_t e = launch_pdl(train_gemm_kernel<MODE, F32, CAP>, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, p);
+  p.stages = RING_BYTES<MODE, F32> / p.stage_bytes < MAX_STAGES ? RING_BYTES<MODE, F32> / p.stage_bytes : MAX_STAGES;
+  cudaError_t e = launch_pdl(train_gemm_kernel<MODE, F32, CAP>, dim3(2 * clusters), dim3(THREADS<MODE, F32>), MAX_SMEM, st, p);
   ctx->launches++;
   if (e != cudaSuccess || join.n == 0) return check_cuda(ctx, e, "train_gemm_kernel launch");
   e = launch_pdl(join_kernel<MODE, F32>, dim3(static_cast<unsigned>(ceil_div(join.threads, 128))), dim3(128), 0, st, join);
@@ -1034,6 +1084,10 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
   n = wanted;
   const int out_n = mode == FORWARD_GATED ? plan.tile_n / 2 : plan.tile_n;
   const int planes6 = f32 ? 6 : 1;
+  // an output box is as wide as a warp's part of the tile, but no wider than 128 bytes (64 where
+  // there are 16 warps)
+  const int part = out_n / (f32 || mode == PLAIN ? 2 : 4), widest = f32 || mode != PLAIN ? 32 : 64;
+  p.box_cols = part < widest ? part : widest;
   long long units = 0;
   for (int i = 0; i < n; ++i) {
     const Product& g = products[order[i]];
@@ -1056,7 +1110,7 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
     d.per = plan.per[order[i]];
     d.C = g.C; d.ldc = g.ldc; d.bias = g.bias;
     d.ragged = (g.ldc * (f32 ? 4 : 2)) % 16 != 0 ? 1 : 0;     // (the tensors themselves start on 16 bytes)
-    if (mode == PLAIN && d.splits == 1 && !d.ragged && (s = encode_out(ctx, f32, g.C, g.M, g.N, g.ldc, &d.c)) != FFSPLIT_OK) return s;
+    if (mode == PLAIN && d.splits == 1 && !d.ragged && (s = encode_out(ctx, f32, g.C, g.M, g.N, g.ldc, p.box_cols, &d.c)) != FFSPLIT_OK) return s;
     if (d.splits > 1) {
       d.partial = reinterpret_cast<float*>(partials);
       d.ldp = (mode == FORWARD_GATED ? 2 : 1) * round_up_ll(g.N, 64);
@@ -1083,6 +1137,10 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
   }
   p.n_prod = n;
   p.tile_n = plan.tile_n;
+  int a_rows = 8;
+  for (int i = 0; i < n; ++i) a_rows = p.prod[i].a_rows > a_rows ? p.prod[i].a_rows : a_rows;
+  p.a_bytes = a_rows * 128;
+  p.stage_bytes = p.a_bytes + plan.tile_n / 2 * 128;
   p.units = static_cast<int>(units);
   const int clusters = units < clusters_max ? static_cast<int>(units) : clusters_max;
   // The product with the longest units is dealt first; where its last round does not reach every cluster and shorter
@@ -1100,6 +1158,14 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
   }
   p.act = act;
   p.hid = hidden;
+  if (mode != PLAIN && !f32) {
+    const bool forward = mode == FORWARD_GATED || mode == FORWARD_ACT;
+    void* outs[2] = {forward ? hidden.H : hidden.dG, mode == BACKWARD_GATED ? hidden.dU : nullptr};
+    for (int i = 0; i < 2; ++i) {
+      ffsplit_status s;
+      if (outs[i] && (s = encode_out(ctx, false, outs[i], products[0].M, products[0].N, hidden.ldm, p.box_cols, &p.hid_map[i])) != FFSPLIT_OK) return s;
+    }
+  }
   p.status = ctx->status();
   join.act = act;
   join.hid = hidden;
