@@ -74,9 +74,9 @@ __global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_cons
 }
 
 // Bias gradients: out[c] = sum over rows of in[r, c], in fp32 and in a fixed order.  Bound by reading dZ and dY once.  A
-// block sums `rows_per` rows of 256 columns (a warp reads 512 contiguous bytes of every eighth row) and leaves a partial;
-// the block that is the last of its columns to arrive (a ticket, zero again afterwards) adds the partials in order.  (One
-// block per 64 columns over all rows had too few loads in flight: 307 us for 4096 rows of 20480 + 5120 columns.)
+// block takes 32 columns (four threads to a row, 64 rows at a time, eight of those in flight).  Where there are few columns
+// and many rows the rows are cut: each block leaves a partial, and the block that is the last of its columns to arrive (a
+// ticket, zero again afterwards) adds them in order.
 struct SumJob {
   const void* in;          // `planes` bf16 planes that add up, or (planes = 0) fp32 values
   void* out;               // bf16, or fp32 with f32_out
@@ -89,65 +89,94 @@ struct SumArgs {
   int n;
   int* tickets;            // one to a block of columns of either job
 };
-constexpr int SUM_COLS = 256;
-// Eight columns of one row: 8 lane + (0 .. 7) of bf16 planes, lane + 32 (0 .. 7) of fp32 values (whose rows may start
-// anywhere).
-__device__ __forceinline__ void add8(const SumJob& j, long long row, int c0, int lane, float* s) {
-  if (j.planes == 0) {
-    const float* p = static_cast<const float*>(j.in) + row * j.ld + c0 + lane;
+constexpr int SUM_COLS = 32;
+// Eight columns c .. c + 7 of one row.
+template <int PLANES>
+__device__ __forceinline__ void add8(const SumJob& j, long long row, int c, float* s) {
+  if constexpr (PLANES == 0) {
+    const float* p = static_cast<const float*>(j.in) + row * j.ld + c;
+    if (c + 8 <= j.cols && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) if (c0 + lane + 32 * i < j.cols) s[i] += __ldg(p + 32 * i);
-    return;
-  }
-  if (c0 + lane * 8 >= j.cols) return;      // (a last group of eight ends inside the row's padding)
-  for (int k = 0; k < j.planes; ++k) {
-    const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(j.in) + k * j.plane_stride + row * j.ld + c0 + lane * 8));
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+      for (int i = 0; i < 2; ++i) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(p) + i);
+        s[4 * i] += v.x; s[4 * i + 1] += v.y; s[4 * i + 2] += v.z; s[4 * i + 3] += v.w;
+      }
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s[2 * i] += __uint_as_float(w[i] << 16);
-      s[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
+      for (int i = 0; i < 8; ++i) if (c + i < j.cols) s[i] += __ldg(p + i);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k) {      // (a last group of eight ends inside the row's padding)
+      const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(j.in) + k * j.plane_stride + row * j.ld + c));
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[2 * i] += __uint_as_float(w[i] << 16);
+        s[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
+      }
     }
   }
 }
+// Rows begin, begin + 64, ... of eight columns.
+template <int PLANES>
+__device__ __forceinline__ void sum_rows(const SumJob& j, long long begin, long long end, int c, float* s) {
+  long long r = begin;
+  for (; r + 448 < end; r += 512) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add8<PLANES>(j, r + 64 * k, c, s);
+  }
+#pragma unroll
+  for (int k = 0; k < 7; ++k)
+    if (r + 64 * k < end) add8<PLANES>(j, r + 64 * k, c, s);
+}
+template <bool F32>
 __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ SumArgs a) {
   __shared__ float red[8][SUM_COLS];
+  __shared__ int last;
   pdl_wait();
-  const SumJob& j = a.job[a.n > 1 && static_cast<int>(blockIdx.x) >= a.job[1].block0 ? 1 : 0];
+  const int second = a.n > 1 && static_cast<int>(blockIdx.x) >= a.job[1].block0 ? 1 : 0;
+  const SumJob& j = a.job[second];
   const int b = blockIdx.x - j.block0, split = b / j.col_blocks, c0 = (b - split * j.col_blocks) * SUM_COLS;
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, mine = c0 + (lane & 3) * 8;
   const long long begin = split * j.rows_per, end = begin + j.rows_per < j.rows ? begin + j.rows_per : j.rows;
   float s[8] = {};
-  long long r = begin + w;
-  for (; r + 56 < end; r += 64) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) add8(j, r + 8 * k, c0, lane, s);
+  if (mine < j.cols) {
+    const long long r = begin + (threadIdx.x >> 2);
+    if constexpr (!F32) sum_rows<1>(j, r, end, mine, s);
+    else if (j.planes == 0) sum_rows<0>(j, r, end, mine, s);
+    else sum_rows<3>(j, r, end, mine, s);
   }
-  for (; r < end; r += 8) add8(j, r, c0, lane, s);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) red[w][j.planes == 0 ? lane + 32 * i : lane * 8 + i] = s[i];
+  for (int i = 0; i < 8; ++i) {
+    s[i] += __shfl_xor_sync(0xffffffffu, s[i], 4);
+    s[i] += __shfl_xor_sync(0xffffffffu, s[i], 8);
+    s[i] += __shfl_xor_sync(0xffffffffu, s[i], 16);
+    if (lane < 4) red[w][lane * 8 + i] = s[i];
+  }
   __syncthreads();
-  const int c = threadIdx.x;
+  const int c = threadIdx.x & (SUM_COLS - 1);
   float t = red[0][c];
   for (int k = 1; k < 8; ++k) t += red[k][c];
   if (j.splits > 1) {
-    if (c0 + c < j.cols) j.partial[static_cast<long long>(split) * j.cols + c0 + c] = t;
+    if (threadIdx.x < SUM_COLS && c0 + c < j.cols) j.partial[static_cast<long long>(split) * j.cols + c0 + c] = t;
     __threadfence();
     __syncthreads();
-    __shared__ int last;
-    int* ticket = a.tickets + (&j == &a.job[1] ? a.job[0].col_blocks : 0) + c0 / SUM_COLS;
-    if (c == 0) {
+    if (threadIdx.x == 0) {
+      int* ticket = a.tickets + (second ? a.job[0].col_blocks : 0) + c0 / SUM_COLS;
       last = atomicAdd(ticket, 1) == j.splits - 1 ? 1 : 0;
       if (last) *ticket = 0;
     }
     __syncthreads();
-    if (!last || c0 + c >= j.cols) return;
+    if (!last) return;
     __threadfence();
-    t = 0.f;
+    if (threadIdx.x < SUM_COLS && c0 + c < j.cols) {
+      t = 0.f;
 #pragma unroll 8
-    for (int k = 0; k < j.splits; ++k) t += __ldcg(j.partial + static_cast<long long>(k) * j.cols + c0 + c);
+      for (int k = 0; k < j.splits; ++k) t += __ldcg(j.partial + static_cast<long long>(k) * j.cols + c0 + c);
+    }
   }
-  if (c0 + c >= j.cols) return;
+  if (threadIdx.x >= SUM_COLS || c0 + c >= j.cols) return;
   if (j.f32_out) static_cast<float*>(j.out)[c0 + c] = t;
   else static_cast<__nv_bfloat16*>(j.out)[c0 + c] = __float2bfloat16_rn(t);
 }
@@ -158,11 +187,11 @@ namespace {
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Row ranges of a column sum: about four blocks of 256 columns to an SM, but no fewer than 64 rows (eight to a warp).
+// Row ranges of a column sum: enough blocks for two on every SM, but no fewer than 512 rows in each.
 int sum_splits(long long rows, int cols) {
   const long long col_blocks = (cols + train::SUM_COLS - 1) / train::SUM_COLS;
-  long long n = (4 * 148 + col_blocks - 1) / col_blocks;
-  if (n > (rows + 63) / 64) n = (rows + 63) / 64;
+  long long n = (2 * 148 + col_blocks - 1) / col_blocks;
+  if (n > (rows + 511) / 512) n = (rows + 511) / 512;
   return static_cast<int>(n < 1 ? 1 : n);
 }
 
@@ -368,7 +397,8 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
     if (grads.db1) add(h.dG, grads.db1, p.L.ldm, T * p.L.ldm, m, p.f32() ? 3 : 1);
     if (grads.db2) add(dY, grads.db2, d, 0, d, p.f32() ? 0 : 1);
     a.tickets = ctx->tickets();     // (columns are only cut along the rows where there are fewer blocks of them than tickets)
-    const cudaError_t e = launch_pdl(train::column_sum_kernel, dim3(blocks), dim3(256), 0, st, a);
+    const cudaError_t e = p.f32() ? launch_pdl(train::column_sum_kernel<true>, dim3(blocks), dim3(256), 0, st, a)
+                                  : launch_pdl(train::column_sum_kernel<false>, dim3(blocks), dim3(256), 0, st, a);
     ctx->launches++;
     return check_cuda(ctx, e, "column_sum_kernel launch");
   }

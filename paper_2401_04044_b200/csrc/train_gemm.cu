@@ -53,7 +53,7 @@ template <int MODE, bool F32> constexpr int THREADS = 32 * (EPI_WARPS<MODE, F32>
 template <int MODE, bool F32>
 constexpr int RING_BYTES = (MAX_SMEM - 1024 - BAR_BYTES - EPI_WARPS<MODE, F32> * OUT_BYTES<MODE, F32>) / 1024 * 1024;
 constexpr int MAX_PRODUCTS = 4;
-constexpr int PROMOTE = 2;   // k-blocks: 8 MMAs, 2.5e-7
+constexpr int PROMOTE = 4;   // k-blocks: 16 MMAs, 5e-7 at most
 
 struct Unit {
   int prod, m_blk, n_blk;
@@ -889,7 +889,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ JoinP
   Kept<F32, GATED> kept;
   if (MODE == BACKWARD_GATED || MODE == BACKWARD_ACT) kept.load(p.hid, row, n0);
   float v[16] = {}, w[16] = {};
-#pragma unroll 2
+#pragma unroll 4
   for (int k = 0; k < d.splits; ++k) {
     const float4* a = reinterpret_cast<const float4*>(d.partial + (k * d.M + row) * d.ldp + n0);
 #pragma unroll
