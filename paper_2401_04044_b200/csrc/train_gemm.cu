@@ -266,38 +266,6 @@ __device__ __forceinline__ void store16_f32(float* base, const float* v) {   // 
 #pragma unroll
   for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(base)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
 }
-// 16 values of a caller's tensor, of which `valid` lie inside; any alignment.
-template <bool F32>
-__device__ __forceinline__ void store16_user(void* C, long long at, int valid, const float* v) {
-  if (F32) {
-    float* base = static_cast<float*>(C) + at;
-    if (valid >= 16 && (reinterpret_cast<uintptr_t>(base) & 15u) == 0) {
-      store16_f32(base, v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) if (i < valid) base[i] = v[i];
-    }
-  } else {
-    __nv_bfloat16* base = static_cast<__nv_bfloat16*>(C) + at;
-    if (valid >= 16 && (reinterpret_cast<uintptr_t>(base) & 31u) == 0) {
-      uint32_t w[8];
-      pack16(v, w);
-      store32_bytes(base, w);
-    } else if (valid >= 8 && (reinterpret_cast<uintptr_t>(base) & 15u) == 0) {
-      reinterpret_cast<uint4*>(base)[0] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-      if (valid >= 16) {
-        reinterpret_cast<uint4*>(base)[1] =
-            make_uint4(pack_bf16x2(v[8], v[9]), pack_bf16x2(v[10], v[11]), pack_bf16x2(v[12], v[13]), pack_bf16x2(v[14], v[15]));
-      } else {
-#pragma unroll
-        for (int i = 8; i < 16; ++i) if (i < valid) base[i] = __float2bfloat16_rn(v[i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) if (i < valid) base[i] = __float2bfloat16_rn(v[i]);
-    }
-  }
-}
 template <bool F32>
 __device__ __forceinline__ void add_bias(const void* bias, int n0, int N, float* v) {
   if (F32) {
@@ -859,57 +827,110 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
   }
 }
 
-// Adds the partials of every product that was cut along K, in order, and finishes it.  One thread per row and 16 columns.
+// Adds the partials of every product that was cut along K, in order, and finishes it.
 struct JoinProduct {
   const float* partial;
   long long M, ldp, ldc;
   int N, chunks, splits;
   void* C;
   const void* bias;
-  long long thread0;     // first thread
+  long long chunk0;      // first chunk of 16 columns of one row
 };
 struct JoinParams {
   JoinProduct prod[MAX_PRODUCTS];
   int n;
-  long long threads;
+  long long chunks;
   int act;
   Hidden hid;
 };
-template <int MODE, bool F32>
-__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ JoinParams p) {
-  constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
-  pdl_wait();
-  const long long t = static_cast<long long>(blockIdx.x) * 128 + threadIdx.x;
-  if (t >= p.threads) return;
-  int i = 0;
-  while (i + 1 < p.n && t >= p.prod[i + 1].thread0) ++i;
-  const JoinProduct& d = p.prod[i];
-  const long long row = (t - d.thread0) / d.chunks;
-  const int n0 = static_cast<int>(t - d.thread0 - row * d.chunks) * 16;
-  Kept<F32, GATED> kept;
-  if (MODE == BACKWARD_GATED || MODE == BACKWARD_ACT) kept.load(p.hid, row, n0);
-  float v[16] = {}, w[16] = {};
-#pragma unroll 4
-  for (int k = 0; k < d.splits; ++k) {
-    const float4* a = reinterpret_cast<const float4*>(d.partial + (k * d.M + row) * d.ldp + n0);
+constexpr int JOIN_THREADS = 128, JOIN_CHUNKS = JOIN_THREADS / 4;
+// The sum of four values over n partials, in order.  Eight loads are issued before the first is used (left to itself the
+// compiler waited for every load in turn), and a warp reads 512 contiguous bytes (with 16 columns to a thread its requests
+// fell into 16 lines each: 6 us for 9 partials of 40 rows).
+__device__ __forceinline__ float4 add_partials(const float* p, long long stride, int n) {
+  constexpr int FLIGHT = 8;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = 0; k0 < n; k0 += FLIGHT) {
+    float4 x[FLIGHT];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float4 x = __ldcg(a + j);
-      v[4 * j] += x.x; v[4 * j + 1] += x.y; v[4 * j + 2] += x.z; v[4 * j + 3] += x.w;
+    for (int k = 0; k < FLIGHT; ++k)
+      x[k] = k0 + k < n ? __ldg(reinterpret_cast<const float4*>(p + (k0 + k) * stride)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) {
+      s.x += x[k].x; s.y += x[k].y; s.z += x[k].z; s.w += x[k].w;
     }
-    if (MODE == FORWARD_GATED) {
-      const float4* b = a + (d.ldp / 2) / 4;
+  }
+  return s;
+}
+// Four threads sum 16 columns of one row; where an activation follows, the block's first warp takes it from there with one
+// thread to 16 columns, as in the products' epilogue.
+template <int MODE, bool F32>
+__global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constant__ JoinParams p) {
+  constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
+  __shared__ float4 sums[MODE == PLAIN ? 1 : MODE == FORWARD_GATED ? 2 : 1][MODE == PLAIN ? 1 : JOIN_THREADS + JOIN_CHUNKS];
+  pdl_wait();
+  const long long chunk0 = static_cast<long long>(blockIdx.x) * JOIN_CHUNKS;
+  const auto place = [&](long long chunk, int* i, long long* row, int* n0) {
+    *i = 0;
+    while (*i + 1 < p.n && chunk >= p.prod[*i + 1].chunk0) ++*i;
+    const JoinProduct& d = p.prod[*i];
+    *row = (chunk - d.chunk0) / d.chunks;
+    *n0 = static_cast<int>(chunk - d.chunk0 - *row * d.chunks) * 16;
+  };
+  int i, n0;
+  long long row;
+  const long long mine = chunk0 + threadIdx.x / 4;
+  if (mine < p.chunks) {
+    place(mine, &i, &row, &n0);
+    const JoinProduct& d = p.prod[i];
+    const int col = n0 + (threadIdx.x & 3) * 4;
+    const float* at = d.partial + row * d.ldp + col;      // (the partials' pitch is a multiple of 64: no chunk is short there)
+    float4 v = add_partials(at, d.M * d.ldp, d.splits);
+    if (MODE != PLAIN) {
+      sums[0][threadIdx.x + threadIdx.x / 4] = v;
+      if (MODE == FORWARD_GATED) sums[MODE == FORWARD_GATED ? 1 : 0][threadIdx.x + threadIdx.x / 4] = add_partials(at + d.ldp / 2, d.M * d.ldp, d.splits);
+    } else {
+      const int valid = d.N - col;
+      float o[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float4 x = __ldcg(b + j);
-        w[4 * j] += x.x; w[4 * j + 1] += x.y; w[4 * j + 2] += x.z; w[4 * j + 3] += x.w;
+      for (int k = 0; k < 4; ++k)
+        if (d.bias && k < valid)
+          o[k] += F32 ? static_cast<const float*>(d.bias)[col + k] : __bfloat162float(static_cast<const __nv_bfloat16*>(d.bias)[col + k]);
+      if constexpr (F32) {
+        float* out = static_cast<float*>(d.C) + row * d.ldc + col;
+        if (valid >= 4 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0) {
+          *reinterpret_cast<float4*>(out) = make_float4(o[0], o[1], o[2], o[3]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) if (k < valid) out[k] = o[k];
+        }
+      } else {
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(d.C) + row * d.ldc + col;
+        if (valid >= 4 && (reinterpret_cast<uintptr_t>(out) & 7u) == 0) {
+          *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) if (k < valid) out[k] = __float2bfloat16_rn(o[k]);
+        }
       }
     }
   }
-  if ((MODE == PLAIN || MODE == FORWARD_ACT) && d.bias) add_bias<F32>(d.bias, n0, d.N, v);
-  if (MODE == PLAIN) {
-    store16_user<F32>(d.C, row * d.ldc + n0, d.N - n0, v);
-  } else {
+  if constexpr (MODE != PLAIN) {
+    __syncthreads();
+    const long long chunk = chunk0 + threadIdx.x;
+    if (threadIdx.x >= JOIN_CHUNKS || chunk >= p.chunks) return;
+    place(chunk, &i, &row, &n0);
+    const JoinProduct& d = p.prod[i];
+    Kept<F32, GATED> kept;
+    if (MODE == BACKWARD_GATED || MODE == BACKWARD_ACT) kept.load(p.hid, row, n0);
+    float v[16], w[16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 x = sums[0][threadIdx.x * 5 + k], y = sums[MODE == FORWARD_GATED ? 1 : 0][threadIdx.x * 5 + k];
+      v[4 * k] = x.x; v[4 * k + 1] = x.y; v[4 * k + 2] = x.z; v[4 * k + 3] = x.w;
+      w[4 * k] = y.x; w[4 * k + 1] = y.y; w[4 * k + 2] = y.z; w[4 * k + 3] = y.w;
+    }
+    if (MODE == FORWARD_ACT && d.bias) add_bias<F32>(d.bias, n0, d.N, v);
     float2 x[8], y[8];
     pairs16(v, x);
     pairs16(w, y);
@@ -973,11 +994,11 @@ struct Plan {
 // Estimated time of a plan in microseconds, from these measurements:
 //  - from launch to the first operands in shared memory 2.8 us;
 //  - a k-block 0.27 us in a 256-wide tile (the tensor cores' rate), 0.2 us in a 128-wide one (shared memory's;
-//    0.26 us among the gradients, both of whose operands are MN-major); where
+//    0.33 us among the gradients, both of whose operands are MN-major); where
 //    every weight is read once (one row of tiles) the clusters at work share 6.2 TB/s;
 //  - an epilogue is bound by what an SM can write, 18 bytes a nanosecond: the rows that exist times the bytes a column
 //    leaves (kept, H; dG, dU; the output; or fp32 partials).  It runs under the next unit's sum;
-//  - a join 3 us and its traffic.
+//  - a join 5 us, launch included, and its traffic (partials, and what an epilogue reads and leaves).
 void estimate(Plan* plan, Mode mode, bool f32, const Product* products, int n, int clusters) {
   const int out_n = mode == FORWARD_GATED ? plan->tile_n / 2 : plan->tile_n;
   double work = 0.0, longest = 0.0, join = 0.0, tail = 0.0;
@@ -992,8 +1013,10 @@ void estimate(Plan* plan, Mode mode, bool f32, const Product* products, int n, i
     else if (mode == FORWARD_ACT) column = f32 ? 10.0 : 4.5;
     else if (mode == BACKWARD_GATED) column = f32 ? 12.0 : 4.0;
     else if (mode == BACKWARD_ACT) column = f32 ? 6.0 : 2.0;
+    // (rows off 16 bytes leave word by word)
+    if (mode == PLAIN && !cut && g.ldc * (f32 ? 4 : 2) % 16 != 0) column *= 2.0;
     const double epilogue = 0.7 + rows * out_n * column / 18e3;
-    const double block = plan->tile_n == 256 ? 0.27 : n == 1 ? 0.2 : 0.26, len = plan->per[i] * block;
+    const double block = plan->tile_n == 256 ? 0.27 : n == 1 ? 0.2 : 0.33, len = plan->per[i] * block;
     const double hbm = g.M <= TILE_M ? plan->per[i] * plan->tile_n * 128.0 / 6.2e6 : 0.0;    // times the clusters at work
     const auto round = [&](long long busy) {
       const double t = len > hbm * busy ? len : hbm * busy;
@@ -1005,11 +1028,14 @@ void estimate(Plan* plan, Mode mode, bool f32, const Product* products, int n, i
     if (len + epilogue > longest) longest = len + epilogue;
     const double last = len < epilogue ? len : epilogue;
     if (last > tail) tail = last;
-    if (cut) join += plan->partial_bytes[i] / 4e6;
+    if (cut) {
+      const double leaves = mode == PLAIN ? 2.0 : mode == FORWARD_GATED ? 7.0 : mode == FORWARD_ACT ? 4.5 : mode == BACKWARD_GATED ? 9.0 : 4.5;
+      join += (plan->partial_bytes[i] + static_cast<double>(g.M) * g.N * leaves * (f32 ? 2.2 : 1.0)) / 4e6;
+    }
   }
   double t = work + tail;
   if (t < longest) t = longest;
-  plan->cost = 2.8 + t + (join > 0.0 ? 3.0 + join : 0.0);
+  plan->cost = 2.8 + t + (join > 0.0 ? 5.0 + join : 0.0);
 }
 
 Plan make_plan(Mode mode, bool f32, const Product* products, int n, int clusters, size_t room) {
@@ -1058,7 +1084,7 @@ ffsplit_status launch_mode(ffsplit_ctx* ctx, Params<CAP>& p, const JoinParams& j
   cudaError_t e = launch_pdl(train_gemm_kernel<MODE, F32, CAP>, dim3(2 * clusters), dim3(THREADS<MODE, F32>), MAX_SMEM, st, p);
   ctx->launches++;
   if (e != cudaSuccess || join.n == 0) return check_cuda(ctx, e, "train_gemm_kernel launch");
-  e = launch_pdl(join_kernel<MODE, F32>, dim3(static_cast<unsigned>(ceil_div(join.threads, 128))), dim3(128), 0, st, join);
+  e = launch_pdl(join_kernel<MODE, F32>, dim3(static_cast<unsigned>(ceil_div(join.chunks, JOIN_CHUNKS))), dim3(JOIN_THREADS), 0, st, join);
   ctx->launches++;
   return check_cuda(ctx, e, "join_kernel launch");
 }
@@ -1120,8 +1146,8 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
       j.M = g.M; j.ldp = d.ldp; j.ldc = g.ldc; j.N = g.N; j.splits = d.splits;
       j.chunks = (g.N + 15) / 16;
       j.C = g.C; j.bias = g.bias;
-      j.thread0 = join.threads;
-      join.threads += g.M * j.chunks;
+      j.chunk0 = join.chunks;
+      join.chunks += g.M * j.chunks;
     }
     // panel height: the tiles in flight form a block whose two sides carry about the same operand bytes
     int best = 1;
