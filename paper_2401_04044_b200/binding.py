@@ -158,6 +158,12 @@ def _stream_ptr(stream=None):
     return C.c_void_p(s.cuda_stream)
 
 
+def _stream_of(stream, device: int) -> int:
+    """The handle of `stream`, or of the device's current stream (without making a Stream object of it: that takes the
+    interpreter longer than a launch)."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
 class GradList:
     """The tensors whose gradients are clipped together, as the array ffsplit_grad_norm() / ffsplit_grad_clip() take.
     `out` holds where the clipped gradients go, tensor by tensor; without it they replace the gradients.  The list
@@ -421,7 +427,7 @@ class Context:
         w = self._train_weights(where, shape, W1, W1u, b1, W2, b2)
         rc = self.lib.ffsplit_train_forward(
             self.h, shape, w, self._operand(where, "X", X, dt, (T, d), False), T, None if saved is None else saved.data_ptr(),
-            0 if saved is None else saved.nbytes, self._operand(where, "Y", Y, dt, (T, d), False), _stream_ptr(stream))
+            0 if saved is None else saved.nbytes, self._operand(where, "Y", Y, dt, (T, d), False), _stream_of(stream, self.device))
         if rc:
             self._check(rc, where)
 
@@ -434,7 +440,7 @@ class Context:
                        op(where, "db1", db1, dt, (m,)), op(where, "dW2", dW2, dt, (m, d)), op(where, "db2", db2, dt, (d,)))
         rc = self.lib.ffsplit_train_backward(
             self.h, shape, w, op(where, "X", X, dt, (T, d), False), T, None if saved is None else saved.data_ptr(),
-            0 if saved is None else saved.nbytes, op(where, "dY", dY, dt, (T, d), False), g, _stream_ptr(stream))
+            0 if saved is None else saved.nbytes, op(where, "dY", dY, dt, (T, d), False), g, _stream_of(stream, self.device))
         if rc:
             self._check(rc, where)
 
@@ -454,12 +460,12 @@ class Context:
     def grad_norm(self, grads: "GradList", norm, stream=None):
         """ffsplit_grad_norm: norm[0] = the 2-norm of all gradients of the list."""
         self._check(self.lib.ffsplit_grad_norm(self.h, C.byref(grads.array), grads.count, self._norm_ptr("ffsplit_grad_norm", norm),
-                                               _stream_ptr(stream)), "ffsplit_grad_norm")
+                                               _stream_of(stream, self.device)), "ffsplit_grad_norm")
 
     def clip_grads(self, grads: "GradList", max_norm: float, norm, stream=None):
         """ffsplit_grad_clip: the norm, then every gradient times min(1, max_norm / (norm + 1e-6))."""
         self._check(self.lib.ffsplit_grad_clip(self.h, C.byref(grads.array), grads.count, max_norm,
-                                               self._norm_ptr("ffsplit_grad_clip", norm), _stream_ptr(stream)), "ffsplit_grad_clip")
+                                               self._norm_ptr("ffsplit_grad_clip", norm), _stream_of(stream, self.device)), "ffsplit_grad_clip")
 
     def debug_wait_timeout(self, limit_cycles: int, stream=None):
         self._check(self.lib.ffsplit_debug_wait_timeout(self.h, int(limit_cycles), _stream_ptr(stream)),
