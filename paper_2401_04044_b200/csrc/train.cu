@@ -335,6 +335,7 @@ ffsplit_status run_train_forward(ffsplit_ctx* ctx, const ffsplit_shape& s, const
   if ((r = tg::launch(ctx, p.gated() ? tg::FORWARD_GATED : tg::FORWARD_ACT, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st)) != FFSPLIT_OK) return r;
   g = product(p.hidden(h.H), 0, w2, 1, T, d, m);
   g.C = Y; g.ldc = d; g.bias = w.b2;
+  g.b_ready = 1;      // W2, or its planes: complete before the launch of the first product began to write
   return tg::launch(ctx, tg::PLAIN, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st);
 }
 

@@ -88,6 +88,7 @@ struct Params {
   // Units are dealt to the clusters in turn.  The first `heavy` ones (the product with the longest tiles) may leave the
   // clusters from `short_from` on one tile short: `extra` of the following units go to those clusters first.
   int heavy, short_from, extra;
+  int early;             // B of the first stages is loaded before the wait for the kernel before
   int act;
   Hidden hid;
   CUtensorMap hid_map[2];  // bf16 layers: H, or dG (dZ) and dU, as outputs
@@ -533,8 +534,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
   ptx::cluster_sync_all();     // also: the other CTA's barriers are set up
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_holder;
-  // Launched with programmatic stream serialisation: all of the above ran under the tail of the kernel before.  The one
-  // after may be set up only now that this CTA holds its tensor memory (see gemm_tc.cu).
+  const uint32_t smem0 = ptx::smem_u32(smem), full0 = ptx::map_to_cta(ptx::smem_u32(full), 0);
+  // This CTA's half of B of one k-block, into stage s.
+  const auto load_b = [&](const CUtensorMap* map, bool mn, int n0, int kb, int plane, int s) {
+    const uint32_t to = smem0 + s * stage_bytes + a_bytes, bar = full0 + s * 8;
+    if (mn) {
+      ptx::tma_load_3d_pair(map, to, bar, n0, kb * BLOCK_K, plane);
+      if (half_n > 64) ptx::tma_load_3d_pair(map, to + BLOCK64_BYTES, bar, n0 + 64, kb * BLOCK_K, plane);
+    } else {
+      ptx::tma_load_3d_pair(map, to, bar, kb * BLOCK_K, n0, plane);
+    }
+  };
+  const auto first_column = [&](const Unit& t) { return t.n_blk * out_n + (MODE == FORWARD_GATED ? 0 : static_cast<int>(rank) * half_n); };
+  const auto stage_tx = [&](const DevProduct& d) {
+    return static_cast<uint32_t>((d.M > CTA_M ? 2 : 1) * d.a_rows * BLOCK_K * 2 + 2 * half_n * BLOCK_K * 2);
+  };
+
+  // Launched with programmatic stream serialisation: all of the above ran under the tail of the kernel before; so do the
+  // loads of weights that it does not write.  The kernel after this one may be set up only now that this CTA holds its
+  // tensor memory (see gemm_tc.cu).
+  int ahead = 0;     // stages of the first unit whose B is on its way
+  if (warp == 0 && p.early) {
+    Walk walk;
+    const int u = walk.take(p);
+    if (u >= 0) {
+      const Unit t = find_unit(p, u);
+      const DevProduct& d = p.prod[t.prod];
+      ahead = t.k1 - t.k0 < stages ? t.k1 - t.k0 : stages;
+      if (ptx::elect_one()) {
+        for (int i = 0; i < ahead; ++i) {
+          if (rank == 0) ptx::mbar_expect_tx(&full[i], stage_tx(d));
+          int pair, pa, pb;
+          const int run = (t.k0 + i) / d.kb;
+          run_planes<F32>(d, run, &pair, &pa, &pb);
+          load_b(&d.b[MODE == FORWARD_GATED ? static_cast<int>(rank) : pair], d.b_mn, first_column(t), t.k0 + i - run * d.kb, pb, i);
+        }
+      }
+      __syncwarp();
+    }
+  }
   pdl_wait();
 
   if (warp == 0) {
@@ -544,48 +582,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
       uint32_t ph = 0;
       int s = 0;
       bool ok = true;
-      const uint32_t smem0 = ptx::smem_u32(smem), full0 = ptx::map_to_cta(ptx::smem_u32(full), 0);
       for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
         const Unit t = find_unit(p, u);
         const DevProduct& d = p.prod[t.prod];
-        const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M;
-        // Few rows: what the box leaves out, and all of rank 1's half where M <= 128, is not staged at all.  Whatever lies
+        const uint32_t tx = stage_tx(d);
+        const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M, n0 = first_column(t);
+        // Few rows: what A's box leaves out, and all of rank 1's half where M <= 128, is not staged at all.  Whatever lies
         // in shared memory there only reaches accumulator rows behind M.  (One token: the empty rows cost as much of the
         // copy engine as real ones, and the weights wait behind them.)
-        const bool load_a = rank == 0 || d.M > CTA_M;
-        const uint32_t tx = (d.M > CTA_M ? 2 : 1) * d.a_rows * BLOCK_K * 2 + 2 * half_n * BLOCK_K * 2;
-        const int n0 = t.n_blk * out_n + (MODE == FORWARD_GATED ? 0 : static_cast<int>(rank) * half_n);
+        const bool has_a = rank == 0 || d.M > CTA_M;
         int run = t.k0 / d.kb, kb = t.k0 - run * d.kb;
-        while (run < d.runs && run * d.kb < t.k1 && ok) {
+        for (; run < d.runs && run * d.kb < t.k1 && ok; ++run, kb = 0) {
           int pair, pa, pb;
           run_planes<F32>(d, run, &pair, &pa, &pb);
           const CUtensorMap* ta = &d.a[pair];
           const CUtensorMap* tb = &d.b[MODE == FORWARD_GATED ? static_cast<int>(rank) : pair];
           const int kb_end = t.k1 - run * d.kb < d.kb ? t.k1 - run * d.kb : d.kb;
           for (; kb < kb_end; ++kb) {
-            if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-            if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);
-            const uint32_t bar = full0 + s * 8;
-            const uint32_t da = smem0 + s * stage_bytes, db = da + a_bytes;
-            const int k0 = kb * BLOCK_K;
-            if (d.a_mn) {
-              if (load_a) {
-                ptx::tma_load_3d_pair(ta, da, bar, m0, k0, pa);
-                if (d.a_rows > 64) ptx::tma_load_3d_pair(ta, da + BLOCK64_BYTES, bar, m0 + 64, k0, pa);
-              }
-            } else if (load_a) {
-              ptx::tma_load_3d_pair(ta, da, bar, k0, m0, pa);
-            }
-            if (d.b_mn) {
-              ptx::tma_load_3d_pair(tb, db, bar, n0, k0, pb);
-              if (half_n > 64) ptx::tma_load_3d_pair(tb, db + BLOCK64_BYTES, bar, n0 + 64, k0, pb);
+            if (ahead > 0) {
+              --ahead;       // (an empty ring: nothing to wait for)
             } else {
-              ptx::tma_load_3d_pair(tb, db, bar, k0, n0, pb);
+              if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+              if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);
+              load_b(tb, d.b_mn, n0, kb, pb, s);
+            }
+            if (has_a) {
+              const uint32_t to = smem0 + s * stage_bytes, bar = full0 + s * 8;
+              if (d.a_mn) {
+                ptx::tma_load_3d_pair(ta, to, bar, m0, kb * BLOCK_K, pa);
+                if (d.a_rows > 64) ptx::tma_load_3d_pair(ta, to + BLOCK64_BYTES, bar, m0 + 64, kb * BLOCK_K, pa);
+              } else {
+                ptx::tma_load_3d_pair(ta, to, bar, kb * BLOCK_K, m0, pa);
+              }
             }
             if (++s == stages) { s = 0; ph ^= 1u; }
           }
-          ++run;
-          kb = 0;
         }
       }
       // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
@@ -609,7 +640,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
       uint32_t tl = 0, ph = 0;
       int s = 0;
       bool ok = true;
-      const uint32_t smem0 = ptx::smem_u32(smem);
       for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
         const Unit t = find_unit(p, u);
         const DevProduct& d = p.prod[t.prod];
@@ -1182,6 +1212,7 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
       p.extra = static_cast<int>(extra < most ? extra : most);
     }
   }
+  p.early = n == 1 && products[0].b_ready ? 1 : 0;
   p.act = act;
   p.hid = hidden;
   if (mode != PLAIN && !f32) {

@@ -37,6 +37,7 @@ struct Product {
                          // the launch is planned: a gradient has the same bits whichever others are asked for
   long long ldc;
   const void* bias;      // [N], the layer's type, or nullptr
+  int b_ready;           // the kernel before this launch in the stream does not write B
 };
 
 // What the activation's epilogue reads and writes: what the forward pass keeps (see Kept in train_gemm.cu; nullptr:
