@@ -20,55 +20,89 @@ namespace train {
 constexpr int MAX_JOBS = 5;
 struct PrepJob {
   const void* in;          // [rows, cols], pitch cols
-  __nv_bfloat16* out;      // pitch ld; fp32: three planes
+  __nv_bfloat16* out;      // pitch ld, a multiple of 64; fp32: three planes
   long long rows, ld, plane_stride;
-  int cols, quads;         // quads of columns in a row
+  int cols, octets;        // octets of columns in a row
   int block0;              // first block
 };
 struct PrepArgs {
   PrepJob job[MAX_JOBS];
   int n;
 };
-constexpr int PREP_THREADS = 256, PREP_UNROLL = 4;
+constexpr int PREP_THREADS = 256;
+template <bool F32> constexpr int PREP_UNROLL = F32 ? 2 : 4;
 
-// fp32 -> three bf16 planes (F32), or a copy of a bf16 matrix to another pitch.  One thread per four columns.
+// fp32 -> three bf16 planes (F32), or a copy of a bf16 matrix to rows of 128 bytes.  Bound by memory: a thread takes eight
+// columns at a time, 16 bytes of every output.  Rows of an odd bf16 matrix start on any two bytes: five aligned words hold
+// the eight values, shifted by half a word in every other row.
 template <bool F32>
 __global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_constant__ PrepArgs a) {
+  constexpr int UNROLL = PREP_UNROLL<F32>;
   pdl_wait();
   int j = 0;
   while (j + 1 < a.n && static_cast<int>(blockIdx.x) >= a.job[j + 1].block0) ++j;
   const PrepJob& job = a.job[j];
-  const long long first = static_cast<long long>(blockIdx.x - job.block0) * (PREP_THREADS * PREP_UNROLL) + threadIdx.x;
-  const long long all = job.rows * job.quads;
+  const long long first = static_cast<long long>(blockIdx.x - job.block0) * (PREP_THREADS * UNROLL) + threadIdx.x;
+  const long long all = job.rows * job.octets;
+  uint32_t w[UNROLL][F32 ? 8 : 5];
+  long long at[UNROLL];
+  bool half[UNROLL];
 #pragma unroll
-  for (int u = 0; u < PREP_UNROLL; ++u) {
+  for (int u = 0; u < UNROLL; ++u) {
     const long long i = first + u * PREP_THREADS;
-    if (i >= all) break;
-    const long long row = i / job.quads;
-    const int c = static_cast<int>(i - row * job.quads) * 4;
-    __nv_bfloat16* out = job.out + row * job.ld + c;      // 8-byte aligned: the pitch is a multiple of 64
-    if (F32) {
+    at[u] = -1;
+    if (i >= all) continue;
+    // (32-bit division where it will do: the 64-bit one takes longer than the copy)
+    const long long row = all <= 0xffffffffll ? static_cast<unsigned>(i) / static_cast<unsigned>(job.octets) : i / job.octets;
+    const int c = static_cast<int>(i - row * job.octets) * 8;
+    at[u] = row * job.ld + c;
+    if constexpr (F32) {
       const float* in = static_cast<const float*>(job.in) + row * job.cols + c;
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
-      if (c + 4 <= job.cols && (reinterpret_cast<uintptr_t>(in) & 15u) == 0) {
-        const float4 t = __ldg(reinterpret_cast<const float4*>(in));
-        v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+      if (c + 8 <= job.cols && (reinterpret_cast<uintptr_t>(in) & 15u) == 0) {
+        const uint4 x = __ldg(reinterpret_cast<const uint4*>(in)), y = __ldg(reinterpret_cast<const uint4*>(in) + 1);
+        w[u][0] = x.x; w[u][1] = x.y; w[u][2] = x.z; w[u][3] = x.w;
+        w[u][4] = y.x; w[u][5] = y.y; w[u][6] = y.z; w[u][7] = y.w;
       } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (c + k < job.cols) v[k] = __ldg(in + k);
+        for (int k = 0; k < 8; ++k) w[u][k] = c + k < job.cols ? __float_as_uint(__ldg(in + k)) : 0u;
       }
-      float w[4][3];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) tg::split3(v[k], w[k]);
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-        *reinterpret_cast<uint2*>(out + k * job.plane_stride) = make_uint2(pack_bf16x2(w[0][k], w[1][k]), pack_bf16x2(w[2][k], w[3][k]));
     } else {
       const unsigned short* in = static_cast<const unsigned short*>(job.in) + row * job.cols + c;
-      unsigned short v[4] = {0, 0, 0, 0};
+      half[u] = (reinterpret_cast<uintptr_t>(in) & 2u) != 0;
+      const uint32_t* word = reinterpret_cast<const uint32_t*>(in - (half[u] ? 1 : 0));
+      // the eight values may run into the next row (pad columns, which nobody reads), but not past the matrix
+      const char* end = static_cast<const char*>(job.in) + job.rows * job.cols * 2;
+      if (reinterpret_cast<const char*>(word + 5) <= end) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) if (c + k < job.cols) v[k] = __ldg(in + k);
-      *reinterpret_cast<uint2*>(out) = make_uint2(v[0] | static_cast<uint32_t>(v[1]) << 16, v[2] | static_cast<uint32_t>(v[3]) << 16);
+        for (int k = 0; k < 5; ++k) w[u][k] = __ldg(word + k);
+      } else {
+        half[u] = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t lo = c + 2 * k < job.cols ? __ldg(in + 2 * k) : 0, hi = c + 2 * k + 1 < job.cols ? __ldg(in + 2 * k + 1) : 0;
+          w[u][k] = lo | hi << 16;
+        }
+        w[u][4] = 0u;
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) {
+    if (at[u] < 0) continue;
+    uint4* out = reinterpret_cast<uint4*>(job.out + at[u]);
+    if constexpr (F32) {
+      float v[8][3];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) tg::split3(__uint_as_float(w[u][k]), v[k]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        *reinterpret_cast<uint4*>(job.out + k * job.plane_stride + at[u]) =
+            make_uint4(pack_bf16x2(v[0][k], v[1][k]), pack_bf16x2(v[2][k], v[3][k]), pack_bf16x2(v[4][k], v[5][k]), pack_bf16x2(v[6][k], v[7][k]));
+    } else {
+      const uint32_t* x = w[u];
+      *out = half[u] ? make_uint4(__funnelshift_r(x[0], x[1], 16), __funnelshift_r(x[1], x[2], 16), __funnelshift_r(x[2], x[3], 16),
+                                  __funnelshift_r(x[3], x[4], 16))
+                     : make_uint4(x[0], x[1], x[2], x[3]);
     }
   }
 }
@@ -284,10 +318,10 @@ struct Pass {
     j.in = p;
     j.out = reinterpret_cast<__nv_bfloat16*>(ws + at);
     j.rows = rows; j.cols = cols; j.ld = ld; j.plane_stride = rows * ld;
-    j.quads = (cols + 3) / 4;
+    j.octets = (cols + 7) / 8;
     j.block0 = prep_blocks;
-    constexpr int per = train::PREP_THREADS * train::PREP_UNROLL;
-    prep_blocks += static_cast<int>((rows * j.quads + per - 1) / per);
+    const int per = train::PREP_THREADS * (f32() ? train::PREP_UNROLL<true> : train::PREP_UNROLL<false>);
+    prep_blocks += static_cast<int>((rows * j.octets + per - 1) / per);
     return {j.out, rows, cols, ld, j.plane_stride, f32() ? 3 : 1};
   }
   tg::Matrix hidden(const void* at) const { return {at, T, s.m, L.ldm, T * L.ldm, f32() ? 3 : 1}; }
