@@ -68,10 +68,6 @@ class TrainGrads(C.Structure):
                 ("db2", C.c_void_p)]
 
 
-class GradTensor(C.Structure):
-    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
-
-
 class FFSplitError(RuntimeError):
     def __init__(self, code: int, where: str, text: str = ""):
         self.code = code
@@ -173,17 +169,19 @@ class GradList:
         self.grads, self.out = list(grads), list(grads) if out is None else list(out)
         if len(self.grads) != len(self.out):
             raise FFSplitError(2, "grad_list", "as many outputs as gradients are needed")
+        words = []
         for g, o in zip(self.grads, self.out):
-            for t in (g, o):
-                if t.dtype not in DTYPE_IDS or t.dtype != g.dtype:
-                    raise FFSplitError(4, "grad_list", "gradients are float32 or bfloat16, and outputs of the same type")
-                if t.numel() != g.numel() or not t.is_contiguous():
-                    raise FFSplitError(2, "grad_list", "tensors must be contiguous, and outputs as long as the gradients")
-                if t.device.type != "cuda" or t.device.index != device:
-                    raise FFSplitError(1, "grad_list", f"tensors must be on cuda:{device}")
+            kind, n = DTYPE_IDS.get(g.dtype), g.numel()
+            if kind is None or o.dtype is not g.dtype:
+                raise FFSplitError(4, "grad_list", "gradients are float32 or bfloat16, and outputs of the same type")
+            if o.numel() != n or not g.is_contiguous() or not o.is_contiguous():
+                raise FFSplitError(2, "grad_list", "tensors must be contiguous, and outputs as long as the gradients")
+            if g.get_device() != device or o.get_device() != device:
+                raise FFSplitError(1, "grad_list", f"tensors must be on cuda:{device}")
+            words += (g.data_ptr(), o.data_ptr(), n, kind)
+        # ffsplit_grad_tensor is four 8-byte words (the type, and padding, in the last)
         self.count = len(self.grads)
-        self.array = (GradTensor * max(1, self.count))(*[
-            GradTensor(g.data_ptr(), o.data_ptr(), g.numel(), DTYPE_IDS[g.dtype]) for g, o in zip(self.grads, self.out)])
+        self.array = (C.c_int64 * max(4, len(words)))(*words)
 
 
 def make_shape(d: int, m: int, act, dtype) -> Shape:

@@ -1028,7 +1028,7 @@ struct Plan {
 //    every weight is read once (one row of tiles) the clusters at work share 6.2 TB/s;
 //  - an epilogue is bound by what an SM can write, 18 bytes a nanosecond: the rows that exist times the bytes a column
 //    leaves (kept, H; dG, dU; the output; or fp32 partials).  It runs under the next unit's sum;
-//  - a join 5 us, launch included, and its traffic (partials, and what an epilogue reads and leaves).
+//  - a join 5 us, launch included, 0.2 us for each partial and its traffic (partials, what an epilogue reads and leaves).
 void estimate(Plan* plan, Mode mode, bool f32, const Product* products, int n, int clusters) {
   const int out_n = mode == FORWARD_GATED ? plan->tile_n / 2 : plan->tile_n;
   double work = 0.0, longest = 0.0, join = 0.0, tail = 0.0;
@@ -1060,7 +1060,7 @@ void estimate(Plan* plan, Mode mode, bool f32, const Product* products, int n, i
     if (last > tail) tail = last;
     if (cut) {
       const double leaves = mode == PLAIN ? 2.0 : mode == FORWARD_GATED ? 7.0 : mode == FORWARD_ACT ? 4.5 : mode == BACKWARD_GATED ? 9.0 : 4.5;
-      join += (plan->partial_bytes[i] + static_cast<double>(g.M) * g.N * leaves * (f32 ? 2.2 : 1.0)) / 4e6;
+      join += 0.2 * plan->splits[i] + (plan->partial_bytes[i] + static_cast<double>(g.M) * g.N * leaves * (f32 ? 2.2 : 1.0)) / 4e6;
     }
   }
   double t = work + tail;
@@ -1123,6 +1123,10 @@ ffsplit_status launch_mode(ffsplit_ctx* ctx, Params<CAP>& p, const JoinParams& j
 template <int CAP>
 ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden,
                                char* partials, size_t partial_room, cudaStream_t st) {
+  // The tensor maps are made by a driver call, which needs a current context; a thread that has only asked the runtime for
+  // its device (autograd's backward threads) has none yet.
+  const cudaError_t bound = cudaSetDevice(ctx->device);
+  if (bound != cudaSuccess) return check_cuda(ctx, bound, "cudaSetDevice");
   Params<CAP> p;
   JoinParams join;
   std::memset(&p, 0, sizeof(p));

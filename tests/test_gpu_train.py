@@ -419,3 +419,55 @@ def test_clipping_refusals(ctx):
         small.grad_norm(small.grad_list([g]), norm)
     assert e.value.code == 5
     small.close()
+
+
+# ------------------------------------------------------------------------------------------------ through PyTorch
+@pytest.mark.parametrize("act", ["swiglu", "gelu_erf"])
+def test_autograd_function_matches_the_calls(ctx, act):
+    from paper_2401_04044_b200 import make_shape
+    from paper_2401_04044_b200.train import ffn
+    L = draw(act, "bf16", 72, 200, 90)
+    want = run(ctx, L, act, "bf16")
+    D = {k: None if v is None else v.cuda().requires_grad_(k != "dY") for k, v in L.items()}
+    Y = ffn(ctx, make_shape(72, 200, act, torch.bfloat16), D["X"], D["W1"], D["W2"], D["b1"], D["b2"], D["W1u"])
+    Y.backward(D["dY"])
+    assert torch.equal(Y.detach().cpu(), want["Y"])
+    for k, t in D.items():
+        if t is not None and k != "dY":
+            assert torch.equal(t.grad.cpu(), want["d" + k]), k
+    # frozen weights: only what is needed is computed
+    X = D["X"].detach().requires_grad_()
+    Y = ffn(ctx, make_shape(72, 200, act, torch.bfloat16), X, *(D[k] if D[k] is None else D[k].detach() for k in ("W1", "W2", "b1", "b2", "W1u")))
+    Y.backward(D["dY"])
+    assert torch.equal(X.grad.cpu(), want["dX"])
+
+
+def test_calls_from_a_thread_that_has_used_no_gpu(ctx):
+    """Autograd runs backward passes on threads of its own, on which no CUDA context is current yet."""
+    import threading
+    L = draw("swiglu", "bf16", 72, 200, 90)
+    want, got = run(ctx, L, "swiglu", "bf16"), {}
+    t = threading.Thread(target=lambda: got.update(run(ctx, L, "swiglu", "bf16")))
+    t.start()
+    t.join()
+    assert got and all(torch.equal(got[k], want[k]) for k in want)
+
+
+def test_clip_grad_norm_in_place(ctx):
+    from paper_2401_04044_b200.train import clip_grad_norm_
+    ps = [torch.nn.Parameter(torch.zeros(n, dtype=t, device="cuda")) for n, t in ((1000, torch.bfloat16), (33, torch.float32), (5, torch.float32))]
+    for p in ps[:2]:
+        p.grad = torch.randn_like(p)
+    want = norm64([p.grad for p in ps[:2]])
+    norm = clip_grad_norm_(ctx, ps, 0.5)
+    ctx.poll()
+    assert abs(float(norm) - want) <= 5e-7 * want
+    assert abs(norm64([p.grad for p in ps[:2]]) - 0.5) < 2e-3
+
+
+@pytest.mark.parametrize("act", ["swiglu", "gelu_tanh"])
+def test_finetuning_recovers_a_rounded_layer(ctx, act):
+    from paper_2401_04044_b200.train import finetune
+    losses, shape, W = finetune(ctx, 128, 320, act, tokens=256, steps=25)
+    assert shape.m == 320 and all(math.isfinite(v) for v in losses)
+    assert sum(losses[-5:]) < 0.8 * sum(losses[:5])
