@@ -91,13 +91,11 @@ __global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_cons
     if (at[u] < 0) continue;
     uint4* out = reinterpret_cast<uint4*>(job.out + at[u]);
     if constexpr (F32) {
-      float v[8][3];
+      uint32_t v[4][3];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) tg::split3(__uint_as_float(w[u][k]), v[k]);
+      for (int k = 0; k < 4; ++k) tg::split3_pair(__uint_as_float(w[u][2 * k]), __uint_as_float(w[u][2 * k + 1]), v[k]);
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
-        *reinterpret_cast<uint4*>(job.out + k * job.plane_stride + at[u]) =
-            make_uint4(pack_bf16x2(v[0][k], v[1][k]), pack_bf16x2(v[2][k], v[3][k]), pack_bf16x2(v[4][k], v[5][k]), pack_bf16x2(v[6][k], v[7][k]));
+      for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(job.out + k * job.plane_stride + at[u]) = make_uint4(v[0][k], v[1][k], v[2][k], v[3][k]);
     } else {
       const uint32_t* x = w[u];
       *out = half[u] ? make_uint4(__funnelshift_r(x[0], x[1], 16), __funnelshift_r(x[1], x[2], 16), __funnelshift_r(x[2], x[3], 16),

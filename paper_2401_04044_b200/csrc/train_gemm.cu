@@ -44,10 +44,11 @@ constexpr int BAR_BYTES = 256;
 constexpr int MAX_SMEM = 232448;
 // Epilogue warps and the output staging of each.  The activations' epilogues need many warps to hide their latencies (dH of
 // a 4096 x 11008 gated layer, 2048 tokens: 154 us with 8, 135 us with 16); plain outputs do not, and leave the tensor cores
-// more of the power and of the issue slots with 8 (the gradients of a 5120 x 20480 layer: 1.68 ms, 1.80 ms with 16); fp32
-// sums take 128 registers of a thread.
+// more of the power and of the issue slots with 8 (the gradients of a 5120 x 20480 layer: 1.68 ms, 1.80 ms with 16).
+// fp32 sums take 128 registers of a thread (with 16 warps, 64 each, 96 in all: no faster); fp32 activations write straight
+// to memory.
 template <int MODE, bool F32> constexpr int EPI_WARPS = F32 || MODE == PLAIN ? 8 : 16;
-template <int MODE, bool F32> constexpr int OUT_BYTES = F32 || MODE == PLAIN || MODE == BACKWARD_GATED ? 4096 : 2048;
+template <int MODE, bool F32> constexpr int OUT_BYTES = MODE == PLAIN ? 4096 : F32 ? 0 : MODE == BACKWARD_GATED ? 4096 : 2048;
 template <int MODE, bool F32> constexpr int THREADS = 32 * (EPI_WARPS<MODE, F32> + 2);
 // What is left for the ring of stages.  A stage holds a_rows rows of A and half a tile's columns of B, 128 bytes each.
 template <int MODE, bool F32>
@@ -191,7 +192,7 @@ __device__ __forceinline__ float2 rcp(float2 x) {
 template <bool F32>
 __device__ __forceinline__ float2 sigmoid2(float2 z) {
   if constexpr (F32) {
-    return make_float2(1.0f / (1.0f + expf(-z.x)), 1.0f / (1.0f + expf(-z.y)));
+    return make_float2(__fdividef(1.0f, 1.0f + expf(-z.x)), __fdividef(1.0f, 1.0f + expf(-z.y)));     // 2 ulp
   } else {
     return rcp(__fadd2_rn(ex2(__fmul2_rn(z, both(-1.4426950408889634f))), both(1.0f)));
   }
@@ -253,11 +254,10 @@ __device__ __forceinline__ void store16_planes(__nv_bfloat16* base, long long pl
     if constexpr (!F32) {
       w[0][i] = pack_bf16x2(v[i].x, v[i].y);
     } else {
-      float o[3], q[3];
-      split3(v[i].x, o);
-      split3(v[i].y, q);
+      uint32_t o[3];
+      split3_pair(v[i].x, v[i].y, o);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) w[k][i] = pack_bf16x2(o[k], q[k]);
+      for (int k = 0; k < 3; ++k) w[k][i] = o[k];
     }
   }
 #pragma unroll
@@ -715,7 +715,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
       if constexpr (F32) {
         // All parts of the sum but the last are added up in registers (a gated tile's two halves lie 128 columns
         // apart); then it goes back to where the last part lies, and on as for bf16.
-        constexpr int BLOCKS = 8, SKIP = MODE == FORWARD_GATED ? TILE_N / 4 : 0;     // (fp32 tiles are 256 wide)
+        constexpr int BLOCKS = TILE_N / GROUPS / 16, SKIP = MODE == FORWARD_GATED ? TILE_N / 2 - BLOCKS * 8 : 0;     // (fp32 tiles are 256 wide)
         float sum[BLOCKS][16];
         bool first = true;
         for (int begin = t.k0;; ++tl) {

@@ -67,6 +67,25 @@ __device__ __forceinline__ void split3(float x, float* o) {
   const float r = x - a, b = __bfloat162float(__float2bfloat16_rn(r));
   o[0] = a; o[1] = b; o[2] = r - b;
 }
+// Two values at once: w[k] holds the k-th term of both.
+__device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ void split3_pair(float x, float y, uint32_t* w) {
+  if (fabsf(x) + fabsf(y) < 3.3e38f) {      // (false for NaN)
+    w[0] = bf16_pair(x, y);
+    const float rx = x - __uint_as_float(w[0] << 16), ry = y - __uint_as_float(w[0] & 0xffff0000u);
+    w[1] = bf16_pair(rx, ry);
+    w[2] = bf16_pair(rx - __uint_as_float(w[1] << 16), ry - __uint_as_float(w[1] & 0xffff0000u));
+  } else {
+    float p[3], q[3];
+    split3(x, p);
+    split3(y, q);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) w[k] = bf16_pair(p[k], q[k]);
+  }
+}
 #endif
 
 // Up to four PLAIN products (or one of the other modes) as one launch, or as two where K is cut.  f32: three-plane
