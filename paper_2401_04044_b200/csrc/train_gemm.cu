@@ -173,8 +173,9 @@ __device__ __forceinline__ int part_end(const DevProduct& d, const Unit& t, int 
 
 // ---------------------------------------------------------------------------------------------- activations
 // Values go through in pairs (the packed fp32 instructions of sm_100): the epilogue of a 256 x 256 tile has 32768 values
-// per SM, and at one instruction issued per clock and scheduler every instruction per value costs 0.14 us.  bf16 layers
-// use the hardware's exponential and reciprocal (a few 2^-22, far below bf16's 2^-9), fp32 layers the library functions.
+// per SM, and at one instruction issued per clock and scheduler every instruction per value costs 0.14 us.  Exponentials
+// and reciprocals are the hardware's (a few 2^-22 of the value), for fp32 layers too: what that adds to a layer's error is
+// below that of its sums (with expf, erfcf and divisions the epilogue of dH took 26 us of 66 for a 1024 x 2752 layer).
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 __device__ __forceinline__ float2 ex2(float2 x) {
   float2 r;
@@ -189,43 +190,31 @@ __device__ __forceinline__ float2 rcp(float2 x) {
   return r;
 }
 // 1 / (1 + exp(-z))
-template <bool F32>
 __device__ __forceinline__ float2 sigmoid2(float2 z) {
-  if constexpr (F32) {
-    return make_float2(__fdividef(1.0f, 1.0f + expf(-z.x)), __fdividef(1.0f, 1.0f + expf(-z.y)));     // 2 ulp
-  } else {
-    return rcp(__fadd2_rn(ex2(__fmul2_rn(z, both(-1.4426950408889634f))), both(1.0f)));
-  }
+  return rcp(__fadd2_rn(ex2(__fmul2_rn(z, both(-1.4426950408889634f))), both(1.0f)));
 }
 // GELU and, where asked for, its slope.
-template <bool F32, bool SLOPE>
+template <bool SLOPE>
 __device__ __forceinline__ void gelu2(float2 z, int act, float2* value, float2* slope) {
   if (act == FFSPLIT_GELU_ERF) {
-    // z Phi(z), Phi + z phi
-    float2 below, density;
-    if constexpr (F32) {
-      below = make_float2(0.5f * erfcf(-0.70710678118654752f * z.x), 0.5f * erfcf(-0.70710678118654752f * z.y));
-      if (SLOPE) density = make_float2(0.3989422804014327f * expf(-0.5f * z.x * z.x), 0.3989422804014327f * expf(-0.5f * z.y * z.y));
-    } else {
-      // Abramowitz and Stegun 7.1.26 (1.5e-7 absolute) for the tail of Phi, on the exponential that phi needs anyway
-      density = ex2(__fmul2_rn(__fmul2_rn(z, z), both(-0.72134752044448170f)));       // exp(-z^2 / 2)
-      const float2 t = rcp(__ffma2_rn(make_float2(fabsf(z.x), fabsf(z.y)), both(0.3275911f * 0.70710678118654752f), both(1.0f)));
-      float2 q = __ffma2_rn(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
-      q = __ffma2_rn(q, t, both(0.5f * 1.421413741f));
-      q = __ffma2_rn(q, t, both(0.5f * -0.284496736f));
-      q = __ffma2_rn(q, t, both(0.5f * 0.254829592f));
-      q = __fmul2_rn(q, __fmul2_rn(t, density));
-      const float2 over = __ffma2_rn(q, both(-1.0f), both(1.0f));
-      below = make_float2(z.x >= 0.f ? over.x : q.x, z.y >= 0.f ? over.y : q.y);
-      if (SLOPE) density = __fmul2_rn(density, both(0.3989422804014327f));
-    }
+    // z Phi(z), Phi + z phi: Abramowitz and Stegun 7.1.26 (1.5e-7 absolute) for the tail of Phi, on the exponential that
+    // phi needs anyway
+    float2 density = ex2(__fmul2_rn(__fmul2_rn(z, z), both(-0.72134752044448170f)));       // exp(-z^2 / 2)
+    const float2 t = rcp(__ffma2_rn(make_float2(fabsf(z.x), fabsf(z.y)), both(0.3275911f * 0.70710678118654752f), both(1.0f)));
+    float2 q = __ffma2_rn(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+    q = __ffma2_rn(q, t, both(0.5f * 1.421413741f));
+    q = __ffma2_rn(q, t, both(0.5f * -0.284496736f));
+    q = __ffma2_rn(q, t, both(0.5f * 0.254829592f));
+    q = __fmul2_rn(q, __fmul2_rn(t, density));
+    const float2 over = __ffma2_rn(q, both(-1.0f), both(1.0f));
+    const float2 below = make_float2(z.x >= 0.f ? over.x : q.x, z.y >= 0.f ? over.y : q.y);
     *value = __fmul2_rn(z, below);
-    if (SLOPE) *slope = __ffma2_rn(z, density, below);
+    if (SLOPE) *slope = __ffma2_rn(z, __fmul2_rn(density, both(0.3989422804014327f)), below);
   } else {
     // tanh form: (1 + tanh u) / 2 = sigmoid(2 u), u = c (z + a z^3)
     const float c = 0.79788456080286536f, a = 0.044715f;
     const float2 z2 = __fmul2_rn(z, z);
-    const float2 s = sigmoid2<F32>(__fmul2_rn(z, __ffma2_rn(z2, both(2.0f * c * a), both(2.0f * c))));
+    const float2 s = sigmoid2(__fmul2_rn(z, __ffma2_rn(z2, both(2.0f * c * a), both(2.0f * c))));
     const float2 v = __fmul2_rn(z, s);
     *value = v;
     if (SLOPE) {
@@ -399,21 +388,21 @@ __device__ __forceinline__ void activate16(const Hidden& h, int act, long long r
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (GATED) x[i] = __fmul2_rn(__fmul2_rn(x[i], sigmoid2<F32>(x[i])), y[i]);
-      else gelu2<F32, false>(x[i], act, &x[i], nullptr);
+      if (GATED) x[i] = __fmul2_rn(__fmul2_rn(x[i], sigmoid2(x[i])), y[i]);
+      else gelu2<false>(x[i], act, &x[i], nullptr);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 g = loaded.first(2 * i);
       if (GATED) {
-        const float2 up = loaded.second(2 * i), s = sigmoid2<F32>(g);
+        const float2 up = loaded.second(2 * i), s = sigmoid2(g);
         const float2 rest = __ffma2_rn(s, both(-1.0f), both(1.0f));
         y[i] = __fmul2_rn(x[i], __fmul2_rn(g, s));
         x[i] = __fmul2_rn(__fmul2_rn(x[i], up), __fmul2_rn(s, __ffma2_rn(g, rest, both(1.0f))));
       } else {
         float2 value, slope;
-        gelu2<F32, true>(g, act, &value, &slope);
+        gelu2<true>(g, act, &value, &slope);
         x[i] = __fmul2_rn(x[i], slope);
       }
     }
@@ -715,8 +704,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
       if constexpr (F32) {
         // All parts of the sum but the last are added up in registers (a gated tile's two halves lie 128 columns
         // apart); then it goes back to where the last part lies, and on as for bf16.
-        constexpr int BLOCKS = TILE_N / GROUPS / 16, SKIP = MODE == FORWARD_GATED ? TILE_N / 2 - BLOCKS * 8 : 0;     // (fp32 tiles are 256 wide)
-        float sum[BLOCKS][16];
+        constexpr int BLOCKS = TILE_N / GROUPS / 32, SKIP = MODE == FORWARD_GATED ? TILE_N / 2 - BLOCKS * 16 : 0;     // (fp32 tiles are 256 wide)
+        float sum[BLOCKS][32];
         bool first = true;
         for (int begin = t.k0;; ++tl) {
           const int end = part_end(d, t, begin);
@@ -727,13 +716,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
           const uint32_t t_part = t_quarter + (tl & 1) * TILE_N;
 #pragma unroll
           for (int b = 0; b < BLOCKS; ++b) {
-            const uint32_t at = t_part + b * 16 + (b >= BLOCKS / 2 ? SKIP : 0);
-            float v[16];
-            ptx::tmem_ld16(at, v);
+            const uint32_t at = t_part + b * 32 + (b >= BLOCKS / 2 ? SKIP : 0);
+            float v[32];
+            ptx::tmem_ld32(at, v);
             ptx::tmem_ld_wait();
+            if (first) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[b][i] = first ? v[i] : sum[b][i] + v[i];
-            if (last) ptx::tmem_st16(at, sum[b]);
+              for (int i = 0; i < 32; ++i) sum[b][i] = v[i];
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) sum[b][i] += v[i];
+            }
+            if (last) {
+              ptx::tmem_st16(at, sum[b]);
+              ptx::tmem_st16(at + 16, sum[b] + 16);
+            }
           }
           first = false;
           if (last) {
