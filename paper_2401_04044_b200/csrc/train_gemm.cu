@@ -24,8 +24,8 @@
 // a second launch (join_kernel) adds them in order and does what the epilogue would have done; or the tile is halved to
 // 256 x 128.  plan() weighs both.
 //
-// Warp roles: 0 TMA producer (both CTAs), 1 MMA issuer (rank 0), from 2 on epilogue (four lane quarters x four groups of
-// columns; fp32 layers two).
+// Warp roles: 0 TMA producer (both CTAs), 1 MMA issuer (rank 0), from 2 on (fp32 layers: from 4 on) epilogue, four lane
+// quarters x two or four groups of columns.
 // Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
 #include <cstring>
 
@@ -45,11 +45,17 @@ constexpr int MAX_SMEM = 232448;
 // Epilogue warps and the output staging of each.  The activations' epilogues need many warps to hide their latencies (dH of
 // a 4096 x 11008 gated layer, 2048 tokens: 154 us with 8, 135 us with 16); plain outputs do not, and leave the tensor cores
 // more of the power and of the issue slots with 8 (the gradients of a 5120 x 20480 layer: 1.68 ms, 1.80 ms with 16).
-// fp32 sums take 128 registers of a thread (with 16 warps, 64 each, 96 in all: no faster); fp32 activations write straight
-// to memory.
+// fp32 sums take 128 registers of a thread; fp32 activations write straight to memory.
 template <int MODE, bool F32> constexpr int EPI_WARPS = F32 || MODE == PLAIN ? 8 : 16;
 template <int MODE, bool F32> constexpr int OUT_BYTES = MODE == PLAIN ? 4096 : F32 ? 0 : MODE == BACKWARD_GATED ? 4096 : 2048;
-template <int MODE, bool F32> constexpr int THREADS = 32 * (EPI_WARPS<MODE, F32> + 2);
+// The first epilogue warp.  fp32 kernels keep it on a warpgroup's boundary, so that registers can move from the group of the
+// producer and the MMA issuer to the epilogue's two: with 168 for every thread the sums were spilled, and with the ring
+// taking nearly all of the SM's memory a spill goes to L2.  384 threads start with 168 registers each (64512); 128 of them go
+// down to 56 and 256 up to 224: 7168 + 57344 = 64512.
+template <bool F32> constexpr int FIRST_EPI = F32 ? 4 : 2;
+constexpr int START_REGS = 168, ROLE_REGS = 56, EPI_REGS = 224;
+static_assert(ROLE_REGS * 128 + EPI_REGS * 256 <= START_REGS * 384, "a split above what the block starts with waits forever");
+template <int MODE, bool F32> constexpr int THREADS = 32 * (EPI_WARPS<MODE, F32> + FIRST_EPI<F32>);
 // What is left for the ring of stages.  A stage holds a_rows rows of A and half a tile's columns of B, 128 bytes each.
 template <int MODE, bool F32>
 constexpr int RING_BYTES = (MAX_SMEM - 1024 - BAR_BYTES - EPI_WARPS<MODE, F32> * OUT_BYTES<MODE, F32>) / 1024 * 1024;
@@ -511,7 +517,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
     *abort_flag = 0;
     ptx::mbar_fence_init();
   }
-  if (warp == 2 && lane < 2) {
+  if (warp == FIRST_EPI<F32> && lane < 2) {
     ptx::prefetch_tmap(&p.prod[0].a[0]);
     ptx::prefetch_tmap(&p.prod[0].b[MODE == FORWARD_GATED ? lane : 0]);
   }
@@ -564,129 +570,133 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
   }
   pdl_wait();
 
-  if (warp == 0) {
-    if (ptx::elect_one()) {
-      // ------------------------------------------------------------ TMA producer
-      Walk walk;
-      uint32_t ph = 0;
-      int s = 0;
-      bool ok = true;
-      for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
-        const Unit t = find_unit(p, u);
-        const DevProduct& d = p.prod[t.prod];
-        const uint32_t tx = stage_tx(d);
-        const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M, n0 = first_column(t);
-        // Few rows: what A's box leaves out, and all of rank 1's half where M <= 128, is not staged at all.  Whatever lies
-        // in shared memory there only reaches accumulator rows behind M.  (One token: the empty rows cost as much of the
-        // copy engine as real ones, and the weights wait behind them.)
-        const bool has_a = rank == 0 || d.M > CTA_M;
-        int run = t.k0 / d.kb, kb = t.k0 - run * d.kb;
-        for (; run < d.runs && run * d.kb < t.k1 && ok; ++run, kb = 0) {
-          int pair, pa, pb;
-          run_planes<F32>(d, run, &pair, &pa, &pb);
-          const CUtensorMap* ta = &d.a[pair];
-          const CUtensorMap* tb = &d.b[MODE == FORWARD_GATED ? static_cast<int>(rank) : pair];
-          const int kb_end = t.k1 - run * d.kb < d.kb ? t.k1 - run * d.kb : d.kb;
-          for (; kb < kb_end; ++kb) {
-            if (ahead > 0) {
-              --ahead;       // (an empty ring: nothing to wait for)
-            } else {
-              if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-              if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);
-              load_b(tb, d.b_mn, n0, kb, pb, s);
-            }
-            if (has_a) {
-              const uint32_t to = smem0 + s * stage_bytes, bar = full0 + s * 8;
-              if (d.a_mn) {
-                ptx::tma_load_3d_pair(ta, to, bar, m0, kb * BLOCK_K, pa);
-                if (d.a_rows > 64) ptx::tma_load_3d_pair(ta, to + BLOCK64_BYTES, bar, m0 + 64, kb * BLOCK_K, pa);
+  if (warp < FIRST_EPI<F32>) {
+    if constexpr (F32) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ROLE_REGS));
+    if (warp == 0) {
+      if (ptx::elect_one()) {
+        // ------------------------------------------------------------ TMA producer
+        Walk walk;
+        uint32_t ph = 0;
+        int s = 0;
+        bool ok = true;
+        for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
+          const Unit t = find_unit(p, u);
+          const DevProduct& d = p.prod[t.prod];
+          const uint32_t tx = stage_tx(d);
+          const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M, n0 = first_column(t);
+          // Few rows: what A's box leaves out, and all of rank 1's half where M <= 128, is not staged at all.  Whatever lies
+          // in shared memory there only reaches accumulator rows behind M.  (One token: the empty rows cost as much of the
+          // copy engine as real ones, and the weights wait behind them.)
+          const bool has_a = rank == 0 || d.M > CTA_M;
+          int run = t.k0 / d.kb, kb = t.k0 - run * d.kb;
+          for (; run < d.runs && run * d.kb < t.k1 && ok; ++run, kb = 0) {
+            int pair, pa, pb;
+            run_planes<F32>(d, run, &pair, &pa, &pb);
+            const CUtensorMap* ta = &d.a[pair];
+            const CUtensorMap* tb = &d.b[MODE == FORWARD_GATED ? static_cast<int>(rank) : pair];
+            const int kb_end = t.k1 - run * d.kb < d.kb ? t.k1 - run * d.kb : d.kb;
+            for (; kb < kb_end; ++kb) {
+              if (ahead > 0) {
+                --ahead;       // (an empty ring: nothing to wait for)
               } else {
-                ptx::tma_load_3d_pair(ta, to, bar, kb * BLOCK_K, m0, pa);
+                if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+                if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);
+                load_b(tb, d.b_mn, n0, kb, pb, s);
               }
+              if (has_a) {
+                const uint32_t to = smem0 + s * stage_bytes, bar = full0 + s * 8;
+                if (d.a_mn) {
+                  ptx::tma_load_3d_pair(ta, to, bar, m0, kb * BLOCK_K, pa);
+                  if (d.a_rows > 64) ptx::tma_load_3d_pair(ta, to + BLOCK64_BYTES, bar, m0 + 64, kb * BLOCK_K, pa);
+                } else {
+                  ptx::tma_load_3d_pair(ta, to, bar, kb * BLOCK_K, m0, pa);
+                }
+              }
+              if (++s == stages) { s = 0; ph ^= 1u; }
             }
-            if (++s == stages) { s = 0; ph ^= 1u; }
           }
         }
+        // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
+        for (int i = 0; i < stages && ok; ++i) {
+          ok = ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag);
+          if (++s == stages) { s = 0; ph ^= 1u; }
+        }
+        if (!ok) {
+          // Copies into this CTA's shared memory are counted on rank 0's barriers: give what is in flight a bounded time
+          // to land before the CTA exits.
+          const long long t0 = clock64();
+          while (clock64() - t0 < ptx::kWaitLimitCycles / 64) {}
+        }
       }
-      // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
-      for (int i = 0; i < stages && ok; ++i) {
-        ok = ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag);
-        if (++s == stages) { s = 0; ph ^= 1u; }
-      }
-      if (!ok) {
-        // Copies into this CTA's shared memory are counted on rank 0's barriers: give what is in flight a bounded time
-        // to land before the CTA exits.
-        const long long t0 = clock64();
-        while (clock64() - t0 < ptx::kWaitLimitCycles / 64) {}
-      }
-    }
-    __syncwarp();
-  } else if (warp == 1) {
-    if (rank == 0) {
-      // ------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
-      const uint32_t idesc0 = ptx::umma_idesc_bf16(TILE_M, p.tile_n);
-      Walk walk;
-      uint32_t tl = 0, ph = 0;
-      int s = 0;
-      bool ok = true;
-      for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
-        const Unit t = find_unit(p, u);
-        const DevProduct& d = p.prod[t.prod];
-        // bits 15, 16: the operand's rows run along memory
-        const uint32_t idesc = idesc0 | (d.a_mn ? 1u << 15 : 0u) | (d.b_mn ? 1u << 16 : 0u);
-        const uint64_t a_desc0 = d.a_mn ? ptx::umma_desc_mn128(smem0, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0);
-        const uint64_t b_desc0 = d.b_mn ? ptx::umma_desc_mn128(smem0 + a_bytes, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0 + a_bytes);
-        // 16 further along K: 32 bytes inside the swizzled row, or 16 rows of 128 bytes (addresses count 16 bytes)
-        const uint32_t a_step = d.a_mn ? 2048 >> 4 : 32 >> 4, b_step = d.b_mn ? 2048 >> 4 : 32 >> 4;
-        // fp32: the unit is summed in parts, each through an accumulator of its own
-        for (int begin = t.k0; begin < t.k1 && ok; ++tl) {
-          const int end = F32 ? part_end(d, t, begin) : t.k1;
-          const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
-          ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aph ^ 1, abort_flag) ? 1 : 0, 0) != 0;
-          if (!ok) break;
-          ptx::tc_fence_after();
-          const uint32_t d_tmem = tmem_base + acc * TILE_N;
-          for (int kb = begin; kb < end; ++kb) {
-            ok = ptx::mbar_wait_warp(&full[s], ph, abort_flag);
+      __syncwarp();
+    } else if (warp == 1) {
+      if (rank == 0) {
+        // ------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
+        const uint32_t idesc0 = ptx::umma_idesc_bf16(TILE_M, p.tile_n);
+        Walk walk;
+        uint32_t tl = 0, ph = 0;
+        int s = 0;
+        bool ok = true;
+        for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
+          const Unit t = find_unit(p, u);
+          const DevProduct& d = p.prod[t.prod];
+          // bits 15, 16: the operand's rows run along memory
+          const uint32_t idesc = idesc0 | (d.a_mn ? 1u << 15 : 0u) | (d.b_mn ? 1u << 16 : 0u);
+          const uint64_t a_desc0 = d.a_mn ? ptx::umma_desc_mn128(smem0, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0);
+          const uint64_t b_desc0 = d.b_mn ? ptx::umma_desc_mn128(smem0 + a_bytes, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0 + a_bytes);
+          // 16 further along K: 32 bytes inside the swizzled row, or 16 rows of 128 bytes (addresses count 16 bytes)
+          const uint32_t a_step = d.a_mn ? 2048 >> 4 : 32 >> 4, b_step = d.b_mn ? 2048 >> 4 : 32 >> 4;
+          // fp32: the unit is summed in parts, each through an accumulator of its own
+          for (int begin = t.k0; begin < t.k1 && ok; ++tl) {
+            const int end = F32 ? part_end(d, t, begin) : t.k1;
+            const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
+            ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aph ^ 1, abort_flag) ? 1 : 0, 0) != 0;
             if (!ok) break;
             ptx::tc_fence_after();
-            const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
-            const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
-            if (ptx::elect_one()) {
-#pragma unroll
-              for (int k = 0; k < BLOCK_K / 16; ++k)
-                ptx::umma_bf16_pair(d_tmem, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb > begin || k > 0) ? 1u : 0u);
-              ptx::umma_commit_pair(&empty[s]);
+            const uint32_t d_tmem = tmem_base + acc * TILE_N;
+            for (int kb = begin; kb < end; ++kb) {
+              ok = ptx::mbar_wait_warp(&full[s], ph, abort_flag);
+              if (!ok) break;
+              ptx::tc_fence_after();
+              const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
+              const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
+              if (ptx::elect_one()) {
+  #pragma unroll
+                for (int k = 0; k < BLOCK_K / 16; ++k)
+                  ptx::umma_bf16_pair(d_tmem, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb > begin || k > 0) ? 1u : 0u);
+                ptx::umma_commit_pair(&empty[s]);
+              }
+              __syncwarp();
+              if (++s == stages) { s = 0; ph ^= 1u; }
             }
-            __syncwarp();
-            if (++s == stages) { s = 0; ph ^= 1u; }
+            if (ok) {
+              if (ptx::elect_one()) ptx::umma_commit_pair(&tfull[acc]);
+              __syncwarp();
+            }
+            begin = end;
           }
-          if (ok) {
-            if (ptx::elect_one()) ptx::umma_commit_pair(&tfull[acc]);
-            __syncwarp();
+        }
+        if (!ok) {
+          // wait (bounded) until the MMAs issued so far have retired before tensor memory is freed
+          if (ptx::elect_one()) {
+            ptx::umma_commit_pair(drain);
+            const long long t0 = clock64();
+            while (!ptx::mbar_try_wait(drain, 0) && clock64() - t0 < ptx::kWaitLimitCycles / 8) {}
           }
-          begin = end;
+          __syncwarp();
         }
-      }
-      if (!ok) {
-        // wait (bounded) until the MMAs issued so far have retired before tensor memory is freed
-        if (ptx::elect_one()) {
-          ptx::umma_commit_pair(drain);
-          const long long t0 = clock64();
-          while (!ptx::mbar_try_wait(drain, 0) && clock64() - t0 < ptx::kWaitLimitCycles / 8) {}
-        }
-        __syncwarp();
       }
     }
   } else {
+    if constexpr (F32) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
     // -------------------------------------------------------------- epilogue warps
     constexpr bool LOADS = MODE == BACKWARD_GATED || MODE == BACKWARD_ACT;
     const int q = warp & 3;                             // tensor-memory lane quarter
     constexpr int GROUPS = EPI_WARPS<MODE, F32> / 4;
     const int cols = out_n / GROUPS;                    // output columns of this warp's part of the tile
-    const int col0 = ((warp - 2) >> 2) * cols;
+    const int col0 = ((warp - FIRST_EPI<F32>) >> 2) * cols;
     const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + col0;
-    uint32_t* buf = reinterpret_cast<uint32_t*>(out_stage + (warp - 2) * OUT_BYTES<MODE, F32>);
+    uint32_t* buf = reinterpret_cast<uint32_t*>(out_stage + (warp - FIRST_EPI<F32>) * OUT_BYTES<MODE, F32>);
     Walk walk;
     uint32_t tl = 0;
     bool live = true;
@@ -1105,6 +1115,13 @@ ffsplit_status launch_mode(ffsplit_ctx* ctx, Params<CAP>& p, const JoinParams& j
   if (!(ctx->attr_train_set & bit)) {
     const cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
     if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(train_gemm_kernel)");
+    if (F32) {
+      // the split of registers in the kernel counts on what the block starts with
+      cudaFuncAttributes attr;
+      const cudaError_t a = cudaFuncGetAttributes(&attr, train_gemm_kernel<MODE, F32, CAP>);
+      if (a != cudaSuccess) return check_cuda(ctx, a, "cudaFuncGetAttributes(train_gemm_kernel)");
+      if (attr.numRegs < START_REGS) return fail(ctx, FFSPLIT_ERR_CUDA, "train_gemm_kernel was built with fewer registers than it divides");
+    }
     ctx->attr_train_set |= bit;
   }
   p.stages = RING_BYTES<MODE, F32> / p.stage_bytes < MAX_STAGES ? RING_BYTES<MODE, F32> / p.stage_bytes : MAX_STAGES;
