@@ -4,7 +4,7 @@
 //
 // Bound by memory: the norm reads every element once, the scaling reads and writes it once.  Two launches: the
 // scaling needs the whole norm.  The list travels as a kernel argument (no copy to the device, nothing to keep
-// alive after the call), cut into launches of at most 1024 tensors.  Every tensor is cut into chunks of 16384
+// alive after the call), cut into launches of at most 960 tensors.  Every tensor is cut into chunks of 16384
 // elements from its first 16-byte boundary on; block b takes chunks b, b + grid, ...  The scaling walks them from
 // the last to the first: what the norm read last is still in L2, and the norm reads everything but its last 80 MB so
 // that it does not stay there (508 -> 498 us for twelve 4096 x 11008 bf16 gradients; three passes at the rate of a
@@ -23,7 +23,7 @@ namespace clip {
 
 constexpr int THREADS = 256;
 constexpr int CHUNK = 16384;         // elements
-constexpr int MAX_TENSORS = 1024;    // per launch
+constexpr int MAX_TENSORS = 960;     // per launch: what 32 KB of arguments hold
 constexpr long long KEEP_BYTES = 80ll << 20;
 constexpr int MAX_BLOCKS = 148 * 8; // per launch: 8 resident blocks on each of a B200's SMs
 
@@ -34,6 +34,8 @@ struct Table {
   long long n[CAP];
   int first[CAP + 1];     // first chunk of each tensor
   unsigned char f32[CAP];
+  unsigned short owner[2 * CAP];    // tensor of each chunk, where there are no more chunks than this (many small tensors:
+                                    // every step of a search is a load that waits for the one before)
   int count;
   int keep;               // the norm reads this many chunks, the last ones, so that they stay in L2
 };
@@ -52,9 +54,10 @@ struct Piece {      // the elements [head, body, tail) of one chunk: body starts
   long long begin, body, body_end, end;
 };
 
-// Tensor of chunk c (binary search over the first chunks) and the chunk's range.
+// Tensor of chunk c (from the list, or by binary search over the first chunks) and the chunk's range.
 template <int CAP>
 __device__ __forceinline__ int find_tensor(const Table<CAP>& t, int c) {
+  if (t.first[t.count] <= 2 * CAP) return t.owner[c];
   int lo = 0, hi = t.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -278,7 +281,9 @@ int fill_table(clip::Table<CAP>* tab, const ffsplit_grad_tensor* t, int n, bool 
     tab->f32[j] = t[i].dtype == FFSPLIT_F32 ? 1 : 0;
     tab->first[j] = chunks;
     bytes += t[i].n * es;
-    chunks += body > clip::CHUNK ? static_cast<int>((body + clip::CHUNK - 1) / clip::CHUNK) : 1;
+    const int mine = body > clip::CHUNK ? static_cast<int>((body + clip::CHUNK - 1) / clip::CHUNK) : 1;
+    for (int c = chunks; c < chunks + mine && c < 2 * CAP; ++c) tab->owner[c] = static_cast<unsigned short>(j);
+    chunks += mine;
   }
   tab->first[tab->count] = chunks;
   tab->keep = chunks > 0 ? static_cast<int>(clip::KEEP_BYTES * chunks / (bytes > 0 ? bytes : 1) < chunks ? clip::KEEP_BYTES * chunks / bytes : chunks) : 0;
@@ -309,6 +314,7 @@ ffsplit_status clip_dispatch(ffsplit_ctx* ctx, const ffsplit_grad_tensor* t, int
   // the argument block is copied with every launch: a short list gets a short one
   if (n <= 32) return clip_launch<32>(ctx, t, n, phase, partial, blocks, total, max_norm, norm, st);
   if (n <= 256) return clip_launch<256>(ctx, t, n, phase, partial, blocks, total, max_norm, norm, st);
+  if (n <= 512) return clip_launch<512>(ctx, t, n, phase, partial, blocks, total, max_norm, norm, st);
   return clip_launch<clip::MAX_TENSORS>(ctx, t, n, phase, partial, blocks, total, max_norm, norm, st);
 }
 
