@@ -119,9 +119,9 @@ struct SumJob {
 struct SumArgs {
   SumJob job[2];
   int n;
-  int* tickets;            // one to a block of columns of either job
+  int* tickets;            // one to a block of columns of a job whose rows are cut, SUM_TICKETS to a job
 };
-constexpr int SUM_COLS = 32;
+constexpr int SUM_COLS = 32, SUM_TICKETS = 512;
 // Eight columns c .. c + 7 of one row.
 template <int PLANES>
 __device__ __forceinline__ void add8(const SumJob& j, long long row, int c, float* s) {
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__
     __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
-      int* ticket = a.tickets + (second ? a.job[0].col_blocks : 0) + c0 / SUM_COLS;
+      int* ticket = a.tickets + second * SUM_TICKETS + c0 / SUM_COLS;
       last = atomicAdd(ticket, 1) == j.splits - 1 ? 1 : 0;
       if (last) *ticket = 0;
     }
@@ -219,10 +219,13 @@ namespace {
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Row ranges of a column sum: enough blocks for two on every SM, but no fewer than 512 rows in each.
+// Row ranges of a column sum: enough blocks for two on every SM, but no fewer than 512 rows in each.  (More than one only
+// where there are fewer than SUM_BLOCKS blocks of columns, so a job needs no more tickets than that.)
+constexpr int SUM_BLOCKS = 2 * 148;
+static_assert(SUM_BLOCKS <= train::SUM_TICKETS && 2 * train::SUM_TICKETS <= kMaxTicketTiles, "tickets of the column sums");
 int sum_splits(long long rows, int cols) {
   const long long col_blocks = (cols + train::SUM_COLS - 1) / train::SUM_COLS;
-  long long n = (2 * 148 + col_blocks - 1) / col_blocks;
+  long long n = (SUM_BLOCKS + col_blocks - 1) / col_blocks;
   if (n > (rows + 511) / 512) n = (rows + 511) / 512;
   return static_cast<int>(n < 1 ? 1 : n);
 }
@@ -429,7 +432,7 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
     };
     if (grads.db1) add(h.dG, grads.db1, p.L.ldm, T * p.L.ldm, m, p.f32() ? 3 : 1);
     if (grads.db2) add(dY, grads.db2, d, 0, d, p.f32() ? 0 : 1);
-    a.tickets = ctx->tickets();     // (columns are only cut along the rows where there are fewer blocks of them than tickets)
+    a.tickets = ctx->tickets();
     const cudaError_t e = p.f32() ? launch_pdl(train::column_sum_kernel<true>, dim3(blocks), dim3(256), 0, st, a)
                                   : launch_pdl(train::column_sum_kernel<false>, dim3(blocks), dim3(256), 0, st, a);
     ctx->launches++;

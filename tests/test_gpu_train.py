@@ -209,6 +209,31 @@ def test_a_non_finite_token_stays_in_its_row(ctx, dtype, bad):
     assert not torch.isfinite(got["dW1"][5]).any()
 
 
+def test_bias_gradients_of_a_very_wide_layer(ctx):
+    """More blocks of columns for db1 than there are tickets, while db2's rows are cut."""
+    import paper_2401_04044_b200 as ff
+    d, m, T = 8, 530_000, 520
+    g = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda s, *dims: (torch.randn(*dims, generator=g, device="cuda") * s).bfloat16()  # noqa: E731
+    X, W1, W2, dY = new(1.0, T, d), new(0.3, d, m), new(0.01, m, d), new(0.01, T, d)
+    shape = ff.make_shape(d, m, "gelu_tanh", torch.bfloat16)
+    saved_bytes, ws = ctx.train_sizes(shape, T)
+    ctx.ensure_workspace(ws)
+    saved = torch.empty(saved_bytes, dtype=torch.uint8, device="cuda")
+    Y, db1, db2 = torch.empty_like(X), torch.full((m,), 7.0, device="cuda").bfloat16(), torch.full((d,), 7.0, device="cuda").bfloat16()
+    for _ in range(2):
+        ctx.train_forward(shape, W1, None, W2, None, X, Y, saved=saved)
+        ctx.train_backward(shape, W1, None, W2, X, saved, dY, db1=db1, db2=db2)
+    ctx.poll()
+    want = dY.double().sum(0)
+    assert float((db2.double() - want).norm() / want.norm()) <= NORM_TOL["bf16"]
+    some = torch.arange(0, m, 997, device="cuda")
+    z = (X.double() @ W1[:, some].double()).requires_grad_()
+    torch.nn.functional.gelu(z, approximate="tanh").backward(dY.double() @ W2[some].double().t())
+    want = z.grad.sum(0)
+    assert float((db1[some].double() - want).norm() / want.norm()) <= NORM_TOL["bf16"]
+
+
 def test_directional_differences(ctx):
     """<gradient, direction> against central differences of the loss sum(Y * dY), fp32.  The direction is the
     gradient's own, scaled to a step of 1 % of the tensor: third-order terms are 1e-4 relative, the rounding of the
