@@ -105,16 +105,17 @@ __global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_cons
   }
 }
 
-// Bias gradients: out[c] = sum over rows of in[r, c], in fp32 and in a fixed order.  Bound by reading dZ and dY once.  A
-// block takes 32 columns (four threads to a row, 64 rows at a time, eight of those in flight).  Where there are few columns
-// and many rows the rows are cut: each block leaves a partial, and the block that is the last of its columns to arrive (a
-// ticket, zero again afterwards) adds them in order.
+// Bias gradients: out[c] = sum over rows of in[r, c], in fp32 and in a fixed order.  db2 sums the rows of dY; for db1 the
+// launch of dH leaves sums of dZ over 32 rows (in fp32, before dZ is rounded: rounded terms that cancel left up to ten times
+// the error) and this adds those.  Bound by reading its input once.  A block takes 32 columns (four threads to a row, 64 rows
+// at a time, eight of those in flight).  Where there are few columns and many rows the rows are cut: each block leaves a
+// partial, and the block that is the last of its columns to arrive (a ticket, zero again afterwards) adds them in order.
 struct SumJob {
-  const void* in;          // `planes` bf16 planes that add up, or (planes = 0) fp32 values
+  const void* in;          // bf16, or fp32 with f32_in; [rows, cols], pitch ld
   void* out;               // bf16, or fp32 with f32_out
   float* partial;          // [splits][cols]
-  long long rows, ld, plane_stride, rows_per;
-  int cols, planes, f32_out, splits, col_blocks, block0;
+  long long rows, ld, rows_per;
+  int cols, f32_in, f32_out, splits, col_blocks, block0;
 };
 struct SumArgs {
   SumJob job[2];
@@ -123,9 +124,9 @@ struct SumArgs {
 };
 constexpr int SUM_COLS = 32, SUM_TICKETS = 512;
 // Eight columns c .. c + 7 of one row.
-template <int PLANES>
+template <bool F32>
 __device__ __forceinline__ void add8(const SumJob& j, long long row, int c, float* s) {
-  if constexpr (PLANES == 0) {
+  if constexpr (F32) {
     const float* p = static_cast<const float*>(j.in) + row * j.ld + c;
     if (c + 8 <= j.cols && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
 #pragma unroll
@@ -137,32 +138,28 @@ __device__ __forceinline__ void add8(const SumJob& j, long long row, int c, floa
 #pragma unroll
       for (int i = 0; i < 8; ++i) if (c + i < j.cols) s[i] += __ldg(p + i);
     }
-  } else {
+  } else {      // (the pitch of a bf16 matrix is a multiple of 8)
+    const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(j.in) + row * j.ld + c));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int k = 0; k < PLANES; ++k) {      // (a last group of eight ends inside the row's padding)
-      const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(j.in) + k * j.plane_stride + row * j.ld + c));
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[2 * i] += __uint_as_float(w[i] << 16);
-        s[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
-      }
+    for (int i = 0; i < 4; ++i) {
+      s[2 * i] += __uint_as_float(w[i] << 16);
+      s[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
     }
   }
 }
 // Rows begin, begin + 64, ... of eight columns.
-template <int PLANES>
+template <bool F32>
 __device__ __forceinline__ void sum_rows(const SumJob& j, long long begin, long long end, int c, float* s) {
   long long r = begin;
   for (; r + 448 < end; r += 512) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) add8<PLANES>(j, r + 64 * k, c, s);
+    for (int k = 0; k < 8; ++k) add8<F32>(j, r + 64 * k, c, s);
   }
 #pragma unroll
   for (int k = 0; k < 7; ++k)
-    if (r + 64 * k < end) add8<PLANES>(j, r + 64 * k, c, s);
+    if (r + 64 * k < end) add8<F32>(j, r + 64 * k, c, s);
 }
-template <bool F32>
 __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ SumArgs a) {
   __shared__ float red[8][SUM_COLS];
   __shared__ int last;
@@ -175,9 +172,8 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__
   float s[8] = {};
   if (mine < j.cols) {
     const long long r = begin + (threadIdx.x >> 2);
-    if constexpr (!F32) sum_rows<1>(j, r, end, mine, s);
-    else if (j.planes == 0) sum_rows<0>(j, r, end, mine, s);
-    else sum_rows<3>(j, r, end, mine, s);
+    if (j.f32_in) sum_rows<true>(j, r, end, mine, s);
+    else sum_rows<false>(j, r, end, mine, s);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -236,7 +232,7 @@ int sum_splits(long long rows, int cols) {
 struct TrainLayout {
   long long ldm, ldd;
   size_t savedH, saved;
-  size_t H, dG, dU, W1, W1u, W2, X, dY, sums, parts, parts_bytes, end;
+  size_t H, dG, dU, W1, W1u, W2, X, dY, sums, groups, parts, parts_bytes, end;
 };
 TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   TrainLayout L;
@@ -267,6 +263,11 @@ TrainLayout train_layout(const ffsplit_shape& s, long long T) {
   const size_t want = 64 * (a > b ? a : b);
   L.parts_bytes = up256(want < (32u << 20) ? want : (32u << 20));
   L.parts = off; off += L.parts_bytes;
+  // sums of dZ over groups of rows, or every row of it where that launch is joined: its partials, at least two times these
+  // rows, are then no more than parts_bytes
+  const size_t rows = static_cast<size_t>((T + tg::COL_SUM_ROWS - 1) / tg::COL_SUM_ROWS), whole = static_cast<size_t>(T) * L.ldm * 4;
+  L.groups = off;
+  if (!gated) off = up256(off + (whole <= L.parts_bytes / 2 ? whole : rows * L.ldm * 4));
   L.end = off;
   return L;
 }
@@ -334,6 +335,7 @@ struct Pass {
     h.dU = reinterpret_cast<__nv_bfloat16*>(ws + L.dU);
     h.ldm = L.ldm;
     h.plane_stride = T * L.ldm;
+    h.col_sums = nullptr;
     return h;
   }
   ffsplit_status prepare() {
@@ -379,7 +381,9 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
   Pass p(ctx, s, T, st);
   const int d = s.d, m = s.m;
   const bool inner = grads.dX || grads.dW1 || grads.dW1u || grads.db1 || grads.dW2;   // anything that needs dH or H
-  const tg::Hidden h = p.buffers(const_cast<char*>(saved));
+  tg::Hidden h = p.buffers(const_cast<char*>(saved));
+  if (grads.db1) h.col_sums = reinterpret_cast<float*>(p.ws + p.L.groups);
+  bool joined = false;
   const tg::Matrix H = p.hidden(h.H), dG = p.hidden(h.dG), dU = p.hidden(h.dU);
   tg::Product out[4];
   int n = 0;
@@ -410,7 +414,9 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
     }
     if ((r = p.prepare()) != FFSPLIT_OK) return r;
     const tg::Product g = product(dy, 0, w2, 0, T, m, d);
-    if ((r = tg::launch(ctx, p.gated() ? tg::BACKWARD_GATED : tg::BACKWARD_ACT, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st)) != FFSPLIT_OK) return r;
+    if ((r = tg::launch(ctx, p.gated() ? tg::BACKWARD_GATED : tg::BACKWARD_ACT, s.act, p.f32(), &g, 1, h, p.ws + p.L.parts, p.L.parts_bytes, st,
+                        &joined)) != FFSPLIT_OK)
+      return r;
     if ((grads.dX || grads.dW1 || grads.dW1u || grads.dW2) && (r = tg::launch(ctx, tg::PLAIN, s.act, p.f32(), out, n, h, p.ws + p.L.parts, p.L.parts_bytes, st)) != FFSPLIT_OK) return r;
   }
   if (grads.db1 || grads.db2) {
@@ -418,23 +424,22 @@ ffsplit_status run_train_backward(ffsplit_ctx* ctx, const ffsplit_shape& s, cons
     std::memset(&a, 0, sizeof(a));
     int blocks = 0;
     float* partial = reinterpret_cast<float*>(p.ws + p.L.sums);
-    const auto add = [&](const void* in, void* to, long long ld, long long plane_stride, int n_cols, int planes) {
+    const auto add = [&](const void* in, bool f32_in, void* to, long long rows, long long ld, int n_cols) {
       train::SumJob& j = a.job[a.n++];
       j.in = in; j.out = to; j.partial = partial;
-      j.rows = T; j.ld = ld; j.plane_stride = plane_stride;
-      j.cols = n_cols; j.planes = planes; j.f32_out = p.f32() ? 1 : 0;
+      j.rows = rows; j.ld = ld;
+      j.cols = n_cols; j.f32_in = f32_in ? 1 : 0; j.f32_out = p.f32() ? 1 : 0;
       j.col_blocks = (n_cols + train::SUM_COLS - 1) / train::SUM_COLS;
-      j.splits = sum_splits(T, n_cols);
-      j.rows_per = (T + j.splits - 1) / j.splits;
+      j.splits = sum_splits(rows, n_cols);
+      j.rows_per = (rows + j.splits - 1) / j.splits;
       j.block0 = blocks;
       blocks += j.splits * j.col_blocks;
       partial += static_cast<size_t>(j.splits) * n_cols;
     };
-    if (grads.db1) add(h.dG, grads.db1, p.L.ldm, T * p.L.ldm, m, p.f32() ? 3 : 1);
-    if (grads.db2) add(dY, grads.db2, d, 0, d, p.f32() ? 0 : 1);
+    if (grads.db1) add(h.col_sums, true, grads.db1, joined ? T : (T + tg::COL_SUM_ROWS - 1) / tg::COL_SUM_ROWS, p.L.ldm, m);
+    if (grads.db2) add(dY, p.f32(), grads.db2, T, d, d);
     a.tickets = ctx->tickets();
-    const cudaError_t e = p.f32() ? launch_pdl(train::column_sum_kernel<true>, dim3(blocks), dim3(256), 0, st, a)
-                                  : launch_pdl(train::column_sum_kernel<false>, dim3(blocks), dim3(256), 0, st, a);
+    const cudaError_t e = launch_pdl(train::column_sum_kernel, dim3(blocks), dim3(256), 0, st, a);
     ctx->launches++;
     return check_cuda(ctx, e, "column_sum_kernel launch");
   }

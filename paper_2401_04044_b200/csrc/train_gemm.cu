@@ -425,6 +425,25 @@ __device__ __forceinline__ void store_hidden16(const Hidden& h, long long row, i
     if (MODE == BACKWARD_GATED) store16_planes<F32>(h.dU + at, h.plane_stride, y);
   }
 }
+__device__ __forceinline__ void pairs_back16(const float2* x, float* v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { v[2 * i] = x[i].x; v[2 * i + 1] = x[i].y; }
+}
+// Column sums over the warp's 32 rows (a lane to a row) of 16 columns, in a fixed order: lane l has that of column l / 2.
+__device__ __forceinline__ float column_sums16(const float2* x, int lane) {
+  float v[16];
+  pairs_back16(x, v);
+#pragma unroll
+  for (int half = 8, bit = 16; half >= 1; half >>= 1, bit >>= 1) {
+    const bool upper = (lane & bit) != 0;
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const float send = upper ? v[i] : v[i + half], keep = upper ? v[i + half] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+    }
+  }
+  return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
+}
 __device__ __forceinline__ void pairs16(const float* v, float2* x) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = make_float2(v[2 * i], v[2 * i + 1]);
@@ -800,6 +819,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
             activate16<MODE, F32>(p.hid, p.act, row, n0, x, y, kept, in);
             // what was kept of the next columns is on its way while these leave
             if (LOADS && in && c + 16 < width) kept.load(p.hid, row, n0 + 16);
+            if (MODE == BACKWARD_ACT && p.hid.col_sums) {
+              if (!in) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = make_float2(0.f, 0.f);
+              }
+              const float sum = column_sums16(x, lane);
+              if (rows > 0 && (lane & 1) == 0) p.hid.col_sums[(row0 / COL_SUM_ROWS) * p.hid.ldm + n0 + (lane >> 1)] = sum;
+            }
           }
           if (MODE != PLAIN && F32) {
             if (in) store_hidden16<MODE, F32>(p.hid, row, n0, x, y);
@@ -973,6 +1000,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
     pairs16(w, y);
     activate16<MODE, F32>(p.hid, p.act, row, n0, x, y, kept, true);
     store_hidden16<MODE, F32>(p.hid, row, n0, x, y);
+    if (MODE == BACKWARD_ACT && p.hid.col_sums) {
+      pairs_back16(x, v);
+      store16_f32(p.hid.col_sums + row * p.hid.ldm + n0, v);
+    }
   }
 }
 
@@ -1136,7 +1167,7 @@ ffsplit_status launch_mode(ffsplit_ctx* ctx, Params<CAP>& p, const JoinParams& j
 // CAP: products that the argument block has room for (it is copied with every launch).
 template <int CAP>
 ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden,
-                               char* partials, size_t partial_room, cudaStream_t st) {
+                               char* partials, size_t partial_room, cudaStream_t st, bool* joined) {
   // The tensor maps are made by a driver call, which needs a current context; a thread that has only asked the runtime for
   // its device (autograd's backward threads) has none yet.
   const cudaError_t bound = cudaSetDevice(ctx->device);
@@ -1244,6 +1275,7 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
   p.status = ctx->status();
   join.act = act;
   join.hid = hidden;
+  if (joined) *joined = join.n > 0;
   if constexpr (CAP > 1) {
     return f32 ? launch_mode<PLAIN, true>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false>(ctx, p, join, clusters, st);
   } else {
@@ -1264,9 +1296,9 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
 }  // namespace
 
 ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, char* partials,
-                      size_t partial_room, cudaStream_t st) {
-  return n == 1 ? launch_products<1>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st)
-                : launch_products<MAX_PRODUCTS>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st);
+                      size_t partial_room, cudaStream_t st, bool* joined) {
+  return n == 1 ? launch_products<1>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st, joined)
+                : launch_products<MAX_PRODUCTS>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st, joined);
 }
 
 }  // namespace tg

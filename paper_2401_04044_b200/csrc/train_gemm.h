@@ -46,7 +46,9 @@ struct Hidden {
   void* kept;
   __nv_bfloat16 *H, *dG, *dU;
   long long ldm, plane_stride;
+  float* col_sums;       // BACKWARD_ACT, or nullptr: sums of dZ before it is rounded, [row groups][ldm], for db1
 };
+constexpr int COL_SUM_ROWS = 32;   // rows of a group; one row where the launch was joined
 // Bytes of what is kept of G and U, or of Z: 20 bits each, all 32 in fp32 layers; whole blocks of 32 rows.
 inline size_t kept_bytes(long long T, long long ldm, bool gated, bool f32) {
   return static_cast<size_t>((T + 31) / 32 * 32) * ldm * (gated ? 2 : 1) * (f32 ? 8 : 5) / 2;
@@ -90,8 +92,9 @@ __device__ __forceinline__ void split3_pair(float x, float y, uint32_t* w) {
 
 // Up to four PLAIN products (or one of the other modes) as one launch, or as two where K is cut.  f32: three-plane
 // operands and fp32 outputs.  partials: scratch for the fp32 partials of products that are cut along K.
+// joined (may be nullptr): whether that was done.
 ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, char* partials,
-                      size_t partial_room, cudaStream_t st);
+                      size_t partial_room, cudaStream_t st, bool* joined = nullptr);
 
 }  // namespace tg
 }  // namespace ffsp
