@@ -406,6 +406,14 @@ class Context:
             raise FFSplitError(1, where, f"{name} must be on cuda:{self.device}")
         return t.data_ptr()
 
+    def _saved(self, where: str, saved):
+        """Address and size of what the forward pass keeps."""
+        if saved is None:
+            return None, 0
+        if saved.get_device() != self.device or not saved.is_contiguous():
+            raise FFSplitError(1, where, f"saved must be contiguous and on cuda:{self.device}")
+        return saved.data_ptr(), saved.nbytes
+
     def _train_weights(self, where, shape, W1, W1u, b1, W2, b2):
         d, m, op, dt = shape.d, shape.m, self._operand, DTYPES[shape.dtype]
         return Weights(op(where, "W1", W1, dt, (d, m), False), op(where, "W1u", W1u, dt, (d, m)), op(where, "b1", b1, dt, (m,)),
@@ -424,8 +432,8 @@ class Context:
         where, T, d, dt = "ffsplit_train_forward", X.shape[0], shape.d, DTYPES[shape.dtype]
         w = self._train_weights(where, shape, W1, W1u, b1, W2, b2)
         rc = self.lib.ffsplit_train_forward(
-            self.h, shape, w, self._operand(where, "X", X, dt, (T, d), False), T, None if saved is None else saved.data_ptr(),
-            0 if saved is None else saved.nbytes, self._operand(where, "Y", Y, dt, (T, d), False), _stream_of(stream, self.device))
+            self.h, shape, w, self._operand(where, "X", X, dt, (T, d), False), T, *self._saved(where, saved),
+            self._operand(where, "Y", Y, dt, (T, d), False), _stream_of(stream, self.device))
         if rc:
             self._check(rc, where)
 
@@ -437,8 +445,8 @@ class Context:
         g = TrainGrads(op(where, "dX", dX, dt, (T, d)), op(where, "dW1", dW1, dt, (d, m)), op(where, "dW1u", dW1u, dt, (d, m)),
                        op(where, "db1", db1, dt, (m,)), op(where, "dW2", dW2, dt, (m, d)), op(where, "db2", db2, dt, (d,)))
         rc = self.lib.ffsplit_train_backward(
-            self.h, shape, w, op(where, "X", X, dt, (T, d), False), T, None if saved is None else saved.data_ptr(),
-            0 if saved is None else saved.nbytes, op(where, "dY", dY, dt, (T, d), False), g, _stream_of(stream, self.device))
+            self.h, shape, w, op(where, "X", X, dt, (T, d), False), T, *self._saved(where, saved),
+            op(where, "dY", dY, dt, (T, d), False), g, _stream_of(stream, self.device))
         if rc:
             self._check(rc, where)
 

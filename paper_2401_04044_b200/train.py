@@ -11,20 +11,21 @@ was rounded from, and takes the result through the library's own path: score, se
 from __future__ import annotations
 
 import argparse
-from typing import Iterable, Optional
+from typing import Iterable, Optional, Union
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from .binding import Context, GradList, Shape, make_shape
 
 
 class _FFN(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, lib: Context, shape: Shape, X, W1, W1u, b1, W2, b2):
+    def forward(ctx, lib: Context, shape: Shape, grad_mode: bool, X, W1, W1u, b1, W2, b2):
         T = X.shape[0]
         saved_bytes, workspace = lib.train_sizes(shape, T)
         lib.ensure_workspace(workspace)
-        keep = any(ctx.needs_input_grad)
+        keep = grad_mode and any(ctx.needs_input_grad)
         saved = torch.empty(saved_bytes, dtype=torch.uint8, device=X.device) if keep else None
         Y = torch.empty_like(X)
         lib.train_forward(shape, W1, b1, W2, b2, X, Y, saved=saved, W1u=W1u)
@@ -33,30 +34,33 @@ class _FFN(torch.autograd.Function):
         return Y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY):
         X, W1, W1u, W2, saved = ctx.saved_tensors
         lib, shape = ctx.lib, ctx.shape
         lib.ensure_workspace(lib.train_sizes(shape, X.shape[0])[1])
-        _, _, need_X, need_W1, need_W1u, need_b1, need_W2, need_b2 = ctx.needs_input_grad
+        _, _, _, need_X, need_W1, need_W1u, need_b1, need_W2, need_b2 = ctx.needs_input_grad
         new = lambda need, *dims: torch.empty(dims, dtype=X.dtype, device=X.device) if need else None  # noqa: E731
         d, m = shape.d, shape.m
         g = {"dX": new(need_X, *X.shape), "dW1": new(need_W1, d, m), "dW1u": new(need_W1u and ctx.has[0], d, m),
              "db1": new(need_b1 and ctx.has[1], m), "dW2": new(need_W2, m, d), "db2": new(need_b2 and ctx.has[2], d)}
         lib.train_backward(shape, W1, None, W2, X, saved, dY.contiguous(), W1u=W1u, **g)
-        return None, None, g["dX"], g["dW1"], g["dW1u"], g["db1"], g["dW2"], g["db2"]
+        return None, None, None, g["dX"], g["dW1"], g["dW1u"], g["db1"], g["dW2"], g["db2"]
 
 
 def ffn(lib: Context, shape: Shape, X, W1, W2, b1=None, b2=None, W1u=None) -> torch.Tensor:
-    """act(X W1 + b1) W2 + b2, or (SiLU(X W1) * (X W1u)) W2 + b2, differentiable in X and the weights.  X [T, d] and the
-    weights are contiguous tensors of the layer's type on the context's device; the calls run on the current stream."""
-    return _FFN.apply(lib, shape, X, W1, W1u, b1, W2, b2)
+    """act(X W1 + b1) W2 + b2, or (SiLU(X W1) * (X W1u)) W2 + b2, differentiable once in X and the weights.  X [T, d] and
+    the weights are contiguous tensors of the layer's type on the context's device; the calls run on the current stream."""
+    return _FFN.apply(lib, shape, torch.is_grad_enabled(), X, W1, W1u, b1, W2, b2)
 
 
-def clip_grad_norm_(lib: Context, parameters: Iterable[torch.Tensor], max_norm: float,
+def clip_grad_norm_(lib: Context, parameters: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float,
                     norm: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scales the parameters' gradients in place so that their norm is at most max_norm; returns the norm (float32[1] on
-    the device, not waited for).  A non-finite norm leaves the gradients as they are and is reported by lib.poll()."""
-    grads = [p.grad for p in parameters if p.grad is not None]
+    the device, not waited for).  A parameter that is named twice counts once.  A non-finite norm leaves the gradients as
+    they are and is reported by lib.poll()."""
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else parameters
+    grads = [p.grad for p in {id(p): p for p in parameters}.values() if p.grad is not None]
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device=f"cuda:{lib.device}")
     lib.ensure_workspace(lib.grad_workspace_size(len(grads)))

@@ -467,6 +467,41 @@ def test_autograd_function_matches_the_calls(ctx, act):
     assert torch.equal(X.grad.cpu(), want["dX"])
 
 
+def test_autograd_function_keeps_nothing_without_grad_and_has_no_second_derivative(ctx):
+    from paper_2401_04044_b200 import make_shape
+    from paper_2401_04044_b200.train import ffn
+    D = {k: None if v is None else v.cuda().requires_grad_(k == "X") for k, v in draw("swiglu", "bf16", 256, 512, 2000).items()}
+    shape = make_shape(256, 512, "swiglu", torch.bfloat16)
+    call = lambda: ffn(ctx, shape, D["X"], D["W1"], D["W2"], W1u=D["W1u"])  # noqa: E731
+    want = call()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.max_memory_allocated()
+    with torch.no_grad():
+        Y = call()
+    assert torch.equal(Y, want.detach())
+    assert torch.cuda.max_memory_allocated() - before < ctx.train_sizes(shape, 2000)[0]
+    (g,) = torch.autograd.grad(want, D["X"], D["dY"].requires_grad_(), create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.float().sum().backward()
+
+
+def test_saved_has_to_lie_on_the_device(ctx):
+    import paper_2401_04044_b200 as ff
+    L = {k: None if v is None else v.cuda() for k, v in draw("swiglu", "bf16", 64, 96, 10).items()}
+    shape = ff.make_shape(64, 96, "swiglu", torch.bfloat16)
+    saved_bytes, ws = ctx.train_sizes(shape, 10)
+    ctx.ensure_workspace(ws)
+    before = ctx.launch_count()
+    host, gaps = torch.empty(saved_bytes, dtype=torch.uint8), torch.empty(2 * saved_bytes, dtype=torch.uint8, device="cuda")[::2]
+    for saved in (host, gaps):
+        for call in (lambda: ctx.train_forward(shape, L["W1"], None, L["W2"], None, L["X"], torch.empty_like(L["X"]), saved=saved, W1u=L["W1u"]),
+                     lambda: ctx.train_backward(shape, L["W1"], None, L["W2"], L["X"], saved, L["dY"], dX=torch.empty_like(L["X"]), W1u=L["W1u"])):
+            with pytest.raises(ff.FFSplitError) as e:
+                call()
+            assert e.value.code == 1
+    assert ctx.launch_count() == before
+
+
 def test_calls_from_a_thread_that_has_used_no_gpu(ctx):
     """Autograd runs backward passes on threads of its own, on which no CUDA context is current yet."""
     import threading
@@ -488,6 +523,19 @@ def test_clip_grad_norm_in_place(ctx):
     ctx.poll()
     assert abs(float(norm) - want) <= 5e-7 * want
     assert abs(norm64([p.grad for p in ps[:2]]) - 0.5) < 2e-3
+
+
+def test_clip_grad_norm_of_one_tensor_and_of_a_tied_parameter(ctx):
+    from paper_2401_04044_b200.train import clip_grad_norm_
+    p = torch.nn.Parameter(torch.zeros(40, 25, device="cuda"))
+    g = torch.randn(40, 25, device="cuda")
+    want = norm64([g])
+    for parameters in (p, [p, p]):
+        p.grad = g.clone()
+        norm = clip_grad_norm_(ctx, parameters, 0.5)
+        ctx.poll()
+        assert abs(float(norm) - want) <= 5e-7 * want
+        assert abs(norm64([p.grad]) - 0.5) < 1e-5
 
 
 @pytest.mark.parametrize("act", ["swiglu", "gelu_tanh"])
