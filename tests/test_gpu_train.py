@@ -485,6 +485,46 @@ def test_autograd_function_keeps_nothing_without_grad_and_has_no_second_derivati
         g.float().sum().backward()
 
 
+@pytest.mark.parametrize("dtype,act,T", [("bf16", "swiglu", 90), ("bf16", "gelu_erf", 700), ("f32", "gelu_tanh", 33)])
+def test_a_captured_pass_reads_its_inputs_anew(ctx, dtype, act, T):
+    """Forward, backward and clipping as one CUDA graph, replayed on other inputs than it was captured with."""
+    import paper_2401_04044_b200 as ff
+    d, m = 72, 203
+    first, other = ({k: None if v is None else v.cuda() for k, v in draw(act, dtype, d, m, T).items()} for _ in range(2))
+    for k in other:
+        if other[k] is not None:
+            other[k] = (other[k].float() * -0.75).to(DT[dtype])
+    shape = ff.make_shape(d, m, act, DT[dtype])
+    saved_bytes, ws = ctx.train_sizes(shape, T)
+    ctx.ensure_workspace(max(ws, ctx.grad_workspace_size(3)))
+    saved, Y, norm = torch.empty(saved_bytes, dtype=torch.uint8, device="cuda"), torch.empty_like(first["X"]), torch.zeros(1, device="cuda")
+    g = {"d" + k: torch.empty_like(first[k]) for k in ("X", "W1", "W1u", "b1", "W2", "b2")
+         if first[k] is not None and not (act == "swiglu" and k == "b1")}
+    grads = ctx.grad_list([g["dX"], g["dW1"], g["dW2"]])
+
+    def step():
+        ctx.train_forward(shape, first["W1"], first["b1"], first["W2"], first["b2"], first["X"], Y, saved=saved, W1u=first["W1u"])
+        ctx.train_backward(shape, first["W1"], None, first["W2"], first["X"], saved, first["dY"], W1u=first["W1u"], **g)
+        ctx.clip_grads(grads, 0.5, norm)
+
+    step()      # sets the kernels' attributes, which a capture may not
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k, v in first.items():
+        if v is not None:
+            v.copy_(other[k])
+    step()
+    want = {k: v.clone() for k, v in {**g, "Y": Y, "norm": norm}.items()}
+    for v in (*g.values(), Y, norm):
+        v.zero_()
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(v, want[k]) for k, v in {**g, "Y": Y, "norm": norm}.items())
+
+
 def test_saved_has_to_lie_on_the_device(ctx):
     import paper_2401_04044_b200 as ff
     L = {k: None if v is None else v.cuda() for k, v in draw("swiglu", "bf16", 64, 96, 10).items()}
