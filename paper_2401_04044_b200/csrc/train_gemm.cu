@@ -832,6 +832,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
             if (in) store_hidden16<MODE, F32>(p.hid, row, n0, x, y);
           } else if (MODE == PLAIN && d.ragged) {
             const int col = c % SPAN;
+            if (c == 0) {
+              // the unit before may have been another product's, whose TMA stores still read the buffer
+              if (lane == 0) ptx::tma_store_wait_read();
+              __syncwarp();
+            }
             stage16<F32>(buf, lane, col, v);
             if (col + 16 == SPAN || c + 16 >= width) {
               __syncwarp();

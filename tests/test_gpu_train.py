@@ -234,6 +234,65 @@ def test_bias_gradients_of_a_very_wide_layer(ctx):
     assert float((db1[some].double() - want).norm() / want.norm()) <= NORM_TOL["bf16"]
 
 
+def ffn64_on_the_device(D, act):
+    """ffn64() with torch, for layers that would take the host long."""
+    z = D["X"] @ D["W1"] + (0 if D["b1"] is None else D["b1"])
+    if act == "swiglu":
+        s = torch.sigmoid(z)
+        a, slope = z * s, s * (1 + z * (1 - s))
+    elif act == "gelu_erf":
+        phi = torch.special.ndtr(z)
+        a, slope = z * phi, phi + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    else:
+        c, k = math.sqrt(2 / math.pi), 0.044715
+        t = torch.tanh(c * (z + k * z ** 3))
+        a, slope = 0.5 * z * (1 + t), 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * c * (1 + 3 * k * z * z)
+    u = None if D["W1u"] is None else D["X"] @ D["W1u"]
+    h = a if u is None else a * u
+    dh = D["dY"] @ D["W2"].t()
+    dz = dh * slope if u is None else dh * slope * u
+    r = {"Y": h @ D["W2"] + (0 if D["b2"] is None else D["b2"]), "dX": dz @ D["W1"].t(), "dW1": D["X"].t() @ dz,
+         "dW2": h.t() @ D["dY"], "db2": D["dY"].sum(0)}
+    if u is not None:
+        r["dX"] += (dh * a) @ D["W1u"].t()
+        r["dW1u"] = D["X"].t() @ (dh * a)
+    else:
+        r["db1"] = dz.sum(0)
+    return r
+
+
+def draw_on_the_device(act, dtype, d, m, T, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(1000 * seed + d + 7 * m + 13 * T)
+    new = lambda s, *shape: (torch.randn(*shape, generator=g, device="cuda") * s).to(DT[dtype])  # noqa: E731
+    gated, w = act == "swiglu", 1.3 / math.sqrt(d)
+    return {"X": new(1.0, T, d), "W1": new(w, d, m), "W1u": new(w, d, m) if gated else None, "b1": None if gated else new(0.2, m),
+            "W2": new(1 / math.sqrt(m), m, d), "b2": new(0.2, d), "dY": new(0.01, T, d)}
+
+
+def check_on_the_device(got, D, act, dtype, tol=None):
+    ref = ffn64_on_the_device({k: None if v is None else v.double() for k, v in D.items()}, act)
+    tol = NORM_TOL[dtype] if tol is None else tol
+    for k, v in got.items():
+        off = v.cuda().double() - ref[k]
+        err, big = float(off.norm() / ref[k].norm()), float(off.abs().max() / ref[k].abs().max())
+        assert err <= tol and big <= 8 * tol, f"{k}: {err:.2e} of the norm (<= {tol}), {big:.2e} of the largest element"
+
+
+@pytest.mark.parametrize("dtype,act,d,m,T", [
+    ("f32", "gelu_erf", 1026, 4096, 128), ("f32", "swiglu", 1001, 4096, 64),                  # dW1, dW1u whole pieces, dW2 not
+    ("bf16", "swiglu", 4416, 517, 71), ("bf16", "gelu_erf", 5120, 20479, 300)])               # dX whole pieces, dW1, dW1u not
+def test_gradients_that_leave_in_both_ways(ctx, dtype, act, d, m, T):
+    """Gradients whose rows start on 16 bytes leave through TMA stores, others word by word, both through the same staging
+    buffers.  Here pairs of CTAs go from a tile of the one kind straight to a short one of the other (59, 54, 24 and 40 times)."""
+    D = draw_on_the_device(act, dtype, d, m, T)
+    first = run(ctx, D, act, dtype)
+    check_on_the_device(first, D, act, dtype)
+    for _ in range(4):
+        again = run(ctx, D, act, dtype)
+        for k in first:
+            assert torch.equal(again[k], first[k]), k
+
+
 def test_directional_differences(ctx):
     """<gradient, direction> against central differences of the loss sum(Y * dY), fp32.  The direction is the
     gradient's own, scaled to a step of 1 % of the tensor: third-order terms are 1e-4 relative, the rounding of the
