@@ -60,7 +60,9 @@ template <int MODE, bool F32> constexpr int THREADS = 32 * (EPI_WARPS<MODE, F32>
 template <int MODE, bool F32>
 constexpr int RING_BYTES = (MAX_SMEM - 1024 - BAR_BYTES - EPI_WARPS<MODE, F32> * OUT_BYTES<MODE, F32>) / 1024 * 1024;
 constexpr int MAX_PRODUCTS = 4;
-constexpr int PROMOTE = 4;   // k-blocks: 16 MMAs, 5e-7 at most
+// k-blocks: 8 MMAs, 2.4e-7 at most.  (Of a 1024 x 2752 gated layer on 1024 tokens 4.0e-7 is left and a pass takes 364 us; 4
+// k-blocks: 7.3e-7 and 333 us.  A 256 x 1024 layer on 128 tokens: 3.0e-7 and 84 us against 5.4e-7 and 78; plain fp32 sums 4.2e-7.)
+constexpr int PROMOTE = 2;
 
 struct Unit {
   int prod, m_blk, n_blk;

@@ -293,6 +293,14 @@ def test_gradients_that_leave_in_both_ways(ctx, dtype, act, d, m, T):
             assert torch.equal(again[k], first[k]), k
 
 
+@pytest.mark.parametrize("act,d,m,T", [("swiglu", 1024, 2752, 1024), ("gelu_erf", 256, 1024, 128), ("gelu_tanh", 640, 4096, 2048)])
+def test_long_fp32_sums(ctx, act, d, m, T):
+    """The tensor cores cut their running sums (3e-8 of the sum to an MMA), so a sum leaves them every eighth MMA: 2.4e-7 of
+    it at most, however long.  Two products in a row and the roundings of 2^-24 in between: 5e-7 of the norm."""
+    D = draw_on_the_device(act, "f32", d, m, T)
+    check_on_the_device(run(ctx, D, act, "f32"), D, act, "f32", tol=5e-7)
+
+
 def test_directional_differences(ctx):
     """<gradient, direction> against central differences of the loss sum(Y * dY), fp32.  The direction is the
     gradient's own, scaled to a step of 1 % of the tensor: third-order terms are 1e-4 relative, the rounding of the
