@@ -17,7 +17,8 @@
  *     is registered, see ffsplit_blob_open()).
  *   - Storage dtype (ffsplit_dtype) applies to X, Y, weights, biases and
  *     factors alike: FFSPLIT_BF16 computes with bf16 tensor-core products and
- *     fp32 accumulation; FFSPLIT_F32 computes in plain fp32 (no TF32).
+ *     fp32 accumulation; FFSPLIT_F32 computes in plain fp32 (no TF32), the training
+ *     calls to the same accuracy on the tensor cores (see there).
  *   - `stream` is a cudaStream_t passed as void* (NULL = default stream).  Calls
  *     enqueue work and return; argument errors are returned synchronously and
  *     launch nothing.  Conditions only the device can see (non-finite score,
@@ -389,8 +390,11 @@ ffsplit_status ffsplit_quant_forward(ffsplit_ctx* ctx, const void* blob, const v
  *   GELU:    Z = X W1 + b1, H = act(Z), Y = H W2 + b2
  * T >= 1 tokens.  Products of bf16 layers are accumulated in fp32; what one product hands to the next (H and the
  * gradients of G, U or Z) is rounded to bf16 once, G, U and Z themselves are kept with at least 12 significant
- * bits.  FFSPLIT_F32 layers keep fp32 accuracy throughout.  An infinity or NaN among the inputs makes the outputs
- * it reaches non-finite (NaN where the formula may give an infinity). */
+ * bits.  FFSPLIT_F32 layers: every matrix is taken as the sum of three bf16 planes (24 bits), a product is the six
+ * largest products of planes with its sums in fp32, and the activations' errors are relative ones of a few units in
+ * the last place.  Outputs are off by a few 1e-7 of their norm, no more than plain fp32 products leave (values below
+ * 2^-110, whose planes are no normal numbers, lose bits).  An infinity or NaN among the inputs makes the outputs it
+ * reaches non-finite (NaN where the formula may give an infinity). */
 
 /* Bytes of `saved` (what the backward pass keeps of the forward pass) and of the workspace that
  * ffsplit_train_forward() and ffsplit_train_backward() need for T tokens of this layer. */

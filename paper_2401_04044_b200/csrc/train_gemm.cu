@@ -61,7 +61,7 @@ template <int MODE, bool F32>
 constexpr int RING_BYTES = (MAX_SMEM - 1024 - BAR_BYTES - EPI_WARPS<MODE, F32> * OUT_BYTES<MODE, F32>) / 1024 * 1024;
 constexpr int MAX_PRODUCTS = 4;
 // k-blocks: 8 MMAs, 2.4e-7 at most.  (Of a 1024 x 2752 gated layer on 1024 tokens 4.0e-7 is left and a pass takes 364 us; 4
-// k-blocks: 7.3e-7 and 333 us.  A 256 x 1024 layer on 128 tokens: 3.0e-7 and 84 us against 5.4e-7 and 78; plain fp32 sums 4.2e-7.)
+// k-blocks: 7.4e-7 and 333 us.  A 256 x 1024 layer on 128 tokens: 2.9e-7 and 87 us against 5.3e-7 and 81; plain fp32 sums 4.2e-7.)
 constexpr int PROMOTE = 2;
 
 struct Unit {
@@ -181,9 +181,12 @@ __device__ __forceinline__ int part_end(const DevProduct& d, const Unit& t, int 
 
 // ---------------------------------------------------------------------------------------------- activations
 // Values go through in pairs (the packed fp32 instructions of sm_100): the epilogue of a 256 x 256 tile has 32768 values
-// per SM, and at one instruction issued per clock and scheduler every instruction per value costs 0.14 us.  Exponentials
-// and reciprocals are the hardware's (a few 2^-22 of the value), for fp32 layers too: what that adds to a layer's error is
-// below that of its sums (with expf, erfcf and divisions the epilogue of dH took 26 us of 66 for a 1024 x 2752 layer).
+// per SM, and at one instruction issued per clock and scheduler every instruction per value costs 0.14 us.  bf16 layers
+// use the hardware's exponential and reciprocal (a few 2^-22 of the value) and for the tail of Phi a polynomial whose error
+// is absolute (1.5e-7: below bf16's 2^-9 of Phi down to z = -5).  fp32 layers use the library functions, whose errors are
+// relative on both sides: with the polynomial GELU(z) was 5e-5 off at z = -3 and 5e-4 at z = -4, and neurons that are mostly
+// negative had their whole share of dW1, db1 and dW2 off by that (GELU layers of 256 x 1024, 128 tokens: 84 us a pass with
+// the polynomial, 87 us; 1007 x 6196, 786 tokens: 545 and 560 us; gated layers the same).
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 __device__ __forceinline__ float2 ex2(float2 x) {
   float2 r;
@@ -198,31 +201,39 @@ __device__ __forceinline__ float2 rcp(float2 x) {
   return r;
 }
 // 1 / (1 + exp(-z))
+template <bool F32>
 __device__ __forceinline__ float2 sigmoid2(float2 z) {
+  if constexpr (F32) return make_float2(__fdividef(1.0f, 1.0f + expf(-z.x)), __fdividef(1.0f, 1.0f + expf(-z.y)));     // 2 ulp
   return rcp(__fadd2_rn(ex2(__fmul2_rn(z, both(-1.4426950408889634f))), both(1.0f)));
 }
 // GELU and, where asked for, its slope.
-template <bool SLOPE>
+template <bool F32, bool SLOPE>
 __device__ __forceinline__ void gelu2(float2 z, int act, float2* value, float2* slope) {
   if (act == FFSPLIT_GELU_ERF) {
-    // z Phi(z), Phi + z phi: Abramowitz and Stegun 7.1.26 (1.5e-7 absolute) for the tail of Phi, on the exponential that
-    // phi needs anyway
-    float2 density = ex2(__fmul2_rn(__fmul2_rn(z, z), both(-0.72134752044448170f)));       // exp(-z^2 / 2)
-    const float2 t = rcp(__ffma2_rn(make_float2(fabsf(z.x), fabsf(z.y)), both(0.3275911f * 0.70710678118654752f), both(1.0f)));
-    float2 q = __ffma2_rn(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
-    q = __ffma2_rn(q, t, both(0.5f * 1.421413741f));
-    q = __ffma2_rn(q, t, both(0.5f * -0.284496736f));
-    q = __ffma2_rn(q, t, both(0.5f * 0.254829592f));
-    q = __fmul2_rn(q, __fmul2_rn(t, density));
-    const float2 over = __ffma2_rn(q, both(-1.0f), both(1.0f));
-    const float2 below = make_float2(z.x >= 0.f ? over.x : q.x, z.y >= 0.f ? over.y : q.y);
+    // z Phi(z), Phi + z phi
+    float2 below, density;
+    if constexpr (F32) {
+      below = make_float2(0.5f * erfcf(-0.70710678118654752f * z.x), 0.5f * erfcf(-0.70710678118654752f * z.y));
+      if (SLOPE) density = make_float2(expf(-0.5f * z.x * z.x), expf(-0.5f * z.y * z.y));
+    } else {
+      // Abramowitz and Stegun 7.1.26 for the tail of Phi, on the exponential that phi needs anyway
+      density = ex2(__fmul2_rn(__fmul2_rn(z, z), both(-0.72134752044448170f)));       // exp(-z^2 / 2)
+      const float2 t = rcp(__ffma2_rn(make_float2(fabsf(z.x), fabsf(z.y)), both(0.3275911f * 0.70710678118654752f), both(1.0f)));
+      float2 q = __ffma2_rn(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+      q = __ffma2_rn(q, t, both(0.5f * 1.421413741f));
+      q = __ffma2_rn(q, t, both(0.5f * -0.284496736f));
+      q = __ffma2_rn(q, t, both(0.5f * 0.254829592f));
+      q = __fmul2_rn(q, __fmul2_rn(t, density));
+      const float2 over = __ffma2_rn(q, both(-1.0f), both(1.0f));
+      below = make_float2(z.x >= 0.f ? over.x : q.x, z.y >= 0.f ? over.y : q.y);
+    }
     *value = __fmul2_rn(z, below);
     if (SLOPE) *slope = __ffma2_rn(z, __fmul2_rn(density, both(0.3989422804014327f)), below);
   } else {
     // tanh form: (1 + tanh u) / 2 = sigmoid(2 u), u = c (z + a z^3)
     const float c = 0.79788456080286536f, a = 0.044715f;
     const float2 z2 = __fmul2_rn(z, z);
-    const float2 s = sigmoid2(__fmul2_rn(z, __ffma2_rn(z2, both(2.0f * c * a), both(2.0f * c))));
+    const float2 s = sigmoid2<F32>(__fmul2_rn(z, __ffma2_rn(z2, both(2.0f * c * a), both(2.0f * c))));
     const float2 v = __fmul2_rn(z, s);
     *value = v;
     if (SLOPE) {
@@ -396,21 +407,21 @@ __device__ __forceinline__ void activate16(const Hidden& h, int act, long long r
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (GATED) x[i] = __fmul2_rn(__fmul2_rn(x[i], sigmoid2(x[i])), y[i]);
-      else gelu2<false>(x[i], act, &x[i], nullptr);
+      if (GATED) x[i] = __fmul2_rn(__fmul2_rn(x[i], sigmoid2<F32>(x[i])), y[i]);
+      else gelu2<F32, false>(x[i], act, &x[i], nullptr);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 g = loaded.first(2 * i);
       if (GATED) {
-        const float2 up = loaded.second(2 * i), s = sigmoid2(g);
+        const float2 up = loaded.second(2 * i), s = sigmoid2<F32>(g);
         const float2 rest = __ffma2_rn(s, both(-1.0f), both(1.0f));
         y[i] = __fmul2_rn(x[i], __fmul2_rn(g, s));
         x[i] = __fmul2_rn(__fmul2_rn(x[i], up), __fmul2_rn(s, __ffma2_rn(g, rest, both(1.0f))));
       } else {
         float2 value, slope;
-        gelu2<true>(g, act, &value, &slope);
+        gelu2<F32, true>(g, act, &value, &slope);
         x[i] = __fmul2_rn(x[i], slope);
       }
     }

@@ -301,6 +301,25 @@ def test_long_fp32_sums(ctx, act, d, m, T):
     check_on_the_device(run(ctx, D, act, "f32"), D, act, "f32", tol=5e-7)
 
 
+@pytest.mark.parametrize("act", ["swiglu", "gelu_erf", "gelu_tanh"])
+def test_neurons_that_are_mostly_negative(ctx, act):
+    """fp32, pre-activations around -4, neuron by neuron (whole-tensor norms hide the tail).  The value and the slope fall off
+    like exp(-z^2 / 2): an error of Z counts |z| + 1 / |z| times, a rounded argument of the exponential z^2 2^-24 (the tanh
+    form: three times that).  Down to z = -6 that is 4e-6 and up to 5e-6; with the products' 1e-6: the library's 1e-5."""
+    D = draw_on_the_device(act, "f32", 256, 512, 200)
+    D["W1"] *= 0.5 / 1.3
+    D["X"][:, 0], D["W1"][0] = 1.0, -4.0
+    got = {k: v.cuda().double() for k, v in run(ctx, D, act, "f32").items()}
+    ref = ffn64_on_the_device({k: None if v is None else v.double() for k, v in D.items()}, act)
+    for k, axis in (("dW1", 0), ("dW1u", 0), ("dW2", 1)):
+        if k in got:
+            off = (got[k] - ref[k]).norm(dim=axis) / ref[k].norm(dim=axis)
+            assert float(off.max()) <= 1e-5, f"{k}: a neuron is {float(off.max()):.2e} off"
+    if "db1" in got:      # (a sum that may cancel: held against the norm of its terms, which is a 16th of its neuron's in X^T dZ)
+        off = (got["db1"] - ref["db1"]).abs() / (ref["dW1"].norm(dim=0) / 16)
+        assert float(off.max()) <= 1e-5, f"db1: a neuron is {float(off.max()):.2e} off"
+
+
 def test_directional_differences(ctx):
     """<gradient, direction> against central differences of the loss sum(Y * dY), fp32.  The direction is the
     gradient's own, scaled to a step of 1 % of the tensor: third-order terms are 1e-4 relative, the rounding of the
