@@ -111,7 +111,9 @@ ffsplit_status ffsplit_workspace_size(const ffsplit_shape* shape, int64_t T_fwd,
 
 /* Give the context its scratch memory (dev, 256-byte aligned, >= 65536 bytes).  The
  * first 65536 bytes hold the device status word and kernel tickets and are cleared
- * here, synchronously.
+ * here: when the call returns they are, for calls on any stream.  Work queued
+ * earlier that uses this memory must have ended, and a condition that the workspace
+ * before it holds is no longer reported (ffsplit_poll() first).
  * The workspace must outlive every call that uses the context, and calls that
  * share a workspace must not overlap on the GPU. */
 ffsplit_status ffsplit_set_workspace(ffsplit_ctx* ctx, void* dev_ptr, size_t bytes);

@@ -228,6 +228,12 @@ class Context:
         return n.value
 
     def set_workspace(self, tensor: torch.Tensor):
+        """ffsplit_set_workspace, once the device is idle: torch hands out memory that work queued on some stream may still
+        use, and takes back the workspace before this one, which calls still running may use.  Not while a graph is captured."""
+        if torch.cuda.is_current_stream_capturing():
+            raise FFSplitError(1, "ffsplit_set_workspace", "a workspace cannot be set while a graph is captured: set one of "
+                                                           "sufficient size before")
+        torch.cuda.synchronize(self.device)
         self._check(self.lib.ffsplit_set_workspace(self.h, _ptr(tensor), tensor.numel() * tensor.element_size()),
                     "ffsplit_set_workspace")
         self._ws = tensor

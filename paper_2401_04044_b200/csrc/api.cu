@@ -43,6 +43,13 @@ bool decode_path_applies(const ffsplit_ctx* ctx, const BlobHeader& h, long long 
 char* noalloc_control_block(int device);   // nullptr until ffsplit_forward_noalloc has run on that device
 size_t decode_scratch_bytes(int dtype, long long T);
 
+// cudaMemset of device memory returns before it has run, on a stream that non-blocking streams do not wait for: calls on one of
+// those could find tickets and status words that are not cleared yet, or have them cleared under their feet.
+cudaError_t clear_and_wait(void* dev_ptr, size_t bytes) {
+  const cudaError_t e = cudaMemset(dev_ptr, 0, bytes);
+  return e != cudaSuccess ? e : cudaStreamSynchronize(nullptr);
+}
+
 ffsplit_status check_shape(ffsplit_ctx* ctx, const ffsplit_shape* s) {
   if (!s) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "shape is NULL");
   if (s->d < 1 || s->m < 1) return fail(ctx, FFSPLIT_ERR_SHAPE, "d and m must be >= 1");
@@ -509,8 +516,8 @@ ffsplit_status ffsplit_set_workspace(ffsplit_ctx* ctx, void* dev_ptr, size_t byt
   if (!dev_ptr || bytes < kCtrlBytes) return fail(ctx, FFSPLIT_ERR_BUFFER_TOO_SMALL, "workspace needs >= 65536 bytes");
   if (reinterpret_cast<uintptr_t>(dev_ptr) % kAlign != 0)
     return fail(ctx, FFSPLIT_ERR_ALIGN, "workspace must be 256-byte aligned");
-  cudaError_t e = cudaMemset(dev_ptr, 0, kCtrlBytes);
-  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaMemset(control block)");
+  const cudaError_t e = clear_and_wait(dev_ptr, kCtrlBytes);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "clearing the control block");
   ctx->ws = static_cast<char*>(dev_ptr);
   ctx->ws_bytes = bytes;
   ctx->tmaps.clear();
@@ -533,8 +540,8 @@ ffsplit_status ffsplit_poll(ffsplit_ctx* ctx, void* stream) {
     e = cudaMemcpy(words, blocks[b], sizeof(words), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return check_cuda(ctx, e, "cudaMemcpy(status block)");
     if (words[0] == 0) continue;
-    e = cudaMemset(blocks[b], 0, kCtrlBytes);
-    if (e != cudaSuccess) return check_cuda(ctx, e, "cudaMemset(control block)");
+    e = clear_and_wait(blocks[b], kCtrlBytes);
+    if (e != cudaSuccess) return check_cuda(ctx, e, "clearing the control block");
     ctx->err = "device status " + std::to_string(words[0]) + " (detail " + std::to_string(words[1]) + ", kernel " +
                std::to_string(words[2]) + ", " + where[b] + ")";
     return static_cast<ffsplit_status>(words[0]);

@@ -373,8 +373,8 @@ extern "C" ffsplit_status ffsplit_forward_noalloc(ffsplit_ctx* ctx, const void* 
       void* ptr = nullptr;
       ce = cudaGetSymbolAddress(&ptr, g_noalloc_scratch);
       if (ce != cudaSuccess || !ptr) return check_cuda(ctx, ce != cudaSuccess ? ce : cudaErrorInvalidSymbol, "cudaGetSymbolAddress(scratch)");
-      ce = cudaMemset(ptr, 0, kNoAllocTicketBytes);   // first use on this device: status words, barrier words and tickets start at zero
-      if (ce != cudaSuccess) return check_cuda(ctx, ce, "cudaMemset(built-in control block)");
+      ce = clear_and_wait(ptr, kNoAllocTicketBytes);   // first use on this device: status words, barrier words and tickets start at zero
+      if (ce != cudaSuccess) return check_cuda(ctx, ce, "clearing the built-in control block");
       g_noalloc_ptr[dev] = static_cast<char*>(ptr);
     }
     base = g_noalloc_ptr[dev];

@@ -342,6 +342,7 @@ size_t ffn_forward_workspace_end(ffsplit_ctx* ctx, const void* blob, long long T
 // argument checks shared by the entry points of all files; defined in api.cu
 ffsplit_status check_ctx(ffsplit_ctx* ctx, bool need_ws);
 ffsplit_status check_shape(ffsplit_ctx* ctx, const ffsplit_shape* s);
+cudaError_t clear_and_wait(void* dev_ptr, size_t bytes);   // zeros, for calls on any stream
 ffsplit_status launch_wait_timeout_probe(ffsplit_ctx* ctx, long long limit_cycles, cudaStream_t st);
 ffsplit_status launch_to_f32(ffsplit_ctx* ctx, int dtype, const void* in, int n, float* out, cudaStream_t st);
 

@@ -670,3 +670,59 @@ def test_finetuning_recovers_a_rounded_layer(ctx, act):
     losses, shape, W = finetune(ctx, 128, 320, act, tokens=256, steps=25)
     assert shape.m == 320 and all(math.isfinite(v) for v in losses)
     assert sum(losses[-5:]) < 0.8 * sum(losses[:5])
+
+
+# ------------------------------------------------------------------------------------------------ the shared workspace
+SLEEP = 50_000_000      # cycles: some 30 ms of a stream that is busy
+
+
+def test_a_new_workspace_is_clear_for_calls_on_any_stream(ctx):
+    """The control block of a workspace full of other data is cleared before calls on a side stream read its tickets, though
+    the default stream, on which the library clears it, is busy."""
+    import paper_2401_04044_b200 as ff
+    d, m, T = 72, 200, 1600      # (db2's rows are cut: its blocks take tickets)
+    L = draw("gelu_erf", "bf16", d, m, T)
+    want = run(ctx, L, "gelu_erf", "bf16")
+    D = {k: None if v is None else v.cuda() for k, v in L.items()}
+    shape = ff.make_shape(d, m, "gelu_erf", torch.bfloat16)
+    saved_bytes, ws = ctx.train_sizes(shape, T)
+    saved, Y = torch.empty(saved_bytes, dtype=torch.uint8, device="cuda"), torch.empty_like(D["X"])
+    g = {"d" + k: torch.zeros_like(D[k]) for k in ("X", "W1", "b1", "W2", "b2")}
+    memory, side, fresh = torch.full((ws,), 0xFF, dtype=torch.uint8, device="cuda"), torch.cuda.Stream(), ff.Context(0)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(SLEEP)
+    with torch.cuda.stream(side):
+        fresh.set_workspace(memory)
+        fresh.train_forward(shape, D["W1"], D["b1"], D["W2"], D["b2"], D["X"], Y, saved=saved)
+        fresh.train_backward(shape, D["W1"], None, D["W2"], D["X"], saved, D["dY"], **g)
+        fresh.poll()
+    assert all(torch.equal(v.cpu(), want[k]) for k, v in g.items())
+    fresh.close()
+
+
+def test_pytorch_calls_grow_the_workspace_on_a_side_stream(ctx):
+    """A fresh context used on a side stream only, nothing synchronised in between; the workspace takes memory that work queued
+    on that stream has yet to read."""
+    import paper_2401_04044_b200 as ff
+    from paper_2401_04044_b200.train import clip_grad_norm_, ffn
+    d, m, T = 72, 200, 1600
+    L = draw("gelu_erf", "bf16", d, m, T)
+    want = run(ctx, L, "gelu_erf", "bf16")
+    shape = ff.make_shape(d, m, "gelu_erf", torch.bfloat16)
+    D = {k: None if v is None else v.cuda().requires_grad_(k != "dY") for k, v in L.items()}
+    side, fresh = torch.cuda.Stream(), ff.Context(0)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        memory = torch.full((ctx.train_sizes(shape, T)[1],), 0xFF, dtype=torch.uint8, device="cuda")
+        torch.cuda._sleep(SLEEP)
+        seen = memory[:1 << 16].clone()
+        del memory
+        Y = ffn(fresh, shape, D["X"], D["W1"], D["W2"], D["b1"], D["b2"])
+        Y.backward(D["dY"])
+        grads = {k: v.grad.clone() for k, v in D.items() if v is not None and k != "dY"}
+        norm = clip_grad_norm_(fresh, [v for k, v in D.items() if v is not None and k != "dY"], 0.5)
+        fresh.poll()
+    assert (seen == 0xFF).all()
+    assert torch.equal(Y.detach().cpu(), want["Y"]) and all(torch.equal(v.cpu(), want["d" + k]) for k, v in grads.items())
+    assert abs(float(norm) - norm64(list(grads.values()))) <= 5e-7 * float(norm)
+    fresh.close()

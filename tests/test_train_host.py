@@ -69,3 +69,36 @@ def test_gradient_list_checks_its_tensors():
         assert e.value.code == code
     empty = GradList(0, [])
     assert empty.count == 0 and C.sizeof(empty.array) >= 32
+
+
+@pytest.fixture
+def idle(monkeypatch):
+    """A context over a library that is not there, and the list of what was done in order."""
+    from paper_2401_04044_b200 import Context
+    done, capturing = [], []
+
+    class Library:
+        def ffsplit_set_workspace(self, handle, ptr, nbytes):
+            done.append("set")
+            return 0
+
+        def ffsplit_last_error(self, handle):
+            return b""
+
+    c = Context.__new__(Context)
+    c.lib, c.h, c.device, c._ws = Library(), None, 0, None
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: done.append("wait"))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: bool(capturing))
+    return c, done, capturing
+
+
+def test_a_workspace_is_set_on_an_idle_device_and_not_in_a_capture(idle):
+    from paper_2401_04044_b200 import FFSplitError
+    c, done, capturing = idle
+    memory = torch.zeros(1 << 17, dtype=torch.uint8)
+    c.set_workspace(memory)
+    assert done == ["wait", "set"] and c._ws is memory
+    capturing.append(True)
+    with pytest.raises(FFSplitError) as e:
+        c.set_workspace(torch.zeros(1 << 18, dtype=torch.uint8))
+    assert e.value.code == 1 and done == ["wait", "set"] and c._ws is memory
