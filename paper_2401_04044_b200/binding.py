@@ -149,6 +149,11 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+def _status_words(workspace: torch.Tensor) -> torch.Tensor:
+    """Where a workspace holds the first condition that a kernel recorded: its code, a detail, the kernel's number."""
+    return workspace.reshape(-1).view(torch.uint8)[:12].view(torch.int32)
+
+
 def _stream_ptr(stream=None):
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.c_void_p(s.cuda_stream)
@@ -239,10 +244,16 @@ class Context:
         self._ws = tensor
 
     def ensure_workspace(self, nbytes: int):
-        """Allocate (with torch) and install a workspace of at least nbytes."""
-        have = 0 if self._ws is None else self._ws.numel()
-        if have < nbytes:
-            self.set_workspace(torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{self.device}"))
+        """Allocate (with torch) and install a workspace of at least nbytes.  A device-side condition that poll() has not
+        reported yet moves on to it."""
+        old = self._ws
+        if old is not None and old.numel() >= nbytes:
+            return
+        new = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{self.device}")
+        self.set_workspace(new)
+        if old is not None:
+            _status_words(new).copy_(_status_words(old))
+            torch.cuda.synchronize(self.device)      # (the next call may be on another stream)
 
     # ------------------------------------------------------------------ entry points
     def score(self, shape: Shape, W1, b1, W2, X, energy, scores=None, mode=SCORE_EQ3, accumulate=False, W1u=None,

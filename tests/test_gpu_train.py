@@ -726,3 +726,18 @@ def test_pytorch_calls_grow_the_workspace_on_a_side_stream(ctx):
     assert torch.equal(Y.detach().cpu(), want["Y"]) and all(torch.equal(v.cpu(), want["d" + k]) for k, v in grads.items())
     assert abs(float(norm) - norm64(list(grads.values()))) <= 5e-7 * float(norm)
     fresh.close()
+
+
+def test_a_non_finite_norm_is_reported_after_the_workspace_has_grown(ctx):
+    import paper_2401_04044_b200 as ff
+    from paper_2401_04044_b200.train import clip_grad_norm_, ffn
+    D = {k: None if v is None else v.cuda() for k, v in draw("swiglu", "bf16", 64, 96, 50).items()}
+    p, fresh = torch.nn.Parameter(torch.zeros(100, device="cuda")), ff.Context(0)
+    p.grad = torch.full_like(p, float("inf"))
+    clip_grad_norm_(fresh, p, 1.0)
+    ffn(fresh, ff.make_shape(64, 96, "swiglu", torch.bfloat16), D["X"], D["W1"], D["W2"], W1u=D["W1u"])
+    with pytest.raises(ff.FFSplitError) as e:
+        fresh.poll()
+    assert e.value.code == 6
+    fresh.poll()
+    fresh.close()

@@ -89,6 +89,8 @@ def idle(monkeypatch):
     c.lib, c.h, c.device, c._ws = Library(), None, 0, None
     monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: done.append("wait"))
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: bool(capturing))
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **k: empty(*a, **k).zero_())
     return c, done, capturing
 
 
@@ -102,3 +104,15 @@ def test_a_workspace_is_set_on_an_idle_device_and_not_in_a_capture(idle):
     with pytest.raises(FFSplitError) as e:
         c.set_workspace(torch.zeros(1 << 18, dtype=torch.uint8))
     assert e.value.code == 1 and done == ["wait", "set"] and c._ws is memory
+
+
+def test_a_growing_workspace_keeps_a_condition_that_was_not_reported(idle):
+    c, done, _ = idle
+    c.ensure_workspace(1 << 16)
+    first = c._ws
+    first[:12].view(torch.int32).copy_(torch.tensor([6, 77, 14], dtype=torch.int32))
+    c.ensure_workspace(1 << 16)
+    assert c._ws is first and done == ["wait", "set"]
+    c.ensure_workspace(1 << 17)
+    assert c._ws is not first and c._ws.numel() == 1 << 17 and done == ["wait", "set", "wait", "set", "wait"]
+    assert c._ws[:12].view(torch.int32).tolist() == [6, 77, 14]
