@@ -154,17 +154,6 @@ def _status_words(workspace: torch.Tensor) -> torch.Tensor:
     return workspace.reshape(-1).view(torch.uint8)[:12].view(torch.int32)
 
 
-def _stream_ptr(stream=None):
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return C.c_void_p(s.cuda_stream)
-
-
-def _stream_of(stream, device: int) -> int:
-    """The handle of `stream`, or of the device's current stream (without making a Stream object of it: that takes the
-    interpreter longer than a launch)."""
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
-
-
 class GradList:
     """The tensors whose gradients are clipped together, as the array ffsplit_grad_norm() / ffsplit_grad_clip() take.
     `out` holds where the clipped gradients go, tensor by tensor; without it they replace the gradients.  The list
@@ -199,6 +188,9 @@ class Context:
     """One ffsplit_ctx bound to a CUDA device, plus the torch tensors that back
     its workspace.  Methods mirror the C entry points one to one."""
 
+    _in_graph = False      # a captured graph uses the workspace
+    _retired = ()          # workspaces before it that captured graphs use
+
     def __init__(self, device: int = 0):
         self.lib = load_library()
         self.device = device
@@ -221,6 +213,14 @@ class Context:
         except Exception:
             pass
 
+    def _stream(self, stream) -> int:
+        """The handle of `stream`, or of the device's current stream (without making a Stream object of it: that takes the
+        interpreter longer than a launch).  Every call that launches asks here, and one that is captured ties the workspace
+        to its graph."""
+        if torch._C._cuda_isCurrentStreamCapturing():
+            self._in_graph = True
+        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
+
     def _check(self, rc: int, where: str):
         if rc != OK:
             raise FFSplitError(rc, where, (self.lib.ffsplit_last_error(self.h) or b"").decode())
@@ -234,13 +234,16 @@ class Context:
 
     def set_workspace(self, tensor: torch.Tensor):
         """ffsplit_set_workspace, once the device is idle: torch hands out memory that work queued on some stream may still
-        use, and takes back the workspace before this one, which calls still running may use.  Not while a graph is captured."""
+        use, and takes back the workspace before this one, which calls still running may use.  Not while a graph is captured.
+        A workspace that a captured graph uses stays allocated as long as the context lives."""
         if torch.cuda.is_current_stream_capturing():
             raise FFSplitError(1, "ffsplit_set_workspace", "a workspace cannot be set while a graph is captured: set one of "
                                                            "sufficient size before")
         torch.cuda.synchronize(self.device)
         self._check(self.lib.ffsplit_set_workspace(self.h, _ptr(tensor), tensor.numel() * tensor.element_size()),
                     "ffsplit_set_workspace")
+        if self._in_graph and self._ws is not tensor:
+            self._retired, self._in_graph = (*self._retired, self._ws), False
         self._ws = tensor
 
     def ensure_workspace(self, nbytes: int):
@@ -260,7 +263,7 @@ class Context:
               stream=None):
         w = Weights(_ptr(W1), _ptr(W1u), _ptr(b1), _ptr(W2), None)
         self._check(self.lib.ffsplit_score(self.h, C.byref(shape), C.byref(w), _ptr(X), X.shape[0], int(mode),
-                                           int(bool(accumulate)), _ptr(energy), _ptr(scores), _stream_ptr(stream)),
+                                           int(bool(accumulate)), _ptr(energy), _ptr(scores), self._stream(stream)),
                     "ffsplit_score")
 
     def score_activations(self, shape: Shape, H, W2, energy, scores=None, mode=SCORE_EQ3, accumulate=False,
@@ -268,11 +271,11 @@ class Context:
         """ffsplit_score_activations: Eq. 3 from a stored activation matrix H [T, m]."""
         self._check(self.lib.ffsplit_score_activations(self.h, C.byref(shape), _ptr(H), H.shape[0], _ptr(W2), mode,
                                                        1 if accumulate else 0, _ptr(energy), _ptr(scores),
-                                                       _stream_ptr(stream)), "ffsplit_score_activations")
+                                                       self._stream(stream)), "ffsplit_score_activations")
 
     def select(self, scores, k: int, heavy_idx, light_idx=None, stream=None):
         self._check(self.lib.ffsplit_select(self.h, _ptr(scores), scores.numel(), k, _ptr(heavy_idx), _ptr(light_idx),
-                                            _stream_ptr(stream)), "ffsplit_select")
+                                            self._stream(stream)), "ffsplit_select")
 
     def pack_size(self, shape: Shape, k: int, r: int):
         a, b = C.c_size_t(), C.c_size_t()
@@ -288,11 +291,11 @@ class Context:
                         _ptr(factors["A2"]), _ptr(factors["B2"]), int(factors["A1"].shape[1]))
             fp = C.byref(f)
         self._check(self.lib.ffsplit_pack(self.h, C.byref(shape), C.byref(w), _ptr(heavy_idx), k, fp, _ptr(blob),
-                                          blob.numel() * blob.element_size(), _stream_ptr(stream)), "ffsplit_pack")
+                                          blob.numel() * blob.element_size(), self._stream(stream)), "ffsplit_pack")
 
     def blob_open(self, blob, stream=None):
         self._check(self.lib.ffsplit_blob_open(self.h, _ptr(blob), blob.numel() * blob.element_size(),
-                                               _stream_ptr(stream)), "ffsplit_blob_open")
+                                               self._stream(stream)), "ffsplit_blob_open")
 
     def blob_close(self, blob):
         self._check(self.lib.ffsplit_blob_close(self.h, _ptr(blob)), "ffsplit_blob_close")
@@ -303,12 +306,12 @@ class Context:
         w = Weights(_ptr(W1), _ptr(W1u), _ptr(b1), _ptr(W2), None)
         self._check(self.lib.ffsplit_score_host(self.h, C.byref(shape), C.byref(w), _ptr(X_host), X_host.shape[0],
                                                 int(mode), int(bool(accumulate)), _ptr(energy), _ptr(scores),
-                                                _stream_ptr(stream)), "ffsplit_score_host")
+                                                self._stream(stream)), "ffsplit_score_host")
 
     def score_finalize(self, shape: Shape, W2, energy, scores, mode=SCORE_EQ3, stream=None):
         """ffsplit_score_finalize: scores from a complete energy vector (after a sharded or multi-call accumulation)."""
         self._check(self.lib.ffsplit_score_finalize(self.h, C.byref(shape), _ptr(W2), int(mode), _ptr(energy),
-                                                    _ptr(scores), _stream_ptr(stream)), "ffsplit_score_finalize")
+                                                    _ptr(scores), self._stream(stream)), "ffsplit_score_finalize")
 
     @staticmethod
     def _blob_array(blobs):
@@ -323,11 +326,11 @@ class Context:
 
     def forward_stack(self, blobs, X, Y, stream=None):
         self._check(self.lib.ffsplit_forward_stack(self.h, self._blob_array(blobs), len(blobs), _ptr(X), X.shape[0],
-                                                   _ptr(Y), _stream_ptr(stream)), "ffsplit_forward_stack")
+                                                   _ptr(Y), self._stream(stream)), "ffsplit_forward_stack")
 
     def forward_stack_host(self, blobs, X_host, Y_host, stream=None):
         self._check(self.lib.ffsplit_forward_stack_host(self.h, self._blob_array(blobs), len(blobs), _ptr(X_host),
-                                                        X_host.shape[0], _ptr(Y_host), _stream_ptr(stream)),
+                                                        X_host.shape[0], _ptr(Y_host), self._stream(stream)),
                     "ffsplit_forward_stack_host")
 
     # ------------------------------------------------------------------ the transformer block around the FFN
@@ -343,7 +346,7 @@ class Context:
         return n.value
 
     def encoder_forward(self, layer: "EncoderLayer", X, Y, stream=None):
-        self._check(self.lib.ffsplit_encoder_forward(self.h, C.byref(layer), _ptr(X), _ptr(Y), _stream_ptr(stream)),
+        self._check(self.lib.ffsplit_encoder_forward(self.h, C.byref(layer), _ptr(X), _ptr(Y), self._stream(stream)),
                     "ffsplit_encoder_forward")
 
     # ------------------------------------------------------------------ on-device light factors (Section 5.1.1)
@@ -366,7 +369,7 @@ class Context:
         w = Weights(_ptr(W1), _ptr(W1u), None, _ptr(W2), None)
         self._check(self.lib.ffsplit_factor_light(self.h, C.byref(shape), C.byref(w), _ptr(light_idx), k, r, iters,
                                                   _ptr(start), _ptr(f["A1"]), _ptr(f["B1"]), _ptr(f["A2"]), _ptr(f["B2"]),
-                                                  _ptr(f.get("A1u")), _ptr(f.get("B1u")), _stream_ptr(stream)),
+                                                  _ptr(f.get("A1u")), _ptr(f.get("B1u")), self._stream(stream)),
                     "ffsplit_factor_light")
         return f
 
@@ -384,12 +387,12 @@ class Context:
     def quant_pack(self, shape: Shape, W1, b1, W2, b2, heavy_idx, k: int, light_idx, blob, W1u=None, stream=None):
         w = Weights(_ptr(W1), _ptr(W1u), _ptr(b1), _ptr(W2), _ptr(b2))
         self._check(self.lib.ffsplit_quant_pack(self.h, C.byref(shape), C.byref(w), _ptr(heavy_idx), k, _ptr(light_idx),
-                                                _ptr(blob), blob.numel() * blob.element_size(), _stream_ptr(stream)),
+                                                _ptr(blob), blob.numel() * blob.element_size(), self._stream(stream)),
                     "ffsplit_quant_pack")
 
     def quant_blob_open(self, blob, stream=None):
         self._check(self.lib.ffsplit_quant_blob_open(self.h, _ptr(blob), blob.numel() * blob.element_size(),
-                                                     _stream_ptr(stream)), "ffsplit_quant_blob_open")
+                                                     self._stream(stream)), "ffsplit_quant_blob_open")
 
     def quant_unpack(self, blob, which: int, rows: int, cols: int, stream=None):
         """-> (codes uint8 [rows, cols], scale float32 [rows, ceil(cols / 128)], lo likewise) of one packed matrix."""
@@ -399,11 +402,11 @@ class Context:
         scale = torch.zeros(rows, ng, dtype=torch.float32, device=dev)
         lo = torch.zeros(rows, ng, dtype=torch.float32, device=dev)
         self._check(self.lib.ffsplit_quant_unpack(self.h, _ptr(blob), which, _ptr(codes), _ptr(scale), _ptr(lo),
-                                                  _stream_ptr(stream)), "ffsplit_quant_unpack")
+                                                  self._stream(stream)), "ffsplit_quant_unpack")
         return codes, scale, lo
 
     def quant_forward(self, blob, X, Y, stream=None):
-        self._check(self.lib.ffsplit_quant_forward(self.h, _ptr(blob), _ptr(X), X.shape[0], _ptr(Y), _stream_ptr(stream)),
+        self._check(self.lib.ffsplit_quant_forward(self.h, _ptr(blob), _ptr(X), X.shape[0], _ptr(Y), self._stream(stream)),
                     "ffsplit_quant_forward")
 
     # ------------------------------------------------------------------ training
@@ -450,7 +453,7 @@ class Context:
         w = self._train_weights(where, shape, W1, W1u, b1, W2, b2)
         rc = self.lib.ffsplit_train_forward(
             self.h, shape, w, self._operand(where, "X", X, dt, (T, d), False), T, *self._saved(where, saved),
-            self._operand(where, "Y", Y, dt, (T, d), False), _stream_of(stream, self.device))
+            self._operand(where, "Y", Y, dt, (T, d), False), self._stream(stream))
         if rc:
             self._check(rc, where)
 
@@ -463,7 +466,7 @@ class Context:
                        op(where, "db1", db1, dt, (m,)), op(where, "dW2", dW2, dt, (m, d)), op(where, "db2", db2, dt, (d,)))
         rc = self.lib.ffsplit_train_backward(
             self.h, shape, w, op(where, "X", X, dt, (T, d), False), T, *self._saved(where, saved),
-            op(where, "dY", dY, dt, (T, d), False), g, _stream_of(stream, self.device))
+            op(where, "dY", dY, dt, (T, d), False), g, self._stream(stream))
         if rc:
             self._check(rc, where)
 
@@ -483,15 +486,15 @@ class Context:
     def grad_norm(self, grads: "GradList", norm, stream=None):
         """ffsplit_grad_norm: norm[0] = the 2-norm of all gradients of the list."""
         self._check(self.lib.ffsplit_grad_norm(self.h, C.byref(grads.array), grads.count, self._norm_ptr("ffsplit_grad_norm", norm),
-                                               _stream_of(stream, self.device)), "ffsplit_grad_norm")
+                                               self._stream(stream)), "ffsplit_grad_norm")
 
     def clip_grads(self, grads: "GradList", max_norm: float, norm, stream=None):
         """ffsplit_grad_clip: the norm, then every gradient times min(1, max_norm / (norm + 1e-6))."""
         self._check(self.lib.ffsplit_grad_clip(self.h, C.byref(grads.array), grads.count, max_norm,
-                                               self._norm_ptr("ffsplit_grad_clip", norm), _stream_of(stream, self.device)), "ffsplit_grad_clip")
+                                               self._norm_ptr("ffsplit_grad_clip", norm), self._stream(stream)), "ffsplit_grad_clip")
 
     def debug_wait_timeout(self, limit_cycles: int, stream=None):
-        self._check(self.lib.ffsplit_debug_wait_timeout(self.h, int(limit_cycles), _stream_ptr(stream)),
+        self._check(self.lib.ffsplit_debug_wait_timeout(self.h, int(limit_cycles), self._stream(stream)),
                     "ffsplit_debug_wait_timeout")
 
     def blob_section(self, blob, which: int):
@@ -501,26 +504,33 @@ class Context:
         return off.value, r.value, c.value, ld.value
 
     def forward(self, blob, X, Y, stream=None):
-        self._check(self.lib.ffsplit_forward(self.h, _ptr(blob), _ptr(X), X.shape[0], _ptr(Y), _stream_ptr(stream)),
+        self._check(self.lib.ffsplit_forward(self.h, _ptr(blob), _ptr(X), X.shape[0], _ptr(Y), self._stream(stream)),
                     "ffsplit_forward")
 
     def forward_dense(self, shape: Shape, W1, b1, W2, b2, X, Y, W1u=None, stream=None):
         """ffsplit_forward_dense: the unsplit FFN from the row-major weights (packed into the workspace per call)."""
         w = Weights(_ptr(W1), _ptr(W1u), _ptr(b1), _ptr(W2), _ptr(b2))
         self._check(self.lib.ffsplit_forward_dense(self.h, C.byref(shape), C.byref(w), _ptr(X), X.shape[0], _ptr(Y),
-                                                   _stream_ptr(stream)), "ffsplit_forward_dense")
+                                                   self._stream(stream)), "ffsplit_forward_dense")
 
     def forward_noalloc(self, blob, X, Y, stream=None):
         """ffsplit_forward_noalloc: up to 8 tokens, bf16, scratch built into the library (no workspace needed)."""
         self._check(self.lib.ffsplit_forward_noalloc(self.h, _ptr(blob), _ptr(X), X.shape[0], _ptr(Y),
-                                                     _stream_ptr(stream)), "ffsplit_forward_noalloc")
+                                                     self._stream(stream)), "ffsplit_forward_noalloc")
 
     def forward_host(self, blob, X_host, Y_host, stream=None):
         self._check(self.lib.ffsplit_forward_host(self.h, _ptr(blob), _ptr(X_host), X_host.shape[0], _ptr(Y_host),
-                                                  _stream_ptr(stream)), "ffsplit_forward_host")
+                                                  self._stream(stream)), "ffsplit_forward_host")
 
     def poll(self, stream=None):
-        self._check(self.lib.ffsplit_poll(self.h, _stream_ptr(stream)), "ffsplit_poll")
+        """ffsplit_poll, and the same for workspaces that only captured graphs still use."""
+        self._check(self.lib.ffsplit_poll(self.h, self._stream(stream)), "ffsplit_poll")
+        for ws in self._retired:
+            code, detail, kernel = _status_words(ws).tolist()
+            if code:
+                ws.reshape(-1).view(torch.uint8)[:65536].zero_()
+                torch.cuda.synchronize(self.device)
+                raise FFSplitError(code, "ffsplit_poll", f"device status {code} (detail {detail}, kernel {kernel}, a captured graph's workspace)")
 
     def profile_begin(self):
         self._check(self.lib.ffsplit_profile_begin(self.h), "ffsplit_profile_begin")
@@ -528,7 +538,7 @@ class Context:
     def profile_end(self, kernel_class: int = 0, stream=None):
         """-> (launches, total milliseconds, total algorithmic work) of one kernel class."""
         n, ms, work = C.c_int32(), C.c_double(), C.c_double()
-        self._check(self.lib.ffsplit_profile_end(self.h, _stream_ptr(stream), kernel_class, C.byref(n), C.byref(ms),
+        self._check(self.lib.ffsplit_profile_end(self.h, self._stream(stream), kernel_class, C.byref(n), C.byref(ms),
                                                  C.byref(work)), "ffsplit_profile_end")
         return n.value, ms.value, work.value
 

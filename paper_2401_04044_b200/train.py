@@ -50,7 +50,10 @@ class _FFN(torch.autograd.Function):
 
 def ffn(lib: Context, shape: Shape, X, W1, W2, b1=None, b2=None, W1u=None) -> torch.Tensor:
     """act(X W1 + b1) W2 + b2, or (SiLU(X W1) * (X W1u)) W2 + b2, differentiable once in X and the weights.  X [T, d] and
-    the weights are contiguous tensors of the layer's type on the context's device; the calls run on the current stream."""
+    the weights are contiguous tensors of the layer's type on the context's device; the calls run on the current stream.
+    Where the context's workspace is too small for T tokens it is replaced, which waits for the device and is refused while a
+    graph is captured (lib.ensure_workspace(lib.train_sizes(shape, T)[1]) does it before).  Calls on one context share its
+    workspace: they may not overlap on the GPU, whatever their streams."""
     return _FFN.apply(lib, shape, torch.is_grad_enabled(), X, W1, W1u, b1, W2, b2)
 
 
@@ -58,7 +61,7 @@ def clip_grad_norm_(lib: Context, parameters: Union[torch.Tensor, Iterable[torch
                     norm: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scales the parameters' gradients in place so that their norm is at most max_norm; returns the norm (float32[1] on
     the device, not waited for).  A parameter that is named twice counts once.  A non-finite norm leaves the gradients as
-    they are and is reported by lib.poll()."""
+    they are and is reported by lib.poll().  Workspace and streams: as for ffn()."""
     parameters = [parameters] if isinstance(parameters, torch.Tensor) else parameters
     grads = [p.grad for p in {id(p): p for p in parameters}.values() if p.grad is not None]
     if norm is None:

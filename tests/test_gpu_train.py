@@ -741,3 +741,41 @@ def test_a_non_finite_norm_is_reported_after_the_workspace_has_grown(ctx):
     assert e.value.code == 6
     fresh.poll()
     fresh.close()
+
+
+def test_a_captured_pass_outlives_its_workspace(ctx):
+    """After the capture a larger call replaces the workspace and other tensors take what memory is free; replays neither read
+    those nor write to them."""
+    import paper_2401_04044_b200 as ff
+    D = {k: None if v is None else v.cuda() for k, v in draw("gelu_erf", "f32", 130, 257, 300).items()}
+    shape, fresh = ff.make_shape(130, 257, "gelu_erf", torch.float32), ff.Context(0)
+    saved_bytes, ws = fresh.train_sizes(shape, 300)
+    fresh.ensure_workspace(ws)
+    saved, Y = torch.empty(saved_bytes, dtype=torch.uint8, device="cuda"), torch.empty_like(D["X"])
+    g = {"d" + k: torch.empty_like(D[k]) for k in ("X", "W1", "b1", "W2", "b2")}
+
+    def step():
+        fresh.train_forward(shape, D["W1"], D["b1"], D["W2"], D["b2"], D["X"], Y, saved=saved)
+        fresh.train_backward(shape, D["W1"], None, D["W2"], D["X"], saved, D["dY"], **g)
+
+    step()
+    torch.cuda.synchronize()
+    want = {k: v.clone() for k, v in {**g, "Y": Y}.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    fresh.ensure_workspace(8 * ws)
+    others = [torch.full((ws,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    for v in (*g.values(), Y):
+        v.zero_()
+    graph.replay()
+    fresh.poll()
+    assert all(torch.equal(v, want[k]) for k, v in {**g, "Y": Y}.items())
+    assert all((o == 0x5A).all() for o in others)
+    with pytest.raises(ff.FFSplitError) as e:
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            step()
+            fresh.ensure_workspace(16 * ws)
+    assert e.value.code == 1
+    torch.cuda.synchronize()
+    fresh.close()

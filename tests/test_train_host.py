@@ -116,3 +116,34 @@ def test_a_growing_workspace_keeps_a_condition_that_was_not_reported(idle):
     c.ensure_workspace(1 << 17)
     assert c._ws is not first and c._ws.numel() == 1 << 17 and done == ["wait", "set", "wait", "set", "wait"]
     assert c._ws[:12].view(torch.int32).tolist() == [6, 77, 14]
+
+
+def test_a_workspace_that_a_graph_uses_stays_allocated(idle, monkeypatch):
+    import weakref
+    from paper_2401_04044_b200 import FFSplitError
+    c, _, _ = idle
+    capturing = []
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: bool(capturing))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    for name in ("ffsplit_grad_norm", "ffsplit_poll"):
+        setattr(c.lib, name, lambda *a: 0)
+    norm = lambda: c.lib.ffsplit_grad_norm(c.h, None, 0, None, c._stream(None))  # noqa: E731
+    c.ensure_workspace(1 << 16)
+    norm()
+    unused = weakref.ref(c._ws)
+    c.ensure_workspace(1 << 17)
+    assert unused() is None
+    capturing.append(True)
+    norm()
+    capturing.clear()
+    used, where = weakref.ref(c._ws), c._ws.data_ptr()
+    c.ensure_workspace(1 << 18)
+    plain = weakref.ref(c._ws)
+    c.ensure_workspace(1 << 19)
+    assert used() is not None and used().data_ptr() == where and plain() is None
+    # what a replay records there is reported as well, once
+    used()[:12].view(torch.int32).copy_(torch.tensor([6, 5, 14], dtype=torch.int32))
+    with pytest.raises(FFSplitError) as e:
+        c.poll()
+    assert e.value.code == 6
+    c.poll()
