@@ -44,7 +44,11 @@ class _FFN(torch.autograd.Function):
         d, m = shape.d, shape.m
         g = {"dX": new(need_X, *X.shape), "dW1": new(need_W1, d, m), "dW1u": new(need_W1u and ctx.has[0], d, m),
              "db1": new(need_b1 and ctx.has[1], m), "dW2": new(need_W2, m, d), "db2": new(need_b2 and ctx.has[2], d)}
-        lib.train_backward(shape, W1, None, W2, X, saved, dY.contiguous(), W1u=W1u, **g)
+        # (what autograd hands over may be expanded, or a piece of a larger gradient that starts anywhere)
+        dY = dY.contiguous()
+        if dY.data_ptr() % 16:
+            dY = dY.clone()
+        lib.train_backward(shape, W1, None, W2, X, saved, dY, W1u=W1u, **g)
         return None, None, None, g["dX"], g["dW1"], g["dW1u"], g["db1"], g["dW2"], g["db2"]
 
 

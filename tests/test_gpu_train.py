@@ -571,6 +571,23 @@ def test_autograd_function_keeps_nothing_without_grad_and_has_no_second_derivati
         g.float().sum().backward()
 
 
+@pytest.mark.parametrize("d,rows", [(33, (7, 12)), (35, (1, 2)), (34, (5, 6))])
+def test_autograd_function_takes_gradients_that_start_anywhere(ctx, d, rows):
+    """Behind torch.cat, a layer's gradient is a piece of a larger one; behind a sum it is one number, expanded."""
+    from paper_2401_04044_b200 import make_shape
+    from paper_2401_04044_b200.train import ffn
+    L = draw("gelu_erf", "f32", d, 40, sum(rows))
+    shape, D = make_shape(d, 40, "gelu_erf", torch.float32), {k: None if v is None else v.cuda() for k, v in L.items()}
+    layer = lambda X: ffn(ctx, shape, X, D["W1"], D["W2"], D["b1"], D["b2"])  # noqa: E731
+    X = D["X"].clone().requires_grad_()
+    pieces = [x.clone() for x in X.split(rows)]      # (as inputs, the pieces have to be aligned)
+    torch.cat([layer(x) for x in pieces]).backward(D["dY"])
+    check({"dX": X.grad.cpu()}, L, "gelu_erf", "f32")
+    X = D["X"].clone().requires_grad_()
+    layer(X).sum().backward()
+    check({"dX": X.grad.cpu()}, {**L, "dY": torch.ones_like(L["dY"])}, "gelu_erf", "f32")
+
+
 @pytest.mark.parametrize("dtype,act,T", [("bf16", "swiglu", 90), ("bf16", "gelu_erf", 700), ("f32", "gelu_tanh", 33)])
 def test_a_captured_pass_reads_its_inputs_anew(ctx, dtype, act, T):
     """Forward, backward and clipping as one CUDA graph, replayed on other inputs than it was captured with."""
