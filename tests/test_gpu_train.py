@@ -209,6 +209,31 @@ def test_a_non_finite_token_stays_in_its_row(ctx, dtype, bad):
     assert not torch.isfinite(got["dW1"][5]).any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["gelu_erf", "gelu_tanh"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_a_non_finite_token_of_a_gelu_layer_stays_in_its_row(ctx, dtype, act, bad):
+    T = 150
+    L = draw(act, dtype, 72, 100, T)
+    clean = run(ctx, L, act, dtype)
+    L["X"][77, 5] = bad
+    got = run(ctx, L, act, dtype)
+    rest = [t for t in range(T) if t != 77]
+    for k in ("Y", "dX"):
+        assert torch.equal(got[k][rest], clean[k][rest])
+        assert not torch.isfinite(got[k][77]).any()
+    assert not torch.isfinite(got["dW1"][5]).any()
+    assert torch.equal(got["db2"], clean["db2"])
+
+
+@pytest.mark.parametrize("dtype,act,d,m", [("bf16", "swiglu", 4096, 11008), ("bf16", "gelu_tanh", 5120, 20480), ("bf16", "swiglu", 1000, 2731),
+                                           ("f32", "gelu_erf", 2048, 4097)])
+@pytest.mark.parametrize("T", [1, 2, 7, 33])
+def test_few_tokens_through_wide_layers(ctx, dtype, act, d, m, T):
+    D = draw_on_the_device(act, dtype, d, m, T)
+    check_on_the_device(run(ctx, D, act, dtype), D, act, dtype)
+
+
 def test_bias_gradients_of_a_very_wide_layer(ctx):
     """More blocks of columns for db1 than there are tickets, while db2's rows are cut."""
     import paper_2401_04044_b200 as ff
