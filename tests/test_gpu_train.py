@@ -509,6 +509,28 @@ def test_norm_outside_the_range_of_fp32_squares(ctx, scale, kind):
     assert abs(float(norm) - want) <= 5e-7 * want
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-3, 1e-38, 1e-40])
+def test_norm_of_mostly_zeros(ctx, kind, scale):
+    """Zeros of both signs everywhere but in a few places, whose values may be subnormal and have squares that are not."""
+    grads = [torch.zeros(n, dtype=DT[kind], device="cuda") for n in (100_000, 7, 40_001)]
+    grads[0][::2] *= -1
+    for g, places in zip(grads, ((3, 4096, 77_777), (6,), (0, 40_000))):
+        for i in places:
+            g[i] = (i % 5 + 1) * scale
+    norm = torch.empty(1, device="cuda")
+    ctx.ensure_workspace(ctx.grad_workspace_size(3))
+    ctx.grad_norm(ctx.grad_list(grads), norm)
+    ctx.poll()
+    want = norm64(grads)
+    assert want > 0 and abs(float(norm) - want) <= 5e-7 * want + 2.0 ** -150     # (half a step of the subnormal numbers)
+    for g in grads:
+        g.zero_()
+    ctx.grad_norm(ctx.grad_list(grads), norm)
+    ctx.poll()
+    assert float(norm) == 0.0
+
+
 def test_clipping_an_empty_list(ctx):
     assert clip_both(ctx, [], 1.0) == 0.0
 
