@@ -89,11 +89,6 @@ __device__ __forceinline__ void add_squares(double& acc, const float* v) {
   if (s >= 8.673617e-19f && s < 1.329228e36f) {
     acc += static_cast<double>(s);
   } else {
-    // (zeros are common, rows of an embedding that no token used; small values are not zeros, though s may be)
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < N; ++i) any = any || v[i] != 0.f;
-    if (!any) return;
 #pragma unroll
     for (int i = 0; i < N; ++i) acc += static_cast<double>(v[i]) * static_cast<double>(v[i]);
   }
