@@ -405,6 +405,8 @@ ffsplit_status ffsplit_train_sizes(const ffsplit_shape* shape, int64_t T, size_t
 /* Y dev [T, d] from X dev [T, d], in the layer's dtype.
  *   saved  dev, 256-byte aligned, saved_bytes >= what ffsplit_train_sizes() says: written for the backward pass
  *          of the same layer, weights and X.  NULL: no backward pass will follow, nothing is kept.
+ * Without `saved` this computes what ffsplit_forward_dense() does, which packs the weights first, on every call; where the
+ * weights change between calls this is the one to use, where they stay a blob packed once with k = m (ffsplit_pack()).
  * X and Y may not overlap.  Uses the workspace. */
 ffsplit_status ffsplit_train_forward(ffsplit_ctx* ctx, const ffsplit_shape* shape, const ffsplit_weights* weights,
                                      const void* X, int64_t T, void* saved, size_t saved_bytes, void* Y, void* stream);

@@ -8,10 +8,14 @@
 // the two it is, is a bit of the instruction descriptor and the shape of the TMA box, both chosen at run time.
 //
 // One persistent pair of CTAs (two SMs, cta_group::2) per 256 x 256 tile: each CTA stages 128 rows of A and 128 rows
-// of B per 64-deep k-block (32 KB) by TMA in a ring of six (more where there are fewer rows or columns), rank 0 issues the MMAs for both, and each CTA finishes the
-// 128 accumulator rows in its own tensor memory.  Two accumulators of 256 columns: a tile's epilogue runs under the
+// of B per 64-deep k-block (32 KB) by TMA in a ring of six (more where there are fewer rows or columns), rank 0 issues the
+// MMAs for both, and each CTA finishes the 128 accumulator rows in its own tensor memory.  Two accumulators of 256 columns: a tile's epilogue runs under the
 // next tile's MMAs.  A gated tile is 256 x 128: rank 0 stages the 128 columns of W1, rank 1 those of W1u, so that
 // every accumulator row holds G next to U and the product H leaves from the same registers.
+//
+// bf16 layers: sums are fp32; H, dG (dZ) and dU are rounded to bf16 between two products, because they are operands of the
+// next one and the tensor cores take both operands in one type (a second plane would double that product).  G, U and Z are
+// kept in 20 bits, see Kept.  Outputs are 2.3e-3 off 64 bits that way; the rounding of the output alone is 1.7e-3.
 //
 // fp32 layers: every fp32 matrix is split into three bf16 planes (x0 = bf16(x), x1 = bf16(x - x0), ...: 24 significant
 // bits), and the six products of planes (i, j), i + j <= 2, are accumulated as six runs over K, the smallest first.
@@ -50,8 +54,9 @@ template <int MODE, bool F32> constexpr int EPI_WARPS = F32 || MODE == PLAIN ? 8
 template <int MODE, bool F32> constexpr int OUT_BYTES = MODE == PLAIN ? 4096 : F32 ? 0 : MODE == BACKWARD_GATED ? 4096 : 2048;
 // The first epilogue warp.  fp32 kernels keep it on a warpgroup's boundary, so that registers can move from the group of the
 // producer and the MMA issuer to the epilogue's two: with 168 for every thread the sums were spilled, and with the ring
-// taking nearly all of the SM's memory a spill goes to L2.  384 threads start with 168 registers each (64512); 128 of them go
-// down to 56 and 256 up to 224: 7168 + 57344 = 64512.
+// taking nearly all of the SM's memory a spill goes to L2 (380 -> 342 us for a 1024 x 2752 gated layer, 1024 tokens; of dH's
+// epilogues 116 bytes a thread still spill where the layer is gated, 16 in GELU layers).  384 threads start with 168 registers
+// each (64512); 128 of them go down to 56 and 256 up to 224: 7168 + 57344 = 64512.
 template <bool F32> constexpr int FIRST_EPI = F32 ? 4 : 2;
 constexpr int START_REGS = 168, ROLE_REGS = 56, EPI_REGS = 224;
 static_assert(ROLE_REGS * 128 + EPI_REGS * 256 <= START_REGS * 384, "a split above what the block starts with waits forever");
