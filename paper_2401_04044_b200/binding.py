@@ -256,6 +256,7 @@ class Context:
         self.set_workspace(new)
         if old is not None:
             _status_words(new).copy_(_status_words(old))
+            _status_words(old).zero_()
             torch.cuda.synchronize(self.device)      # (the next call may be on another stream)
 
     # ------------------------------------------------------------------ entry points

@@ -147,3 +147,16 @@ def test_a_workspace_that_a_graph_uses_stays_allocated(idle, monkeypatch):
         c.poll()
     assert e.value.code == 6
     c.poll()
+
+
+def test_a_condition_that_moved_on_is_reported_once(idle, monkeypatch):
+    c, _, _ = idle
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    c.lib.ffsplit_poll = lambda *a: 0      # (the library reports, and clears, what the new workspace holds)
+    c.ensure_workspace(1 << 16)
+    c._in_graph = True
+    c._ws[:12].view(torch.int32).copy_(torch.tensor([6, 0, 14], dtype=torch.int32))
+    c.ensure_workspace(1 << 17)
+    assert len(c._retired) == 1 and c._ws[:12].view(torch.int32).tolist() == [6, 0, 14]
+    c.poll()
