@@ -454,6 +454,85 @@ ffsplit_status ffsplit_grad_norm(ffsplit_ctx* ctx, const ffsplit_grad_tensor* te
 ffsplit_status ffsplit_grad_clip(ffsplit_ctx* ctx, const ffsplit_grad_tensor* tensors, int32_t count, float max_norm,
                                  float* norm, void* stream);
 
+/* ---- Updating matrices by orthogonalised momentum -------------------------------------------------------
+ * An optimiser step for the layer's matrices (or an adapter's factors).  For one matrix [rows, cols]:
+ *   M' = beta M + G,   U = G + beta M' (nesterov) or M',   X = U / (|U| + 1e-7)   (|.| over all elements)
+ *   X <- a X + (b S + c S^2) X with S = X X^T, once for each (a, b, c); where rows > cols, X (b S + c S^2) with S = X^T X
+ *   W' = (1 - decay) W - step X
+ * The coefficients move the singular values of X towards 1 and leave its singular vectors: a Newton-Schulz iteration.
+ *
+ * Arithmetic: sums in fp32 and more.  Where the gradient is bf16, X is kept in 22 bits, and the operands of the products
+ * are fp16 (11 bits); what is rounded off an operand perturbs X by a factor close to 1, not by a term, so small singular
+ * values do not drown in it: X is off by 2e-4 to 2e-3 of its norm.  Where the gradient is fp32, operands carry 22 bits
+ * too: 1e-6.  Momentum is fp32 whatever the type of the gradient. */
+
+typedef struct {
+  const void* grad;           /* dev [rows, cols], grad_dtype                                         */
+  const float* momentum;      /* dev [rows, cols], NULL: U is the gradient itself                     */
+  float* momentum_out;        /* dev [rows, cols], may be momentum; NULL where momentum is            */
+  const void* weight;         /* dev [rows, cols], weight_dtype; NULL: out = X, the orthogonal factor */
+  void* out;                  /* dev [rows, cols], weight_dtype; may be weight                        */
+  int32_t rows, cols;         /* >= 1 */
+  int32_t grad_dtype, weight_dtype;   /* ffsplit_dtype */
+  float step, decay;          /* not looked at where weight is NULL */
+} ffsplit_muon_tensor;
+
+/* Workspace that the call below needs for this list (only shapes and types are looked at). */
+ffsplit_status ffsplit_muon_workspace_size(const ffsplit_muon_tensor* tensors, int32_t count, size_t* bytes);
+
+/* One step for every matrix of the list (a host array, read before the call returns).  coefficients: host
+ * [iterations][3], or NULL for iterations times (3.4445, -4.7750, 2.0315); 1 <= iterations <= 16.  Coefficients that
+ * can carry a singular value in [0, 1] above 1.5, or that are larger than 64, are refused (INVALID_ARG).
+ * Tensors are aligned to their element size (no 16-byte rule); outputs may be the inputs they replace and overlap
+ * nothing else.  Matrices of one shape are worked on together: give one list rather than many.
+ * A matrix whose U is not finite is left as it is, its momentum too (out = NaN where weight is NULL), and
+ * FFSPLIT_ERR_NONFINITE is reported through ffsplit_poll().  A matrix of zeros has X = 0.  Uses the workspace. */
+ffsplit_status ffsplit_muon_step(ffsplit_ctx* ctx, const ffsplit_muon_tensor* tensors, int32_t count, float beta,
+                                 int32_t nesterov, const float* coefficients, int32_t iterations, void* stream);
+
+/* ---- Low-rank adapters of many requests beside a shared projection ---------------------------------------
+ * A batch of T tokens goes through one projection [in, out]; each token may carry an adapter of its own, a rank-r
+ * pair of factors that its request was fine-tuned with:
+ *   Y[t] = X[t] W + bias + scale_i (X[t] A_i) B_i,   i = index[t]
+ * W may be missing: the adapters' part is then added to `base`, what some other path gave for the same tokens (a split
+ * layer's forward, for instance), or is Y alone. */
+
+typedef struct { int32_t in, out, dtype; } ffsplit_projection;
+
+typedef struct {
+  const void* A;          /* dev [n, in, r]                                                                    */
+  const void* B;          /* dev [n, r, out]                                                                   */
+  const float* scale;     /* dev [n], NULL: 1                                                                  */
+  const int32_t* index;   /* dev [T]: the adapter of each token, negative: none.  An index of n or more counts as
+                             none and is reported as FFSPLIT_ERR_BAD_INDEX through ffsplit_poll()               */
+  int32_t n, r;           /* 1 <= r <= 128; adapters of a smaller rank are padded with zeros                    */
+} ffsplit_adapters;
+
+/* Workspace that the two calls below need. */
+ffsplit_status ffsplit_adapter_workspace_size(const ffsplit_projection* projection, int32_t n, int32_t r, int64_t T,
+                                              size_t* bytes);
+
+/* Y dev [T, out] from X dev [T, in].  W dev [in, out] and bias dev [out] (may be NULL), or base dev [T, out] (may be Y)
+ * with W and bias NULL, or none of them.  X A_i is summed in fp32 and, for FFSPLIT_BF16, rounded to bf16 before it meets B_i
+ * (the tensor cores take both operands in one type).  Fastest where the tokens of an adapter lie together.
+ * Y may not overlap X, W or the factors.  Uses the workspace. */
+ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W,
+                                       const void* bias, const void* base, const ffsplit_adapters* adapters,
+                                       const void* X, int64_t T, void* Y, void* stream);
+
+/* Gradients for fine-tuning adapters beside a projection that stays as it is.  NULL: not wanted. */
+typedef struct {
+  void* dX;   /* [T, in] = dY W^T, or base, or nothing, + scale_i (dY B_i^T) A_i^T */
+  void* dA;   /* [n, in, r], zero for adapters without tokens                     */
+  void* dB;   /* [n, r, out], likewise                                            */
+} ffsplit_adapter_grads;
+
+/* dY dev [T, out].  W and base: as above, for dX (base dev [T, in], may be dX); neither is looked at where dX is not
+ * wanted.  No gradient may overlap another or an input (but base).  Sums over tokens are taken in a fixed order. */
+ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W,
+                                        const void* base, const ffsplit_adapters* adapters, const void* X, int64_t T,
+                                        const void* dY, const ffsplit_adapter_grads* grads, void* stream);
+
 /* Synchronise `stream`, then return and clear the first device-side condition found in the workspace's
  * status word or in that of the built-in scratch of ffsplit_forward_noalloc() on the context's device
  * (FFSPLIT_OK if no kernel recorded one).  Works on a context without a workspace. */

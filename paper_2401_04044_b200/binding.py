@@ -41,6 +41,8 @@ EXPORTS = [
     "ffsplit_factor_workspace_size", "ffsplit_factor_light", "ffsplit_encoder_workspace_size", "ffsplit_encoder_forward",
     "ffsplit_train_sizes", "ffsplit_train_forward", "ffsplit_train_backward",
     "ffsplit_grad_workspace_size", "ffsplit_grad_norm", "ffsplit_grad_clip",
+    "ffsplit_muon_workspace_size", "ffsplit_muon_step",
+    "ffsplit_adapter_workspace_size", "ffsplit_adapter_forward", "ffsplit_adapter_backward",
 ]
 
 
@@ -66,6 +68,29 @@ class Factors(C.Structure):
 class TrainGrads(C.Structure):
     _fields_ = [("dX", C.c_void_p), ("dW1", C.c_void_p), ("dW1u", C.c_void_p), ("db1", C.c_void_p), ("dW2", C.c_void_p),
                 ("db2", C.c_void_p)]
+
+
+class MuonTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("momentum", C.c_void_p), ("momentum_out", C.c_void_p), ("weight", C.c_void_p),
+                ("out", C.c_void_p), ("rows", C.c_int32), ("cols", C.c_int32), ("grad_dtype", C.c_int32),
+                ("weight_dtype", C.c_int32), ("step", C.c_float), ("decay", C.c_float)]
+
+
+class Projection(C.Structure):
+    """A shared projection [inner, outer] and the type of its tensors."""
+    _fields_ = [("inner", C.c_int32), ("outer", C.c_int32), ("dtype", C.c_int32)]
+
+    def __init__(self, inner: int, outer: int, dtype):
+        super().__init__(inner, outer, DTYPE_IDS[dtype] if isinstance(dtype, torch.dtype) else int(dtype))
+
+
+class Adapters(C.Structure):
+    _fields_ = [("A", C.c_void_p), ("B", C.c_void_p), ("scale", C.c_void_p), ("index", C.c_void_p), ("n", C.c_int32),
+                ("r", C.c_int32)]
+
+
+class AdapterGrads(C.Structure):
+    _fields_ = [("dX", C.c_void_p), ("dA", C.c_void_p), ("dB", C.c_void_p)]
 
 
 class FFSplitError(RuntimeError):
@@ -127,6 +152,11 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.ffsplit_grad_workspace_size.argtypes = [i32, P(sz)]
     lib.ffsplit_grad_norm.argtypes = [vp, vp, i32, vp, vp]
     lib.ffsplit_grad_clip.argtypes = [vp, vp, i32, C.c_float, vp, vp]
+    lib.ffsplit_muon_workspace_size.argtypes = [vp, i32, P(sz)]
+    lib.ffsplit_muon_step.argtypes = [vp, vp, i32, C.c_float, i32, vp, i32, vp]
+    lib.ffsplit_adapter_workspace_size.argtypes = [P(Projection), i32, i32, i64, P(sz)]
+    lib.ffsplit_adapter_forward.argtypes = [vp, P(Projection), vp, vp, vp, P(Adapters), vp, i64, vp, vp]
+    lib.ffsplit_adapter_backward.argtypes = [vp, P(Projection), vp, vp, P(Adapters), vp, i64, vp, P(AdapterGrads), vp]
     lib.ffsplit_poll.argtypes = [vp, vp]
     lib.ffsplit_profile_begin.argtypes = [vp]
     lib.ffsplit_profile_end.argtypes = [vp, vp, i32, P(i32), P(C.c_double), P(C.c_double)]
@@ -176,6 +206,42 @@ class GradList:
         # ffsplit_grad_tensor is four 8-byte words (the type, and padding, in the last)
         self.count = len(self.grads)
         self.array = (C.c_int64 * max(4, len(words)))(*words)
+
+
+class MuonList:
+    """The matrices that one call updates (or orthogonalises), as the array ffsplit_muon_step() takes.  `step` and `decay`
+    are numbers, or one for each matrix.  Without out_weights and out_momenta both are updated in place.  The list keeps
+    the tensors alive and names their memory: make a new one when a tensor moves or a rate changes."""
+
+    def __init__(self, device: int, grads, weights=None, momenta=None, step=0.0, decay=0.0, out=None, out_momenta=None):
+        self.grads, n = list(grads), len(grads)
+        whole = lambda v: [None] * n if v is None else list(v)  # noqa: E731
+        self.weights, self.momenta = whole(weights), whole(momenta)
+        self.out = list(self.weights if out is None else out)
+        self.out_momenta = list(self.momenta if out_momenta is None else out_momenta)
+        rates = [list(v) if isinstance(v, (list, tuple)) else [v] * n for v in (step, decay)]
+        if any(len(v) != n for v in (self.weights, self.momenta, self.out, self.out_momenta, *rates)):
+            raise FFSplitError(2, "muon_list", "lists must be of the same length")
+        self.count = n
+        self.array = (MuonTensor * max(1, n))()
+        for e, g, w, m, o, mo, s, d in zip(self.array, self.grads, self.weights, self.momenta, self.out, self.out_momenta, *rates):
+            if g.dtype not in DTYPE_IDS or o is None or o.dtype not in DTYPE_IDS or (w is not None and w.dtype is not o.dtype):
+                raise FFSplitError(4, "muon_list", "gradients and weights are float32 or bfloat16, outputs of the weights' type")
+            if any(v is not None and v.dtype is not torch.float32 for v in (m, mo)):
+                raise FFSplitError(4, "muon_list", "momentum is float32")
+            if (m is None) != (mo is None):
+                raise FFSplitError(1, "muon_list", "momentum goes with an output for it")
+            if g.dim() != 2:
+                raise FFSplitError(2, "muon_list", "matrices have two dimensions")
+            for v in (g, w, m, o, mo):
+                if v is not None and (v.shape != g.shape or not v.is_contiguous()):
+                    raise FFSplitError(2, "muon_list", "a matrix's tensors must be contiguous and of one shape")
+            if any(v is not None and v.get_device() != device for v in (g, w, m, o, mo)):
+                raise FFSplitError(1, "muon_list", f"tensors must be on cuda:{device}")
+            e.grad, e.out, e.rows, e.cols = g.data_ptr(), o.data_ptr(), g.shape[0], g.shape[1]
+            e.weight = None if w is None else w.data_ptr()
+            e.momentum, e.momentum_out = (None, None) if m is None else (m.data_ptr(), mo.data_ptr())
+            e.grad_dtype, e.weight_dtype, e.step, e.decay = DTYPE_IDS[g.dtype], DTYPE_IDS[o.dtype], s, d
 
 
 def make_shape(d: int, m: int, act, dtype) -> Shape:
@@ -493,6 +559,75 @@ class Context:
         """ffsplit_grad_clip: the norm, then every gradient times min(1, max_norm / (norm + 1e-6))."""
         self._check(self.lib.ffsplit_grad_clip(self.h, C.byref(grads.array), grads.count, max_norm,
                                                self._norm_ptr("ffsplit_grad_clip", norm), self._stream(stream)), "ffsplit_grad_clip")
+
+    # ------------------------------------------------------------------ orthogonalised momentum
+    def muon_list(self, weights, grads, momenta, step, decay=0.0, out_weights=None, out_momenta=None) -> "MuonList":
+        return MuonList(self.device, grads, weights, momenta, step, decay, out_weights, out_momenta)
+
+    def orthogonal_list(self, matrices, out) -> "MuonList":
+        return MuonList(self.device, matrices, out=out)
+
+    def muon_workspace_size(self, tensors: "MuonList") -> int:
+        n = C.c_size_t()
+        self._check(self.lib.ffsplit_muon_workspace_size(C.byref(tensors.array), tensors.count, C.byref(n)), "ffsplit_muon_workspace_size")
+        return n.value
+
+    def muon_step(self, tensors: "MuonList", beta: float = 0.95, nesterov: bool = True, coefficients=None, iterations: int = 5,
+                  stream=None):
+        """ffsplit_muon_step: momentum, its orthogonal factor, decay and step for every matrix of the list.  `coefficients`:
+        one (a, b, c) to an iteration, in place of `iterations` times (3.4445, -4.7750, 2.0315)."""
+        c = None
+        if coefficients is not None:
+            iterations = len(coefficients)
+            if any(len(v) != 3 for v in coefficients):
+                raise FFSplitError(2, "ffsplit_muon_step", "three coefficients to an iteration")
+            c = (C.c_float * max(3, 3 * iterations))(*[x for v in coefficients for x in v])
+        self._check(self.lib.ffsplit_muon_step(self.h, C.byref(tensors.array), tensors.count, beta, int(bool(nesterov)),
+                                               c, iterations, self._stream(stream)), "ffsplit_muon_step")
+
+    def orthogonalize(self, tensors: "MuonList", coefficients=None, iterations: int = 5, stream=None):
+        """ffsplit_muon_step on a list without weights and momentum: out = the orthogonal factor of every matrix."""
+        self.muon_step(tensors, 0.0, False, coefficients, iterations, stream)
+
+    # ------------------------------------------------------------------ low-rank adapters beside a shared projection
+    def adapter_workspace_size(self, projection: Projection, n: int, r: int, T: int) -> int:
+        b = C.c_size_t()
+        rc = self.lib.ffsplit_adapter_workspace_size(C.byref(projection), n, r, T, C.byref(b))
+        if rc != OK:
+            raise FFSplitError(rc, "ffsplit_adapter_workspace_size")
+        return b.value
+
+    def _adapters(self, where, p, A, B, index, scale, T):
+        if A.dim() != 3:
+            raise FFSplitError(2, where, "A must be of shape (adapters, inner, rank)")
+        n, r, dt, op = A.shape[0], A.shape[2], DTYPES[p.dtype], self._operand
+        return Adapters(op(where, "A", A, dt, (n, p.inner, r), False), op(where, "B", B, dt, (n, r, p.outer), False),
+                        op(where, "scale", scale, torch.float32, (n,)), op(where, "index", index, torch.int32, (T,), False), n, r)
+
+    def adapter_forward(self, projection: Projection, X, A, B, index, Y, W=None, b=None, base=None, scale=None, stream=None):
+        """ffsplit_adapter_forward: Y = (X W + b, or base, or nothing) + scale_i (X A_i) B_i, i = index[t] (negative: none)."""
+        where, T, p, op = "ffsplit_adapter_forward", X.shape[0], projection, self._operand
+        dt, k, m = DTYPES[p.dtype], p.inner, p.outer
+        rc = self.lib.ffsplit_adapter_forward(
+            self.h, p, op(where, "W", W, dt, (k, m)), op(where, "b", b, dt, (m,)), op(where, "base", base, dt, (T, m)),
+            self._adapters(where, p, A, B, index, scale, T), op(where, "X", X, dt, (T, k), False), T,
+            op(where, "Y", Y, dt, (T, m), False), self._stream(stream))
+        if rc:
+            self._check(rc, where)
+
+    def adapter_backward(self, projection: Projection, X, A, B, index, dY, W=None, base=None, scale=None, dX=None, dA=None,
+                         dB=None, stream=None):
+        """ffsplit_adapter_backward: writes the gradients that are given (None: not wanted)."""
+        where, T, p, op = "ffsplit_adapter_backward", X.shape[0], projection, self._operand
+        dt, k, m = DTYPES[p.dtype], p.inner, p.outer
+        a = self._adapters(where, p, A, B, index, scale, T)
+        rc = self.lib.ffsplit_adapter_backward(
+            self.h, p, op(where, "W", W, dt, (k, m)), op(where, "base", base, dt, (T, k)), a, op(where, "X", X, dt, (T, k), False),
+            T, op(where, "dY", dY, dt, (T, m), False),
+            AdapterGrads(op(where, "dX", dX, dt, (T, k)), op(where, "dA", dA, dt, (a.n, k, a.r)), op(where, "dB", dB, dt, (a.n, a.r, m))),
+            self._stream(stream))
+        if rc:
+            self._check(rc, where)
 
     def debug_wait_timeout(self, limit_cycles: int, stream=None):
         self._check(self.lib.ffsplit_debug_wait_timeout(self.h, int(limit_cycles), self._stream(stream)),

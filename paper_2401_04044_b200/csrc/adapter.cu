@@ -1,0 +1,404 @@
+// Low-rank adapters of many requests beside a shared projection.
+//
+//   forward:   P[t] = s_i (X[t] A_i),  Y[t] = X[t] W + bias + P[t] B_i,             i = index[t]
+//   backward:  D[t] = s_i (dY[t] B_i^T),  dX[t] = dY[t] W^T + D[t] A_i^T,  dA_i = sum_t X[t]^T D[t],  dB_i = sum_t P[t]^T dY[t]
+//
+// The shared product runs on the tensor cores (train_gemm.cu).  The adapters' products have a side of at most 128: they are
+// taken on the CUDA cores in fp32, eight tokens to a block, which share a factor's elements where they use the same adapter.
+#include <cstring>
+
+#include "epilogue.cuh"
+#include "train_gemm.h"
+
+namespace ffsp {
+namespace adapter {
+
+constexpr int MAX_RANK = 128;
+constexpr int GROUP = 8;             // tokens of a block
+constexpr int THREADS = 256;
+constexpr int CHUNK = 256;           // elements along a contraction that are staged at a time
+
+template <bool F32>
+__device__ __forceinline__ float load(const void* p, long long i) {
+  return F32 ? __ldg(static_cast<const float*>(p) + i) : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+template <bool F32>
+__device__ __forceinline__ void store(void* p, long long i, float v) {
+  if (F32) static_cast<float*>(p)[i] = v;
+  else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+}
+__device__ __forceinline__ int adapter_of(const int* index, long long t, int n) {
+  const int i = __ldg(index + t);
+  return i < 0 || i >= n ? -1 : i;
+}
+
+// P[t][j] = scale_i sum_k V[t][k] F_i(k, j).  F lies as [n][K][r] (k_minor = 0) or [n][r][K].
+struct ShrinkJob {
+  const void *V, *F;
+  float* P;               // [T][r]
+  int K, k_minor;
+};
+struct ShrinkArgs {
+  ShrinkJob job[2];
+  const int* index;
+  const float* scale;
+  long long T;
+  int n, r, lanes;        // lanes: a power of two, at least r
+  int* status;
+};
+template <bool F32>
+__global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__ ShrinkArgs a) {
+  __shared__ float x[GROUP][CHUNK];
+  __shared__ float part[THREADS][GROUP + 1];
+  pdl_wait();
+  const ShrinkJob& job = a.job[blockIdx.y];
+  const long long t0 = static_cast<long long>(blockIdx.x) * GROUP;
+  const int count = a.T - t0 < GROUP ? static_cast<int>(a.T - t0) : GROUP;
+  int of[GROUP];
+#pragma unroll
+  for (int g = 0; g < GROUP; ++g) {
+    of[g] = g < count ? adapter_of(a.index, t0 + g, a.n) : -1;
+    if (threadIdx.x == 0 && blockIdx.y == 0 && g < count && __ldg(a.index + t0 + g) >= a.n)
+      record_status(a.status, FFSPLIT_ERR_BAD_INDEX, static_cast<int>(t0 + g), KID_ADAPTER);
+  }
+  const int lanes = a.lanes, slices = THREADS / lanes, j = threadIdx.x & (lanes - 1), slice = threadIdx.x / lanes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int first = 0; first < count; ++first) {
+    const int i = of[first];
+    unsigned mask = 0;
+#pragma unroll
+    for (int g = 0; g < GROUP; ++g) mask |= of[g] == i ? 1u << g : 0u;
+    if (i < 0 || (mask & ((1u << first) - 1u))) continue;      // none, or taken with an earlier token
+    const float scale = a.scale ? __ldg(a.scale + i) : 1.f;
+    const long long f0 = static_cast<long long>(i) * job.K * a.r;
+    if (!job.k_minor) {
+      float acc[GROUP] = {};
+      for (int k0 = 0; k0 < job.K; k0 += CHUNK) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < GROUP * CHUNK; e += THREADS) {
+          const int g = e / CHUNK, k = e % CHUNK;
+          x[g][k] = (mask >> g & 1u) && k0 + k < job.K ? load<F32>(job.V, (t0 + g) * job.K + k0 + k) : 0.f;
+        }
+        __syncthreads();
+        const int end = job.K - k0 < CHUNK ? job.K - k0 : CHUNK;
+        if (j < a.r) {
+          for (int k = slice; k < end; k += slices) {
+            const float f = load<F32>(job.F, f0 + static_cast<long long>(k0 + k) * a.r + j);
+#pragma unroll
+            for (int g = 0; g < GROUP; ++g) acc[g] = fmaf(x[g][k], f, acc[g]);
+          }
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < GROUP; ++g) part[threadIdx.x][g] = acc[g];
+      __syncthreads();
+      for (int e = threadIdx.x; e < a.r * GROUP; e += THREADS) {
+        const int g = e / a.r, c = e - g * a.r;
+        if (!(mask >> g & 1u)) continue;
+        float s = 0.f;
+        for (int k = 0; k < slices; ++k) s += part[k * lanes + c][g];
+        job.P[(t0 + g) * a.r + c] = scale * s;
+      }
+    } else {
+      // a warp to a rank, lanes along the contraction
+      for (int c = warp; c < a.r; c += THREADS / 32) {
+        float acc[GROUP] = {};
+        for (int k = lane; k < job.K; k += 32) {
+          const float f = load<F32>(job.F, f0 + static_cast<long long>(c) * job.K + k);
+#pragma unroll
+          for (int g = 0; g < GROUP; ++g)
+            if (mask >> g & 1u) acc[g] = fmaf(load<F32>(job.V, (t0 + g) * job.K + k), f, acc[g]);
+        }
+#pragma unroll
+        for (int g = 0; g < GROUP; ++g) {
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) acc[g] += __shfl_xor_sync(0xffffffffu, acc[g], o);
+          if (lane == 0 && (mask >> g & 1u)) job.P[(t0 + g) * a.r + c] = scale * acc[g];
+        }
+      }
+    }
+  }
+}
+
+// Y[t][c] = base[t][c] + sum_j P[t][j] F_i(j, c).  F lies as [n][r][N] (r_minor = 0) or [n][N][r].
+struct ExpandArgs {
+  const float* P;
+  const void *F, *base;
+  void* Y;
+  const int* index;
+  long long T;
+  int N, n, r, r_minor;
+};
+template <bool F32>
+__global__ void __launch_bounds__(THREADS) expand_kernel(const __grid_constant__ ExpandArgs a) {
+  __shared__ float p[MAX_RANK][GROUP];
+  pdl_wait();
+  const long long t0 = static_cast<long long>(blockIdx.x) * GROUP;
+  const int count = a.T - t0 < GROUP ? static_cast<int>(a.T - t0) : GROUP, c = blockIdx.y * THREADS + threadIdx.x;
+  int of[GROUP];
+#pragma unroll
+  for (int g = 0; g < GROUP; ++g) of[g] = g < count ? adapter_of(a.index, t0 + g, a.n) : -1;
+  for (int e = threadIdx.x; e < GROUP * a.r; e += THREADS) {
+    const int g = e / a.r, j = e - g * a.r;
+    p[j][g] = g < count && adapter_of(a.index, t0 + g, a.n) >= 0 ? __ldcg(a.P + (t0 + g) * a.r + j) : 0.f;
+  }
+  __syncthreads();
+  if (c >= a.N) return;
+  float acc[GROUP] = {};
+  for (int first = 0; first < count; ++first) {
+    const int i = of[first];
+    unsigned mask = 0;
+#pragma unroll
+    for (int g = 0; g < GROUP; ++g) mask |= of[g] == i ? 1u << g : 0u;
+    if (i < 0 || (mask & ((1u << first) - 1u))) continue;
+    const long long f0 = static_cast<long long>(i) * a.N * a.r;
+    for (int j = 0; j < a.r; ++j) {
+      const float f = load<F32>(a.F, f0 + (a.r_minor ? static_cast<long long>(c) * a.r + j : static_cast<long long>(j) * a.N + c));
+#pragma unroll
+      for (int g = 0; g < GROUP; ++g) if (mask >> g & 1u) acc[g] = fmaf(p[j][g], f, acc[g]);
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < GROUP; ++g) {
+    if (g >= count) break;
+    const long long at = (t0 + g) * a.N + c;
+    store<F32>(a.Y, at, a.base ? (F32 ? static_cast<const float*>(a.base)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(a.base)[at])) + acc[g] : acc[g]);
+  }
+}
+
+// out_i(j, c) = sum over the tokens of adapter i, in order, of P[t][j] V[t][c]; lies as [n][r][N], or [n][N][r] (r_minor).
+struct GradJob {
+  const float* P;
+  const void* V;
+  void* out;
+  int N, r_minor, blocks;
+};
+struct GradArgs {
+  GradJob job[2];
+  const int* index;
+  long long T;
+  int n, r;
+};
+constexpr int GRAD_COLS = 32, GRAD_TOKENS = 32;
+template <bool F32>
+__global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant__ GradArgs a) {
+  __shared__ float p[GRAD_TOKENS][MAX_RANK], v[GRAD_TOKENS][GRAD_COLS];
+  __shared__ int list[THREADS], found[THREADS / 32];
+  pdl_wait();
+  const int which = static_cast<int>(blockIdx.x) >= a.job[0].blocks ? 1 : 0, i = blockIdx.y;
+  const GradJob& job = a.job[which];
+  const int c0 = (blockIdx.x - (which ? a.job[0].blocks : 0)) * GRAD_COLS;
+  const int col = threadIdx.x & 31, jg = threadIdx.x >> 5, lane = col;
+  float acc[MAX_RANK / 8] = {};
+  for (long long t0 = 0; t0 < a.T; t0 += THREADS) {
+    const bool mine = t0 + threadIdx.x < a.T && __ldg(a.index + t0 + threadIdx.x) == i;
+    const unsigned votes = __ballot_sync(0xffffffffu, mine);
+    if (lane == 0) found[jg] = __popc(votes);
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < jg) before += found[w];
+      all += found[w];
+    }
+    if (mine) list[before + __popc(votes & ((1u << lane) - 1u))] = threadIdx.x;
+    __syncthreads();
+    for (int b = 0; b < all; b += GRAD_TOKENS) {
+      const int m = all - b < GRAD_TOKENS ? all - b : GRAD_TOKENS;
+      for (int e = threadIdx.x; e < m * a.r; e += THREADS) {
+        const int q = e / a.r, j = e - q * a.r;
+        p[q][j] = __ldcg(job.P + (t0 + list[b + q]) * a.r + j);
+      }
+      for (int e = threadIdx.x; e < m * GRAD_COLS; e += THREADS) {
+        const int q = e / GRAD_COLS, c = e % GRAD_COLS;
+        v[q][c] = c0 + c < job.N ? load<F32>(job.V, (t0 + list[b + q]) * job.N + c0 + c) : 0.f;
+      }
+      __syncthreads();
+      for (int q = 0; q < m; ++q) {
+        const float x = v[q][col];
+#pragma unroll
+        for (int u = 0; u < MAX_RANK / 8; ++u) if (jg + 8 * u < a.r) acc[u] = fmaf(p[q][jg + 8 * u], x, acc[u]);
+      }
+      __syncthreads();
+    }
+  }
+  if (c0 + col >= job.N) return;
+#pragma unroll
+  for (int u = 0; u < MAX_RANK / 8; ++u) {
+    const int j = jg + 8 * u;
+    if (j >= a.r) break;
+    const long long base = static_cast<long long>(i) * job.N * a.r;
+    store<F32>(job.out, base + (job.r_minor ? static_cast<long long>(c0 + col) * a.r + j : static_cast<long long>(j) * job.N + c0 + col), acc[u]);
+  }
+}
+
+}  // namespace adapter
+
+namespace {
+
+inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+struct AdapterLayout {
+  long long ldi, ldo;
+  size_t P, D, X, dY, W, parts, parts_bytes, end;
+};
+AdapterLayout adapter_layout(const ffsplit_projection& p, int r, long long T) {
+  AdapterLayout L;
+  const bool f32 = p.dtype == FFSPLIT_F32;
+  const size_t planes = f32 ? 3 : 1;
+  L.ldi = round_up_ll(p.in, 64);
+  L.ldo = round_up_ll(p.out, 64);
+  size_t off = 0;
+  L.P = off; off = up256(off + static_cast<size_t>(T) * r * 4);
+  L.D = off; off = up256(off + static_cast<size_t>(T) * r * 4);
+  L.X = off; off = up256(off + (f32 || p.in % 8 ? static_cast<size_t>(T) * L.ldi * 2 * planes : 0));
+  L.dY = off; off = up256(off + (f32 || p.out % 8 ? static_cast<size_t>(T) * L.ldo * 2 * planes : 0));
+  L.W = off; off = up256(off + (f32 || p.out % 8 ? static_cast<size_t>(p.in) * L.ldo * 2 * planes : 0));
+  const size_t want = 64 * static_cast<size_t>(T) * (L.ldi > L.ldo ? L.ldi : L.ldo);
+  L.parts_bytes = up256(want < (32u << 20) ? want : (32u << 20));
+  L.parts = off; off += L.parts_bytes;
+  L.end = off;
+  return L;
+}
+
+ffsplit_status check_projection(ffsplit_ctx* ctx, const ffsplit_projection* p, int n, int r, long long T) {
+  if (!p) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "projection is NULL");
+  if (p->dtype != FFSPLIT_F32 && p->dtype != FFSPLIT_BF16) return fail(ctx, FFSPLIT_ERR_DTYPE, "unknown dtype");
+  if (p->in < 1 || p->out < 1 || p->in > (1 << 23) || p->out > (1 << 23)) return fail(ctx, FFSPLIT_ERR_SHAPE, "in and out must be in [1, 2^23]");
+  if (n < 1 || n > 65535) return fail(ctx, FFSPLIT_ERR_SHAPE, "1 to 65535 adapters");
+  if (r < 1 || r > adapter::MAX_RANK) return fail(ctx, FFSPLIT_ERR_SHAPE, "ranks of 1 to 128");
+  if (T < 1 || T > 0x7fffff00ll) return fail(ctx, FFSPLIT_ERR_SHAPE, "T must be in [1, 2^31 - 256]");
+  return FFSPLIT_OK;
+}
+ffsplit_status check_adapters(ffsplit_ctx* ctx, const ffsplit_projection* p, const ffsplit_adapters* a, const void* X, long long T) {
+  ffsplit_status s = check_ctx(ctx, true);
+  if (s != FFSPLIT_OK) return s;
+  if (!a) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "adapters is NULL");
+  if ((s = check_projection(ctx, p, a->n, a->r, T)) != FFSPLIT_OK) return s;
+  if (!a->A || !a->B || !a->index || !X) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "NULL tensor");
+  if (!aligned16(a->A) || !aligned16(a->B) || !aligned16(X)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(a->index) & 3u) || (reinterpret_cast<uintptr_t>(a->scale) & 3u))
+    return fail(ctx, FFSPLIT_ERR_ALIGN, "index and scale must be 4-byte aligned");
+  if (kCtrlBytes + adapter_layout(*p, a->r, T).end > ctx->ws_bytes)
+    return fail(ctx, FFSPLIT_ERR_BUFFER_TOO_SMALL, "workspace too small for this call (ffsplit_adapter_workspace_size)");
+  ctx->score_prep.valid = false;   // the scoring buffers share the workspace
+  return FFSPLIT_OK;
+}
+
+// C [T, N] = V [T, K] times W [in, out] (transposed: its transpose).
+ffsplit_status shared_product(ffsplit_ctx* ctx, const ffsplit_projection& p, const AdapterLayout& L, const void* V, const void* W,
+                              const void* bias, bool transposed, long long T, void* C, cudaStream_t st) {
+  char* ws = ctx->ws + kCtrlBytes;
+  const bool f32 = p.dtype == FFSPLIT_F32;
+  train::PrepArgs prep;
+  std::memset(&prep, 0, sizeof(prep));
+  int blocks = 0;
+  const int K = transposed ? p.out : p.in, N = transposed ? p.in : p.out;
+  tg::Product g;
+  std::memset(&g, 0, sizeof(g));
+  g.a[0] = train::operand(&prep, &blocks, f32, V, T, K, transposed ? L.ldo : L.ldi, ws + (transposed ? L.dY : L.X));
+  g.b[0] = train::operand(&prep, &blocks, f32, W, p.in, p.out, L.ldo, ws + L.W);
+  g.pairs = 1;
+  g.b_mn = transposed ? 0 : 1;
+  g.M = T; g.N = N; g.K = K;
+  g.C = C; g.ldc = N; g.bias = bias;
+  const ffsplit_status s = train::launch_prepare(ctx, prep, blocks, f32, st);
+  if (s != FFSPLIT_OK) return s;
+  return tg::launch(ctx, tg::PLAIN, 0, f32, &g, 1, tg::Hidden{}, ws + L.parts, L.parts_bytes, st);
+}
+
+ffsplit_status launch_shrink(ffsplit_ctx* ctx, bool f32, adapter::ShrinkArgs& s, int jobs, const ffsplit_adapters& a, long long T, cudaStream_t st) {
+  s.index = a.index; s.scale = a.scale; s.T = T; s.n = a.n; s.r = a.r; s.status = ctx->status();
+  s.lanes = 1;
+  while (s.lanes < a.r) s.lanes *= 2;
+  const dim3 grid(static_cast<unsigned>((T + adapter::GROUP - 1) / adapter::GROUP), jobs);
+  const cudaError_t e = f32 ? launch_pdl(adapter::shrink_kernel<true>, grid, dim3(adapter::THREADS), 0, st, s)
+                            : launch_pdl(adapter::shrink_kernel<false>, grid, dim3(adapter::THREADS), 0, st, s);
+  ctx->launches++;
+  return check_cuda(ctx, e, "adapter::shrink_kernel launch");
+}
+ffsplit_status launch_expand(ffsplit_ctx* ctx, bool f32, const adapter::ExpandArgs& x, cudaStream_t st) {
+  const dim3 grid(static_cast<unsigned>((x.T + adapter::GROUP - 1) / adapter::GROUP), (x.N + adapter::THREADS - 1) / adapter::THREADS);
+  const cudaError_t e = f32 ? launch_pdl(adapter::expand_kernel<true>, grid, dim3(adapter::THREADS), 0, st, x)
+                            : launch_pdl(adapter::expand_kernel<false>, grid, dim3(adapter::THREADS), 0, st, x);
+  ctx->launches++;
+  return check_cuda(ctx, e, "adapter::expand_kernel launch");
+}
+
+}  // namespace
+}  // namespace ffsp
+
+extern "C" {
+
+ffsplit_status ffsplit_adapter_workspace_size(const ffsplit_projection* projection, int32_t n, int32_t r, int64_t T, size_t* bytes) {
+  using namespace ffsp;
+  if (!bytes) return FFSPLIT_ERR_INVALID_ARG;
+  const ffsplit_status s = check_projection(nullptr, projection, n, r, T);
+  if (s != FFSPLIT_OK) return s;
+  *bytes = kCtrlBytes + adapter_layout(*projection, r, T).end;
+  return FFSPLIT_OK;
+}
+
+ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W, const void* bias,
+                                       const void* base, const ffsplit_adapters* adapters, const void* X, int64_t T, void* Y,
+                                       void* stream) {
+  using namespace ffsp;
+  ffsplit_status s = check_adapters(ctx, projection, adapters, X, T);
+  if (s != FFSPLIT_OK) return s;
+  if (!Y) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "NULL tensor");
+  if ((W && base) || (bias && !W)) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "W (with or without bias), or base, or neither");
+  if (!aligned16(W) || !aligned16(bias) || !aligned16(base) || !aligned16(Y)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const ffsplit_projection& p = *projection;
+  const AdapterLayout L = adapter_layout(p, adapters->r, T);
+  const bool f32 = p.dtype == FFSPLIT_F32;
+  float* P = reinterpret_cast<float*>(ctx->ws + kCtrlBytes + L.P);
+  adapter::ShrinkArgs sh;
+  std::memset(&sh, 0, sizeof(sh));
+  sh.job[0] = {X, adapters->A, P, p.in, 0};
+  if ((s = launch_shrink(ctx, f32, sh, 1, *adapters, T, st)) != FFSPLIT_OK) return s;
+  if (W && (s = shared_product(ctx, p, L, X, W, bias, false, T, Y, st)) != FFSPLIT_OK) return s;
+  return launch_expand(ctx, f32, {P, adapters->B, W ? Y : base, Y, adapters->index, T, p.out, adapters->n, adapters->r, 0}, st);
+}
+
+ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W, const void* base,
+                                        const ffsplit_adapters* adapters, const void* X, int64_t T, const void* dY,
+                                        const ffsplit_adapter_grads* grads, void* stream) {
+  using namespace ffsp;
+  ffsplit_status s = check_adapters(ctx, projection, adapters, X, T);
+  if (s != FFSPLIT_OK) return s;
+  if (!dY || !grads) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "NULL tensor");
+  if (!grads->dX && !grads->dA && !grads->dB) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "no gradient asked for");
+  if (grads->dX && W && base) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "W, or base, or neither");
+  for (const void* q : {dY, W, base, static_cast<const void*>(grads->dX), static_cast<const void*>(grads->dA), static_cast<const void*>(grads->dB)})
+    if (!aligned16(q)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const ffsplit_projection& p = *projection;
+  const AdapterLayout L = adapter_layout(p, adapters->r, T);
+  const bool f32 = p.dtype == FFSPLIT_F32;
+  float *P = reinterpret_cast<float*>(ctx->ws + kCtrlBytes + L.P), *D = reinterpret_cast<float*>(ctx->ws + kCtrlBytes + L.D);
+  adapter::ShrinkArgs sh;
+  std::memset(&sh, 0, sizeof(sh));
+  int jobs = 0;
+  if (grads->dX || grads->dA) sh.job[jobs++] = {dY, adapters->B, D, p.out, 1};
+  if (grads->dB) sh.job[jobs++] = {X, adapters->A, P, p.in, 0};
+  if ((s = launch_shrink(ctx, f32, sh, jobs, *adapters, T, st)) != FFSPLIT_OK) return s;
+  if (grads->dX) {
+    if (W && (s = shared_product(ctx, p, L, dY, W, nullptr, true, T, grads->dX, st)) != FFSPLIT_OK) return s;
+    if ((s = launch_expand(ctx, f32, {D, adapters->A, W ? grads->dX : base, grads->dX, adapters->index, T, p.in, adapters->n, adapters->r, 1}, st)) != FFSPLIT_OK) return s;
+  }
+  if (!grads->dA && !grads->dB) return FFSPLIT_OK;
+  adapter::GradArgs g;
+  std::memset(&g, 0, sizeof(g));
+  int n = 0;
+  if (grads->dA) g.job[n++] = {D, X, grads->dA, p.in, 1, (p.in + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
+  if (grads->dB) g.job[n++] = {P, dY, grads->dB, p.out, 0, (p.out + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
+  g.index = adapters->index; g.T = T; g.n = adapters->n; g.r = adapters->r;
+  const dim3 grid(g.job[0].blocks + g.job[1].blocks, adapters->n);
+  const cudaError_t e = f32 ? launch_pdl(adapter::gradient_kernel<true>, grid, dim3(adapter::THREADS), 0, st, g)
+                            : launch_pdl(adapter::gradient_kernel<false>, grid, dim3(adapter::THREADS), 0, st, g);
+  ctx->launches++;
+  return check_cuda(ctx, e, "adapter::gradient_kernel launch");
+}
+
+}  // extern "C"

@@ -30,7 +30,7 @@ constexpr size_t kCtrlBytes = 65536;
 constexpr long long kMaxTicketTiles = (kCtrlBytes - kStatusBytes) / 4;
 
 enum KernelId : int {
-  KID_SELECT = 1, KID_PACK = 2, KID_GEMM_TC = 3, KID_GEMM_SIMT = 4, KID_SCORE = 5, KID_DECODE = 6, KID_FUSED = 7, KID_PROBE = 8, KID_QUANT = 9, KID_FACTOR = 10, KID_ENCODER = 11, KID_GEMM_AR = 12, KID_TRAIN = 13, KID_CLIP = 14
+  KID_SELECT = 1, KID_PACK = 2, KID_GEMM_TC = 3, KID_GEMM_SIMT = 4, KID_SCORE = 5, KID_DECODE = 6, KID_FUSED = 7, KID_PROBE = 8, KID_QUANT = 9, KID_FACTOR = 10, KID_ENCODER = 11, KID_GEMM_AR = 12, KID_TRAIN = 13, KID_CLIP = 14, KID_MUON = 15, KID_ADAPTER = 16
 };
 
 __device__ __forceinline__ void record_status(int* status, int code, int detail, int kid) {

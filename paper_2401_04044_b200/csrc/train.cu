@@ -17,21 +17,6 @@
 namespace ffsp {
 namespace train {
 
-constexpr int MAX_JOBS = 5;
-struct PrepJob {
-  const void* in;          // [rows, cols], pitch cols
-  __nv_bfloat16* out;      // pitch ld, a multiple of 64; fp32: three planes
-  long long rows, ld, plane_stride;
-  int cols, octets;        // octets of columns in a row
-  int block0;              // first block
-};
-struct PrepArgs {
-  PrepJob job[MAX_JOBS];
-  int n;
-};
-constexpr int PREP_THREADS = 256;
-template <bool F32> constexpr int PREP_UNROLL = F32 ? 2 : 4;
-
 // fp32 -> three bf16 planes (F32), or a copy of a bf16 matrix to rows of 128 bytes.  Bound by memory: a thread takes eight
 // columns at a time, 16 bytes of every output.  Rows of an odd bf16 matrix start on any two bytes: five aligned words hold
 // the eight values, shifted by half a word in every other row.
@@ -209,6 +194,26 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__
   else static_cast<__nv_bfloat16*>(j.out)[c0 + c] = __float2bfloat16_rn(t);
 }
 
+tg::Matrix operand(PrepArgs* prep, int* blocks, bool f32, const void* p, long long rows, int cols, long long ld, void* copy) {
+  if (!f32 && cols % 8 == 0) return {p, rows, cols, cols, rows * cols, 1};
+  PrepJob& j = prep->job[prep->n++];
+  j.in = p;
+  j.out = static_cast<__nv_bfloat16*>(copy);
+  j.rows = rows; j.cols = cols; j.ld = ld; j.plane_stride = rows * ld;
+  j.octets = (cols + 7) / 8;
+  j.block0 = *blocks;
+  const int per = PREP_THREADS * (f32 ? PREP_UNROLL<true> : PREP_UNROLL<false>);
+  *blocks += static_cast<int>((rows * j.octets + per - 1) / per);
+  return {j.out, rows, cols, ld, j.plane_stride, f32 ? 3 : 1};
+}
+ffsplit_status launch_prepare(ffsplit_ctx* ctx, const PrepArgs& prep, int blocks, bool f32, cudaStream_t st) {
+  if (prep.n == 0) return FFSPLIT_OK;
+  const cudaError_t e = f32 ? launch_pdl(prepare_kernel<true>, dim3(blocks), dim3(PREP_THREADS), 0, st, prep)
+                            : launch_pdl(prepare_kernel<false>, dim3(blocks), dim3(PREP_THREADS), 0, st, prep);
+  ctx->launches++;
+  return check_cuda(ctx, e, "train::prepare_kernel launch");
+}
+
 }  // namespace train
 
 namespace {
@@ -315,16 +320,7 @@ struct Pass {
 
   // A caller's tensor [rows, cols]: as it is, or as copied to `at` by the preparation launch.
   tg::Matrix tensor(const void* p, long long rows, int cols, long long ld, size_t at) {
-    if (!f32() && cols % 8 == 0) return {p, rows, cols, cols, rows * cols, 1};
-    train::PrepJob& j = prep.job[prep.n++];
-    j.in = p;
-    j.out = reinterpret_cast<__nv_bfloat16*>(ws + at);
-    j.rows = rows; j.cols = cols; j.ld = ld; j.plane_stride = rows * ld;
-    j.octets = (cols + 7) / 8;
-    j.block0 = prep_blocks;
-    const int per = train::PREP_THREADS * (f32() ? train::PREP_UNROLL<true> : train::PREP_UNROLL<false>);
-    prep_blocks += static_cast<int>((rows * j.octets + per - 1) / per);
-    return {j.out, rows, cols, ld, j.plane_stride, f32() ? 3 : 1};
+    return train::operand(&prep, &prep_blocks, f32(), p, rows, cols, ld, ws + at);
   }
   tg::Matrix hidden(const void* at) const { return {at, T, s.m, L.ldm, T * L.ldm, f32() ? 3 : 1}; }
   tg::Hidden buffers(char* saved) const {
@@ -338,13 +334,7 @@ struct Pass {
     h.col_sums = nullptr;
     return h;
   }
-  ffsplit_status prepare() {
-    if (prep.n == 0) return FFSPLIT_OK;
-    const cudaError_t e = f32() ? launch_pdl(train::prepare_kernel<true>, dim3(prep_blocks), dim3(train::PREP_THREADS), 0, st, prep)
-                                : launch_pdl(train::prepare_kernel<false>, dim3(prep_blocks), dim3(train::PREP_THREADS), 0, st, prep);
-    ctx->launches++;
-    return check_cuda(ctx, e, "train::prepare_kernel launch");
-  }
+  ffsplit_status prepare() { return train::launch_prepare(ctx, prep, prep_blocks, f32(), st); }
 };
 
 tg::Product product(const tg::Matrix& a, int a_mn, const tg::Matrix& b, int b_mn, long long M, int N, long long K) {

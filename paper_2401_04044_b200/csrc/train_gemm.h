@@ -97,4 +97,29 @@ ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Prod
                       size_t partial_room, cudaStream_t st, bool* joined = nullptr);
 
 }  // namespace tg
+
+// Operands that the tensor maps cannot take as they lie are copied first, one launch for all of a call (train.cu).
+namespace train {
+
+constexpr int MAX_JOBS = 5;
+struct PrepJob {
+  const void* in;          // [rows, cols], pitch cols
+  __nv_bfloat16* out;      // pitch ld, a multiple of 64; fp32: three planes
+  long long rows, ld, plane_stride;
+  int cols, octets;        // octets of columns in a row
+  int block0;              // first block
+};
+struct PrepArgs {
+  PrepJob job[MAX_JOBS];
+  int n;
+};
+constexpr int PREP_THREADS = 256;
+template <bool F32> constexpr int PREP_UNROLL = F32 ? 2 : 4;
+
+
+// A caller's tensor [rows, cols] as an operand: where it lies, or as the preparation launch copies it to `copy` (pitch ld).
+tg::Matrix operand(PrepArgs* prep, int* blocks, bool f32, const void* p, long long rows, int cols, long long ld, void* copy);
+ffsplit_status launch_prepare(ffsplit_ctx* ctx, const PrepArgs& prep, int blocks, bool f32, cudaStream_t st);
+
+}  // namespace train
 }  // namespace ffsp
