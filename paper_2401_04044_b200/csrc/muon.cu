@@ -4,13 +4,14 @@
 //   X <- a X + (b S + c S^2) X, S = X X^T   (rows <= cols; else X (b S + c S^2), S = X^T X),  once per (a, b, c)
 //   W' = (1 - decay) W - step X
 //
-// Two passes over the gradients (the norm, then X and M'; both read G and M), three products per iteration.  The first
-// form of the products: 64 x 64 tiles in fp32 on the CUDA cores.
+// Two passes over the gradients (the norm, then X and M'; both read G and M), then three products per iteration on the tensor
+// cores (muon_gemm.cu), the last of which updates the matrices.  Matrices of one shape are one launch, up to four shapes
+// share it.
 #include <cmath>
 #include <cstring>
 
 #include "epilogue.cuh"
-#include "internal.h"
+#include "muon.h"
 
 namespace ffsp {
 namespace muon {
@@ -19,20 +20,14 @@ constexpr int MAX_TENSORS = 128;        // of one launch's table
 constexpr int THREADS = 256;
 constexpr int MAX_PARTS = 256;          // partial sums of one matrix's squares
 
-// What the last product's epilogue needs of a matrix; lies in the workspace, written by prepare_kernel.
-struct Target {
-  const void* W;
-  void* out;
-  float keep, step;       // out = keep W - step X; without W: out = -step X
-  int f32;
-};
 struct Entry {
   const void* G;
   const float* M;
   float* Mo;
   const void* W;
   void* out;
-  float* X;               // [rows][ld]
+  __half* X;              // [rows][ld], the second plane `plane` elements on
+  long long plane;
   int rows, cols, octets; // octets of columns in a row
   int g_f32, w_f32, wide; // wide: every octet of G, M, Mo starts on 16 bytes
   int ld;
@@ -157,6 +152,7 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
   if (part == 0 && threadIdx.x == 0) {
     Target o;
     o.W = e.W; o.out = e.out; o.f32 = e.w_f32;
+    o.wide = e.cols % 8 == 0 && ((reinterpret_cast<uintptr_t>(e.W) | reinterpret_cast<uintptr_t>(e.out)) & 15u) == 0;
     o.keep = finite ? 1.0f - e.decay : 1.0f;
     o.step = e.W ? (finite ? e.step : 0.f) : finite ? -1.0f : __int_as_float(0x7fffffff);
     t.target[which] = o;
@@ -184,74 +180,227 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
         for (int k = 0; k < 8; ++k) if (c + k < e.cols) e.Mo[at + k] = m[k];
       }
     }
-    float* x = e.X + static_cast<long long>(row) * e.ld + c;
+    __align__(16) __half hi[8], lo[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = finite ? u[k] * inv : 0.f;
+    for (int k = 0; k < 8; ++k) split_half(finite ? u[k] * inv * HELD : 0.f, &hi[k], &lo[k]);
+    __half* x = e.X + static_cast<long long>(row) * e.ld + c;
+    *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(hi);
+    *reinterpret_cast<uint4*>(x + e.plane) = *reinterpret_cast<const uint4*>(lo);
   }
 }
 
-// C = alpha A B + beta D; A [M, K] lies as [K, M] rows where a_t, B [K, N] as [N, K] where b_t.  With target: the result
-// is X, and the matrix is updated instead.
-struct ProductArgs {
-  const float *A, *B, *D;
-  float* C;
-  long long batch;        // elements from one matrix of the operands to the next are as below
-  long long sA, sB, sD, sC;
-  int M, N, K, lda, ldb, ldd, ldc;
-  int a_t, b_t;
-  float alpha, beta;
-  const Target* target;
-  int cols;
+// ------------------------------------------------------------------------------------------------ thin matrices
+// p = min(rows, cols) <= 32 (an adapter's factors): the tensor cores' tiles would be nearly empty, and 15 launches are what
+// the work is not.  X stays in the row space of U, so X_n = Q U with Q a polynomial in S = U U^T: one pass over U for S, the
+// iteration on p x p matrices (S <- A S A, Q <- A Q, A = a I + b S + c S S), one pass for Q U.  S has the squares of U's
+// singular values and Q their inverses: all of that is held in fp64, so that nothing is lost over the direct form; Q U is
+// taken in fp32 where the gradient is bf16 (4e-5 at worst: entries of Q reach 485 / |U| and cancel to 0.7).
+// Bound by reading U twice; the fp64 units take 3 us of it for 32 matrices of p = 16, q = 8000.
+constexpr int THIN = 32, THIN_PARTS = 32, THIN_CHUNK = 128;
+struct ThinTable {
+  Entry t[MAX_TENSORS];
+  double* S[MAX_TENSORS];      // [parts][p][p]
+  double* Q[MAX_TENSORS];      // [p][p], for U itself (not divided by its norm)
+  int n;
+  float beta;
+  int nesterov, iterations;
+  float coefficients[48];
+  int* status;
 };
-__global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ ProductArgs p) {
-  __shared__ float As[16][65], Bs[16][65];
-  pdl_wait();
-  const int z = blockIdx.z, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const float *A = p.A + z * p.sA, *B = p.B + z * p.sB;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < p.K; k0 += 16) {
-    for (int i = threadIdx.x; i < 1024; i += 256) {
-      {
-        const int m = p.a_t ? i & 63 : i >> 4, k = p.a_t ? i >> 6 : i & 15;
-        const bool in = m0 + m < p.M && k0 + k < p.K;
-        As[k][m] = !in ? 0.f : p.a_t ? A[static_cast<long long>(k0 + k) * p.lda + m0 + m] : A[static_cast<long long>(m0 + m) * p.lda + k0 + k];
-      }
-      {
-        const int n = p.b_t ? i >> 4 : i & 63, k = p.b_t ? i & 15 : i >> 6;
-        const bool in = n0 + n < p.N && k0 + k < p.K;
-        Bs[k][n] = !in ? 0.f : p.b_t ? B[static_cast<long long>(n0 + n) * p.ldb + k0 + k] : B[static_cast<long long>(k0 + k) * p.ldb + n0 + n];
+// Columns (rows, where the matrix is tall) [begin, end) of U as u[i][k - begin], i < p, zeros behind `end`; M' is written.
+template <typename R, bool WRITE>
+__device__ __forceinline__ void load_thin(const Entry& e, float beta, int nesterov, int begin, int end, bool write_m, R (*u)[THIN_CHUNK + 1]) {
+  const bool tall = e.rows > e.cols;
+  const int p = tall ? e.cols : e.rows;
+  const int across = tall ? e.octets : (end - begin + 7) / 8, octets = (tall ? end - begin : p) * across;
+  for (int o = threadIdx.x; o < octets; o += THREADS) {
+    const int r = o / across, row = tall ? begin + r : r, octet = (tall ? 0 : begin / 8) + o - r * across;
+    float m[8], x[8];
+    load_u8(e, beta, nesterov, row, octet, m, x);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int c = octet * 8 + k;
+      if (tall) {
+        if (c < p) u[c][row - begin] = x[k];
+      } else {
+        u[row][c - begin] = x[k];      // (zero behind the last column)
       }
     }
+    if constexpr (WRITE) {
+      if (e.M) {
+        const long long at = static_cast<long long>(row) * e.cols + octet * 8;
+        if (!write_m) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) if (e.Mo != e.M && octet * 8 + k < e.cols) e.Mo[at + k] = e.M[at + k];
+        } else if (e.wide) {
+          float4* q = reinterpret_cast<float4*>(e.Mo + at);
+          q[0] = make_float4(m[0], m[1], m[2], m[3]);
+          q[1] = make_float4(m[4], m[5], m[6], m[7]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) if (octet * 8 + k < e.cols) e.Mo[at + k] = m[k];
+        }
+      }
+    }
+  }
+}
+// Columns of part `part` of a matrix: whole chunks.
+__device__ __forceinline__ void thin_range(const Entry& e, int part, int* begin, int* end) {
+  const int q = e.rows > e.cols ? e.rows : e.cols, chunks = (q + THIN_CHUNK - 1) / THIN_CHUNK, per = (chunks + e.parts - 1) / e.parts;
+  *begin = part * per * THIN_CHUNK;
+  *end = *begin + per * THIN_CHUNK < q ? *begin + per * THIN_CHUNK : q;
+}
+
+__global__ void __launch_bounds__(THREADS) thin_gram_kernel(const __grid_constant__ ThinTable t) {
+  __shared__ double u[THIN][THIN_CHUNK + 1];
+  pdl_wait();
+  int which = 0;
+  while (which + 1 < t.n && static_cast<int>(blockIdx.x) >= t.t[which + 1].block0) ++which;
+  const Entry& e = t.t[which];
+  const int part = blockIdx.x - e.block0, p = e.rows > e.cols ? e.cols : e.rows;
+  int begin, end;
+  thin_range(e, part, &begin, &end);
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  double s00 = 0.0, s01 = 0.0, s11 = 0.0, s10 = 0.0;
+  for (int k0 = begin; k0 < end; k0 += THIN_CHUNK) {
+    const int k1 = end - k0 < THIN_CHUNK ? end : k0 + THIN_CHUNK;
+    __syncthreads();
+    load_thin<double, false>(e, t.beta, t.nesterov, k0, k1, false, u);
+    __syncthreads();
+    if (ty >= p || tx >= p) continue;
+    if (p <= 16) {
+#pragma unroll 4
+      for (int k = 0; k < k1 - k0; ++k) s00 = fma(u[ty][k], u[tx][k], s00);
+    } else {
+      // (rows behind p hold what was there before: their sums are not written)
+#pragma unroll 4
+      for (int k = 0; k < k1 - k0; ++k) {
+        const double a = u[ty][k], b = u[ty + 16][k], c = u[tx][k], d = u[tx + 16][k];
+        s00 = fma(a, c, s00); s01 = fma(a, d, s01); s10 = fma(b, c, s10); s11 = fma(b, d, s11);
+      }
+    }
+  }
+  double* S = t.S[which] + static_cast<long long>(part) * p * p;
+  if (ty < p && tx < p) S[ty * p + tx] = s00;
+  if (ty < p && tx + 16 < p) S[ty * p + tx + 16] = s01;
+  if (ty + 16 < p && tx < p) S[(ty + 16) * p + tx] = s10;
+  if (ty + 16 < p && tx + 16 < p) S[(ty + 16) * p + tx + 16] = s11;
+}
+
+// C = A B, each p x p (padded with zeros to 32); a thread to four entries.
+__device__ __forceinline__ void thin_product(const double (*A)[THIN + 1], const double (*B)[THIN + 1], int p, double* c) {
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  c[0] = c[1] = c[2] = c[3] = 0.0;
+#pragma unroll 4
+  for (int k = 0; k < p; ++k) {
+    const double a = A[ty][k], b = A[ty + 16][k], x = B[k][tx], y = B[k][tx + 16];
+    c[0] = fma(a, x, c[0]); c[1] = fma(a, y, c[1]); c[2] = fma(b, x, c[2]); c[3] = fma(b, y, c[3]);
+  }
+}
+__global__ void __launch_bounds__(THREADS) thin_solve_kernel(const __grid_constant__ ThinTable t) {
+  __shared__ double S[THIN][THIN + 1], A[THIN][THIN + 1], Q[THIN][THIN + 1];
+  __shared__ double norm;
+  pdl_wait();
+  const Entry& e = t.t[blockIdx.x];
+  const int p = e.rows > e.cols ? e.cols : e.rows;
+  const double* partial = t.S[blockIdx.x];
+  for (int i = threadIdx.x; i < THIN * THIN; i += THREADS) {
+    const int r = i / THIN, c = i % THIN;
+    double s = 0.0;
+    if (r < p && c < p) {
+#pragma unroll 8
+      for (int k = 0; k < e.parts; ++k) s += __ldcg(partial + static_cast<long long>(k) * p * p + r * p + c);
+    }
+    S[r][c] = s;
+    Q[r][c] = r == c ? 1.0 : 0.0;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double trace = 0.0;
+    for (int i = 0; i < p; ++i) trace += S[i][i];
+    norm = sqrt(trace);
+  }
+  __syncthreads();
+  const bool finite = isfinite(static_cast<float>(norm));
+  const double inv = finite ? 1.0 / (norm + 1e-7) : 0.0;
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  const int row[4] = {ty, ty, ty + 16, ty + 16}, col[4] = {tx, tx + 16, tx, tx + 16};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) S[row[i]][col[i]] *= inv * inv;
+  __syncthreads();
+  for (int it = 0; it < t.iterations && finite; ++it) {
+    const double a = t.coefficients[3 * it], b = t.coefficients[3 * it + 1], c = t.coefficients[3 * it + 2];
+    double x[4];
+    thin_product(S, S, p, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) A[row[i]][col[i]] = fma(c, x[i], fma(b, S[row[i]][col[i]], row[i] == col[i] ? a : 0.0));
+    __syncthreads();
+    double y[4];
+    thin_product(A, Q, p, x);
+    thin_product(A, S, p, y);
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      float a[4], b[4];
+    for (int i = 0; i < 4; ++i) { Q[row[i]][col[i]] = x[i]; S[row[i]][col[i]] = y[i]; }
+    __syncthreads();
+    thin_product(S, A, p, x);
+    __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { a[i] = As[k][ty + 16 * i]; b[i] = Bs[k][tx + 16 * i]; }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
-    }
+    for (int i = 0; i < 4; ++i) S[row[i]][col[i]] = x[i];
     __syncthreads();
   }
+  // what is not finite leaves here as NaN: the last kernel leaves such a matrix alone
 #pragma unroll
   for (int i = 0; i < 4; ++i)
+    if (row[i] < p && col[i] < p) t.Q[blockIdx.x][row[i] * p + col[i]] = finite ? Q[row[i]][col[i]] * inv : __longlong_as_double(0x7fffffffffffffffll);
+  if (threadIdx.x == 0 && !finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, blockIdx.x, KID_MUON);
+}
+
+template <typename R>
+__global__ void __launch_bounds__(THREADS) thin_apply_kernel(const __grid_constant__ ThinTable t) {
+  __shared__ R u[THIN][THIN_CHUNK + 1], Q[THIN][THIN];
+  pdl_wait();
+  int which = 0;
+  while (which + 1 < t.n && static_cast<int>(blockIdx.x) >= t.t[which + 1].block0) ++which;
+  const Entry& e = t.t[which];
+  const bool tall = e.rows > e.cols;
+  const int p = tall ? e.cols : e.rows, part = blockIdx.x - e.block0;
+  for (int i = threadIdx.x; i < p * p; i += THREADS) Q[i / p][i % p] = static_cast<R>(__ldcg(t.Q[which] + i));
+  int begin, end;
+  thin_range(e, part, &begin, &end);
+  const int k = threadIdx.x & (THIN_CHUNK - 1), group = threadIdx.x / THIN_CHUNK;
+  constexpr int AT_ONCE = 4;
+  bool finite = true;
+  for (int k0 = begin; k0 < end; k0 += THIN_CHUNK) {
+    const int k1 = end - k0 < THIN_CHUNK ? end : k0 + THIN_CHUNK;
+    __syncthreads();
+    if (k0 == begin) finite = Q[0][0] == Q[0][0];
+    load_thin<R, true>(e, t.beta, t.nesterov, k0, k1, finite, u);
+    __syncthreads();
+    if (k0 + k >= k1) continue;
+    for (int j0 = group * AT_ONCE; j0 < p; j0 += THREADS / THIN_CHUNK * AT_ONCE) {
+      R acc[AT_ONCE] = {};
+      for (int i = 0; i < p; ++i) {
+        const R x = u[i][k];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-      if (m >= p.M || n >= p.N) continue;
-      float v = p.alpha * acc[i][j];
-      if (p.D) v = fmaf(p.beta, p.D[z * p.sD + static_cast<long long>(m) * p.ldd + n], v);
-      if (p.target) {
-        const Target& t = p.target[z];
-        const long long at = static_cast<long long>(m) * p.cols + n;
-        if (t.f32) static_cast<float*>(t.out)[at] = (t.W ? t.keep * static_cast<const float*>(t.W)[at] : 0.f) - t.step * v;
-        else static_cast<__nv_bfloat16*>(t.out)[at] = __float2bfloat16_rn((t.W ? t.keep * __bfloat162float(static_cast<const __nv_bfloat16*>(t.W)[at]) : 0.f) - t.step * v);
-      } else {
-        p.C[z * p.sC + static_cast<long long>(m) * p.ldc + n] = v;
+        for (int j = 0; j < AT_ONCE; ++j) acc[j] = fma(Q[j0 + j < THIN ? j0 + j : 0][i], x, acc[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        if (j0 + j >= p) break;
+        const long long at = tall ? static_cast<long long>(k0 + k) * e.cols + j0 + j : static_cast<long long>(j0 + j) * e.cols + k0 + k;
+        const float x = static_cast<float>(acc[j]);
+        float o;
+        if (!e.W) {
+          o = x;
+        } else {
+          const float w = e.w_f32 ? static_cast<const float*>(e.W)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(e.W)[at]);
+          o = finite ? fmaf(1.0f - e.decay, w, -e.step * x) : w;
+        }
+        if (e.w_f32) static_cast<float*>(e.out)[at] = o;
+        else static_cast<__nv_bfloat16*>(e.out)[at] = __float2bfloat16_rn(o);
       }
     }
+  }
 }
 
 }  // namespace muon
@@ -262,11 +411,17 @@ constexpr float kStandard[3] = {3.4445f, -4.7750f, 2.0315f};
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Bytes of one matrix's buffers: X twice, S and b S + c S^2.
+// Bytes of one matrix's buffers: X twice, S and P = b S + c S^2, two planes each.
+size_t x_bytes(int rows, int cols) { return static_cast<size_t>(rows) * round_up(cols, 64) * 4; }
+int thin_parts(int rows, int cols) {
+  const int chunks = ((rows < cols ? cols : rows) + muon::THIN_CHUNK - 1) / muon::THIN_CHUNK;
+  return chunks < muon::THIN_PARTS ? chunks : muon::THIN_PARTS;
+}
+bool is_thin(int rows, int cols) { return (rows < cols ? rows : cols) <= muon::THIN; }
 size_t matrix_bytes(int rows, int cols) {
   const int p = rows < cols ? rows : cols;
-  const size_t x = up256(static_cast<size_t>(rows) * round_up(cols, 64) * 4), s = up256(static_cast<size_t>(p) * round_up(p, 64) * 4);
-  return 2 * x + 2 * s;
+  if (is_thin(rows, cols)) return up256(static_cast<size_t>(thin_parts(rows, cols) + 1) * p * p * sizeof(double));
+  return 2 * x_bytes(rows, cols) + 2 * x_bytes(p, p);
 }
 constexpr size_t kTableBytes = muon::MAX_TENSORS * (muon::MAX_PARTS * sizeof(double) + sizeof(muon::Target));
 // Matrices are worked on in runs: as many as fit the tables and half a gigabyte, one at least.
@@ -296,7 +451,7 @@ ffsplit_status check_list(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int co
   return FFSPLIT_OK;
 }
 
-// Whether the iteration keeps singular values of [0, 1] below 1.5.
+// Whether the iteration keeps singular values of [0, 1] below 1.5 and P = b S + c S^2 below 200.
 bool coefficients_hold(const float* c, int iterations) {
   double top = 1.0;
   for (int i = 0; i < iterations; ++i, c += 3) {
@@ -305,6 +460,7 @@ bool coefficients_hold(const float* c, int iterations) {
     for (int k = 0; k <= 4096; ++k) {
       const double s = top * k / 4096, v = std::fabs(s * (c[0] + s * s * (c[1] + s * s * c[2])));
       if (v > most) most = v;
+      if (!(std::fabs(s * s * (c[1] + s * s * c[2])) <= 200.0)) return false;
     }
     if (!(most <= 1.5)) return false;
     top = most;
@@ -312,11 +468,102 @@ bool coefficients_hold(const float* c, int iterations) {
   return true;
 }
 
-ffsplit_status run_products(ffsplit_ctx* ctx, muon::ProductArgs& p, int batch, cudaStream_t st) {
-  const dim3 grid((p.N + 63) / 64, (p.M + 63) / 64, batch);
-  const cudaError_t e = launch_pdl(muon::product_kernel, grid, dim3(256), 0, st, p);
-  ctx->launches++;
-  return check_cuda(ctx, e, "muon::product_kernel launch");
+// Matrices of one shape and precision.
+struct Group {
+  int first, count, rows, cols;
+  bool precise;
+  muon::Matrices X[2], S, P;
+};
+
+// All iterations of up to MAX_GROUPS groups of one precision.
+ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon::Target* targets, const float* coefficients, int iterations, cudaStream_t st) {
+  const bool precise = groups[0]->precise;
+  for (int it = 0; it < iterations; ++it) {
+    const float* k = coefficients ? coefficients + 3 * it : kStandard;
+    muon::Product q[muon::MAX_GROUPS];
+    for (int step = 0; step < 3; ++step) {
+      std::memset(q, 0, sizeof(q));
+      for (int i = 0; i < n; ++i) {
+        Group& g = *groups[i];
+        const bool tall = g.rows > g.cols;
+        const muon::Matrices &X = g.X[it & 1], &Y = g.X[(it + 1) & 1];
+        muon::Product& p = q[i];
+        p.alpha = 1.f / muon::HELD;
+        if (step == 0) {             // S = X X^T
+          p.a = p.b = X; p.c = g.S;
+          p.a_mn = p.b_mn = tall;
+          p.M = p.N = g.S.rows; p.K = tall ? g.rows : g.cols;
+          p.symmetric = 1;
+          p.c_low = precise;
+        } else if (step == 1) {      // P = b S + c S S
+          p.a = p.b = g.S; p.c = g.P;
+          p.M = p.N = p.K = g.S.rows;
+          p.alpha *= k[2]; p.beta = k[1];
+          p.d = &g.S; p.d_low = precise;
+          p.symmetric = 1;
+          p.c_low = precise;
+        } else {                     // a X + P X, or a X + X P
+          p.a = tall ? X : g.P; p.b = tall ? g.P : X; p.c = Y;
+          p.b_mn = !tall;
+          p.M = g.rows; p.N = g.cols; p.K = g.S.rows;
+          p.beta = k[0];
+          p.d = &X; p.d_low = 1;
+          p.c_low = 1;
+          if (it + 1 == iterations) p.target = targets + g.first;
+        }
+      }
+      const ffsplit_status s = muon::launch_products(ctx, precise, q, n, st);
+      if (s != FFSPLIT_OK) return s;
+    }
+  }
+  return FFSPLIT_OK;
+}
+
+// What every kernel needs of a matrix.
+muon::Entry entry_for(const ffsplit_muon_tensor& s) {
+  muon::Entry e;
+  std::memset(&e, 0, sizeof(e));
+  e.G = s.grad; e.M = s.momentum; e.Mo = s.momentum_out; e.W = s.weight; e.out = s.out;
+  e.rows = s.rows; e.cols = s.cols; e.octets = (s.cols + 7) / 8;
+  e.g_f32 = s.grad_dtype == FFSPLIT_F32; e.w_f32 = s.weight_dtype == FFSPLIT_F32;
+  e.wide = s.cols % 8 == 0 && aligned16(s.grad) && aligned16(s.momentum) && aligned16(s.momentum_out);
+  e.step = s.step; e.decay = s.decay;
+  return e;
+}
+
+// The thin matrices of one precision among t: three launches.
+ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, bool precise, float beta, int nesterov, const float* coefficients,
+                        int iterations, char* at, cudaStream_t st) {
+  muon::ThinTable tab;
+  std::memset(&tab, 0, sizeof(tab));
+  tab.beta = beta; tab.nesterov = nesterov; tab.iterations = iterations;
+  for (int i = 0; i < 3 * iterations; ++i) tab.coefficients[i] = coefficients ? coefficients[i] : kStandard[i % 3];
+  tab.status = ctx->status();
+  int blocks = 0;
+  for (int i = 0; i < n; ++i) {
+    const ffsplit_muon_tensor& s = t[i];
+    if (!is_thin(s.rows, s.cols) || (s.grad_dtype == FFSPLIT_F32) != precise) continue;
+    const int p = s.rows < s.cols ? s.rows : s.cols, parts = thin_parts(s.rows, s.cols);
+    muon::Entry& e = tab.t[tab.n];
+    e = entry_for(s);
+    e.parts = parts;
+    // (parts are whole chunks: fewer of them may do)
+    const int chunks = ((s.rows < s.cols ? s.cols : s.rows) + muon::THIN_CHUNK - 1) / muon::THIN_CHUNK, per = (chunks + parts - 1) / parts;
+    e.parts = (chunks + per - 1) / per;
+    e.block0 = blocks;
+    blocks += e.parts;
+    tab.S[tab.n] = reinterpret_cast<double*>(at);
+    tab.Q[tab.n] = tab.S[tab.n] + static_cast<size_t>(parts) * p * p;
+    at += matrix_bytes(s.rows, s.cols);
+    ++tab.n;
+  }
+  if (tab.n == 0) return FFSPLIT_OK;
+  cudaError_t e = launch_pdl(muon::thin_gram_kernel, dim3(blocks), dim3(muon::THREADS), 0, st, tab);
+  if (e == cudaSuccess) e = launch_pdl(muon::thin_solve_kernel, dim3(tab.n), dim3(muon::THREADS), 0, st, tab);
+  if (e == cudaSuccess) e = precise ? launch_pdl(muon::thin_apply_kernel<double>, dim3(blocks), dim3(muon::THREADS), 0, st, tab)
+                                    : launch_pdl(muon::thin_apply_kernel<float>, dim3(blocks), dim3(muon::THREADS), 0, st, tab);
+  ctx->launches += 3;
+  return check_cuda(ctx, e, "muon::thin kernels launch");
 }
 
 ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, float beta, int nesterov, const float* coefficients,
@@ -324,32 +571,45 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
   char* ws = ctx->ws + kCtrlBytes;
   muon::Table tab;
   std::memset(&tab, 0, sizeof(tab));
-  tab.n = n; tab.beta = beta; tab.nesterov = nesterov;
+  tab.beta = beta; tab.nesterov = nesterov;
   tab.partial = reinterpret_cast<double*>(ws);
   tab.target = reinterpret_cast<muon::Target*>(ws + sizeof(double) * muon::MAX_TENSORS * muon::MAX_PARTS);
   tab.status = ctx->status();
   char* at = ws + up256(kTableBytes);
+  for (int precise = 0; precise < 2; ++precise) {
+    const ffsplit_status s = run_thin(ctx, t, n, precise != 0, beta, nesterov, coefficients, iterations, at, st);
+    if (s != FFSPLIT_OK) return s;
+    for (int i = 0; i < n; ++i)
+      if (is_thin(t[i].rows, t[i].cols) && (t[i].grad_dtype == FFSPLIT_F32) == (precise != 0)) at += matrix_bytes(t[i].rows, t[i].cols);
+  }
   // matrices of one shape lie one after the other, whatever their place in the list
-  struct Group { int first, count, rows, cols; char *X0, *X1, *S, *P; };
   Group groups[muon::MAX_TENSORS];
   int order[muon::MAX_TENSORS], n_groups = 0, placed = 0;
   bool done[muon::MAX_TENSORS] = {};
+  const auto matrices = [&](int rows, int cols, int count) {
+    muon::Matrices m;
+    m.p = reinterpret_cast<__half*>(at);
+    m.rows = rows; m.cols = cols; m.ld = round_up(cols, 64); m.count = count;
+    m.each = static_cast<long long>(rows) * m.ld; m.plane = m.each * count;
+    at += x_bytes(rows, cols) * count;
+    return m;
+  };
   for (int i = 0; i < n; ++i) {
-    if (done[i]) continue;
+    if (done[i] || is_thin(t[i].rows, t[i].cols)) continue;
     Group& g = groups[n_groups++];
     g.first = placed; g.count = 0; g.rows = t[i].rows; g.cols = t[i].cols;
+    g.precise = t[i].grad_dtype == FFSPLIT_F32;
     for (int j = i; j < n; ++j)
-      if (!done[j] && t[j].rows == g.rows && t[j].cols == g.cols) {
+      if (!done[j] && t[j].rows == g.rows && t[j].cols == g.cols && (t[j].grad_dtype == FFSPLIT_F32) == g.precise) {
         done[j] = true;
         order[placed++] = j;
         ++g.count;
       }
     const int p = g.rows < g.cols ? g.rows : g.cols;
-    const size_t x = up256(static_cast<size_t>(g.rows) * round_up(g.cols, 64) * 4), s = up256(static_cast<size_t>(p) * round_up(p, 64) * 4);
-    g.X0 = at; at += x * g.count;
-    g.X1 = at; at += x * g.count;
-    g.S = at; at += s * g.count;
-    g.P = at; at += s * g.count;
+    g.X[0] = matrices(g.rows, g.cols, g.count);
+    g.X[1] = matrices(g.rows, g.cols, g.count);
+    g.S = matrices(p, p, g.count);
+    g.P = matrices(p, p, g.count);
   }
   int blocks = 0;
   for (int gi = 0, k = 0; gi < n_groups; ++gi) {
@@ -357,57 +617,34 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
     for (int j = 0; j < g.count; ++j, ++k) {
       const ffsplit_muon_tensor& s = t[order[k]];
       muon::Entry& e = tab.t[k];
-      e.G = s.grad; e.M = s.momentum; e.Mo = s.momentum_out; e.W = s.weight; e.out = s.out;
-      e.rows = s.rows; e.cols = s.cols; e.octets = (s.cols + 7) / 8;
-      e.g_f32 = s.grad_dtype == FFSPLIT_F32; e.w_f32 = s.weight_dtype == FFSPLIT_F32;
-      e.ld = round_up(s.cols, 64);
-      e.X = reinterpret_cast<float*>(g.X0 + j * up256(static_cast<size_t>(s.rows) * e.ld * 4));
-      e.wide = s.cols % 8 == 0 && aligned16(s.grad) && aligned16(s.momentum) && aligned16(s.momentum_out);
-      e.step = s.step; e.decay = s.decay;
+      e = entry_for(s);
+      e.ld = g.X[0].ld;
+      e.X = g.X[0].p + j * g.X[0].each;
+      e.plane = g.X[0].plane;
       const long long octets = static_cast<long long>(s.rows) * e.octets;
       e.parts = static_cast<int>(octets < 512ll * muon::MAX_PARTS ? (octets + 511) / 512 : muon::MAX_PARTS);
       e.block0 = blocks;
       blocks += e.parts;
     }
   }
+  if (placed == 0) return FFSPLIT_OK;
+  tab.n = placed;
   cudaError_t e = launch_pdl(muon::norm_kernel, dim3(blocks), dim3(muon::THREADS), 0, st, tab);
   ctx->launches++;
   if (e != cudaSuccess) return check_cuda(ctx, e, "muon::norm_kernel launch");
   e = launch_pdl(muon::prepare_kernel, dim3(blocks), dim3(muon::THREADS), 0, st, tab);
   ctx->launches++;
   if (e != cudaSuccess) return check_cuda(ctx, e, "muon::prepare_kernel launch");
-  for (int gi = 0; gi < n_groups; ++gi) {
-    const Group& g = groups[gi];
-    const bool tall = g.rows > g.cols;
-    const int p = tall ? g.cols : g.rows, ldx = round_up(g.cols, 64), lds = round_up(p, 64);
-    const long long sx = static_cast<long long>(up256(static_cast<size_t>(g.rows) * ldx * 4)) / 4, ss = static_cast<long long>(up256(static_cast<size_t>(p) * lds * 4)) / 4;
-    float *X = reinterpret_cast<float*>(g.X0), *Y = reinterpret_cast<float*>(g.X1), *S = reinterpret_cast<float*>(g.S), *P = reinterpret_cast<float*>(g.P);
-    for (int it = 0; it < iterations; ++it) {
-      const float a = coefficients ? coefficients[3 * it] : kStandard[0], b = coefficients ? coefficients[3 * it + 1] : kStandard[1],
-                  c = coefficients ? coefficients[3 * it + 2] : kStandard[2];
-      muon::ProductArgs q;
-      std::memset(&q, 0, sizeof(q));
-      q.A = q.B = X; q.sA = q.sB = sx; q.lda = q.ldb = ldx;
-      q.M = q.N = p; q.K = tall ? g.rows : g.cols;
-      q.a_t = tall; q.b_t = !tall;
-      q.C = S; q.sC = ss; q.ldc = lds; q.alpha = 1.f;
-      ffsplit_status r = run_products(ctx, q, g.count, st);
-      if (r != FFSPLIT_OK) return r;
-      std::memset(&q, 0, sizeof(q));
-      q.A = q.B = q.D = S; q.sA = q.sB = q.sD = ss; q.lda = q.ldb = q.ldd = lds;
-      q.M = q.N = q.K = p;
-      q.b_t = 1;
-      q.C = P; q.sC = ss; q.ldc = lds; q.alpha = c; q.beta = b;
-      if ((r = run_products(ctx, q, g.count, st)) != FFSPLIT_OK) return r;
-      std::memset(&q, 0, sizeof(q));
-      q.M = g.rows; q.N = g.cols; q.K = p;
-      q.A = tall ? X : P; q.sA = tall ? sx : ss; q.lda = tall ? ldx : lds;
-      q.B = tall ? P : X; q.sB = tall ? ss : sx; q.ldb = tall ? lds : ldx;
-      q.D = X; q.sD = sx; q.ldd = ldx; q.alpha = 1.f; q.beta = a;
-      q.C = Y; q.sC = sx; q.ldc = ldx;
-      if (it + 1 == iterations) { q.target = tab.target + g.first; q.cols = g.cols; }
-      if ((r = run_products(ctx, q, g.count, st)) != FFSPLIT_OK) return r;
-      float* swap = X; X = Y; Y = swap;
+  for (int precise = 0; precise < 2; ++precise) {
+    Group* some[muon::MAX_GROUPS];
+    int m = 0;
+    for (int gi = 0; gi <= n_groups; ++gi) {
+      if (gi < n_groups && groups[gi].precise == (precise != 0)) some[m++] = &groups[gi];
+      if (m == muon::MAX_GROUPS || (gi == n_groups && m > 0)) {
+        const ffsplit_status s = iterate(ctx, some, m, tab.target, coefficients, iterations, st);
+        if (s != FFSPLIT_OK) return s;
+        m = 0;
+      }
     }
   }
   return FFSPLIT_OK;

@@ -1,0 +1,58 @@
+// The products of a Newton-Schulz iteration, as muon_gemm.cu runs them.  Not part of the public ABI.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include "internal.h"
+
+namespace ffsp {
+namespace muon {
+
+// X, S = X X^T and P = b S + c S^2 are held as fp16 times 256, which keeps values from 2.4e-7 to 200 normal: singular
+// values of X stay below 1.5, so its elements do, S's below 2.3, and P is checked to stay below 200.  A second plane holds
+// what the first one rounds off, times 2048: 22 bits together.
+constexpr float HELD = 256.f, LOW = 2048.f;
+
+// `count` matrices [rows, cols] with pitch ld (a multiple of 64), one after the other; the second plane `plane` elements on.
+struct Matrices {
+  __half* p;
+  int rows, cols, ld, count;
+  long long each, plane;
+};
+
+// What the last product's epilogue needs of a matrix; lies in the workspace.
+struct Target {
+  const void* W;
+  void* out;
+  float keep, step;       // out = keep W - step X; without W: out = -step X
+  int f32, wide;          // wide: every 16 columns of W and out start on 16 bytes
+};
+
+// C = alpha A B^ + beta D for every matrix of a group.
+struct Product {
+  Matrices a, b, c;       // a: [M, K], or [K, M] with a_mn; b: [N, K], or [K, N] with b_mn
+  int a_mn, b_mn;
+  int M, N, K;
+  float alpha, beta;
+  const Matrices* d;      // nullptr: no second term
+  int d_low;              // its second plane is added too
+  int symmetric;          // C = C^T: tiles above the diagonal only, and mirrored
+  int c_low;              // the second plane of C is written
+  const Target* target;   // the last product: the matrices are updated, nothing is written to c
+};
+
+constexpr int MAX_GROUPS = 4;
+// precise: operands count with both planes (three products of planes), sums leave the tensor cores every few k-blocks.
+ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* products, int n, cudaStream_t st);
+
+#ifdef __CUDACC__
+// One value's two planes.
+__device__ __forceinline__ void split_half(float x, __half* hi, __half* lo) {
+  *hi = __float2half_rn(x);
+  *lo = __float2half_rn((x - __half2float(*hi)) * LOW);
+}
+#endif
+
+}  // namespace muon
+}  // namespace ffsp

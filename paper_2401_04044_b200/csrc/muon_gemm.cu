@@ -1,0 +1,580 @@
+// The three products of a Newton-Schulz iteration on the tensor cores:
+//
+//   S = X X^T,   P = b S + c S S,   X <- a X + P X          (rows > cols: S = X^T X, X <- a X + X P)
+//
+// for a group of matrices of one shape, up to four groups to a launch.  A persistent pair of CTAs (cta_group::2) takes
+// 256 x 256 (or 256 x 128) tiles: TMA into a ring of stages, one thread issues the MMAs of both CTAs, two accumulators, the
+// epilogue of a tile under the MMAs of the next.  X lies as it came: whichever of its axes a product sums over, the operand
+// is staged K-major or MN-major (a bit of the instruction descriptor and the shape of the TMA box).
+//
+// S and S S are symmetric: only tiles on and above the diagonal are computed, the others are written by their mirror images
+// (of 3 p^2 q + 2 p^3 multiply-adds per iteration, p <= q, (p^2 q + p^3) / 2 go).
+//
+// Operands are fp16 (11 bits; bf16 has 8 at the same rate).  Rounding S or P multiplies X by a matrix close to the identity,
+// which the iteration corrects or carries along as it is.  Rounding X would add noise in every direction, and directions
+// with small singular values would drown in what is rounded off the large ones (a momentum with a few strong directions: 1e-2
+// of the result, with bf16 8e-2).  So X has a second plane for the next 11 bits, which the term a X reads but the tensor
+// cores do not: 1.5e-4 to 2e-3, for 2 bytes more read and written per element.  precise: the tensor cores take the second
+// planes too (three products of planes, the small ones first), and sums leave them every PROMOTE k-blocks, because their
+// running sums are cut, not rounded (see train_gemm.cu).
+//
+// Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
+#include <cstring>
+
+#include "epilogue.cuh"
+#include "muon.h"
+#include "ptx.cuh"
+
+namespace ffsp {
+namespace muon {
+
+constexpr int CTA_M = 128, TILE_M = 256, TILE_N = 256, BLOCK_K = 64;
+constexpr int MAX_STAGES = 8;
+constexpr int BLOCK64_BYTES = 64 * BLOCK_K * 2;
+constexpr int TMEM_COLS = 512;
+constexpr int BAR_BYTES = 256;
+constexpr int MAX_SMEM = 232448;
+constexpr int RING_BYTES = (MAX_SMEM - 1024 - BAR_BYTES) / 1024 * 1024;
+constexpr int EPI_WARPS = 8, GROUPS = EPI_WARPS / 4;
+// precise: the epilogue's sums take 128 registers a thread; it starts on a warpgroup's boundary so that registers can move
+// to it (384 threads start with 168 each; 128 of them go down to 56 and 256 up to 224: 64512 in all).
+template <bool PRECISE> constexpr int FIRST_EPI = PRECISE ? 4 : 2;
+constexpr int START_REGS = 168, ROLE_REGS = 56, EPI_REGS = 224;
+static_assert(ROLE_REGS * 128 + EPI_REGS * 256 <= START_REGS * 384, "a split above what the block starts with waits forever");
+template <bool PRECISE> constexpr int GEMM_THREADS = 32 * (EPI_WARPS + FIRST_EPI<PRECISE>);
+constexpr int PROMOTE = 4;
+
+struct DevProduct {
+  CUtensorMap a, b;
+  int M, N, kb, count;
+  int a_mn, b_mn, symmetric;
+  int tiles_m, tiles_n, tiles, panel_m;
+  int unit0;
+  float alpha, beta;
+  const __half* D;
+  long long d_each, d_plane;
+  int ldd, d_low;
+  __half* C;
+  long long c_each, c_plane;
+  int ldc, c_low;
+  const Target* target;
+};
+struct Params {
+  DevProduct prod[MAX_GROUPS];
+  int n, units, tile_n, stages, stage_bytes;
+  int* status;
+};
+struct Unit {
+  int prod, batch, m_blk, n_blk;
+};
+__device__ __forceinline__ Unit find_unit(const Params& p, int u) {
+  Unit r;
+  r.prod = 0;
+  while (r.prod + 1 < p.n && u >= p.prod[r.prod + 1].unit0) ++r.prod;
+  const DevProduct& d = p.prod[r.prod];
+  const int in = u - d.unit0;
+  r.batch = in / d.tiles;
+  int tile = in - r.batch * d.tiles;
+  if (d.symmetric) {
+    // row block m starts at the column block that holds its diagonal
+    const int step = TILE_M / p.tile_n;
+    int m = 0, width = d.tiles_n;
+    while (tile >= width) { tile -= width; ++m; width -= step; }
+    r.m_blk = m;
+    r.n_blk = m * step + tile;
+  } else {
+    const int per_panel = d.panel_m * d.tiles_n;
+    const int panel = tile / per_panel, in_panel = tile - panel * per_panel, m0 = panel * d.panel_m;
+    const int h = d.tiles_m - m0 < d.panel_m ? d.tiles_m - m0 : d.panel_m;
+    r.n_blk = in_panel / h;
+    r.m_blk = m0 + (in_panel - r.n_blk * h);
+  }
+  return r;
+}
+// precise: k-blocks of a unit are counted over three runs, (low, high), (high, low), (high, high).  End of the part of the
+// sum that begins at `begin`: both small runs are one part.
+__device__ __forceinline__ int part_end(int kb, int begin) {
+  const int small = 2 * kb;
+  if (begin < small) return small;
+  return begin + PROMOTE < 3 * kb ? begin + PROMOTE : 3 * kb;
+}
+
+__device__ __forceinline__ void store32_bytes(void* base, const uint32_t* w) {   // 32-byte aligned
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(base), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+               "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ void load32_bytes(const void* base, uint32_t* w) {
+  const uint4 x = __ldcg(static_cast<const uint4*>(base)), y = __ldcg(static_cast<const uint4*>(base) + 1);
+  w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; w[4] = y.x; w[5] = y.y; w[6] = y.z; w[7] = y.w;
+}
+__device__ __forceinline__ float2 half_pair(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ uint32_t pair_half(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The last product: 16 columns of one row of a matrix, updated.  v: X times HELD.
+__device__ __forceinline__ void update16(const Target& t, long long row, int n0, int N, const float* v) {
+  const long long at = row * N + n0;
+  const float step = t.step * (1.f / HELD), keep = t.keep;
+  if (t.wide) {       // (then N is a multiple of 8: 16 columns, or 8)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (n0 + 8 * h >= N) break;
+      const float* x = v + 8 * h;
+      if (t.f32) {
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = -step * x[i];
+        if (t.W) {
+          const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(t.W) + at) + 2 * h;
+          const float4 a = p[0], b = p[1];
+          const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = fmaf(keep, w[i], o[i]);
+        }
+        float4* q = reinterpret_cast<float4*>(static_cast<float*>(t.out) + at) + 2 * h;
+        q[0] = make_float4(o[0], o[1], o[2], o[3]);
+        q[1] = make_float4(o[4], o[5], o[6], o[7]);
+      } else {
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        if (t.W) {
+          const uint4 q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.W) + at)[h];
+          w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float lo = -step * x[2 * i], hi = -step * x[2 * i + 1];
+          if (t.W) {
+            lo = fmaf(keep, __uint_as_float(w[i] << 16), lo);
+            hi = fmaf(keep, __uint_as_float(w[i] & 0xffff0000u), hi);
+          }
+          const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+          w[i] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(t.out) + at)[h] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (n0 + i >= N) break;
+    float o = -step * v[i];
+    if (t.f32) {
+      if (t.W) o = fmaf(keep, static_cast<const float*>(t.W)[at + i], o);
+      static_cast<float*>(t.out)[at + i] = o;
+    } else {
+      if (t.W) o = fmaf(keep, __bfloat162float(static_cast<const __nv_bfloat16*>(t.W)[at + i]), o);
+      static_cast<__nv_bfloat16*>(t.out)[at + i] = __float2bfloat16_rn(o);
+    }
+  }
+}
+
+template <bool PRECISE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE>, 1) muon_gemm_kernel(const __grid_constant__ Params p) {
+  constexpr int FIRST = FIRST_EPI<PRECISE>;
+  const int half_n = p.tile_n / 2;          // rows of B that one CTA stages
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RING_BYTES);
+  uint64_t* full = bars;                    // [stages] TMA of both CTAs -> MMA (rank 0's are used)
+  uint64_t* empty = full + MAX_STAGES;      // [stages] MMA -> TMA, one set in each CTA
+  uint64_t* tfull = empty + MAX_STAGES;     // [2] MMA -> epilogue, one set in each CTA
+  uint64_t* tempty = tfull + 2;             // [2] epilogue warps of both CTAs -> MMA (rank 0's are used)
+  uint64_t* drain = tempty + 2;             // used only when giving up
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int stages = p.stages, stage_bytes = p.stage_bytes;
+  constexpr int a_bytes = CTA_M * BLOCK_K * 2;
+  const uint32_t rank = ptx::cluster_rank();
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(&tfull[a], 1);
+      ptx::mbar_init(&tempty[a], 2 * EPI_WARPS);
+    }
+    ptx::mbar_init(drain, 1);
+    *abort_flag = 0;
+    ptx::mbar_fence_init();
+  }
+  if (warp == FIRST && lane == 0) {
+    ptx::prefetch_tmap(&p.prod[0].a);
+    ptx::prefetch_tmap(&p.prod[0].b);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(tmem_holder, TMEM_COLS);
+    ptx::tmem_relinquish_pair();
+  }
+  ptx::tc_fence_before();
+  ptx::cluster_sync_all();     // also: the other CTA's barriers are set up
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_holder;
+  const uint32_t smem0 = ptx::smem_u32(smem), full0 = ptx::map_to_cta(ptx::smem_u32(full), 0);
+  pdl_wait();
+
+  const int first_unit = blockIdx.x >> 1, unit_step = gridDim.x >> 1;
+  if (warp < FIRST) {
+    if constexpr (PRECISE) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ROLE_REGS));
+    if (warp == 0) {
+      if (ptx::elect_one()) {
+        // ------------------------------------------------------------ TMA producer
+        uint32_t ph = 0;
+        int s = 0;
+        bool ok = true;
+        const uint32_t tx = 2u * stage_bytes;
+        for (int u = first_unit; u < p.units && ok; u += unit_step) {
+          const Unit t = find_unit(p, u);
+          const DevProduct& d = p.prod[t.prod];
+          const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M, n0 = t.n_blk * p.tile_n + static_cast<int>(rank) * half_n;
+          for (int run = 0; run < (PRECISE ? 3 : 1) && ok; ++run) {
+            const int za = (PRECISE && run == 0 ? d.count : 0) + t.batch, zb = (PRECISE && run == 1 ? d.count : 0) + t.batch;
+            for (int kb = 0; kb < d.kb; ++kb) {
+              if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+              if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);
+              const uint32_t to = smem0 + s * stage_bytes, bar = full0 + s * 8;
+              if (d.a_mn) {
+                ptx::tma_load_3d_pair(&d.a, to, bar, m0, kb * BLOCK_K, za);
+                ptx::tma_load_3d_pair(&d.a, to + BLOCK64_BYTES, bar, m0 + 64, kb * BLOCK_K, za);
+              } else {
+                ptx::tma_load_3d_pair(&d.a, to, bar, kb * BLOCK_K, m0, za);
+              }
+              if (d.b_mn) {
+                ptx::tma_load_3d_pair(&d.b, to + a_bytes, bar, n0, kb * BLOCK_K, zb);
+                if (half_n > 64) ptx::tma_load_3d_pair(&d.b, to + a_bytes + BLOCK64_BYTES, bar, n0 + 64, kb * BLOCK_K, zb);
+              } else {
+                ptx::tma_load_3d_pair(&d.b, to + a_bytes, bar, kb * BLOCK_K, n0, zb);
+              }
+              if (++s == stages) { s = 0; ph ^= 1u; }
+            }
+          }
+        }
+        // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
+        for (int i = 0; i < stages && ok; ++i) {
+          ok = ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag);
+          if (++s == stages) { s = 0; ph ^= 1u; }
+        }
+        if (!ok) {
+          // Copies into this CTA's shared memory are counted on rank 0's barriers: give what is in flight a bounded time
+          // to land before the CTA exits.
+          const long long t0 = clock64();
+          while (clock64() - t0 < ptx::kWaitLimitCycles / 64) {}
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1 && rank == 0) {
+      // -------------------------------------------------------------- MMA issuer (the whole warp walks, one lane issues)
+      const uint32_t idesc0 = ptx::umma_idesc_f16(TILE_M, p.tile_n);
+      uint32_t tl = 0, ph = 0;
+      int s = 0;
+      bool ok = true;
+      for (int u = first_unit; u < p.units && ok; u += unit_step) {
+        const Unit t = find_unit(p, u);
+        const DevProduct& d = p.prod[t.prod];
+        // bits 15, 16: the operand's rows run along memory
+        const uint32_t idesc = idesc0 | (d.a_mn ? 1u << 15 : 0u) | (d.b_mn ? 1u << 16 : 0u);
+        const uint64_t a_desc0 = d.a_mn ? ptx::umma_desc_mn128(smem0, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0);
+        const uint64_t b_desc0 = d.b_mn ? ptx::umma_desc_mn128(smem0 + a_bytes, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0 + a_bytes);
+        const uint32_t a_step = d.a_mn ? 2048 >> 4 : 32 >> 4, b_step = d.b_mn ? 2048 >> 4 : 32 >> 4;
+        const int all = (PRECISE ? 3 : 1) * d.kb;
+        for (int begin = 0; begin < all && ok; ++tl) {
+          const int end = PRECISE ? part_end(d.kb, begin) : all;
+          const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
+          ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aph ^ 1, abort_flag) ? 1 : 0, 0) != 0;
+          if (!ok) break;
+          ptx::tc_fence_after();
+          const uint32_t d_tmem = tmem_base + acc * TILE_N;
+          for (int kb = begin; kb < end; ++kb) {
+            ok = ptx::mbar_wait_warp(&full[s], ph, abort_flag);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            const uint64_t a_desc = a_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
+            const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
+            if (ptx::elect_one()) {
+#pragma unroll
+              for (int k = 0; k < BLOCK_K / 16; ++k)
+                ptx::umma_bf16_pair(d_tmem, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb > begin || k > 0) ? 1u : 0u);
+              ptx::umma_commit_pair(&empty[s]);
+            }
+            __syncwarp();
+            if (++s == stages) { s = 0; ph ^= 1u; }
+          }
+          if (ok) {
+            if (ptx::elect_one()) ptx::umma_commit_pair(&tfull[acc]);
+            __syncwarp();
+          }
+          begin = end;
+        }
+      }
+      if (!ok) {
+        // wait (bounded) until the MMAs issued so far have retired before tensor memory is freed
+        if (ptx::elect_one()) {
+          ptx::umma_commit_pair(drain);
+          const long long t0 = clock64();
+          while (!ptx::mbar_try_wait(drain, 0) && clock64() - t0 < ptx::kWaitLimitCycles / 8) {}
+        }
+        __syncwarp();
+      }
+    }
+  } else {
+    if constexpr (PRECISE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
+    // -------------------------------------------------------------- epilogue warps
+    const int q = warp & 3;                                // tensor-memory lane quarter
+    const int cols = p.tile_n / GROUPS;                    // columns of this warp's part of the tile
+    const int col0 = ((warp - FIRST) >> 2) * cols;
+    const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + col0;
+    uint32_t tl = 0;
+    bool live = true;
+    for (int u = first_unit; u < p.units && live; u += unit_step, ++tl) {
+      const Unit t = find_unit(p, u);
+      const DevProduct& d = p.prod[t.prod];
+      const int row0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M + q * 32, row = row0 + lane;
+      const bool in = row < d.M;
+      const int c0 = t.n_blk * p.tile_n + col0;
+      const int width = d.N - c0 < cols ? d.N - c0 : cols;       // (may be negative)
+      const bool mirror = d.symmetric && t.n_blk * p.tile_n >= (t.m_blk + 1) * TILE_M;
+      const __half* D = d.D ? d.D + t.batch * d.d_each + static_cast<long long>(row) * d.ldd + c0 : nullptr;
+      __half* C = d.C + t.batch * d.c_each + static_cast<long long>(row) * d.ldc + c0;
+      // what is added is on its way before the sum is complete
+      uint32_t high[8], low[8];
+      if (D && in && width > 0) {
+        load32_bytes(D, high);
+        if (d.d_low) load32_bytes(D + d.d_plane, low);
+      }
+      if constexpr (PRECISE) {
+        // All parts of the sum but the last are added up in registers; then it goes back to where the last part lies.
+        constexpr int BLOCKS = TILE_N / GROUPS / 32;             // (precise tiles are 256 wide)
+        float sum[BLOCKS][32];
+        for (int begin = 0;; ++tl) {
+          const int end = part_end(d.kb, begin);
+          const bool last = end == 3 * d.kb;
+          if (!ptx::mbar_wait(&tfull[tl & 1], (tl >> 1) & 1, abort_flag)) { live = false; break; }
+          ptx::tc_fence_after();
+          const uint32_t t_part = t_quarter + (tl & 1) * TILE_N;
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b) {
+            const uint32_t at = t_part + b * 32;
+            float v[32];
+            ptx::tmem_ld32(at, v);
+            ptx::tmem_ld_wait();
+            if (begin == 0) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) sum[b][i] = v[i] * (1.f / LOW);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) sum[b][i] += v[i];
+            }
+            if (last) {
+              ptx::tmem_st16(at, sum[b]);
+              ptx::tmem_st16(at + 16, sum[b] + 16);
+            }
+          }
+          if (last) {
+            ptx::tmem_st_wait();
+            break;
+          }
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(&tempty[tl & 1]), 0));
+          begin = end;
+        }
+        if (!live) break;
+      } else {
+        if (!ptx::mbar_wait(&tfull[tl & 1], (tl >> 1) & 1, abort_flag)) break;
+        ptx::tc_fence_after();
+      }
+      const uint32_t acc = tl & 1, t_row = t_quarter + acc * TILE_N;
+#pragma unroll 1
+      for (int c = 0; c < width; c += 16) {
+        float v[16];
+        ptx::tmem_ld16(t_row + c, v);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= d.alpha;
+        if (D && in) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float2 x = half_pair(high[i]);
+            if (d.d_low) {
+              const float2 y = half_pair(low[i]);
+              x.x = fmaf(y.x, 1.f / LOW, x.x);
+              x.y = fmaf(y.y, 1.f / LOW, x.y);
+            }
+            v[2 * i] = fmaf(d.beta, x.x, v[2 * i]);
+            v[2 * i + 1] = fmaf(d.beta, x.y, v[2 * i + 1]);
+          }
+          if (c + 16 < width) {
+            load32_bytes(D + c + 16, high);
+            if (d.d_low) load32_bytes(D + d.d_plane + c + 16, low);
+          }
+        }
+        if (d.target) {
+          if (in) update16(d.target[t.batch], row, c0 + c, d.N, v);
+          continue;
+        }
+        uint32_t hi[8], lo[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          hi[i] = pair_half(v[2 * i], v[2 * i + 1]);
+          const float2 x = half_pair(hi[i]);
+          lo[i] = pair_half((v[2 * i] - x.x) * LOW, (v[2 * i + 1] - x.y) * LOW);
+        }
+        if (in) {
+          store32_bytes(C + c, hi);
+          if (d.c_low) store32_bytes(C + d.c_plane + c, lo);
+        }
+        if (mirror) {
+          // the 32 rows of this warp lie side by side in the mirror image
+          __half* T = d.C + t.batch * d.c_each + static_cast<long long>(c0 + c) * d.ldc + row;
+          const unsigned short* h = reinterpret_cast<const unsigned short*>(hi);
+          const unsigned short* l = reinterpret_cast<const unsigned short*>(lo);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            if (!in || c + i >= width) continue;
+            *reinterpret_cast<unsigned short*>(T + static_cast<long long>(i) * d.ldc) = h[i];
+            if (d.c_low) *reinterpret_cast<unsigned short*>(T + d.c_plane + static_cast<long long>(i) * d.ldc) = l[i];
+          }
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(&tempty[acc]), 0));
+    }
+  }
+
+  ptx::tc_fence_before();
+  ptx::cluster_sync_all();     // neither CTA leaves while the other may still signal it or read its shared memory
+  if (threadIdx.x == 0 && *abort_flag) record_status(p.status, FFSPLIT_ERR_TIMEOUT, blockIdx.x, KID_MUON);
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc_pair(tmem_base, TMEM_COLS);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// Tensor map over [2 planes x count][rows][cols]; box of 64 columns by box_rows rows, 128-byte swizzle, zeros outside.
+ffsplit_status encode(ffsplit_ctx* ctx, const Matrices& m, int box_rows, int planes, CUtensorMap* out) {
+  if (!ctx->encode_fn) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+    if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn)
+      return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    ctx->encode_fn = fn;
+  }
+  // (the second plane follows the first without a gap, so both are one run of matrices)
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows), static_cast<cuuint64_t>(m.count) * planes};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(m.ld) * 2, static_cast<cuuint64_t>(m.each) * 2};
+  cuuint32_t box[3] = {BLOCK_K, static_cast<cuuint32_t>(box_rows), 1}, estr[3] = {1, 1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_fn)(
+      out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, m.p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
+  return FFSPLIT_OK;
+}
+
+int tiles_of(const Product& g, int tile_n) {
+  const int tm = (g.M + TILE_M - 1) / TILE_M, tn = (g.N + tile_n - 1) / tile_n, step = TILE_M / tile_n;
+  if (!g.symmetric) return tm * tn;
+  int tiles = 0;
+  for (int m = 0; m < tm; ++m) tiles += tn - m * step;
+  return tiles;
+}
+
+}  // namespace
+
+ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* products, int n, cudaStream_t st) {
+  // The tensor maps are made by a driver call, which needs a current context (see train_gemm.cu).
+  const cudaError_t bound = cudaSetDevice(ctx->device);
+  if (bound != cudaSuccess) return check_cuda(ctx, bound, "cudaSetDevice");
+  const unsigned bit = precise ? 2u : 1u;
+  if (!(ctx->attr_muon_set & bit)) {
+    const auto kernel = precise ? muon_gemm_kernel<true> : muon_gemm_kernel<false>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
+    if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(muon_gemm_kernel)");
+    if (precise) {
+      cudaFuncAttributes attr;
+      const cudaError_t a = cudaFuncGetAttributes(&attr, kernel);
+      if (a != cudaSuccess) return check_cuda(ctx, a, "cudaFuncGetAttributes(muon_gemm_kernel)");
+      if (attr.numRegs < START_REGS) return fail(ctx, FFSPLIT_ERR_CUDA, "muon_gemm_kernel was built with fewer registers than it divides");
+    }
+    ctx->attr_muon_set |= bit;
+  }
+  Params p;
+  std::memset(&p, 0, sizeof(p));
+  const int clusters_max = ctx->num_sms / 2;
+  // longest sums first
+  int order[MAX_GROUPS];
+  for (int i = 0; i < n; ++i) {
+    int at = i;
+    for (; at > 0 && products[order[at - 1]].K < products[i].K; --at) order[at] = order[at - 1];
+    order[at] = i;
+  }
+  // 256 x 128 tiles where the wide ones leave pairs of SMs idle: a k-block takes 0.27 us in a wide tile (the tensor cores'
+  // rate) and 0.2 us in a narrow one (shared memory's)
+  p.tile_n = TILE_N;
+  if (!precise) {
+    long long wide = 0, narrow = 0;
+    for (int i = 0; i < n; ++i) {
+      wide += static_cast<long long>(tiles_of(products[i], 256)) * products[i].c.count;
+      narrow += static_cast<long long>(tiles_of(products[i], 128)) * products[i].c.count;
+    }
+    if (((narrow + clusters_max - 1) / clusters_max) * 0.2 < ((wide + clusters_max - 1) / clusters_max) * 0.27) p.tile_n = 128;
+  }
+  p.stage_bytes = (CTA_M + p.tile_n / 2) * BLOCK_K * 2;
+  p.stages = RING_BYTES / p.stage_bytes < MAX_STAGES ? RING_BYTES / p.stage_bytes : MAX_STAGES;
+  long long units = 0;
+  for (int i = 0; i < n; ++i) {
+    const Product& g = products[order[i]];
+    DevProduct& d = p.prod[i];
+    ffsplit_status s;
+    const int planes = precise ? 2 : 1;
+    if ((s = encode(ctx, g.a, g.a_mn ? BLOCK_K : CTA_M, planes, &d.a)) != FFSPLIT_OK) return s;
+    if ((s = encode(ctx, g.b, g.b_mn ? BLOCK_K : p.tile_n / 2, planes, &d.b)) != FFSPLIT_OK) return s;
+    d.M = g.M; d.N = g.N; d.count = g.c.count;
+    d.kb = (g.K + BLOCK_K - 1) / BLOCK_K;
+    d.a_mn = g.a_mn; d.b_mn = g.b_mn; d.symmetric = g.symmetric;
+    d.tiles_m = (g.M + TILE_M - 1) / TILE_M;
+    d.tiles_n = (g.N + p.tile_n - 1) / p.tile_n;
+    d.tiles = tiles_of(g, p.tile_n);
+    d.unit0 = static_cast<int>(units);
+    d.alpha = g.alpha; d.beta = g.beta;
+    if (g.d) { d.D = g.d->p; d.d_each = g.d->each; d.d_plane = g.d->plane; d.ldd = g.d->ld; d.d_low = g.d_low; }
+    d.C = g.c.p; d.c_each = g.c.each; d.c_plane = g.c.plane; d.ldc = g.c.ld; d.c_low = g.c_low;
+    d.target = g.target;
+    // panel height: the tiles in flight form a block whose two sides carry about the same operand bytes
+    d.panel_m = 1;
+    double best = 1e300;
+    for (int h = 1; h <= d.tiles_m && h <= clusters_max; ++h) {
+      const double w = static_cast<double>(clusters_max) / h;
+      const double cost = h * 256.0 + (w < d.tiles_n ? w : d.tiles_n) * p.tile_n;
+      if (cost < best - 1e-9) { best = cost; d.panel_m = h; }
+    }
+    units += static_cast<long long>(d.tiles) * d.count;
+    if (units > 0x3fffffffll) return fail(ctx, FFSPLIT_ERR_SHAPE, "more than 2^30 tiles in one product");
+  }
+  p.n = n;
+  p.units = static_cast<int>(units);
+  p.status = ctx->status();
+  const int clusters = units < clusters_max ? static_cast<int>(units) : clusters_max;
+  const cudaError_t e = precise ? launch_pdl(muon_gemm_kernel<true>, dim3(2 * clusters), dim3(GEMM_THREADS<true>), MAX_SMEM, st, p)
+                                : launch_pdl(muon_gemm_kernel<false>, dim3(2 * clusters), dim3(GEMM_THREADS<false>), MAX_SMEM, st, p);
+  ctx->launches++;
+  return check_cuda(ctx, e, "muon_gemm_kernel launch");
+}
+
+}  // namespace muon
+}  // namespace ffsp
