@@ -3,17 +3,18 @@
 //   forward:   P[t] = s_i (X[t] A_i),  Y[t] = X[t] W + bias + P[t] B_i,             i = index[t]
 //   backward:  D[t] = s_i (dY[t] B_i^T),  dX[t] = dY[t] W^T + D[t] A_i^T,  dA_i = sum_t X[t]^T D[t],  dB_i = sum_t P[t]^T dY[t]
 //
-// The shared product runs on the tensor cores (train_gemm.cu).  The adapters' products have a side of at most 128: they are
-// taken on the CUDA cores in fp32, eight tokens to a block, which share a factor's elements where they use the same adapter.
+// The shared product runs on the tensor cores (train_gemm.cu).  So do the adapters' products of bf16 batches of more than
+// FEW tokens (adapter_tc.cu).  Those of few tokens and of fp32 layers are taken here, on the CUDA cores in fp32, eight tokens
+// to a block, which share a factor's elements where they use the same adapter.
 #include <cstring>
 
+#include "adapter.h"
 #include "epilogue.cuh"
-#include "train_gemm.h"
 
 namespace ffsp {
 namespace adapter {
 
-constexpr int MAX_RANK = 128;
+constexpr int FEW = 64;
 constexpr int GROUP = 8;             // tokens of a block
 constexpr int THREADS = 256;
 constexpr int CHUNK = 256;           // elements along a contraction that are staged at a time
@@ -238,25 +239,36 @@ namespace {
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
+// Batches whose adapters' products run on the tensor cores.
+bool on_tensor_cores(const ffsplit_projection& p, int n, long long T) {
+  return p.dtype == FFSPLIT_BF16 && T > adapter::FEW && adapter::tile_bound(T, n) <= 65535;
+}
+
 struct AdapterLayout {
-  long long ldi, ldo;
-  size_t P, D, X, dY, W, parts, parts_bytes, end;
+  long long ldi, ldo, ldr;
+  size_t P, D, sorted, X, dY, W, A, B, parts, parts_bytes, end;
 };
-AdapterLayout adapter_layout(const ffsplit_projection& p, int r, long long T) {
+AdapterLayout adapter_layout(const ffsplit_projection& p, int n, int r, long long T) {
   AdapterLayout L;
-  const bool f32 = p.dtype == FFSPLIT_F32;
+  const bool f32 = p.dtype == FFSPLIT_F32, tc = on_tensor_cores(p, n, T);
   const size_t planes = f32 ? 3 : 1;
   L.ldi = round_up_ll(p.in, 64);
   L.ldo = round_up_ll(p.out, 64);
+  L.ldr = round_up_ll(r, 8);
   size_t off = 0;
-  L.P = off; off = up256(off + static_cast<size_t>(T) * r * 4);
-  L.D = off; off = up256(off + static_cast<size_t>(T) * r * 4);
-  L.X = off; off = up256(off + (f32 || p.in % 8 ? static_cast<size_t>(T) * L.ldi * 2 * planes : 0));
-  L.dY = off; off = up256(off + (f32 || p.out % 8 ? static_cast<size_t>(T) * L.ldo * 2 * planes : 0));
-  L.W = off; off = up256(off + (f32 || p.out % 8 ? static_cast<size_t>(p.in) * L.ldo * 2 * planes : 0));
+  const auto take = [&](size_t* at, size_t bytes) { *at = off; off = up256(off + bytes); };
+  const size_t inner = tc ? static_cast<size_t>(adapter::tile_bound(T, n)) * adapter::TOKENS * adapter::rank_pitch(r) * 2 : static_cast<size_t>(T) * r * 4;
+  take(&L.P, inner);
+  take(&L.D, inner);
+  take(&L.sorted, tc ? (static_cast<size_t>(T) + 2 * (static_cast<size_t>(n) + 1)) * 4 : 0);
+  take(&L.X, f32 || p.in % 8 ? static_cast<size_t>(T) * L.ldi * 2 * planes : 0);
+  take(&L.dY, f32 || p.out % 8 ? static_cast<size_t>(T) * L.ldo * 2 * planes : 0);
+  take(&L.W, f32 || p.out % 8 ? static_cast<size_t>(p.in) * L.ldo * 2 * planes : 0);
+  take(&L.A, tc && r % 8 ? static_cast<size_t>(n) * p.in * L.ldr * 2 : 0);
+  take(&L.B, tc && p.out % 8 ? static_cast<size_t>(n) * r * L.ldo * 2 : 0);
   const size_t want = 64 * static_cast<size_t>(T) * (L.ldi > L.ldo ? L.ldi : L.ldo);
   L.parts_bytes = up256(want < (32u << 20) ? want : (32u << 20));
-  L.parts = off; off += L.parts_bytes;
+  take(&L.parts, L.parts_bytes);
   L.end = off;
   return L;
 }
@@ -279,33 +291,64 @@ ffsplit_status check_adapters(ffsplit_ctx* ctx, const ffsplit_projection* p, con
   if (!aligned16(a->A) || !aligned16(a->B) || !aligned16(X)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
   if ((reinterpret_cast<uintptr_t>(a->index) & 3u) || (reinterpret_cast<uintptr_t>(a->scale) & 3u))
     return fail(ctx, FFSPLIT_ERR_ALIGN, "index and scale must be 4-byte aligned");
-  if (kCtrlBytes + adapter_layout(*p, a->r, T).end > ctx->ws_bytes)
+  if (kCtrlBytes + adapter_layout(*p, a->n, a->r, T).end > ctx->ws_bytes)
     return fail(ctx, FFSPLIT_ERR_BUFFER_TOO_SMALL, "workspace too small for this call (ffsplit_adapter_workspace_size)");
   ctx->score_prep.valid = false;   // the scoring buffers share the workspace
   return FFSPLIT_OK;
 }
 
-// C [T, N] = V [T, K] times W [in, out] (transposed: its transpose).
-ffsplit_status shared_product(ffsplit_ctx* ctx, const ffsplit_projection& p, const AdapterLayout& L, const void* V, const void* W,
-                              const void* bias, bool transposed, long long T, void* C, cudaStream_t st) {
-  char* ws = ctx->ws + kCtrlBytes;
-  const bool f32 = p.dtype == FFSPLIT_F32;
+// The operands of a call: the caller's tensors, or their planes (or padded copies) in the workspace.
+struct Call {
+  ffsplit_ctx* ctx;
+  const ffsplit_projection& p;
+  const ffsplit_adapters& a;
+  long long T;
+  AdapterLayout L;
+  char* ws;
+  cudaStream_t st;
+  bool f32, tc;
   train::PrepArgs prep;
-  std::memset(&prep, 0, sizeof(prep));
-  int blocks = 0;
-  const int K = transposed ? p.out : p.in, N = transposed ? p.in : p.out;
-  tg::Product g;
-  std::memset(&g, 0, sizeof(g));
-  g.a[0] = train::operand(&prep, &blocks, f32, V, T, K, transposed ? L.ldo : L.ldi, ws + (transposed ? L.dY : L.X));
-  g.b[0] = train::operand(&prep, &blocks, f32, W, p.in, p.out, L.ldo, ws + L.W);
-  g.pairs = 1;
-  g.b_mn = transposed ? 0 : 1;
-  g.M = T; g.N = N; g.K = K;
-  g.C = C; g.ldc = N; g.bias = bias;
-  const ffsplit_status s = train::launch_prepare(ctx, prep, blocks, f32, st);
-  if (s != FFSPLIT_OK) return s;
-  return tg::launch(ctx, tg::PLAIN, 0, f32, &g, 1, tg::Hidden{}, ws + L.parts, L.parts_bytes, st);
-}
+  int prep_blocks = 0;
+  tg::Matrix X{}, dY{}, W{};
+  adapter::Factor A{}, B{};
+  adapter::Sorted sorted{};
+
+  Call(ffsplit_ctx* c, const ffsplit_projection& projection, const ffsplit_adapters& adapters, long long tokens, void* stream)
+      : ctx(c), p(projection), a(adapters), T(tokens), L(adapter_layout(projection, adapters.n, adapters.r, tokens)), ws(c->ws + kCtrlBytes),
+        st(static_cast<cudaStream_t>(stream)), f32(projection.dtype == FFSPLIT_F32), tc(on_tensor_cores(projection, adapters.n, tokens)) {
+    std::memset(&prep, 0, sizeof(prep));
+  }
+  float* inner(size_t at) const { return reinterpret_cast<float*>(ws + at); }
+  __nv_bfloat16* tiles(size_t at) const { return reinterpret_cast<__nv_bfloat16*>(ws + at); }
+  void use_X(const void* x) { X = train::operand(&prep, &prep_blocks, f32, x, T, p.in, L.ldi, ws + L.X); }
+  void use_dY(const void* y) { dY = train::operand(&prep, &prep_blocks, f32, y, T, p.out, L.ldo, ws + L.dY); }
+  void use_W(const void* w) { W = train::operand(&prep, &prep_blocks, f32, w, p.in, p.out, L.ldo, ws + L.W); }
+  void use_A() { A = {train::operand(&prep, &prep_blocks, false, a.A, static_cast<long long>(a.n) * p.in, a.r, L.ldr, ws + L.A), p.in, a.r, 0}; }
+  void use_B() { B = {train::operand(&prep, &prep_blocks, false, a.B, static_cast<long long>(a.n) * a.r, p.out, L.ldo, ws + L.B), a.r, p.out, 1}; }
+  ffsplit_status prepare() {
+    if (tc) {
+      sorted.count = reinterpret_cast<int*>(ws + L.sorted);
+      sorted.offset = sorted.count + a.n + 1;
+      sorted.order = sorted.offset + a.n + 1;
+      sorted.n = a.n;
+      sorted.T = T;
+      const ffsplit_status s = adapter::launch_sort(ctx, a.index, sorted, st);
+      if (s != FFSPLIT_OK) return s;
+    }
+    return train::launch_prepare(ctx, prep, prep_blocks, f32, st);
+  }
+  // C [T, N] = V [T, K] times W [in, out] (transposed: its transpose).
+  ffsplit_status shared_product(const tg::Matrix& V, const void* bias, bool transposed, void* C) {
+    tg::Product g;
+    std::memset(&g, 0, sizeof(g));
+    g.a[0] = V; g.b[0] = W;
+    g.pairs = 1;
+    g.b_mn = transposed ? 0 : 1;
+    g.M = T; g.N = transposed ? p.in : p.out; g.K = transposed ? p.out : p.in;
+    g.C = C; g.ldc = g.N; g.bias = bias;
+    return tg::launch(ctx, tg::PLAIN, 0, f32, &g, 1, tg::Hidden{}, ws + L.parts, L.parts_bytes, st);
+  }
+};
 
 ffsplit_status launch_shrink(ffsplit_ctx* ctx, bool f32, adapter::ShrinkArgs& s, int jobs, const ffsplit_adapters& a, long long T, cudaStream_t st) {
   s.index = a.index; s.scale = a.scale; s.T = T; s.n = a.n; s.r = a.r; s.status = ctx->status();
@@ -335,7 +378,7 @@ ffsplit_status ffsplit_adapter_workspace_size(const ffsplit_projection* projecti
   if (!bytes) return FFSPLIT_ERR_INVALID_ARG;
   const ffsplit_status s = check_projection(nullptr, projection, n, r, T);
   if (s != FFSPLIT_OK) return s;
-  *bytes = kCtrlBytes + adapter_layout(*projection, r, T).end;
+  *bytes = kCtrlBytes + adapter_layout(*projection, n, r, T).end;
   return FFSPLIT_OK;
 }
 
@@ -348,17 +391,26 @@ ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projectio
   if (!Y) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "NULL tensor");
   if ((W && base) || (bias && !W)) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "W (with or without bias), or base, or neither");
   if (!aligned16(W) || !aligned16(bias) || !aligned16(base) || !aligned16(Y)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const ffsplit_projection& p = *projection;
-  const AdapterLayout L = adapter_layout(p, adapters->r, T);
-  const bool f32 = p.dtype == FFSPLIT_F32;
-  float* P = reinterpret_cast<float*>(ctx->ws + kCtrlBytes + L.P);
-  adapter::ShrinkArgs sh;
-  std::memset(&sh, 0, sizeof(sh));
-  sh.job[0] = {X, adapters->A, P, p.in, 0};
-  if ((s = launch_shrink(ctx, f32, sh, 1, *adapters, T, st)) != FFSPLIT_OK) return s;
-  if (W && (s = shared_product(ctx, p, L, X, W, bias, false, T, Y, st)) != FFSPLIT_OK) return s;
-  return launch_expand(ctx, f32, {P, adapters->B, W ? Y : base, Y, adapters->index, T, p.out, adapters->n, adapters->r, 0}, st);
+  Call c(ctx, *projection, *adapters, T, stream);
+  if (W || c.tc) c.use_X(X);
+  if (W) c.use_W(W);
+  if (c.tc) {
+    c.use_A();
+    c.use_B();
+  }
+  if ((s = c.prepare()) != FFSPLIT_OK) return s;
+  if (c.tc) {
+    const adapter::Shrink job = {c.X, c.A, c.tiles(c.L.P), c.p.in};
+    if ((s = adapter::launch_shrink_tc(ctx, &job, 1, c.sorted, c.a.r, c.a.scale, c.st)) != FFSPLIT_OK) return s;
+  } else {
+    adapter::ShrinkArgs sh;
+    std::memset(&sh, 0, sizeof(sh));
+    sh.job[0] = {X, adapters->A, c.inner(c.L.P), c.p.in, 0};
+    if ((s = launch_shrink(ctx, c.f32, sh, 1, c.a, T, c.st)) != FFSPLIT_OK) return s;
+  }
+  if (W && (s = c.shared_product(c.X, bias, false, Y)) != FFSPLIT_OK) return s;
+  if (c.tc) return adapter::launch_expand_tc(ctx, c.tiles(c.L.P), c.B, c.p.out, W ? Y : base, Y, c.sorted, c.a.r, c.st);
+  return launch_expand(ctx, c.f32, {c.inner(c.L.P), adapters->B, W ? Y : base, Y, adapters->index, T, c.p.out, c.a.n, c.a.r, 0}, c.st);
 }
 
 ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W, const void* base,
@@ -372,31 +424,53 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
   if (grads->dX && W && base) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "W, or base, or neither");
   for (const void* q : {dY, W, base, static_cast<const void*>(grads->dX), static_cast<const void*>(grads->dA), static_cast<const void*>(grads->dB)})
     if (!aligned16(q)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const ffsplit_projection& p = *projection;
-  const AdapterLayout L = adapter_layout(p, adapters->r, T);
-  const bool f32 = p.dtype == FFSPLIT_F32;
-  float *P = reinterpret_cast<float*>(ctx->ws + kCtrlBytes + L.P), *D = reinterpret_cast<float*>(ctx->ws + kCtrlBytes + L.D);
-  adapter::ShrinkArgs sh;
-  std::memset(&sh, 0, sizeof(sh));
-  int jobs = 0;
-  if (grads->dX || grads->dA) sh.job[jobs++] = {dY, adapters->B, D, p.out, 1};
-  if (grads->dB) sh.job[jobs++] = {X, adapters->A, P, p.in, 0};
-  if ((s = launch_shrink(ctx, f32, sh, jobs, *adapters, T, st)) != FFSPLIT_OK) return s;
-  if (grads->dX) {
-    if (W && (s = shared_product(ctx, p, L, dY, W, nullptr, true, T, grads->dX, st)) != FFSPLIT_OK) return s;
-    if ((s = launch_expand(ctx, f32, {D, adapters->A, W ? grads->dX : base, grads->dX, adapters->index, T, p.in, adapters->n, adapters->r, 1}, st)) != FFSPLIT_OK) return s;
+  Call c(ctx, *projection, *adapters, T, stream);
+  const bool dX = grads->dX != nullptr, dA = grads->dA != nullptr, dB = grads->dB != nullptr;
+  if (c.tc && (dA || dB)) c.use_X(X);
+  if ((dX && W) || c.tc) c.use_dY(dY);
+  if (dX && W) c.use_W(W);
+  if (c.tc) {
+    c.use_A();
+    if (dX || dA) c.use_B();
   }
-  if (!grads->dA && !grads->dB) return FFSPLIT_OK;
+  if ((s = c.prepare()) != FFSPLIT_OK) return s;
+  int n = 0;
+  if (c.tc) {
+    adapter::Shrink jobs[2];
+    if (dX || dA) jobs[n++] = {c.dY, c.B, c.tiles(c.L.D), c.p.out};
+    if (dB) jobs[n++] = {c.X, c.A, c.tiles(c.L.P), c.p.in};
+    if ((s = adapter::launch_shrink_tc(ctx, jobs, n, c.sorted, c.a.r, c.a.scale, c.st)) != FFSPLIT_OK) return s;
+  } else {
+    adapter::ShrinkArgs sh;
+    std::memset(&sh, 0, sizeof(sh));
+    if (dX || dA) sh.job[n++] = {dY, adapters->B, c.inner(c.L.D), c.p.out, 1};
+    if (dB) sh.job[n++] = {X, adapters->A, c.inner(c.L.P), c.p.in, 0};
+    if ((s = launch_shrink(ctx, c.f32, sh, n, c.a, T, c.st)) != FFSPLIT_OK) return s;
+  }
+  if (dX) {
+    if (W && (s = c.shared_product(c.dY, nullptr, true, grads->dX)) != FFSPLIT_OK) return s;
+    const void* add = W ? grads->dX : base;
+    s = c.tc ? adapter::launch_expand_tc(ctx, c.tiles(c.L.D), c.A, c.p.in, add, grads->dX, c.sorted, c.a.r, c.st)
+             : launch_expand(ctx, c.f32, {c.inner(c.L.D), adapters->A, add, grads->dX, adapters->index, T, c.p.in, c.a.n, c.a.r, 1}, c.st);
+    if (s != FFSPLIT_OK) return s;
+  }
+  if (!dA && !dB) return FFSPLIT_OK;
+  if (c.tc) {
+    adapter::Gradient jobs[2];
+    n = 0;
+    if (dA) jobs[n++] = {c.X, c.tiles(c.L.D), grads->dA, c.p.in, 0};
+    if (dB) jobs[n++] = {c.dY, c.tiles(c.L.P), grads->dB, c.p.out, 1};
+    return adapter::launch_gradients_tc(ctx, jobs, n, c.sorted, c.a.r, c.st);
+  }
   adapter::GradArgs g;
   std::memset(&g, 0, sizeof(g));
-  int n = 0;
-  if (grads->dA) g.job[n++] = {D, X, grads->dA, p.in, 1, (p.in + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
-  if (grads->dB) g.job[n++] = {P, dY, grads->dB, p.out, 0, (p.out + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
-  g.index = adapters->index; g.T = T; g.n = adapters->n; g.r = adapters->r;
-  const dim3 grid(g.job[0].blocks + g.job[1].blocks, adapters->n);
-  const cudaError_t e = f32 ? launch_pdl(adapter::gradient_kernel<true>, grid, dim3(adapter::THREADS), 0, st, g)
-                            : launch_pdl(adapter::gradient_kernel<false>, grid, dim3(adapter::THREADS), 0, st, g);
+  n = 0;
+  if (dA) g.job[n++] = {c.inner(c.L.D), X, grads->dA, c.p.in, 1, (c.p.in + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
+  if (dB) g.job[n++] = {c.inner(c.L.P), dY, grads->dB, c.p.out, 0, (c.p.out + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
+  g.index = adapters->index; g.T = T; g.n = c.a.n; g.r = c.a.r;
+  const dim3 grid(g.job[0].blocks + g.job[1].blocks, c.a.n);
+  const cudaError_t e = c.f32 ? launch_pdl(adapter::gradient_kernel<true>, grid, dim3(adapter::THREADS), 0, c.st, g)
+                              : launch_pdl(adapter::gradient_kernel<false>, grid, dim3(adapter::THREADS), 0, c.st, g);
   ctx->launches++;
   return check_cuda(ctx, e, "adapter::gradient_kernel launch");
 }

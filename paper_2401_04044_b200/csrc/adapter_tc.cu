@@ -1,0 +1,659 @@
+// Low-rank adapters on the tensor cores, for batches of more than a few tokens (bf16).
+//
+// The tokens are sorted by adapter first (a list of indices; nothing moves), so that every tile of 128 rows belongs to one
+// adapter.  (One product over tiles as they come, with the rows of other adapters set to zero, would be simpler; but zero
+// times an infinity or NaN is NaN, and a broken adapter or token would reach the other requests of its tile.)  Rows are
+// gathered by TMA, four to an instruction; rows behind a tile's last token are not loaded, or zeros.
+//
+//   shrink    P = scale_i V F_i       tiles x ranges of K; the ranges of a tile are a cluster and add up over shared memory
+//   expand    Y = base + P F_i        tiles x 128 columns
+//   gradient  out_i = V^T P           adapters x 128 columns, over the adapter's tokens
+//
+// All three read one wide matrix once and are bound by that: with r <= 128 there are at most 2 r operations to an element.
+// P is rounded to bf16 between two products (the tensor cores take both operands in one type), as H is in a training pass.
+// Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
+#include <cstring>
+
+#include "adapter.h"
+#include "epilogue.cuh"
+#include "ptx.cuh"
+
+namespace ffsp {
+namespace adapter {
+
+constexpr int TC_THREADS = 192;         // warps 0 - 3 epilogue (a row of the tile to a lane), 4 copies, 5 issues the MMAs
+constexpr int COPY_WARP = 4, MMA_WARP = 5;
+constexpr int BLOCK_K = 64, BLOCK64_BYTES = 64 * BLOCK_K * 2;
+constexpr int A_BYTES = TOKENS * BLOCK_K * 2, B_BYTES = MAX_RANK * BLOCK_K * 2;
+
+// ---------------------------------------------------------------------------------------------- sorting
+// A warp to a group: one pass counts its tokens and those of the groups before it, another writes them.
+__global__ void __launch_bounds__(256) sort_kernel(const int* __restrict__ index, Sorted s, int* status) {
+  pdl_wait();
+  const int g = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (g > s.n) return;
+  constexpr int FLIGHT = 8;
+  const auto group_of = [&](int i) { return i < 0 || i >= s.n ? s.n : i; };
+  int mine = 0, before = 0;
+  for (long long t0 = lane; t0 < s.T; t0 += 32 * FLIGHT) {
+    int v[FLIGHT];
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) v[k] = t0 + 32 * k < s.T ? group_of(__ldg(index + t0 + 32 * k)) : s.n + 1;
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) {
+      mine += v[k] == g;
+      before += v[k] < g;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+  }
+  if (lane == 0) {
+    s.count[g] = mine;
+    s.offset[g] = before;
+  }
+  if (mine == 0) return;
+  int at = before;
+  for (long long t0 = 0; t0 < s.T; t0 += 32 * FLIGHT) {
+    int v[FLIGHT];
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) v[k] = t0 + 32 * k + lane < s.T ? __ldg(index + t0 + 32 * k + lane) : 0;
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) {
+      const bool hit = t0 + 32 * k + lane < s.T && group_of(v[k]) == g;
+      const unsigned votes = __ballot_sync(0xffffffffu, hit);
+      if (hit) s.order[at + __popc(votes & ((1u << lane) - 1u))] = static_cast<int>(t0 + 32 * k + lane);
+      at += __popc(votes);
+      if (g == s.n && hit && v[k] >= s.n) record_status(status, FFSPLIT_ERR_BAD_INDEX, static_cast<int>(t0 + 32 * k + lane), KID_ADAPTER);
+    }
+  }
+}
+
+struct Tile {
+  int group, first, rows;     // the group (-1: no such tile), the place of its first token in the order, its tokens
+};
+// Tile u of groups 0 .. groups - 1, by one whole warp.
+__device__ __forceinline__ Tile find_tile(const Sorted& s, int groups, int u) {
+  const int lane = threadIdx.x & 31;
+  for (int g0 = 0; g0 < groups; g0 += 32) {
+    const int c = g0 + lane < groups ? __ldcg(s.count + g0 + lane) : 0, tiles = (c + TOKENS - 1) / TOKENS;
+    int upto = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    const unsigned votes = __ballot_sync(0xffffffffu, u < upto);
+    if (votes) {
+      const int l = __ffs(votes) - 1;
+      const int j = u - (__shfl_sync(0xffffffffu, upto, l) - __shfl_sync(0xffffffffu, tiles, l));
+      const int count = __shfl_sync(0xffffffffu, c, l) - j * TOKENS;
+      return {g0 + l, __ldcg(s.offset + g0 + l) + j * TOKENS, count < TOKENS ? count : TOKENS};
+    }
+    u -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return {-1, 0, 0};
+}
+// Tiles of the groups before g.
+__device__ __forceinline__ int tiles_before(const Sorted& s, int g) {
+  const int lane = threadIdx.x & 31;
+  int n = 0;
+  for (int i = lane; i < g; i += 32) n += (__ldcg(s.count + i) + TOKENS - 1) / TOKENS;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+  return n;
+}
+
+// Four rows of 64 columns from x on, one below the other at smem_dst (rows behind the tensor's last one: zeros).
+__device__ __forceinline__ void gather4(const CUtensorMap* tm, uint32_t smem_dst, uint32_t bar, int x, const int* rows) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(smem_dst),
+      "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(x), "r"(rows[0]), "r"(rows[1]), "r"(rows[2]), "r"(rows[3])
+      : "memory");
+}
+__device__ __forceinline__ void load_3d(const CUtensorMap* tm, uint32_t smem_dst, uint32_t bar, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_dst),
+               "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+// The places of four tokens of a tile in the batch; T (behind the last row) where there are fewer.
+__device__ __forceinline__ void four_tokens(const Sorted& s, int first, int rows, int r0, int* out) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = r0 + i < rows ? __ldcg(s.order + first + r0 + i) : static_cast<int>(s.T);
+}
+
+// What the three kernels share: barriers, tensor memory, and the way out.
+struct Frame {
+  uint32_t smem0;             // 1024-byte aligned
+  uint64_t *full, *empty, *done, *drain;
+  uint32_t tmem;
+  volatile int* abort_flag;
+};
+constexpr int FRAME_BYTES = 256, FRAME_STAGES = 8;
+__device__ __forceinline__ Frame frame_open(uint8_t* raw, int bytes, int stages, uint32_t tmem_cols) {
+  Frame f;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  f.smem0 = ptx::smem_u32(smem);
+  f.full = reinterpret_cast<uint64_t*>(smem + bytes);
+  f.empty = f.full + FRAME_STAGES;
+  f.done = f.empty + FRAME_STAGES;
+  f.drain = f.done + 1;
+  uint32_t* holder = reinterpret_cast<uint32_t*>(f.drain + 1);
+  f.abort_flag = reinterpret_cast<volatile int*>(holder + 1);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      ptx::mbar_init(&f.full[s], 1);
+      ptx::mbar_init(&f.empty[s], 1);
+    }
+    ptx::mbar_init(f.done, 1);
+    ptx::mbar_init(f.drain, 1);
+    *f.abort_flag = 0;
+    ptx::mbar_fence_init();
+  }
+  if (threadIdx.x >> 5 == MMA_WARP) {
+    ptx::tmem_alloc(holder, tmem_cols);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  f.tmem = *holder;
+  return f;
+}
+// The MMA warp waits (bounded) for its MMAs, the copy warp gives its copies a bounded time to land, when giving up.
+__device__ __forceinline__ void mma_gave_up(const Frame& f) {
+  if (ptx::elect_one()) {
+    ptx::umma_commit(f.drain);
+    const long long t0 = clock64();
+    while (!ptx::mbar_try_wait(f.drain, 0) && clock64() - t0 < ptx::kWaitLimitCycles / 8) {}
+  }
+  __syncwarp();
+}
+__device__ __forceinline__ void copies_gave_up() {
+  const long long t0 = clock64();
+  while (clock64() - t0 < ptx::kWaitLimitCycles / 64) {}
+}
+__device__ __forceinline__ void frame_close(const Frame& f, uint32_t tmem_cols, int* status) {
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *f.abort_flag) record_status(status, FFSPLIT_ERR_TIMEOUT, blockIdx.x, KID_ADAPTER);
+  if (threadIdx.x >> 5 == MMA_WARP) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(f.tmem, tmem_cols);
+  }
+}
+// One k-block of `steps` MMAs of 16.
+__device__ __forceinline__ void issue(uint32_t d, uint64_t a, uint32_t a_step, uint64_t b, uint32_t b_step, uint32_t idesc, int steps, bool first) {
+  for (int k = 0; k < steps; ++k) ptx::umma_bf16(d, a + k * a_step, b + k * b_step, idesc, first && k == 0 ? 0u : 1u);
+}
+__device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+
+// ---------------------------------------------------------------------------------------------- shrink
+struct ShrinkDev {
+  CUtensorMap V, F;
+  __nv_bfloat16* P;
+  int kb, f_mn;               // f_mn: the rank runs along memory
+};
+struct ShrinkParams {
+  ShrinkDev job[2];
+  Sorted s;
+  const float* scale;
+  int r, cols, pitch;         // cols: r rounded up to 16
+  int* status;
+};
+constexpr int SHRINK_STAGES = 4, SHRINK_RING = SHRINK_STAGES * (A_BYTES + B_BYTES);
+constexpr int SHRINK_SMEM = 1024 + SHRINK_RING + FRAME_BYTES;
+constexpr uint32_t SHRINK_TMEM = 128;
+static_assert(SHRINK_RING >= TOKENS * (MAX_RANK + 4) * 4, "the partial sums take the place of the ring");
+
+__global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_constant__ ShrinkParams p) {
+  extern __shared__ uint8_t raw[];
+  pdl_wait();
+  const ShrinkDev& job = p.job[blockIdx.z];
+  const int ranges = gridDim.x, range = blockIdx.x;         // a cluster spans x
+  const Tile tile = find_tile(p.s, p.s.n, blockIdx.y);
+  if (tile.group < 0) return;                               // (the whole cluster)
+  const Frame f = frame_open(raw, SHRINK_RING, SHRINK_STAGES, SHRINK_TMEM);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int per = (job.kb + ranges - 1) / ranges, k0 = range * per, k1 = k0 + per < job.kb ? k0 + per : job.kb;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  float* part = reinterpret_cast<float*>(smem);
+  const int part_pitch = p.cols + 4;
+  if (warp == COPY_WARP) {
+    int rows[4];
+    four_tokens(p.s, tile.first, tile.rows, lane * 4, rows);
+    const bool has = lane * 4 < tile.rows;
+    // the factor's box: 64 k x 64 ranks, one or two of them; or all ranks (as many rows as there are columns of the tile) x 64 k
+    const uint32_t tx = static_cast<uint32_t>((tile.rows + 3) / 4 * 512 + (job.f_mn ? (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES : p.cols * BLOCK_K * 2));
+    bool ok = true;
+    for (int kb = k0, i = 0; kb < k1; ++kb, ++i) {
+      const int s = i % SHRINK_STAGES;
+      ok = ptx::mbar_wait_warp(&f.empty[s], ((i / SHRINK_STAGES) & 1) ^ 1, f.abort_flag);
+      if (!ok) break;
+      const uint32_t to = f.smem0 + s * (A_BYTES + B_BYTES), bar = ptx::smem_u32(&f.full[s]);
+      if (lane == 0) {
+        ptx::mbar_expect_tx(&f.full[s], tx);
+        if (job.f_mn) {
+          load_3d(&job.F, to + A_BYTES, bar, 0, kb * BLOCK_K, tile.group);
+          if (p.cols > 64) load_3d(&job.F, to + A_BYTES + BLOCK64_BYTES, bar, 64, kb * BLOCK_K, tile.group);
+        } else {
+          load_3d(&job.F, to + A_BYTES, bar, kb * BLOCK_K, 0, tile.group);
+        }
+      }
+      __syncwarp();
+      if (has) gather4(&job.V, to + lane * 512, bar, kb * BLOCK_K, rows);
+    }
+    if (!ok) copies_gave_up();
+    __syncwarp();
+  } else if (warp == MMA_WARP) {
+    const uint32_t idesc = ptx::umma_idesc_bf16(TOKENS, p.cols) | (job.f_mn ? 1u << 16 : 0u);
+    bool ok = true;
+    for (int kb = k0, i = 0; kb < k1; ++kb, ++i) {
+      const int s = i % SHRINK_STAGES;
+      ok = ptx::mbar_wait_warp(&f.full[s], (i / SHRINK_STAGES) & 1, f.abort_flag);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      const uint32_t at = f.smem0 + s * (A_BYTES + B_BYTES);
+      if (ptx::elect_one()) {
+        issue(f.tmem, ptx::umma_desc_k128(at), 32 >> 4, job.f_mn ? ptx::umma_desc_mn128(at + A_BYTES, BLOCK64_BYTES) : ptx::umma_desc_k128(at + A_BYTES),
+              job.f_mn ? 2048 >> 4 : 32 >> 4, idesc, BLOCK_K / 16, i == 0);
+        ptx::umma_commit(&f.empty[s]);
+      }
+      __syncwarp();
+    }
+    if (ok) {
+      if (ptx::elect_one()) ptx::umma_commit(f.done);
+      __syncwarp();
+    } else {
+      mma_gave_up(f);
+    }
+  } else {
+    const bool any = k0 < k1;
+    if (ptx::mbar_wait(f.done, 0, f.abort_flag)) {
+      ptx::tc_fence_after();
+      // every copy has landed and every MMA has read it: the ring is free
+      for (int c = 0; c < p.cols; c += 16) {
+        float v[16];
+        ptx::tmem_ld16(f.tmem + (static_cast<uint32_t>(warp * 32) << 16) + c, v);
+        ptx::tmem_ld_wait();
+        float4* to = reinterpret_cast<float4*>(part + (warp * 32 + lane) * part_pitch + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = any ? make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    }
+    __syncwarp();
+  }
+  __syncwarp();
+  ptx::cluster_sync_all();
+  // the ranges' sums, in order; every CTA of the cluster takes a share of the tile
+  const float scale = p.scale ? __ldg(p.scale + tile.group) : 1.f;
+  const int pairs = p.cols / 2;
+  __nv_bfloat16* P = job.P + static_cast<long long>(blockIdx.y) * TOKENS * p.pitch;
+  const uint32_t part0 = ptx::smem_u32(part);
+  for (int e = range * TC_THREADS + threadIdx.x; e < TOKENS * pairs; e += ranges * TC_THREADS) {
+    const int row = e / pairs, c = (e - row * pairs) * 2;
+    float x = 0.f, y = 0.f;
+    if (row < tile.rows) {
+      for (int k = 0; k < ranges; ++k) {
+        float a, b;
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(a), "=f"(b) : "r"(ptx::map_to_cta(part0 + (row * part_pitch + c) * 4, k)));
+        x += a; y += b;
+      }
+    }
+    *reinterpret_cast<uint32_t*>(P + static_cast<long long>(row) * p.pitch + c) = bf16_pair(scale * x, scale * y);
+  }
+  ptx::cluster_sync_all();      // nobody leaves while its sums are read
+  frame_close(f, SHRINK_TMEM, p.status);
+}
+
+// ---------------------------------------------------------------------------------------------- expand
+struct ExpandParams {
+  CUtensorMap P, F;
+  Sorted s;
+  const __nv_bfloat16* base;
+  __nv_bfloat16* Y;
+  int N, r, f_mn, wide;       // f_mn: the columns run along memory; wide: rows start on 16 bytes
+  int* status;
+};
+constexpr int EXPAND_COLS = 128;
+constexpr int EXPAND_BYTES = 2 * (A_BYTES + EXPAND_COLS * BLOCK_K * 2), EXPAND_SMEM = 1024 + EXPAND_BYTES + FRAME_BYTES;
+constexpr uint32_t EXPAND_TMEM = 128;
+
+__global__ void __launch_bounds__(TC_THREADS) expand_tc_kernel(const __grid_constant__ ExpandParams p) {
+  extern __shared__ uint8_t raw[];
+  pdl_wait();
+  const Tile tile = find_tile(p.s, p.s.n + 1, blockIdx.y);
+  if (tile.group < 0) return;
+  const bool none = tile.group == p.s.n;
+  if (none && p.base == p.Y) return;
+  const Frame f = frame_open(raw, EXPAND_BYTES, 1, EXPAND_TMEM);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n0 = blockIdx.x * EXPAND_COLS;
+  const int blocks = p.r > BLOCK_K ? 2 : 1;
+  if (none) {
+    // nothing to add
+  } else if (warp == COPY_WARP) {
+    if (ptx::elect_one()) {
+      ptx::mbar_expect_tx(&f.full[0], blocks * (A_BYTES + EXPAND_COLS * BLOCK_K * 2));
+      const uint32_t bar = ptx::smem_u32(&f.full[0]);
+      for (int b = 0; b < blocks; ++b) {
+        const uint32_t to = f.smem0 + b * (A_BYTES + EXPAND_COLS * BLOCK_K * 2);
+        load_3d(&p.P, to, bar, b * BLOCK_K, blockIdx.y * TOKENS, 0);
+        if (p.f_mn) {
+          load_3d(&p.F, to + A_BYTES, bar, n0, b * BLOCK_K, tile.group);
+          load_3d(&p.F, to + A_BYTES + BLOCK64_BYTES, bar, n0 + 64, b * BLOCK_K, tile.group);
+        } else {
+          load_3d(&p.F, to + A_BYTES, bar, b * BLOCK_K, n0, tile.group);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == MMA_WARP) {
+    const uint32_t idesc = ptx::umma_idesc_bf16(TOKENS, EXPAND_COLS) | (p.f_mn ? 1u << 16 : 0u);
+    if (ptx::mbar_wait_warp(&f.full[0], 0, f.abort_flag)) {
+      ptx::tc_fence_after();
+      if (ptx::elect_one()) {
+        for (int b = 0; b < blocks; ++b) {
+          const uint32_t at = f.smem0 + b * (A_BYTES + EXPAND_COLS * BLOCK_K * 2);
+          const int left = (p.r - b * BLOCK_K + 15) / 16;
+          issue(f.tmem, ptx::umma_desc_k128(at), 32 >> 4, p.f_mn ? ptx::umma_desc_mn128(at + A_BYTES, BLOCK64_BYTES) : ptx::umma_desc_k128(at + A_BYTES),
+                p.f_mn ? 2048 >> 4 : 32 >> 4, idesc, left < 4 ? left : 4, b == 0);
+        }
+        ptx::umma_commit(f.done);
+      }
+      __syncwarp();
+    } else {
+      copies_gave_up();
+    }
+  }
+  if (warp < 4) {
+    const int row = warp * 32 + lane, width = p.N - n0 < EXPAND_COLS ? p.N - n0 : EXPAND_COLS;
+    const bool in = row < tile.rows;
+    const long long at = in ? static_cast<long long>(__ldcg(p.s.order + tile.first + row)) * p.N + n0 : 0;
+    const bool ready = none || ptx::mbar_wait(f.done, 0, f.abort_flag);
+    if (ready && warp * 32 < tile.rows) {
+      ptx::tc_fence_after();
+#pragma unroll 2
+      for (int c = 0; c < width; c += 16) {
+        float v[16];
+        if (none) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        } else {
+          ptx::tmem_ld16(f.tmem + (static_cast<uint32_t>(warp * 32) << 16) + c, v);
+          ptx::tmem_ld_wait();
+        }
+        if (in && p.wide) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (c + 8 * h >= width) break;
+            float* x = v + 8 * h;
+            if (p.base) {
+              const uint4 q = *reinterpret_cast<const uint4*>(p.base + at + c + 8 * h);
+              const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                x[2 * i] += __uint_as_float(w[i] << 16);
+                x[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
+              }
+            }
+            *reinterpret_cast<uint4*>(p.Y + at + c + 8 * h) =
+                make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+          }
+        } else if (in) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            if (c + i >= width) break;
+            p.Y[at + c + i] = __float2bfloat16_rn(p.base ? __bfloat162float(p.base[at + c + i]) + v[i] : v[i]);
+          }
+        }
+        __syncwarp();
+      }
+    }
+    __syncwarp();
+  }
+  frame_close(f, EXPAND_TMEM, p.status);
+}
+
+// ---------------------------------------------------------------------------------------------- gradients
+struct GradientDev {
+  CUtensorMap V, P;
+  __nv_bfloat16* out;
+  int N, rank_rows, blocks;
+};
+struct GradientParams {
+  GradientDev job[2];
+  Sorted s;
+  int r, cols, wide;          // wide: r is a multiple of 8
+  int* status;
+};
+constexpr int GRADIENT_STAGES = 3, GRADIENT_RING = GRADIENT_STAGES * (A_BYTES + B_BYTES), GRADIENT_SMEM = 1024 + GRADIENT_RING + FRAME_BYTES;
+constexpr uint32_t GRADIENT_TMEM = 128;
+
+__global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_constant__ GradientParams p) {
+  extern __shared__ uint8_t raw[];
+  pdl_wait();
+  const int which = static_cast<int>(blockIdx.x) >= p.job[0].blocks ? 1 : 0, i = blockIdx.y;
+  const GradientDev& job = p.job[which];
+  const int c0 = (blockIdx.x - (which ? p.job[0].blocks : 0)) * TOKENS;     // 128 columns of V: the rows of the tile
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int count = __ldcg(p.s.count + i), first = __ldcg(p.s.offset + i);
+  const Frame f = frame_open(raw, GRADIENT_RING, GRADIENT_STAGES, GRADIENT_TMEM);
+  const int kb = (count + BLOCK_K - 1) / BLOCK_K;
+  if (warp == COPY_WARP) {
+    const int tile0 = tiles_before(p.s, i);
+    const uint32_t tx = A_BYTES + (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES;
+    bool ok = true;
+    for (int k = 0; k < kb; ++k) {
+      const int s = k % GRADIENT_STAGES;
+      int rows[4];
+      four_tokens(p.s, first + k * BLOCK_K, count - k * BLOCK_K, (lane & 15) * 4, rows);
+      ok = ptx::mbar_wait_warp(&f.empty[s], ((k / GRADIENT_STAGES) & 1) ^ 1, f.abort_flag);
+      if (!ok) break;
+      const uint32_t to = f.smem0 + s * (A_BYTES + B_BYTES), bar = ptx::smem_u32(&f.full[s]);
+      if (lane == 0) {
+        ptx::mbar_expect_tx(&f.full[s], tx);
+        load_3d(&job.P, to + A_BYTES, bar, 0, tile0 * TOKENS + k * BLOCK_K, 0);
+        if (p.cols > 64) load_3d(&job.P, to + A_BYTES + BLOCK64_BYTES, bar, 64, tile0 * TOKENS + k * BLOCK_K, 0);
+      }
+      __syncwarp();
+      gather4(&job.V, to + (lane >> 4) * BLOCK64_BYTES + (lane & 15) * 512, bar, c0 + (lane >> 4) * 64, rows);
+    }
+    if (!ok) copies_gave_up();
+    __syncwarp();
+  } else if (warp == MMA_WARP) {
+    const uint32_t idesc = ptx::umma_idesc_bf16(TOKENS, p.cols) | 1u << 15 | 1u << 16;
+    bool ok = true;
+    for (int k = 0; k < kb; ++k) {
+      const int s = k % GRADIENT_STAGES;
+      ok = ptx::mbar_wait_warp(&f.full[s], (k / GRADIENT_STAGES) & 1, f.abort_flag);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      const uint32_t at = f.smem0 + s * (A_BYTES + B_BYTES);
+      if (ptx::elect_one()) {
+        issue(f.tmem, ptx::umma_desc_mn128(at, BLOCK64_BYTES), 2048 >> 4, ptx::umma_desc_mn128(at + A_BYTES, BLOCK64_BYTES), 2048 >> 4, idesc, BLOCK_K / 16, k == 0);
+        ptx::umma_commit(&f.empty[s]);
+      }
+      __syncwarp();
+    }
+    if (ok) {
+      if (ptx::elect_one()) ptx::umma_commit(f.done);
+      __syncwarp();
+    } else {
+      mma_gave_up(f);
+    }
+  } else {
+    const int col = c0 + warp * 32 + lane;
+    const bool in = col < job.N;
+    if (ptx::mbar_wait(f.done, 0, f.abort_flag)) {
+      ptx::tc_fence_after();
+      for (int c = 0; c < p.r; c += 16) {
+        float v[16];
+        ptx::tmem_ld16(f.tmem + (static_cast<uint32_t>(warp * 32) << 16) + c, v);
+        ptx::tmem_ld_wait();
+        if (kb == 0) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = 0.f;
+        }
+        if (in && job.rank_rows) {
+          __nv_bfloat16* out = job.out + (static_cast<long long>(i) * p.r + c) * job.N + col;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) if (c + k < p.r) out[static_cast<long long>(k) * job.N] = __float2bfloat16_rn(v[k]);
+        } else if (in) {
+          __nv_bfloat16* out = job.out + (static_cast<long long>(i) * job.N + col) * p.r + c;
+          if (p.wide) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float* x = v + 8 * h;
+              if (c + 8 * h < p.r)
+                *reinterpret_cast<uint4*>(out + 8 * h) = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) if (c + k < p.r) out[k] = __float2bfloat16_rn(v[k]);
+          }
+        }
+        __syncwarp();
+      }
+    }
+    __syncwarp();
+  }
+  frame_close(f, GRADIENT_TMEM, p.status);
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// [planes][rows][cols] with pitch ld: boxes of 64 columns x box_rows, 128-byte swizzle, zeros outside.
+ffsplit_status encode(ffsplit_ctx* ctx, const void* at, long long cols, long long rows, long long planes, long long ld, int rank, int box_rows, CUtensorMap* out) {
+  if (!ctx->encode_fn) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+    if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn)
+      return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    ctx->encode_fn = fn;
+  }
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(planes)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld * rows) * 2};
+  cuuint32_t box[3] = {BLOCK_K, static_cast<cuuint32_t>(box_rows), 1}, estr[3] = {1, 1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_fn)(
+      out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(at), dims, strides, box, estr,
+      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
+  return FFSPLIT_OK;
+}
+ffsplit_status encode_gather(ffsplit_ctx* ctx, const tg::Matrix& m, CUtensorMap* out) { return encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, 1, out); }
+ffsplit_status encode_factor(ffsplit_ctx* ctx, const Factor& f, int n, int box_rows, CUtensorMap* out) {
+  return encode(ctx, f.m.p, f.cols, f.rows, n, f.m.ld, 3, box_rows, out);
+}
+
+// The tensor maps are made by a driver call, which needs a current context; and the kernels take more than 48 KB.
+ffsplit_status set_up(ffsplit_ctx* ctx) {
+  const cudaError_t bound = cudaSetDevice(ctx->device);
+  if (bound != cudaSuccess) return check_cuda(ctx, bound, "cudaSetDevice");
+  if (ctx->attr_adapter_set) return FFSPLIT_OK;
+  cudaError_t e = cudaFuncSetAttribute(shrink_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SHRINK_SMEM);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(expand_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EXPAND_SMEM);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(gradient_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GRADIENT_SMEM);
+  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(adapter kernels)");
+  ctx->attr_adapter_set = true;
+  return FFSPLIT_OK;
+}
+
+}  // namespace
+
+ffsplit_status launch_sort(ffsplit_ctx* ctx, const int* index, const Sorted& s, cudaStream_t st) {
+  const cudaError_t e = launch_pdl(sort_kernel, dim3((s.n + 8) / 8), dim3(256), 0, st, index, s, ctx->status());
+  ctx->launches++;
+  return check_cuda(ctx, e, "adapter::sort_kernel launch");
+}
+
+ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, const Sorted& s, int r, const float* scale, cudaStream_t st) {
+  ffsplit_status rc = set_up(ctx);
+  if (rc != FFSPLIT_OK) return rc;
+  ShrinkParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.s = s; p.scale = scale; p.r = r; p.cols = round_up(r, 16); p.pitch = rank_pitch(r); p.status = ctx->status();
+  int kb = 1;
+  for (int i = 0; i < n; ++i) {
+    ShrinkDev& d = p.job[i];
+    if ((rc = encode_gather(ctx, jobs[i].V, &d.V)) != FFSPLIT_OK) return rc;
+    d.f_mn = jobs[i].F.rank_rows ? 0 : 1;
+    if ((rc = encode_factor(ctx, jobs[i].F, s.n, d.f_mn ? BLOCK_K : p.cols, &d.F)) != FFSPLIT_OK) return rc;
+    d.P = jobs[i].P;
+    d.kb = (jobs[i].K + BLOCK_K - 1) / BLOCK_K;
+    if (d.kb > kb) kb = d.kb;
+  }
+  // ranges of K: as many CTAs as SMs, four k-blocks each at least (the cluster's exchange takes about as long)
+  const long long tiles = tile_bound(s.T, s.n);
+  int ranges = 1;
+  while (ranges < 8 && 2 * ranges * tiles * n <= ctx->num_sms && 8 * ranges <= kb) ranges *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ranges, static_cast<unsigned>(tiles), n);
+  cfg.blockDim = dim3(TC_THREADS);
+  cfg.dynamicSmemBytes = SHRINK_SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ranges;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, shrink_tc_kernel, p);
+  ctx->launches++;
+  return check_cuda(ctx, e, "adapter::shrink_tc_kernel launch");
+}
+
+ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const Factor& F, int N, const void* base, void* Y, const Sorted& s,
+                                int r, cudaStream_t st) {
+  ffsplit_status rc = set_up(ctx);
+  if (rc != FFSPLIT_OK) return rc;
+  ExpandParams p;
+  std::memset(&p, 0, sizeof(p));
+  const long long tiles = tile_bound(s.T, s.n);
+  p.f_mn = F.rank_rows;
+  if ((rc = encode(ctx, P, rank_pitch(r), tiles * TOKENS, 1, rank_pitch(r), 3, TOKENS, &p.P)) != FFSPLIT_OK) return rc;
+  if ((rc = encode_factor(ctx, F, s.n, p.f_mn ? BLOCK_K : EXPAND_COLS, &p.F)) != FFSPLIT_OK) return rc;
+  p.s = s;
+  p.base = static_cast<const __nv_bfloat16*>(base); p.Y = static_cast<__nv_bfloat16*>(Y);
+  p.N = N; p.r = r; p.wide = N % 8 == 0; p.status = ctx->status();
+  const cudaError_t e = launch_pdl(expand_tc_kernel, dim3((N + EXPAND_COLS - 1) / EXPAND_COLS, static_cast<unsigned>(tiles)), dim3(TC_THREADS), EXPAND_SMEM, st, p);
+  ctx->launches++;
+  return check_cuda(ctx, e, "adapter::expand_tc_kernel launch");
+}
+
+ffsplit_status launch_gradients_tc(ffsplit_ctx* ctx, const Gradient* jobs, int n, const Sorted& s, int r, cudaStream_t st) {
+  ffsplit_status rc = set_up(ctx);
+  if (rc != FFSPLIT_OK) return rc;
+  GradientParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.s = s; p.r = r; p.cols = round_up(r, 16); p.wide = r % 8 == 0; p.status = ctx->status();
+  int blocks = 0;
+  for (int i = 0; i < n; ++i) {
+    GradientDev& d = p.job[i];
+    if ((rc = encode_gather(ctx, jobs[i].V, &d.V)) != FFSPLIT_OK) return rc;
+    if ((rc = encode(ctx, jobs[i].P, rank_pitch(r), tile_bound(s.T, s.n) * TOKENS, 1, rank_pitch(r), 3, BLOCK_K, &d.P)) != FFSPLIT_OK) return rc;
+    d.out = static_cast<__nv_bfloat16*>(jobs[i].out);
+    d.N = jobs[i].N; d.rank_rows = jobs[i].rank_rows;
+    d.blocks = (jobs[i].N + TOKENS - 1) / TOKENS;
+    blocks += d.blocks;
+  }
+  const cudaError_t e = launch_pdl(gradient_tc_kernel, dim3(blocks, s.n), dim3(TC_THREADS), GRADIENT_SMEM, st, p);
+  ctx->launches++;
+  return check_cuda(ctx, e, "adapter::gradient_tc_kernel launch");
+}
+
+}  // namespace adapter
+}  // namespace ffsp

@@ -211,6 +211,7 @@ struct ffsplit_ctx {
   bool attr_ares_set = false;
   bool attr_layer_set = false;
   bool attr_att_set = false;
+  bool attr_adapter_set = false;
   unsigned attr_train_set = 0;   // one bit to an instance of the training products' kernel
   unsigned attr_muon_set = 0;    // likewise, of the Newton-Schulz products' kernel
   int* status() const { return reinterpret_cast<int*>(ws); }
