@@ -4,8 +4,7 @@
 //   backward:  D[t] = s_i (dY[t] B_i^T),  dX[t] = dY[t] W^T + D[t] A_i^T,  dA_i = sum_t X[t]^T D[t],  dB_i = sum_t P[t]^T dY[t]
 //
 // The shared product runs on the tensor cores (train_gemm.cu).  So do the adapters' products of bf16 batches of more than
-// FEW tokens (adapter_tc.cu).  Those of few tokens and of fp32 layers are taken here, on the CUDA cores in fp32, eight tokens
-// to a block, which share a factor's elements where they use the same adapter.
+// FEW tokens (adapter_tc.cu).  Those of few tokens and of fp32 layers are taken here, on the CUDA cores in fp32.
 #include <cstring>
 
 #include "adapter.h"
@@ -15,13 +14,31 @@ namespace ffsp {
 namespace adapter {
 
 constexpr int FEW = 64;
-constexpr int GROUP = 8;             // tokens of a block
 constexpr int THREADS = 256;
-constexpr int CHUNK = 256;           // elements along a contraction that are staged at a time
+constexpr int CHUNK = 512;           // elements along a contraction that are staged at a time
+constexpr int MAX_SPLITS = 32;
+// Tokens of a block.  Tokens of one adapter share its elements; one token to a block where each may have its own.
+constexpr int MANY = 8, SOME = 4;
+template <bool F32> constexpr int VEC = F32 ? 4 : 8;      // elements of 16 bytes
 
 template <bool F32>
 __device__ __forceinline__ float load(const void* p, long long i) {
   return F32 ? __ldg(static_cast<const float*>(p) + i) : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+template <bool F32>
+__device__ __forceinline__ void load_vec(const void* p, long long i, float* v) {      // 16-byte aligned
+  if constexpr (F32) {
+    const float4 q = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p) + i));
+    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+  } else {
+    const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + i));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = __uint_as_float(w[k] << 16);
+      v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+    }
+  }
 }
 template <bool F32>
 __device__ __forceinline__ void store(void* p, long long i, float v) {
@@ -33,10 +50,11 @@ __device__ __forceinline__ int adapter_of(const int* index, long long t, int n) 
   return i < 0 || i >= n ? -1 : i;
 }
 
-// P[t][j] = scale_i sum_k V[t][k] F_i(k, j).  F lies as [n][K][r] (k_minor = 0) or [n][r][K].
+// P[t][j] = scale_i sum_k V[t][k] F_i(k, j).  F lies as [n][K][r] (k_minor = 0) or [n][r][K].  K is cut into ranges, so that
+// few tokens occupy all SMs; the ranges' sums are added by whoever reads P.  Bound by reading each token's factor once.
 struct ShrinkJob {
   const void *V, *F;
-  float* P;               // [T][r]
+  float* P;               // [splits][T][r]
   int K, k_minor;
 };
 struct ShrinkArgs {
@@ -44,126 +62,256 @@ struct ShrinkArgs {
   const int* index;
   const float* scale;
   long long T;
-  int n, r, lanes;        // lanes: a power of two, at least r
+  int n, r, splits;
   int* status;
 };
-template <bool F32>
+template <bool F32, int G>
 __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__ ShrinkArgs a) {
-  __shared__ float x[GROUP][CHUNK];
-  __shared__ float part[THREADS][GROUP + 1];
+  constexpr int V = VEC<F32>;
+  __shared__ float x[G][CHUNK];
+  __shared__ float part[THREADS * V * G < MAX_RANK * G * 8 ? MAX_RANK * G * 8 : THREADS * V * G];
   pdl_wait();
   const ShrinkJob& job = a.job[blockIdx.y];
-  const long long t0 = static_cast<long long>(blockIdx.x) * GROUP;
-  const int count = a.T - t0 < GROUP ? static_cast<int>(a.T - t0) : GROUP;
-  int of[GROUP];
+  const long long t0 = static_cast<long long>(blockIdx.x) * G;
+  const int count = a.T - t0 < G ? static_cast<int>(a.T - t0) : G;
+  int of[G];
 #pragma unroll
-  for (int g = 0; g < GROUP; ++g) {
+  for (int g = 0; g < G; ++g) {
     of[g] = g < count ? adapter_of(a.index, t0 + g, a.n) : -1;
-    if (threadIdx.x == 0 && blockIdx.y == 0 && g < count && __ldg(a.index + t0 + g) >= a.n)
+    if (threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && g < count && __ldg(a.index + t0 + g) >= a.n)
       record_status(a.status, FFSPLIT_ERR_BAD_INDEX, static_cast<int>(t0 + g), KID_ADAPTER);
   }
-  const int lanes = a.lanes, slices = THREADS / lanes, j = threadIdx.x & (lanes - 1), slice = threadIdx.x / lanes;
+  const int per = ((job.K + a.splits - 1) / a.splits + 63) / 64 * 64, begin = blockIdx.z * per, end = begin + per < job.K ? begin + per : job.K;
+  float* P = job.P + blockIdx.z * a.T * a.r;
+  const bool wide = (job.k_minor ? job.K : a.r) % V == 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // the rank along memory: a thread to `step` ranks of every slices-th k
+  const int step = wide ? V : 1, across = (a.r + step - 1) / step, slices = THREADS / across;
+  const int slice = threadIdx.x / across, j0 = (threadIdx.x - slice * across) * step;
   for (int first = 0; first < count; ++first) {
-    const int i = of[first];
+    int i = -1;
     unsigned mask = 0;
 #pragma unroll
-    for (int g = 0; g < GROUP; ++g) mask |= of[g] == i ? 1u << g : 0u;
+    for (int g = 0; g < G; ++g) if (g == first) i = of[g];
+#pragma unroll
+    for (int g = 0; g < G; ++g) mask |= of[g] == i ? 1u << g : 0u;
     if (i < 0 || (mask & ((1u << first) - 1u))) continue;      // none, or taken with an earlier token
     const float scale = a.scale ? __ldg(a.scale + i) : 1.f;
     const long long f0 = static_cast<long long>(i) * job.K * a.r;
-    if (!job.k_minor) {
-      float acc[GROUP] = {};
-      for (int k0 = 0; k0 < job.K; k0 += CHUNK) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < GROUP * CHUNK; e += THREADS) {
-          const int g = e / CHUNK, k = e % CHUNK;
-          x[g][k] = (mask >> g & 1u) && k0 + k < job.K ? load<F32>(job.V, (t0 + g) * job.K + k0 + k) : 0.f;
-        }
-        __syncthreads();
-        const int end = job.K - k0 < CHUNK ? job.K - k0 : CHUNK;
-        if (j < a.r) {
-          for (int k = slice; k < end; k += slices) {
-            const float f = load<F32>(job.F, f0 + static_cast<long long>(k0 + k) * a.r + j);
+    float acc[V][G];
 #pragma unroll
-            for (int g = 0; g < GROUP; ++g) acc[g] = fmaf(x[g][k], f, acc[g]);
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int g = 0; g < G; ++g) acc[v][g] = 0.f;
+    bool fresh = true;
+    for (int k0 = begin; k0 < end; k0 += CHUNK) {
+      const int m = end - k0 < CHUNK ? end - k0 : CHUNK;
+      __syncthreads();
+      for (int e = threadIdx.x; e < G * CHUNK; e += THREADS) {
+        const int g = e / CHUNK, k = e % CHUNK;
+        x[g][k] = (mask >> g & 1u) && k < m ? load<F32>(job.V, (t0 + g) * job.K + k0 + k) : 0.f;
+      }
+      __syncthreads();
+      if (!job.k_minor) {
+        if (slice < slices) {
+          if (wide) {
+#pragma unroll 4
+            for (int k = slice; k < m; k += slices) {
+              float f[V];
+              load_vec<F32>(job.F, f0 + static_cast<long long>(k0 + k) * a.r + j0, f);
+#pragma unroll
+              for (int g = 0; g < G; ++g) {
+                const float y = x[g][k];
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v][g] = fmaf(y, f[v], acc[v][g]);
+              }
+            }
+          } else {
+#pragma unroll 4
+            for (int k = slice; k < m; k += slices) {
+              const float f = load<F32>(job.F, f0 + static_cast<long long>(k0 + k) * a.r + j0);
+#pragma unroll
+              for (int g = 0; g < G; ++g) acc[0][g] = fmaf(x[g][k], f, acc[0][g]);
+            }
+          }
+        }
+      } else {
+        // a warp to a rank, lanes along the contraction
+        for (int c = warp; c < a.r; c += THREADS / 32) {
+          float sum[G] = {};
+          const long long at = f0 + static_cast<long long>(c) * job.K + k0;
+          if (wide) {
+#pragma unroll 2
+            for (int k = lane * V; k < m; k += 32 * V) {
+              float f[V];
+              load_vec<F32>(job.F, at + k, f);
+#pragma unroll
+              for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[g] = fmaf(x[g][k + v], f[v], sum[g]);
+            }
+          } else {
+#pragma unroll 4
+            for (int k = lane; k < m; k += 32) {
+              const float f = load<F32>(job.F, at + k);
+#pragma unroll
+              for (int g = 0; g < G; ++g) sum[g] = fmaf(x[g][k], f, sum[g]);
+            }
+          }
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], o);
+            if (lane == 0) part[c * G + g] = fresh ? sum[g] : part[c * G + g] + sum[g];
           }
         }
       }
-#pragma unroll
-      for (int g = 0; g < GROUP; ++g) part[threadIdx.x][g] = acc[g];
-      __syncthreads();
-      for (int e = threadIdx.x; e < a.r * GROUP; e += THREADS) {
-        const int g = e / a.r, c = e - g * a.r;
-        if (!(mask >> g & 1u)) continue;
-        float s = 0.f;
-        for (int k = 0; k < slices; ++k) s += part[k * lanes + c][g];
-        job.P[(t0 + g) * a.r + c] = scale * s;
-      }
-    } else {
-      // a warp to a rank, lanes along the contraction
-      for (int c = warp; c < a.r; c += THREADS / 32) {
-        float acc[GROUP] = {};
-        for (int k = lane; k < job.K; k += 32) {
-          const float f = load<F32>(job.F, f0 + static_cast<long long>(c) * job.K + k);
-#pragma unroll
-          for (int g = 0; g < GROUP; ++g)
-            if (mask >> g & 1u) acc[g] = fmaf(load<F32>(job.V, (t0 + g) * job.K + k), f, acc[g]);
-        }
-#pragma unroll
-        for (int g = 0; g < GROUP; ++g) {
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) acc[g] += __shfl_xor_sync(0xffffffffu, acc[g], o);
-          if (lane == 0 && (mask >> g & 1u)) job.P[(t0 + g) * a.r + c] = scale * acc[g];
-        }
-      }
+      fresh = false;
     }
+    __syncthreads();
+    if (!job.k_minor) {
+      if (slice < slices) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (v < step)
+#pragma unroll
+            for (int g = 0; g < G; ++g) part[(slice * a.r + j0 + v) * G + g] = acc[v][g];
+      }
+      __syncthreads();
+    }
+    for (int e = threadIdx.x; e < a.r * G; e += THREADS) {
+      const int c = e / G, g = e - c * G;
+      if (!(mask >> g & 1u)) continue;
+      float s = 0.f;
+      if (begin < end) {
+        const int sums = job.k_minor ? 1 : slices;
+        for (int k = 0; k < sums; ++k) s += part[(k * a.r + c) * G + g];
+      }
+      P[(t0 + g) * a.r + c] = scale * s;
+    }
+    __syncthreads();
   }
 }
 
-// Y[t][c] = base[t][c] + sum_j P[t][j] F_i(j, c).  F lies as [n][r][N] (r_minor = 0) or [n][N][r].
+// Y[t][c] = base[t][c] + sum_j P[t][j] F_i(j, c).  F lies as [n][r][N] (r_minor = 0) or [n][N][r].  Bound by reading the
+// factors and, of many tokens, base and Y.
 struct ExpandArgs {
-  const float* P;
+  const float* P;         // [splits][T][r]
   const void *F, *base;
   void* Y;
   const int* index;
   long long T;
-  int N, n, r, r_minor;
+  int N, n, r, r_minor, splits;
 };
-template <bool F32>
-__global__ void __launch_bounds__(THREADS) expand_kernel(const __grid_constant__ ExpandArgs a) {
-  __shared__ float p[MAX_RANK][GROUP];
+constexpr int EXPAND_THREADS = 128;
+template <bool F32, int G>
+__global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_constant__ ExpandArgs a) {
+  constexpr int V = VEC<F32>;
+  __shared__ float p[MAX_RANK][G];
   pdl_wait();
-  const long long t0 = static_cast<long long>(blockIdx.x) * GROUP;
-  const int count = a.T - t0 < GROUP ? static_cast<int>(a.T - t0) : GROUP, c = blockIdx.y * THREADS + threadIdx.x;
-  int of[GROUP];
+  const bool wide = (a.r_minor ? a.r : a.N) % V == 0;
+  const int step = wide && !a.r_minor ? V : 1;              // columns of a thread
+  const long long t0 = static_cast<long long>(blockIdx.x) * G;
+  const int count = a.T - t0 < G ? static_cast<int>(a.T - t0) : G, c = (blockIdx.y * EXPAND_THREADS + threadIdx.x) * step;
+  if (blockIdx.y * EXPAND_THREADS * step >= static_cast<unsigned>(a.N)) return;
+  int of[G];
 #pragma unroll
-  for (int g = 0; g < GROUP; ++g) of[g] = g < count ? adapter_of(a.index, t0 + g, a.n) : -1;
-  for (int e = threadIdx.x; e < GROUP * a.r; e += THREADS) {
+  for (int g = 0; g < G; ++g) of[g] = g < count ? adapter_of(a.index, t0 + g, a.n) : -1;
+  for (int e = threadIdx.x; e < G * a.r; e += EXPAND_THREADS) {
     const int g = e / a.r, j = e - g * a.r;
-    p[j][g] = g < count && adapter_of(a.index, t0 + g, a.n) >= 0 ? __ldcg(a.P + (t0 + g) * a.r + j) : 0.f;
+    float s = 0.f;
+    if (g < count && adapter_of(a.index, t0 + g, a.n) >= 0) {
+#pragma unroll 8
+      for (int k = 0; k < a.splits; ++k) s += __ldcg(a.P + (k * a.T + t0 + g) * a.r + j);
+    }
+    p[j][g] = s;
   }
   __syncthreads();
   if (c >= a.N) return;
-  float acc[GROUP] = {};
+  float acc[V][G];
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int g = 0; g < G; ++g) acc[v][g] = 0.f;
   for (int first = 0; first < count; ++first) {
-    const int i = of[first];
+    int i = -1;
     unsigned mask = 0;
 #pragma unroll
-    for (int g = 0; g < GROUP; ++g) mask |= of[g] == i ? 1u << g : 0u;
+    for (int g = 0; g < G; ++g) if (g == first) i = of[g];
+#pragma unroll
+    for (int g = 0; g < G; ++g) mask |= of[g] == i ? 1u << g : 0u;
     if (i < 0 || (mask & ((1u << first) - 1u))) continue;
     const long long f0 = static_cast<long long>(i) * a.N * a.r;
-    for (int j = 0; j < a.r; ++j) {
-      const float f = load<F32>(a.F, f0 + (a.r_minor ? static_cast<long long>(c) * a.r + j : static_cast<long long>(j) * a.N + c));
+    if (a.r_minor) {
+      const long long at = f0 + static_cast<long long>(c) * a.r;
+      if (wide) {
+#pragma unroll 2
+        for (int j = 0; j < a.r; j += V) {
+          float f[V];
+          load_vec<F32>(a.F, at + j, f);
 #pragma unroll
-      for (int g = 0; g < GROUP; ++g) if (mask >> g & 1u) acc[g] = fmaf(p[j][g], f, acc[g]);
+          for (int g = 0; g < G; ++g)
+            if (mask >> g & 1u)
+#pragma unroll
+              for (int v = 0; v < V; ++v) acc[0][g] = fmaf(p[j + v][g], f[v], acc[0][g]);
+        }
+      } else {
+#pragma unroll 4
+        for (int j = 0; j < a.r; ++j) {
+          const float f = load<F32>(a.F, at + j);
+#pragma unroll
+          for (int g = 0; g < G; ++g) if (mask >> g & 1u) acc[0][g] = fmaf(p[j][g], f, acc[0][g]);
+        }
+      }
+    } else if (wide) {
+#pragma unroll 8
+      for (int j = 0; j < a.r; ++j) {
+        float f[V];
+        load_vec<F32>(a.F, f0 + static_cast<long long>(j) * a.N + c, f);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+          if (mask >> g & 1u)
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[v][g] = fmaf(p[j][g], f[v], acc[v][g]);
+      }
+    } else {
+#pragma unroll 8
+      for (int j = 0; j < a.r; ++j) {
+        const float f = load<F32>(a.F, f0 + static_cast<long long>(j) * a.N + c);
+#pragma unroll
+        for (int g = 0; g < G; ++g) if (mask >> g & 1u) acc[0][g] = fmaf(p[j][g], f, acc[0][g]);
+      }
     }
   }
 #pragma unroll
-  for (int g = 0; g < GROUP; ++g) {
+  for (int g = 0; g < G; ++g) {
     if (g >= count) break;
+    if (of[g] < 0 && a.base == a.Y) continue;
     const long long at = (t0 + g) * a.N + c;
-    store<F32>(a.Y, at, a.base ? (F32 ? static_cast<const float*>(a.base)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(a.base)[at])) + acc[g] : acc[g]);
+    if (step > 1) {      // (then c + V <= N)
+      float b[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) b[v] = 0.f;
+      if constexpr (F32) {
+        if (a.base) {
+          const float4 q = *reinterpret_cast<const float4*>(static_cast<const float*>(a.base) + at);
+          b[0] = q.x; b[1] = q.y; b[2] = q.z; b[3] = q.w;
+        }
+        *reinterpret_cast<float4*>(static_cast<float*>(a.Y) + at) = make_float4(b[0] + acc[0][g], b[1] + acc[1][g], b[2] + acc[2][g], b[3] + acc[3][g]);
+      } else {
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        if (a.base) {
+          const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.base) + at);
+          w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = pack_bf16x2(__uint_as_float(w[k] << 16) + acc[2 * k][g], __uint_as_float(w[k] & 0xffff0000u) + acc[2 * k + 1][g]);
+        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.Y) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    } else {
+      const float b = !a.base ? 0.f : F32 ? static_cast<const float*>(a.base)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(a.base)[at]);
+      store<F32>(a.Y, at, b + acc[0][g]);
+    }
   }
 }
 
@@ -178,7 +326,7 @@ struct GradArgs {
   GradJob job[2];
   const int* index;
   long long T;
-  int n, r;
+  int n, r, splits;
 };
 constexpr int GRAD_COLS = 32, GRAD_TOKENS = 32;
 template <bool F32>
@@ -208,7 +356,10 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant
       const int m = all - b < GRAD_TOKENS ? all - b : GRAD_TOKENS;
       for (int e = threadIdx.x; e < m * a.r; e += THREADS) {
         const int q = e / a.r, j = e - q * a.r;
-        p[q][j] = __ldcg(job.P + (t0 + list[b + q]) * a.r + j);
+        float s = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < a.splits; ++k) s += __ldcg(job.P + (k * a.T + t0 + list[b + q]) * a.r + j);
+        p[q][j] = s;
       }
       for (int e = threadIdx.x; e < m * GRAD_COLS; e += THREADS) {
         const int q = e / GRAD_COLS, c = e % GRAD_COLS;
@@ -244,6 +395,19 @@ bool on_tensor_cores(const ffsplit_projection& p, int n, long long T) {
   return p.dtype == FFSPLIT_BF16 && T > adapter::FEW && adapter::tile_bound(T, n) <= 65535;
 }
 
+// Ranges of K of the products on the CUDA cores: as many blocks as SMs twice over, 64 elements each at least.
+int tokens_per_block(const ffsplit_projection& p, int n, long long T) {
+  if (T > adapter::FEW) return p.dtype == FFSPLIT_F32 ? adapter::MANY : adapter::SOME;      // (bf16: 65000 adapters and more)
+  return n == 1 ? adapter::SOME : 1;
+}
+int splits_of(const ffsplit_projection& p, int n, long long T) {
+  const int group = tokens_per_block(p, n, T), K = p.in > p.out ? p.in : p.out;
+  const long long blocks = (T + group - 1) / group;
+  long long s = (2 * 148 + blocks - 1) / blocks;
+  if (s > K / 64) s = K / 64;
+  return static_cast<int>(s < 1 ? 1 : s > adapter::MAX_SPLITS ? adapter::MAX_SPLITS : s);
+}
+
 struct AdapterLayout {
   long long ldi, ldo, ldr;
   size_t P, D, sorted, X, dY, W, A, B, parts, parts_bytes, end;
@@ -257,7 +421,7 @@ AdapterLayout adapter_layout(const ffsplit_projection& p, int n, int r, long lon
   L.ldr = round_up_ll(r, 8);
   size_t off = 0;
   const auto take = [&](size_t* at, size_t bytes) { *at = off; off = up256(off + bytes); };
-  const size_t inner = tc ? static_cast<size_t>(adapter::tile_bound(T, n)) * adapter::TOKENS * adapter::rank_pitch(r) * 2 : static_cast<size_t>(T) * r * 4;
+  const size_t inner = tc ? static_cast<size_t>(adapter::tile_bound(T, n)) * adapter::TOKENS * adapter::rank_pitch(r) * 2 : static_cast<size_t>(splits_of(p, n, T)) * T * r * 4;
   take(&L.P, inner);
   take(&L.D, inner);
   take(&L.sorted, tc ? (static_cast<size_t>(T) + 2 * (static_cast<size_t>(n) + 1)) * 4 : 0);
@@ -346,26 +510,46 @@ struct Call {
     g.b_mn = transposed ? 0 : 1;
     g.M = T; g.N = transposed ? p.in : p.out; g.K = transposed ? p.out : p.in;
     g.C = C; g.ldc = g.N; g.bias = bias;
+    g.b_ready = 1;      // (the launch before is a shrink: W, or its copy, is complete)
     return tg::launch(ctx, tg::PLAIN, 0, f32, &g, 1, tg::Hidden{}, ws + L.parts, L.parts_bytes, st);
   }
 };
 
-ffsplit_status launch_shrink(ffsplit_ctx* ctx, bool f32, adapter::ShrinkArgs& s, int jobs, const ffsplit_adapters& a, long long T, cudaStream_t st) {
-  s.index = a.index; s.scale = a.scale; s.T = T; s.n = a.n; s.r = a.r; s.status = ctx->status();
-  s.lanes = 1;
-  while (s.lanes < a.r) s.lanes *= 2;
-  const dim3 grid(static_cast<unsigned>((T + adapter::GROUP - 1) / adapter::GROUP), jobs);
-  const cudaError_t e = f32 ? launch_pdl(adapter::shrink_kernel<true>, grid, dim3(adapter::THREADS), 0, st, s)
-                            : launch_pdl(adapter::shrink_kernel<false>, grid, dim3(adapter::THREADS), 0, st, s);
-  ctx->launches++;
-  return check_cuda(ctx, e, "adapter::shrink_kernel launch");
+template <int G>
+ffsplit_status launch_shrink_g(const Call& c, const adapter::ShrinkArgs& s, int jobs) {
+  const dim3 grid(static_cast<unsigned>((c.T + G - 1) / G), jobs, s.splits);
+  constexpr int G16 = G < adapter::MANY ? G : adapter::SOME;
+  const cudaError_t e = c.f32 ? launch_pdl(adapter::shrink_kernel<true, G>, grid, dim3(adapter::THREADS), 0, c.st, s)
+                              : launch_pdl(adapter::shrink_kernel<false, G16>, grid, dim3(adapter::THREADS), 0, c.st, s);
+  c.ctx->launches++;
+  return check_cuda(c.ctx, e, "adapter::shrink_kernel launch");
 }
-ffsplit_status launch_expand(ffsplit_ctx* ctx, bool f32, const adapter::ExpandArgs& x, cudaStream_t st) {
-  const dim3 grid(static_cast<unsigned>((x.T + adapter::GROUP - 1) / adapter::GROUP), (x.N + adapter::THREADS - 1) / adapter::THREADS);
-  const cudaError_t e = f32 ? launch_pdl(adapter::expand_kernel<true>, grid, dim3(adapter::THREADS), 0, st, x)
-                            : launch_pdl(adapter::expand_kernel<false>, grid, dim3(adapter::THREADS), 0, st, x);
-  ctx->launches++;
-  return check_cuda(ctx, e, "adapter::expand_kernel launch");
+ffsplit_status launch_shrink(const Call& c, adapter::ShrinkArgs& s, int jobs) {
+  s.index = c.a.index; s.scale = c.a.scale; s.T = c.T; s.n = c.a.n; s.r = c.a.r; s.status = c.ctx->status();
+  s.splits = splits_of(c.p, c.a.n, c.T);
+  switch (tokens_per_block(c.p, c.a.n, c.T)) {
+    case adapter::MANY: return launch_shrink_g<adapter::MANY>(c, s, jobs);
+    case adapter::SOME: return launch_shrink_g<adapter::SOME>(c, s, jobs);
+    default: return launch_shrink_g<1>(c, s, jobs);
+  }
+}
+template <int G>
+ffsplit_status launch_expand_g(const Call& c, const adapter::ExpandArgs& x) {
+  const int vec = c.f32 ? adapter::VEC<true> : adapter::VEC<false>, step = !x.r_minor && x.N % vec == 0 ? vec : 1;
+  const dim3 grid(static_cast<unsigned>((x.T + G - 1) / G), (x.N + adapter::EXPAND_THREADS * step - 1) / (adapter::EXPAND_THREADS * step));
+  constexpr int G16 = G < adapter::MANY ? G : adapter::SOME;
+  const cudaError_t e = c.f32 ? launch_pdl(adapter::expand_kernel<true, G>, grid, dim3(adapter::EXPAND_THREADS), 0, c.st, x)
+                              : launch_pdl(adapter::expand_kernel<false, G16>, grid, dim3(adapter::EXPAND_THREADS), 0, c.st, x);
+  c.ctx->launches++;
+  return check_cuda(c.ctx, e, "adapter::expand_kernel launch");
+}
+ffsplit_status launch_expand(const Call& c, const float* P, const void* F, const void* base, void* Y, int N, int r_minor) {
+  const adapter::ExpandArgs x = {P, F, base, Y, c.a.index, c.T, N, c.a.n, c.a.r, r_minor, splits_of(c.p, c.a.n, c.T)};
+  switch (tokens_per_block(c.p, c.a.n, c.T)) {
+    case adapter::MANY: return launch_expand_g<adapter::MANY>(c, x);
+    case adapter::SOME: return launch_expand_g<adapter::SOME>(c, x);
+    default: return launch_expand_g<1>(c, x);
+  }
 }
 
 }  // namespace
@@ -406,11 +590,11 @@ ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projectio
     adapter::ShrinkArgs sh;
     std::memset(&sh, 0, sizeof(sh));
     sh.job[0] = {X, adapters->A, c.inner(c.L.P), c.p.in, 0};
-    if ((s = launch_shrink(ctx, c.f32, sh, 1, c.a, T, c.st)) != FFSPLIT_OK) return s;
+    if ((s = launch_shrink(c, sh, 1)) != FFSPLIT_OK) return s;
   }
   if (W && (s = c.shared_product(c.X, bias, false, Y)) != FFSPLIT_OK) return s;
   if (c.tc) return adapter::launch_expand_tc(ctx, c.tiles(c.L.P), c.B, c.p.out, W ? Y : base, Y, c.sorted, c.a.r, c.st);
-  return launch_expand(ctx, c.f32, {c.inner(c.L.P), adapters->B, W ? Y : base, Y, adapters->index, T, c.p.out, c.a.n, c.a.r, 0}, c.st);
+  return launch_expand(c, c.inner(c.L.P), adapters->B, W ? Y : base, Y, c.p.out, 0);
 }
 
 ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W, const void* base,
@@ -445,13 +629,13 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
     std::memset(&sh, 0, sizeof(sh));
     if (dX || dA) sh.job[n++] = {dY, adapters->B, c.inner(c.L.D), c.p.out, 1};
     if (dB) sh.job[n++] = {X, adapters->A, c.inner(c.L.P), c.p.in, 0};
-    if ((s = launch_shrink(ctx, c.f32, sh, n, c.a, T, c.st)) != FFSPLIT_OK) return s;
+    if ((s = launch_shrink(c, sh, n)) != FFSPLIT_OK) return s;
   }
   if (dX) {
     if (W && (s = c.shared_product(c.dY, nullptr, true, grads->dX)) != FFSPLIT_OK) return s;
     const void* add = W ? grads->dX : base;
     s = c.tc ? adapter::launch_expand_tc(ctx, c.tiles(c.L.D), c.A, c.p.in, add, grads->dX, c.sorted, c.a.r, c.st)
-             : launch_expand(ctx, c.f32, {c.inner(c.L.D), adapters->A, add, grads->dX, adapters->index, T, c.p.in, c.a.n, c.a.r, 1}, c.st);
+             : launch_expand(c, c.inner(c.L.D), adapters->A, add, grads->dX, c.p.in, 1);
     if (s != FFSPLIT_OK) return s;
   }
   if (!dA && !dB) return FFSPLIT_OK;
@@ -467,7 +651,7 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
   n = 0;
   if (dA) g.job[n++] = {c.inner(c.L.D), X, grads->dA, c.p.in, 1, (c.p.in + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
   if (dB) g.job[n++] = {c.inner(c.L.P), dY, grads->dB, c.p.out, 0, (c.p.out + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
-  g.index = adapters->index; g.T = T; g.n = c.a.n; g.r = c.a.r;
+  g.index = adapters->index; g.T = T; g.n = c.a.n; g.r = c.a.r; g.splits = splits_of(c.p, c.a.n, T);
   const dim3 grid(g.job[0].blocks + g.job[1].blocks, c.a.n);
   const cudaError_t e = c.f32 ? launch_pdl(adapter::gradient_kernel<true>, grid, dim3(adapter::THREADS), 0, c.st, g)
                               : launch_pdl(adapter::gradient_kernel<false>, grid, dim3(adapter::THREADS), 0, c.st, g);

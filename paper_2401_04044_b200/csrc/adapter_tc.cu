@@ -27,20 +27,20 @@ constexpr int BLOCK_K = 64, BLOCK64_BYTES = 64 * BLOCK_K * 2;
 constexpr int A_BYTES = TOKENS * BLOCK_K * 2, B_BYTES = MAX_RANK * BLOCK_K * 2;
 
 // ---------------------------------------------------------------------------------------------- sorting
-// A warp to a group: one pass counts its tokens and those of the groups before it, another writes them.
-__global__ void __launch_bounds__(256) sort_kernel(const int* __restrict__ index, Sorted s, int* status) {
+// A block to a group: one pass counts its tokens and those of the groups before it, another writes them in their order.
+constexpr int SORT_THREADS = 256, SORT_FLIGHT = 4;
+__global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const int* __restrict__ index, Sorted s, int* status) {
+  __shared__ int red[2][SORT_THREADS / 32], found[SORT_FLIGHT][SORT_THREADS / 32];
   pdl_wait();
-  const int g = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (g > s.n) return;
-  constexpr int FLIGHT = 8;
+  const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const auto group_of = [&](int i) { return i < 0 || i >= s.n ? s.n : i; };
   int mine = 0, before = 0;
-  for (long long t0 = lane; t0 < s.T; t0 += 32 * FLIGHT) {
-    int v[FLIGHT];
+  for (long long t0 = threadIdx.x; t0 < s.T; t0 += SORT_THREADS * SORT_FLIGHT) {
+    int v[SORT_FLIGHT];
 #pragma unroll
-    for (int k = 0; k < FLIGHT; ++k) v[k] = t0 + 32 * k < s.T ? group_of(__ldg(index + t0 + 32 * k)) : s.n + 1;
+    for (int k = 0; k < SORT_FLIGHT; ++k) v[k] = t0 + SORT_THREADS * k < s.T ? group_of(__ldg(index + t0 + SORT_THREADS * k)) : s.n + 1;
 #pragma unroll
-    for (int k = 0; k < FLIGHT; ++k) {
+    for (int k = 0; k < SORT_FLIGHT; ++k) {
       mine += v[k] == g;
       before += v[k] < g;
     }
@@ -50,24 +50,45 @@ __global__ void __launch_bounds__(256) sort_kernel(const int* __restrict__ index
     mine += __shfl_xor_sync(0xffffffffu, mine, o);
     before += __shfl_xor_sync(0xffffffffu, before, o);
   }
-  if (lane == 0) {
+  if (lane == 0) { red[0][warp] = mine; red[1][warp] = before; }
+  __syncthreads();
+  mine = before = 0;
+#pragma unroll
+  for (int w = 0; w < SORT_THREADS / 32; ++w) { mine += red[0][w]; before += red[1][w]; }
+  if (threadIdx.x == 0) {
     s.count[g] = mine;
     s.offset[g] = before;
   }
   if (mine == 0) return;
   int at = before;
-  for (long long t0 = 0; t0 < s.T; t0 += 32 * FLIGHT) {
-    int v[FLIGHT];
+  for (long long t0 = 0; t0 < s.T; t0 += SORT_THREADS * SORT_FLIGHT) {
+    unsigned votes[SORT_FLIGHT];
+    bool hit[SORT_FLIGHT];
 #pragma unroll
-    for (int k = 0; k < FLIGHT; ++k) v[k] = t0 + 32 * k + lane < s.T ? __ldg(index + t0 + 32 * k + lane) : 0;
-#pragma unroll
-    for (int k = 0; k < FLIGHT; ++k) {
-      const bool hit = t0 + 32 * k + lane < s.T && group_of(v[k]) == g;
-      const unsigned votes = __ballot_sync(0xffffffffu, hit);
-      if (hit) s.order[at + __popc(votes & ((1u << lane) - 1u))] = static_cast<int>(t0 + 32 * k + lane);
-      at += __popc(votes);
-      if (g == s.n && hit && v[k] >= s.n) record_status(status, FFSPLIT_ERR_BAD_INDEX, static_cast<int>(t0 + 32 * k + lane), KID_ADAPTER);
+    for (int k = 0; k < SORT_FLIGHT; ++k) {
+      const long long t = t0 + SORT_THREADS * k + threadIdx.x;
+      const int v = t < s.T ? __ldg(index + t) : 0;
+      hit[k] = t < s.T && group_of(v) == g;
+      if (hit[k] && v >= s.n) record_status(status, FFSPLIT_ERR_BAD_INDEX, static_cast<int>(t), KID_ADAPTER);
     }
+#pragma unroll
+    for (int k = 0; k < SORT_FLIGHT; ++k) {
+      votes[k] = __ballot_sync(0xffffffffu, hit[k]);
+      if (lane == 0) found[k][warp] = __popc(votes[k]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SORT_FLIGHT; ++k) {
+      int ahead = 0, all = 0;
+#pragma unroll
+      for (int w = 0; w < SORT_THREADS / 32; ++w) {
+        if (w < warp) ahead += found[k][w];
+        all += found[k][w];
+      }
+      if (hit[k]) s.order[at + ahead + __popc(votes[k] & ((1u << lane) - 1u))] = static_cast<int>(t0 + SORT_THREADS * k + threadIdx.x);
+      at += all;
+    }
+    __syncthreads();
   }
 }
 
@@ -118,10 +139,33 @@ __device__ __forceinline__ void load_3d(const CUtensorMap* tm, uint32_t smem_dst
                "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(x), "r"(y), "r"(z)
                : "memory");
 }
-// The places of four tokens of a tile in the batch; T (behind the last row) where there are fewer.
-__device__ __forceinline__ void four_tokens(const Sorted& s, int first, int rows, int r0, int* out) {
+// Sixteen tokens of a tile, as a lane loads them: where they lie one after the other as one box, else four to an
+// instruction (a gather takes the copy engine nearly as long for four rows as a box for sixteen: 1.4 us for 128 rows).
+constexpr int ROWS = 16;
+struct Rows {
+  int at[ROWS];
+  bool any, run;
+};
+__device__ __forceinline__ Rows rows_of(const Sorted& s, int first, int rows, int r0) {
+  Rows r;
+  r.any = r0 < rows;
+  r.run = r0 + ROWS <= rows;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) out[i] = r0 + i < rows ? __ldcg(s.order + first + r0 + i) : static_cast<int>(s.T);
+  for (int i = 0; i < ROWS; ++i) r.at[i] = r0 + i < rows ? __ldcg(s.order + first + r0 + i) : static_cast<int>(s.T);      // T: behind the last row
+#pragma unroll
+  for (int i = 1; i < ROWS; ++i) r.run = r.run && r.at[i] == r.at[0] + i;
+  return r;
+}
+// 64 columns from x on of the rows to smem_dst, 128 bytes each.
+__device__ __forceinline__ void load_rows(const CUtensorMap* box, const CUtensorMap* gather, uint32_t smem_dst, uint32_t bar, int x, const Rows& r) {
+  if (r.run) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_dst),
+                 "l"(reinterpret_cast<uint64_t>(box)), "r"(bar), "r"(x), "r"(r.at[0])
+                 : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < ROWS; i += 4) gather4(gather, smem_dst + i * 128, bar, x, r.at + i);
+  }
 }
 
 // What the three kernels share: barriers, tensor memory, and the way out.
@@ -195,7 +239,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
 
 // ---------------------------------------------------------------------------------------------- shrink
 struct ShrinkDev {
-  CUtensorMap V, F;
+  CUtensorMap V, V_box, F;
   __nv_bfloat16* P;
   int kb, f_mn;               // f_mn: the rank runs along memory
 };
@@ -225,11 +269,10 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
   float* part = reinterpret_cast<float*>(smem);
   const int part_pitch = p.cols + 4;
   if (warp == COPY_WARP) {
-    int rows[4];
-    four_tokens(p.s, tile.first, tile.rows, lane * 4, rows);
-    const bool has = lane * 4 < tile.rows;
+    const Rows rows = rows_of(p.s, tile.first, tile.rows, (lane & 7) * ROWS);
+    const bool has = lane < 8 && rows.any;
     // the factor's box: 64 k x 64 ranks, one or two of them; or all ranks (as many rows as there are columns of the tile) x 64 k
-    const uint32_t tx = static_cast<uint32_t>((tile.rows + 3) / 4 * 512 + (job.f_mn ? (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES : p.cols * BLOCK_K * 2));
+    const uint32_t tx = static_cast<uint32_t>((tile.rows + ROWS - 1) / ROWS * (ROWS * 128) + (job.f_mn ? (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES : p.cols * BLOCK_K * 2));
     bool ok = true;
     for (int kb = k0, i = 0; kb < k1; ++kb, ++i) {
       const int s = i % SHRINK_STAGES;
@@ -246,7 +289,7 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
         }
       }
       __syncwarp();
-      if (has) gather4(&job.V, to + lane * 512, bar, kb * BLOCK_K, rows);
+      if (has) load_rows(&job.V_box, &job.V, to + lane * (ROWS * 128), bar, kb * BLOCK_K, rows);
     }
     if (!ok) copies_gave_up();
     __syncwarp();
@@ -374,11 +417,18 @@ __global__ void __launch_bounds__(TC_THREADS) expand_tc_kernel(const __grid_cons
     const int row = warp * 32 + lane, width = p.N - n0 < EXPAND_COLS ? p.N - n0 : EXPAND_COLS;
     const bool in = row < tile.rows;
     const long long at = in ? static_cast<long long>(__ldcg(p.s.order + tile.first + row)) * p.N + n0 : 0;
+    // the whole of base is on its way before the product is complete
+    constexpr int PIECES = EXPAND_COLS / 8;
+    uint4 base[PIECES];
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k)
+      base[k] = p.wide && p.base && in && k * 8 < width ? *reinterpret_cast<const uint4*>(p.base + at + 8 * k) : make_uint4(0u, 0u, 0u, 0u);
     const bool ready = none || ptx::mbar_wait(f.done, 0, f.abort_flag);
     if (ready && warp * 32 < tile.rows) {
       ptx::tc_fence_after();
-#pragma unroll 2
-      for (int c = 0; c < width; c += 16) {
+#pragma unroll
+      for (int k = 0; k < PIECES; k += 2) {
+        const int c = 8 * k;
         float v[16];
         if (none) {
 #pragma unroll
@@ -390,26 +440,18 @@ __global__ void __launch_bounds__(TC_THREADS) expand_tc_kernel(const __grid_cons
         if (in && p.wide) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            if (c + 8 * h >= width) break;
-            float* x = v + 8 * h;
-            if (p.base) {
-              const uint4 q = *reinterpret_cast<const uint4*>(p.base + at + c + 8 * h);
-              const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            const uint4 q = base[k + h];
+            const uint32_t b[4] = {q.x, q.y, q.z, q.w};
+            uint32_t w[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                x[2 * i] += __uint_as_float(w[i] << 16);
-                x[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
-              }
-            }
-            *reinterpret_cast<uint4*>(p.Y + at + c + 8 * h) =
-                make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+            for (int i = 0; i < 4; ++i)
+              w[i] = bf16_pair(__uint_as_float(b[i] << 16) + v[8 * h + 2 * i], __uint_as_float(b[i] & 0xffff0000u) + v[8 * h + 2 * i + 1]);
+            if (c + 8 * h < width) *reinterpret_cast<uint4*>(p.Y + at + c + 8 * h) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         } else if (in) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if (c + i >= width) break;
-            p.Y[at + c + i] = __float2bfloat16_rn(p.base ? __bfloat162float(p.base[at + c + i]) + v[i] : v[i]);
-          }
+          for (int i = 0; i < 16; ++i)
+            if (c + i < width) p.Y[at + c + i] = __float2bfloat16_rn(p.base ? __bfloat162float(p.base[at + c + i]) + v[i] : v[i]);
         }
         __syncwarp();
       }
@@ -421,7 +463,7 @@ __global__ void __launch_bounds__(TC_THREADS) expand_tc_kernel(const __grid_cons
 
 // ---------------------------------------------------------------------------------------------- gradients
 struct GradientDev {
-  CUtensorMap V, P;
+  CUtensorMap V, V_box, P;
   __nv_bfloat16* out;
   int N, rank_rows, blocks;
 };
@@ -450,8 +492,7 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
     bool ok = true;
     for (int k = 0; k < kb; ++k) {
       const int s = k % GRADIENT_STAGES;
-      int rows[4];
-      four_tokens(p.s, first + k * BLOCK_K, count - k * BLOCK_K, (lane & 15) * 4, rows);
+      const Rows rows = rows_of(p.s, first + k * BLOCK_K, count - k * BLOCK_K, (lane & 3) * ROWS);
       ok = ptx::mbar_wait_warp(&f.empty[s], ((k / GRADIENT_STAGES) & 1) ^ 1, f.abort_flag);
       if (!ok) break;
       const uint32_t to = f.smem0 + s * (A_BYTES + B_BYTES), bar = ptx::smem_u32(&f.full[s]);
@@ -461,7 +502,7 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
         if (p.cols > 64) load_3d(&job.P, to + A_BYTES + BLOCK64_BYTES, bar, 64, tile0 * TOKENS + k * BLOCK_K, 0);
       }
       __syncwarp();
-      gather4(&job.V, to + (lane >> 4) * BLOCK64_BYTES + (lane & 15) * 512, bar, c0 + (lane >> 4) * 64, rows);
+      if (lane < 8) load_rows(&job.V_box, &job.V, to + (lane >> 2) * BLOCK64_BYTES + (lane & 3) * (ROWS * 128), bar, c0 + (lane >> 2) * 64, rows);
     }
     if (!ok) copies_gave_up();
     __syncwarp();
@@ -551,7 +592,10 @@ ffsplit_status encode(ffsplit_ctx* ctx, const void* at, long long cols, long lon
   if (r != CUDA_SUCCESS) return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
   return FFSPLIT_OK;
 }
-ffsplit_status encode_gather(ffsplit_ctx* ctx, const tg::Matrix& m, CUtensorMap* out) { return encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, 1, out); }
+ffsplit_status encode_rows(ffsplit_ctx* ctx, const tg::Matrix& m, CUtensorMap* gather, CUtensorMap* box) {
+  const ffsplit_status s = encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, 1, gather);
+  return s != FFSPLIT_OK ? s : encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, ROWS, box);
+}
 ffsplit_status encode_factor(ffsplit_ctx* ctx, const Factor& f, int n, int box_rows, CUtensorMap* out) {
   return encode(ctx, f.m.p, f.cols, f.rows, n, f.m.ld, 3, box_rows, out);
 }
@@ -572,7 +616,7 @@ ffsplit_status set_up(ffsplit_ctx* ctx) {
 }  // namespace
 
 ffsplit_status launch_sort(ffsplit_ctx* ctx, const int* index, const Sorted& s, cudaStream_t st) {
-  const cudaError_t e = launch_pdl(sort_kernel, dim3((s.n + 8) / 8), dim3(256), 0, st, index, s, ctx->status());
+  const cudaError_t e = launch_pdl(sort_kernel, dim3(s.n + 1), dim3(SORT_THREADS), 0, st, index, s, ctx->status());
   ctx->launches++;
   return check_cuda(ctx, e, "adapter::sort_kernel launch");
 }
@@ -586,7 +630,7 @@ ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, con
   int kb = 1;
   for (int i = 0; i < n; ++i) {
     ShrinkDev& d = p.job[i];
-    if ((rc = encode_gather(ctx, jobs[i].V, &d.V)) != FFSPLIT_OK) return rc;
+    if ((rc = encode_rows(ctx, jobs[i].V, &d.V, &d.V_box)) != FFSPLIT_OK) return rc;
     d.f_mn = jobs[i].F.rank_rows ? 0 : 1;
     if ((rc = encode_factor(ctx, jobs[i].F, s.n, d.f_mn ? BLOCK_K : p.cols, &d.F)) != FFSPLIT_OK) return rc;
     d.P = jobs[i].P;
@@ -643,7 +687,7 @@ ffsplit_status launch_gradients_tc(ffsplit_ctx* ctx, const Gradient* jobs, int n
   int blocks = 0;
   for (int i = 0; i < n; ++i) {
     GradientDev& d = p.job[i];
-    if ((rc = encode_gather(ctx, jobs[i].V, &d.V)) != FFSPLIT_OK) return rc;
+    if ((rc = encode_rows(ctx, jobs[i].V, &d.V, &d.V_box)) != FFSPLIT_OK) return rc;
     if ((rc = encode(ctx, jobs[i].P, rank_pitch(r), tile_bound(s.T, s.n) * TOKENS, 1, rank_pitch(r), 3, BLOCK_K, &d.P)) != FFSPLIT_OK) return rc;
     d.out = static_cast<__nv_bfloat16*>(jobs[i].out);
     d.N = jobs[i].N; d.rank_rows = jobs[i].rank_rows;
