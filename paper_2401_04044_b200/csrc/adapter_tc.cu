@@ -141,6 +141,7 @@ __device__ __forceinline__ void load_3d(const CUtensorMap* tm, uint32_t smem_dst
 }
 // Sixteen tokens of a tile, as a lane loads them: where they lie one after the other as one box, else four to an
 // instruction (a gather takes the copy engine nearly as long for four rows as a box for sixteen: 1.4 us for 128 rows).
+// Tokens of an adapter are in their order, so a stretch of them is a run if its ends are as far apart as it is long.
 constexpr int ROWS = 16;
 struct Rows {
   int at[ROWS];
@@ -150,18 +151,24 @@ __device__ __forceinline__ Rows rows_of(const Sorted& s, int first, int rows, in
   Rows r;
   r.any = r0 < rows;
   r.run = r0 + ROWS <= rows;
+  r.at[0] = r.any ? __ldcg(s.order + first + r0) : static_cast<int>(s.T);      // T: behind the last row
+  r.at[ROWS - 1] = r.run ? __ldcg(s.order + first + r0 + ROWS - 1) : static_cast<int>(s.T);
+  r.run = r.run && r.at[ROWS - 1] == r.at[0] + ROWS - 1;
+  if (r.any && !r.run) {
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) r.at[i] = r0 + i < rows ? __ldcg(s.order + first + r0 + i) : static_cast<int>(s.T);      // T: behind the last row
-#pragma unroll
-  for (int i = 1; i < ROWS; ++i) r.run = r.run && r.at[i] == r.at[0] + i;
+    for (int i = 1; i < ROWS; ++i) r.at[i] = r0 + i < rows ? __ldcg(s.order + first + r0 + i) : static_cast<int>(s.T);
+  }
   return r;
 }
-// 64 columns from x on of the rows to smem_dst, 128 bytes each.
+__device__ __forceinline__ void load_2d(const CUtensorMap* tm, uint32_t smem_dst, uint32_t bar, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_dst),
+               "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(x), "r"(y)
+               : "memory");
+}
+// 64 columns from x on of the rows to smem_dst, 128 bytes each (without any: zeros).
 __device__ __forceinline__ void load_rows(const CUtensorMap* box, const CUtensorMap* gather, uint32_t smem_dst, uint32_t bar, int x, const Rows& r) {
-  if (r.run) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_dst),
-                 "l"(reinterpret_cast<uint64_t>(box)), "r"(bar), "r"(x), "r"(r.at[0])
-                 : "memory");
+  if (r.run || !r.any) {
+    load_2d(box, smem_dst, bar, x, r.at[0]);
   } else {
 #pragma unroll
     for (int i = 0; i < ROWS; i += 4) gather4(gather, smem_dst + i * 128, bar, x, r.at + i);
@@ -171,12 +178,13 @@ __device__ __forceinline__ void load_rows(const CUtensorMap* box, const CUtensor
 // What the three kernels share: barriers, tensor memory, and the way out.
 struct Frame {
   uint32_t smem0;             // 1024-byte aligned
-  uint64_t *full, *empty, *done, *drain;
+  uint64_t *full, *empty, *done, *drain;      // (drain[1]: expand's epilogue warps -> MMA)
   uint32_t tmem;
   volatile int* abort_flag;
 };
 constexpr int FRAME_BYTES = 256, FRAME_STAGES = 8;
-__device__ __forceinline__ Frame frame_open(uint8_t* raw, int bytes, int stages, uint32_t tmem_cols) {
+template <int MMA = MMA_WARP>
+__device__ __forceinline__ Frame frame_open(uint8_t* raw, int bytes, int stages, uint32_t tmem_cols, int drain_count = 1) {
   Frame f;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   f.smem0 = ptx::smem_u32(smem);
@@ -184,7 +192,7 @@ __device__ __forceinline__ Frame frame_open(uint8_t* raw, int bytes, int stages,
   f.empty = f.full + FRAME_STAGES;
   f.done = f.empty + FRAME_STAGES;
   f.drain = f.done + 1;
-  uint32_t* holder = reinterpret_cast<uint32_t*>(f.drain + 1);
+  uint32_t* holder = reinterpret_cast<uint32_t*>(f.drain + 2);
   f.abort_flag = reinterpret_cast<volatile int*>(holder + 1);
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
@@ -193,10 +201,11 @@ __device__ __forceinline__ Frame frame_open(uint8_t* raw, int bytes, int stages,
     }
     ptx::mbar_init(f.done, 1);
     ptx::mbar_init(f.drain, 1);
+    ptx::mbar_init(f.drain + 1, drain_count);
     *f.abort_flag = 0;
     ptx::mbar_fence_init();
   }
-  if (threadIdx.x >> 5 == MMA_WARP) {
+  if (threadIdx.x >> 5 == MMA) {
     ptx::tmem_alloc(holder, tmem_cols);
     ptx::tmem_relinquish();
   }
@@ -219,11 +228,12 @@ __device__ __forceinline__ void copies_gave_up() {
   const long long t0 = clock64();
   while (clock64() - t0 < ptx::kWaitLimitCycles / 64) {}
 }
+template <int MMA = MMA_WARP>
 __device__ __forceinline__ void frame_close(const Frame& f, uint32_t tmem_cols, int* status) {
   ptx::tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *f.abort_flag) record_status(status, FFSPLIT_ERR_TIMEOUT, blockIdx.x, KID_ADAPTER);
-  if (threadIdx.x >> 5 == MMA_WARP) {
+  if (threadIdx.x >> 5 == MMA) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(f.tmem, tmem_cols);
   }
@@ -239,7 +249,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
 
 // ---------------------------------------------------------------------------------------------- shrink
 struct ShrinkDev {
-  CUtensorMap V, V_box, F;
+  CUtensorMap V, V_box, V_tile, F;
   __nv_bfloat16* P;
   int kb, f_mn;               // f_mn: the rank runs along memory
 };
@@ -248,12 +258,15 @@ struct ShrinkParams {
   Sorted s;
   const float* scale;
   int r, cols, pitch;         // cols: r rounded up to 16
+  int stage;                  // bytes: the rows and 64 or 128 ranks
   int* status;
 };
-constexpr int SHRINK_STAGES = 4, SHRINK_RING = SHRINK_STAGES * (A_BYTES + B_BYTES);
-constexpr int SHRINK_SMEM = 1024 + SHRINK_RING + FRAME_BYTES;
+constexpr int SHRINK_STAGES = 4;
 constexpr uint32_t SHRINK_TMEM = 128;
-static_assert(SHRINK_RING >= TOKENS * (MAX_RANK + 4) * 4, "the partial sums take the place of the ring");
+static_assert(SHRINK_STAGES * (A_BYTES + B_BYTES / 2) >= TOKENS * (MAX_RANK / 2 + 4) * 4 && SHRINK_STAGES * (A_BYTES + B_BYTES) >= TOKENS * (MAX_RANK + 4) * 4,
+              "the partial sums take the place of the ring");
+
+constexpr int MAX_RANGES = 8;
 
 __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_constant__ ShrinkParams p) {
   extern __shared__ uint8_t raw[];
@@ -262,23 +275,27 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
   const int ranges = gridDim.x, range = blockIdx.x;         // a cluster spans x
   const Tile tile = find_tile(p.s, p.s.n, blockIdx.y);
   if (tile.group < 0) return;                               // (the whole cluster)
-  const Frame f = frame_open(raw, SHRINK_RING, SHRINK_STAGES, SHRINK_TMEM);
+  const Frame f = frame_open(raw, SHRINK_STAGES * p.stage, SHRINK_STAGES, SHRINK_TMEM);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int per = (job.kb + ranges - 1) / ranges, k0 = range * per, k1 = k0 + per < job.kb ? k0 + per : job.kb;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   float* part = reinterpret_cast<float*>(smem);
   const int part_pitch = p.cols + 4;
   if (warp == COPY_WARP) {
-    const Rows rows = rows_of(p.s, tile.first, tile.rows, (lane & 7) * ROWS);
-    const bool has = lane < 8 && rows.any;
+    // a tile that is one run: one box (rows behind its last token are other tokens', and their sums are not written)
+    const int top = __ldcg(p.s.order + tile.first);
+    const bool whole = __ldcg(p.s.order + tile.first + tile.rows - 1) - top == tile.rows - 1;
+    Rows rows;
+    if (!whole) rows = rows_of(p.s, tile.first, tile.rows, (lane & 7) * ROWS);
+    const bool has = whole ? lane == 0 : lane < 8 && rows.any;
     // the factor's box: 64 k x 64 ranks, one or two of them; or all ranks (as many rows as there are columns of the tile) x 64 k
-    const uint32_t tx = static_cast<uint32_t>((tile.rows + ROWS - 1) / ROWS * (ROWS * 128) + (job.f_mn ? (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES : p.cols * BLOCK_K * 2));
+    const uint32_t tx = static_cast<uint32_t>((whole ? A_BYTES : (tile.rows + ROWS - 1) / ROWS * (ROWS * 128)) + (job.f_mn ? (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES : p.cols * BLOCK_K * 2));
     bool ok = true;
     for (int kb = k0, i = 0; kb < k1; ++kb, ++i) {
       const int s = i % SHRINK_STAGES;
       ok = ptx::mbar_wait_warp(&f.empty[s], ((i / SHRINK_STAGES) & 1) ^ 1, f.abort_flag);
       if (!ok) break;
-      const uint32_t to = f.smem0 + s * (A_BYTES + B_BYTES), bar = ptx::smem_u32(&f.full[s]);
+      const uint32_t to = f.smem0 + s * p.stage, bar = ptx::smem_u32(&f.full[s]);
       if (lane == 0) {
         ptx::mbar_expect_tx(&f.full[s], tx);
         if (job.f_mn) {
@@ -289,7 +306,10 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
         }
       }
       __syncwarp();
-      if (has) load_rows(&job.V_box, &job.V, to + lane * (ROWS * 128), bar, kb * BLOCK_K, rows);
+      if (has) {
+        if (whole) load_2d(&job.V_tile, to, bar, kb * BLOCK_K, top);
+        else load_rows(&job.V_box, &job.V, to + lane * (ROWS * 128), bar, kb * BLOCK_K, rows);
+      }
     }
     if (!ok) copies_gave_up();
     __syncwarp();
@@ -301,7 +321,7 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
       ok = ptx::mbar_wait_warp(&f.full[s], (i / SHRINK_STAGES) & 1, f.abort_flag);
       if (!ok) break;
       ptx::tc_fence_after();
-      const uint32_t at = f.smem0 + s * (A_BYTES + B_BYTES);
+      const uint32_t at = f.smem0 + s * p.stage;
       if (ptx::elect_one()) {
         issue(f.tmem, ptx::umma_desc_k128(at), 32 >> 4, job.f_mn ? ptx::umma_desc_mn128(at + A_BYTES, BLOCK64_BYTES) : ptx::umma_desc_k128(at + A_BYTES),
               job.f_mn ? 2048 >> 4 : 32 >> 4, idesc, BLOCK_K / 16, i == 0);
@@ -342,11 +362,15 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
     const int row = e / pairs, c = (e - row * pairs) * 2;
     float x = 0.f, y = 0.f;
     if (row < tile.rows) {
-      for (int k = 0; k < ranges; ++k) {
-        float a, b;
-        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(a), "=f"(b) : "r"(ptx::map_to_cta(part0 + (row * part_pitch + c) * 4, k)));
-        x += a; y += b;
+      // (all loads first: each is a trip to another SM)
+      float a[MAX_RANGES], b[MAX_RANGES];
+#pragma unroll
+      for (int k = 0; k < MAX_RANGES; ++k) {
+        a[k] = b[k] = 0.f;
+        if (k < ranges) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(a[k]), "=f"(b[k]) : "r"(ptx::map_to_cta(part0 + (row * part_pitch + c) * 4, k)));
       }
+#pragma unroll
+      for (int k = 0; k < MAX_RANGES; ++k) { x += a[k]; y += b[k]; }
     }
     *reinterpret_cast<uint32_t*>(P + static_cast<long long>(row) * p.pitch + c) = bf16_pair(scale * x, scale * y);
   }
@@ -360,110 +384,161 @@ struct ExpandParams {
   Sorted s;
   const __nv_bfloat16* base;
   __nv_bfloat16* Y;
-  int N, r, f_mn, wide;       // f_mn: the columns run along memory; wide: rows start on 16 bytes
+  int N, r, f_mn, wide;       // f_mn: the columns run along memory; wide: rows start on 8 bytes
+  int blocks;                 // k-blocks of the rank: 1 or 2
   int* status;
 };
-constexpr int EXPAND_COLS = 128;
-constexpr int EXPAND_BYTES = 2 * (A_BYTES + EXPAND_COLS * BLOCK_K * 2), EXPAND_SMEM = 1024 + EXPAND_BYTES + FRAME_BYTES;
+// A CTA keeps a tile's P and goes through every gridDim.x-th block of columns: the factor's next block is on its way while
+// one is added.  Two CTAs to an SM keep the loads of base going.
+constexpr int EXPAND_COLS = 128, EXPAND_F = EXPAND_COLS * BLOCK_K * 2;
+// eight epilogue warps: four quarters of the rows, two halves of the columns
+constexpr int EXPAND_WARPS = 8, EXPAND_COPY = 8, EXPAND_MMA = 9, EXPAND_TC_THREADS = 320;
+constexpr int TURN_PITCH = 36, TURN_BYTES = 32 * TURN_PITCH * 4 + 32 * 8;      // 32 columns of 32 rows, and where the rows lie
 constexpr uint32_t EXPAND_TMEM = 128;
 
-__global__ void __launch_bounds__(TC_THREADS) expand_tc_kernel(const __grid_constant__ ExpandParams p) {
+__global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const __grid_constant__ ExpandParams p) {
   extern __shared__ uint8_t raw[];
   pdl_wait();
   const Tile tile = find_tile(p.s, p.s.n + 1, blockIdx.y);
   if (tile.group < 0) return;
   const bool none = tile.group == p.s.n;
   if (none && p.base == p.Y) return;
-  const Frame f = frame_open(raw, EXPAND_BYTES, 1, EXPAND_TMEM);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n0 = blockIdx.x * EXPAND_COLS;
-  const int blocks = p.r > BLOCK_K ? 2 : 1;
+  const Frame f = frame_open<EXPAND_MMA>(raw, p.blocks * (A_BYTES + 2 * EXPAND_F), 3, EXPAND_TMEM, EXPAND_WARPS);     // (stages 0, 1: the factor, 2: P)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int all = (p.N + EXPAND_COLS - 1) / EXPAND_COLS;
+  const uint32_t factor0 = f.smem0 + p.blocks * A_BYTES;
   if (none) {
     // nothing to add
-  } else if (warp == COPY_WARP) {
-    if (ptx::elect_one()) {
-      ptx::mbar_expect_tx(&f.full[0], blocks * (A_BYTES + EXPAND_COLS * BLOCK_K * 2));
-      const uint32_t bar = ptx::smem_u32(&f.full[0]);
-      for (int b = 0; b < blocks; ++b) {
-        const uint32_t to = f.smem0 + b * (A_BYTES + EXPAND_COLS * BLOCK_K * 2);
-        load_3d(&p.P, to, bar, b * BLOCK_K, blockIdx.y * TOKENS, 0);
-        if (p.f_mn) {
-          load_3d(&p.F, to + A_BYTES, bar, n0, b * BLOCK_K, tile.group);
-          load_3d(&p.F, to + A_BYTES + BLOCK64_BYTES, bar, n0 + 64, b * BLOCK_K, tile.group);
-        } else {
-          load_3d(&p.F, to + A_BYTES, bar, b * BLOCK_K, n0, tile.group);
+  } else if (warp == EXPAND_COPY) {
+    bool ok = true;
+    for (int i = 0, cb = blockIdx.x; cb < all; cb += gridDim.x, ++i) {
+      const int s = i & 1;
+      ok = ptx::mbar_wait_warp(&f.empty[s], ((i >> 1) & 1) ^ 1, f.abort_flag);
+      if (!ok) break;
+      if (ptx::elect_one()) {
+        if (i == 0) {
+          ptx::mbar_expect_tx(&f.full[2], p.blocks * A_BYTES);
+          for (int b = 0; b < p.blocks; ++b) load_3d(&p.P, f.smem0 + b * A_BYTES, ptx::smem_u32(&f.full[2]), b * BLOCK_K, blockIdx.y * TOKENS, 0);
+        }
+        ptx::mbar_expect_tx(&f.full[s], p.blocks * EXPAND_F);
+        const uint32_t bar = ptx::smem_u32(&f.full[s]);
+        const int n0 = cb * EXPAND_COLS;
+        for (int b = 0; b < p.blocks; ++b) {
+          const uint32_t to = factor0 + (s * p.blocks + b) * EXPAND_F;
+          if (p.f_mn) {
+            load_3d(&p.F, to, bar, n0, b * BLOCK_K, tile.group);
+            load_3d(&p.F, to + BLOCK64_BYTES, bar, n0 + 64, b * BLOCK_K, tile.group);
+          } else {
+            load_3d(&p.F, to, bar, b * BLOCK_K, n0, tile.group);
+          }
         }
       }
+      __syncwarp();
     }
+    if (!ok) copies_gave_up();
     __syncwarp();
-  } else if (warp == MMA_WARP) {
+  } else if (warp == EXPAND_MMA) {
     const uint32_t idesc = ptx::umma_idesc_bf16(TOKENS, EXPAND_COLS) | (p.f_mn ? 1u << 16 : 0u);
-    if (ptx::mbar_wait_warp(&f.full[0], 0, f.abort_flag)) {
+    bool ok = ptx::mbar_wait_warp(&f.full[2], 0, f.abort_flag);
+    for (int i = 0, cb = blockIdx.x; cb < all && ok; cb += gridDim.x, ++i) {
+      const int s = i & 1;
+      ok = ptx::mbar_wait_warp(&f.full[s], (i >> 1) & 1, f.abort_flag) && ptx::mbar_wait_warp(f.drain + 1, (i & 1) ^ 1, f.abort_flag);
+      if (!ok) break;
       ptx::tc_fence_after();
       if (ptx::elect_one()) {
-        for (int b = 0; b < blocks; ++b) {
-          const uint32_t at = f.smem0 + b * (A_BYTES + EXPAND_COLS * BLOCK_K * 2);
+        for (int b = 0; b < p.blocks; ++b) {
+          const uint32_t at = factor0 + (s * p.blocks + b) * EXPAND_F;
           const int left = (p.r - b * BLOCK_K + 15) / 16;
-          issue(f.tmem, ptx::umma_desc_k128(at), 32 >> 4, p.f_mn ? ptx::umma_desc_mn128(at + A_BYTES, BLOCK64_BYTES) : ptx::umma_desc_k128(at + A_BYTES),
+          issue(f.tmem, ptx::umma_desc_k128(f.smem0 + b * A_BYTES), 32 >> 4, p.f_mn ? ptx::umma_desc_mn128(at, BLOCK64_BYTES) : ptx::umma_desc_k128(at),
                 p.f_mn ? 2048 >> 4 : 32 >> 4, idesc, left < 4 ? left : 4, b == 0);
         }
+        ptx::umma_commit(&f.empty[s]);
         ptx::umma_commit(f.done);
       }
       __syncwarp();
-    } else {
-      copies_gave_up();
     }
+    if (!ok) mma_gave_up(f);
   }
-  if (warp < 4) {
-    const int row = warp * 32 + lane, width = p.N - n0 < EXPAND_COLS ? p.N - n0 : EXPAND_COLS;
-    const bool in = row < tile.rows;
-    const long long at = in ? static_cast<long long>(__ldcg(p.s.order + tile.first + row)) * p.N + n0 : 0;
-    // the whole of base is on its way before the product is complete
-    constexpr int PIECES = EXPAND_COLS / 8;
-    uint4 base[PIECES];
+  if (warp < EXPAND_WARPS) {
+    // Rows of the tile lie anywhere in the batch: a warp goes along them, four rows of 32 columns to an instruction (with a row
+    // to a lane, as tensor memory has them, every load and store fell into 32 lines: 1.3 TB/s).  The sums change places
+    // through shared memory; base is on its way before they are complete.
+    const int quarter = warp & 3, half = warp >> 2;
+    const int rows = tile.rows - quarter * 32 < 32 ? tile.rows - quarter * 32 : 32;       // (may be negative)
+    uint8_t* area = raw + (f.smem0 - ptx::smem_u32(raw)) + p.blocks * (A_BYTES + 2 * EXPAND_F) + FRAME_BYTES + warp * TURN_BYTES;
+    float* turn = reinterpret_cast<float*>(area);
+    long long* row_at = reinterpret_cast<long long*>(area + 32 * TURN_PITCH * 4);
+    row_at[lane] = lane < rows ? static_cast<long long>(__ldcg(p.s.order + tile.first + quarter * 32 + lane)) * p.N : -1;
+    __syncwarp();
+    const int up = lane >> 3, col = (lane & 7) * 4;
+    for (int i = 0, cb = blockIdx.x; cb < all; cb += gridDim.x, ++i) {
+      const int c0 = cb * EXPAND_COLS + half * 64 + col;
+      uint2 base[2][8];
 #pragma unroll
-    for (int k = 0; k < PIECES; ++k)
-      base[k] = p.wide && p.base && in && k * 8 < width ? *reinterpret_cast<const uint4*>(p.base + at + 8 * k) : make_uint4(0u, 0u, 0u, 0u);
-    const bool ready = none || ptx::mbar_wait(f.done, 0, f.abort_flag);
-    if (ready && warp * 32 < tile.rows) {
+      for (int h = 0; h < 2; ++h) {
+        const int c = c0 + 32 * h;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const long long at = row_at[4 * k + up];
+          base[h][k] = make_uint2(0u, 0u);
+          if (p.base && at >= 0 && c < p.N) {
+            if (p.wide) {
+              base[h][k] = *reinterpret_cast<const uint2*>(p.base + at + c);
+            } else {
+              const unsigned short* q = reinterpret_cast<const unsigned short*>(p.base + at + c);
+              base[h][k].x = q[0] | (c + 1 < p.N ? static_cast<uint32_t>(q[1]) << 16 : 0u);
+              base[h][k].y = (c + 2 < p.N ? q[2] : 0u) | (c + 3 < p.N ? static_cast<uint32_t>(q[3]) << 16 : 0u);
+            }
+          }
+        }
+      }
+      if (!none && !ptx::mbar_wait(f.done, i & 1, f.abort_flag)) break;
       ptx::tc_fence_after();
 #pragma unroll
-      for (int k = 0; k < PIECES; k += 2) {
-        const int c = 8 * k;
-        float v[16];
-        if (none) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = 0.f;
-        } else {
-          ptx::tmem_ld16(f.tmem + (static_cast<uint32_t>(warp * 32) << 16) + c, v);
+      for (int h = 0; h < 2; ++h) {
+        const int c = c0 + 32 * h;
+        if (!none) {
+          float v[32];
+          ptx::tmem_ld32(f.tmem + (static_cast<uint32_t>(quarter * 32) << 16) + half * 64 + 32 * h, v);
           ptx::tmem_ld_wait();
+          float4* to = reinterpret_cast<float4*>(turn + lane * TURN_PITCH);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) to[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
         }
-        if (in && p.wide) {
+        __syncwarp();
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint4 q = base[k + h];
-            const uint32_t b[4] = {q.x, q.y, q.z, q.w};
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w[i] = bf16_pair(__uint_as_float(b[i] << 16) + v[8 * h + 2 * i], __uint_as_float(b[i] & 0xffff0000u) + v[8 * h + 2 * i + 1]);
-            if (c + 8 * h < width) *reinterpret_cast<uint4*>(p.Y + at + c + 8 * h) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int k = 0; k < 8; ++k) {
+          const long long at = row_at[4 * k + up];
+          const float4 x = none ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(turn + (4 * k + up) * TURN_PITCH + col);
+          const uint2 q = base[h][k];
+          const uint32_t lo = bf16_pair(__uint_as_float(q.x << 16) + x.x, __uint_as_float(q.x & 0xffff0000u) + x.y);
+          const uint32_t hi = bf16_pair(__uint_as_float(q.y << 16) + x.z, __uint_as_float(q.y & 0xffff0000u) + x.w);
+          if (at >= 0 && c < p.N) {
+            if (p.wide) {
+              *reinterpret_cast<uint2*>(p.Y + at + c) = make_uint2(lo, hi);
+            } else {
+              unsigned short* o = reinterpret_cast<unsigned short*>(p.Y + at + c);
+              o[0] = static_cast<unsigned short>(lo);
+              if (c + 1 < p.N) o[1] = static_cast<unsigned short>(lo >> 16);
+              if (c + 2 < p.N) o[2] = static_cast<unsigned short>(hi);
+              if (c + 3 < p.N) o[3] = static_cast<unsigned short>(hi >> 16);
+            }
           }
-        } else if (in) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (c + i < width) p.Y[at + c + i] = __float2bfloat16_rn(p.base ? __bfloat162float(p.base[at + c + i]) + v[i] : v[i]);
         }
         __syncwarp();
       }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(f.drain + 1);      // the accumulator may be written again
     }
     __syncwarp();
   }
-  frame_close(f, EXPAND_TMEM, p.status);
+  frame_close<EXPAND_MMA>(f, EXPAND_TMEM, p.status);
 }
 
 // ---------------------------------------------------------------------------------------------- gradients
 struct GradientDev {
-  CUtensorMap V, V_box, P;
+  CUtensorMap V, V_box, V_tile, P;
   __nv_bfloat16* out;
   int N, rank_rows, blocks;
 };
@@ -471,9 +546,10 @@ struct GradientParams {
   GradientDev job[2];
   Sorted s;
   int r, cols, wide;          // wide: r is a multiple of 8
+  int stage;
   int* status;
 };
-constexpr int GRADIENT_STAGES = 3, GRADIENT_RING = GRADIENT_STAGES * (A_BYTES + B_BYTES), GRADIENT_SMEM = 1024 + GRADIENT_RING + FRAME_BYTES;
+constexpr int GRADIENT_STAGES = 4;
 constexpr uint32_t GRADIENT_TMEM = 128;
 
 __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_constant__ GradientParams p) {
@@ -484,25 +560,35 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
   const int c0 = (blockIdx.x - (which ? p.job[0].blocks : 0)) * TOKENS;     // 128 columns of V: the rows of the tile
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int count = __ldcg(p.s.count + i), first = __ldcg(p.s.offset + i);
-  const Frame f = frame_open(raw, GRADIENT_RING, GRADIENT_STAGES, GRADIENT_TMEM);
+  const Frame f = frame_open(raw, GRADIENT_STAGES * p.stage, GRADIENT_STAGES, GRADIENT_TMEM);
   const int kb = (count + BLOCK_K - 1) / BLOCK_K;
   if (warp == COPY_WARP) {
     const int tile0 = tiles_before(p.s, i);
     const uint32_t tx = A_BYTES + (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES;
+    const int top0 = count > 0 ? __ldcg(p.s.order + first) : 0;
+    const bool run = count > 0 && __ldcg(p.s.order + first + count - 1) - top0 == count - 1;
     bool ok = true;
     for (int k = 0; k < kb; ++k) {
       const int s = k % GRADIENT_STAGES;
-      const Rows rows = rows_of(p.s, first + k * BLOCK_K, count - k * BLOCK_K, (lane & 3) * ROWS);
+      // a k-block that is one run: one box for each half of the columns
+      const int left = count - k * BLOCK_K, top = run ? top0 + k * BLOCK_K : 0;
+      const bool whole = run && left >= BLOCK_K;
+      Rows rows;
+      if (!whole) rows = rows_of(p.s, first + k * BLOCK_K, left, (lane & 3) * ROWS);
       ok = ptx::mbar_wait_warp(&f.empty[s], ((k / GRADIENT_STAGES) & 1) ^ 1, f.abort_flag);
       if (!ok) break;
-      const uint32_t to = f.smem0 + s * (A_BYTES + B_BYTES), bar = ptx::smem_u32(&f.full[s]);
+      const uint32_t to = f.smem0 + s * p.stage, bar = ptx::smem_u32(&f.full[s]);
       if (lane == 0) {
         ptx::mbar_expect_tx(&f.full[s], tx);
         load_3d(&job.P, to + A_BYTES, bar, 0, tile0 * TOKENS + k * BLOCK_K, 0);
         if (p.cols > 64) load_3d(&job.P, to + A_BYTES + BLOCK64_BYTES, bar, 64, tile0 * TOKENS + k * BLOCK_K, 0);
       }
       __syncwarp();
-      if (lane < 8) load_rows(&job.V_box, &job.V, to + (lane >> 2) * BLOCK64_BYTES + (lane & 3) * (ROWS * 128), bar, c0 + (lane >> 2) * 64, rows);
+      if (whole) {
+        if (lane < 2) load_2d(&job.V_tile, to + lane * BLOCK64_BYTES, bar, c0 + lane * 64, top);
+      } else if (lane < 8) {
+        load_rows(&job.V_box, &job.V, to + (lane >> 2) * BLOCK64_BYTES + (lane & 3) * (ROWS * 128), bar, c0 + (lane >> 2) * 64, rows);
+      }
     }
     if (!ok) copies_gave_up();
     __syncwarp();
@@ -514,7 +600,7 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
       ok = ptx::mbar_wait_warp(&f.full[s], (k / GRADIENT_STAGES) & 1, f.abort_flag);
       if (!ok) break;
       ptx::tc_fence_after();
-      const uint32_t at = f.smem0 + s * (A_BYTES + B_BYTES);
+      const uint32_t at = f.smem0 + s * p.stage;
       if (ptx::elect_one()) {
         issue(f.tmem, ptx::umma_desc_mn128(at, BLOCK64_BYTES), 2048 >> 4, ptx::umma_desc_mn128(at + A_BYTES, BLOCK64_BYTES), 2048 >> 4, idesc, BLOCK_K / 16, k == 0);
         ptx::umma_commit(&f.empty[s]);
@@ -592,22 +678,28 @@ ffsplit_status encode(ffsplit_ctx* ctx, const void* at, long long cols, long lon
   if (r != CUDA_SUCCESS) return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
   return FFSPLIT_OK;
 }
-ffsplit_status encode_rows(ffsplit_ctx* ctx, const tg::Matrix& m, CUtensorMap* gather, CUtensorMap* box) {
-  const ffsplit_status s = encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, 1, gather);
-  return s != FFSPLIT_OK ? s : encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, ROWS, box);
+// Rows one by one, sixteen at a time, and `most` at a time.
+ffsplit_status encode_rows(ffsplit_ctx* ctx, const tg::Matrix& m, int most, CUtensorMap* gather, CUtensorMap* box, CUtensorMap* tile) {
+  ffsplit_status s = encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, 1, gather);
+  if (s == FFSPLIT_OK) s = encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, ROWS, box);
+  return s != FFSPLIT_OK ? s : encode(ctx, m.p, m.cols, m.rows, 1, m.ld, 2, most, tile);
 }
 ffsplit_status encode_factor(ffsplit_ctx* ctx, const Factor& f, int n, int box_rows, CUtensorMap* out) {
   return encode(ctx, f.m.p, f.cols, f.rows, n, f.m.ld, 3, box_rows, out);
 }
+
+inline int expand_smem(int r) { return 1024 + (r > BLOCK_K ? 2 : 1) * (A_BYTES + 2 * EXPAND_F) + FRAME_BYTES + EXPAND_WARPS * TURN_BYTES; }
+inline int stage_bytes(int r) { return A_BYTES + (r > 64 ? B_BYTES : B_BYTES / 2); }
+inline int smem_of(int stages, int r) { return 1024 + stages * stage_bytes(r) + FRAME_BYTES; }
 
 // The tensor maps are made by a driver call, which needs a current context; and the kernels take more than 48 KB.
 ffsplit_status set_up(ffsplit_ctx* ctx) {
   const cudaError_t bound = cudaSetDevice(ctx->device);
   if (bound != cudaSuccess) return check_cuda(ctx, bound, "cudaSetDevice");
   if (ctx->attr_adapter_set) return FFSPLIT_OK;
-  cudaError_t e = cudaFuncSetAttribute(shrink_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SHRINK_SMEM);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(expand_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EXPAND_SMEM);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(gradient_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GRADIENT_SMEM);
+  cudaError_t e = cudaFuncSetAttribute(shrink_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(SHRINK_STAGES, MAX_RANK));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(expand_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, expand_smem(MAX_RANK));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(gradient_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(GRADIENT_STAGES, MAX_RANK));
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(adapter kernels)");
   ctx->attr_adapter_set = true;
   return FFSPLIT_OK;
@@ -626,25 +718,25 @@ ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, con
   if (rc != FFSPLIT_OK) return rc;
   ShrinkParams p;
   std::memset(&p, 0, sizeof(p));
-  p.s = s; p.scale = scale; p.r = r; p.cols = round_up(r, 16); p.pitch = rank_pitch(r); p.status = ctx->status();
+  p.s = s; p.scale = scale; p.r = r; p.cols = round_up(r, 16); p.pitch = rank_pitch(r); p.stage = stage_bytes(r); p.status = ctx->status();
   int kb = 1;
   for (int i = 0; i < n; ++i) {
     ShrinkDev& d = p.job[i];
-    if ((rc = encode_rows(ctx, jobs[i].V, &d.V, &d.V_box)) != FFSPLIT_OK) return rc;
+    if ((rc = encode_rows(ctx, jobs[i].V, TOKENS, &d.V, &d.V_box, &d.V_tile)) != FFSPLIT_OK) return rc;
     d.f_mn = jobs[i].F.rank_rows ? 0 : 1;
     if ((rc = encode_factor(ctx, jobs[i].F, s.n, d.f_mn ? BLOCK_K : p.cols, &d.F)) != FFSPLIT_OK) return rc;
     d.P = jobs[i].P;
     d.kb = (jobs[i].K + BLOCK_K - 1) / BLOCK_K;
     if (d.kb > kb) kb = d.kb;
   }
-  // ranges of K: as many CTAs as SMs, four k-blocks each at least (the cluster's exchange takes about as long)
+  // ranges of K: two CTAs to an SM, four k-blocks each at least (the cluster's exchange takes about as long)
   const long long tiles = tile_bound(s.T, s.n);
   int ranges = 1;
-  while (ranges < 8 && 2 * ranges * tiles * n <= ctx->num_sms && 8 * ranges <= kb) ranges *= 2;
+  while (ranges < MAX_RANGES && ranges * tiles * n < ctx->num_sms && 8 * ranges <= kb) ranges *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranges, static_cast<unsigned>(tiles), n);
   cfg.blockDim = dim3(TC_THREADS);
-  cfg.dynamicSmemBytes = SHRINK_SMEM;
+  cfg.dynamicSmemBytes = smem_of(SHRINK_STAGES, r);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -672,8 +764,14 @@ ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const 
   if ((rc = encode_factor(ctx, F, s.n, p.f_mn ? BLOCK_K : EXPAND_COLS, &p.F)) != FFSPLIT_OK) return rc;
   p.s = s;
   p.base = static_cast<const __nv_bfloat16*>(base); p.Y = static_cast<__nv_bfloat16*>(Y);
-  p.N = N; p.r = r; p.wide = N % 8 == 0; p.status = ctx->status();
-  const cudaError_t e = launch_pdl(expand_tc_kernel, dim3((N + EXPAND_COLS - 1) / EXPAND_COLS, static_cast<unsigned>(tiles)), dim3(TC_THREADS), EXPAND_SMEM, st, p);
+  p.N = N; p.r = r; p.wide = N % 4 == 0; p.status = ctx->status();
+  p.blocks = r > BLOCK_K ? 2 : 1;
+  // Two CTAs to an SM where there are few tiles, else four blocks of columns to a CTA: its start is paid once, and the last
+  // round of CTAs stays short (fourteen blocks each, 342 CTAs on 296 places: 114 us instead of 57).
+  const long long blocks = (N + EXPAND_COLS - 1) / EXPAND_COLS, fill = (2 * ctx->num_sms + tiles - 1) / tiles, four = (blocks + 3) / 4;
+  const long long wanted = fill > four ? fill : four;
+  const cudaError_t e = launch_pdl(expand_tc_kernel, dim3(static_cast<unsigned>(wanted < blocks ? wanted : blocks), static_cast<unsigned>(tiles)), dim3(EXPAND_TC_THREADS),
+                                   expand_smem(r), st, p);
   ctx->launches++;
   return check_cuda(ctx, e, "adapter::expand_tc_kernel launch");
 }
@@ -683,18 +781,18 @@ ffsplit_status launch_gradients_tc(ffsplit_ctx* ctx, const Gradient* jobs, int n
   if (rc != FFSPLIT_OK) return rc;
   GradientParams p;
   std::memset(&p, 0, sizeof(p));
-  p.s = s; p.r = r; p.cols = round_up(r, 16); p.wide = r % 8 == 0; p.status = ctx->status();
+  p.s = s; p.r = r; p.cols = round_up(r, 16); p.wide = r % 8 == 0; p.stage = stage_bytes(r); p.status = ctx->status();
   int blocks = 0;
   for (int i = 0; i < n; ++i) {
     GradientDev& d = p.job[i];
-    if ((rc = encode_rows(ctx, jobs[i].V, &d.V, &d.V_box)) != FFSPLIT_OK) return rc;
+    if ((rc = encode_rows(ctx, jobs[i].V, BLOCK_K, &d.V, &d.V_box, &d.V_tile)) != FFSPLIT_OK) return rc;
     if ((rc = encode(ctx, jobs[i].P, rank_pitch(r), tile_bound(s.T, s.n) * TOKENS, 1, rank_pitch(r), 3, BLOCK_K, &d.P)) != FFSPLIT_OK) return rc;
     d.out = static_cast<__nv_bfloat16*>(jobs[i].out);
     d.N = jobs[i].N; d.rank_rows = jobs[i].rank_rows;
     d.blocks = (jobs[i].N + TOKENS - 1) / TOKENS;
     blocks += d.blocks;
   }
-  const cudaError_t e = launch_pdl(gradient_tc_kernel, dim3(blocks, s.n), dim3(TC_THREADS), GRADIENT_SMEM, st, p);
+  const cudaError_t e = launch_pdl(gradient_tc_kernel, dim3(blocks, s.n), dim3(TC_THREADS), smem_of(GRADIENT_STAGES, r), st, p);
   ctx->launches++;
   return check_cuda(ctx, e, "adapter::gradient_tc_kernel launch");
 }
