@@ -411,7 +411,7 @@ constexpr float kStandard[3] = {3.4445f, -4.7750f, 2.0315f};
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Bytes of one matrix's buffers: X twice, S and P = b S + c S^2, two planes each.
+// Bytes of one matrix's buffers: X twice, S and P, two planes each.
 size_t x_bytes(int rows, int cols) { return static_cast<size_t>(rows) * round_up(cols, 64) * 4; }
 int thin_parts(int rows, int cols) {
   const int chunks = ((rows < cols ? cols : rows) + muon::THIN_CHUNK - 1) / muon::THIN_CHUNK;
@@ -451,7 +451,7 @@ ffsplit_status check_list(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int co
   return FFSPLIT_OK;
 }
 
-// Whether the iteration keeps singular values of [0, 1] below 1.5 and P = b S + c S^2 below 200.
+// Whether the iteration keeps singular values of [0, 1] below 1.5 and P = a I + b S + c S^2 below 200.
 bool coefficients_hold(const float* c, int iterations) {
   double top = 1.0;
   for (int i = 0; i < iterations; ++i, c += 3) {
@@ -460,7 +460,7 @@ bool coefficients_hold(const float* c, int iterations) {
     for (int k = 0; k <= 4096; ++k) {
       const double s = top * k / 4096, v = std::fabs(s * (c[0] + s * s * (c[1] + s * s * c[2])));
       if (v > most) most = v;
-      if (!(std::fabs(s * s * (c[1] + s * s * c[2])) <= 200.0)) return false;
+      if (!(std::fabs(c[0] + s * s * (c[1] + s * s * c[2])) <= 200.0)) return false;
     }
     if (!(most <= 1.5)) return false;
     top = most;
@@ -495,19 +495,21 @@ ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon
           p.M = p.N = g.S.rows; p.K = tall ? g.rows : g.cols;
           p.symmetric = 1;
           p.c_low = precise;
-        } else if (step == 1) {      // P = b S + c S S
+        } else if (step == 1) {      // P = a I + b S + c S S
           p.a = p.b = g.S; p.c = g.P;
           p.M = p.N = p.K = g.S.rows;
-          p.alpha *= k[2]; p.beta = k[1];
-          p.d = &g.S; p.d_low = precise;
+          p.alpha *= k[2]; p.beta = k[1]; p.diagonal = k[0];
+          p.d = &g.S; p.d_high = 1; p.d_low = precise;
           p.symmetric = 1;
           p.c_low = precise;
-        } else {                     // a X + P X, or a X + X P
+        } else {                     // P X, or X P
           p.a = tall ? X : g.P; p.b = tall ? g.P : X; p.c = Y;
           p.b_mn = !tall;
           p.M = g.rows; p.N = g.cols; p.K = g.S.rows;
-          p.beta = k[0];
-          p.d = &X; p.d_low = 1;
+          if (!precise) {            // (of the second plane only the term a X)
+            p.beta = k[0];
+            p.d = &X; p.d_low = 1;
+          }
           p.c_low = 1;
           if (it + 1 == iterations) p.target = targets + g.first;
         }

@@ -9,7 +9,7 @@
 namespace ffsp {
 namespace muon {
 
-// X, S = X X^T and P = b S + c S^2 are held as fp16 times 256, which keeps values from 2.4e-7 to 200 normal: singular
+// X, S = X X^T and P = a I + b S + c S^2 are held as fp16 times 256, which keeps values from 2.4e-7 to 200 normal: singular
 // values of X stay below 1.5, so its elements do, S's below 2.3, and P is checked to stay below 200.  A second plane holds
 // what the first one rounds off, times 2048: 22 bits together.
 constexpr float HELD = 256.f, LOW = 2048.f;
@@ -29,14 +29,14 @@ struct Target {
   int f32, wide;          // wide: every 16 columns of W and out start on 16 bytes
 };
 
-// C = alpha A B^ + beta D for every matrix of a group.
+// C = alpha A B + beta D + diagonal I for every matrix of a group.
 struct Product {
   Matrices a, b, c;       // a: [M, K], or [K, M] with a_mn; b: [N, K], or [K, N] with b_mn
   int a_mn, b_mn;
   int M, N, K;
-  float alpha, beta;
+  float alpha, beta, diagonal;
   const Matrices* d;      // nullptr: no second term
-  int d_low;              // its second plane is added too
+  int d_high, d_low;      // which of its planes
   int symmetric;          // C = C^T: tiles above the diagonal only, and mirrored
   int c_low;              // the second plane of C is written
   const Target* target;   // the last product: the matrices are updated, nothing is written to c

@@ -1,6 +1,6 @@
 // The three products of a Newton-Schulz iteration on the tensor cores:
 //
-//   S = X X^T,   P = b S + c S S,   X <- a X + P X          (rows > cols: S = X^T X, X <- a X + X P)
+//   S = X X^T,   P = a I + b S + c S S,   X <- P X          (rows > cols: S = X^T X, X <- X P)
 //
 // for a group of matrices of one shape, up to four groups to a launch.  A persistent pair of CTAs (cta_group::2) takes
 // 256 x 256 (or 256 x 128) tiles: TMA into a ring of stages, one thread issues the MMAs of both CTAs, two accumulators, the
@@ -13,10 +13,11 @@
 // Operands are fp16 (11 bits; bf16 has 8 at the same rate).  Rounding S or P multiplies X by a matrix close to the identity,
 // which the iteration corrects or carries along as it is.  Rounding X would add noise in every direction, and directions
 // with small singular values would drown in what is rounded off the large ones (a momentum with a few strong directions: 1e-2
-// of the result, with bf16 8e-2).  So X has a second plane for the next 11 bits, which the term a X reads but the tensor
-// cores do not: 1.5e-4 to 2e-3, for 2 bytes more read and written per element.  precise: the tensor cores take the second
-// planes too (three products of planes, the small ones first), and sums leave them every PROMOTE k-blocks, because their
-// running sums are cut, not rounded (see train_gemm.cu).
+// of the result, with bf16 8e-2).  So X has a second plane for the next 11 bits.  a is added to the diagonal of P, so that the
+// tensor cores form a X + P X from the first plane, and the epilogue adds a times the second: 6e-4 to 2e-3, for 2 bytes read and
+// written per element.  precise: the tensor cores take the second planes of all operands (three products of planes, the small
+// ones first), and sums leave them every PROMOTE k-blocks, because their running sums are cut, not rounded (see
+// train_gemm.cu).
 //
 // Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
 #include <cstring>
@@ -35,13 +36,16 @@ constexpr int TMEM_COLS = 512;
 constexpr int BAR_BYTES = 256;
 constexpr int MAX_SMEM = 232448;
 constexpr int RING_BYTES = (MAX_SMEM - 1024 - BAR_BYTES) / 1024 * 1024;
-constexpr int EPI_WARPS = 8, GROUPS = EPI_WARPS / 4;
+// An epilogue reads 2 bytes of every value and writes 4 while the tensor cores take 17 us over a tile (K = 4096): with 8 warps,
+// each waiting for its next 16 columns, it took 35 us.  precise: 8, for the sake of their registers.
+template <bool PRECISE> constexpr int EPI_WARPS = PRECISE ? 8 : 16;
+template <bool PRECISE> constexpr int GROUPS = EPI_WARPS<PRECISE> / 4;
 // precise: the epilogue's sums take 128 registers a thread; it starts on a warpgroup's boundary so that registers can move
 // to it (384 threads start with 168 each; 128 of them go down to 56 and 256 up to 224: 64512 in all).
 template <bool PRECISE> constexpr int FIRST_EPI = PRECISE ? 4 : 2;
 constexpr int START_REGS = 168, ROLE_REGS = 56, EPI_REGS = 224;
 static_assert(ROLE_REGS * 128 + EPI_REGS * 256 <= START_REGS * 384, "a split above what the block starts with waits forever");
-template <bool PRECISE> constexpr int GEMM_THREADS = 32 * (EPI_WARPS + FIRST_EPI<PRECISE>);
+template <bool PRECISE> constexpr int GEMM_THREADS = 32 * (EPI_WARPS<PRECISE> + FIRST_EPI<PRECISE>);
 constexpr int PROMOTE = 4;
 
 struct DevProduct {
@@ -50,10 +54,10 @@ struct DevProduct {
   int a_mn, b_mn, symmetric;
   int tiles_m, tiles_n, tiles, panel_m;
   int unit0;
-  float alpha, beta;
-  const __half* D;
-  long long d_each, d_plane;
-  int ldd, d_low;
+  float alpha, beta, beta_low, diagonal;
+  const __half *D, *D_low;    // either may be missing
+  long long d_each;
+  int ldd;
   __half* C;
   long long c_each, c_plane;
   int ldc, c_low;
@@ -99,16 +103,26 @@ __device__ __forceinline__ int part_end(int kb, int begin) {
   return begin + PROMOTE < 3 * kb ? begin + PROMOTE : 3 * kb;
 }
 
+__device__ __forceinline__ float2 half_pair(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 __device__ __forceinline__ void store32_bytes(void* base, const uint32_t* w) {   // 32-byte aligned
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(base), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
                "r"(w[5]), "r"(w[6]), "r"(w[7])
                : "memory");
 }
 __device__ __forceinline__ void load32_bytes(const void* base, uint32_t* w) {
-  const uint4 x = __ldcg(static_cast<const uint4*>(base)), y = __ldcg(static_cast<const uint4*>(base) + 1);
-  w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; w[4] = y.x; w[5] = y.y; w[6] = y.z; w[7] = y.w;
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(base));
 }
-__device__ __forceinline__ float2 half_pair(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+// v += beta times 16 halves
+__device__ __forceinline__ void add16(float* v, float beta, const uint32_t* w) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 x = half_pair(w[i]);
+    v[2 * i] = fmaf(beta, x.x, v[2 * i]);
+    v[2 * i + 1] = fmaf(beta, x.y, v[2 * i + 1]);
+  }
+}
 __device__ __forceinline__ uint32_t pair_half(float x, float y) {
   const __half2 h = __floats2half2_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -199,7 +213,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&tfull[a], 1);
-      ptx::mbar_init(&tempty[a], 2 * EPI_WARPS);
+      ptx::mbar_init(&tempty[a], 2 * EPI_WARPS<PRECISE>);
     }
     ptx::mbar_init(drain, 1);
     *abort_flag = 0;
@@ -327,7 +341,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
     if constexpr (PRECISE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
     // -------------------------------------------------------------- epilogue warps
     const int q = warp & 3;                                // tensor-memory lane quarter
-    const int cols = p.tile_n / GROUPS;                    // columns of this warp's part of the tile
+    const int cols = p.tile_n / GROUPS<PRECISE>;                    // columns of this warp's part of the tile
     const int col0 = ((warp - FIRST) >> 2) * cols;
     const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + col0;
     uint32_t tl = 0;
@@ -340,17 +354,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
       const int c0 = t.n_blk * p.tile_n + col0;
       const int width = d.N - c0 < cols ? d.N - c0 : cols;       // (may be negative)
       const bool mirror = d.symmetric && t.n_blk * p.tile_n >= (t.m_blk + 1) * TILE_M;
-      const __half* D = d.D ? d.D + t.batch * d.d_each + static_cast<long long>(row) * d.ldd + c0 : nullptr;
+      const long long d_at = t.batch * d.d_each + static_cast<long long>(row) * d.ldd + c0;
+      const __half *D = d.D && in ? d.D + d_at : nullptr, *D_low = d.D_low && in ? d.D_low + d_at : nullptr;
       __half* C = d.C + t.batch * d.c_each + static_cast<long long>(row) * d.ldc + c0;
-      // what is added is on its way before the sum is complete
-      uint32_t high[8], low[8];
-      if (D && in && width > 0) {
-        load32_bytes(D, high);
-        if (d.d_low) load32_bytes(D + d.d_plane, low);
+      // What is added is on its way two pieces of 16 columns ahead: those of the first plane here, or of the second where
+      // there is no first (only precise products have both).
+      const __half* ahead = D ? D : D_low;
+      const float beta = D ? d.beta : d.beta_low;
+      uint32_t next[2][8];
+      if (ahead) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) if (16 * k < width) load32_bytes(ahead + 16 * k, next[k]);
       }
       if constexpr (PRECISE) {
         // All parts of the sum but the last are added up in registers; then it goes back to where the last part lies.
-        constexpr int BLOCKS = TILE_N / GROUPS / 32;             // (precise tiles are 256 wide)
+        constexpr int BLOCKS = TILE_N / GROUPS<PRECISE> / 32;             // (precise tiles are 256 wide)
         float sum[BLOCKS][32];
         for (int begin = 0;; ++tl) {
           const int end = part_end(d.kb, begin);
@@ -391,29 +409,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
         ptx::tc_fence_after();
       }
       const uint32_t acc = tl & 1, t_row = t_quarter + acc * TILE_N;
-#pragma unroll 1
-      for (int c = 0; c < width; c += 16) {
+#pragma unroll 2
+      for (int c = 0, k = 0; c < width; c += 16, k ^= 1) {
         float v[16];
         ptx::tmem_ld16(t_row + c, v);
         ptx::tmem_ld_wait();
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] *= d.alpha;
-        if (D && in) {
+        if (ahead) {
+          add16(v, beta, next[k]);
+          if (c + 32 < width) load32_bytes(ahead + c + 32, next[k]);
+        }
+        if (PRECISE && D && D_low) {
+          uint32_t low[8];
+          load32_bytes(D_low + c, low);
+          add16(v, d.beta_low, low);
+        }
+        if (d.diagonal != 0.f && row >= c0 + c && row < c0 + c + 16) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float2 x = half_pair(high[i]);
-            if (d.d_low) {
-              const float2 y = half_pair(low[i]);
-              x.x = fmaf(y.x, 1.f / LOW, x.x);
-              x.y = fmaf(y.y, 1.f / LOW, x.y);
-            }
-            v[2 * i] = fmaf(d.beta, x.x, v[2 * i]);
-            v[2 * i + 1] = fmaf(d.beta, x.y, v[2 * i + 1]);
-          }
-          if (c + 16 < width) {
-            load32_bytes(D + c + 16, high);
-            if (d.d_low) load32_bytes(D + d.d_plane + c + 16, low);
-          }
+          for (int i = 0; i < 16; ++i) if (row == c0 + c + i) v[i] += d.diagonal;
         }
         if (d.target) {
           if (in) update16(d.target[t.batch], row, c0 + c, d.N, v);
@@ -552,7 +566,13 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
     d.tiles = tiles_of(g, p.tile_n);
     d.unit0 = static_cast<int>(units);
     d.alpha = g.alpha; d.beta = g.beta;
-    if (g.d) { d.D = g.d->p; d.d_each = g.d->each; d.d_plane = g.d->plane; d.ldd = g.d->ld; d.d_low = g.d_low; }
+    if (g.d) {
+      d.D = g.d_high ? g.d->p : nullptr;
+      d.D_low = g.d_low ? g.d->p + g.d->plane : nullptr;
+      d.d_each = g.d->each; d.ldd = g.d->ld;
+    }
+    d.beta_low = g.beta * (1.f / LOW);
+    d.diagonal = g.diagonal * HELD;
     d.C = g.c.p; d.c_each = g.c.each; d.c_plane = g.c.plane; d.ldc = g.c.ld; d.c_low = g.c_low;
     d.target = g.target;
     // panel height: the tiles in flight form a block whose two sides carry about the same operand bytes
