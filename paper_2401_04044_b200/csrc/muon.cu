@@ -26,8 +26,8 @@ struct Entry {
   float* Mo;
   const void* W;
   void* out;
-  __half* X;              // [rows][ld], the second plane `plane` elements on
-  long long plane;
+  __half *X, *X_low;      // [rows][ld], and the second plane: likewise, or in blocks
+  int blocks;
   int rows, cols, octets; // octets of columns in a row
   int g_f32, w_f32, wide; // wide: every octet of G, M, Mo starts on 16 bytes
   int ld;
@@ -95,17 +95,20 @@ __device__ __forceinline__ const Entry& entry_of(const Table& t, int block, int*
   *which = lo;
   return t.t[lo];
 }
-// Octets begin .. end of block `part` of a matrix.
-__device__ __forceinline__ void range_of(const Entry& e, int part, long long* begin, long long* end) {
-  const long long all = static_cast<long long>(e.rows) * e.octets, per = (all + e.parts - 1) / e.parts;
+// A matrix is gone through in pieces of 32 rows x 64 columns, eight columns to a thread: eight threads read a line of G, and what
+// a piece leaves in a second plane of blocks is whole sectors.  Pieces begin .. end of block `part`.
+__device__ __forceinline__ int pieces_across(const Entry& e) { return (e.octets + 7) / 8; }
+__device__ __forceinline__ void range_of(const Entry& e, int part, int* begin, int* end) {
+  const int all = (e.rows + 31) / 32 * pieces_across(e), per = (all + e.parts - 1) / e.parts;
   *begin = part * per;
   *end = *begin + per < all ? *begin + per : all;
 }
-__device__ __forceinline__ void place(const Entry& e, long long i, int* row, int* octet) {
-  const long long all = static_cast<long long>(e.rows) * e.octets;
-  const long long r = all <= 0xffffffffll ? static_cast<unsigned>(i) / static_cast<unsigned>(e.octets) : i / e.octets;
-  *row = static_cast<int>(r);
-  *octet = static_cast<int>(i - r * e.octets);
+// This thread's columns of a piece; false: there are none.
+__device__ __forceinline__ bool place(const Entry& e, int piece, int* row, int* octet) {
+  const int across = pieces_across(e), r = piece / across;
+  *row = r * 32 + (threadIdx.x >> 3);
+  *octet = (piece - r * across) * 8 + (threadIdx.x & 7);
+  return *row < e.rows && *octet < e.octets;
 }
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
@@ -123,12 +126,13 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ T
   int which;
   const Entry& e = entry_of(t, blockIdx.x, &which);
   const int part = blockIdx.x - e.block0;
-  long long begin, end;
+  int begin, end;
   range_of(e, part, &begin, &end);
   double acc = 0.0;
-  for (long long i = begin + threadIdx.x; i < end; i += THREADS) {
+#pragma unroll 2
+  for (int i = begin; i < end; ++i) {
     int row, octet;
-    place(e, i, &row, &octet);
+    if (!place(e, i, &row, &octet)) continue;
     float m[8], u[8];
     load_u8(e, t.beta, t.nesterov, row, octet, m, u);
 #pragma unroll
@@ -158,11 +162,12 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
     t.target[which] = o;
     if (!finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, which, KID_MUON);
   }
-  long long begin, end;
+  int begin, end;
   range_of(e, part, &begin, &end);
-  for (long long i = begin + threadIdx.x; i < end; i += THREADS) {
+#pragma unroll 2
+  for (int i = begin; i < end; ++i) {
     int row, octet;
-    place(e, i, &row, &octet);
+    if (!place(e, i, &row, &octet)) continue;
     float m[8], u[8];
     load_u8(e, t.beta, t.nesterov, row, octet, m, u);
     const int c = octet * 8;
@@ -185,7 +190,8 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
     for (int k = 0; k < 8; ++k) split_half(finite ? u[k] * inv * HELD : 0.f, &hi[k], &lo[k]);
     __half* x = e.X + static_cast<long long>(row) * e.ld + c;
     *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(hi);
-    *reinterpret_cast<uint4*>(x + e.plane) = *reinterpret_cast<const uint4*>(lo);
+    __half* x_low = e.X_low + (e.blocks ? block_at(row, octet, e.ld) : static_cast<long long>(row) * e.ld + c);
+    *reinterpret_cast<uint4*>(x_low) = *reinterpret_cast<const uint4*>(lo);
   }
 }
 
@@ -412,7 +418,7 @@ constexpr float kStandard[3] = {3.4445f, -4.7750f, 2.0315f};
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // Bytes of one matrix's buffers: X twice, S and P, two planes each.
-size_t x_bytes(int rows, int cols) { return static_cast<size_t>(rows) * round_up(cols, 64) * 4; }
+size_t x_bytes(int rows, int cols) { return static_cast<size_t>(rows + muon::block_rows(rows)) * round_up(cols, 64) * 2; }
 int thin_parts(int rows, int cols) {
   const int chunks = ((rows < cols ? cols : rows) + muon::THIN_CHUNK - 1) / muon::THIN_CHUNK;
   return chunks < muon::THIN_PARTS ? chunks : muon::THIN_PARTS;
@@ -424,8 +430,8 @@ size_t matrix_bytes(int rows, int cols) {
   return 2 * x_bytes(rows, cols) + 2 * x_bytes(p, p);
 }
 constexpr size_t kTableBytes = muon::MAX_TENSORS * (muon::MAX_PARTS * sizeof(double) + sizeof(muon::Target));
-// Matrices are worked on in runs: as many as fit the tables and half a gigabyte, one at least.
-constexpr size_t kRunBytes = 512u << 20;
+// Matrices are worked on in runs: as many as fit the tables and two gigabytes, one at least.
+constexpr size_t kRunBytes = static_cast<size_t>(2) << 30;
 int run_length(const ffsplit_muon_tensor* t, int count, size_t* bytes) {
   size_t sum = 0;
   int n = 0;
@@ -588,11 +594,13 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
   Group groups[muon::MAX_TENSORS];
   int order[muon::MAX_TENSORS], n_groups = 0, placed = 0;
   bool done[muon::MAX_TENSORS] = {};
-  const auto matrices = [&](int rows, int cols, int count) {
+  const auto matrices = [&](int rows, int cols, int count, bool precise) {
     muon::Matrices m;
     m.p = reinterpret_cast<__half*>(at);
     m.rows = rows; m.cols = cols; m.ld = round_up(cols, 64); m.count = count;
-    m.each = static_cast<long long>(rows) * m.ld; m.plane = m.each * count;
+    m.each = static_cast<long long>(rows) * m.ld;
+    m.low_each = precise ? m.each : muon::block_rows(rows) * m.ld;
+    m.low = m.p + m.each * count;
     at += x_bytes(rows, cols) * count;
     return m;
   };
@@ -608,10 +616,10 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
         ++g.count;
       }
     const int p = g.rows < g.cols ? g.rows : g.cols;
-    g.X[0] = matrices(g.rows, g.cols, g.count);
-    g.X[1] = matrices(g.rows, g.cols, g.count);
-    g.S = matrices(p, p, g.count);
-    g.P = matrices(p, p, g.count);
+    g.X[0] = matrices(g.rows, g.cols, g.count, g.precise);
+    g.X[1] = matrices(g.rows, g.cols, g.count, g.precise);
+    g.S = matrices(p, p, g.count, g.precise);
+    g.P = matrices(p, p, g.count, g.precise);
   }
   int blocks = 0;
   for (int gi = 0, k = 0; gi < n_groups; ++gi) {
@@ -622,9 +630,10 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
       e = entry_for(s);
       e.ld = g.X[0].ld;
       e.X = g.X[0].p + j * g.X[0].each;
-      e.plane = g.X[0].plane;
-      const long long octets = static_cast<long long>(s.rows) * e.octets;
-      e.parts = static_cast<int>(octets < 512ll * muon::MAX_PARTS ? (octets + 511) / 512 : muon::MAX_PARTS);
+      e.X_low = g.X[0].low + j * g.X[0].low_each;
+      e.blocks = g.precise ? 0 : 1;
+      const long long pieces = (s.rows + 31ll) / 32 * ((e.octets + 7) / 8);
+      e.parts = static_cast<int>(pieces < 2 * muon::MAX_PARTS ? (pieces + 1) / 2 : muon::MAX_PARTS);
       e.block0 = blocks;
       blocks += e.parts;
     }

@@ -14,12 +14,15 @@ namespace muon {
 // what the first one rounds off, times 2048: 22 bits together.
 constexpr float HELD = 256.f, LOW = 2048.f;
 
-// `count` matrices [rows, cols] with pitch ld (a multiple of 64), one after the other; the second plane `plane` elements on.
+// `count` matrices [rows, cols] with pitch ld (a multiple of 64), one after the other.  The second plane: the same, count * each
+// elements on, where the tensor cores take it too (precise); else only epilogues read and write it, a lane to a row, and it lies
+// in blocks of 32 rows x 16 columns, which is what a warp handles at once: 8 columns of 32 rows, then the other 8.
 struct Matrices {
-  __half* p;
+  __half *p, *low;
   int rows, cols, ld, count;
-  long long each, plane;
+  long long each, low_each;
 };
+inline long long block_rows(int rows) { return (rows + 31) / 32 * 32; }
 
 // What the last product's epilogue needs of a matrix; lies in the workspace.
 struct Target {
@@ -36,7 +39,7 @@ struct Product {
   int M, N, K;
   float alpha, beta, diagonal;
   const Matrices* d;      // nullptr: no second term
-  int d_high, d_low;      // which of its planes
+  int d_high, d_low;      // which of its planes (both: precise; the second alone: in blocks)
   int symmetric;          // C = C^T: tiles above the diagonal only, and mirrored
   int c_low;              // the second plane of C is written
   const Target* target;   // the last product: the matrices are updated, nothing is written to c
@@ -47,6 +50,10 @@ constexpr int MAX_GROUPS = 4;
 ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* products, int n, cudaStream_t st);
 
 #ifdef __CUDACC__
+// Where 8 columns (octet of them) of one row lie in a second plane of blocks.
+__device__ __forceinline__ long long block_at(int row, int octet, int ld) {
+  return (static_cast<long long>(row >> 5) * (ld >> 4) + (octet >> 1)) * 512 + (octet & 1) * 256 + (row & 31) * 8;
+}
 // One value's two planes.
 __device__ __forceinline__ void split_half(float x, __half* hi, __half* lo) {
   *hi = __float2half_rn(x);

@@ -35,7 +35,10 @@ constexpr int BLOCK64_BYTES = 64 * BLOCK_K * 2;
 constexpr int TMEM_COLS = 512;
 constexpr int BAR_BYTES = 256;
 constexpr int MAX_SMEM = 232448;
-constexpr int RING_BYTES = (MAX_SMEM - 1024 - BAR_BYTES) / 1024 * 1024;
+// Outputs leave through shared memory: 32 x 32 values of a warp at a time, one TMA store to a plane, and another to the mirror
+// image.  (A row to a lane, as the sums lie in tensor memory, every store falls into 32 lines: 11 us for a tile of X instead of
+// TILE_US.)  What is left holds the ring.
+constexpr int BOX = 32, BOX_BYTES = BOX * BOX * 2;
 // An epilogue reads 2 bytes of every value and writes 4 while the tensor cores take 17 us over a tile (K = 4096): with 8 warps,
 // each waiting for its next 16 columns, it took 35 us.  precise: 8, for the sake of their registers.
 template <bool PRECISE> constexpr int EPI_WARPS = PRECISE ? 8 : 16;
@@ -49,23 +52,24 @@ template <bool PRECISE> constexpr int GEMM_THREADS = 32 * (EPI_WARPS<PRECISE> + 
 constexpr int PROMOTE = 4;
 
 struct DevProduct {
-  CUtensorMap a, b;
+  CUtensorMap a, b, c;
   int M, N, kb, count;
   int a_mn, b_mn, symmetric;
   int tiles_m, tiles_n, tiles, panel_m;
   int unit0;
   float alpha, beta, beta_low, diagonal;
   const __half *D, *D_low;    // either may be missing
-  long long d_each;
+  long long d_each, d_low_each;
   int ldd;
-  __half* C;
-  long long c_each, c_plane;
-  int ldc, c_low;
+  __half* C_low;              // in blocks, or nullptr
+  long long c_low_each;
+  int ldc;
   const Target* target;
 };
 struct Params {
   DevProduct prod[MAX_GROUPS];
   int n, units, tile_n, stages, stage_bytes;
+  int ring_bytes, out_bytes;  // out_bytes: of one epilogue warp
   int* status;
 };
 struct Unit {
@@ -104,11 +108,37 @@ __device__ __forceinline__ int part_end(int kb, int begin) {
 }
 
 __device__ __forceinline__ float2 half_pair(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-__device__ __forceinline__ void store32_bytes(void* base, const uint32_t* w) {   // 32-byte aligned
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(base), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
-               "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
+// 16 columns of one row in a second plane of blocks.
+__device__ __forceinline__ void store_block(__half* at, const uint32_t* w) {
+  reinterpret_cast<uint4*>(at)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  reinterpret_cast<uint4*>(at)[32] = make_uint4(w[4], w[5], w[6], w[7]);
 }
+__device__ __forceinline__ void load_block(const __half* at, uint32_t* w) {
+  const uint4 x = __ldcg(reinterpret_cast<const uint4*>(at)), y = __ldcg(reinterpret_cast<const uint4*>(at) + 32);
+  w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; w[4] = y.x; w[5] = y.y; w[6] = y.z; w[7] = y.w;
+}
+// 16 columns of a lane's row into a box of 32 x 32 with the 64-byte swizzle: 16-byte piece j of row r at j ^ (r / 2 % 4).
+__device__ __forceinline__ void stage16(uint8_t* buf, int lane, int col, const uint32_t* w) {
+  uint8_t* row = buf + lane * (BOX * 2);
+  const int turn = (lane >> 1) & 3, j = col >> 3;
+  *reinterpret_cast<uint4*>(row + ((j ^ turn) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+  *reinterpret_cast<uint4*>(row + (((j + 1) ^ turn) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+}
+// The same, rows and columns exchanged.  (Four addresses, the rest are immediate offsets: sixteen of them in registers spilled.)
+__device__ __forceinline__ void stage16_turned(uint8_t* buf, int lane, int col, const uint32_t* w) {
+  const uint32_t base = ptx::smem_u32(buf) + (lane & 7) * 2;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t at = base + (((lane >> 3) ^ q) << 4);
+#pragma unroll
+    for (int i = 2 * q; i < 16; i += 8) {       // rows i and i + 1
+      const uint32_t to = at + (col + i) * (BOX * 2);
+      asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"(static_cast<unsigned short>(w[i >> 1])) : "memory");
+      asm volatile("st.shared.u16 [%0 + 64], %1;" ::"r"(to), "h"(static_cast<unsigned short>(w[i >> 1] >> 16)) : "memory");
+    }
+  }
+}
+static_assert(BOX * 2 == 64, "the offset of the next row");
 __device__ __forceinline__ void load32_bytes(const void* base, uint32_t* w) {
   asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
@@ -186,13 +216,15 @@ __device__ __forceinline__ void update16(const Target& t, long long row, int n0,
   }
 }
 
-template <bool PRECISE>
+// LAST: the matrices are updated with the product.
+template <bool PRECISE, bool LAST>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE>, 1) muon_gemm_kernel(const __grid_constant__ Params p) {
   constexpr int FIRST = FIRST_EPI<PRECISE>;
   const int half_n = p.tile_n / 2;          // rows of B that one CTA stages
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RING_BYTES);
+  uint8_t* out_stage = smem + p.ring_bytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(out_stage + EPI_WARPS<PRECISE> * p.out_bytes);
   uint64_t* full = bars;                    // [stages] TMA of both CTAs -> MMA (rank 0's are used)
   uint64_t* empty = full + MAX_STAGES;      // [stages] MMA -> TMA, one set in each CTA
   uint64_t* tfull = empty + MAX_STAGES;     // [2] MMA -> epilogue, one set in each CTA
@@ -344,6 +376,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
     const int cols = p.tile_n / GROUPS<PRECISE>;                    // columns of this warp's part of the tile
     const int col0 = ((warp - FIRST) >> 2) * cols;
     const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + col0;
+    uint8_t* buf = out_stage + (warp - FIRST) * p.out_bytes;
     uint32_t tl = 0;
     bool live = true;
     for (int u = first_unit; u < p.units && live; u += unit_step, ++tl) {
@@ -353,18 +386,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
       const bool in = row < d.M;
       const int c0 = t.n_blk * p.tile_n + col0;
       const int width = d.N - c0 < cols ? d.N - c0 : cols;       // (may be negative)
+      const bool leaves = row0 < d.M;                            // (a warp without rows stores nothing)
       const bool mirror = d.symmetric && t.n_blk * p.tile_n >= (t.m_blk + 1) * TILE_M;
-      const long long d_at = t.batch * d.d_each + static_cast<long long>(row) * d.ldd + c0;
-      const __half *D = d.D && in ? d.D + d_at : nullptr, *D_low = d.D_low && in ? d.D_low + d_at : nullptr;
-      __half* C = d.C + t.batch * d.c_each + static_cast<long long>(row) * d.ldc + c0;
-      // What is added is on its way two pieces of 16 columns ahead: those of the first plane here, or of the second where
-      // there is no first (only precise products have both).
-      const __half* ahead = D ? D : D_low;
-      const float beta = D ? d.beta : d.beta_low;
+      // What is added is on its way two pieces of 16 columns ahead: the first plane of S, or the second of X.
+      const bool blocks = !PRECISE && !d.D;                      // (how that lies)
+      const __half* add = nullptr;
+      if (in && d.D) add = d.D + t.batch * d.d_each + static_cast<long long>(row) * d.ldd + c0;
+      else if (in && blocks && d.D_low) add = d.D_low + t.batch * d.d_low_each + block_at(row, c0 >> 3, d.ldd);
+      const float beta = blocks ? d.beta_low : d.beta;
       uint32_t next[2][8];
-      if (ahead) {
+      const auto load_ahead = [&](int c, uint32_t* w) {
+        if (blocks) load_block(add + c * 32, w);
+        else load32_bytes(add + c, w);
+      };
+      if (add) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) if (16 * k < width) load32_bytes(ahead + 16 * k, next[k]);
+        for (int k = 0; k < 2; ++k) if (16 * k < width) load_ahead(16 * k, next[k]);
       }
       if constexpr (PRECISE) {
         // All parts of the sum but the last are added up in registers; then it goes back to where the last part lies.
@@ -409,51 +446,72 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
         ptx::tc_fence_after();
       }
       const uint32_t acc = tl & 1, t_row = t_quarter + acc * TILE_N;
-#pragma unroll 2
-      for (int c = 0, k = 0; c < width; c += 16, k ^= 1) {
-        float v[16];
-        ptx::tmem_ld16(t_row + c, v);
-        ptx::tmem_ld_wait();
+#pragma unroll 1
+      for (int c0b = 0; c0b < width; c0b += BOX) {
+        if constexpr (!LAST) {
+          // the stores before must have read the buffers
+          if (lane == 0) ptx::tma_store_wait_read();
+          __syncwarp();
+        }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] *= d.alpha;
-        if (ahead) {
-          add16(v, beta, next[k]);
-          if (c + 32 < width) load32_bytes(ahead + c + 32, next[k]);
-        }
-        if (PRECISE && D && D_low) {
-          uint32_t low[8];
-          load32_bytes(D_low + c, low);
-          add16(v, d.beta_low, low);
-        }
-        if (d.diagonal != 0.f && row >= c0 + c && row < c0 + c + 16) {
+        for (int k = 0; k < 2; ++k) {
+          const int c = c0b + 16 * k;
+          if (c >= width) break;
+          float v[16];
+          ptx::tmem_ld16(t_row + c, v);
+          ptx::tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) if (row == c0 + c + i) v[i] += d.diagonal;
-        }
-        if (d.target) {
-          if (in) update16(d.target[t.batch], row, c0 + c, d.N, v);
-          continue;
-        }
-        uint32_t hi[8], lo[8];
+          for (int i = 0; i < 16; ++i) v[i] *= d.alpha;
+          if (add) {
+            add16(v, beta, next[k]);
+            if (c + 32 < width) load_ahead(c + 32, next[k]);
+            if (PRECISE && !LAST && d.D_low) {
+              uint32_t low[8];
+              load32_bytes(d.D_low + (add - d.D) + c, low);
+              add16(v, d.beta_low, low);
+            }
+          }
+          if (!LAST && d.diagonal != 0.f && row >= c0 + c && row < c0 + c + 16) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          hi[i] = pair_half(v[2 * i], v[2 * i + 1]);
-          const float2 x = half_pair(hi[i]);
-          lo[i] = pair_half((v[2 * i] - x.x) * LOW, (v[2 * i + 1] - x.y) * LOW);
-        }
-        if (in) {
-          store32_bytes(C + c, hi);
-          if (d.c_low) store32_bytes(C + d.c_plane + c, lo);
-        }
-        if (mirror) {
-          // the 32 rows of this warp lie side by side in the mirror image
-          __half* T = d.C + t.batch * d.c_each + static_cast<long long>(c0 + c) * d.ldc + row;
-          const unsigned short* h = reinterpret_cast<const unsigned short*>(hi);
-          const unsigned short* l = reinterpret_cast<const unsigned short*>(lo);
+            for (int i = 0; i < 16; ++i) if (row == c0 + c + i) v[i] += d.diagonal;
+          }
+          if constexpr (LAST) {
+            if (in) update16(d.target[t.batch], row, c0 + c, d.N, v);
+            continue;
+          }
+          uint32_t w[8];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if (!in || c + i >= width) continue;
-            *reinterpret_cast<unsigned short*>(T + static_cast<long long>(i) * d.ldc) = h[i];
-            if (d.c_low) *reinterpret_cast<unsigned short*>(T + d.c_plane + static_cast<long long>(i) * d.ldc) = l[i];
+          for (int i = 0; i < 8; ++i) {
+            w[i] = pair_half(v[2 * i], v[2 * i + 1]);
+            const float2 x = half_pair(w[i]);
+            v[2 * i] = (v[2 * i] - x.x) * LOW;
+            v[2 * i + 1] = (v[2 * i + 1] - x.y) * LOW;
+          }
+          stage16(buf, lane, 16 * k, w);
+          if (mirror) stage16_turned(buf + (PRECISE ? 2 : 1) * BOX_BYTES, lane, 16 * k, w);
+          if (PRECISE || d.C_low) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = pair_half(v[2 * i], v[2 * i + 1]);
+            if (!PRECISE) {
+              if (in) store_block(d.C_low + t.batch * d.c_low_each + block_at(row, (c0 + c) >> 3, d.ldc), w);
+            } else {
+              stage16(buf + BOX_BYTES, lane, 16 * k, w);
+              if (mirror) stage16_turned(buf + 3 * BOX_BYTES, lane, 16 * k, w);
+            }
+          }
+        }
+        if constexpr (!LAST) {
+          ptx::fence_proxy_async();
+          __syncwarp();
+          if (lane == 0 && leaves) {
+            const int n0 = c0 + c0b;
+            const uint32_t from = ptx::smem_u32(buf);
+            ptx::tma_store_3d(&d.c, from, n0, row0, t.batch);
+            if (PRECISE) ptx::tma_store_3d(&d.c, from + BOX_BYTES, n0, row0, d.count + t.batch);
+            if (mirror) {
+              ptx::tma_store_3d(&d.c, from + (PRECISE ? 2 : 1) * BOX_BYTES, row0, n0, t.batch);
+              if (PRECISE) ptx::tma_store_3d(&d.c, from + 3 * BOX_BYTES, row0, n0, d.count + t.batch);
+            }
           }
         }
       }
@@ -461,6 +519,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(&tempty[acc]), 0));
     }
+    if (lane == 0) ptx::tma_store_wait();
   }
 
   ptx::tc_fence_before();
@@ -479,8 +538,9 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Tensor map over [2 planes x count][rows][cols]; box of 64 columns by box_rows rows, 128-byte swizzle, zeros outside.
-ffsplit_status encode(ffsplit_ctx* ctx, const Matrices& m, int box_rows, int planes, CUtensorMap* out) {
+// Tensor map over [planes x count][rows][cols]; box of 64 (32) columns by box_rows rows, 128-byte (64-byte) swizzle, zeros
+// outside.
+ffsplit_status encode(ffsplit_ctx* ctx, const Matrices& m, int box_cols, int box_rows, int planes, CUtensorMap* out) {
   if (!ctx->encode_fn) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult qres;
@@ -492,10 +552,10 @@ ffsplit_status encode(ffsplit_ctx* ctx, const Matrices& m, int box_rows, int pla
   // (the second plane follows the first without a gap, so both are one run of matrices)
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows), static_cast<cuuint64_t>(m.count) * planes};
   cuuint64_t strides[2] = {static_cast<cuuint64_t>(m.ld) * 2, static_cast<cuuint64_t>(m.each) * 2};
-  cuuint32_t box[3] = {BLOCK_K, static_cast<cuuint32_t>(box_rows), 1}, estr[3] = {1, 1, 1};
+  cuuint32_t box[3] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows), 1}, estr[3] = {1, 1, 1};
   const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_fn)(
       out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, m.p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+      box_cols == BOX ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(ctx, FFSPLIT_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
   return FFSPLIT_OK;
 }
@@ -514,9 +574,11 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
   // The tensor maps are made by a driver call, which needs a current context (see train_gemm.cu).
   const cudaError_t bound = cudaSetDevice(ctx->device);
   if (bound != cudaSuccess) return check_cuda(ctx, bound, "cudaSetDevice");
-  const unsigned bit = precise ? 2u : 1u;
+  const bool last = products[0].target != nullptr;      // (all of a launch, or none)
+  const unsigned bit = 1u << ((precise ? 2 : 0) + (last ? 1 : 0));
+  const auto kernel = precise ? (last ? muon_gemm_kernel<true, true> : muon_gemm_kernel<true, false>)
+                              : (last ? muon_gemm_kernel<false, true> : muon_gemm_kernel<false, false>);
   if (!(ctx->attr_muon_set & bit)) {
-    const auto kernel = precise ? muon_gemm_kernel<true> : muon_gemm_kernel<false>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
     if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(muon_gemm_kernel)");
     if (precise) {
@@ -549,15 +611,21 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
     if (((narrow + clusters_max - 1) / clusters_max) * 0.2 < ((wide + clusters_max - 1) / clusters_max) * 0.27) p.tile_n = 128;
   }
   p.stage_bytes = (CTA_M + p.tile_n / 2) * BLOCK_K * 2;
-  p.stages = RING_BYTES / p.stage_bytes < MAX_STAGES ? RING_BYTES / p.stage_bytes : MAX_STAGES;
+  bool mirrored = false;
+  for (int i = 0; i < n; ++i) mirrored = mirrored || products[i].symmetric;
+  p.out_bytes = (precise ? 2 : 1) * (mirrored ? 2 : last ? 0 : 1) * BOX_BYTES;
+  const int room = MAX_SMEM - 1024 - BAR_BYTES - (precise ? EPI_WARPS<true> : EPI_WARPS<false>) * p.out_bytes;
+  p.stages = room / p.stage_bytes < MAX_STAGES ? room / p.stage_bytes : MAX_STAGES;
+  p.ring_bytes = p.stages * p.stage_bytes;
   long long units = 0;
   for (int i = 0; i < n; ++i) {
     const Product& g = products[order[i]];
     DevProduct& d = p.prod[i];
     ffsplit_status s;
     const int planes = precise ? 2 : 1;
-    if ((s = encode(ctx, g.a, g.a_mn ? BLOCK_K : CTA_M, planes, &d.a)) != FFSPLIT_OK) return s;
-    if ((s = encode(ctx, g.b, g.b_mn ? BLOCK_K : p.tile_n / 2, planes, &d.b)) != FFSPLIT_OK) return s;
+    if ((s = encode(ctx, g.a, BLOCK_K, g.a_mn ? BLOCK_K : CTA_M, planes, &d.a)) != FFSPLIT_OK) return s;
+    if ((s = encode(ctx, g.b, BLOCK_K, g.b_mn ? BLOCK_K : p.tile_n / 2, planes, &d.b)) != FFSPLIT_OK) return s;
+    if (!g.target && (s = encode(ctx, g.c, BOX, BOX, planes, &d.c)) != FFSPLIT_OK) return s;
     d.M = g.M; d.N = g.N; d.count = g.c.count;
     d.kb = (g.K + BLOCK_K - 1) / BLOCK_K;
     d.a_mn = g.a_mn; d.b_mn = g.b_mn; d.symmetric = g.symmetric;
@@ -568,12 +636,13 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
     d.alpha = g.alpha; d.beta = g.beta;
     if (g.d) {
       d.D = g.d_high ? g.d->p : nullptr;
-      d.D_low = g.d_low ? g.d->p + g.d->plane : nullptr;
-      d.d_each = g.d->each; d.ldd = g.d->ld;
+      d.D_low = g.d_low ? g.d->low : nullptr;
+      d.d_each = g.d->each; d.d_low_each = g.d->low_each; d.ldd = g.d->ld;
     }
     d.beta_low = g.beta * (1.f / LOW);
     d.diagonal = g.diagonal * HELD;
-    d.C = g.c.p; d.c_each = g.c.each; d.c_plane = g.c.plane; d.ldc = g.c.ld; d.c_low = g.c_low;
+    d.C_low = g.c_low && !precise ? g.c.low : nullptr;
+    d.c_low_each = g.c.low_each; d.ldc = g.c.ld;
     d.target = g.target;
     // panel height: the tiles in flight form a block whose two sides carry about the same operand bytes
     d.panel_m = 1;
@@ -590,8 +659,7 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
   p.units = static_cast<int>(units);
   p.status = ctx->status();
   const int clusters = units < clusters_max ? static_cast<int>(units) : clusters_max;
-  const cudaError_t e = precise ? launch_pdl(muon_gemm_kernel<true>, dim3(2 * clusters), dim3(GEMM_THREADS<true>), MAX_SMEM, st, p)
-                                : launch_pdl(muon_gemm_kernel<false>, dim3(2 * clusters), dim3(GEMM_THREADS<false>), MAX_SMEM, st, p);
+  const cudaError_t e = launch_pdl(kernel, dim3(2 * clusters), dim3(precise ? GEMM_THREADS<true> : GEMM_THREADS<false>), MAX_SMEM, st, p);
   ctx->launches++;
   return check_cuda(ctx, e, "muon_gemm_kernel launch");
 }
