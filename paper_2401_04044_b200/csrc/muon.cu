@@ -29,13 +29,16 @@ struct Entry {
   __half *X, *X_low;      // [rows][ld], and the second plane: likewise, or in blocks
   int blocks;
   int rows, cols, octets; // octets of columns in a row
-  int g_f32, w_f32, wide; // wide: every octet of G, M, Mo starts on 16 bytes
+  int g_f32, w_f32;
+  int wide, wide_w;       // every octet of G, M, Mo (of W, out) starts on 16 bytes
   int ld;
-  int parts, block0;
+  int parts;
   float step, decay;
 };
+// (The argument block is copied with every launch and read through the constant cache: a short list gets a short one.)
+template <int CAP>
 struct Table {
-  Entry t[MAX_TENSORS];
+  Entry t[CAP];
   int n;
   float beta;
   int nesterov;
@@ -86,15 +89,6 @@ __device__ __forceinline__ void load_u8(const Entry& e, float beta, int nesterov
     }
   }
 }
-__device__ __forceinline__ const Entry& entry_of(const Table& t, int block, int* which) {
-  int lo = 0, hi = t.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.t[mid].block0 <= block) lo = mid; else hi = mid - 1;
-  }
-  *which = lo;
-  return t.t[lo];
-}
 // A matrix is gone through in pieces of 32 rows x 64 columns, eight columns to a thread: eight threads read a line of G, and what
 // a piece leaves in a second plane of blocks is whole sectors.  Pieces begin .. end of block `part`.
 __device__ __forceinline__ int pieces_across(const Entry& e) { return (e.octets + 7) / 8; }
@@ -120,12 +114,14 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
   return t;
 }
 
-__global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ Table t) {
+// A row of blocks to a matrix; those behind its parts have nothing to do.
+template <int CAP>
+__global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ Table<CAP> t) {
   __shared__ double red[THREADS / 32];
   pdl_wait();
-  int which;
-  const Entry& e = entry_of(t, blockIdx.x, &which);
-  const int part = blockIdx.x - e.block0;
+  const int which = blockIdx.y, part = blockIdx.x;
+  const Entry& e = t.t[which];
+  if (part >= e.parts) return;
   int begin, end;
   range_of(e, part, &begin, &end);
   double acc = 0.0;
@@ -143,12 +139,13 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ T
 }
 
 // X = U / (norm + 1e-7), M', and what the last product does with the matrix.
-__global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant__ Table t) {
+template <int CAP>
+__global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant__ Table<CAP> t) {
   __shared__ double red[THREADS / 32];
   pdl_wait();
-  int which;
-  const Entry& e = entry_of(t, blockIdx.x, &which);
-  const int part = blockIdx.x - e.block0;
+  const int which = blockIdx.y, part = blockIdx.x;
+  const Entry& e = t.t[which];
+  if (part >= e.parts) return;
   const double squares = block_sum(threadIdx.x < e.parts ? __ldcg(t.partial + which * MAX_PARTS + threadIdx.x) : 0.0, red);
   const float norm = static_cast<float>(sqrt(squares));
   const bool finite = isfinite(norm);
@@ -156,7 +153,7 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
   if (part == 0 && threadIdx.x == 0) {
     Target o;
     o.W = e.W; o.out = e.out; o.f32 = e.w_f32;
-    o.wide = e.cols % 8 == 0 && ((reinterpret_cast<uintptr_t>(e.W) | reinterpret_cast<uintptr_t>(e.out)) & 15u) == 0;
+    o.wide = e.wide_w;
     o.keep = finite ? 1.0f - e.decay : 1.0f;
     o.step = e.W ? (finite ? e.step : 0.f) : finite ? -1.0f : __int_as_float(0x7fffffff);
     t.target[which] = o;
@@ -196,44 +193,67 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------------ thin matrices
-// p = min(rows, cols) <= 32 (an adapter's factors): the tensor cores' tiles would be nearly empty, and 15 launches are what
+// p = min(rows, cols) <= 64 (an adapter's factors): the tensor cores' tiles would be nearly empty, and 15 launches are what
 // the work is not.  X stays in the row space of U, so X_n = Q U with Q a polynomial in S = U U^T: one pass over U for S, the
 // iteration on p x p matrices (S <- A S A, Q <- A Q, A = a I + b S + c S S), one pass for Q U.  S has the squares of U's
-// singular values and Q their inverses: all of that is held in fp64, so that nothing is lost over the direct form; Q U is
-// taken in fp32 where the gradient is bf16 (4e-5 at worst: entries of Q reach 485 / |U| and cancel to 0.7).
-// Bound by reading U twice; the fp64 units take 3 us of it for 32 matrices of p = 16, q = 8000.
-constexpr int THIN = 32, THIN_PARTS = 32, THIN_CHUNK = 128;
+// singular values and Q their inverses: all of that is held in fp64, so that nothing is lost over the direct form.
+// The products are fp64 matrix instructions of 8 x 8 x 4 (with scalar ones the loads from shared memory were the bound: 100 us
+// for 32 factors of rank 16).
+constexpr int THIN = 64, THIN_PARTS = 64;
+constexpr int SQUARE_PITCH = THIN + 4;      // doubles: the 4 rows x 4 columns of half a fragment fall into 32 banks
+constexpr int WARPS = THREADS / 32;
+// p in tiles of 8, 1, 2, 4 or 8 of them; a block takes so many of U's columns at a time that every thread has two octets.
+__host__ __device__ __forceinline__ int thin_tiles(int p) { return p <= 8 ? 1 : p <= 16 ? 2 : p <= 32 ? 4 : 8; }
+__host__ __device__ __forceinline__ int thin_chunk(int tiles) { return 512 / tiles; }
+constexpr size_t THIN_U_BYTES = (8 * 512 + 8 * 4 * 8) * sizeof(double);      // the most that 8 tiles (chunk + 4) takes
+inline size_t square_bytes(int tiles) { return static_cast<size_t>(tiles) * 8 * SQUARE_PITCH * sizeof(double); }
+template <int CAP>
 struct ThinTable {
-  Entry t[MAX_TENSORS];
-  double* S[MAX_TENSORS];      // [parts][p][p]
-  double* Q[MAX_TENSORS];      // [p][p], for U itself (not divided by its norm)
+  Entry t[CAP];
+  double* S[CAP];      // [parts][p][p]
+  double* Q[CAP];      // [p][p], for U itself (not divided by its norm)
   int n;
+  int tiles;           // thin_tiles() of the largest p
   float beta;
   int nesterov, iterations;
   float coefficients[48];
   int* status;
 };
-// Columns (rows, where the matrix is tall) [begin, end) of U as u[i][k - begin], i < p, zeros behind `end`; M' is written.
-template <typename R, bool WRITE>
-__device__ __forceinline__ void load_thin(const Entry& e, float beta, int nesterov, int begin, int end, bool write_m, R (*u)[THIN_CHUNK + 1]) {
+typedef double (*Square)[SQUARE_PITCH];
+
+// c (8 x 8) += a (8 x 4) b (4 x 8): lane l holds a[l / 4][l % 4], b[l % 4][l / 4], c[l / 4][2 (l % 4) + {0, 1}].
+__device__ __forceinline__ void mma8(double* c, double a, double b) {
+  asm volatile("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};" : "+d"(c[0]), "+d"(c[1]) : "d"(a), "d"(b));
+}
+// `chunk` columns (rows, where the matrix is tall) of U from `begin` on as u[i * pitch + k], i < p, zeros behind the last; M' is
+// written.
+template <bool WRITE>
+__device__ __forceinline__ void load_thin(const Entry& e, float beta, int nesterov, int begin, int chunk, bool write_m, double* u) {
   const bool tall = e.rows > e.cols;
-  const int p = tall ? e.cols : e.rows;
-  const int across = tall ? e.octets : (end - begin + 7) / 8, octets = (tall ? end - begin : p) * across;
+  const int p = tall ? e.cols : e.rows, pitch = chunk + 4;
+  const int across = tall ? e.octets : chunk / 8, octets = (tall ? chunk : p) * across;
+#pragma unroll 2
   for (int o = threadIdx.x; o < octets; o += THREADS) {
     const int r = o / across, row = tall ? begin + r : r, octet = (tall ? 0 : begin / 8) + o - r * across;
     float m[8], x[8];
-    load_u8(e, beta, nesterov, row, octet, m, x);
+    const bool in = row < e.rows && octet < e.octets;
+    if (in) {
+      load_u8(e, beta, nesterov, row, octet, m, x);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int c = octet * 8 + k;
-      if (tall) {
-        if (c < p) u[c][row - begin] = x[k];
-      } else {
-        u[row][c - begin] = x[k];      // (zero behind the last column)
-      }
+      for (int k = 0; k < 8; ++k) x[k] = 0.f;
+    }
+    if (!tall) {      // (zero behind the last column)
+      double* to = u + row * pitch + octet * 8 - begin;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) to[k] = x[k];
+    } else {
+      double* to = u + octet * 8 * pitch + r;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) if (octet * 8 + k < p) to[k * pitch] = x[k];
     }
     if constexpr (WRITE) {
-      if (e.M) {
+      if (e.M && in) {
         const long long at = static_cast<long long>(row) * e.cols + octet * 8;
         if (!write_m) {
 #pragma unroll
@@ -251,159 +271,235 @@ __device__ __forceinline__ void load_thin(const Entry& e, float beta, int nester
   }
 }
 // Columns of part `part` of a matrix: whole chunks.
-__device__ __forceinline__ void thin_range(const Entry& e, int part, int* begin, int* end) {
-  const int q = e.rows > e.cols ? e.rows : e.cols, chunks = (q + THIN_CHUNK - 1) / THIN_CHUNK, per = (chunks + e.parts - 1) / e.parts;
-  *begin = part * per * THIN_CHUNK;
-  *end = *begin + per * THIN_CHUNK < q ? *begin + per * THIN_CHUNK : q;
+__device__ __forceinline__ void thin_range(const Entry& e, int part, int chunk, int* begin, int* end) {
+  const int q = e.rows > e.cols ? e.rows : e.cols, chunks = (q + chunk - 1) / chunk, per = (chunks + e.parts - 1) / e.parts;
+  *begin = part * per * chunk;
+  *end = *begin + per * chunk < q ? *begin + per * chunk : q;
 }
 
-__global__ void __launch_bounds__(THREADS) thin_gram_kernel(const __grid_constant__ ThinTable t) {
-  __shared__ double u[THIN][THIN_CHUNK + 1];
+// Partial sums of S: a warp to a row of tiles; where there are fewer than eight, the warps share the columns of a chunk.
+template <int CAP>
+__global__ void __launch_bounds__(THREADS) thin_gram_kernel(const __grid_constant__ ThinTable<CAP> t) {
+  extern __shared__ double thin_smem[];
+  double* u = thin_smem;
   pdl_wait();
-  int which = 0;
-  while (which + 1 < t.n && static_cast<int>(blockIdx.x) >= t.t[which + 1].block0) ++which;
+  const int which = blockIdx.y, part = blockIdx.x;
   const Entry& e = t.t[which];
-  const int part = blockIdx.x - e.block0, p = e.rows > e.cols ? e.cols : e.rows;
+  if (part >= e.parts) return;
+  const int p = e.rows > e.cols ? e.cols : e.rows, tiles = thin_tiles(p), chunk = thin_chunk(tiles), pitch = chunk + 4, groups = WARPS / tiles;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ti = warp % tiles, group = warp / tiles;
   int begin, end;
-  thin_range(e, part, &begin, &end);
-  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  double s00 = 0.0, s01 = 0.0, s11 = 0.0, s10 = 0.0;
-  for (int k0 = begin; k0 < end; k0 += THIN_CHUNK) {
-    const int k1 = end - k0 < THIN_CHUNK ? end : k0 + THIN_CHUNK;
+  thin_range(e, part, chunk, &begin, &end);
+  double c[8][2] = {};
+  const double* mine = u + (lane >> 2) * pitch + (lane & 3);
+  for (int k0 = begin; k0 < end; k0 += chunk) {
     __syncthreads();
-    load_thin<double, false>(e, t.beta, t.nesterov, k0, k1, false, u);
+    load_thin<false>(e, t.beta, t.nesterov, k0, chunk, false, u);
     __syncthreads();
-    if (ty >= p || tx >= p) continue;
-    if (p <= 16) {
-#pragma unroll 4
-      for (int k = 0; k < k1 - k0; ++k) s00 = fma(u[ty][k], u[tx][k], s00);
-    } else {
-      // (rows behind p hold what was there before: their sums are not written)
-#pragma unroll 4
-      for (int k = 0; k < k1 - k0; ++k) {
-        const double a = u[ty][k], b = u[ty + 16][k], c = u[tx][k], d = u[tx + 16][k];
-        s00 = fma(a, c, s00); s01 = fma(a, d, s01); s10 = fma(b, c, s10); s11 = fma(b, d, s11);
+    // (rows behind p hold anything: their sums are not written)
+#pragma unroll 2
+    for (int k = group * 4; k < chunk; k += 4 * groups) {
+      const double a = mine[8 * ti * pitch + k];
+#pragma unroll
+      for (int tj = 0; tj < 8; ++tj) {
+        if (tj >= tiles) break;
+        mma8(c[tj], a, mine[8 * tj * pitch + k]);
       }
     }
   }
+  // the groups' sums, one after the other
+  const Square sum = reinterpret_cast<Square>(thin_smem);
+  for (int g = 0; g < groups; ++g) {
+    __syncthreads();
+    if (group == g) {
+#pragma unroll
+      for (int tj = 0; tj < 8; ++tj) {
+        if (tj >= tiles) break;
+        double* to = &sum[8 * ti + (lane >> 2)][8 * tj + 2 * (lane & 3)];
+        to[0] = g == 0 ? c[tj][0] : to[0] + c[tj][0];
+        to[1] = g == 0 ? c[tj][1] : to[1] + c[tj][1];
+      }
+    }
+  }
+  __syncthreads();
   double* S = t.S[which] + static_cast<long long>(part) * p * p;
-  if (ty < p && tx < p) S[ty * p + tx] = s00;
-  if (ty < p && tx + 16 < p) S[ty * p + tx + 16] = s01;
-  if (ty + 16 < p && tx < p) S[(ty + 16) * p + tx] = s10;
-  if (ty + 16 < p && tx + 16 < p) S[(ty + 16) * p + tx + 16] = s11;
+  for (int i = threadIdx.x; i < p * p; i += THREADS) S[i] = sum[i / p][i % p];
 }
 
-// C = A B, each p x p (padded with zeros to 32); a thread to four entries.
-__device__ __forceinline__ void thin_product(const double (*A)[THIN + 1], const double (*B)[THIN + 1], int p, double* c) {
-  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  c[0] = c[1] = c[2] = c[3] = 0.0;
+// C = A B of tiles x tiles tiles: f(row, column, two values) for every pair of C.  Everything is symmetric up to rounding (all
+// are polynomials in S), so B is read along its rows like A.
+template <typename F>
+__device__ __forceinline__ void thin_product(const Square A, const Square B, int tiles, F f) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = warp; i < tiles * tiles; i += blockDim.x / 32) {
+    const int ti = i / tiles, tj = i - ti * tiles;
+    double c[2][2] = {};
 #pragma unroll 4
-  for (int k = 0; k < p; ++k) {
-    const double a = A[ty][k], b = A[ty + 16][k], x = B[k][tx], y = B[k][tx + 16];
-    c[0] = fma(a, x, c[0]); c[1] = fma(a, y, c[1]); c[2] = fma(b, x, c[2]); c[3] = fma(b, y, c[3]);
+    for (int k = 0; k < 8 * tiles; k += 8) {
+      mma8(c[0], A[8 * ti + (lane >> 2)][k + (lane & 3)], B[8 * tj + (lane >> 2)][k + (lane & 3)]);
+      mma8(c[1], A[8 * ti + (lane >> 2)][k + 4 + (lane & 3)], B[8 * tj + (lane >> 2)][k + 4 + (lane & 3)]);
+    }
+    f(8 * ti + (lane >> 2), 8 * tj + 2 * (lane & 3), c[0][0] + c[1][0], c[0][1] + c[1][1]);
   }
 }
-__global__ void __launch_bounds__(THREADS) thin_solve_kernel(const __grid_constant__ ThinTable t) {
-  __shared__ double S[THIN][THIN + 1], A[THIN][THIN + 1], Q[THIN][THIN + 1];
+constexpr int SOLVE_THREADS = 512;
+template <int CAP>
+__global__ void __launch_bounds__(SOLVE_THREADS) thin_solve_kernel(const __grid_constant__ ThinTable<CAP> t) {
+  extern __shared__ double thin_smem[];
   __shared__ double norm;
+  const int rows = t.tiles * 8;
+  // S and Q move between two buffers each
+  const Square S0 = reinterpret_cast<Square>(thin_smem), S1 = S0 + rows, Q0 = S1 + rows, Q1 = Q0 + rows, A = Q1 + rows;
   pdl_wait();
   const Entry& e = t.t[blockIdx.x];
-  const int p = e.rows > e.cols ? e.cols : e.rows;
+  const int p = e.rows > e.cols ? e.cols : e.rows, tiles = (p + 7) / 8;
   const double* partial = t.S[blockIdx.x];
-  for (int i = threadIdx.x; i < THIN * THIN; i += THREADS) {
-    const int r = i / THIN, c = i % THIN;
+  for (int i = threadIdx.x; i < 64 * tiles * tiles; i += SOLVE_THREADS) {
+    const int r = i / (8 * tiles), c = i % (8 * tiles);
     double s = 0.0;
     if (r < p && c < p) {
 #pragma unroll 8
       for (int k = 0; k < e.parts; ++k) s += __ldcg(partial + static_cast<long long>(k) * p * p + r * p + c);
     }
-    S[r][c] = s;
-    Q[r][c] = r == c ? 1.0 : 0.0;
+    S0[r][c] = s;
+    Q0[r][c] = r == c ? 1.0 : 0.0;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x < 32) {
     double trace = 0.0;
-    for (int i = 0; i < p; ++i) trace += S[i][i];
-    norm = sqrt(trace);
+    for (int i = threadIdx.x; i < p; i += 32) trace += S0[i][i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) trace += __shfl_xor_sync(0xffffffffu, trace, o);
+    if (threadIdx.x == 0) norm = sqrt(trace);
   }
   __syncthreads();
   const bool finite = isfinite(static_cast<float>(norm));
   const double inv = finite ? 1.0 / (norm + 1e-7) : 0.0;
-  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  const int row[4] = {ty, ty, ty + 16, ty + 16}, col[4] = {tx, tx + 16, tx, tx + 16};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) S[row[i]][col[i]] *= inv * inv;
+  for (int i = threadIdx.x; i < 64 * tiles * tiles; i += SOLVE_THREADS) S0[i / (8 * tiles)][i % (8 * tiles)] *= inv * inv;
   __syncthreads();
+  Square S = S0, S_next = S1, Q = Q0, Q_next = Q1;
   for (int it = 0; it < t.iterations && finite; ++it) {
     const double a = t.coefficients[3 * it], b = t.coefficients[3 * it + 1], c = t.coefficients[3 * it + 2];
-    double x[4];
-    thin_product(S, S, p, x);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) A[row[i]][col[i]] = fma(c, x[i], fma(b, S[row[i]][col[i]], row[i] == col[i] ? a : 0.0));
+    thin_product(S, S, tiles, [&](int r, int k, double x, double y) {
+      A[r][k] = fma(c, x, fma(b, S[r][k], r == k ? a : 0.0));
+      A[r][k + 1] = fma(c, y, fma(b, S[r][k + 1], r == k + 1 ? a : 0.0));
+    });
     __syncthreads();
-    double y[4];
-    thin_product(A, Q, p, x);
-    thin_product(A, S, p, y);
+    thin_product(A, Q, tiles, [&](int r, int k, double x, double y) { Q_next[r][k] = x; Q_next[r][k + 1] = y; });
+    thin_product(A, S, tiles, [&](int r, int k, double x, double y) { S_next[r][k] = x; S_next[r][k + 1] = y; });
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { Q[row[i]][col[i]] = x[i]; S[row[i]][col[i]] = y[i]; }
+    thin_product(S_next, A, tiles, [&](int r, int k, double x, double y) { S[r][k] = x; S[r][k + 1] = y; });
     __syncthreads();
-    thin_product(S, A, p, x);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) S[row[i]][col[i]] = x[i];
-    __syncthreads();
+    const Square q = Q;
+    Q = Q_next;
+    Q_next = q;
   }
   // what is not finite leaves here as NaN: the last kernel leaves such a matrix alone
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (row[i] < p && col[i] < p) t.Q[blockIdx.x][row[i] * p + col[i]] = finite ? Q[row[i]][col[i]] * inv : __longlong_as_double(0x7fffffffffffffffll);
+  for (int i = threadIdx.x; i < p * p; i += SOLVE_THREADS)
+    t.Q[blockIdx.x][i] = finite ? Q[i / p][i % p] * inv : __longlong_as_double(0x7fffffffffffffffll);
   if (threadIdx.x == 0 && !finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, blockIdx.x, KID_MUON);
 }
 
-template <typename R>
-__global__ void __launch_bounds__(THREADS) thin_apply_kernel(const __grid_constant__ ThinTable t) {
-  __shared__ R u[THIN][THIN_CHUNK + 1], Q[THIN][THIN];
+// W' = keep W - step Q U for every chunk, and M'.  A warp to every eighth eight columns.
+template <int CAP>
+__global__ void __launch_bounds__(THREADS) thin_apply_kernel(const __grid_constant__ ThinTable<CAP> t) {
+  extern __shared__ double thin_smem[];
   pdl_wait();
-  int which = 0;
-  while (which + 1 < t.n && static_cast<int>(blockIdx.x) >= t.t[which + 1].block0) ++which;
+  const int which = blockIdx.y, part = blockIdx.x;
   const Entry& e = t.t[which];
+  if (part >= e.parts) return;
   const bool tall = e.rows > e.cols;
-  const int p = tall ? e.cols : e.rows, part = blockIdx.x - e.block0;
-  for (int i = threadIdx.x; i < p * p; i += THREADS) Q[i / p][i % p] = static_cast<R>(__ldcg(t.Q[which] + i));
+  const int p = tall ? e.cols : e.rows, tiles = thin_tiles(p), chunk = thin_chunk(tiles), pitch = chunk + 4;
+  double* u = thin_smem + THIN_U_BYTES / sizeof(double);
+  const Square Q = reinterpret_cast<Square>(u);
+  u = thin_smem;
+  for (int i = threadIdx.x; i < 64 * tiles * tiles; i += THREADS) {
+    const int r = i / (8 * tiles), c = i % (8 * tiles);
+    Q[r][c] = r < p && c < p ? __ldcg(t.Q[which] + r * p + c) : 0.0;
+  }
+  for (int i = p * pitch + threadIdx.x; i < 8 * tiles * pitch; i += THREADS) u[i] = 0.0;      // (rows behind p count with a zero of Q: no NaN there)
   int begin, end;
-  thin_range(e, part, &begin, &end);
-  const int k = threadIdx.x & (THIN_CHUNK - 1), group = threadIdx.x / THIN_CHUNK;
-  constexpr int AT_ONCE = 4;
+  thin_range(e, part, chunk, &begin, &end);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool finite = true;
-  for (int k0 = begin; k0 < end; k0 += THIN_CHUNK) {
-    const int k1 = end - k0 < THIN_CHUNK ? end : k0 + THIN_CHUNK;
+  for (int k0 = begin; k0 < end; k0 += chunk) {
     __syncthreads();
     if (k0 == begin) finite = Q[0][0] == Q[0][0];
-    load_thin<R, true>(e, t.beta, t.nesterov, k0, k1, finite, u);
+    load_thin<true>(e, t.beta, t.nesterov, k0, chunk, finite, u);
     __syncthreads();
-    if (k0 + k >= k1) continue;
-    for (int j0 = group * AT_ONCE; j0 < p; j0 += THREADS / THIN_CHUNK * AT_ONCE) {
-      R acc[AT_ONCE] = {};
-      for (int i = 0; i < p; ++i) {
-        const R x = u[i][k];
+    for (int n0 = 8 * warp; n0 < chunk; n0 += 8 * WARPS) {
+      double c[8][2] = {};
+      for (int k = 0; k < 8 * tiles; k += 4) {
+        const double b = u[(k + (lane & 3)) * pitch + n0 + (lane >> 2)];
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) acc[j] = fma(Q[j0 + j < THIN ? j0 + j : 0][i], x, acc[j]);
-      }
-#pragma unroll
-      for (int j = 0; j < AT_ONCE; ++j) {
-        if (j0 + j >= p) break;
-        const long long at = tall ? static_cast<long long>(k0 + k) * e.cols + j0 + j : static_cast<long long>(j0 + j) * e.cols + k0 + k;
-        const float x = static_cast<float>(acc[j]);
-        float o;
-        if (!e.W) {
-          o = x;
-        } else {
-          const float w = e.w_f32 ? static_cast<const float*>(e.W)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(e.W)[at]);
-          o = finite ? fmaf(1.0f - e.decay, w, -e.step * x) : w;
+        for (int ti = 0; ti < 8; ++ti) {
+          if (ti >= tiles) break;
+          mma8(c[ti], Q[8 * ti + (lane >> 2)][k + (lane & 3)], b);
         }
-        if (e.w_f32) static_cast<float*>(e.out)[at] = o;
-        else static_cast<__nv_bfloat16*>(e.out)[at] = __float2bfloat16_rn(o);
+      }
+      __syncwarp();
+      // (a warp reads and writes its own columns only)
+#pragma unroll
+      for (int ti = 0; ti < 8; ++ti) {
+        const int r = 8 * ti + (lane >> 2);
+        if (ti >= tiles || r >= p) break;
+        u[r * pitch + n0 + 2 * (lane & 3)] = c[ti][0];
+        u[r * pitch + n0 + 2 * (lane & 3) + 1] = c[ti][1];
+      }
+      __syncwarp();
+    }
+    __syncthreads();
+    // as load_thin() went over U
+    const int across = tall ? e.octets : chunk / 8, octets = (tall ? chunk : p) * across;
+#pragma unroll 2
+    for (int o = threadIdx.x; o < octets; o += THREADS) {
+      const int r = o / across, row = tall ? k0 + r : r, octet = (tall ? 0 : k0 / 8) + o - r * across;
+      if (row >= e.rows || octet >= e.octets) continue;
+      const long long at = static_cast<long long>(row) * e.cols + octet * 8;
+      const float keep = finite ? 1.0f - e.decay : 1.0f, step = finite ? e.step : 0.f;
+      float x[8], w[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int col = octet * 8 + k;
+        x[k] = static_cast<float>(tall ? (col < p ? u[col * pitch + r] : 0.0) : u[row * pitch + col - k0]);
+        w[k] = 0.f;
+      }
+      if (e.W) {
+        if (e.wide_w && e.w_f32) {
+          const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(e.W) + at);
+          const float4 f = q[0], g = q[1];
+          w[0] = f.x; w[1] = f.y; w[2] = f.z; w[3] = f.w; w[4] = g.x; w[5] = g.y; w[6] = g.z; w[7] = g.w;
+        } else if (e.wide_w) {
+          const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(e.W) + at);
+          const uint32_t v[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            w[2 * k] = __uint_as_float(v[k] << 16);
+            w[2 * k + 1] = __uint_as_float(v[k] & 0xffff0000u);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (octet * 8 + k < e.cols) w[k] = e.w_f32 ? static_cast<const float*>(e.W)[at + k] : __bfloat162float(static_cast<const __nv_bfloat16*>(e.W)[at + k]);
+        }
+        // (where nothing is to be updated Q U is NaN)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = finite ? fmaf(keep, w[k], -step * x[k]) : w[k];
+      }
+      if (e.wide_w && e.w_f32) {
+        float4* q = reinterpret_cast<float4*>(static_cast<float*>(e.out) + at);
+        q[0] = make_float4(x[0], x[1], x[2], x[3]);
+        q[1] = make_float4(x[4], x[5], x[6], x[7]);
+      } else if (e.wide_w) {
+        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(e.out) + at) =
+            make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (octet * 8 + k >= e.cols) break;
+          if (e.w_f32) static_cast<float*>(e.out)[at + k] = x[k];
+          else static_cast<__nv_bfloat16*>(e.out)[at + k] = __float2bfloat16_rn(x[k]);
+        }
       }
     }
   }
@@ -419,9 +515,10 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // Bytes of one matrix's buffers: X twice, S and P, two planes each.
 size_t x_bytes(int rows, int cols) { return static_cast<size_t>(rows + muon::block_rows(rows)) * round_up(cols, 64) * 2; }
-int thin_parts(int rows, int cols) {
-  const int chunks = ((rows < cols ? cols : rows) + muon::THIN_CHUNK - 1) / muon::THIN_CHUNK;
-  return chunks < muon::THIN_PARTS ? chunks : muon::THIN_PARTS;
+int thin_parts(int rows, int cols) {      // (parts are whole chunks)
+  const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows, chunk = muon::thin_chunk(muon::thin_tiles(p));
+  const int chunks = (q + chunk - 1) / chunk, most = chunks < muon::THIN_PARTS ? chunks : muon::THIN_PARTS, per = (chunks + most - 1) / most;
+  return (chunks + per - 1) / per;
 }
 bool is_thin(int rows, int cols) { return (rows < cols ? rows : cols) <= muon::THIN; }
 size_t matrix_bytes(int rows, int cols) {
@@ -535,61 +632,80 @@ muon::Entry entry_for(const ffsplit_muon_tensor& s) {
   e.rows = s.rows; e.cols = s.cols; e.octets = (s.cols + 7) / 8;
   e.g_f32 = s.grad_dtype == FFSPLIT_F32; e.w_f32 = s.weight_dtype == FFSPLIT_F32;
   e.wide = s.cols % 8 == 0 && aligned16(s.grad) && aligned16(s.momentum) && aligned16(s.momentum_out);
+  e.wide_w = s.cols % 8 == 0 && aligned16(s.weight) && aligned16(s.out);
   e.step = s.step; e.decay = s.decay;
   return e;
 }
 
-// The thin matrices of one precision among t: three launches.
-ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, bool precise, float beta, int nesterov, const float* coefficients,
-                        int iterations, char* at, cudaStream_t st) {
-  muon::ThinTable tab;
+// The thin matrices among t: three launches.
+template <int CAP>
+ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, float beta, int nesterov, const float* coefficients, int iterations,
+                        char* at, cudaStream_t st) {
+  muon::ThinTable<CAP> tab;
   std::memset(&tab, 0, sizeof(tab));
   tab.beta = beta; tab.nesterov = nesterov; tab.iterations = iterations;
   for (int i = 0; i < 3 * iterations; ++i) tab.coefficients[i] = coefficients ? coefficients[i] : kStandard[i % 3];
   tab.status = ctx->status();
-  int blocks = 0;
+  int blocks = 0, most = 1;
   for (int i = 0; i < n; ++i) {
     const ffsplit_muon_tensor& s = t[i];
-    if (!is_thin(s.rows, s.cols) || (s.grad_dtype == FFSPLIT_F32) != precise) continue;
-    const int p = s.rows < s.cols ? s.rows : s.cols, parts = thin_parts(s.rows, s.cols);
+    if (!is_thin(s.rows, s.cols)) continue;
+    const int p = s.rows < s.cols ? s.rows : s.cols;
     muon::Entry& e = tab.t[tab.n];
     e = entry_for(s);
-    e.parts = parts;
-    // (parts are whole chunks: fewer of them may do)
-    const int chunks = ((s.rows < s.cols ? s.cols : s.rows) + muon::THIN_CHUNK - 1) / muon::THIN_CHUNK, per = (chunks + parts - 1) / parts;
-    e.parts = (chunks + per - 1) / per;
-    e.block0 = blocks;
-    blocks += e.parts;
+    e.parts = thin_parts(s.rows, s.cols);
     tab.S[tab.n] = reinterpret_cast<double*>(at);
-    tab.Q[tab.n] = tab.S[tab.n] + static_cast<size_t>(parts) * p * p;
+    tab.Q[tab.n] = tab.S[tab.n] + static_cast<size_t>(e.parts) * p * p;
     at += matrix_bytes(s.rows, s.cols);
+    if (p > most) most = p;
+    if (e.parts > blocks) blocks = e.parts;
     ++tab.n;
   }
-  if (tab.n == 0) return FFSPLIT_OK;
-  cudaError_t e = launch_pdl(muon::thin_gram_kernel, dim3(blocks), dim3(muon::THREADS), 0, st, tab);
-  if (e == cudaSuccess) e = launch_pdl(muon::thin_solve_kernel, dim3(tab.n), dim3(muon::THREADS), 0, st, tab);
-  if (e == cudaSuccess) e = precise ? launch_pdl(muon::thin_apply_kernel<double>, dim3(blocks), dim3(muon::THREADS), 0, st, tab)
-                                    : launch_pdl(muon::thin_apply_kernel<float>, dim3(blocks), dim3(muon::THREADS), 0, st, tab);
+  tab.tiles = muon::thin_tiles(most);
+  const int apply_bytes = static_cast<int>(muon::THIN_U_BYTES + muon::square_bytes(tab.tiles));
+  cudaError_t e = cudaFuncSetAttribute(muon::thin_solve_kernel<CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(5 * muon::square_bytes(8)));
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(muon::thin_apply_kernel<CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(muon::THIN_U_BYTES + muon::square_bytes(8)));
+  if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(muon::thin kernels)");
+  e = launch_pdl(muon::thin_gram_kernel<CAP>, dim3(blocks, tab.n), dim3(muon::THREADS), muon::THIN_U_BYTES, st, tab);
+  if (e == cudaSuccess) e = launch_pdl(muon::thin_solve_kernel<CAP>, dim3(tab.n), dim3(muon::SOLVE_THREADS), 5 * muon::square_bytes(tab.tiles), st, tab);
+  if (e == cudaSuccess) e = launch_pdl(muon::thin_apply_kernel<CAP>, dim3(blocks, tab.n), dim3(muon::THREADS), apply_bytes, st, tab);
   ctx->launches += 3;
   return check_cuda(ctx, e, "muon::thin kernels launch");
+}
+
+// The first two passes over the other matrices.
+template <int CAP>
+ffsplit_status run_first(ffsplit_ctx* ctx, const muon::Entry* entries, int n, int blocks, float beta, int nesterov, double* partial, muon::Target* target,
+                         cudaStream_t st) {
+  muon::Table<CAP> tab;
+  std::memset(&tab, 0, sizeof(tab));
+  std::memcpy(tab.t, entries, sizeof(muon::Entry) * n);
+  tab.n = n; tab.beta = beta; tab.nesterov = nesterov;
+  tab.partial = partial; tab.target = target; tab.status = ctx->status();
+  cudaError_t e = launch_pdl(muon::norm_kernel<CAP>, dim3(blocks, n), dim3(muon::THREADS), 0, st, tab);
+  if (e == cudaSuccess) e = launch_pdl(muon::prepare_kernel<CAP>, dim3(blocks, n), dim3(muon::THREADS), 0, st, tab);
+  ctx->launches += 2;
+  return check_cuda(ctx, e, "muon::prepare_kernel launch");
 }
 
 ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, float beta, int nesterov, const float* coefficients,
                             int iterations, cudaStream_t st) {
   char* ws = ctx->ws + kCtrlBytes;
-  muon::Table tab;
-  std::memset(&tab, 0, sizeof(tab));
-  tab.beta = beta; tab.nesterov = nesterov;
-  tab.partial = reinterpret_cast<double*>(ws);
-  tab.target = reinterpret_cast<muon::Target*>(ws + sizeof(double) * muon::MAX_TENSORS * muon::MAX_PARTS);
-  tab.status = ctx->status();
+  double* partial = reinterpret_cast<double*>(ws);
+  muon::Target* target = reinterpret_cast<muon::Target*>(ws + sizeof(double) * muon::MAX_TENSORS * muon::MAX_PARTS);
   char* at = ws + up256(kTableBytes);
-  for (int precise = 0; precise < 2; ++precise) {
-    const ffsplit_status s = run_thin(ctx, t, n, precise != 0, beta, nesterov, coefficients, iterations, at, st);
+  int thin = 0;
+  for (int i = 0; i < n; ++i) thin += is_thin(t[i].rows, t[i].cols) ? 1 : 0;
+  if (thin > 0) {
+    const ffsplit_status s = thin <= 4    ? run_thin<4>(ctx, t, n, beta, nesterov, coefficients, iterations, at, st)
+                             : thin <= 32 ? run_thin<32>(ctx, t, n, beta, nesterov, coefficients, iterations, at, st)
+                                          : run_thin<muon::MAX_TENSORS>(ctx, t, n, beta, nesterov, coefficients, iterations, at, st);
     if (s != FFSPLIT_OK) return s;
     for (int i = 0; i < n; ++i)
-      if (is_thin(t[i].rows, t[i].cols) && (t[i].grad_dtype == FFSPLIT_F32) == (precise != 0)) at += matrix_bytes(t[i].rows, t[i].cols);
+      if (is_thin(t[i].rows, t[i].cols)) at += matrix_bytes(t[i].rows, t[i].cols);
   }
+  if (thin == n) return FFSPLIT_OK;
   // matrices of one shape lie one after the other, whatever their place in the list
   Group groups[muon::MAX_TENSORS];
   int order[muon::MAX_TENSORS], n_groups = 0, placed = 0;
@@ -621,12 +737,13 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
     g.S = matrices(p, p, g.count, g.precise);
     g.P = matrices(p, p, g.count, g.precise);
   }
+  muon::Entry entries[muon::MAX_TENSORS];
   int blocks = 0;
   for (int gi = 0, k = 0; gi < n_groups; ++gi) {
     const Group& g = groups[gi];
     for (int j = 0; j < g.count; ++j, ++k) {
       const ffsplit_muon_tensor& s = t[order[k]];
-      muon::Entry& e = tab.t[k];
+      muon::Entry& e = entries[k];
       e = entry_for(s);
       e.ld = g.X[0].ld;
       e.X = g.X[0].p + j * g.X[0].each;
@@ -634,25 +751,20 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
       e.blocks = g.precise ? 0 : 1;
       const long long pieces = (s.rows + 31ll) / 32 * ((e.octets + 7) / 8);
       e.parts = static_cast<int>(pieces < 2 * muon::MAX_PARTS ? (pieces + 1) / 2 : muon::MAX_PARTS);
-      e.block0 = blocks;
-      blocks += e.parts;
+      if (e.parts > blocks) blocks = e.parts;
     }
   }
-  if (placed == 0) return FFSPLIT_OK;
-  tab.n = placed;
-  cudaError_t e = launch_pdl(muon::norm_kernel, dim3(blocks), dim3(muon::THREADS), 0, st, tab);
-  ctx->launches++;
-  if (e != cudaSuccess) return check_cuda(ctx, e, "muon::norm_kernel launch");
-  e = launch_pdl(muon::prepare_kernel, dim3(blocks), dim3(muon::THREADS), 0, st, tab);
-  ctx->launches++;
-  if (e != cudaSuccess) return check_cuda(ctx, e, "muon::prepare_kernel launch");
+  const ffsplit_status first = placed <= 4    ? run_first<4>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st)
+                               : placed <= 32 ? run_first<32>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st)
+                                              : run_first<muon::MAX_TENSORS>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st);
+  if (first != FFSPLIT_OK) return first;
   for (int precise = 0; precise < 2; ++precise) {
     Group* some[muon::MAX_GROUPS];
     int m = 0;
     for (int gi = 0; gi <= n_groups; ++gi) {
       if (gi < n_groups && groups[gi].precise == (precise != 0)) some[m++] = &groups[gi];
       if (m == muon::MAX_GROUPS || (gi == n_groups && m > 0)) {
-        const ffsplit_status s = iterate(ctx, some, m, tab.target, coefficients, iterations, st);
+        const ffsplit_status s = iterate(ctx, some, m, target, coefficients, iterations, st);
         if (s != FFSPLIT_OK) return s;
         m = 0;
       }
