@@ -513,7 +513,8 @@ constexpr float kStandard[3] = {3.4445f, -4.7750f, 2.0315f};
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Bytes of one matrix's buffers: X twice, S and P, two planes each.
+// Bytes of one matrix's buffers: X twice, S and P (in pairs of iterations two more of these), two planes each.
+bool in_pairs(int rows, int cols, bool precise);
 size_t x_bytes(int rows, int cols) { return static_cast<size_t>(rows + muon::block_rows(rows)) * round_up(cols, 64) * 2; }
 int thin_parts(int rows, int cols) {      // (parts are whole chunks)
   const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows, chunk = muon::thin_chunk(muon::thin_tiles(p));
@@ -521,10 +522,10 @@ int thin_parts(int rows, int cols) {      // (parts are whole chunks)
   return (chunks + per - 1) / per;
 }
 bool is_thin(int rows, int cols) { return (rows < cols ? rows : cols) <= muon::THIN; }
-size_t matrix_bytes(int rows, int cols) {
+size_t matrix_bytes(int rows, int cols, bool precise) {
   const int p = rows < cols ? rows : cols;
   if (is_thin(rows, cols)) return up256(static_cast<size_t>(thin_parts(rows, cols) + 1) * p * p * sizeof(double));
-  return 2 * x_bytes(rows, cols) + 2 * x_bytes(p, p);
+  return 2 * x_bytes(rows, cols) + (in_pairs(rows, cols, precise) ? 4 : 2) * x_bytes(p, p);
 }
 constexpr size_t kTableBytes = muon::MAX_TENSORS * (muon::MAX_PARTS * sizeof(double) + sizeof(muon::Target));
 // Matrices are worked on in runs: as many as fit the tables and two gigabytes, one at least.
@@ -533,7 +534,7 @@ int run_length(const ffsplit_muon_tensor* t, int count, size_t* bytes) {
   size_t sum = 0;
   int n = 0;
   while (n < count && n < muon::MAX_TENSORS) {
-    const size_t more = matrix_bytes(t[n].rows, t[n].cols);
+    const size_t more = matrix_bytes(t[n].rows, t[n].cols, t[n].grad_dtype == FFSPLIT_F32);
     if (n > 0 && sum + more > kRunBytes) break;
     sum += more;
     ++n;
@@ -574,52 +575,80 @@ bool coefficients_hold(const float* c, int iterations) {
 // Matrices of one shape and precision.
 struct Group {
   int first, count, rows, cols;
-  bool precise;
-  muon::Matrices X[2], S, P;
+  bool precise, paired;
+  muon::Matrices X[2], S, P, T, R;      // T, R: paired only
+  int at;                               // which X is the current one
 };
+// Two iterations at once.  The second one's S is P S P (all of these are polynomials in S), so X need not be formed between the
+// two: X <- (P2 P) X with P2 = a I + b S2 + c S2 S2, S2 = (P S) P.  3 p^2 q + 5 p^3 multiply-adds instead of 6 p^2 q + 2 p^3,
+// and X is read and written once instead of twice; for two roundings more, which leave up to 3e-3 of the result instead of
+// 2e-3.  Small matrices would pay for one launch more (256 x 1024: 50 us for a pair either way).
+bool in_pairs(int rows, int cols, bool precise) {
+  const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
+  return !precise && p >= 512 && 2ll * q >= 3ll * p;
+}
 
-// All iterations of up to MAX_GROUPS groups of one precision.
+// All iterations of up to MAX_GROUPS groups that go alike.
 ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon::Target* targets, const float* coefficients, int iterations, cudaStream_t st) {
   const bool precise = groups[0]->precise;
-  for (int it = 0; it < iterations; ++it) {
-    const float* k = coefficients ? coefficients + 3 * it : kStandard;
-    muon::Product q[muon::MAX_GROUPS];
-    for (int step = 0; step < 3; ++step) {
-      std::memset(q, 0, sizeof(q));
-      for (int i = 0; i < n; ++i) {
-        Group& g = *groups[i];
-        const bool tall = g.rows > g.cols;
-        const muon::Matrices &X = g.X[it & 1], &Y = g.X[(it + 1) & 1];
-        muon::Product& p = q[i];
-        p.alpha = 1.f / muon::HELD;
-        if (step == 0) {             // S = X X^T
-          p.a = p.b = X; p.c = g.S;
-          p.a_mn = p.b_mn = tall;
-          p.M = p.N = g.S.rows; p.K = tall ? g.rows : g.cols;
-          p.symmetric = 1;
-          p.c_low = precise;
-        } else if (step == 1) {      // P = a I + b S + c S S
-          p.a = p.b = g.S; p.c = g.P;
-          p.M = p.N = p.K = g.S.rows;
-          p.alpha *= k[2]; p.beta = k[1]; p.diagonal = k[0];
-          p.d = &g.S; p.d_high = 1; p.d_low = precise;
-          p.symmetric = 1;
-          p.c_low = precise;
-        } else {                     // P X, or X P
-          p.a = tall ? X : g.P; p.b = tall ? g.P : X; p.c = Y;
-          p.b_mn = !tall;
-          p.M = g.rows; p.N = g.cols; p.K = g.S.rows;
-          if (!precise) {            // (of the second plane only the term a X)
-            p.beta = k[0];
-            p.d = &X; p.d_low = 1;
-          }
-          p.c_low = 1;
-          if (it + 1 == iterations) p.target = targets + g.first;
-        }
-      }
-      const ffsplit_status s = muon::launch_products(ctx, precise, q, n, st);
-      if (s != FFSPLIT_OK) return s;
+  muon::Product q[muon::MAX_GROUPS];
+  // one launch: `fill` says what it is for each group
+  const auto launch = [&](auto fill) {
+    std::memset(q, 0, sizeof(q));
+    for (int i = 0; i < n; ++i) {
+      q[i].alpha = 1.f / muon::HELD;
+      fill(*groups[i], q[i]);
     }
+    return muon::launch_products(ctx, precise, q, n, st);
+  };
+  // C = alpha A B of p x p matrices that commute
+  const auto square = [&](muon::Product& p, const muon::Matrices& A, const muon::Matrices& B, const muon::Matrices& C) {
+    p.a = A; p.b = B; p.c = C;
+    p.M = p.N = p.K = A.rows;
+    p.symmetric = 1;
+    p.c_low = precise;
+  };
+  // P = a I + b S + c S S
+  const auto polynomial = [&](muon::Product& p, const float* k, const muon::Matrices& S, const muon::Matrices* add, const muon::Matrices& P) {
+    square(p, S, S, P);
+    p.alpha *= k[2]; p.beta = k[1]; p.diagonal = k[0];
+    p.d = add; p.d_high = 1; p.d_low = precise;
+  };
+  ffsplit_status s;
+  for (int i = 0; i < n; ++i) groups[i]->at = 0;
+  for (int it = 0; it < iterations;) {
+    const float *k = coefficients ? coefficients + 3 * it : kStandard, *k2 = coefficients ? k + 3 : kStandard;
+    const bool pair = groups[0]->paired && it + 2 <= iterations;
+    if ((s = launch([&](Group& g, muon::Product& p) {                  // S = X X^T
+           const bool tall = g.rows > g.cols;
+           p.a = p.b = g.X[g.at]; p.c = g.S;
+           p.a_mn = p.b_mn = tall;
+           p.M = p.N = g.S.rows; p.K = tall ? g.rows : g.cols;
+           p.symmetric = 1;
+           p.c_low = precise;
+         })) != FFSPLIT_OK) return s;
+    if ((s = launch([&](Group& g, muon::Product& p) { polynomial(p, k, g.S, &g.S, g.P); })) != FFSPLIT_OK) return s;
+    if (pair) {
+      if ((s = launch([&](Group& g, muon::Product& p) { square(p, g.P, g.S, g.T); })) != FFSPLIT_OK) return s;            // T = P S
+      if ((s = launch([&](Group& g, muon::Product& p) { square(p, g.T, g.P, g.S); })) != FFSPLIT_OK) return s;            // S2 = T P
+      if ((s = launch([&](Group& g, muon::Product& p) { polynomial(p, k2, g.S, &g.S, g.T); })) != FFSPLIT_OK) return s;   // P2
+      if ((s = launch([&](Group& g, muon::Product& p) { square(p, g.T, g.P, g.R); })) != FFSPLIT_OK) return s;            // R = P2 P
+    }
+    it += pair ? 2 : 1;
+    if ((s = launch([&](Group& g, muon::Product& p) {                  // P X (R X), or X P
+           const bool tall = g.rows > g.cols;
+           const muon::Matrices &X = g.X[g.at], &P = pair ? g.R : g.P;
+           p.a = tall ? X : P; p.b = tall ? P : X; p.c = g.X[1 - g.at];
+           p.b_mn = !tall;
+           p.M = g.rows; p.N = g.cols; p.K = P.rows;
+           if (!precise) {            // (of the second plane only the term a X)
+             p.beta = pair ? k[0] * k2[0] : k[0];
+             p.d = &X; p.d_low = 1;
+           }
+           p.c_low = 1;
+           if (it == iterations) p.target = targets + g.first;
+         })) != FFSPLIT_OK) return s;
+    for (int i = 0; i < n; ++i) groups[i]->at = 1 - groups[i]->at;
   }
   return FFSPLIT_OK;
 }
@@ -656,7 +685,7 @@ ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, f
     e.parts = thin_parts(s.rows, s.cols);
     tab.S[tab.n] = reinterpret_cast<double*>(at);
     tab.Q[tab.n] = tab.S[tab.n] + static_cast<size_t>(e.parts) * p * p;
-    at += matrix_bytes(s.rows, s.cols);
+    at += matrix_bytes(s.rows, s.cols, s.grad_dtype == FFSPLIT_F32);
     if (p > most) most = p;
     if (e.parts > blocks) blocks = e.parts;
     ++tab.n;
@@ -703,7 +732,7 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
                                           : run_thin<muon::MAX_TENSORS>(ctx, t, n, beta, nesterov, coefficients, iterations, at, st);
     if (s != FFSPLIT_OK) return s;
     for (int i = 0; i < n; ++i)
-      if (is_thin(t[i].rows, t[i].cols)) at += matrix_bytes(t[i].rows, t[i].cols);
+      if (is_thin(t[i].rows, t[i].cols)) at += matrix_bytes(t[i].rows, t[i].cols, t[i].grad_dtype == FFSPLIT_F32);
   }
   if (thin == n) return FFSPLIT_OK;
   // matrices of one shape lie one after the other, whatever their place in the list
@@ -736,6 +765,11 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
     g.X[1] = matrices(g.rows, g.cols, g.count, g.precise);
     g.S = matrices(p, p, g.count, g.precise);
     g.P = matrices(p, p, g.count, g.precise);
+    g.paired = in_pairs(g.rows, g.cols, g.precise);
+    if (g.paired) {
+      g.T = matrices(p, p, g.count, g.precise);
+      g.R = matrices(p, p, g.count, g.precise);
+    }
   }
   muon::Entry entries[muon::MAX_TENSORS];
   int blocks = 0;
@@ -758,11 +792,11 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
                                : placed <= 32 ? run_first<32>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st)
                                               : run_first<muon::MAX_TENSORS>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st);
   if (first != FFSPLIT_OK) return first;
-  for (int precise = 0; precise < 2; ++precise) {
+  for (int kind = 0; kind < 3; ++kind) {      // precise, in pairs, neither: groups of one kind go together
     Group* some[muon::MAX_GROUPS];
     int m = 0;
     for (int gi = 0; gi <= n_groups; ++gi) {
-      if (gi < n_groups && groups[gi].precise == (precise != 0)) some[m++] = &groups[gi];
+      if (gi < n_groups && (groups[gi].precise ? 0 : groups[gi].paired ? 1 : 2) == kind) some[m++] = &groups[gi];
       if (m == muon::MAX_GROUPS || (gi == n_groups && m > 0)) {
         const ffsplit_status s = iterate(ctx, some, m, target, coefficients, iterations, st);
         if (s != FFSPLIT_OK) return s;
