@@ -50,6 +50,18 @@ __device__ __forceinline__ int adapter_of(const int* index, long long t, int n) 
   return i < 0 || i >= n ? -1 : i;
 }
 
+// This block's tokens and their adapters (-1: none); how many there are.
+template <int G>
+__device__ __forceinline__ int tokens_of(const int* index, const int* order, long long T, int n, int* token, int* of) {
+  const long long t0 = static_cast<long long>(blockIdx.x) * G;
+  const int count = T - t0 < G ? static_cast<int>(T - t0) : G;
+#pragma unroll
+  for (int g = 0; g < G; ++g) token[g] = g >= count ? 0 : order ? __ldcg(order + t0 + g) : static_cast<int>(t0 + g);
+#pragma unroll
+  for (int g = 0; g < G; ++g) of[g] = g < count ? adapter_of(index, token[g], n) : -1;
+  return count;
+}
+
 // P[t][j] = scale_i sum_k V[t][k] F_i(k, j).  F lies as [n][K][r] (k_minor = 0) or [n][r][K].  K is cut into ranges, so that
 // few tokens occupy all SMs; the ranges' sums are added by whoever reads P.  Bound by reading each token's factor once.
 struct ShrinkJob {
@@ -60,6 +72,7 @@ struct ShrinkJob {
 struct ShrinkArgs {
   ShrinkJob job[2];
   const int* index;
+  const int* order;       // the tokens sorted by adapter, or nullptr: as they come
   const float* scale;
   long long T;
   int n, r, splits;
@@ -72,14 +85,12 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
   __shared__ float part[THREADS * V * G < MAX_RANK * G * 8 ? MAX_RANK * G * 8 : THREADS * V * G];
   pdl_wait();
   const ShrinkJob& job = a.job[blockIdx.y];
-  const long long t0 = static_cast<long long>(blockIdx.x) * G;
-  const int count = a.T - t0 < G ? static_cast<int>(a.T - t0) : G;
-  int of[G];
+  int token[G], of[G];
+  const int count = tokens_of<G>(a.index, a.order, a.T, a.n, token, of);
+  if (threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) {
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    of[g] = g < count ? adapter_of(a.index, t0 + g, a.n) : -1;
-    if (threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && g < count && __ldg(a.index + t0 + g) >= a.n)
-      record_status(a.status, FFSPLIT_ERR_BAD_INDEX, static_cast<int>(t0 + g), KID_ADAPTER);
+    for (int g = 0; g < G; ++g)
+      if (g < count && __ldg(a.index + token[g]) >= a.n) record_status(a.status, FFSPLIT_ERR_BAD_INDEX, token[g], KID_ADAPTER);
   }
   const int per = ((job.K + a.splits - 1) / a.splits + 63) / 64 * 64, begin = blockIdx.z * per, end = begin + per < job.K ? begin + per : job.K;
   float* P = job.P + blockIdx.z * a.T * a.r;
@@ -88,6 +99,7 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
   // the rank along memory: a thread to `step` ranks of every slices-th k
   const int step = wide ? V : 1, across = (a.r + step - 1) / step, slices = THREADS / across;
   const int slice = threadIdx.x / across, j0 = (threadIdx.x - slice * across) * step;
+  bool staged = false;
   for (int first = 0; first < count; ++first) {
     int i = -1;
     unsigned mask = 0;
@@ -106,12 +118,14 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
     bool fresh = true;
     for (int k0 = begin; k0 < end; k0 += CHUNK) {
       const int m = end - k0 < CHUNK ? end - k0 : CHUNK;
-      __syncthreads();
-      for (int e = threadIdx.x; e < G * CHUNK; e += THREADS) {
-        const int g = e / CHUNK, k = e % CHUNK;
-        x[g][k] = (mask >> g & 1u) && k < m ? load<F32>(job.V, (t0 + g) * job.K + k0 + k) : 0.f;
+      if (!staged) {
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+          for (int k = threadIdx.x; k < CHUNK; k += THREADS) x[g][k] = g < count && k < m ? load<F32>(job.V, static_cast<long long>(token[g]) * job.K + k0 + k) : 0.f;
+        __syncthreads();
+        staged = end - begin <= CHUNK;      // (all of this block's range: the other adapters find it there)
       }
-      __syncthreads();
       if (!job.k_minor) {
         if (slice < slices) {
           if (wide) {
@@ -179,6 +193,7 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
       }
       __syncthreads();
     }
+    // (sums of tokens that use another adapter were taken along; they are not written)
     for (int e = threadIdx.x; e < a.r * G; e += THREADS) {
       const int c = e / G, g = e - c * G;
       if (!(mask >> g & 1u)) continue;
@@ -187,53 +202,68 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
         const int sums = job.k_minor ? 1 : slices;
         for (int k = 0; k < sums; ++k) s += part[(k * a.r + c) * G + g];
       }
-      P[(t0 + g) * a.r + c] = scale * s;
+      int to = 0;
+#pragma unroll
+      for (int q = 0; q < G; ++q) if (q == g) to = token[q];
+      P[static_cast<long long>(to) * a.r + c] = scale * s;
     }
     __syncthreads();
   }
 }
 
+// P = the ranges' sums of P, in order (where many blocks read it).
+__global__ void __launch_bounds__(THREADS) add_ranges_kernel(float* P0, float* P1, long long count, int splits) {
+  pdl_wait();
+  float* P = blockIdx.y ? P1 : P0;
+  const long long i = static_cast<long long>(blockIdx.x) * THREADS + threadIdx.x;
+  if (i >= count) return;
+  float s = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < splits; ++k) s += __ldcg(P + k * count + i);
+  P[i] = s;
+}
+
 // Y[t][c] = base[t][c] + sum_j P[t][j] F_i(j, c).  F lies as [n][r][N] (r_minor = 0) or [n][N][r].  Bound by reading the
-// factors and, of many tokens, base and Y.
+// factors and, of many tokens, base and Y.  The four warps of a block share the ranks (one thread through all of 88: 26 us for
+// three tokens).
 struct ExpandArgs {
   const float* P;         // [splits][T][r]
   const void *F, *base;
   void* Y;
-  const int* index;
+  const int *index, *order;
   long long T;
   int N, n, r, r_minor, splits;
 };
-constexpr int EXPAND_THREADS = 128;
+constexpr int EXPAND_THREADS = 128, SHARES = EXPAND_THREADS / 32;
 template <bool F32, int G>
 __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_constant__ ExpandArgs a) {
   constexpr int V = VEC<F32>;
-  __shared__ float p[MAX_RANK][G];
+  __shared__ float p[MAX_RANK][G], sums[SHARES][V][G][32];
   pdl_wait();
   const bool wide = (a.r_minor ? a.r : a.N) % V == 0;
   const int step = wide && !a.r_minor ? V : 1;              // columns of a thread
-  const long long t0 = static_cast<long long>(blockIdx.x) * G;
-  const int count = a.T - t0 < G ? static_cast<int>(a.T - t0) : G, c = (blockIdx.y * EXPAND_THREADS + threadIdx.x) * step;
-  if (blockIdx.y * EXPAND_THREADS * step >= static_cast<unsigned>(a.N)) return;
-  int of[G];
+  const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, c = (blockIdx.y * 32 + lane) * step;
+  int token[G], of[G];
+  const int count = tokens_of<G>(a.index, a.order, a.T, a.n, token, of);
 #pragma unroll
-  for (int g = 0; g < G; ++g) of[g] = g < count ? adapter_of(a.index, t0 + g, a.n) : -1;
-  for (int e = threadIdx.x; e < G * a.r; e += EXPAND_THREADS) {
-    const int g = e / a.r, j = e - g * a.r;
-    float s = 0.f;
-    if (g < count && adapter_of(a.index, t0 + g, a.n) >= 0) {
+  for (int g = 0; g < G; ++g)
+    for (int j = threadIdx.x; j < a.r; j += EXPAND_THREADS) {
+      float s = 0.f;
+      if (of[g] >= 0) {
 #pragma unroll 8
-      for (int k = 0; k < a.splits; ++k) s += __ldcg(a.P + (k * a.T + t0 + g) * a.r + j);
+        for (int k = 0; k < a.splits; ++k) s += __ldcg(a.P + (k * a.T + token[g]) * a.r + j);
+      }
+      p[j][g] = s;
     }
-    p[j][g] = s;
-  }
   __syncthreads();
-  if (c >= a.N) return;
+  // this warp's ranks, whole vectors of them
+  const int each = ((a.r + SHARES - 1) / SHARES + V - 1) / V * V, j0 = share * each, j1 = j0 + each < a.r ? j0 + each : a.r;
   float acc[V][G];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
     for (int g = 0; g < G; ++g) acc[v][g] = 0.f;
-  for (int first = 0; first < count; ++first) {
+  for (int first = 0; first < count && c < a.N; ++first) {
     int i = -1;
     unsigned mask = 0;
 #pragma unroll
@@ -246,7 +276,7 @@ __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_con
       const long long at = f0 + static_cast<long long>(c) * a.r;
       if (wide) {
 #pragma unroll 2
-        for (int j = 0; j < a.r; j += V) {
+        for (int j = j0; j < j1; j += V) {
           float f[V];
           load_vec<F32>(a.F, at + j, f);
 #pragma unroll
@@ -257,15 +287,15 @@ __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_con
         }
       } else {
 #pragma unroll 4
-        for (int j = 0; j < a.r; ++j) {
+        for (int j = j0; j < j1; ++j) {
           const float f = load<F32>(a.F, at + j);
 #pragma unroll
           for (int g = 0; g < G; ++g) if (mask >> g & 1u) acc[0][g] = fmaf(p[j][g], f, acc[0][g]);
         }
       }
     } else if (wide) {
-#pragma unroll 8
-      for (int j = 0; j < a.r; ++j) {
+#pragma unroll 4
+      for (int j = j0; j < j1; ++j) {
         float f[V];
         load_vec<F32>(a.F, f0 + static_cast<long long>(j) * a.N + c, f);
 #pragma unroll
@@ -275,8 +305,8 @@ __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_con
             for (int v = 0; v < V; ++v) acc[v][g] = fmaf(p[j][g], f[v], acc[v][g]);
       }
     } else {
-#pragma unroll 8
-      for (int j = 0; j < a.r; ++j) {
+#pragma unroll 4
+      for (int j = j0; j < j1; ++j) {
         const float f = load<F32>(a.F, f0 + static_cast<long long>(j) * a.N + c);
 #pragma unroll
         for (int g = 0; g < G; ++g) if (mask >> g & 1u) acc[0][g] = fmaf(p[j][g], f, acc[0][g]);
@@ -284,20 +314,28 @@ __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_con
     }
   }
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    if (g >= count) break;
-    if (of[g] < 0 && a.base == a.Y) continue;
-    const long long at = (t0 + g) * a.N + c;
-    if (step > 1) {      // (then c + V <= N)
-      float b[V];
+  for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int v = 0; v < V; ++v) b[v] = 0.f;
+    for (int g = 0; g < G; ++g) sums[share][v][g][lane] = acc[v][g];
+  __syncthreads();
+  if (c >= a.N) return;
+  // the shares' sums in order; a warp to every fourth token
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    if (g >= count || g % SHARES != share || (of[g] < 0 && a.base == a.Y)) continue;
+    const long long at = static_cast<long long>(token[g]) * a.N + c;
+    float s[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      s[v] = sums[0][v][g][lane];
+#pragma unroll
+      for (int k = 1; k < SHARES; ++k) s[v] += sums[k][v][g][lane];
+    }
+    if (step > 1) {      // (then c + V <= N)
       if constexpr (F32) {
-        if (a.base) {
-          const float4 q = *reinterpret_cast<const float4*>(static_cast<const float*>(a.base) + at);
-          b[0] = q.x; b[1] = q.y; b[2] = q.z; b[3] = q.w;
-        }
-        *reinterpret_cast<float4*>(static_cast<float*>(a.Y) + at) = make_float4(b[0] + acc[0][g], b[1] + acc[1][g], b[2] + acc[2][g], b[3] + acc[3][g]);
+        float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (a.base) q = *reinterpret_cast<const float4*>(static_cast<const float*>(a.base) + at);
+        *reinterpret_cast<float4*>(static_cast<float*>(a.Y) + at) = make_float4(q.x + s[0], q.y + s[1], q.z + s[2], q.w + s[3]);
       } else {
         uint32_t w[4] = {0u, 0u, 0u, 0u};
         if (a.base) {
@@ -305,12 +343,13 @@ __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_con
           w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = pack_bf16x2(__uint_as_float(w[k] << 16) + acc[2 * k][g], __uint_as_float(w[k] & 0xffff0000u) + acc[2 * k + 1][g]);
+        for (int k = 0; k < 4; ++k)
+          w[k] = pack_bf16x2(__uint_as_float(w[k] << 16) + s[V > 4 ? 2 * k : 0], __uint_as_float(w[k] & 0xffff0000u) + s[V > 4 ? 2 * k + 1 : 0]);
         *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.Y) + at) = make_uint4(w[0], w[1], w[2], w[3]);
       }
     } else {
       const float b = !a.base ? 0.f : F32 ? static_cast<const float*>(a.base)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(a.base)[at]);
-      store<F32>(a.Y, at, b + acc[0][g]);
+      store<F32>(a.Y, at, b + s[0]);
     }
   }
 }
@@ -325,8 +364,9 @@ struct GradJob {
 struct GradArgs {
   GradJob job[2];
   const int* index;
+  const int *count, *offset, *order;      // the tokens sorted by adapter, or nullptr: there are no more than THREADS
   long long T;
-  int n, r, splits;
+  int n, r;
 };
 constexpr int GRAD_COLS = 32, GRAD_TOKENS = 32;
 template <bool F32>
@@ -339,31 +379,36 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant
   const int c0 = (blockIdx.x - (which ? a.job[0].blocks : 0)) * GRAD_COLS;
   const int col = threadIdx.x & 31, jg = threadIdx.x >> 5, lane = col;
   float acc[MAX_RANK / 8] = {};
-  for (long long t0 = 0; t0 < a.T; t0 += THREADS) {
-    const bool mine = t0 + threadIdx.x < a.T && __ldg(a.index + t0 + threadIdx.x) == i;
-    const unsigned votes = __ballot_sync(0xffffffffu, mine);
-    if (lane == 0) found[jg] = __popc(votes);
-    __syncthreads();
-    int before = 0, all = 0;
+  const int mine = a.order ? __ldcg(a.count + i) : static_cast<int>(a.T), from = a.order ? __ldcg(a.offset + i) : 0;
+  for (int t0 = 0; t0 < mine; t0 += THREADS) {
+    int all;
+    if (a.order) {
+      all = mine - t0 < THREADS ? mine - t0 : THREADS;
+      if (static_cast<int>(threadIdx.x) < all) list[threadIdx.x] = __ldcg(a.order + from + t0 + threadIdx.x);
+    } else {
+      const bool hit = static_cast<int>(threadIdx.x) < mine && __ldg(a.index + threadIdx.x) == i;
+      const unsigned votes = __ballot_sync(0xffffffffu, hit);
+      if (lane == 0) found[jg] = __popc(votes);
+      __syncthreads();
+      int before = 0;
+      all = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-      if (w < jg) before += found[w];
-      all += found[w];
+      for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < jg) before += found[w];
+        all += found[w];
+      }
+      if (hit) list[before + __popc(votes & ((1u << lane) - 1u))] = threadIdx.x;
     }
-    if (mine) list[before + __popc(votes & ((1u << lane) - 1u))] = threadIdx.x;
     __syncthreads();
     for (int b = 0; b < all; b += GRAD_TOKENS) {
       const int m = all - b < GRAD_TOKENS ? all - b : GRAD_TOKENS;
       for (int e = threadIdx.x; e < m * a.r; e += THREADS) {
         const int q = e / a.r, j = e - q * a.r;
-        float s = 0.f;
-#pragma unroll 4
-        for (int k = 0; k < a.splits; ++k) s += __ldcg(job.P + (k * a.T + t0 + list[b + q]) * a.r + j);
-        p[q][j] = s;
+        p[q][j] = __ldcg(job.P + static_cast<long long>(list[b + q]) * a.r + j);
       }
       for (int e = threadIdx.x; e < m * GRAD_COLS; e += THREADS) {
         const int q = e / GRAD_COLS, c = e % GRAD_COLS;
-        v[q][c] = c0 + c < job.N ? load<F32>(job.V, (t0 + list[b + q]) * job.N + c0 + c) : 0.f;
+        v[q][c] = c0 + c < job.N ? load<F32>(job.V, static_cast<long long>(list[b + q]) * job.N + c0 + c) : 0.f;
       }
       __syncthreads();
       for (int q = 0; q < m; ++q) {
@@ -395,6 +440,9 @@ bool on_tensor_cores(const ffsplit_projection& p, int n, long long T) {
   return p.dtype == FFSPLIT_BF16 && T > adapter::FEW && adapter::tile_bound(T, n) <= 65535;
 }
 
+// Batches whose tokens are sorted by adapter first (few tokens are not: that is a launch more).
+bool is_sorted(long long T) { return T > adapter::FEW; }
+
 // Ranges of K of the products on the CUDA cores: as many blocks as SMs twice over, 64 elements each at least.
 int tokens_per_block(const ffsplit_projection& p, int n, long long T) {
   if (T > adapter::FEW) return p.dtype == FFSPLIT_F32 ? adapter::MANY : adapter::SOME;      // (bf16: 65000 adapters and more)
@@ -424,7 +472,7 @@ AdapterLayout adapter_layout(const ffsplit_projection& p, int n, int r, long lon
   const size_t inner = tc ? static_cast<size_t>(adapter::tile_bound(T, n)) * adapter::TOKENS * adapter::rank_pitch(r) * 2 : static_cast<size_t>(splits_of(p, n, T)) * T * r * 4;
   take(&L.P, inner);
   take(&L.D, inner);
-  take(&L.sorted, tc ? (static_cast<size_t>(T) + 2 * (static_cast<size_t>(n) + 1)) * 4 : 0);
+  take(&L.sorted, is_sorted(T) ? (static_cast<size_t>(T) + 2 * (static_cast<size_t>(n) + 1)) * 4 : 0);
   take(&L.X, f32 || p.in % 8 ? static_cast<size_t>(T) * L.ldi * 2 * planes : 0);
   take(&L.dY, f32 || p.out % 8 ? static_cast<size_t>(T) * L.ldo * 2 * planes : 0);
   take(&L.W, f32 || p.out % 8 ? static_cast<size_t>(p.in) * L.ldo * 2 * planes : 0);
@@ -490,7 +538,7 @@ struct Call {
   void use_A() { A = {train::operand(&prep, &prep_blocks, false, a.A, static_cast<long long>(a.n) * p.in, a.r, L.ldr, ws + L.A), p.in, a.r, 0}; }
   void use_B() { B = {train::operand(&prep, &prep_blocks, false, a.B, static_cast<long long>(a.n) * a.r, p.out, L.ldo, ws + L.B), a.r, p.out, 1}; }
   ffsplit_status prepare() {
-    if (tc) {
+    if (is_sorted(T)) {
       sorted.count = reinterpret_cast<int*>(ws + L.sorted);
       sorted.offset = sorted.count + a.n + 1;
       sorted.order = sorted.offset + a.n + 1;
@@ -525,7 +573,7 @@ ffsplit_status launch_shrink_g(const Call& c, const adapter::ShrinkArgs& s, int 
   return check_cuda(c.ctx, e, "adapter::shrink_kernel launch");
 }
 ffsplit_status launch_shrink(const Call& c, adapter::ShrinkArgs& s, int jobs) {
-  s.index = c.a.index; s.scale = c.a.scale; s.T = c.T; s.n = c.a.n; s.r = c.a.r; s.status = c.ctx->status();
+  s.index = c.a.index; s.order = c.sorted.order; s.scale = c.a.scale; s.T = c.T; s.n = c.a.n; s.r = c.a.r; s.status = c.ctx->status();
   s.splits = splits_of(c.p, c.a.n, c.T);
   switch (tokens_per_block(c.p, c.a.n, c.T)) {
     case adapter::MANY: return launch_shrink_g<adapter::MANY>(c, s, jobs);
@@ -536,15 +584,15 @@ ffsplit_status launch_shrink(const Call& c, adapter::ShrinkArgs& s, int jobs) {
 template <int G>
 ffsplit_status launch_expand_g(const Call& c, const adapter::ExpandArgs& x) {
   const int vec = c.f32 ? adapter::VEC<true> : adapter::VEC<false>, step = !x.r_minor && x.N % vec == 0 ? vec : 1;
-  const dim3 grid(static_cast<unsigned>((x.T + G - 1) / G), (x.N + adapter::EXPAND_THREADS * step - 1) / (adapter::EXPAND_THREADS * step));
+  const dim3 grid(static_cast<unsigned>((x.T + G - 1) / G), (x.N + 32 * step - 1) / (32 * step));
   constexpr int G16 = G < adapter::MANY ? G : adapter::SOME;
   const cudaError_t e = c.f32 ? launch_pdl(adapter::expand_kernel<true, G>, grid, dim3(adapter::EXPAND_THREADS), 0, c.st, x)
                               : launch_pdl(adapter::expand_kernel<false, G16>, grid, dim3(adapter::EXPAND_THREADS), 0, c.st, x);
   c.ctx->launches++;
   return check_cuda(c.ctx, e, "adapter::expand_kernel launch");
 }
-ffsplit_status launch_expand(const Call& c, const float* P, const void* F, const void* base, void* Y, int N, int r_minor) {
-  const adapter::ExpandArgs x = {P, F, base, Y, c.a.index, c.T, N, c.a.n, c.a.r, r_minor, splits_of(c.p, c.a.n, c.T)};
+ffsplit_status launch_expand(const Call& c, const float* P, int splits, const void* F, const void* base, void* Y, int N, int r_minor) {
+  const adapter::ExpandArgs x = {P, F, base, Y, c.a.index, c.sorted.order, c.T, N, c.a.n, c.a.r, r_minor, splits};
   switch (tokens_per_block(c.p, c.a.n, c.T)) {
     case adapter::MANY: return launch_expand_g<adapter::MANY>(c, x);
     case adapter::SOME: return launch_expand_g<adapter::SOME>(c, x);
@@ -594,7 +642,7 @@ ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projectio
   }
   if (W && (s = c.shared_product(c.X, bias, false, Y)) != FFSPLIT_OK) return s;
   if (c.tc) return adapter::launch_expand_tc(ctx, c.tiles(c.L.P), c.B, c.p.out, W ? Y : base, Y, c.sorted, c.a.r, c.st);
-  return launch_expand(c, c.inner(c.L.P), adapters->B, W ? Y : base, Y, c.p.out, 0);
+  return launch_expand(c, c.inner(c.L.P), splits_of(c.p, c.a.n, T), adapters->B, W ? Y : base, Y, c.p.out, 0);
 }
 
 ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W, const void* base,
@@ -618,7 +666,7 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
     if (dX || dA) c.use_B();
   }
   if ((s = c.prepare()) != FFSPLIT_OK) return s;
-  int n = 0;
+  int n = 0, splits = splits_of(c.p, c.a.n, T);
   if (c.tc) {
     adapter::Shrink jobs[2];
     if (dX || dA) jobs[n++] = {c.dY, c.B, c.tiles(c.L.D), c.p.out};
@@ -630,12 +678,20 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
     if (dX || dA) sh.job[n++] = {dY, adapters->B, c.inner(c.L.D), c.p.out, 1};
     if (dB) sh.job[n++] = {X, adapters->A, c.inner(c.L.P), c.p.in, 0};
     if ((s = launch_shrink(c, sh, n)) != FFSPLIT_OK) return s;
+    if (splits > 1 && (dA || dB)) {
+      const long long count = T * c.a.r;
+      const cudaError_t e = launch_pdl(adapter::add_ranges_kernel, dim3(static_cast<unsigned>((count + adapter::THREADS - 1) / adapter::THREADS), n),
+                                       dim3(adapter::THREADS), 0, c.st, sh.job[0].P, sh.job[1].P, count, splits);
+      ctx->launches++;
+      if (e != cudaSuccess) return check_cuda(ctx, e, "adapter::add_ranges_kernel launch");
+      splits = 1;
+    }
   }
   if (dX) {
     if (W && (s = c.shared_product(c.dY, nullptr, true, grads->dX)) != FFSPLIT_OK) return s;
     const void* add = W ? grads->dX : base;
     s = c.tc ? adapter::launch_expand_tc(ctx, c.tiles(c.L.D), c.A, c.p.in, add, grads->dX, c.sorted, c.a.r, c.st)
-             : launch_expand(c, c.inner(c.L.D), adapters->A, add, grads->dX, c.p.in, 1);
+             : launch_expand(c, c.inner(c.L.D), splits, adapters->A, add, grads->dX, c.p.in, 1);
     if (s != FFSPLIT_OK) return s;
   }
   if (!dA && !dB) return FFSPLIT_OK;
@@ -651,7 +707,8 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
   n = 0;
   if (dA) g.job[n++] = {c.inner(c.L.D), X, grads->dA, c.p.in, 1, (c.p.in + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
   if (dB) g.job[n++] = {c.inner(c.L.P), dY, grads->dB, c.p.out, 0, (c.p.out + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
-  g.index = adapters->index; g.T = T; g.n = c.a.n; g.r = c.a.r; g.splits = splits_of(c.p, c.a.n, T);
+  g.index = adapters->index; g.T = T; g.n = c.a.n; g.r = c.a.r;
+  g.count = c.sorted.count; g.offset = c.sorted.offset; g.order = c.sorted.order;
   const dim3 grid(g.job[0].blocks + g.job[1].blocks, c.a.n);
   const cudaError_t e = c.f32 ? launch_pdl(adapter::gradient_kernel<true>, grid, dim3(adapter::THREADS), 0, c.st, g)
                               : launch_pdl(adapter::gradient_kernel<false>, grid, dim3(adapter::THREADS), 0, c.st, g);

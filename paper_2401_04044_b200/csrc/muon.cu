@@ -89,19 +89,20 @@ __device__ __forceinline__ void load_u8(const Entry& e, float beta, int nesterov
     }
   }
 }
-// A matrix is gone through in pieces of 32 rows x 64 columns, eight columns to a thread: eight threads read a line of G, and what
-// a piece leaves in a second plane of blocks is whole sectors.  Pieces begin .. end of block `part`.
-__device__ __forceinline__ int pieces_across(const Entry& e) { return (e.octets + 7) / 8; }
+// A matrix is gone through in pieces of 16 rows x 128 columns, eight columns to a thread: a warp reads 256 bytes of each of two
+// rows of G, and what it leaves in a second plane of blocks is whole sectors.  Pieces begin .. end of block `part`.
+constexpr int PIECE_ROWS = 16, PIECE_OCTETS = 16;
+__host__ __device__ __forceinline__ int pieces_across(int octets) { return (octets + PIECE_OCTETS - 1) / PIECE_OCTETS; }
 __device__ __forceinline__ void range_of(const Entry& e, int part, int* begin, int* end) {
-  const int all = (e.rows + 31) / 32 * pieces_across(e), per = (all + e.parts - 1) / e.parts;
+  const int all = (e.rows + PIECE_ROWS - 1) / PIECE_ROWS * pieces_across(e.octets), per = (all + e.parts - 1) / e.parts;
   *begin = part * per;
   *end = *begin + per < all ? *begin + per : all;
 }
 // This thread's columns of a piece; false: there are none.
 __device__ __forceinline__ bool place(const Entry& e, int piece, int* row, int* octet) {
-  const int across = pieces_across(e), r = piece / across;
-  *row = r * 32 + (threadIdx.x >> 3);
-  *octet = (piece - r * across) * 8 + (threadIdx.x & 7);
+  const int across = pieces_across(e.octets), r = piece / across;
+  *row = r * PIECE_ROWS + (threadIdx.x >> 4);
+  *octet = (piece - r * across) * PIECE_OCTETS + (threadIdx.x & 15);
   return *row < e.rows && *octet < e.octets;
 }
 __device__ __forceinline__ double block_sum(double v, double* red) {
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
   if (part == 0 && threadIdx.x == 0) {
     Target o;
     o.W = e.W; o.out = e.out; o.f32 = e.w_f32;
-    o.wide = e.wide_w;
+    o.even = e.cols % 2 == 0 && ((reinterpret_cast<uintptr_t>(e.W) | reinterpret_cast<uintptr_t>(e.out)) & 3u) == 0;
     o.keep = finite ? 1.0f - e.decay : 1.0f;
     o.step = e.W ? (finite ? e.step : 0.f) : finite ? -1.0f : __int_as_float(0x7fffffff);
     t.target[which] = o;
@@ -783,7 +784,7 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
       e.X = g.X[0].p + j * g.X[0].each;
       e.X_low = g.X[0].low + j * g.X[0].low_each;
       e.blocks = g.precise ? 0 : 1;
-      const long long pieces = (s.rows + 31ll) / 32 * ((e.octets + 7) / 8);
+      const long long pieces = (s.rows + muon::PIECE_ROWS - 1ll) / muon::PIECE_ROWS * muon::pieces_across(e.octets);
       e.parts = static_cast<int>(pieces < 2 * muon::MAX_PARTS ? (pieces + 1) / 2 : muon::MAX_PARTS);
       if (e.parts > blocks) blocks = e.parts;
     }

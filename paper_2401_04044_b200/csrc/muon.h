@@ -29,7 +29,7 @@ struct Target {
   const void* W;
   void* out;
   float keep, step;       // out = keep W - step X; without W: out = -step X
-  int f32, wide;          // wide: every 16 columns of W and out start on 16 bytes
+  int f32, even;          // even: rows of W and out start on 4 bytes
 };
 
 // C = alpha A B + beta D + diagonal I for every matrix of a group.

@@ -36,8 +36,8 @@ constexpr int TMEM_COLS = 512;
 constexpr int BAR_BYTES = 256;
 constexpr int MAX_SMEM = 232448;
 // Outputs leave through shared memory: 32 x 32 values of a warp at a time, one TMA store to a plane, and another to the mirror
-// image.  (A row to a lane, as the sums lie in tensor memory, every store falls into 32 lines: 11 us for a tile of X instead of
-// TILE_US.)  What is left holds the ring.
+// image.  (A row to a lane, as the sums lie in tensor memory, every store falls into 32 lines: 126 us for the third product of
+// twelve 1024 x 4096 matrices, now 95.)  What is left holds the ring.
 constexpr int BOX = 32, BOX_BYTES = BOX * BOX * 2;
 // An epilogue reads 2 bytes of every value and writes 4 while the tensor cores take 17 us over a tile (K = 4096): with 8 warps,
 // each waiting for its next 16 columns, it took 35 us.  precise: 8, for the sake of their registers.
@@ -158,61 +158,56 @@ __device__ __forceinline__ uint32_t pair_half(float x, float y) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The last product: 16 columns of one row of a matrix, updated.  v: X times HELD.
-__device__ __forceinline__ void update16(const Target& t, long long row, int n0, int N, const float* v) {
-  const long long at = row * N + n0;
+// The last product: 32 x 32 values of a warp (X times HELD), turned to rows in shared memory, update a matrix.  A warp goes along
+// its rows, two columns to a lane and two rows at a time where the matrix allows words of two (`even`), else a row at a time;
+// the weights of 16 rows are on their way at once.  (A row to a lane: 190 us for twelve 1024 x 4096 matrices where the same product
+// without an update takes 126, and 150 instead of 50 for 1000 x 2731, whose rows start anywhere.)
+constexpr int TURN_PITCH = 33, TURN_BYTES = BOX * TURN_PITCH * 4;
+template <bool F32>
+__device__ __forceinline__ void update_rows(const Target& t, const float* turn, int lane, long long row0, int rows, int n0, int N) {
   const float step = t.step * (1.f / HELD), keep = t.keep;
-  if (t.wide) {       // (then N is a multiple of 8: 16 columns, or 8)
+  const int col = n0 + lane;
+  if (col >= N) return;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (n0 + 8 * h >= N) break;
-      const float* x = v + 8 * h;
-      if (t.f32) {
-        float o[8];
+  for (int r0 = 0; r0 < BOX; r0 += 16) {
+    float w[16];
+    const long long at = (row0 + r0) * N + col;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = -step * x[i];
-        if (t.W) {
-          const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(t.W) + at) + 2 * h;
-          const float4 a = p[0], b = p[1];
-          const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = fmaf(keep, w[i], o[i]);
-        }
-        float4* q = reinterpret_cast<float4*>(static_cast<float*>(t.out) + at) + 2 * h;
-        q[0] = make_float4(o[0], o[1], o[2], o[3]);
-        q[1] = make_float4(o[4], o[5], o[6], o[7]);
-      } else {
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (t.W) {
-          const uint4 q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.W) + at)[h];
-          w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float lo = -step * x[2 * i], hi = -step * x[2 * i + 1];
-          if (t.W) {
-            lo = fmaf(keep, __uint_as_float(w[i] << 16), lo);
-            hi = fmaf(keep, __uint_as_float(w[i] & 0xffff0000u), hi);
-          }
-          const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-          w[i] = *reinterpret_cast<const uint32_t*>(&b);
-        }
-        reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(t.out) + at)[h] = make_uint4(w[0], w[1], w[2], w[3]);
-      }
+    for (int i = 0; i < 16; ++i) {
+      w[i] = 0.f;
+      if (t.W && r0 + i < rows)
+        w[i] = F32 ? static_cast<const float*>(t.W)[at + static_cast<long long>(i) * N] : __bfloat162float(static_cast<const __nv_bfloat16*>(t.W)[at + static_cast<long long>(i) * N]);
     }
-    return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (r0 + i >= rows) break;
+      const float x = turn[(r0 + i) * TURN_PITCH + lane], o = t.W ? fmaf(keep, w[i], -step * x) : -step * x;
+      if (F32) static_cast<float*>(t.out)[at + static_cast<long long>(i) * N] = o;
+      else static_cast<__nv_bfloat16*>(t.out)[at + static_cast<long long>(i) * N] = __float2bfloat16_rn(o);
+    }
+  }
+}
+__device__ __forceinline__ void update_rows_even(const Target& t, const float* turn, int lane, long long row0, int rows, int n0, int N) {
+  const float step = t.step * (1.f / HELD), keep = t.keep;
+  const int c = (lane & 15) * 2, up = lane >> 4;
+  if (n0 + c >= N) return;      // (N is even)
+  const long long at = (row0 + up) * N + n0 + c;
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    w[i] = 0u;
+    if (t.W && 2 * i + up < rows) w[i] = *reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(t.W) + at + 2ll * i * N);
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    if (n0 + i >= N) break;
-    float o = -step * v[i];
-    if (t.f32) {
-      if (t.W) o = fmaf(keep, static_cast<const float*>(t.W)[at + i], o);
-      static_cast<float*>(t.out)[at + i] = o;
-    } else {
-      if (t.W) o = fmaf(keep, __bfloat162float(static_cast<const __nv_bfloat16*>(t.W)[at + i]), o);
-      static_cast<__nv_bfloat16*>(t.out)[at + i] = __float2bfloat16_rn(o);
+    if (2 * i + up >= rows) break;
+    const float* x = turn + (2 * i + up) * TURN_PITCH + c;
+    float lo = -step * x[0], hi = -step * x[1];
+    if (t.W) {
+      lo = fmaf(keep, __uint_as_float(w[i] << 16), lo);
+      hi = fmaf(keep, __uint_as_float(w[i] & 0xffff0000u), hi);
     }
+    *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(t.out) + at + 2ll * i * N) = pack_bf16x2(lo, hi);
   }
 }
 
@@ -476,7 +471,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
             for (int i = 0; i < 16; ++i) if (row == c0 + c + i) v[i] += d.diagonal;
           }
           if constexpr (LAST) {
-            if (in) update16(d.target[t.batch], row, c0 + c, d.N, v);
+            float* to = reinterpret_cast<float*>(buf) + lane * TURN_PITCH + 16 * k;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) to[i] = v[i];
             continue;
           }
           uint32_t w[8];
@@ -500,7 +497,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
             }
           }
         }
-        if constexpr (!LAST) {
+        if constexpr (LAST) {
+          __syncwarp();
+          const Target& to = d.target[t.batch];
+          const float* turn = reinterpret_cast<const float*>(buf);
+          const int rows = d.M - row0;
+          if (to.f32) update_rows<true>(to, turn, lane, row0, rows, c0 + c0b, d.N);
+          else if (to.even) update_rows_even(to, turn, lane, row0, rows, c0 + c0b, d.N);
+          else update_rows<false>(to, turn, lane, row0, rows, c0 + c0b, d.N);
+          __syncwarp();
+        } else {
           ptx::fence_proxy_async();
           __syncwarp();
           if (lane == 0 && leaves) {
@@ -613,7 +619,7 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
   p.stage_bytes = (CTA_M + p.tile_n / 2) * BLOCK_K * 2;
   bool mirrored = false;
   for (int i = 0; i < n; ++i) mirrored = mirrored || products[i].symmetric;
-  p.out_bytes = (precise ? 2 : 1) * (mirrored ? 2 : last ? 0 : 1) * BOX_BYTES;
+  p.out_bytes = last ? round_up(TURN_BYTES, 128) : (precise ? 2 : 1) * (mirrored ? 2 : 1) * BOX_BYTES;
   const int room = MAX_SMEM - 1024 - BAR_BYTES - (precise ? EPI_WARPS<true> : EPI_WARPS<false>) * p.out_bytes;
   p.stages = room / p.stage_bytes < MAX_STAGES ? room / p.stage_bytes : MAX_STAGES;
   p.ring_bytes = p.stages * p.stage_bytes;
