@@ -183,6 +183,7 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
       fresh = false;
     }
     __syncthreads();
+    int left = 1;
     if (!job.k_minor) {
       if (slice < slices) {
 #pragma unroll
@@ -192,6 +193,13 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
             for (int g = 0; g < G; ++g) part[(slice * a.r + j0 + v) * G + g] = acc[v][g];
       }
       __syncthreads();
+      // halves of the slices onto each other, as long as there are many (one after the other, 85 of them took 1.3 us)
+      for (left = slices; left > 4;) {
+        const int half = (left + 1) / 2, size = a.r * G;
+        for (int e = threadIdx.x; e < (left - half) * size; e += THREADS) part[e] += part[half * size + e];
+        left = half;
+        __syncthreads();
+      }
     }
     // (sums of tokens that use another adapter were taken along; they are not written)
     for (int e = threadIdx.x; e < a.r * G; e += THREADS) {
@@ -199,8 +207,7 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
       if (!(mask >> g & 1u)) continue;
       float s = 0.f;
       if (begin < end) {
-        const int sums = job.k_minor ? 1 : slices;
-        for (int k = 0; k < sums; ++k) s += part[(k * a.r + c) * G + g];
+        for (int k = 0; k < left; ++k) s += part[(k * a.r + c) * G + g];
       }
       int to = 0;
 #pragma unroll
@@ -239,22 +246,27 @@ template <bool F32, int G>
 __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_constant__ ExpandArgs a) {
   constexpr int V = VEC<F32>;
   __shared__ float p[MAX_RANK][G], sums[SHARES][V][G][32];
+  __shared__ int row[G];
   pdl_wait();
   const bool wide = (a.r_minor ? a.r : a.N) % V == 0;
   const int step = wide && !a.r_minor ? V : 1;              // columns of a thread
   const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, c = (blockIdx.y * 32 + lane) * step;
   int token[G], of[G];
   const int count = tokens_of<G>(a.index, a.order, a.T, a.n, token, of);
+  if (threadIdx.x == 0) {
 #pragma unroll
-  for (int g = 0; g < G; ++g)
-    for (int j = threadIdx.x; j < a.r; j += EXPAND_THREADS) {
-      float s = 0.f;
-      if (of[g] >= 0) {
+    for (int g = 0; g < G; ++g) row[g] = of[g] >= 0 ? token[g] : -1;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.r * G; e += EXPAND_THREADS) {
+    const int g = e / a.r, j = e - g * a.r;
+    float s = 0.f;
+    if (row[g] >= 0) {
 #pragma unroll 8
-        for (int k = 0; k < a.splits; ++k) s += __ldcg(a.P + (k * a.T + token[g]) * a.r + j);
-      }
-      p[j][g] = s;
+      for (int k = 0; k < a.splits; ++k) s += __ldcg(a.P + (k * a.T + row[g]) * a.r + j);
     }
+    p[j][g] = s;
+  }
   __syncthreads();
   // this warp's ranks, whole vectors of them
   const int each = ((a.r + SHARES - 1) / SHARES + V - 1) / V * V, j0 = share * each, j1 = j0 + each < a.r ? j0 + each : a.r;
@@ -368,8 +380,9 @@ struct GradArgs {
   long long T;
   int n, r;
 };
-constexpr int GRAD_COLS = 32, GRAD_TOKENS = 32;
-template <bool F32>
+constexpr int GRAD_COLS = 32, GRAD_TOKENS = 64;
+// U: ranks of a thread, at least r / 8.
+template <bool F32, int U>
 __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant__ GradArgs a) {
   __shared__ float p[GRAD_TOKENS][MAX_RANK], v[GRAD_TOKENS][GRAD_COLS];
   __shared__ int list[THREADS], found[THREADS / 32];
@@ -378,7 +391,7 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant
   const GradJob& job = a.job[which];
   const int c0 = (blockIdx.x - (which ? a.job[0].blocks : 0)) * GRAD_COLS;
   const int col = threadIdx.x & 31, jg = threadIdx.x >> 5, lane = col;
-  float acc[MAX_RANK / 8] = {};
+  float acc[U] = {};
   const int mine = a.order ? __ldcg(a.count + i) : static_cast<int>(a.T), from = a.order ? __ldcg(a.offset + i) : 0;
   for (int t0 = 0; t0 < mine; t0 += THREADS) {
     int all;
@@ -414,14 +427,14 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant
       for (int q = 0; q < m; ++q) {
         const float x = v[q][col];
 #pragma unroll
-        for (int u = 0; u < MAX_RANK / 8; ++u) if (jg + 8 * u < a.r) acc[u] = fmaf(p[q][jg + 8 * u], x, acc[u]);
+        for (int u = 0; u < U; ++u) if (jg + 8 * u < a.r) acc[u] = fmaf(p[q][jg + 8 * u], x, acc[u]);
       }
       __syncthreads();
     }
   }
   if (c0 + col >= job.N) return;
 #pragma unroll
-  for (int u = 0; u < MAX_RANK / 8; ++u) {
+  for (int u = 0; u < U; ++u) {
     const int j = jg + 8 * u;
     if (j >= a.r) break;
     const long long base = static_cast<long long>(i) * job.N * a.r;
@@ -443,7 +456,8 @@ bool on_tensor_cores(const ffsplit_projection& p, int n, long long T) {
 // Batches whose tokens are sorted by adapter first (few tokens are not: that is a launch more).
 bool is_sorted(long long T) { return T > adapter::FEW; }
 
-// Ranges of K of the products on the CUDA cores: as many blocks as SMs twice over, 64 elements each at least.
+// Ranges of K of the products on the CUDA cores: two blocks to an SM (as many as fit: a few more take twice as long), 64
+// elements each at least.
 int tokens_per_block(const ffsplit_projection& p, int n, long long T) {
   if (T > adapter::FEW) return p.dtype == FFSPLIT_F32 ? adapter::MANY : adapter::SOME;      // (bf16: 65000 adapters and more)
   return n == 1 ? adapter::SOME : 1;
@@ -451,7 +465,7 @@ int tokens_per_block(const ffsplit_projection& p, int n, long long T) {
 int splits_of(const ffsplit_projection& p, int n, long long T) {
   const int group = tokens_per_block(p, n, T), K = p.in > p.out ? p.in : p.out;
   const long long blocks = (T + group - 1) / group;
-  long long s = (2 * 148 + blocks - 1) / blocks;
+  long long s = 2 * 148 / blocks;
   if (s > K / 64) s = K / 64;
   return static_cast<int>(s < 1 ? 1 : s > adapter::MAX_SPLITS ? adapter::MAX_SPLITS : s);
 }
@@ -710,8 +724,10 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
   g.index = adapters->index; g.T = T; g.n = c.a.n; g.r = c.a.r;
   g.count = c.sorted.count; g.offset = c.sorted.offset; g.order = c.sorted.order;
   const dim3 grid(g.job[0].blocks + g.job[1].blocks, c.a.n);
-  const cudaError_t e = c.f32 ? launch_pdl(adapter::gradient_kernel<true>, grid, dim3(adapter::THREADS), 0, c.st, g)
-                              : launch_pdl(adapter::gradient_kernel<false>, grid, dim3(adapter::THREADS), 0, c.st, g);
+  const auto kernel = c.a.r <= 16 ? (c.f32 ? adapter::gradient_kernel<true, 2> : adapter::gradient_kernel<false, 2>)
+                      : c.a.r <= 64 ? (c.f32 ? adapter::gradient_kernel<true, 8> : adapter::gradient_kernel<false, 8>)
+                                    : (c.f32 ? adapter::gradient_kernel<true, 16> : adapter::gradient_kernel<false, 16>);
+  const cudaError_t e = launch_pdl(kernel, grid, dim3(adapter::THREADS), 0, c.st, g);
   ctx->launches++;
   return check_cuda(ctx, e, "adapter::gradient_kernel launch");
 }
