@@ -270,12 +270,19 @@ constexpr int MAX_RANGES = 8;
 
 __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_constant__ ShrinkParams p) {
   extern __shared__ uint8_t raw[];
-  pdl_wait();
   const ShrinkDev& job = p.job[blockIdx.z];
   const int ranges = gridDim.x, range = blockIdx.x;         // a cluster spans x
+  if (threadIdx.x == 0) {
+    ptx::prefetch_tmap(&job.V_tile);
+    ptx::prefetch_tmap(&job.F);
+  }
+  const Frame f = frame_open(raw, SHRINK_STAGES * p.stage, SHRINK_STAGES, SHRINK_TMEM);     // (under the tail of the kernel before)
+  pdl_wait();
   const Tile tile = find_tile(p.s, p.s.n, blockIdx.y);
-  if (tile.group < 0) return;                               // (the whole cluster)
-  const Frame f = frame_open(raw, SHRINK_STAGES * p.stage, SHRINK_STAGES, SHRINK_TMEM);
+  if (tile.group < 0) {                                     // (the whole cluster)
+    frame_close(f, SHRINK_TMEM, p.status);
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int per = (job.kb + ranges - 1) / ranges, k0 = range * per, k1 = k0 + per < job.kb ? k0 + per : job.kb;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -384,7 +391,7 @@ struct ExpandParams {
   Sorted s;
   const __nv_bfloat16* base;
   __nv_bfloat16* Y;
-  int N, r, f_mn, wide;       // f_mn: the columns run along memory; wide: rows start on 8 bytes
+  int N, r, f_mn;             // f_mn: the columns run along memory
   int blocks;                 // k-blocks of the rank: 1 or 2
   int* status;
 };
@@ -396,14 +403,22 @@ constexpr int EXPAND_WARPS = 8, EXPAND_COPY = 8, EXPAND_MMA = 9, EXPAND_TC_THREA
 constexpr int TURN_PITCH = 36, TURN_BYTES = 32 * TURN_PITCH * 4 + 32 * 8;      // 32 columns of 32 rows, and where the rows lie
 constexpr uint32_t EXPAND_TMEM = 128;
 
+// WIDE: rows start on 8 bytes, and lie within 2^32 pieces of 8 bytes.
+template <bool WIDE>
 __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const __grid_constant__ ExpandParams p) {
   extern __shared__ uint8_t raw[];
+  if (threadIdx.x == 0) {
+    ptx::prefetch_tmap(&p.P);
+    ptx::prefetch_tmap(&p.F);
+  }
+  const Frame f = frame_open<EXPAND_MMA>(raw, p.blocks * (A_BYTES + 2 * EXPAND_F), 3, EXPAND_TMEM, EXPAND_WARPS);     // (stages 0, 1: the factor, 2: P)
   pdl_wait();
   const Tile tile = find_tile(p.s, p.s.n + 1, blockIdx.y);
-  if (tile.group < 0) return;
   const bool none = tile.group == p.s.n;
-  if (none && p.base == p.Y) return;
-  const Frame f = frame_open<EXPAND_MMA>(raw, p.blocks * (A_BYTES + 2 * EXPAND_F), 3, EXPAND_TMEM, EXPAND_WARPS);     // (stages 0, 1: the factor, 2: P)
+  if (tile.group < 0 || (none && p.base == p.Y)) {
+    frame_close<EXPAND_MMA>(f, EXPAND_TMEM, p.status);
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int all = (p.N + EXPAND_COLS - 1) / EXPAND_COLS;
   const uint32_t factor0 = f.smem0 + p.blocks * A_BYTES;
@@ -468,9 +483,21 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
     uint8_t* area = raw + (f.smem0 - ptx::smem_u32(raw)) + p.blocks * (A_BYTES + 2 * EXPAND_F) + FRAME_BYTES + warp * TURN_BYTES;
     float* turn = reinterpret_cast<float*>(area);
     long long* row_at = reinterpret_cast<long long*>(area + 32 * TURN_PITCH * 4);
-    row_at[lane] = lane < rows ? static_cast<long long>(__ldcg(p.s.order + tile.first + quarter * 32 + lane)) * p.N : -1;
-    __syncwarp();
     const int up = lane >> 3, col = (lane & 7) * 4;
+    // where this lane's rows 4 k + up lie, in pieces of 8 bytes (from shared memory it was two more loads to four values)
+    uint32_t piece[8];
+    if (WIDE) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int row = 4 * k + up;
+        piece[k] = row < rows ? static_cast<uint32_t>(static_cast<unsigned long long>(__ldcg(p.s.order + tile.first + quarter * 32 + row)) * p.N / 4) : 0u;
+      }
+    } else {
+      row_at[lane] = lane < rows ? static_cast<long long>(__ldcg(p.s.order + tile.first + quarter * 32 + lane)) * p.N : -1;
+    }
+    __syncwarp();
+    const uint2* base8 = reinterpret_cast<const uint2*>(p.base);
+    uint2* Y8 = reinterpret_cast<uint2*>(p.Y);
     for (int i = 0, cb = blockIdx.x; cb < all; cb += gridDim.x, ++i) {
       const int c0 = cb * EXPAND_COLS + half * 64 + col;
       uint2 base[2][8];
@@ -479,12 +506,12 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
         const int c = c0 + 32 * h;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const long long at = row_at[4 * k + up];
           base[h][k] = make_uint2(0u, 0u);
-          if (p.base && at >= 0 && c < p.N) {
-            if (p.wide) {
-              base[h][k] = *reinterpret_cast<const uint2*>(p.base + at + c);
-            } else {
+          if (WIDE) {
+            if (p.base && 4 * k + up < rows && c < p.N) base[h][k] = base8[static_cast<size_t>(piece[k]) + (c >> 2)];
+          } else {
+            const long long at = row_at[4 * k + up];
+            if (p.base && at >= 0 && c < p.N) {
               const unsigned short* q = reinterpret_cast<const unsigned short*>(p.base + at + c);
               base[h][k].x = q[0] | (c + 1 < p.N ? static_cast<uint32_t>(q[1]) << 16 : 0u);
               base[h][k].y = (c + 2 < p.N ? q[2] : 0u) | (c + 3 < p.N ? static_cast<uint32_t>(q[3]) << 16 : 0u);
@@ -508,15 +535,15 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
         __syncwarp();
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const long long at = row_at[4 * k + up];
           const float4 x = none ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(turn + (4 * k + up) * TURN_PITCH + col);
           const uint2 q = base[h][k];
           const uint32_t lo = bf16_pair(__uint_as_float(q.x << 16) + x.x, __uint_as_float(q.x & 0xffff0000u) + x.y);
           const uint32_t hi = bf16_pair(__uint_as_float(q.y << 16) + x.z, __uint_as_float(q.y & 0xffff0000u) + x.w);
-          if (at >= 0 && c < p.N) {
-            if (p.wide) {
-              *reinterpret_cast<uint2*>(p.Y + at + c) = make_uint2(lo, hi);
-            } else {
+          if (WIDE) {
+            if (4 * k + up < rows && c < p.N) Y8[static_cast<size_t>(piece[k]) + (c >> 2)] = make_uint2(lo, hi);
+          } else {
+            const long long at = row_at[4 * k + up];
+            if (at >= 0 && c < p.N) {
               unsigned short* o = reinterpret_cast<unsigned short*>(p.Y + at + c);
               o[0] = static_cast<unsigned short>(lo);
               if (c + 1 < p.N) o[1] = static_cast<unsigned short>(lo >> 16);
@@ -554,13 +581,17 @@ constexpr uint32_t GRADIENT_TMEM = 128;
 
 __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_constant__ GradientParams p) {
   extern __shared__ uint8_t raw[];
-  pdl_wait();
   const int which = static_cast<int>(blockIdx.x) >= p.job[0].blocks ? 1 : 0, i = blockIdx.y;
   const GradientDev& job = p.job[which];
   const int c0 = (blockIdx.x - (which ? p.job[0].blocks : 0)) * TOKENS;     // 128 columns of V: the rows of the tile
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int count = __ldcg(p.s.count + i), first = __ldcg(p.s.offset + i);
+  if (threadIdx.x == 0) {
+    ptx::prefetch_tmap(&job.V_tile);
+    ptx::prefetch_tmap(&job.P);
+  }
   const Frame f = frame_open(raw, GRADIENT_STAGES * p.stage, GRADIENT_STAGES, GRADIENT_TMEM);
+  pdl_wait();
+  const int count = __ldcg(p.s.count + i), first = __ldcg(p.s.offset + i);
   const int kb = (count + BLOCK_K - 1) / BLOCK_K;
   if (warp == COPY_WARP) {
     const int tile0 = tiles_before(p.s, i);
@@ -698,7 +729,8 @@ ffsplit_status set_up(ffsplit_ctx* ctx) {
   if (bound != cudaSuccess) return check_cuda(ctx, bound, "cudaSetDevice");
   if (ctx->attr_adapter_set) return FFSPLIT_OK;
   cudaError_t e = cudaFuncSetAttribute(shrink_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(SHRINK_STAGES, MAX_RANK));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(expand_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, expand_smem(MAX_RANK));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(expand_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, expand_smem(MAX_RANK));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(expand_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, expand_smem(MAX_RANK));
   if (e == cudaSuccess) e = cudaFuncSetAttribute(gradient_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(GRADIENT_STAGES, MAX_RANK));
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(adapter kernels)");
   ctx->attr_adapter_set = true;
@@ -764,13 +796,14 @@ ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const 
   if ((rc = encode_factor(ctx, F, s.n, p.f_mn ? BLOCK_K : EXPAND_COLS, &p.F)) != FFSPLIT_OK) return rc;
   p.s = s;
   p.base = static_cast<const __nv_bfloat16*>(base); p.Y = static_cast<__nv_bfloat16*>(Y);
-  p.N = N; p.r = r; p.wide = N % 4 == 0; p.status = ctx->status();
+  p.N = N; p.r = r; p.status = ctx->status();
   p.blocks = r > BLOCK_K ? 2 : 1;
   // Two CTAs to an SM where there are few tiles, else four blocks of columns to a CTA: its start is paid once, and the last
   // round of CTAs stays short (fourteen blocks each, 342 CTAs on 296 places: 114 us instead of 57).
   const long long blocks = (N + EXPAND_COLS - 1) / EXPAND_COLS, fill = (2 * ctx->num_sms + tiles - 1) / tiles, four = (blocks + 3) / 4;
   const long long wanted = fill > four ? fill : four;
-  const cudaError_t e = launch_pdl(expand_tc_kernel, dim3(static_cast<unsigned>(wanted < blocks ? wanted : blocks), static_cast<unsigned>(tiles)), dim3(EXPAND_TC_THREADS),
+  const bool wide = N % 4 == 0 && s.T * (N / 4) <= 0xffffffffll;
+  const cudaError_t e = launch_pdl(wide ? expand_tc_kernel<true> : expand_tc_kernel<false>, dim3(static_cast<unsigned>(wanted < blocks ? wanted : blocks), static_cast<unsigned>(tiles)), dim3(EXPAND_TC_THREADS),
                                    expand_smem(r), st, p);
   ctx->launches++;
   return check_cuda(ctx, e, "adapter::expand_tc_kernel launch");
