@@ -288,13 +288,11 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   float* part = reinterpret_cast<float*>(smem);
   const int part_pitch = p.cols + 4;
+  // A tile that is one run: one box (rows behind its last token are other tokens', and their sums are not written), by the copy
+  // warp.  Else every epilogue warp copies its 32 rows (one warp alone took 1.4 us for 128 rows, most of it to issue).
+  const int top = __ldcg(p.s.order + tile.first);
+  const bool whole = __ldcg(p.s.order + tile.first + tile.rows - 1) - top == tile.rows - 1;
   if (warp == COPY_WARP) {
-    // a tile that is one run: one box (rows behind its last token are other tokens', and their sums are not written)
-    const int top = __ldcg(p.s.order + tile.first);
-    const bool whole = __ldcg(p.s.order + tile.first + tile.rows - 1) - top == tile.rows - 1;
-    Rows rows;
-    if (!whole) rows = rows_of(p.s, tile.first, tile.rows, (lane & 7) * ROWS);
-    const bool has = whole ? lane == 0 : lane < 8 && rows.any;
     // the factor's box: 64 k x 64 ranks, one or two of them; or all ranks (as many rows as there are columns of the tile) x 64 k
     const uint32_t tx = static_cast<uint32_t>((whole ? A_BYTES : (tile.rows + ROWS - 1) / ROWS * (ROWS * 128)) + (job.f_mn ? (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES : p.cols * BLOCK_K * 2));
     bool ok = true;
@@ -303,8 +301,9 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
       ok = ptx::mbar_wait_warp(&f.empty[s], ((i / SHRINK_STAGES) & 1) ^ 1, f.abort_flag);
       if (!ok) break;
       const uint32_t to = f.smem0 + s * p.stage, bar = ptx::smem_u32(&f.full[s]);
-      if (lane == 0) {
+      if (ptx::elect_one()) {
         ptx::mbar_expect_tx(&f.full[s], tx);
+        if (whole) load_2d(&job.V_tile, to, bar, kb * BLOCK_K, top);
         if (job.f_mn) {
           load_3d(&job.F, to + A_BYTES, bar, 0, kb * BLOCK_K, tile.group);
           if (p.cols > 64) load_3d(&job.F, to + A_BYTES + BLOCK64_BYTES, bar, 64, kb * BLOCK_K, tile.group);
@@ -313,10 +312,6 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
         }
       }
       __syncwarp();
-      if (has) {
-        if (whole) load_2d(&job.V_tile, to, bar, kb * BLOCK_K, top);
-        else load_rows(&job.V_box, &job.V, to + lane * (ROWS * 128), bar, kb * BLOCK_K, rows);
-      }
     }
     if (!ok) copies_gave_up();
     __syncwarp();
@@ -344,6 +339,21 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
     }
   } else {
     const bool any = k0 < k1;
+    if (!whole && warp * 32 < tile.rows) {
+      // (what these copies bring is counted by the copy warp, before or after them)
+      const Rows rows = rows_of(p.s, tile.first, tile.rows, warp * 32 + (lane & 1) * ROWS);
+      bool ok = true;
+      for (int kb = k0, i = 0; kb < k1; ++kb, ++i) {
+        const int s = i % SHRINK_STAGES;
+        ok = ptx::mbar_wait_warp(&f.empty[s], ((i / SHRINK_STAGES) & 1) ^ 1, f.abort_flag);
+        if (!ok) break;
+        if (lane < 2 && rows.any)
+          load_rows(&job.V_box, &job.V, f.smem0 + s * p.stage + (warp * 32 + lane * ROWS) * 128, ptx::smem_u32(&f.full[s]), kb * BLOCK_K, rows);
+        __syncwarp();
+      }
+      if (!ok) copies_gave_up();
+      __syncwarp();
+    }
     if (ptx::mbar_wait(f.done, 0, f.abort_flag)) {
       ptx::tc_fence_after();
       // every copy has landed and every MMA has read it: the ring is free
