@@ -470,8 +470,25 @@ int splits_of(const ffsplit_projection& p, int n, long long T) {
   return static_cast<int>(s < 1 ? 1 : s > adapter::MAX_SPLITS ? adapter::MAX_SPLITS : s);
 }
 
+// The adapters' part inside the shared product, in a product of `width` columns over `sum`: entries to a tile of 256 rows.  An
+// entry costs a tile as much as one or two k-blocks of its sum; where a tile has more adapters than half its k-blocks, or than
+// 32, a second pass over Y is cheaper.  So it is where Y is small: the pass moves 2.7 TB/s (63 us of 335 for 4096 x 11008), while
+// checking the factors and planning the entries take 20 us and the entries of 24 adapters 30 us in that product.  The entries
+// take 32 KB (64 KB) each, 256 MB in all at most.
+int extension_most(const ffsplit_projection& p, int n, int r, long long T, int sum, int width) {
+  if (!on_tensor_cores(p, n, T) || T * width < (32ll << 20)) return 0;
+  const long long blocks = (sum + 63) / 64, pitch = adapter::rank_pitch(r);
+  long long most = blocks / (2 * (pitch / 64));
+  if (most > 32) most = 32;
+  if (most > n) most = n;
+  const long long room = (256ll << 20) / (adapter::extension_tiles(T) * adapter::EXTENSION_ROWS * pitch * 2);
+  return static_cast<int>(most < room ? most : room);
+}
+
 struct AdapterLayout {
   long long ldi, ldo, ldr;
+  int most, most_back;      // entries to a tile forward, backward
+  size_t slot, Q;
   size_t P, D, sorted, X, dY, W, A, B, parts, parts_bytes, end;
 };
 AdapterLayout adapter_layout(const ffsplit_projection& p, int n, int r, long long T) {
@@ -487,6 +504,11 @@ AdapterLayout adapter_layout(const ffsplit_projection& p, int n, int r, long lon
   take(&L.P, inner);
   take(&L.D, inner);
   take(&L.sorted, is_sorted(T) ? (static_cast<size_t>(T) + 2 * (static_cast<size_t>(n) + 1)) * 4 : 0);
+  L.most = extension_most(p, n, r, T, p.in, p.out);
+  L.most_back = extension_most(p, n, r, T, p.out, p.in);
+  const size_t tiles = static_cast<size_t>(adapter::extension_tiles(T)), most = L.most > L.most_back ? L.most : L.most_back;
+  take(&L.slot, most ? (static_cast<size_t>(T) + 2 * tiles * (most + 1) + n) * 4 : 0);
+  take(&L.Q, tiles * most * adapter::EXTENSION_ROWS * adapter::rank_pitch(r) * 2);
   take(&L.X, f32 || p.in % 8 ? static_cast<size_t>(T) * L.ldi * 2 * planes : 0);
   take(&L.dY, f32 || p.out % 8 ? static_cast<size_t>(T) * L.ldo * 2 * planes : 0);
   take(&L.W, f32 || p.out % 8 ? static_cast<size_t>(p.in) * L.ldo * 2 * planes : 0);
@@ -551,20 +573,34 @@ struct Call {
   void use_W(const void* w) { W = train::operand(&prep, &prep_blocks, f32, w, p.in, p.out, L.ldo, ws + L.W); }
   void use_A() { A = {train::operand(&prep, &prep_blocks, false, a.A, static_cast<long long>(a.n) * p.in, a.r, L.ldr, ws + L.A), p.in, a.r, 0}; }
   void use_B() { B = {train::operand(&prep, &prep_blocks, false, a.B, static_cast<long long>(a.n) * a.r, p.out, L.ldo, ws + L.B), a.r, p.out, 1}; }
-  ffsplit_status prepare() {
+  // most > 0: the adapters' part is taken along in the shared product, where `F` is the factor (as it came: `each` elements)
+  ffsplit_status prepare(int most, const void* F, long long each) {
     if (is_sorted(T)) {
       sorted.count = reinterpret_cast<int*>(ws + L.sorted);
       sorted.offset = sorted.count + a.n + 1;
       sorted.order = sorted.offset + a.n + 1;
       sorted.n = a.n;
       sorted.T = T;
-      const ffsplit_status s = adapter::launch_sort(ctx, a.index, sorted, st);
+      if (most > 0) {
+        const size_t tiles = static_cast<size_t>(adapter::extension_tiles(T));
+        sorted.most = most;
+        sorted.slot = reinterpret_cast<int*>(ws + L.slot);
+        sorted.entries = sorted.slot + T;
+        sorted.ids = sorted.entries + tiles;
+        sorted.left = sorted.ids + tiles * most;
+        sorted.list = sorted.left + tiles;
+        sorted.broken = sorted.list + tiles * most;
+        sorted.Q = reinterpret_cast<__nv_bfloat16*>(ws + L.Q);
+        sorted.pitch = adapter::rank_pitch(a.r);
+      }
+      ffsplit_status s = adapter::launch_sort(ctx, a.index, sorted, st);
+      if (s == FFSPLIT_OK && most > 0) s = adapter::launch_check(ctx, F, each, sorted, st);
       if (s != FFSPLIT_OK) return s;
     }
     return train::launch_prepare(ctx, prep, prep_blocks, f32, st);
   }
   // C [T, N] = V [T, K] times W [in, out] (transposed: its transpose).
-  ffsplit_status shared_product(const tg::Matrix& V, const void* bias, bool transposed, void* C) {
+  ffsplit_status shared_product(const tg::Matrix& V, const void* bias, bool transposed, void* C, const adapter::Factor* F = nullptr) {
     tg::Product g;
     std::memset(&g, 0, sizeof(g));
     g.a[0] = V; g.b[0] = W;
@@ -573,7 +609,17 @@ struct Call {
     g.M = T; g.N = transposed ? p.in : p.out; g.K = transposed ? p.out : p.in;
     g.C = C; g.ldc = g.N; g.bias = bias;
     g.b_ready = 1;      // (the launch before is a shrink: W, or its copy, is complete)
-    return tg::launch(ctx, tg::PLAIN, 0, f32, &g, 1, tg::Hidden{}, ws + L.parts, L.parts_bytes, st);
+    tg::Extension e;
+    std::memset(&e, 0, sizeof(e));
+    if (F) {
+      e.Q = sorted.Q;
+      e.entries = adapter::extension_tiles(T) * sorted.most;
+      e.pitch = sorted.pitch; e.most = sorted.most;
+      e.F = {F->m.p, F->rows, F->cols, F->m.ld, F->rows * F->m.ld, a.n};
+      e.rank = a.r;
+      e.count = sorted.left; e.list = sorted.list;
+    }
+    return tg::launch(ctx, tg::PLAIN, 0, f32, &g, 1, tg::Hidden{}, ws + L.parts, L.parts_bytes, st, nullptr, F ? &e : nullptr);
   }
 };
 
@@ -644,9 +690,10 @@ ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projectio
     c.use_A();
     c.use_B();
   }
-  if ((s = c.prepare()) != FFSPLIT_OK) return s;
+  const bool extended = W && c.L.most > 0;
+  if ((s = c.prepare(extended ? c.L.most : 0, adapters->B, static_cast<long long>(c.a.r) * c.p.out)) != FFSPLIT_OK) return s;
   if (c.tc) {
-    const adapter::Shrink job = {c.X, c.A, c.tiles(c.L.P), c.p.in};
+    const adapter::Shrink job = {c.X, c.A, c.tiles(c.L.P), c.p.in, extended ? 1 : 0};
     if ((s = adapter::launch_shrink_tc(ctx, &job, 1, c.sorted, c.a.r, c.a.scale, c.st)) != FFSPLIT_OK) return s;
   } else {
     adapter::ShrinkArgs sh;
@@ -654,8 +701,8 @@ ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projectio
     sh.job[0] = {X, adapters->A, c.inner(c.L.P), c.p.in, 0};
     if ((s = launch_shrink(c, sh, 1)) != FFSPLIT_OK) return s;
   }
-  if (W && (s = c.shared_product(c.X, bias, false, Y)) != FFSPLIT_OK) return s;
-  if (c.tc) return adapter::launch_expand_tc(ctx, c.tiles(c.L.P), c.B, c.p.out, W ? Y : base, Y, c.sorted, c.a.r, c.st);
+  if (W && (s = c.shared_product(c.X, bias, false, Y, extended ? &c.B : nullptr)) != FFSPLIT_OK) return s;
+  if (c.tc) return adapter::launch_expand_tc(ctx, c.tiles(c.L.P), c.B, c.p.out, W ? Y : base, Y, c.sorted, c.a.r, extended, c.st);
   return launch_expand(c, c.inner(c.L.P), splits_of(c.p, c.a.n, T), adapters->B, W ? Y : base, Y, c.p.out, 0);
 }
 
@@ -679,12 +726,13 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
     c.use_A();
     if (dX || dA) c.use_B();
   }
-  if ((s = c.prepare()) != FFSPLIT_OK) return s;
+  const bool extended = dX && W && c.L.most_back > 0;
+  if ((s = c.prepare(extended ? c.L.most_back : 0, adapters->A, static_cast<long long>(c.p.in) * c.a.r)) != FFSPLIT_OK) return s;
   int n = 0, splits = splits_of(c.p, c.a.n, T);
   if (c.tc) {
     adapter::Shrink jobs[2];
-    if (dX || dA) jobs[n++] = {c.dY, c.B, c.tiles(c.L.D), c.p.out};
-    if (dB) jobs[n++] = {c.X, c.A, c.tiles(c.L.P), c.p.in};
+    if (dX || dA) jobs[n++] = {c.dY, c.B, c.tiles(c.L.D), c.p.out, extended ? 1 : 0};
+    if (dB) jobs[n++] = {c.X, c.A, c.tiles(c.L.P), c.p.in, 0};
     if ((s = adapter::launch_shrink_tc(ctx, jobs, n, c.sorted, c.a.r, c.a.scale, c.st)) != FFSPLIT_OK) return s;
   } else {
     adapter::ShrinkArgs sh;
@@ -702,9 +750,9 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
     }
   }
   if (dX) {
-    if (W && (s = c.shared_product(c.dY, nullptr, true, grads->dX)) != FFSPLIT_OK) return s;
+    if (W && (s = c.shared_product(c.dY, nullptr, true, grads->dX, extended ? &c.A : nullptr)) != FFSPLIT_OK) return s;
     const void* add = W ? grads->dX : base;
-    s = c.tc ? adapter::launch_expand_tc(ctx, c.tiles(c.L.D), c.A, c.p.in, add, grads->dX, c.sorted, c.a.r, c.st)
+    s = c.tc ? adapter::launch_expand_tc(ctx, c.tiles(c.L.D), c.A, c.p.in, add, grads->dX, c.sorted, c.a.r, extended, c.st)
              : launch_expand(c, c.inner(c.L.D), splits, adapters->A, add, grads->dX, c.p.in, 1);
     if (s != FFSPLIT_OK) return s;
   }

@@ -15,7 +15,18 @@ struct Sorted {
   int* order;               // [T]
   int n;
   long long T;
+  // The adapters' part of a shared product inside that product (see tg::Extension): entries for the tiles of 256 rows that
+  // have no more than `most` adapters.  most = 0: there are none.
+  int most;
+  int* slot;                // [T]: the entry of each token's adapter in its tile, -1: the tile has no entries
+  int *entries, *ids;       // [tiles], [tiles][most]
+  int *left, *list;         // the same without broken ones, as tg::Extension has them
+  int* broken;              // [n]: an adapter's factor holds an infinity or NaN, which would reach all rows of a tile
+  __nv_bfloat16* Q;         // [tiles][most][256][pitch]
+  int pitch;
 };
+constexpr int EXTENSION_ROWS = 256;
+inline long long extension_tiles(long long T) { return (T + EXTENSION_ROWS - 1) / EXTENSION_ROWS; }
 // Tiles of all groups, group after group: no more than this.
 inline long long tile_bound(long long T, int n) { return (T + TOKENS - 1) / TOKENS + (n + 1 < T ? n + 1 : T); }
 inline int rank_pitch(int r) { return r <= 64 ? 64 : 128; }
@@ -27,19 +38,23 @@ struct Factor {
 };
 
 ffsplit_status launch_sort(ffsplit_ctx* ctx, const int* index, const Sorted& s, cudaStream_t st);
+// broken[i] of the adapters that are used, from their factors: `each` elements one after the other.
+ffsplit_status launch_check(ffsplit_ctx* ctx, const void* F, long long each, const Sorted& s, cudaStream_t st);
 
-// P = scale_i V F_i for every tile: [tiles][128][pitch] bf16, zero rows behind the last token.  Up to two at once.
+// P = scale_i V F_i for every tile: [tiles][128][pitch] bf16, zero rows behind the last token; and into the entries of the
+// extension, where the tokens have one.  Up to two at once.
 struct Shrink {
   tg::Matrix V;             // [T, K]
   Factor F;
   __nv_bfloat16* P;
   int K;
+  int extends;
 };
 ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, const Sorted& s, int r, const float* scale, cudaStream_t st);
 
-// Y[t] = base[t] + P F_i: [T, N], pitch N.
+// Y[t] = base[t] + P F_i: [T, N], pitch N.  rest: only the tokens that the extension leaves out.
 ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const Factor& F, int N, const void* base, void* Y, const Sorted& s,
-                                int r, cudaStream_t st);
+                                int r, bool rest, cudaStream_t st);
 
 // out_i = sum over the adapter's tokens of V[t]^T P[t] ([n][N][r], rank_rows: its transpose, [n][r][N]).  Up to two at once.
 struct Gradient {

@@ -29,10 +29,54 @@ constexpr int A_BYTES = TOKENS * BLOCK_K * 2, B_BYTES = MAX_RANK * BLOCK_K * 2;
 // ---------------------------------------------------------------------------------------------- sorting
 // A block to a group: one pass counts its tokens and those of the groups before it, another writes them in their order.
 constexpr int SORT_THREADS = 256, SORT_FLIGHT = 4;
+// Blocks behind the groups: the entries of a tile of 256 rows, and zeros where their rows will be.
+__device__ __forceinline__ void plan_tile(const int* __restrict__ index, const Sorted& s, int tile) {
+  __shared__ __align__(16) int of[EXTENSION_ROWS];
+  __shared__ int ids[EXTENSION_ROWS], firsts[EXTENSION_ROWS / 32];
+  const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
+  const long long t = static_cast<long long>(tile) * EXTENSION_ROWS + i;
+  int mine = t < s.T ? __ldg(index + t) : -1;
+  if (mine >= s.n) mine = -1;
+  of[i] = mine;
+  __syncthreads();
+  bool first = mine >= 0;
+#pragma unroll 4
+  for (int k = 0; k < i; k += 4) {
+    const int4 q = *reinterpret_cast<const int4*>(of + k);
+    first = first && q.x != mine && (k + 1 >= i || q.y != mine) && (k + 2 >= i || q.z != mine) && (k + 3 >= i || q.w != mine);
+  }
+  const unsigned votes = __ballot_sync(0xffffffffu, first);
+  if (lane == 0) firsts[warp] = __popc(votes);
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < EXTENSION_ROWS / 32; ++w) {
+    if (w < warp) before += firsts[w];
+    all += firsts[w];
+  }
+  if (first) ids[before + __popc(votes & ((1u << lane) - 1u))] = mine;
+  __syncthreads();
+  const bool kept = all <= s.most;
+  int slot = -1;
+  if (kept && mine >= 0)
+    for (int k = 0; k < all; ++k) if (ids[k] == mine) slot = k;
+  if (t < s.T) s.slot[t] = slot;
+  if (i == 0) s.entries[tile] = kept ? all : 0;
+  if (!kept) return;
+  if (i < all) s.ids[static_cast<long long>(tile) * s.most + i] = ids[i];
+  uint4* Q = reinterpret_cast<uint4*>(s.Q + static_cast<long long>(tile) * s.most * EXTENSION_ROWS * s.pitch);
+  for (int k = i; k < all * EXTENSION_ROWS * s.pitch / 8; k += SORT_THREADS) Q[k] = make_uint4(0u, 0u, 0u, 0u);
+}
+static_assert(SORT_THREADS == EXTENSION_ROWS, "a thread to a row");
 __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const int* __restrict__ index, Sorted s, int* status) {
   __shared__ int red[2][SORT_THREADS / 32], found[SORT_FLIGHT][SORT_THREADS / 32];
   pdl_wait();
   const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (g > s.n) {
+    plan_tile(index, s, g - s.n - 1);
+    return;
+  }
+  if (s.most && g < s.n && threadIdx.x == 0) s.broken[g] = 0;
   const auto group_of = [&](int i) { return i < 0 || i >= s.n ? s.n : i; };
   int mine = 0, before = 0;
   for (long long t0 = threadIdx.x; t0 < s.T; t0 += SORT_THREADS * SORT_FLIGHT) {
@@ -90,6 +134,32 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const int* __restric
     }
     __syncthreads();
   }
+}
+
+// A row of blocks to an adapter.
+constexpr int CHECK_CHUNK = 32768;      // elements
+__global__ void __launch_bounds__(256) check_kernel(const __nv_bfloat16* __restrict__ F, long long each, Sorted s) {
+  pdl_wait();
+  const int i = blockIdx.y;
+  if (__ldcg(s.count + i) == 0) return;
+  const long long begin = static_cast<long long>(blockIdx.x) * CHECK_CHUNK, end = begin + CHECK_CHUNK < each ? begin + CHECK_CHUNK : each;
+  const unsigned short* p = reinterpret_cast<const unsigned short*>(F) + i * each;
+  bool bad = false;
+  const int lead = static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(p + begin) & 15u)) & 15u) / 2);
+  const long long body = begin + lead < end ? begin + lead : end, vectors = (end - body) / 8;
+  const uint4* v = reinterpret_cast<const uint4*>(p + body);
+#pragma unroll 4
+  for (long long k = threadIdx.x; k < vectors; k += 256) {
+    const uint4 q = __ldg(v + k);
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bad = bad || (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
+  }
+  if (threadIdx.x < 16) {      // what is left at either end
+    const long long k = threadIdx.x < 8 ? begin + threadIdx.x : body + vectors * 8 + threadIdx.x - 8;
+    if (k < (threadIdx.x < 8 ? body : end)) bad = bad || (__ldg(p + k) & 0x7f80u) == 0x7f80u;
+  }
+  if (__syncthreads_or(bad ? 1 : 0) && threadIdx.x == 0) s.broken[i] = 1;
 }
 
 struct Tile {
@@ -252,6 +322,7 @@ struct ShrinkDev {
   CUtensorMap V, V_box, V_tile, F;
   __nv_bfloat16* P;
   int kb, f_mn;               // f_mn: the rank runs along memory
+  int extends;
 };
 struct ShrinkParams {
   ShrinkDev job[2];
@@ -278,6 +349,16 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
   }
   const Frame f = frame_open(raw, SHRINK_STAGES * p.stage, SHRINK_STAGES, SHRINK_TMEM);     // (under the tail of the kernel before)
   pdl_wait();
+  // in passing: the lists of the extension's tiles, now that the factors are checked
+  if (p.s.most && blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x < 32 && blockIdx.y < (p.s.T + EXTENSION_ROWS - 1) / EXTENSION_ROWS) {
+    const int e = threadIdx.x, at = blockIdx.y * p.s.most + e;
+    const bool in = e < __ldcg(p.s.entries + blockIdx.y);   // (no more than 32)
+    const int id = in ? __ldcg(p.s.ids + at) : 0;
+    const bool sound = in && __ldcg(p.s.broken + id) == 0;
+    const unsigned votes = __ballot_sync(0xffffffffu, sound);
+    if (sound) p.s.list[blockIdx.y * p.s.most + __popc(votes & ((1u << e) - 1u))] = id | e << 16;
+    if (e == 0) p.s.left[blockIdx.y] = __popc(votes);
+  }
   const Tile tile = find_tile(p.s, p.s.n, blockIdx.y);
   if (tile.group < 0) {                                     // (the whole cluster)
     frame_close(f, SHRINK_TMEM, p.status);
@@ -389,7 +470,13 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
 #pragma unroll
       for (int k = 0; k < MAX_RANGES; ++k) { x += a[k]; y += b[k]; }
     }
-    *reinterpret_cast<uint32_t*>(P + static_cast<long long>(row) * p.pitch + c) = bf16_pair(scale * x, scale * y);
+    const uint32_t pair = bf16_pair(scale * x, scale * y);
+    *reinterpret_cast<uint32_t*>(P + static_cast<long long>(row) * p.pitch + c) = pair;
+    if (job.extends && row < tile.rows) {
+      const int token = __ldcg(p.s.order + tile.first + row), slot = __ldcg(p.s.slot + token);
+      if (slot >= 0)
+        *reinterpret_cast<uint32_t*>(p.s.Q + ((static_cast<long long>(token / EXTENSION_ROWS) * p.s.most + slot) * EXTENSION_ROWS + token % EXTENSION_ROWS) * p.pitch + c) = pair;
+    }
   }
   ptx::cluster_sync_all();      // nobody leaves while its sums are read
   frame_close(f, SHRINK_TMEM, p.status);
@@ -403,6 +490,7 @@ struct ExpandParams {
   __nv_bfloat16* Y;
   int N, r, f_mn;             // f_mn: the columns run along memory
   int blocks;                 // k-blocks of the rank: 1 or 2
+  int rest;                   // rows that the extension has added are left as they are
   int* status;
 };
 // A CTA keeps a tile's P and goes through every gridDim.x-th block of columns: the factor's next block is on its way while
@@ -425,7 +513,11 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
   pdl_wait();
   const Tile tile = find_tile(p.s, p.s.n + 1, blockIdx.y);
   const bool none = tile.group == p.s.n;
-  if (tile.group < 0 || (none && p.base == p.Y)) {
+  bool leave = tile.group < 0 || (none && p.base == p.Y);
+  const bool by_slot = p.rest && !leave && __ldcg(p.s.broken + tile.group) == 0;
+  const auto done_before = [&](int row) { return by_slot && __ldcg(p.s.slot + __ldcg(p.s.order + tile.first + row)) >= 0; };
+  if (by_slot) leave = __syncthreads_or(static_cast<int>(threadIdx.x) < tile.rows && !done_before(threadIdx.x)) == 0;
+  if (leave) {
     frame_close<EXPAND_MMA>(f, EXPAND_TMEM, p.status);
     return;
   }
@@ -496,6 +588,8 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
     const int up = lane >> 3, col = (lane & 7) * 4;
     // where this lane's rows 4 k + up lie, in pieces of 8 bytes (from shared memory it was two more loads to four values)
     uint32_t piece[8];
+    // (bit 4 k + up: that row is to be written)
+    const uint32_t live = __ballot_sync(0xffffffffu, lane < rows && !done_before(quarter * 32 + lane));
     if (WIDE) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -503,7 +597,7 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
         piece[k] = row < rows ? static_cast<uint32_t>(static_cast<unsigned long long>(__ldcg(p.s.order + tile.first + quarter * 32 + row)) * p.N / 4) : 0u;
       }
     } else {
-      row_at[lane] = lane < rows ? static_cast<long long>(__ldcg(p.s.order + tile.first + quarter * 32 + lane)) * p.N : -1;
+      row_at[lane] = live >> lane & 1u ? static_cast<long long>(__ldcg(p.s.order + tile.first + quarter * 32 + lane)) * p.N : -1;
     }
     __syncwarp();
     const uint2* base8 = reinterpret_cast<const uint2*>(p.base);
@@ -518,7 +612,7 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
         for (int k = 0; k < 8; ++k) {
           base[h][k] = make_uint2(0u, 0u);
           if (WIDE) {
-            if (p.base && 4 * k + up < rows && c < p.N) base[h][k] = base8[static_cast<size_t>(piece[k]) + (c >> 2)];
+            if (p.base && (live >> (4 * k + up) & 1u) && c < p.N) base[h][k] = base8[static_cast<size_t>(piece[k]) + (c >> 2)];
           } else {
             const long long at = row_at[4 * k + up];
             if (p.base && at >= 0 && c < p.N) {
@@ -550,7 +644,7 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
           const uint32_t lo = bf16_pair(__uint_as_float(q.x << 16) + x.x, __uint_as_float(q.x & 0xffff0000u) + x.y);
           const uint32_t hi = bf16_pair(__uint_as_float(q.y << 16) + x.z, __uint_as_float(q.y & 0xffff0000u) + x.w);
           if (WIDE) {
-            if (4 * k + up < rows && c < p.N) Y8[static_cast<size_t>(piece[k]) + (c >> 2)] = make_uint2(lo, hi);
+            if ((live >> (4 * k + up) & 1u) && c < p.N) Y8[static_cast<size_t>(piece[k]) + (c >> 2)] = make_uint2(lo, hi);
           } else {
             const long long at = row_at[4 * k + up];
             if (at >= 0 && c < p.N) {
@@ -750,9 +844,17 @@ ffsplit_status set_up(ffsplit_ctx* ctx) {
 }  // namespace
 
 ffsplit_status launch_sort(ffsplit_ctx* ctx, const int* index, const Sorted& s, cudaStream_t st) {
-  const cudaError_t e = launch_pdl(sort_kernel, dim3(s.n + 1), dim3(SORT_THREADS), 0, st, index, s, ctx->status());
+  const unsigned blocks = static_cast<unsigned>(s.n + 1 + (s.most ? extension_tiles(s.T) : 0));
+  const cudaError_t e = launch_pdl(sort_kernel, dim3(blocks), dim3(SORT_THREADS), 0, st, index, s, ctx->status());
   ctx->launches++;
   return check_cuda(ctx, e, "adapter::sort_kernel launch");
+}
+
+ffsplit_status launch_check(ffsplit_ctx* ctx, const void* F, long long each, const Sorted& s, cudaStream_t st) {
+  const dim3 grid(static_cast<unsigned>((each + CHECK_CHUNK - 1) / CHECK_CHUNK), s.n);
+  const cudaError_t e = launch_pdl(check_kernel, grid, dim3(256), 0, st, static_cast<const __nv_bfloat16*>(F), each, s);
+  ctx->launches++;
+  return check_cuda(ctx, e, "adapter::check_kernel launch");
 }
 
 ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, const Sorted& s, int r, const float* scale, cudaStream_t st) {
@@ -768,6 +870,7 @@ ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, con
     d.f_mn = jobs[i].F.rank_rows ? 0 : 1;
     if ((rc = encode_factor(ctx, jobs[i].F, s.n, d.f_mn ? BLOCK_K : p.cols, &d.F)) != FFSPLIT_OK) return rc;
     d.P = jobs[i].P;
+    d.extends = jobs[i].extends;
     d.kb = (jobs[i].K + BLOCK_K - 1) / BLOCK_K;
     if (d.kb > kb) kb = d.kb;
   }
@@ -795,7 +898,7 @@ ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, con
 }
 
 ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const Factor& F, int N, const void* base, void* Y, const Sorted& s,
-                                int r, cudaStream_t st) {
+                                int r, bool rest, cudaStream_t st) {
   ffsplit_status rc = set_up(ctx);
   if (rc != FFSPLIT_OK) return rc;
   ExpandParams p;
@@ -806,12 +909,13 @@ ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const 
   if ((rc = encode_factor(ctx, F, s.n, p.f_mn ? BLOCK_K : EXPAND_COLS, &p.F)) != FFSPLIT_OK) return rc;
   p.s = s;
   p.base = static_cast<const __nv_bfloat16*>(base); p.Y = static_cast<__nv_bfloat16*>(Y);
-  p.N = N; p.r = r; p.status = ctx->status();
+  p.N = N; p.r = r; p.rest = rest ? 1 : 0; p.status = ctx->status();
   p.blocks = r > BLOCK_K ? 2 : 1;
   // Two CTAs to an SM where there are few tiles, else four blocks of columns to a CTA: its start is paid once, and the last
   // round of CTAs stays short (fourteen blocks each, 342 CTAs on 296 places: 114 us instead of 57).
   const long long blocks = (N + EXPAND_COLS - 1) / EXPAND_COLS, fill = (2 * ctx->num_sms + tiles - 1) / tiles, four = (blocks + 3) / 4;
-  const long long wanted = fill > four ? fill : four;
+  // (the rest is most often nothing: CTAs that leave at once)
+  const long long wanted = rest ? (fill < four ? fill : four) : fill > four ? fill : four;
   const bool wide = N % 4 == 0 && s.T * (N / 4) <= 0xffffffffll;
   const cudaError_t e = launch_pdl(wide ? expand_tc_kernel<true> : expand_tc_kernel<false>, dim3(static_cast<unsigned>(wanted < blocks ? wanted : blocks), static_cast<unsigned>(tiles)), dim3(EXPAND_TC_THREADS),
                                    expand_smem(r), st, p);

@@ -110,6 +110,19 @@ struct Params {
   int* status;
 };
 
+// The same with an extension (PLAIN, bf16, one product).
+struct ExtendedParams : Params<1> {
+  CUtensorMap q, f;
+  const int *count, *list;
+  int most, blocks, steps; // k-blocks of an entry, and MMAs of 16
+};
+template <int CAP, bool EXTENDED> struct KernelParams { typedef Params<CAP> type; };
+template <> struct KernelParams<1, true> { typedef ExtendedParams type; };
+// How many entries follow the last k-block of a unit.
+__device__ __forceinline__ int entries_of(const ExtendedParams& p, const Unit& t) {
+  return t.k1 == p.prod[0].runs * p.prod[0].kb ? __ldcg(p.count + t.m_blk) : 0;
+}
+
 // Units of one cluster in order.
 struct Walk {
   int c, C, next, phase, given;
@@ -520,8 +533,9 @@ __device__ __forceinline__ void write_staged(const uint32_t* buf, int lane, void
 }
 
 // ---------------------------------------------------------------------------------------------- the kernel
-template <int MODE, bool F32, int CAP>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 1) train_gemm_kernel(const __grid_constant__ Params<CAP> p) {
+template <int MODE, bool F32, int CAP, bool EXTENDED = false>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 1)
+    train_gemm_kernel(const __grid_constant__ typename KernelParams<CAP, EXTENDED>::type p) {
   constexpr bool GATED = MODE == FORWARD_GATED || MODE == BACKWARD_GATED;
   const int out_n = MODE == FORWARD_GATED ? p.tile_n / 2 : p.tile_n;     // output columns of a tile
   const int half_n = p.tile_n / 2;                                       // rows of B that one CTA stages
@@ -620,6 +634,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
           const Unit t = find_unit(p, u);
           const DevProduct& d = p.prod[t.prod];
           const uint32_t tx = stage_tx(d);
+          int entries = 0;
+          if constexpr (EXTENDED) entries = entries_of(p, t);
           const int m0 = t.m_blk * TILE_M + static_cast<int>(rank) * CTA_M, n0 = first_column(t);
           // Few rows: what A's box leaves out, and all of rank 1's half where M <= 128, is not staged at all.  Whatever lies
           // in shared memory there only reaches accumulator rows behind M.  (One token: the empty rows cost as much of the
@@ -652,6 +668,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
               if (++s == stages) { s = 0; ph ^= 1u; }
             }
           }
+          if constexpr (EXTENDED) {
+            // the entries of this tile, behind the last k-block of its sum; the next one's word is loaded ahead
+            const int* list = p.list + t.m_blk * p.most;
+            int word = entries > 0 ? __ldcg(list) : 0;
+            for (int e = 0; e < entries && ok; ++e) {
+              const int now = word;
+              if (e + 1 < entries) word = __ldcg(list + e + 1);
+              for (int b = 0; b < p.blocks; ++b) {
+                if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+                if (rank == 0) ptx::mbar_expect_tx(&full[s], tx);
+                load_b(&p.f, d.b_mn, n0, b, now & 0xffff, s);
+                if (has_a)
+                  ptx::tma_load_3d_pair(&p.q, smem0 + s * stage_bytes, full0 + s * 8, b * BLOCK_K,
+                                        (t.m_blk * p.most + (now >> 16)) * TILE_M + static_cast<int>(rank) * CTA_M, 0);
+                if (++s == stages) { s = 0; ph ^= 1u; }
+              }
+            }
+          }
         }
         // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
         for (int i = 0; i < stages && ok; ++i) {
@@ -674,9 +708,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
         uint32_t tl = 0, ph = 0;
         int s = 0;
         bool ok = true;
+        const auto steps_left = [&](int block) {
+          if constexpr (EXTENDED) return p.steps - (block % p.blocks) * (BLOCK_K / 16);
+          else return BLOCK_K / 16;
+        };
         for (int u = walk.take(p); u >= 0 && ok; u = walk.take(p)) {
           const Unit t = find_unit(p, u);
           const DevProduct& d = p.prod[t.prod];
+          int more = 0;      // k-blocks of entries (the load is over long before it is needed)
+          if constexpr (EXTENDED) more = entries_of(p, t) * p.blocks;
           // bits 15, 16: the operand's rows run along memory
           const uint32_t idesc = idesc0 | (d.a_mn ? 1u << 15 : 0u) | (d.b_mn ? 1u << 16 : 0u);
           const uint64_t a_desc0 = d.a_mn ? ptx::umma_desc_mn128(smem0, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0);
@@ -691,7 +731,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
             if (!ok) break;
             ptx::tc_fence_after();
             const uint32_t d_tmem = tmem_base + acc * TILE_N;
-            for (int kb = begin; kb < end; ++kb) {
+            for (int kb = begin; kb < end || (EXTENDED && kb < end + more); ++kb) {
               ok = ptx::mbar_wait_warp(&full[s], ph, abort_flag);
               if (!ok) break;
               ptx::tc_fence_after();
@@ -699,8 +739,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
               const uint64_t b_desc = b_desc0 + static_cast<uint32_t>(s) * (stage_bytes >> 4);
               if (ptx::elect_one()) {
   #pragma unroll
-                for (int k = 0; k < BLOCK_K / 16; ++k)
+                for (int k = 0; k < BLOCK_K / 16; ++k) {
+                  // (of an entry's last block what its rank needs)
+                  if (EXTENDED && kb >= end && k >= steps_left(kb - end)) break;
                   ptx::umma_bf16_pair(d_tmem, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb > begin || k > 0) ? 1u : 0u);
+                }
                 ptx::umma_commit_pair(&empty[s]);
               }
               __syncwarp();
@@ -1163,23 +1206,23 @@ Plan make_plan(Mode mode, bool f32, const Product* products, int n, int clusters
   return best;
 }
 
-template <int MODE, bool F32, int CAP>
-ffsplit_status launch_mode(ffsplit_ctx* ctx, Params<CAP>& p, const JoinParams& join, int clusters, cudaStream_t st) {
-  const unsigned bit = 1u << (MODE * 2 + (F32 ? 1 : 0) + (CAP > 1 ? 10 : 0));
+template <int MODE, bool F32, int CAP, bool EXTENDED = false>
+ffsplit_status launch_mode(ffsplit_ctx* ctx, typename KernelParams<CAP, EXTENDED>::type& p, const JoinParams& join, int clusters, cudaStream_t st) {
+  const unsigned bit = EXTENDED ? 1u << 31 : 1u << (MODE * 2 + (F32 ? 1 : 0) + (CAP > 1 ? 10 : 0));
   if (!(ctx->attr_train_set & bit)) {
-    const cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(train_gemm_kernel<MODE, F32, CAP, EXTENDED>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
     if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(train_gemm_kernel)");
     if (F32) {
       // the split of registers in the kernel counts on what the block starts with
       cudaFuncAttributes attr;
-      const cudaError_t a = cudaFuncGetAttributes(&attr, train_gemm_kernel<MODE, F32, CAP>);
+      const cudaError_t a = cudaFuncGetAttributes(&attr, train_gemm_kernel<MODE, F32, CAP, EXTENDED>);
       if (a != cudaSuccess) return check_cuda(ctx, a, "cudaFuncGetAttributes(train_gemm_kernel)");
       if (attr.numRegs < START_REGS) return fail(ctx, FFSPLIT_ERR_CUDA, "train_gemm_kernel was built with fewer registers than it divides");
     }
     ctx->attr_train_set |= bit;
   }
   p.stages = RING_BYTES<MODE, F32> / p.stage_bytes < MAX_STAGES ? RING_BYTES<MODE, F32> / p.stage_bytes : MAX_STAGES;
-  cudaError_t e = launch_pdl(train_gemm_kernel<MODE, F32, CAP>, dim3(2 * clusters), dim3(THREADS<MODE, F32>), MAX_SMEM, st, p);
+  cudaError_t e = launch_pdl(train_gemm_kernel<MODE, F32, CAP, EXTENDED>, dim3(2 * clusters), dim3(THREADS<MODE, F32>), MAX_SMEM, st, p);
   ctx->launches++;
   if (e != cudaSuccess || join.n == 0) return check_cuda(ctx, e, "train_gemm_kernel launch");
   e = launch_pdl(join_kernel<MODE, F32>, dim3(static_cast<unsigned>(ceil_div(join.chunks, JOIN_CHUNKS))), dim3(JOIN_THREADS), 0, st, join);
@@ -1190,7 +1233,7 @@ ffsplit_status launch_mode(ffsplit_ctx* ctx, Params<CAP>& p, const JoinParams& j
 // CAP: products that the argument block has room for (it is copied with every launch).
 template <int CAP>
 ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden,
-                               char* partials, size_t partial_room, cudaStream_t st, bool* joined) {
+                               char* partials, size_t partial_room, cudaStream_t st, bool* joined, const Extension* extension) {
   // The tensor maps are made by a driver call, which needs a current context; a thread that has only asked the runtime for
   // its device (autograd's backward threads) has none yet.
   const cudaError_t bound = cudaSetDevice(ctx->device);
@@ -1299,19 +1342,36 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
   join.act = act;
   join.hid = hidden;
   if (joined) *joined = join.n > 0;
+  if constexpr (CAP == 1) {
+    if (extension) {
+      ExtendedParams x;
+      std::memset(&x, 0, sizeof(x));
+      static_cast<Params<1>&>(x) = p;
+      const Extension& e = *extension;
+      const Matrix q = {e.Q, e.entries * TILE_M, e.pitch, e.pitch, e.entries * TILE_M * e.pitch, 1};
+      ffsplit_status s;
+      if ((s = encode(ctx, q, p.prod[0].a_rows, &x.q)) != FFSPLIT_OK) return s;
+      if ((s = encode(ctx, e.F, products[0].b_mn ? BLOCK_K : p.tile_n / 2, &x.f)) != FFSPLIT_OK) return s;
+      x.count = e.count; x.list = e.list;
+      x.most = e.most;
+      x.blocks = e.pitch / BLOCK_K;
+      x.steps = (e.rank + 15) / 16;
+      return launch_mode<PLAIN, false, 1, true>(ctx, x, join, clusters, st);
+    }
+  }
   if constexpr (CAP > 1) {
-    return f32 ? launch_mode<PLAIN, true>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false>(ctx, p, join, clusters, st);
+    return f32 ? launch_mode<PLAIN, true, CAP>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false, CAP>(ctx, p, join, clusters, st);
   } else {
     switch (mode) {
-      case PLAIN: return f32 ? launch_mode<PLAIN, true>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false>(ctx, p, join, clusters, st);
+      case PLAIN: return f32 ? launch_mode<PLAIN, true, CAP>(ctx, p, join, clusters, st) : launch_mode<PLAIN, false, CAP>(ctx, p, join, clusters, st);
       case FORWARD_GATED:
-        return f32 ? launch_mode<FORWARD_GATED, true>(ctx, p, join, clusters, st) : launch_mode<FORWARD_GATED, false>(ctx, p, join, clusters, st);
+        return f32 ? launch_mode<FORWARD_GATED, true, CAP>(ctx, p, join, clusters, st) : launch_mode<FORWARD_GATED, false, CAP>(ctx, p, join, clusters, st);
       case FORWARD_ACT:
-        return f32 ? launch_mode<FORWARD_ACT, true>(ctx, p, join, clusters, st) : launch_mode<FORWARD_ACT, false>(ctx, p, join, clusters, st);
+        return f32 ? launch_mode<FORWARD_ACT, true, CAP>(ctx, p, join, clusters, st) : launch_mode<FORWARD_ACT, false, CAP>(ctx, p, join, clusters, st);
       case BACKWARD_GATED:
-        return f32 ? launch_mode<BACKWARD_GATED, true>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_GATED, false>(ctx, p, join, clusters, st);
+        return f32 ? launch_mode<BACKWARD_GATED, true, CAP>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_GATED, false, CAP>(ctx, p, join, clusters, st);
       default:
-        return f32 ? launch_mode<BACKWARD_ACT, true>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_ACT, false>(ctx, p, join, clusters, st);
+        return f32 ? launch_mode<BACKWARD_ACT, true, CAP>(ctx, p, join, clusters, st) : launch_mode<BACKWARD_ACT, false, CAP>(ctx, p, join, clusters, st);
     }
   }
 }
@@ -1319,9 +1379,9 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
 }  // namespace
 
 ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, char* partials,
-                      size_t partial_room, cudaStream_t st, bool* joined) {
-  return n == 1 ? launch_products<1>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st, joined)
-                : launch_products<MAX_PRODUCTS>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st, joined);
+                      size_t partial_room, cudaStream_t st, bool* joined, const Extension* extension) {
+  return n == 1 ? launch_products<1>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st, joined, extension)
+                : launch_products<MAX_PRODUCTS>(ctx, mode, act, f32, products, n, hidden, partials, partial_room, st, joined, nullptr);
 }
 
 }  // namespace tg

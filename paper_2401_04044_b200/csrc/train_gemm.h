@@ -54,6 +54,18 @@ inline size_t kept_bytes(long long T, long long ldm, bool gated, bool f32) {
   return static_cast<size_t>((T + 31) / 32 * 32) * ldm * (gated ? 2 : 1) * (f32 ? 8 : 5) / 2;
 }
 
+// More terms of a bf16 PLAIN product, of few k-blocks and different for each tile of 256 rows: C += Q_e F_i for what the tile's
+// list names, i in the lower half of a word and e in the upper one.  Q_e of tile m is number m * most + e of [256, pitch] (pitch
+// 64 or 128; columns from `rank` rounded up to 16 on are not read), rows that do not use it are zeros.  F lies along the axes of
+// the product's own B.
+struct Extension {
+  const __nv_bfloat16* Q;
+  long long entries;       // there is room for
+  int pitch, most, rank;
+  Matrix F;                // [planes][rows][cols], one plane to an i
+  const int *count, *list; // [tiles], [tiles][most]
+};
+
 #ifdef __CUDACC__
 // x = x0 + x1 + x2 with bf16 terms; non-finite values stay in x0 alone, and a finite x0 does not round to infinity.
 __device__ __forceinline__ void split3(float x, float* o) {
@@ -94,7 +106,7 @@ __device__ __forceinline__ void split3_pair(float x, float y, uint32_t* w) {
 // operands and fp32 outputs.  partials: scratch for the fp32 partials of products that are cut along K.
 // joined (may be nullptr): whether that was done.
 ffsplit_status launch(ffsplit_ctx* ctx, Mode mode, int act, bool f32, const Product* products, int n, const Hidden& hidden, char* partials,
-                      size_t partial_room, cudaStream_t st, bool* joined = nullptr);
+                      size_t partial_room, cudaStream_t st, bool* joined = nullptr, const Extension* extension = nullptr);
 
 }  // namespace tg
 

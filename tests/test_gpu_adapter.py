@@ -266,3 +266,40 @@ def test_other_stream_and_captured_replay(ctx):
         torch.cuda.synchronize()
         check({"Y": Y.cpu(), "dX": dX.cpu(), "dA": dA.cpu(), "dB": dB.cpu()}, L, "bf16")
     ctx.poll()
+
+
+# (the last two: outputs of more than 2^25 elements, whose adapters are taken along in the shared product)
+@pytest.mark.parametrize("T,n,k,m", [(40, 4, 264, 520), (300, 4, 264, 520), (700, 20, 264, 520), (4200, 4, 264, 8200), (4201, 3, 8200, 264)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_broken_adapter_reaches_its_own_tokens_only(ctx, T, n, k, m, value):
+    """Zero times an infinity is NaN: the rows of other requests in the same tile must not meet a factor that holds one."""
+    L = draw("bf16", k, m, T, n, 16, order="mixed", seed=13)
+    clean = run(ctx, L, "bf16")
+    bad = L["index"] == 2
+    L["A"][2, 5, 3], L["B"][2, 1, 7] = value, value
+    got = run(ctx, L, "bf16")
+    for o in ("Y", "dX"):
+        assert torch.equal(got[o][~bad], clean[o][~bad]), o
+    assert not torch.isfinite(got["Y"][bad][:, 7]).any() and not torch.isfinite(got["dX"][bad][:, 5]).any()
+    others = [i for i in range(n) if i != 2]
+    assert torch.equal(got["dA"][others], clean["dA"][others]) and torch.equal(got["dB"][others], clean["dB"][others])
+    # columns that the broken element does not reach
+    L["A"][2, 5, 3] = 0.0
+    once = run(ctx, L, "bf16", want=("Y",))["Y"]
+    keep = [c for c in range(m) if c != 7]
+    L["B"][2, 1, 7] = 0.0
+    ref = reference(L)["Y"][:, keep]
+    x = once[:, keep].double().numpy()
+    assert np.linalg.norm(x - ref) <= TOL["bf16"] * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("shared", ["weight", "base"])
+@pytest.mark.parametrize("T,n,r,k,m", [(1024, 40, 16, 640, 776), (777, 40, 72, 640, 776), (513, 12, 128, 640, 776), (4300, 40, 16, 648, 8008), (4201, 12, 72, 8200, 456),
+                                       (4111, 12, 128, 712, 8200), (6500, 1, 24, 5201, 257)])
+def test_tiles_with_few_and_with_many_adapters_in_one_batch(ctx, T, n, r, k, m, shared):
+    """Of the first rows all of one adapter, of the middle some without any, of the rest each another one."""
+    L = draw("bf16", k, m, T, n, r, order="mixed", shared=shared, seed=14)
+    L["index"][:250] = n - 1
+    L["index"][250:500] = -1
+    L["index"][300:310] = 0
+    check(run(ctx, L, "bf16"), L, "bf16")
