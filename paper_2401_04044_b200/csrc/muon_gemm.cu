@@ -400,7 +400,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
       }
       if constexpr (PRECISE) {
         // All parts of the sum but the last are added up in registers; then it goes back to where the last part lies.
-        constexpr int BLOCKS = TILE_N / GROUPS<PRECISE> / 32;             // (precise tiles are 256 wide)
+        constexpr int BLOCKS = TILE_N / GROUPS<PRECISE> / 32;             // (the first half of them in narrow tiles)
         float sum[BLOCKS][32];
         for (int begin = 0;; ++tl) {
           const int end = part_end(d.kb, begin);
@@ -410,6 +410,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
           const uint32_t t_part = t_quarter + (tl & 1) * TILE_N;
 #pragma unroll
           for (int b = 0; b < BLOCKS; ++b) {
+            if (b * 32 >= cols) break;
             const uint32_t at = t_part + b * 32;
             float v[32];
             ptx::tmem_ld32(at, v);
@@ -608,7 +609,7 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
   // 256 x 128 tiles where the wide ones leave pairs of SMs idle: a k-block takes 0.27 us in a wide tile (the tensor cores'
   // rate) and 0.2 us in a narrow one (shared memory's)
   p.tile_n = TILE_N;
-  if (!precise) {
+  {
     long long wide = 0, narrow = 0;
     for (int i = 0; i < n; ++i) {
       wide += static_cast<long long>(tiles_of(products[i], 256)) * products[i].c.count;
