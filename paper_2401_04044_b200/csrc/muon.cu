@@ -18,7 +18,7 @@ namespace muon {
 
 constexpr int MAX_TENSORS = 128;        // of one launch's table
 constexpr int THREADS = 256;
-constexpr int MAX_PARTS = 256;          // partial sums of one matrix's squares
+constexpr int MAX_PARTS = 1024;         // partial sums of one matrix's squares (256 of them read 90 MB at 1.2 TB/s: too few blocks)
 
 struct Entry {
   const void* G;
@@ -147,7 +147,11 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
   const int which = blockIdx.y, part = blockIdx.x;
   const Entry& e = t.t[which];
   if (part >= e.parts) return;
-  const double squares = block_sum(threadIdx.x < e.parts ? __ldcg(t.partial + which * MAX_PARTS + threadIdx.x) : 0.0, red);
+  double mine = 0.0;
+#pragma unroll
+  for (int k = 0; k < MAX_PARTS / THREADS; ++k)
+    if (k * THREADS + static_cast<int>(threadIdx.x) < e.parts) mine += __ldcg(t.partial + which * MAX_PARTS + k * THREADS + threadIdx.x);
+  const double squares = block_sum(mine, red);
   const float norm = static_cast<float>(sqrt(squares));
   const bool finite = isfinite(norm);
   const float inv = finite ? 1.0f / (norm + 1e-7f) : 0.f;
@@ -529,8 +533,8 @@ size_t matrix_bytes(int rows, int cols, bool precise) {
   return 2 * x_bytes(rows, cols) + (in_pairs(rows, cols, precise) ? 4 : 2) * x_bytes(p, p);
 }
 constexpr size_t kTableBytes = muon::MAX_TENSORS * (muon::MAX_PARTS * sizeof(double) + sizeof(muon::Target));
-// Matrices are worked on in runs: as many as fit the tables and two gigabytes, one at least.
-constexpr size_t kRunBytes = static_cast<size_t>(2) << 30;
+// Matrices are worked on in runs: as many as fit the tables and three gigabytes, one at least.
+constexpr size_t kRunBytes = static_cast<size_t>(3) << 30;
 int run_length(const ffsplit_muon_tensor* t, int count, size_t* bytes) {
   size_t sum = 0;
   int n = 0;
@@ -785,7 +789,7 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
       e.X_low = g.X[0].low + j * g.X[0].low_each;
       e.blocks = g.precise ? 0 : 1;
       const long long pieces = (s.rows + muon::PIECE_ROWS - 1ll) / muon::PIECE_ROWS * muon::pieces_across(e.octets);
-      e.parts = static_cast<int>(pieces < 2 * muon::MAX_PARTS ? (pieces + 1) / 2 : muon::MAX_PARTS);
+      e.parts = static_cast<int>(pieces < 4 * muon::MAX_PARTS ? (pieces + 3) / 4 : muon::MAX_PARTS);
       if (e.parts > blocks) blocks = e.parts;
     }
   }
