@@ -461,10 +461,13 @@ ffsplit_status ffsplit_grad_clip(ffsplit_ctx* ctx, const ffsplit_grad_tensor* te
  *   W' = (1 - decay) W - step X
  * The coefficients move the singular values of X towards 1 and leave its singular vectors: a Newton-Schulz iteration.
  *
- * Arithmetic: sums in fp32 and more.  Where the gradient is bf16, X is kept in 22 bits, and the operands of the products
- * are fp16 (11 bits); what is rounded off an operand perturbs X by a factor close to 1, not by a term, so small singular
- * values do not drown in it: X is off by 2e-4 to 2e-3 of its norm.  Where the gradient is fp32, operands carry 22 bits
- * too: 1e-6.  Momentum is fp32 whatever the type of the gradient. */
+ * Arithmetic: sums in fp32 and more.  X is kept in 22 bits.  Where the gradient is bf16, the operands of the products are
+ * fp16 (11 bits); what is rounded off an operand perturbs X by a factor close to 1, not by a term, so small singular values
+ * do not drown in it: X is off by 5e-4 to 3e-3 of its norm.  Where the gradient is fp32, operands carry 22 bits too: 1e-7 to
+ * 2e-6.  (A direction in which the matrix has less than 2^-22 of its norm is filled with what is rounded off X, times up to
+ * 3.44^5: 1e-4 of the result for matrices of nearly lower rank.)  Matrices with a side of at most 64 are worked on through
+ * their Gram matrix in fp64.  Momentum is fp32 whatever the type of the gradient.
+ * Same inputs give the same bits, whatever else is in the list. */
 
 typedef struct {
   const void* grad;           /* dev [rows, cols], grad_dtype                                         */
@@ -512,10 +515,11 @@ typedef struct {
 ffsplit_status ffsplit_adapter_workspace_size(const ffsplit_projection* projection, int32_t n, int32_t r, int64_t T,
                                               size_t* bytes);
 
-/* Y dev [T, out] from X dev [T, in].  W dev [in, out] and bias dev [out] (may be NULL), or base dev [T, out] (may be Y)
- * with W and bias NULL, or none of them.  X A_i is summed in fp32 and, for FFSPLIT_BF16, rounded to bf16 before it meets B_i
- * (the tensor cores take both operands in one type).  Fastest where the tokens of an adapter lie together.
- * Y may not overlap X, W or the factors.  Uses the workspace. */
+/* Y dev [T, out] from X dev [T, in], T >= 1.  W dev [in, out] and bias dev [out] (may be NULL), or base dev [T, out] (may be
+ * Y) with W and bias NULL, or none of them.  X A_i is summed in fp32 and, for FFSPLIT_BF16 and more than 64 tokens, rounded to
+ * bf16 before it meets B_i (the tensor cores take both operands in one type).  An infinity or NaN in a token or in an
+ * adapter's factors reaches the rows (and gradients) of that token or adapter only.  Fastest where the tokens of an adapter
+ * lie together.  Y may not overlap X, W or the factors.  Uses the workspace. */
 ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W,
                                        const void* bias, const void* base, const ffsplit_adapters* adapters,
                                        const void* X, int64_t T, void* Y, void* stream);
