@@ -475,7 +475,7 @@ typedef struct {
   float* momentum_out;        /* dev [rows, cols], may be momentum; NULL where momentum is            */
   const void* weight;         /* dev [rows, cols], weight_dtype; NULL: out = X, the orthogonal factor */
   void* out;                  /* dev [rows, cols], weight_dtype; may be weight                        */
-  int32_t rows, cols;         /* >= 1 */
+  int32_t rows, cols;         /* 1 .. 2^30, 2^36 elements, the smaller one at most 2^17 */
   int32_t grad_dtype, weight_dtype;   /* ffsplit_dtype */
   float step, decay;          /* not looked at where weight is NULL */
 } ffsplit_muon_tensor;
@@ -488,7 +488,7 @@ ffsplit_status ffsplit_muon_workspace_size(const ffsplit_muon_tensor* tensors, i
  * can carry a singular value in [0, 1] above 1.5, or that are larger than 64, are refused (INVALID_ARG).
  * Tensors are aligned to their element size (no 16-byte rule); outputs may be the inputs they replace and overlap
  * nothing else.  Matrices of one shape are worked on together: give one list rather than many.
- * A matrix whose U is not finite is left as it is, its momentum too (out = NaN where weight is NULL), and
+ * A matrix whose U (or its norm, in fp32) is not finite is left as it is, its momentum too (out = NaN where weight is NULL), and
  * FFSPLIT_ERR_NONFINITE is reported through ffsplit_poll().  A matrix of zeros has X = 0.  Uses the workspace. */
 ffsplit_status ffsplit_muon_step(ffsplit_ctx* ctx, const ffsplit_muon_tensor* tensors, int32_t count, float beta,
                                  int32_t nesterov, const float* coefficients, int32_t iterations, void* stream);

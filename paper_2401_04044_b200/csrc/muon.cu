@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
   const double squares = block_sum(mine, red);
   const float norm = static_cast<float>(sqrt(squares));
   const bool finite = isfinite(norm);
-  const float inv = finite ? 1.0f / (norm + 1e-7f) : 0.f;
+  const float inv = finite ? HELD / (norm + 1e-7f) : 0.f;      // (with the factor X is held with: 1 / norm may be below the normal numbers)
   if (part == 0 && threadIdx.x == 0) {
     Target o;
     o.W = e.W; o.out = e.out; o.f32 = e.w_f32;
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
     }
     __align__(16) __half hi[8], lo[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) split_half(finite ? u[k] * inv * HELD : 0.f, &hi[k], &lo[k]);
+    for (int k = 0; k < 8; ++k) split_half(finite ? u[k] * inv : 0.f, &hi[k], &lo[k]);
     __half* x = e.X + static_cast<long long>(row) * e.ld + c;
     *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(hi);
     __half* x_low = e.X_low + (e.blocks ? block_at(row, octet, e.ld) : static_cast<long long>(row) * e.ld + c);
@@ -551,7 +551,8 @@ int run_length(const ffsplit_muon_tensor* t, int count, size_t* bytes) {
 ffsplit_status check_list(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int count) {
   if (count < 0 || (count > 0 && !t)) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "NULL list, or a negative count");
   for (int i = 0; i < count; ++i) {
-    if (t[i].rows < 1 || t[i].cols < 1) return fail(ctx, FFSPLIT_ERR_SHAPE, "a matrix without rows or columns");
+    if (t[i].rows < 1 || t[i].cols < 1 || t[i].rows > (1 << 30) || t[i].cols > (1 << 30))
+      return fail(ctx, FFSPLIT_ERR_SHAPE, "rows and columns must be in [1, 2^30]");
     if (static_cast<long long>(t[i].rows) * t[i].cols > (1ll << 36) || (t[i].rows < t[i].cols ? t[i].rows : t[i].cols) > (1 << 17))
       return fail(ctx, FFSPLIT_ERR_SHAPE, "a matrix of more than 2^36 elements, or both sides above 2^17");
     for (const int32_t d : {t[i].grad_dtype, t[i].weight_dtype})

@@ -37,7 +37,7 @@ constexpr int BAR_BYTES = 256;
 constexpr int MAX_SMEM = 232448;
 // Outputs leave through shared memory: 32 x 32 values of a warp at a time, one TMA store to a plane, and another to the mirror
 // image.  (A row to a lane, as the sums lie in tensor memory, every store falls into 32 lines: 126 us for the third product of
-// twelve 1024 x 4096 matrices, now 95.)  What is left holds the ring.
+// twelve 1024 x 4096 matrices, now 98.)  What is left holds the ring.
 constexpr int BOX = 32, BOX_BYTES = BOX * BOX * 2;
 // An epilogue reads 2 bytes of every value and writes 4 while the tensor cores take 17 us over a tile (K = 4096): with 8 warps,
 // each waiting for its next 16 columns, it took 35 us.  precise: 8, for the sake of their registers.

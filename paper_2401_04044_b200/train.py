@@ -80,7 +80,7 @@ def clip_grad_norm_(lib: Context, parameters: Union[torch.Tensor, Iterable[torch
 
 def _matrices(t: torch.Tensor):
     """The matrices of a parameter: itself, or one to each leading index (a stack of adapters' factors)."""
-    return [t] if t.dim() == 2 else list(t.reshape(-1, *t.shape[-2:]))
+    return [t] if t.dim() == 2 else list(t.view(-1, *t.shape[-2:]))      # (a view: what is updated is the parameter itself)
 
 
 class Muon(torch.optim.Optimizer):

@@ -269,15 +269,16 @@ def test_other_stream_and_captured_replay(ctx):
 
 
 # (the last two: outputs of more than 2^25 elements, whose adapters are taken along in the shared product)
-@pytest.mark.parametrize("T,n,k,m", [(40, 4, 264, 520), (300, 4, 264, 520), (700, 20, 264, 520), (4200, 4, 264, 8200), (4201, 3, 8200, 264)])
+@pytest.mark.parametrize("dtype,T,n,k,m", [("bf16", 40, 4, 264, 520), ("bf16", 300, 4, 264, 520), ("bf16", 700, 20, 264, 520), ("f32", 40, 4, 60, 100),
+                                           ("f32", 300, 4, 60, 100), ("bf16", 4200, 4, 264, 8200), ("bf16", 4201, 3, 8200, 264)])
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
-def test_a_broken_adapter_reaches_its_own_tokens_only(ctx, T, n, k, m, value):
+def test_a_broken_adapter_reaches_its_own_tokens_only(ctx, dtype, T, n, k, m, value):
     """Zero times an infinity is NaN: the rows of other requests in the same tile must not meet a factor that holds one."""
-    L = draw("bf16", k, m, T, n, 16, order="mixed", seed=13)
-    clean = run(ctx, L, "bf16")
+    L = draw(dtype, k, m, T, n, 16, order="mixed", seed=13)
+    clean = run(ctx, L, dtype)
     bad = L["index"] == 2
     L["A"][2, 5, 3], L["B"][2, 1, 7] = value, value
-    got = run(ctx, L, "bf16")
+    got = run(ctx, L, dtype)
     for o in ("Y", "dX"):
         assert torch.equal(got[o][~bad], clean[o][~bad]), o
     assert not torch.isfinite(got["Y"][bad][:, 7]).any() and not torch.isfinite(got["dX"][bad][:, 5]).any()
@@ -285,12 +286,12 @@ def test_a_broken_adapter_reaches_its_own_tokens_only(ctx, T, n, k, m, value):
     assert torch.equal(got["dA"][others], clean["dA"][others]) and torch.equal(got["dB"][others], clean["dB"][others])
     # columns that the broken element does not reach
     L["A"][2, 5, 3] = 0.0
-    once = run(ctx, L, "bf16", want=("Y",))["Y"]
+    once = run(ctx, L, dtype, want=("Y",))["Y"]
     keep = [c for c in range(m) if c != 7]
     L["B"][2, 1, 7] = 0.0
     ref = reference(L)["Y"][:, keep]
     x = once[:, keep].double().numpy()
-    assert np.linalg.norm(x - ref) <= TOL["bf16"] * np.linalg.norm(ref)
+    assert np.linalg.norm(x - ref) <= TOL[dtype] * np.linalg.norm(ref)
 
 
 @pytest.mark.parametrize("shared", ["weight", "base"])
@@ -303,3 +304,20 @@ def test_tiles_with_few_and_with_many_adapters_in_one_batch(ctx, T, n, r, k, m, 
     L["index"][250:500] = -1
     L["index"][300:310] = 0
     check(run(ctx, L, "bf16"), L, "bf16")
+
+
+def test_more_adapters_than_the_tensor_cores_tiles_allow(ctx):
+    """65535 adapters and 70000 tokens: the batch stays on the CUDA cores."""
+    L = draw("bf16", 8, 16, 70000, 65535, 1, order="mixed", seed=15)
+    D = {k: None if v is None else v.double() for k, v in L.items() if k not in ("index", "scale", "base", "base_dX")}
+    got = run(ctx, L, "bf16")
+    i = L["index"].long()
+    used, at = (i >= 0).double().unsqueeze(1), i.clamp_min(0)
+    s = L["scale"].double()[at].unsqueeze(1) * used
+    A, B = D["A"][at, :, 0], D["B"][at, 0, :]
+    P, G = s * (D["X"] * A).sum(1, keepdim=True), s * (D["dY"] * B).sum(1, keepdim=True)
+    ref = {"Y": D["X"] @ D["W"] + D["b"] + P * B, "dX": D["dY"] @ D["W"].t() + G * A,
+           "dA": torch.zeros_like(D["A"][:, :, 0]).index_add_(0, at, G * D["X"]).unsqueeze(2),
+           "dB": torch.zeros_like(D["B"][:, 0, :]).index_add_(0, at, P * D["dY"]).unsqueeze(1)}
+    for o, v in got.items():
+        assert float((v.double() - ref[o]).norm() / ref[o].norm()) <= TOL["bf16"], o

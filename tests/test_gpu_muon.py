@@ -95,7 +95,7 @@ def test_many_tiles(ctx, rows, cols, dtype):
     near(got, orthogonal64(m.double().numpy()), TOL[dtype])
 
 
-@pytest.mark.parametrize("kind", ["rank one", "spread", "gauss", "small", "large"])
+@pytest.mark.parametrize("kind", ["rank one", "spread", "gauss", "small", "large", "largest"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,cols", [(20, 90), (96, 300)])
 def test_spectra(ctx, kind, dtype, rows, cols):
@@ -110,7 +110,8 @@ def test_spectra(ctx, kind, dtype, rows, cols):
     p = min(rows, cols)
     m = {"rank one": lambda: r(rows, 1) @ r(1, cols),
          "spread": lambda: torch.linalg.qr(r(rows, p))[0] * torch.logspace(0, -3, p, dtype=torch.float64) @ torch.linalg.qr(r(cols, p))[0].T,
-         "gauss": lambda: r(rows, cols), "small": lambda: 1e-12 * r(rows, cols), "large": lambda: 1e15 * r(rows, cols)}[kind]().to(DT[dtype])
+         "gauss": lambda: r(rows, cols), "small": lambda: 1e-12 * r(rows, cols), "large": lambda: 1e15 * r(rows, cols),
+         "largest": lambda: 1e36 * r(rows, cols)}[kind]().to(DT[dtype])
     got, = orthogonalize(ctx, [m])
     ref = orthogonal64(m.double().numpy())
     near(got, ref, TOL[dtype] + 9.5e-5 / np.linalg.norm(ref))

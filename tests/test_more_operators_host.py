@@ -32,7 +32,7 @@ def test_muon_sizes(lib):
     few, many = muon_size(lib, [(4096, 11008, b.BF16, b.BF16)] * 4)[1], muon_size(lib, [(4096, 11008, b.BF16, b.BF16)] * 96)[1]
     assert few <= many <= 4 << 30
     assert muon_size(lib, [(0, 4, b.BF16, b.BF16)])[0] == 2 and muon_size(lib, [(4, -1, b.BF16, b.BF16)])[0] == 2
-    assert muon_size(lib, [(1 << 20, 1 << 20, b.BF16, b.BF16)])[0] == 2
+    assert muon_size(lib, [(1 << 20, 1 << 20, b.BF16, b.BF16)])[0] == 2 and muon_size(lib, [((1 << 31) - 1, 1, b.BF16, b.BF16)])[0] == 2
     assert muon_size(lib, [(4, 4, 7, b.BF16)])[0] == 4 and muon_size(lib, [(4, 4, b.F32, -1)])[0] == 4
     assert muon_size(lib, [], -1)[0] == 1
     assert lib.ffsplit_muon_workspace_size(None, 0, None) == 1 and lib.ffsplit_muon_workspace_size(None, 2, C.byref(C.c_size_t())) == 1
