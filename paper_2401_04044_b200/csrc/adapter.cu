@@ -609,6 +609,7 @@ struct Call {
     g.M = T; g.N = transposed ? p.in : p.out; g.K = transposed ? p.out : p.in;
     g.C = C; g.ldc = g.N; g.bias = bias;
     g.b_ready = 1;      // (the launch before is a shrink: W, or its copy, is complete)
+    g.apart = F ? 0 : 1;
     tg::Extension e;
     std::memset(&e, 0, sizeof(e));
     if (F) {

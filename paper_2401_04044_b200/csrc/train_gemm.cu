@@ -103,6 +103,7 @@ struct Params {
   // clusters from `short_from` on one tile short: `extra` of the following units go to those clusters first.
   int heavy, short_from, extra;
   int early;             // B of the first stages is loaded before the wait for the kernel before
+  int apart;             // that wait is at the end
   int act;
   Hidden hid;
   CUtensorMap hid_map[2];  // bf16 layers: H, or dG (dZ) and dU, as outputs
@@ -619,7 +620,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
       __syncwarp();
     }
   }
-  pdl_wait();
+  if (!p.apart) pdl_wait();
 
   if (warp < FIRST_EPI<F32>) {
     if constexpr (F32) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ROLE_REGS));
@@ -948,6 +949,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS<MODE, F32>, 
     if (lane == 0) ptx::tma_store_wait();
   }
 
+  if (p.apart) pdl_wait();     // (so that this kernel's end is the end of the one before, too)
   ptx::tc_fence_before();
   ptx::cluster_sync_all();     // neither CTA leaves while the other may still signal it or read its shared memory
   if (threadIdx.x == 0 && *abort_flag) record_status(p.status, FFSPLIT_ERR_TIMEOUT, blockIdx.x, KID_TRAIN);
@@ -1327,7 +1329,8 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, Mode mode, int act, bool f32, c
       p.extra = static_cast<int>(extra < most ? extra : most);
     }
   }
-  p.early = n == 1 && products[0].b_ready ? 1 : 0;
+  p.apart = n == 1 && products[0].apart ? 1 : 0;
+  p.early = n == 1 && products[0].b_ready && !p.apart ? 1 : 0;
   p.act = act;
   p.hid = hidden;
   if (mode != PLAIN && !f32) {

@@ -38,6 +38,8 @@ struct Product {
   long long ldc;
   const void* bias;      // [N], the layer's type, or nullptr
   int b_ready;           // the kernel before this launch in the stream does not write B
+  int apart;             // ... writes nothing that this launch reads or writes, and reads nothing that it writes, and waited itself
+                         // for those before it (one product): they run side by side, and whoever follows finds both done
 };
 
 // What the activation's epilogue reads and writes: what the forward pass keeps (see Kept in train_gemm.cu; nullptr:
