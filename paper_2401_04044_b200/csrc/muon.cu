@@ -790,7 +790,9 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
       e.X_low = g.X[0].low + j * g.X[0].low_each;
       e.blocks = g.precise ? 0 : 1;
       const long long pieces = (s.rows + muon::PIECE_ROWS - 1ll) / muon::PIECE_ROWS * muon::pieces_across(e.octets);
-      e.parts = static_cast<int>(pieces < 4 * muon::MAX_PARTS ? (pieces + 3) / 4 : muon::MAX_PARTS);
+      // (a block to a piece as long as they find room at once, four pieces to a block then)
+      const long long few = pieces < 256 ? pieces : 256, many = (pieces + 3) / 4;
+      e.parts = static_cast<int>(many < few ? few : many < muon::MAX_PARTS ? many : muon::MAX_PARTS);
       if (e.parts > blocks) blocks = e.parts;
     }
   }
