@@ -581,7 +581,7 @@ bool coefficients_hold(const float* c, int iterations) {
 // Matrices of one shape and precision.
 struct Group {
   int first, count, rows, cols;
-  bool precise, paired;
+  bool precise, paired, fused;
   muon::Matrices X[2], S, P, T, R;      // T, R: paired only
   int at;                               // which X is the current one
 };
@@ -592,6 +592,14 @@ struct Group {
 bool in_pairs(int rows, int cols, bool precise) {
   const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
   return !precise && p >= 512 && 2ll * q >= 3ll * p;
+}
+
+// S and P in one launch, which has a pair of SMs to a matrix whatever p and q are: not where the sum over q is long and there are
+// few rows, which goes faster in tiles of 128 columns (an iteration on 65 x 4096: 27.9 us that way, 29.2 in one launch; 128 x 128:
+// 14.4 and 11.3; 256 x 4096: 31.1 and 30.7, 64 of them 141 and 131).
+bool in_squares(int rows, int cols, bool precise) {
+  const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
+  return !precise && p <= muon::SQUARE_MOST && q <= 16 * p;
 }
 
 // All iterations of up to MAX_GROUPS groups that go alike.
@@ -625,7 +633,15 @@ ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon
   for (int it = 0; it < iterations;) {
     const float *k = coefficients ? coefficients + 3 * it : kStandard, *k2 = coefficients ? k + 3 : kStandard;
     const bool pair = groups[0]->paired && it + 2 <= iterations;
-    if ((s = launch([&](Group& g, muon::Product& p) {                  // S = X X^T
+    if (groups[0]->fused) {                                            // S and P
+      muon::Gram squares[muon::MAX_GROUPS];
+      for (int i = 0; i < n; ++i) {
+        const Group& g = *groups[i];
+        const bool tall = g.rows > g.cols;
+        squares[i] = {g.X[g.at], g.P, tall, tall ? g.rows : g.cols, k[0], k[1], k[2]};
+      }
+      if ((s = muon::launch_squares(ctx, squares, n, st)) != FFSPLIT_OK) return s;
+    } else if ((s = launch([&](Group& g, muon::Product& p) {           // S = X X^T
            const bool tall = g.rows > g.cols;
            p.a = p.b = g.X[g.at]; p.c = g.S;
            p.a_mn = p.b_mn = tall;
@@ -633,7 +649,7 @@ ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon
            p.symmetric = 1;
            p.c_low = precise;
          })) != FFSPLIT_OK) return s;
-    if ((s = launch([&](Group& g, muon::Product& p) { polynomial(p, k, g.S, &g.S, g.P); })) != FFSPLIT_OK) return s;
+    if (!groups[0]->fused && (s = launch([&](Group& g, muon::Product& p) { polynomial(p, k, g.S, &g.S, g.P); })) != FFSPLIT_OK) return s;
     if (pair) {
       if ((s = launch([&](Group& g, muon::Product& p) { square(p, g.P, g.S, g.T); })) != FFSPLIT_OK) return s;            // T = P S
       if ((s = launch([&](Group& g, muon::Product& p) { square(p, g.T, g.P, g.S); })) != FFSPLIT_OK) return s;            // S2 = T P
@@ -772,6 +788,7 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
     g.S = matrices(p, p, g.count, g.precise);
     g.P = matrices(p, p, g.count, g.precise);
     g.paired = in_pairs(g.rows, g.cols, g.precise);
+    g.fused = in_squares(g.rows, g.cols, g.precise);
     if (g.paired) {
       g.T = matrices(p, p, g.count, g.precise);
       g.R = matrices(p, p, g.count, g.precise);
@@ -800,11 +817,11 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
                                : placed <= 32 ? run_first<32>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st)
                                               : run_first<muon::MAX_TENSORS>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st);
   if (first != FFSPLIT_OK) return first;
-  for (int kind = 0; kind < 3; ++kind) {      // precise, in pairs, neither: groups of one kind go together
+  for (int kind = 0; kind < 4; ++kind) {      // precise, in pairs, in squares, none of these: groups of one kind go together
     Group* some[muon::MAX_GROUPS];
     int m = 0;
     for (int gi = 0; gi <= n_groups; ++gi) {
-      if (gi < n_groups && (groups[gi].precise ? 0 : groups[gi].paired ? 1 : 2) == kind) some[m++] = &groups[gi];
+      if (gi < n_groups && (groups[gi].precise ? 0 : groups[gi].paired ? 1 : groups[gi].fused ? 2 : 3) == kind) some[m++] = &groups[gi];
       if (m == muon::MAX_GROUPS || (gi == n_groups && m > 0)) {
         const ffsplit_status s = iterate(ctx, some, m, target, coefficients, iterations, st);
         if (s != FFSPLIT_OK) return s;

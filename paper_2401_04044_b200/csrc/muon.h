@@ -49,6 +49,15 @@ constexpr int MAX_GROUPS = 4;
 // precise: operands count with both planes (three products of planes), sums leave the tensor cores every few k-blocks.
 ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* products, int n, cudaStream_t st);
 
+// P = a I + b S + c S S with S = X X^T (X^T X) in one launch, for matrices with p <= SQUARE_MOST: a pair of CTAs to a matrix.
+constexpr int SQUARE_MOST = 256;
+struct Gram {
+  Matrices X, P;
+  int mn, K;              // mn: S = X^T X
+  float a, b, c;
+};
+ffsplit_status launch_squares(ffsplit_ctx* ctx, const Gram* squares, int n, cudaStream_t st);
+
 #ifdef __CUDACC__
 // Where 8 columns (octet of them) of one row lie in a second plane of blocks.
 __device__ __forceinline__ long long block_at(int row, int octet, int ld) {

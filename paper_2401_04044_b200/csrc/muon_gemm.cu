@@ -538,6 +538,219 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
   }
 }
 
+// ---------------------------------------------------------------------------------------------- small squares
+// p <= 256: S is one tile, so the pair of CTAs that has summed it can go on to P.  Each CTA rounds its 128 rows of S into shared
+// memory, where they are at once its rows of A and its half of the rows of B of the product S S; the sum of S itself has such
+// operands too, so X is staged once.  One launch instead of two: 17.1 us an
+// iteration on a 256 x 1024 matrix instead of 19.7, 41 instead of 49 on 74 of them; most of what is left is latency.
+constexpr int SQUARE_STAGES = 8, SQUARE_STAGE_BYTES = CTA_M * BLOCK_K * 2, SQUARE_S_BYTES = CTA_M * SQUARE_MOST * 2;
+constexpr int SQUARE_WARPS = 16, SQUARE_FIRST = 2, SQUARE_THREADS = 32 * (SQUARE_WARPS + SQUARE_FIRST);
+constexpr int SQUARE_SMEM = 1024 + SQUARE_STAGES * SQUARE_STAGE_BYTES + SQUARE_S_BYTES + SQUARE_WARPS * BOX_BYTES + BAR_BYTES;
+static_assert(SQUARE_STAGES <= MAX_STAGES && SQUARE_SMEM <= MAX_SMEM && SQUARE_MOST == TILE_M, "one tile");
+struct DevSquare {
+  CUtensorMap x, p;
+  int rows, kb, mn, unit0;
+  float a, b, c;
+};
+struct SquareParams {
+  DevSquare square[MAX_GROUPS];
+  int n;
+  int* status;
+};
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(SQUARE_THREADS, 1) muon_square_kernel(const __grid_constant__ SquareParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* S = smem + SQUARE_STAGES * SQUARE_STAGE_BYTES;         // [4 blocks of 64 columns][128 rows], 128-byte swizzle
+  uint8_t* out_stage = S + SQUARE_S_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(out_stage + SQUARE_WARPS * BOX_BYTES);
+  uint64_t* full = bars;                    // [stages] TMA of both CTAs -> MMA (rank 0's are used)
+  uint64_t* empty = full + MAX_STAGES;      // [stages] MMA -> TMA, one set in each CTA
+  uint64_t* sums = empty + MAX_STAGES;      // [2] MMA -> epilogue: S, S S, one set in each CTA
+  uint64_t* rounded = sums + 2;             // epilogue warps of both CTAs -> MMA (rank 0's is used)
+  uint64_t* drain = rounded + 1;            // used only when giving up
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = ptx::cluster_rank();
+  const int unit = blockIdx.x >> 1;
+  int which = 0;
+  while (which + 1 < p.n && unit >= p.square[which + 1].unit0) ++which;
+  const DevSquare& d = p.square[which];
+  const int batch = unit - d.unit0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < SQUARE_STAGES; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) ptx::mbar_init(&sums[a], 1);
+    ptx::mbar_init(rounded, 2 * SQUARE_WARPS);
+    ptx::mbar_init(drain, 1);
+    *abort_flag = 0;
+    ptx::mbar_fence_init();
+  }
+  if (warp == SQUARE_FIRST && lane == 0) {
+    ptx::prefetch_tmap(&d.x);
+    ptx::prefetch_tmap(&d.p);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(tmem_holder, TMEM_COLS);
+    ptx::tmem_relinquish_pair();
+  }
+  ptx::tc_fence_before();
+  ptx::cluster_sync_all();     // also: the other CTA's barriers are set up
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_holder;
+  const uint32_t smem0 = ptx::smem_u32(smem), S0 = ptx::smem_u32(S), full0 = ptx::map_to_cta(ptx::smem_u32(full), 0);
+  pdl_wait();
+
+  if (warp == 0) {
+    if (ptx::elect_one()) {
+      // -------------------------------------------------------------- TMA producer
+      bool ok = true;
+      const int m0 = static_cast<int>(rank) * CTA_M;
+      for (int kb = 0; kb < d.kb; ++kb) {
+        const int s = kb % SQUARE_STAGES;
+        if (!ptx::mbar_wait(&empty[s], ((kb / SQUARE_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
+        if (rank == 0) ptx::mbar_expect_tx(&full[s], 2 * SQUARE_STAGE_BYTES);
+        const uint32_t to = smem0 + s * SQUARE_STAGE_BYTES, bar = full0 + s * 8;
+        if (d.mn) {
+          ptx::tma_load_3d_pair(&d.x, to, bar, m0, kb * BLOCK_K, batch);
+          ptx::tma_load_3d_pair(&d.x, to + BLOCK64_BYTES, bar, m0 + 64, kb * BLOCK_K, batch);
+        } else {
+          ptx::tma_load_3d_pair(&d.x, to, bar, kb * BLOCK_K, m0, batch);
+        }
+      }
+      // The last stages: their release arrives here from rank 0, and must find this CTA's barriers still in place.
+      for (int i = 0; i < SQUARE_STAGES && i < d.kb && ok; ++i) {
+        const int kb = d.kb - 1 - i;
+        ok = ptx::mbar_wait(&empty[kb % SQUARE_STAGES], (kb / SQUARE_STAGES) & 1, abort_flag);
+      }
+      if (!ok) {
+        // give the copies in flight a bounded time to land before the CTA exits
+        const long long t0 = clock64();
+        while (clock64() - t0 < ptx::kWaitLimitCycles / 64) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      // -------------------------------------------------------------- MMA issuer (the whole warp walks, one lane issues)
+      const uint32_t idesc = ptx::umma_idesc_f16(TILE_M, SQUARE_MOST);
+      const uint32_t idesc_x = idesc | (d.mn ? 3u << 15 : 0u);
+      const uint64_t desc0 = d.mn ? ptx::umma_desc_mn128(smem0, BLOCK64_BYTES) : ptx::umma_desc_k128(smem0);
+      const uint32_t step = d.mn ? 2048 >> 4 : 32 >> 4;
+      bool ok = true;
+      for (int kb = 0; kb < d.kb; ++kb) {
+        const int s = kb % SQUARE_STAGES;
+        ok = ptx::mbar_wait_warp(&full[s], (kb / SQUARE_STAGES) & 1, abort_flag);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        const uint64_t x = desc0 + static_cast<uint32_t>(s) * (SQUARE_STAGE_BYTES >> 4);
+        if (ptx::elect_one()) {
+#pragma unroll
+          for (int k = 0; k < BLOCK_K / 16; ++k) ptx::umma_bf16_pair(tmem_base, x + k * step, x + k * step, idesc_x, (kb > 0 || k > 0) ? 1u : 0u);
+          ptx::umma_commit_pair(&empty[s]);
+        }
+        __syncwarp();
+      }
+      if (ok) {
+        if (ptx::elect_one()) ptx::umma_commit_pair(&sums[0]);
+        __syncwarp();
+        ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(rounded, 0, abort_flag) ? 1 : 0, 0) != 0;
+      }
+      if (ok) {
+        ptx::tc_fence_after();
+        const int blocks = (d.rows + BLOCK_K - 1) / BLOCK_K;
+        if (ptx::elect_one()) {
+          for (int b = 0; b < blocks; ++b) {
+            const uint64_t x = ptx::umma_desc_k128(S0 + b * SQUARE_STAGE_BYTES);
+#pragma unroll
+            for (int k = 0; k < BLOCK_K / 16; ++k)
+              ptx::umma_bf16_pair(tmem_base + TILE_N, x + k * (32 >> 4), x + k * (32 >> 4), idesc, (b > 0 || k > 0) ? 1u : 0u);
+          }
+          ptx::umma_commit_pair(&sums[1]);
+        }
+        __syncwarp();
+      } else {
+        // wait (bounded) until the MMAs issued so far have retired before tensor memory is freed
+        if (ptx::elect_one()) {
+          ptx::umma_commit_pair(drain);
+          const long long t0 = clock64();
+          while (!ptx::mbar_try_wait(drain, 0) && clock64() - t0 < ptx::kWaitLimitCycles / 8) {}
+        }
+        __syncwarp();
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- epilogue warps: 32 rows x one block of 64 columns
+    const int q = warp & 3, block = (warp - SQUARE_FIRST) >> 2;
+    const int local = q * 32 + lane, row0 = static_cast<int>(rank) * CTA_M + q * 32, row = row0 + lane;
+    const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + block * 64;
+    uint8_t* s_row = S + block * SQUARE_STAGE_BYTES + local * 128;
+    uint8_t* buf = out_stage + (warp - SQUARE_FIRST) * BOX_BYTES;
+    if (ptx::mbar_wait(&sums[0], 0, abort_flag)) {
+      ptx::tc_fence_after();
+#pragma unroll 1
+      for (int c = 0; c < 64; c += 16) {
+        float v[16];
+        ptx::tmem_ld16(t_row + c, v);
+        ptx::tmem_ld_wait();
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = pair_half(v[2 * i] * (1.f / HELD), v[2 * i + 1] * (1.f / HELD));
+        const int j = c >> 3;
+        *reinterpret_cast<uint4*>(s_row + ((j ^ (local & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(s_row + (((j + 1) ^ (local & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+      }
+      ptx::fence_proxy_async();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(rounded), 0));
+    }
+    __syncwarp();
+    if (ptx::mbar_wait(&sums[1], 0, abort_flag)) {
+      ptx::tc_fence_after();
+#pragma unroll 1
+      for (int c0 = 0; c0 < 64; c0 += BOX) {
+        if (lane == 0) ptx::tma_store_wait_read();
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int c = c0 + 16 * k, j = c >> 3;
+          float v[16];
+          ptx::tmem_ld16(t_row + TILE_N + c, v);
+          ptx::tmem_ld_wait();
+          const uint4 x = *reinterpret_cast<const uint4*>(s_row + ((j ^ (local & 7)) << 4)), y = *reinterpret_cast<const uint4*>(s_row + (((j + 1) ^ (local & 7)) << 4));
+          uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] *= d.c;
+          add16(v, d.b, w);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) if (row == block * 64 + c + i) v[i] += d.a;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] = pair_half(v[2 * i], v[2 * i + 1]);
+          stage16(buf, lane, 16 * k, w);
+        }
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0 && row0 < d.rows && block * 64 + c0 < d.rows) ptx::tma_store_3d(&d.p, ptx::smem_u32(buf), block * 64 + c0, row0, batch);
+      }
+    }
+    if (lane == 0) ptx::tma_store_wait();
+    __syncwarp();
+  }
+
+  ptx::tc_fence_before();
+  ptx::cluster_sync_all();     // neither CTA leaves while the other may still signal it or read its shared memory
+  if (threadIdx.x == 0 && *abort_flag) record_status(p.status, FFSPLIT_ERR_TIMEOUT, blockIdx.x, KID_MUON);
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc_pair(tmem_base, TMEM_COLS);
+  }
+}
+
 // ---------------------------------------------------------------------------------------------- host side
 namespace {
 
@@ -669,6 +882,37 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
   const cudaError_t e = launch_pdl(kernel, dim3(2 * clusters), dim3(precise ? GEMM_THREADS<true> : GEMM_THREADS<false>), MAX_SMEM, st, p);
   ctx->launches++;
   return check_cuda(ctx, e, "muon_gemm_kernel launch");
+}
+
+ffsplit_status launch_squares(ffsplit_ctx* ctx, const Gram* squares, int n, cudaStream_t st) {
+  const cudaError_t bound = cudaSetDevice(ctx->device);      // (see launch_products())
+  if (bound != cudaSuccess) return check_cuda(ctx, bound, "cudaSetDevice");
+  if (!(ctx->attr_muon_set & 16u)) {
+    const cudaError_t e = cudaFuncSetAttribute(muon_square_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SQUARE_SMEM);
+    if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(muon_square_kernel)");
+    ctx->attr_muon_set |= 16u;
+  }
+  SquareParams p;
+  std::memset(&p, 0, sizeof(p));
+  int units = 0;
+  for (int i = 0; i < n; ++i) {
+    const Gram& g = squares[i];
+    DevSquare& d = p.square[i];
+    ffsplit_status s;
+    if ((s = encode(ctx, g.X, BLOCK_K, g.mn ? BLOCK_K : CTA_M, 1, &d.x)) != FFSPLIT_OK) return s;
+    if ((s = encode(ctx, g.P, BOX, BOX, 1, &d.p)) != FFSPLIT_OK) return s;
+    d.rows = g.P.rows;
+    d.kb = (g.K + BLOCK_K - 1) / BLOCK_K;
+    d.mn = g.mn;
+    d.a = g.a * HELD; d.b = g.b; d.c = g.c / HELD;
+    d.unit0 = units;
+    units += g.P.count;
+  }
+  p.n = n;
+  p.status = ctx->status();
+  const cudaError_t e = launch_pdl(muon_square_kernel, dim3(2 * units), dim3(SQUARE_THREADS), SQUARE_SMEM, st, p);
+  ctx->launches++;
+  return check_cuda(ctx, e, "muon_square_kernel launch");
 }
 
 }  // namespace muon

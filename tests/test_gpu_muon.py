@@ -88,6 +88,25 @@ def test_orthogonal_factor(ctx, rows, cols, dtype):
     near(got, orthogonal64(m.double().numpy()), TOL[dtype])
 
 
+@pytest.mark.parametrize("rows,cols", [(65, 65), (66, 1056), (66, 1057), (128, 2048), (193, 200), (255, 4080), (256, 257), (4096, 256), (1001, 250)])
+@pytest.mark.parametrize("iterations", [1, 2, 5])
+def test_small_squares(ctx, rows, cols, iterations):
+    """Sides of at most 256, on both sides of q = 16 p, where the square and the polynomial of it are one launch."""
+    m = draw(rows, cols, torch.bfloat16, seed=4)
+    got, = orthogonalize(ctx, [m], coefficients=STANDARD[:iterations])
+    near(got, orthogonal64(m.double().numpy(), STANDARD[:iterations]), TOL["bf16"])
+
+
+def test_more_small_squares_than_pairs_of_multiprocessors(ctx):
+    shapes = [(65, 90), (256, 300), (300, 256), (130, 129), (90, 65), (200, 200)]
+    ms = [draw(*shapes[i % 6], torch.bfloat16, seed=i) for i in range(170)]
+    for i, (m, o) in enumerate(zip(ms, orthogonalize(ctx, ms))):
+        near(o, orthogonal64(m.double().numpy()), TOL["bf16"], f"matrix {i}")
+        if i % 17 == 0:
+            alone, = orthogonalize(ctx, [m])
+            assert torch.equal(alone, o), f"matrix {i}"
+
+
 @pytest.mark.parametrize("rows,cols,dtype", [(1500, 4100, "bf16"), (2900, 1100, "bf16"), (1100, 2000, "f32")])
 def test_many_tiles(ctx, rows, cols, dtype):
     m = draw(rows, cols, DT[dtype], seed=1)
