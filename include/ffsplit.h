@@ -500,7 +500,7 @@ ffsplit_status ffsplit_muon_step(ffsplit_ctx* ctx, const ffsplit_muon_tensor* te
  * W may be missing: the adapters' part is then added to `base`, what some other path gave for the same tokens (a split
  * layer's forward, for instance), or is Y alone. */
 
-typedef struct { int32_t in, out, dtype; } ffsplit_projection;
+typedef struct { int32_t in, out, dtype; } ffsplit_projection;      /* 1 .. 2^23 each */
 
 typedef struct {
   const void* A;          /* dev [n, in, r]                                                                    */
@@ -508,7 +508,7 @@ typedef struct {
   const float* scale;     /* dev [n], NULL: 1                                                                  */
   const int32_t* index;   /* dev [T]: the adapter of each token, negative: none.  An index of n or more counts as
                              none and is reported as FFSPLIT_ERR_BAD_INDEX through ffsplit_poll()               */
-  int32_t n, r;           /* 1 <= r <= 128; adapters of a smaller rank are padded with zeros                    */
+  int32_t n, r;           /* 1 <= n <= 65535, 1 <= r <= 128; adapters of a smaller rank are padded with zeros   */
 } ffsplit_adapters;
 
 /* Workspace that the two calls below need. */

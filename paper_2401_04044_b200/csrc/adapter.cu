@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_con
   pdl_wait();
   const bool wide = (a.r_minor ? a.r : a.N) % V == 0;
   const int step = wide && !a.r_minor ? V : 1;              // columns of a thread
-  const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, c = (blockIdx.y * 32 + lane) * step;
+  const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, c = ((blockIdx.z * gridDim.y + blockIdx.y) * 32 + lane) * step;
   int token[G], of[G];
   const int count = tokens_of<G>(a.index, a.order, a.T, a.n, token, of);
   if (threadIdx.x == 0) {
@@ -645,7 +645,8 @@ ffsplit_status launch_shrink(const Call& c, adapter::ShrinkArgs& s, int jobs) {
 template <int G>
 ffsplit_status launch_expand_g(const Call& c, const adapter::ExpandArgs& x) {
   const int vec = c.f32 ? adapter::VEC<true> : adapter::VEC<false>, step = !x.r_minor && x.N % vec == 0 ? vec : 1;
-  const dim3 grid(static_cast<unsigned>((x.T + G - 1) / G), (x.N + 32 * step - 1) / (32 * step));
+  const unsigned across = (x.N + 32 * step - 1) / (32 * step), y = across < 32768 ? across : 32768;      // (a grid has 65535 rows at most)
+  const dim3 grid(static_cast<unsigned>((x.T + G - 1) / G), y, (across + y - 1) / y);
   constexpr int G16 = G < adapter::MANY ? G : adapter::SOME;
   const cudaError_t e = c.f32 ? launch_pdl(adapter::expand_kernel<true, G>, grid, dim3(adapter::EXPAND_THREADS), 0, c.st, x)
                               : launch_pdl(adapter::expand_kernel<false, G16>, grid, dim3(adapter::EXPAND_THREADS), 0, c.st, x);

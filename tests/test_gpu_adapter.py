@@ -321,3 +321,10 @@ def test_more_adapters_than_the_tensor_cores_tiles_allow(ctx):
            "dB": torch.zeros_like(D["B"][:, 0, :]).index_add_(0, at, P * D["dY"]).unsqueeze(1)}
     for o, v in got.items():
         assert float((v.double() - ref[o]).norm() / ref[o].norm()) <= TOL["bf16"], o
+
+
+@pytest.mark.parametrize("dtype,T", [("f32", 3), ("bf16", 3), ("bf16", 70)])
+@pytest.mark.parametrize("k,m", [(5, (1 << 21) + 35), ((1 << 21) + 35, 5)])
+def test_more_columns_than_a_grid_has_rows_of_blocks(ctx, dtype, T, k, m):
+    L = draw(dtype, k, m, T, 2, 3, shared="base")
+    check(run(ctx, L, dtype, in_place=True), L, dtype)
