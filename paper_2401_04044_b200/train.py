@@ -95,10 +95,20 @@ class Muon(torch.optim.Optimizer):
         self.lib = lib
         super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, coefficients=coefficients,
                                       iterations=iterations))
-        for group in self.param_groups:
-            for p in group["params"]:
-                if p.dim() < 2 or p.dtype not in (torch.float32, torch.bfloat16):
-                    raise FFSplitError(2, "Muon", "parameters are float32 or bfloat16 matrices, or stacks of them")
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        if any(p.dim() < 2 or p.dtype not in (torch.float32, torch.bfloat16) for p in self.param_groups[-1]["params"]):
+            self.param_groups.pop()
+            raise FFSplitError(2, "Muon", "parameters are float32 or bfloat16 matrices, or stacks of them")
+
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)
+        # (which gives a state its parameter's type: momentum is float32 beside bfloat16 parameters too)
+        saved = [i for group in state_dict["param_groups"] for i in group["params"]]
+        for i, p in zip(saved, (p for group in self.param_groups for p in group["params"])):
+            if "momentum" in state_dict["state"].get(i, {}):
+                self.state[p]["momentum"] = state_dict["state"][i]["momentum"].to(p.device, torch.float32, copy=True)
 
     @torch.no_grad()
     def step(self, closure=None):

@@ -73,3 +73,24 @@ def test_muon_list_checks_its_tensors():
             MuonList(0, **kw)
         assert e.value.code == code, kw
     assert MuonList(0, []).count == 0
+
+
+def test_the_optimiser_checks_later_groups_and_loads_its_momentum_in_32_bits():
+    from paper_2401_04044_b200 import FFSplitError
+    from paper_2401_04044_b200.train import Muon
+    params = lambda: [torch.ones(3, 5, dtype=torch.bfloat16, requires_grad=True), torch.ones(2, 4, 6, requires_grad=True)]  # noqa: E731
+    first, second = params(), params()
+    a, b = Muon(None, first[:1]), Muon(None, second[:1], lr=1.0)
+    for opt, p in ((a, first[1]), (b, second[1])):
+        opt.add_param_group({"params": [p], "lr": 0.5})
+        for bad in (torch.ones(4, requires_grad=True), torch.ones(4, 4, dtype=torch.float16, requires_grad=True)):
+            with pytest.raises(FFSplitError):
+                opt.add_param_group({"params": [bad]})
+        assert len(opt.param_groups) == 2
+    for p in first:
+        a.state[p]["momentum"] = torch.randn(p.shape)
+    b.load_state_dict(a.state_dict())
+    assert b.param_groups[0]["lr"] == 0.02
+    for p, q in zip(first, second):
+        m, n = a.state[p]["momentum"], b.state[q]["momentum"]
+        assert n.dtype is torch.float32 and torch.equal(m, n) and m.data_ptr() != n.data_ptr()
