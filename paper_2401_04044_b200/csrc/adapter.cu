@@ -240,6 +240,7 @@ struct ExpandArgs {
   const int *index, *order;
   long long T;
   int N, n, r, r_minor, splits;
+  int late;               // the kernel before, which gives base, was launched behind all else that is read here: waited for before base
 };
 constexpr int EXPAND_THREADS = 128, SHARES = EXPAND_THREADS / 32;
 template <bool F32, int G>
@@ -247,7 +248,7 @@ __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_con
   constexpr int V = VEC<F32>;
   __shared__ float p[MAX_RANK][G], sums[SHARES][V][G][32];
   __shared__ int row[G];
-  pdl_wait();
+  if (!a.late) pdl_wait();
   const bool wide = (a.r_minor ? a.r : a.N) % V == 0;
   const int step = wide && !a.r_minor ? V : 1;              // columns of a thread
   const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, c = ((blockIdx.z * gridDim.y + blockIdx.y) * 32 + lane) * step;
@@ -330,6 +331,7 @@ __global__ void __launch_bounds__(EXPAND_THREADS) expand_kernel(const __grid_con
 #pragma unroll
     for (int g = 0; g < G; ++g) sums[share][v][g][lane] = acc[v][g];
   __syncthreads();
+  if (a.late) pdl_wait();
   if (c >= a.N) return;
   // the shares' sums in order; a warp to every fourth token
 #pragma unroll
@@ -379,6 +381,7 @@ struct GradArgs {
   const int *count, *offset, *order;      // the tokens sorted by adapter, or nullptr: there are no more than THREADS
   long long T;
   int n, r;
+  int apart;                              // as in expand's launch, but waited for at the end
 };
 constexpr int GRAD_COLS = 32, GRAD_TOKENS = 64;
 // U: ranks of a thread, at least r / 8.
@@ -386,7 +389,7 @@ template <bool F32, int U>
 __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant__ GradArgs a) {
   __shared__ float p[GRAD_TOKENS][MAX_RANK], v[GRAD_TOKENS][GRAD_COLS];
   __shared__ int list[THREADS], found[THREADS / 32];
-  pdl_wait();
+  if (!a.apart) pdl_wait();
   const int which = static_cast<int>(blockIdx.x) >= a.job[0].blocks ? 1 : 0, i = blockIdx.y;
   const GradJob& job = a.job[which];
   const int c0 = (blockIdx.x - (which ? a.job[0].blocks : 0)) * GRAD_COLS;
@@ -432,14 +435,14 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant
       __syncthreads();
     }
   }
-  if (c0 + col >= job.N) return;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int j = jg + 8 * u;
-    if (j >= a.r) break;
+    if (j >= a.r || c0 + col >= job.N) break;
     const long long base = static_cast<long long>(i) * job.N * a.r;
     store<F32>(job.out, base + (job.r_minor ? static_cast<long long>(c0 + col) * a.r + j : static_cast<long long>(j) * job.N + c0 + col), acc[u]);
   }
+  if (a.apart) pdl_wait();
 }
 
 }  // namespace adapter
@@ -653,8 +656,8 @@ ffsplit_status launch_expand_g(const Call& c, const adapter::ExpandArgs& x) {
   c.ctx->launches++;
   return check_cuda(c.ctx, e, "adapter::expand_kernel launch");
 }
-ffsplit_status launch_expand(const Call& c, const float* P, int splits, const void* F, const void* base, void* Y, int N, int r_minor) {
-  const adapter::ExpandArgs x = {P, F, base, Y, c.a.index, c.sorted.order, c.T, N, c.a.n, c.a.r, r_minor, splits};
+ffsplit_status launch_expand(const Call& c, const float* P, int splits, const void* F, const void* base, void* Y, int N, int r_minor, bool late) {
+  const adapter::ExpandArgs x = {P, F, base, Y, c.a.index, c.sorted.order, c.T, N, c.a.n, c.a.r, r_minor, splits, late};
   switch (tokens_per_block(c.p, c.a.n, c.T)) {
     case adapter::MANY: return launch_expand_g<adapter::MANY>(c, x);
     case adapter::SOME: return launch_expand_g<adapter::SOME>(c, x);
@@ -704,8 +707,8 @@ ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projectio
     if ((s = launch_shrink(c, sh, 1)) != FFSPLIT_OK) return s;
   }
   if (W && (s = c.shared_product(c.X, bias, false, Y, extended ? &c.B : nullptr)) != FFSPLIT_OK) return s;
-  if (c.tc) return adapter::launch_expand_tc(ctx, c.tiles(c.L.P), c.B, c.p.out, W ? Y : base, Y, c.sorted, c.a.r, extended, c.st);
-  return launch_expand(c, c.inner(c.L.P), splits_of(c.p, c.a.n, T), adapters->B, W ? Y : base, Y, c.p.out, 0);
+  if (c.tc) return adapter::launch_expand_tc(ctx, c.tiles(c.L.P), c.B, c.p.out, W ? Y : base, Y, c.sorted, c.a.r, extended, W != nullptr, c.st);
+  return launch_expand(c, c.inner(c.L.P), splits_of(c.p, c.a.n, T), adapters->B, W ? Y : base, Y, c.p.out, 0, W != nullptr);
 }
 
 ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W, const void* base,
@@ -754,8 +757,8 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
   if (dX) {
     if (W && (s = c.shared_product(c.dY, nullptr, true, grads->dX, extended ? &c.A : nullptr)) != FFSPLIT_OK) return s;
     const void* add = W ? grads->dX : base;
-    s = c.tc ? adapter::launch_expand_tc(ctx, c.tiles(c.L.D), c.A, c.p.in, add, grads->dX, c.sorted, c.a.r, extended, c.st)
-             : launch_expand(c, c.inner(c.L.D), splits, adapters->A, add, grads->dX, c.p.in, 1);
+    s = c.tc ? adapter::launch_expand_tc(ctx, c.tiles(c.L.D), c.A, c.p.in, add, grads->dX, c.sorted, c.a.r, extended, W != nullptr, c.st)
+             : launch_expand(c, c.inner(c.L.D), splits, adapters->A, add, grads->dX, c.p.in, 1, W != nullptr);
     if (s != FFSPLIT_OK) return s;
   }
   if (!dA && !dB) return FFSPLIT_OK;
@@ -764,14 +767,14 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
     n = 0;
     if (dA) jobs[n++] = {c.X, c.tiles(c.L.D), grads->dA, c.p.in, 0};
     if (dB) jobs[n++] = {c.dY, c.tiles(c.L.P), grads->dB, c.p.out, 1};
-    return adapter::launch_gradients_tc(ctx, jobs, n, c.sorted, c.a.r, c.st);
+    return adapter::launch_gradients_tc(ctx, jobs, n, c.sorted, c.a.r, dX, c.st);
   }
   adapter::GradArgs g;
   std::memset(&g, 0, sizeof(g));
   n = 0;
   if (dA) g.job[n++] = {c.inner(c.L.D), X, grads->dA, c.p.in, 1, (c.p.in + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
   if (dB) g.job[n++] = {c.inner(c.L.P), dY, grads->dB, c.p.out, 0, (c.p.out + adapter::GRAD_COLS - 1) / adapter::GRAD_COLS};
-  g.index = adapters->index; g.T = T; g.n = c.a.n; g.r = c.a.r;
+  g.index = adapters->index; g.T = T; g.n = c.a.n; g.r = c.a.r; g.apart = dX;
   g.count = c.sorted.count; g.offset = c.sorted.offset; g.order = c.sorted.order;
   const dim3 grid(g.job[0].blocks + g.job[1].blocks, c.a.n);
   const auto kernel = c.a.r <= 16 ? (c.f32 ? adapter::gradient_kernel<true, 2> : adapter::gradient_kernel<false, 2>)

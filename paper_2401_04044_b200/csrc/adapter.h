@@ -52,9 +52,10 @@ struct Shrink {
 };
 ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, const Sorted& s, int r, const float* scale, cudaStream_t st);
 
-// Y[t] = base[t] + P F_i: [T, N], pitch N.  rest: only the tokens that the extension leaves out.
+// Y[t] = base[t] + P F_i: [T, N], pitch N.  rest: only the tokens that the extension leaves out.  late: base comes from the launches
+// behind the shrink; what else is read here is complete when they start to leave room for this kernel.
 ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const Factor& F, int N, const void* base, void* Y, const Sorted& s,
-                                int r, bool rest, cudaStream_t st);
+                                int r, bool rest, bool late, cudaStream_t st);
 
 // out_i = sum over the adapter's tokens of V[t]^T P[t] ([n][N][r], rank_rows: its transpose, [n][r][N]).  Up to two at once.
 struct Gradient {
@@ -63,7 +64,7 @@ struct Gradient {
   void* out;
   int N, rank_rows;
 };
-ffsplit_status launch_gradients_tc(ffsplit_ctx* ctx, const Gradient* jobs, int n, const Sorted& s, int r, cudaStream_t st);
+ffsplit_status launch_gradients_tc(ffsplit_ctx* ctx, const Gradient* jobs, int n, const Sorted& s, int r, bool apart, cudaStream_t st);
 
 }  // namespace adapter
 }  // namespace ffsp

@@ -491,6 +491,7 @@ struct ExpandParams {
   int N, r, f_mn;             // f_mn: the columns run along memory
   int blocks;                 // k-blocks of the rank: 1 or 2
   int rest;                   // rows that the extension has added are left as they are
+  int late;                   // the kernel before, which gives base, was launched behind all else that is read here: waited for before base
   int* status;
 };
 // A CTA keeps a tile's P and goes through every gridDim.x-th block of columns: the factor's next block is on its way while
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
     ptx::prefetch_tmap(&p.F);
   }
   const Frame f = frame_open<EXPAND_MMA>(raw, p.blocks * (A_BYTES + 2 * EXPAND_F), 3, EXPAND_TMEM, EXPAND_WARPS);     // (stages 0, 1: the factor, 2: P)
-  pdl_wait();
+  if (!p.late) pdl_wait();
   const Tile tile = find_tile(p.s, p.s.n + 1, blockIdx.y);
   const bool none = tile.group == p.s.n;
   bool leave = tile.group < 0 || (none && p.base == p.Y);
@@ -518,6 +519,7 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
   const auto done_before = [&](int row) { return by_slot && __ldcg(p.s.slot + __ldcg(p.s.order + tile.first + row)) >= 0; };
   if (by_slot) leave = __syncthreads_or(static_cast<int>(threadIdx.x) < tile.rows && !done_before(threadIdx.x)) == 0;
   if (leave) {
+    if (p.late) pdl_wait();
     frame_close<EXPAND_MMA>(f, EXPAND_TMEM, p.status);
     return;
   }
@@ -602,6 +604,7 @@ __global__ void __launch_bounds__(EXPAND_TC_THREADS, 2) expand_tc_kernel(const _
     __syncwarp();
     const uint2* base8 = reinterpret_cast<const uint2*>(p.base);
     uint2* Y8 = reinterpret_cast<uint2*>(p.Y);
+    if (p.late) pdl_wait();
     for (int i = 0, cb = blockIdx.x; cb < all; cb += gridDim.x, ++i) {
       const int c0 = cb * EXPAND_COLS + half * 64 + col;
       uint2 base[2][8];
@@ -677,6 +680,7 @@ struct GradientParams {
   GradientDev job[2];
   Sorted s;
   int r, cols, wide;          // wide: r is a multiple of 8
+  int apart;                  // the kernel before was launched behind all that is read here, and does not touch what is written: waited for at the end
   int stage;
   int* status;
 };
@@ -694,7 +698,7 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
     ptx::prefetch_tmap(&job.P);
   }
   const Frame f = frame_open(raw, GRADIENT_STAGES * p.stage, GRADIENT_STAGES, GRADIENT_TMEM);
-  pdl_wait();
+  if (!p.apart) pdl_wait();
   const int count = __ldcg(p.s.count + i), first = __ldcg(p.s.offset + i);
   const int kb = (count + BLOCK_K - 1) / BLOCK_K;
   if (warp == COPY_WARP) {
@@ -785,6 +789,7 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
     __syncwarp();
   }
   frame_close(f, GRADIENT_TMEM, p.status);
+  if (p.apart) pdl_wait();
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -898,7 +903,7 @@ ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, con
 }
 
 ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const Factor& F, int N, const void* base, void* Y, const Sorted& s,
-                                int r, bool rest, cudaStream_t st) {
+                                int r, bool rest, bool late, cudaStream_t st) {
   ffsplit_status rc = set_up(ctx);
   if (rc != FFSPLIT_OK) return rc;
   ExpandParams p;
@@ -909,7 +914,7 @@ ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const 
   if ((rc = encode_factor(ctx, F, s.n, p.f_mn ? BLOCK_K : EXPAND_COLS, &p.F)) != FFSPLIT_OK) return rc;
   p.s = s;
   p.base = static_cast<const __nv_bfloat16*>(base); p.Y = static_cast<__nv_bfloat16*>(Y);
-  p.N = N; p.r = r; p.rest = rest ? 1 : 0; p.status = ctx->status();
+  p.N = N; p.r = r; p.rest = rest ? 1 : 0; p.late = late ? 1 : 0; p.status = ctx->status();
   p.blocks = r > BLOCK_K ? 2 : 1;
   // Two CTAs to an SM where there are few tiles, else four blocks of columns to a CTA: its start is paid once, and the last
   // round of CTAs stays short (fourteen blocks each, 342 CTAs on 296 places: 114 us instead of 57).
@@ -923,12 +928,12 @@ ffsplit_status launch_expand_tc(ffsplit_ctx* ctx, const __nv_bfloat16* P, const 
   return check_cuda(ctx, e, "adapter::expand_tc_kernel launch");
 }
 
-ffsplit_status launch_gradients_tc(ffsplit_ctx* ctx, const Gradient* jobs, int n, const Sorted& s, int r, cudaStream_t st) {
+ffsplit_status launch_gradients_tc(ffsplit_ctx* ctx, const Gradient* jobs, int n, const Sorted& s, int r, bool apart, cudaStream_t st) {
   ffsplit_status rc = set_up(ctx);
   if (rc != FFSPLIT_OK) return rc;
   GradientParams p;
   std::memset(&p, 0, sizeof(p));
-  p.s = s; p.r = r; p.cols = round_up(r, 16); p.wide = r % 8 == 0; p.stage = stage_bytes(r); p.status = ctx->status();
+  p.s = s; p.r = r; p.cols = round_up(r, 16); p.wide = r % 8 == 0; p.stage = stage_bytes(r); p.apart = apart ? 1 : 0; p.status = ctx->status();
   int blocks = 0;
   for (int i = 0; i < n; ++i) {
     GradientDev& d = p.job[i];
