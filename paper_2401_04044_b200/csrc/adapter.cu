@@ -600,6 +600,7 @@ struct Call {
       if (s == FFSPLIT_OK && most > 0) s = adapter::launch_check(ctx, F, each, sorted, st);
       if (s != FFSPLIT_OK) return s;
     }
+    prep.apart = is_sorted(T);      // (beside the sort)
     return train::launch_prepare(ctx, prep, prep_blocks, f32, st);
   }
   // C [T, N] = V [T, K] times W [in, out] (transposed: its transpose).

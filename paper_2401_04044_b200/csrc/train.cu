@@ -23,7 +23,7 @@ namespace train {
 template <bool F32>
 __global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_constant__ PrepArgs a) {
   constexpr int UNROLL = PREP_UNROLL<F32>;
-  pdl_wait();
+  if (!a.apart) pdl_wait();
   int j = 0;
   while (j + 1 < a.n && static_cast<int>(blockIdx.x) >= a.job[j + 1].block0) ++j;
   const PrepJob& job = a.job[j];
@@ -88,6 +88,7 @@ __global__ void __launch_bounds__(PREP_THREADS) prepare_kernel(const __grid_cons
                      : make_uint4(x[0], x[1], x[2], x[3]);
     }
   }
+  if (a.apart) pdl_wait();
 }
 
 // Bias gradients: out[c] = sum over rows of in[r, c], in fp32 and in a fixed order.  db2 sums the rows of dY; for db1 the

@@ -126,6 +126,7 @@ struct PrepJob {
 struct PrepArgs {
   PrepJob job[MAX_JOBS];
   int n;
+  int apart;             // the launch before neither gives nor takes these tensors, and waited itself: waited for at the end
 };
 constexpr int PREP_THREADS = 256;
 template <bool F32> constexpr int PREP_UNROLL = F32 ? 2 : 4;
