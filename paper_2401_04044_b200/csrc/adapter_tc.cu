@@ -29,7 +29,7 @@ constexpr int A_BYTES = TOKENS * BLOCK_K * 2, B_BYTES = MAX_RANK * BLOCK_K * 2;
 // ---------------------------------------------------------------------------------------------- sorting
 // A block to a group: one pass counts its tokens and those of the groups before it, another writes them in their order.
 constexpr int SORT_THREADS = 256, SORT_FLIGHT = 4;
-// Blocks behind the groups: the entries of a tile of 256 rows, and zeros where their rows will be.
+// Blocks behind the groups: the entries of a tile of 256 rows.
 __device__ __forceinline__ void plan_tile(const int* __restrict__ index, const Sorted& s, int tile) {
   __shared__ __align__(16) int of[EXTENSION_ROWS];
   __shared__ int ids[EXTENSION_ROWS], firsts[EXTENSION_ROWS / 32];
@@ -64,8 +64,6 @@ __device__ __forceinline__ void plan_tile(const int* __restrict__ index, const S
   if (i == 0) s.entries[tile] = kept ? all : 0;
   if (!kept) return;
   if (i < all) s.ids[static_cast<long long>(tile) * s.most + i] = ids[i];
-  uint4* Q = reinterpret_cast<uint4*>(s.Q + static_cast<long long>(tile) * s.most * EXTENSION_ROWS * s.pitch);
-  for (int k = i; k < all * EXTENSION_ROWS * s.pitch / 8; k += SORT_THREADS) Q[k] = make_uint4(0u, 0u, 0u, 0u);
 }
 static_assert(SORT_THREADS == EXTENSION_ROWS, "a thread to a row");
 __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const int* __restrict__ index, Sorted s, int* status) {
@@ -136,11 +134,20 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const int* __restric
   }
 }
 
-// A row of blocks to an adapter.
+// A row of blocks to an adapter.  In passing: zeros where the rows of the tiles' entries will be (800 KB for a tile of 24 adapters of
+// rank 32: the block that plans the tile took 6 us for that alone).
 constexpr int CHECK_CHUNK = 32768;      // elements
 __global__ void __launch_bounds__(256) check_kernel(const __nv_bfloat16* __restrict__ F, long long each, Sorted s) {
   pdl_wait();
-  const int i = blockIdx.y;
+  const int i = blockIdx.y, tiles = static_cast<int>((s.T + EXTENSION_ROWS - 1) / EXTENSION_ROWS);
+  // (as many blocks to a tile as there are, or as many tiles to a block)
+  const int blocks = gridDim.x * gridDim.y, block = blockIdx.y * gridDim.x + blockIdx.x, share = blocks > tiles ? blocks / tiles : 1;
+  const int entry = EXTENSION_ROWS * s.pitch / 8;
+  for (int t = block / share; t < tiles; t += blocks / share) {
+    uint4* Q = reinterpret_cast<uint4*>(s.Q) + static_cast<long long>(t) * s.most * entry;
+    const int vectors = __ldcg(s.entries + t) * entry;      // (no more than 32 entries)
+    for (int k = block % share * 256 + threadIdx.x; k < vectors; k += share * 256) Q[k] = make_uint4(0u, 0u, 0u, 0u);
+  }
   if (__ldcg(s.count + i) == 0) return;
   const long long begin = static_cast<long long>(blockIdx.x) * CHECK_CHUNK, end = begin + CHECK_CHUNK < each ? begin + CHECK_CHUNK : each;
   const unsigned short* p = reinterpret_cast<const unsigned short*>(F) + i * each;
