@@ -476,7 +476,7 @@ int splits_of(const ffsplit_projection& p, int n, long long T) {
 // The adapters' part inside the shared product, in a product of `width` columns over `sum`: entries to a tile of 256 rows.  An
 // entry costs a tile as much as one or two k-blocks of its sum; where a tile has more adapters than half its k-blocks, or than
 // 32, a second pass over Y is cheaper.  So it is where Y is small: the pass moves 2.7 TB/s (63 us of 335 for 4096 x 11008), while
-// checking the factors and planning the entries take 20 us and the entries of 24 adapters 30 us in that product.  The entries
+// checking the factors and planning the entries take 15 us and the entries of 24 adapters 30 us in that product.  The entries
 // take 32 KB (64 KB) each, 256 MB in all at most.
 int extension_most(const ffsplit_projection& p, int n, int r, long long T, int sum, int width) {
   if (!on_tensor_cores(p, n, T) || T * width < (32ll << 20)) return 0;
