@@ -12,6 +12,7 @@
 
 #include "epilogue.cuh"
 #include "muon.h"
+#include "ptx.cuh"
 
 namespace ffsp {
 namespace muon {
@@ -331,23 +332,33 @@ __global__ void __launch_bounds__(THREADS) thin_gram_kernel(const __grid_constan
   for (int i = threadIdx.x; i < p * p; i += THREADS) S[i] = sum[i / p][i % p];
 }
 
-// C = A B of tiles x tiles tiles: f(row, column, two values) for every pair of C.  Everything is symmetric up to rounding (all
-// are polynomials in S), so B is read along its rows like A.
+// C = A B of tiles x tiles tiles: f(row, column, value) for every element of C.  Everything is symmetric up to rounding (all are
+// polynomials in S), so B is read along its rows like A, and tiles below the diagonal are those above it, turned: 36 of 64 for
+// p = 64, which the fp64 instructions are busy with for 1.2 us instead of 2.1.
 template <typename F>
 __device__ __forceinline__ void thin_product(const Square A, const Square B, int tiles, F f) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = warp; i < tiles * tiles; i += blockDim.x / 32) {
-    const int ti = i / tiles, tj = i - ti * tiles;
+  for (int i = warp; i < tiles * (tiles + 1) / 2; i += blockDim.x / 32) {
+    int ti = 0, tj = i;
+    while (tj >= tiles - ti) tj -= tiles - ti++;
+    tj += ti;
     double c[2][2] = {};
 #pragma unroll 4
     for (int k = 0; k < 8 * tiles; k += 8) {
       mma8(c[0], A[8 * ti + (lane >> 2)][k + (lane & 3)], B[8 * tj + (lane >> 2)][k + (lane & 3)]);
       mma8(c[1], A[8 * ti + (lane >> 2)][k + 4 + (lane & 3)], B[8 * tj + (lane >> 2)][k + 4 + (lane & 3)]);
     }
-    f(8 * ti + (lane >> 2), 8 * tj + 2 * (lane & 3), c[0][0] + c[1][0], c[0][1] + c[1][1]);
+    const int row = 8 * ti + (lane >> 2), col = 8 * tj + 2 * (lane & 3);
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const double x = c[0][v] + c[1][v];
+      f(row, col + v, x);
+      if (ti != tj) f(col + v, row, x);
+    }
   }
 }
 constexpr int SOLVE_THREADS = 512;
+// A block to a matrix, or a cluster whose blocks share the adding up of the parts (2 MB for 64 parts of p = 64: 45 us alone).
 template <int CAP>
 __global__ void __launch_bounds__(SOLVE_THREADS) thin_solve_kernel(const __grid_constant__ ThinTable<CAP> t) {
   extern __shared__ double thin_smem[];
@@ -356,20 +367,22 @@ __global__ void __launch_bounds__(SOLVE_THREADS) thin_solve_kernel(const __grid_
   // S and Q move between two buffers each
   const Square S0 = reinterpret_cast<Square>(thin_smem), S1 = S0 + rows, Q0 = S1 + rows, Q1 = Q0 + rows, A = Q1 + rows;
   pdl_wait();
-  const Entry& e = t.t[blockIdx.x];
+  const int which = blockIdx.y;
+  const Entry& e = t.t[which];
   const int p = e.rows > e.cols ? e.cols : e.rows, tiles = (p + 7) / 8;
-  const double* partial = t.S[blockIdx.x];
-  for (int i = threadIdx.x; i < 64 * tiles * tiles; i += SOLVE_THREADS) {
+  const double* partial = t.S[which];
+  for (int i = blockIdx.x * SOLVE_THREADS + threadIdx.x; i < 64 * tiles * tiles; i += gridDim.x * SOLVE_THREADS) {
     const int r = i / (8 * tiles), c = i % (8 * tiles);
     double s = 0.0;
     if (r < p && c < p) {
-#pragma unroll 8
+#pragma unroll 16
       for (int k = 0; k < e.parts; ++k) s += __ldcg(partial + static_cast<long long>(k) * p * p + r * p + c);
     }
-    S0[r][c] = s;
-    Q0[r][c] = r == c ? 1.0 : 0.0;
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(ptx::map_to_cta(ptx::smem_u32(&S0[r][c]), 0)), "d"(s) : "memory");
   }
-  __syncthreads();
+  if (gridDim.x > 1) ptx::cluster_sync_all();
+  else __syncthreads();
+  if (blockIdx.x > 0) return;
   if (threadIdx.x < 32) {
     double trace = 0.0;
     for (int i = threadIdx.x; i < p; i += 32) trace += S0[i][i];
@@ -385,15 +398,18 @@ __global__ void __launch_bounds__(SOLVE_THREADS) thin_solve_kernel(const __grid_
   Square S = S0, S_next = S1, Q = Q0, Q_next = Q1;
   for (int it = 0; it < t.iterations && finite; ++it) {
     const double a = t.coefficients[3 * it], b = t.coefficients[3 * it + 1], c = t.coefficients[3 * it + 2];
-    thin_product(S, S, tiles, [&](int r, int k, double x, double y) {
+    // (Q is the identity before the first iteration, and nobody asks for S after the last one)
+    thin_product(S, S, tiles, [&](int r, int k, double x) {
       A[r][k] = fma(c, x, fma(b, S[r][k], r == k ? a : 0.0));
-      A[r][k + 1] = fma(c, y, fma(b, S[r][k + 1], r == k + 1 ? a : 0.0));
+      if (it == 0) Q_next[r][k] = A[r][k];
     });
     __syncthreads();
-    thin_product(A, Q, tiles, [&](int r, int k, double x, double y) { Q_next[r][k] = x; Q_next[r][k + 1] = y; });
-    thin_product(A, S, tiles, [&](int r, int k, double x, double y) { S_next[r][k] = x; S_next[r][k + 1] = y; });
-    __syncthreads();
-    thin_product(S_next, A, tiles, [&](int r, int k, double x, double y) { S[r][k] = x; S[r][k + 1] = y; });
+    if (it > 0) thin_product(A, Q, tiles, [&](int r, int k, double x) { Q_next[r][k] = x; });
+    if (it + 1 < t.iterations) {
+      thin_product(A, S, tiles, [&](int r, int k, double x) { S_next[r][k] = x; });
+      __syncthreads();
+      thin_product(S_next, A, tiles, [&](int r, int k, double x) { S[r][k] = x; });
+    }
     __syncthreads();
     const Square q = Q;
     Q = Q_next;
@@ -401,8 +417,8 @@ __global__ void __launch_bounds__(SOLVE_THREADS) thin_solve_kernel(const __grid_
   }
   // what is not finite leaves here as NaN: the last kernel leaves such a matrix alone
   for (int i = threadIdx.x; i < p * p; i += SOLVE_THREADS)
-    t.Q[blockIdx.x][i] = finite ? Q[i / p][i % p] * inv : __longlong_as_double(0x7fffffffffffffffll);
-  if (threadIdx.x == 0 && !finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, blockIdx.x, KID_MUON);
+    t.Q[which][i] = finite ? Q[i / p][i % p] * inv : __longlong_as_double(0x7fffffffffffffffll);
+  if (threadIdx.x == 0 && !finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, which, KID_MUON);
 }
 
 // W' = keep W - step Q U for every chunk, and M'.  A warp to every eighth eight columns.
@@ -719,7 +735,24 @@ ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, f
     e = cudaFuncSetAttribute(muon::thin_apply_kernel<CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(muon::THIN_U_BYTES + muon::square_bytes(8)));
   if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(muon::thin kernels)");
   e = launch_pdl(muon::thin_gram_kernel<CAP>, dim3(blocks, tab.n), dim3(muon::THREADS), muon::THIN_U_BYTES, st, tab);
-  if (e == cudaSuccess) e = launch_pdl(muon::thin_solve_kernel<CAP>, dim3(tab.n), dim3(muon::SOLVE_THREADS), 5 * muon::square_bytes(tab.tiles), st, tab);
+  if (e == cudaSuccess) {
+    // (a block of the largest p takes an SM)
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks >= 8 && 8 * tab.n <= ctx->num_sms ? 8 : 1, tab.n);
+    cfg.blockDim = dim3(muon::SOLVE_THREADS);
+    cfg.dynamicSmemBytes = 5 * muon::square_bytes(tab.tiles);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cfg.gridDim.x;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, muon::thin_solve_kernel<CAP>, tab);
+  }
   if (e == cudaSuccess) e = launch_pdl(muon::thin_apply_kernel<CAP>, dim3(blocks, tab.n), dim3(muon::THREADS), apply_bytes, st, tab);
   ctx->launches += 3;
   return check_cuda(ctx, e, "muon::thin kernels launch");
