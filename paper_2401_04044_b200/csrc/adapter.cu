@@ -6,6 +6,7 @@
 // The shared product runs on the tensor cores (train_gemm.cu).  So do the adapters' products of bf16 batches of more than
 // FEW tokens (adapter_tc.cu).  Those of few tokens and of fp32 layers are taken here, on the CUDA cores in fp32.
 #include <cstring>
+#include <type_traits>
 
 #include "adapter.h"
 #include "epilogue.cuh"
@@ -150,34 +151,57 @@ __global__ void __launch_bounds__(THREADS) shrink_kernel(const __grid_constant__
           }
         }
       } else {
-        // a warp to a rank, lanes along the contraction
-        for (int c = warp; c < a.r; c += THREADS / 32) {
-          float sum[G] = {};
-          const long long at = f0 + static_cast<long long>(c) * job.K + k0;
+        // a warp to R ranks at a time, lanes along the contraction (one rank after the other waits for every load: 32 us instead of 19
+        // for 27 tokens of rank 96, K = 8120)
+        constexpr int R = G == 1 ? 4 : 2, STEP = THREADS / 32;
+        for (int c = warp; c < a.r; c += R * STEP) {
+          float sum[R][G] = {};
+          const long long at = f0 + static_cast<long long>(c) * job.K + k0, next = static_cast<long long>(STEP) * job.K;
           if (wide) {
 #pragma unroll 2
             for (int k = lane * V; k < m; k += 32 * V) {
-              float f[V];
-              load_vec<F32>(job.F, at + k, f);
+              float f[R][V];
+#pragma unroll
+              for (int q = 0; q < R; ++q) {
+                if (c + q * STEP < a.r) {
+                  load_vec<F32>(job.F, at + q * next + k, f[q]);
+                } else {
+#pragma unroll
+                  for (int v = 0; v < V; ++v) f[q][v] = 0.f;
+                }
+              }
 #pragma unroll
               for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int v = 0; v < V; ++v) sum[g] = fmaf(x[g][k + v], f[v], sum[g]);
+                for (int v = 0; v < V; ++v) {
+                  const float y = x[g][k + v];
+#pragma unroll
+                  for (int q = 0; q < R; ++q) sum[q][g] = fmaf(y, f[q][v], sum[q][g]);
+                }
             }
           } else {
 #pragma unroll 4
             for (int k = lane; k < m; k += 32) {
-              const float f = load<F32>(job.F, at + k);
+              float f[R];
 #pragma unroll
-              for (int g = 0; g < G; ++g) sum[g] = fmaf(x[g][k], f, sum[g]);
+              for (int q = 0; q < R; ++q) f[q] = c + q * STEP < a.r ? load<F32>(job.F, at + q * next + k) : 0.f;
+#pragma unroll
+              for (int g = 0; g < G; ++g) {
+                const float y = x[g][k];
+#pragma unroll
+                for (int q = 0; q < R; ++q) sum[q][g] = fmaf(y, f[q], sum[q][g]);
+              }
             }
           }
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
+          for (int q = 0; q < R; ++q)
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], o);
-            if (lane == 0) part[c * G + g] = fresh ? sum[g] : part[c * G + g] + sum[g];
-          }
+            for (int g = 0; g < G; ++g) {
+#pragma unroll
+              for (int o = 16; o > 0; o >>= 1) sum[q][g] += __shfl_xor_sync(0xffffffffu, sum[q][g], o);
+              float* to = part + (c + q * STEP) * G + g;
+              if (lane == 0 && c + q * STEP < a.r) *to = fresh ? sum[q][g] : *to + sum[q][g];
+            }
         }
       }
       fresh = false;
@@ -383,18 +407,25 @@ struct GradArgs {
   int n, r;
   int apart;                              // as in expand's launch, but waited for at the end
 };
-constexpr int GRAD_COLS = 32, GRAD_TOKENS = 64;
+// A block takes 64 columns, two to a thread, and all ranks.  Bound by writing the gradients, most of them zeros where a few tokens
+// meet many adapters (57 of rank 88 and 10256 columns, 10 tokens: 92 us with 32 columns and 2 bytes to a store, 41 us so).
+constexpr int GRAD_COLS = 64, GRAD_TOKENS = 32;
 // U: ranks of a thread, at least r / 8.
 template <bool F32, int U>
 __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant__ GradArgs a) {
-  __shared__ float p[GRAD_TOKENS][MAX_RANK], v[GRAD_TOKENS][GRAD_COLS];
+  using Value = std::conditional_t<F32, float, __nv_bfloat16>;
+  constexpr int RANKS = 8 * U;
+  constexpr size_t P_BYTES = GRAD_TOKENS * RANKS * 4, OUT_BYTES = GRAD_COLS * RANKS * sizeof(Value);
+  __shared__ __align__(16) char area[P_BYTES > OUT_BYTES ? P_BYTES : OUT_BYTES];
+  __shared__ __align__(16) float v[GRAD_TOKENS][GRAD_COLS];
   __shared__ int list[THREADS], found[THREADS / 32];
+  float(*p)[RANKS] = reinterpret_cast<float(*)[RANKS]>(area);
   if (!a.apart) pdl_wait();
   const int which = static_cast<int>(blockIdx.x) >= a.job[0].blocks ? 1 : 0, i = blockIdx.y;
   const GradJob& job = a.job[which];
   const int c0 = (blockIdx.x - (which ? a.job[0].blocks : 0)) * GRAD_COLS;
-  const int col = threadIdx.x & 31, jg = threadIdx.x >> 5, lane = col;
-  float acc[U] = {};
+  const int lane = threadIdx.x & 31, jg = threadIdx.x >> 5;
+  float acc[U][2] = {};
   const int mine = a.order ? __ldcg(a.count + i) : static_cast<int>(a.T), from = a.order ? __ldcg(a.offset + i) : 0;
   for (int t0 = 0; t0 < mine; t0 += THREADS) {
     int all;
@@ -428,19 +459,50 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(const __grid_constant
       }
       __syncthreads();
       for (int q = 0; q < m; ++q) {
-        const float x = v[q][col];
+        const float2 x = *reinterpret_cast<const float2*>(&v[q][2 * lane]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) if (jg + 8 * u < a.r) acc[u] = fmaf(p[q][jg + 8 * u], x, acc[u]);
+        for (int u = 0; u < U; ++u)
+          if (jg + 8 * u < a.r) {
+            acc[u][0] = fmaf(p[q][jg + 8 * u], x.x, acc[u][0]);
+            acc[u][1] = fmaf(p[q][jg + 8 * u], x.y, acc[u][1]);
+          }
       }
       __syncthreads();
     }
   }
+  const long long first = static_cast<long long>(i) * job.N * a.r;
+  if (job.r_minor) {
+    // these columns' ranks are one run of memory
+    Value* turn = reinterpret_cast<Value*>(area);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int j = jg + 8 * u;
-    if (j >= a.r || c0 + col >= job.N) break;
-    const long long base = static_cast<long long>(i) * job.N * a.r;
-    store<F32>(job.out, base + (job.r_minor ? static_cast<long long>(c0 + col) * a.r + j : static_cast<long long>(j) * job.N + c0 + col), acc[u]);
+    for (int u = 0; u < U; ++u)
+      if (jg + 8 * u < a.r) {
+        store<F32>(turn, 2 * lane * a.r + jg + 8 * u, acc[u][0]);
+        store<F32>(turn, (2 * lane + 1) * a.r + jg + 8 * u, acc[u][1]);
+      }
+    __syncthreads();
+    const int n = (job.N - c0 < GRAD_COLS ? job.N - c0 : GRAD_COLS) * a.r;
+    Value* out = static_cast<Value*>(job.out) + first + static_cast<long long>(c0) * a.r;
+    constexpr int V = VEC<F32>;
+    const int whole = (reinterpret_cast<uintptr_t>(out) & 15u) == 0 ? n / V : 0;
+    for (int e = threadIdx.x; e < whole; e += THREADS) reinterpret_cast<uint4*>(out)[e] = reinterpret_cast<const uint4*>(turn)[e];
+    for (int e = whole * V + threadIdx.x; e < n; e += THREADS) out[e] = turn[e];
+  } else {
+    const int c = c0 + 2 * lane;
+    const bool even = job.N % 2 == 0;      // (then every row starts on two elements)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = jg + 8 * u;
+      if (j >= a.r || c >= job.N) break;
+      const long long at = first + static_cast<long long>(j) * job.N + c;
+      if (even) {
+        if constexpr (F32) *reinterpret_cast<float2*>(static_cast<float*>(job.out) + at) = make_float2(acc[u][0], acc[u][1]);
+        else *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(job.out) + at) = pack_bf16x2(acc[u][0], acc[u][1]);
+      } else {
+        store<F32>(job.out, at, acc[u][0]);
+        if (c + 1 < job.N) store<F32>(job.out, at + 1, acc[u][1]);
+      }
+    }
   }
   if (a.apart) pdl_wait();
 }

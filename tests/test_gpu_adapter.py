@@ -328,3 +328,12 @@ def test_more_adapters_than_the_tensor_cores_tiles_allow(ctx):
 def test_more_columns_than_a_grid_has_rows_of_blocks(ctx, dtype, T, k, m):
     L = draw(dtype, k, m, T, 2, 3, shared="base")
     check(run(ctx, L, dtype, in_place=True), L, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shared", ["weight", "base"])
+@pytest.mark.parametrize("k,m,T,n,r", [(200, 415, 10, 57, 88), (131, 64, 64, 3, 128), (66, 130, 33, 5, 17), (63, 65, 2, 9, 8)])
+def test_few_tokens_of_many_ranks(ctx, dtype, shared, k, m, T, n, r):
+    """Columns that fill no block of 64, ranks that fill no round of warps, adapters without a token."""
+    L = draw(dtype, k, m, T, n, r, shared=shared, seed=6)
+    check(run(ctx, L, dtype), L, dtype)
