@@ -358,7 +358,7 @@ __device__ __forceinline__ void thin_product(const Square A, const Square B, int
   }
 }
 constexpr int SOLVE_THREADS = 512;
-// A block to a matrix, or a cluster whose blocks share the adding up of the parts (2 MB for 64 parts of p = 64: 45 us alone).
+// A block to a matrix, or a cluster whose blocks share the adding up of the parts (2 MB for 64 parts of p = 64: 100 of 200 us alone).
 template <int CAP>
 __global__ void __launch_bounds__(SOLVE_THREADS) thin_solve_kernel(const __grid_constant__ ThinTable<CAP> t) {
   extern __shared__ double thin_smem[];
