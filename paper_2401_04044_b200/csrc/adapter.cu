@@ -783,6 +783,7 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
   if (!dY || !grads) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "NULL tensor");
   if (!grads->dX && !grads->dA && !grads->dB) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "no gradient asked for");
   if (grads->dX && W && base) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "W, or base, or neither");
+  if (!grads->dX) W = base = nullptr;
   for (const void* q : {dY, W, base, static_cast<const void*>(grads->dX), static_cast<const void*>(grads->dA), static_cast<const void*>(grads->dB)})
     if (!aligned16(q)) return fail(ctx, FFSPLIT_ERR_ALIGN, "tensors must be 16-byte aligned");
   Call c(ctx, *projection, *adapters, T, stream);

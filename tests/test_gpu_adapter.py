@@ -337,3 +337,15 @@ def test_few_tokens_of_many_ranks(ctx, dtype, shared, k, m, T, n, r):
     """Columns that fill no block of 64, ranks that fill no round of warps, adapters without a token."""
     L = draw(dtype, k, m, T, n, r, shared=shared, seed=6)
     check(run(ctx, L, dtype), L, dtype)
+
+
+def test_a_weight_is_not_looked_at_where_its_gradient_is_not_wanted(ctx):
+    from paper_2401_04044_b200 import Projection
+    L = draw("bf16", 72, 88, 20, 3, 8)
+    D = {k: None if v is None else v.cuda() for k, v in L.items()}
+    W = torch.full((72 * 88 + 8,), float("nan"), dtype=torch.bfloat16, device="cuda")[1:1 + 72 * 88].view(72, 88)      # on two bytes
+    p, dA, dB = Projection(72, 88, torch.bfloat16), torch.empty_like(D["A"]), torch.empty_like(D["B"])
+    ctx.ensure_workspace(ctx.adapter_workspace_size(p, 3, 8, 20))
+    ctx.adapter_backward(p, D["X"], D["A"], D["B"], D["index"], D["dY"], W=W, base=D["X"], scale=D["scale"], dA=dA, dB=dB)
+    ctx.poll()
+    check({"dA": dA.cpu(), "dB": dB.cpu()}, L, "bf16")
