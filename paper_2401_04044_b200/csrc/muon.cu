@@ -366,6 +366,7 @@ __global__ void __launch_bounds__(SOLVE_THREADS) thin_solve_kernel(const __grid_
   const int rows = t.tiles * 8;
   // S and Q move between two buffers each
   const Square S0 = reinterpret_cast<Square>(thin_smem), S1 = S0 + rows, Q0 = S1 + rows, Q1 = Q0 + rows, A = Q1 + rows;
+  if (gridDim.x > 1) ptx::cluster_sync_all();      // (the first block is known to run before the others write to it; under the tail of the kernel before)
   pdl_wait();
   const int which = blockIdx.y;
   const Entry& e = t.t[which];
