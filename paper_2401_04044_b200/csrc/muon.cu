@@ -578,18 +578,31 @@ ffsplit_status check_list(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int co
   return FFSPLIT_OK;
 }
 
-// Whether the iteration keeps singular values of [0, 1] below 1.5 and P = a I + b S + c S^2 below 200.
-bool coefficients_hold(const float* c, int iterations) {
+// What a list of coefficients allows.
+struct Coefficients {
+  const float* k;                       // [iterations][3], or nullptr: the standard ones
+  int iterations;
+  bool pair[16];                        // iterations i and i + 1 may be taken as one
+};
+
+// Whether the iteration keeps singular values of [0, 1] below 1.5 and P = a I + b S + c S^2 below 200; and which iterations
+// keep P2 P below 200 together with the one after them (each may be steep where the other one shrinks).
+bool coefficients_hold(Coefficients* list) {
+  const auto polynomial = [](const float* c, double s) { return c[0] + s * s * (c[1] + s * s * c[2]); };
+  const float* c = list->k;
+  for (int i = 0; i < 3 * list->iterations; ++i) if (!(std::fabs(c[i]) <= 64.f)) return false;
   double top = 1.0;
-  for (int i = 0; i < iterations; ++i, c += 3) {
-    for (int k = 0; k < 3; ++k) if (!(std::fabs(c[k]) <= 64.f)) return false;
-    double most = 0.0;
+  for (int i = 0; i < list->iterations; ++i, c += 3) {
+    const bool followed = i + 1 < list->iterations;
+    double most = 0.0, both = 0.0;
     for (int k = 0; k <= 4096; ++k) {
-      const double s = top * k / 4096, v = std::fabs(s * (c[0] + s * s * (c[1] + s * s * c[2])));
+      const double s = top * k / 4096, p = polynomial(c, s), v = std::fabs(s * p);
+      if (!(std::fabs(p) <= 200.0)) return false;
       if (v > most) most = v;
-      if (!(std::fabs(c[0] + s * s * (c[1] + s * s * c[2])) <= 200.0)) return false;
+      if (followed) both = std::fmax(both, std::fabs(p * polynomial(c + 3, v)));
     }
     if (!(most <= 1.5)) return false;
+    list->pair[i] = followed && both <= 200.0;
     top = most;
   }
   return true;
@@ -602,10 +615,11 @@ struct Group {
   muon::Matrices X[2], S, P, T, R;      // T, R: paired only
   int at;                               // which X is the current one
 };
-// Two iterations at once.  The second one's S is P S P (all of these are polynomials in S), so X need not be formed between the
-// two: X <- (P2 P) X with P2 = a I + b S2 + c S2 S2, S2 = (P S) P.  3 p^2 q + 5 p^3 multiply-adds instead of 6 p^2 q + 2 p^3,
-// and X is read and written once instead of twice; for two roundings more, which leave up to 3e-3 of the result instead of
-// 2e-3.  Small matrices would pay for one launch more (256 x 1024: 50 us for a pair either way).
+// Two iterations at once, where P2 P stays below 200 (see coefficients_hold()).  The second one's S is P S P (all of these are
+// polynomials in S), so X need not be formed between the two: X <- (P2 P) X with P2 = a I + b S2 + c S2 S2, S2 = (P S) P.
+// 3 p^2 q + 5 p^3 multiply-adds instead of 6 p^2 q + 2 p^3, and X is read and written once instead of twice; for two roundings
+// more, which leave up to 3e-3 of the result instead of 2e-3.  Small matrices would pay for one launch more (256 x 1024: 50 us
+// for a pair either way).
 bool in_pairs(int rows, int cols, bool precise) {
   const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;
   return !precise && p >= 512 && 2ll * q >= 3ll * p;
@@ -620,7 +634,9 @@ bool in_squares(int rows, int cols, bool precise) {
 }
 
 // All iterations of up to MAX_GROUPS groups that go alike.
-ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon::Target* targets, const float* coefficients, int iterations, cudaStream_t st) {
+ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon::Target* targets, const Coefficients& list, cudaStream_t st) {
+  const float* coefficients = list.k;
+  const int iterations = list.iterations;
   const bool precise = groups[0]->precise;
   muon::Product q[muon::MAX_GROUPS];
   // one launch: `fill` says what it is for each group
@@ -649,7 +665,7 @@ ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon
   for (int i = 0; i < n; ++i) groups[i]->at = 0;
   for (int it = 0; it < iterations;) {
     const float *k = coefficients ? coefficients + 3 * it : kStandard, *k2 = coefficients ? k + 3 : kStandard;
-    const bool pair = groups[0]->paired && it + 2 <= iterations;
+    const bool pair = groups[0]->paired && list.pair[it];
     if (groups[0]->fused) {                                            // S and P
       muon::Gram squares[muon::MAX_GROUPS];
       for (int i = 0; i < n; ++i) {
@@ -774,8 +790,7 @@ ffsplit_status run_first(ffsplit_ctx* ctx, const muon::Entry* entries, int n, in
   return check_cuda(ctx, e, "muon::prepare_kernel launch");
 }
 
-ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, float beta, int nesterov, const float* coefficients,
-                            int iterations, cudaStream_t st) {
+ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, float beta, int nesterov, const Coefficients& list, cudaStream_t st) {
   char* ws = ctx->ws + kCtrlBytes;
   double* partial = reinterpret_cast<double*>(ws);
   muon::Target* target = reinterpret_cast<muon::Target*>(ws + sizeof(double) * muon::MAX_TENSORS * muon::MAX_PARTS);
@@ -783,9 +798,9 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
   int thin = 0;
   for (int i = 0; i < n; ++i) thin += is_thin(t[i].rows, t[i].cols) ? 1 : 0;
   if (thin > 0) {
-    const ffsplit_status s = thin <= 4    ? run_thin<4>(ctx, t, n, beta, nesterov, coefficients, iterations, at, st)
-                             : thin <= 32 ? run_thin<32>(ctx, t, n, beta, nesterov, coefficients, iterations, at, st)
-                                          : run_thin<muon::MAX_TENSORS>(ctx, t, n, beta, nesterov, coefficients, iterations, at, st);
+    const ffsplit_status s = thin <= 4    ? run_thin<4>(ctx, t, n, beta, nesterov, list.k, list.iterations, at, st)
+                             : thin <= 32 ? run_thin<32>(ctx, t, n, beta, nesterov, list.k, list.iterations, at, st)
+                                          : run_thin<muon::MAX_TENSORS>(ctx, t, n, beta, nesterov, list.k, list.iterations, at, st);
     if (s != FFSPLIT_OK) return s;
     for (int i = 0; i < n; ++i)
       if (is_thin(t[i].rows, t[i].cols)) at += matrix_bytes(t[i].rows, t[i].cols, t[i].grad_dtype == FFSPLIT_F32);
@@ -857,7 +872,7 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
     for (int gi = 0; gi <= n_groups; ++gi) {
       if (gi < n_groups && (groups[gi].precise ? 0 : groups[gi].paired ? 1 : groups[gi].fused ? 2 : 3) == kind) some[m++] = &groups[gi];
       if (m == muon::MAX_GROUPS || (gi == n_groups && m > 0)) {
-        const ffsplit_status s = iterate(ctx, some, m, target, coefficients, iterations, st);
+        const ffsplit_status s = iterate(ctx, some, m, target, list, st);
         if (s != FFSPLIT_OK) return s;
         m = 0;
       }
@@ -894,8 +909,12 @@ ffsplit_status ffsplit_muon_step(ffsplit_ctx* ctx, const ffsplit_muon_tensor* te
   if ((s = check_list(ctx, tensors, count)) != FFSPLIT_OK) return s;
   if (iterations < 1 || iterations > 16) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "1 to 16 iterations");
   if (!std::isfinite(beta)) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "beta must be finite");
-  if (coefficients && !coefficients_hold(coefficients, iterations))
+  Coefficients list = {coefficients, iterations, {}};
+  if (!coefficients) {
+    for (int i = 0; i + 1 < iterations; ++i) list.pair[i] = true;      // (P is 3.4445 at most)
+  } else if (!coefficients_hold(&list)) {
     return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "coefficients that may carry a singular value above 1.5");
+  }
   for (int i = 0; i < count; ++i) {
     const ffsplit_muon_tensor& t = tensors[i];
     if (!t.grad || !t.out) return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "NULL tensor in the list");
@@ -914,7 +933,7 @@ ffsplit_status ffsplit_muon_step(ffsplit_ctx* ctx, const ffsplit_muon_tensor* te
   for (int at = 0; at < count;) {
     size_t mine;
     const int n = run_length(tensors + at, count - at, &mine);
-    if ((s = run_matrices(ctx, tensors + at, n, beta, nesterov, coefficients, iterations, static_cast<cudaStream_t>(stream))) != FFSPLIT_OK) return s;
+    if ((s = run_matrices(ctx, tensors + at, n, beta, nesterov, list, static_cast<cudaStream_t>(stream))) != FFSPLIT_OK) return s;
     at += n;
   }
   return FFSPLIT_OK;
