@@ -485,7 +485,8 @@ ffsplit_status ffsplit_muon_workspace_size(const ffsplit_muon_tensor* tensors, i
 
 /* One step for every matrix of the list (a host array, read before the call returns).  coefficients: host
  * [iterations][3], or NULL for iterations times (3.4445, -4.7750, 2.0315); 1 <= iterations <= 16.  Coefficients that
- * can carry a singular value in [0, 1] above 1.5, or that are larger than 64, are refused (INVALID_ARG).
+ * can carry a singular value in [0, 1] above 1.5, that are larger than 64, or that carry all of them below 2^-10 (but not
+ * to zero) before another iteration, are refused (INVALID_ARG).
  * Tensors are aligned to their element size (no 16-byte rule); outputs may be the inputs they replace and overlap
  * nothing else.  Matrices of one shape are worked on together: give one list rather than many.
  * A matrix whose U (or its norm, in fp32) is not finite is left as it is, its momentum too (out = NaN where weight is NULL), and

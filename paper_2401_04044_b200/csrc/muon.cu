@@ -585,8 +585,9 @@ struct Coefficients {
   bool pair[16];                        // iterations i and i + 1 may be taken as one
 };
 
-// Whether the iteration keeps singular values of [0, 1] below 1.5 and P = a I + b S + c S^2 below 200; and which iterations
-// keep P2 P below 200 together with the one after them (each may be steep where the other one shrinks).
+// Whether the iteration keeps singular values of [0, 1] below 1.5 and P = a I + b S + c S^2 below 200, and does not carry all of
+// them below 2^-10 and on from there (X would leave what its two planes hold; zeros stay zeros); and which iterations keep
+// P2 P below 200 together with the one after them (each may be steep where the other one shrinks).
 bool coefficients_hold(Coefficients* list) {
   const auto polynomial = [](const float* c, double s) { return c[0] + s * s * (c[1] + s * s * c[2]); };
   const float* c = list->k;
@@ -601,7 +602,7 @@ bool coefficients_hold(Coefficients* list) {
       if (v > most) most = v;
       if (followed) both = std::fmax(both, std::fabs(p * polynomial(c + 3, v)));
     }
-    if (!(most <= 1.5)) return false;
+    if (!(most <= 1.5) || (followed && most > 0.0 && most < 0x1p-10)) return false;
     list->pair[i] = followed && both <= 200.0;
     top = most;
   }
@@ -913,7 +914,7 @@ ffsplit_status ffsplit_muon_step(ffsplit_ctx* ctx, const ffsplit_muon_tensor* te
   if (!coefficients) {
     for (int i = 0; i + 1 < iterations; ++i) list.pair[i] = true;      // (P is 3.4445 at most)
   } else if (!coefficients_hold(&list)) {
-    return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "coefficients that may carry a singular value above 1.5");
+    return fail(ctx, FFSPLIT_ERR_INVALID_ARG, "coefficients that may carry a singular value above 1.5, or all of them below 2^-10 before the last iteration");
   }
   for (int i = 0; i < count; ++i) {
     const ffsplit_muon_tensor& t = tensors[i];

@@ -43,3 +43,22 @@ def test_pairs_whose_product_is_large(ctx, shape, dtype, triples):
     m = draw(*shape, torch.float32 if dtype == "f32" else torch.bfloat16, seed=7)
     got, = orthogonalize(ctx, [m], coefficients=triples)
     near(got, orthogonal64(m.double().numpy(), triples), TOL[dtype], triples)
+
+
+def test_lists_that_leave_next_to_nothing_before_an_iteration_are_refused(ctx):
+    """1e-15 of the matrix is below what X is held with, and 64^8 of that is not: 0.28."""
+    from paper_2401_04044_b200 import FFSplitError
+    for shape in ((24, 100), (200, 90), (640, 2000)):
+        m = draw(*shape, torch.bfloat16, seed=8)
+        for triples in ([(1e-3, 0.0, 0.0)] * 5 + [(64.0, 0.0, 0.0)] * 8, [(0.9e-3, 0.0, 0.0), (64.0, 0.0, 0.0)]):
+            with pytest.raises(FFSplitError) as e:
+                orthogonalize(ctx, [m], coefficients=triples)
+            assert e.value.code == 1
+        # a list may end small, or with zeros
+        for triples in ([(1e-3, 0.0, 0.0)], [(1.1e-3, 0.0, 0.0), (64.0, 0.0, 0.0)], [(0.0, 0.0, 0.0), (64.0, 0.0, 0.0)]):
+            got, = orthogonalize(ctx, [m], coefficients=triples)
+            ref = orthogonal64(m.double().numpy(), triples)
+            if triples[0][0] == 0.0:
+                assert (got == 0).all()
+            else:
+                near(got, ref, TOL["bf16"], triples)
