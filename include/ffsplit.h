@@ -490,7 +490,8 @@ ffsplit_status ffsplit_muon_workspace_size(const ffsplit_muon_tensor* tensors, i
  * Tensors are aligned to their element size (no 16-byte rule); outputs may be the inputs they replace and overlap
  * nothing else.  Matrices of one shape are worked on together: give one list rather than many.
  * A matrix whose U (or its norm, in fp32) is not finite is left as it is, its momentum too (out = NaN where weight is NULL), and
- * FFSPLIT_ERR_NONFINITE is reported through ffsplit_poll().  A matrix of zeros has X = 0.  Uses the workspace. */
+ * FFSPLIT_ERR_NONFINITE is reported through ffsplit_poll(), with the place in the list of one such matrix as its detail.  A
+ * matrix of zeros has X = 0.  Uses the workspace. */
 ffsplit_status ffsplit_muon_step(ffsplit_ctx* ctx, const ffsplit_muon_tensor* tensors, int32_t count, float beta,
                                  int32_t nesterov, const float* coefficients, int32_t iterations, void* stream);
 

@@ -34,6 +34,7 @@ struct Entry {
   int wide, wide_w;       // every octet of G, M, Mo (of W, out) starts on 16 bytes
   int ld;
   int parts;
+  int place;              // in the caller's list
   float step, decay;
 };
 // (The argument block is copied with every launch and read through the constant cache: a short list gets a short one.)
@@ -163,7 +164,7 @@ __global__ void __launch_bounds__(THREADS) prepare_kernel(const __grid_constant_
     o.keep = finite ? 1.0f - e.decay : 1.0f;
     o.step = e.W ? (finite ? e.step : 0.f) : finite ? -1.0f : __int_as_float(0x7fffffff);
     t.target[which] = o;
-    if (!finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, which, KID_MUON);
+    if (!finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, e.place, KID_MUON);
   }
   int begin, end;
   range_of(e, part, &begin, &end);
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(SOLVE_THREADS) thin_solve_kernel(const __grid_
   // what is not finite leaves here as NaN: the last kernel leaves such a matrix alone
   for (int i = threadIdx.x; i < p * p; i += SOLVE_THREADS)
     t.Q[which][i] = finite ? Q[i / p][i % p] * inv : __longlong_as_double(0x7fffffffffffffffll);
-  if (threadIdx.x == 0 && !finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, which, KID_MUON);
+  if (threadIdx.x == 0 && !finite) record_status(t.status, FFSPLIT_ERR_NONFINITE, e.place, KID_MUON);
 }
 
 // W' = keep W - step Q U for every chunk, and M'.  A warp to every eighth eight columns.
@@ -710,7 +711,7 @@ ffsplit_status iterate(ffsplit_ctx* ctx, Group* const* groups, int n, const muon
 }
 
 // What every kernel needs of a matrix.
-muon::Entry entry_for(const ffsplit_muon_tensor& s) {
+muon::Entry entry_for(const ffsplit_muon_tensor& s, int place) {
   muon::Entry e;
   std::memset(&e, 0, sizeof(e));
   e.G = s.grad; e.M = s.momentum; e.Mo = s.momentum_out; e.W = s.weight; e.out = s.out;
@@ -718,13 +719,13 @@ muon::Entry entry_for(const ffsplit_muon_tensor& s) {
   e.g_f32 = s.grad_dtype == FFSPLIT_F32; e.w_f32 = s.weight_dtype == FFSPLIT_F32;
   e.wide = s.cols % 8 == 0 && aligned16(s.grad) && aligned16(s.momentum) && aligned16(s.momentum_out);
   e.wide_w = s.cols % 8 == 0 && aligned16(s.weight) && aligned16(s.out);
-  e.step = s.step; e.decay = s.decay;
+  e.place = place; e.step = s.step; e.decay = s.decay;
   return e;
 }
 
-// The thin matrices among t: three launches.
+// The thin matrices among t, which begins at place `first` of the caller's list: three launches.
 template <int CAP>
-ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, float beta, int nesterov, const float* coefficients, int iterations,
+ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int first, int n, float beta, int nesterov, const float* coefficients, int iterations,
                         char* at, cudaStream_t st) {
   muon::ThinTable<CAP> tab;
   std::memset(&tab, 0, sizeof(tab));
@@ -737,7 +738,7 @@ ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, f
     if (!is_thin(s.rows, s.cols)) continue;
     const int p = s.rows < s.cols ? s.rows : s.cols;
     muon::Entry& e = tab.t[tab.n];
-    e = entry_for(s);
+    e = entry_for(s, first + i);
     e.parts = thin_parts(s.rows, s.cols);
     tab.S[tab.n] = reinterpret_cast<double*>(at);
     tab.Q[tab.n] = tab.S[tab.n] + static_cast<size_t>(e.parts) * p * p;
@@ -791,7 +792,7 @@ ffsplit_status run_first(ffsplit_ctx* ctx, const muon::Entry* entries, int n, in
   return check_cuda(ctx, e, "muon::prepare_kernel launch");
 }
 
-ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int n, float beta, int nesterov, const Coefficients& list, cudaStream_t st) {
+ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int first, int n, float beta, int nesterov, const Coefficients& list, cudaStream_t st) {
   char* ws = ctx->ws + kCtrlBytes;
   double* partial = reinterpret_cast<double*>(ws);
   muon::Target* target = reinterpret_cast<muon::Target*>(ws + sizeof(double) * muon::MAX_TENSORS * muon::MAX_PARTS);
@@ -799,9 +800,9 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
   int thin = 0;
   for (int i = 0; i < n; ++i) thin += is_thin(t[i].rows, t[i].cols) ? 1 : 0;
   if (thin > 0) {
-    const ffsplit_status s = thin <= 4    ? run_thin<4>(ctx, t, n, beta, nesterov, list.k, list.iterations, at, st)
-                             : thin <= 32 ? run_thin<32>(ctx, t, n, beta, nesterov, list.k, list.iterations, at, st)
-                                          : run_thin<muon::MAX_TENSORS>(ctx, t, n, beta, nesterov, list.k, list.iterations, at, st);
+    const ffsplit_status s = thin <= 4    ? run_thin<4>(ctx, t, first, n, beta, nesterov, list.k, list.iterations, at, st)
+                             : thin <= 32 ? run_thin<32>(ctx, t, first, n, beta, nesterov, list.k, list.iterations, at, st)
+                                          : run_thin<muon::MAX_TENSORS>(ctx, t, first, n, beta, nesterov, list.k, list.iterations, at, st);
     if (s != FFSPLIT_OK) return s;
     for (int i = 0; i < n; ++i)
       if (is_thin(t[i].rows, t[i].cols)) at += matrix_bytes(t[i].rows, t[i].cols, t[i].grad_dtype == FFSPLIT_F32);
@@ -851,7 +852,7 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
     for (int j = 0; j < g.count; ++j, ++k) {
       const ffsplit_muon_tensor& s = t[order[k]];
       muon::Entry& e = entries[k];
-      e = entry_for(s);
+      e = entry_for(s, first + order[k]);
       e.ld = g.X[0].ld;
       e.X = g.X[0].p + j * g.X[0].each;
       e.X_low = g.X[0].low + j * g.X[0].low_each;
@@ -863,10 +864,10 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
       if (e.parts > blocks) blocks = e.parts;
     }
   }
-  const ffsplit_status first = placed <= 4    ? run_first<4>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st)
-                               : placed <= 32 ? run_first<32>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st)
-                                              : run_first<muon::MAX_TENSORS>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st);
-  if (first != FFSPLIT_OK) return first;
+  const ffsplit_status rc = placed <= 4    ? run_first<4>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st)
+                            : placed <= 32 ? run_first<32>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st)
+                                           : run_first<muon::MAX_TENSORS>(ctx, entries, placed, blocks, beta, nesterov, partial, target, st);
+  if (rc != FFSPLIT_OK) return rc;
   for (int kind = 0; kind < 4; ++kind) {      // precise, in pairs, in squares, none of these: groups of one kind go together
     Group* some[muon::MAX_GROUPS];
     int m = 0;
@@ -934,7 +935,7 @@ ffsplit_status ffsplit_muon_step(ffsplit_ctx* ctx, const ffsplit_muon_tensor* te
   for (int at = 0; at < count;) {
     size_t mine;
     const int n = run_length(tensors + at, count - at, &mine);
-    if ((s = run_matrices(ctx, tensors + at, n, beta, nesterov, list, static_cast<cudaStream_t>(stream))) != FFSPLIT_OK) return s;
+    if ((s = run_matrices(ctx, tensors + at, at, n, beta, nesterov, list, static_cast<cudaStream_t>(stream))) != FFSPLIT_OK) return s;
     at += n;
   }
   return FFSPLIT_OK;

@@ -36,3 +36,19 @@ def test_few_thin_matrices_again_and_again(ctx, rows, cols, dtype):
         ctx.poll()
         assert all(torch.equal(a, b) for a, b in zip(outs, many))
     near(many[3], orthogonal64(ms[3].double().numpy()), TOL[dtype])
+
+
+@pytest.mark.parametrize("broken", [0, 1, 2, 4, 5, 200, 299])
+def test_a_report_names_the_matrix_by_its_place_in_the_list(ctx, broken):
+    """Thin and other matrices, several shapes, and more of them than one run takes."""
+    from paper_2401_04044_b200 import FFSplitError
+    shapes = [(300, 200), (16, 40), (130, 260), (300, 200), (40, 16), (70, 71)] + [(9, 11), (66, 67), (12, 8)] * 98
+    g = [torch.randn(*s, device="cuda") for s in shapes]
+    g[broken][-1, -1] = float("nan")
+    lst = ctx.orthogonal_list(g, [torch.empty_like(t) for t in g])
+    ctx.ensure_workspace(ctx.muon_workspace_size(lst))
+    ctx.orthogonalize(lst)
+    with pytest.raises(FFSplitError, match=rf"\(detail {broken}, ") as e:
+        ctx.poll()
+    assert e.value.code == 6
+    ctx.poll()
