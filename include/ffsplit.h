@@ -534,7 +534,8 @@ typedef struct {
 } ffsplit_adapter_grads;
 
 /* dY dev [T, out].  W and base: as above, for dX (base dev [T, in], may be dX); neither is looked at where dX is not
- * wanted.  No gradient may overlap another or an input (but base).  Sums over tokens are taken in a fixed order. */
+ * wanted.  No gradient may overlap another or an input (but base).  Sums are taken in a fixed order: same inputs give the
+ * same bits, whichever gradients are asked for. */
 ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W,
                                         const void* base, const ffsplit_adapters* adapters, const void* X, int64_t T,
                                         const void* dY, const ffsplit_adapter_grads* grads, void* stream);

@@ -762,7 +762,7 @@ ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projectio
   if ((s = c.prepare(extended ? c.L.most : 0, adapters->B, static_cast<long long>(c.a.r) * c.p.out)) != FFSPLIT_OK) return s;
   if (c.tc) {
     const adapter::Shrink job = {c.X, c.A, c.tiles(c.L.P), c.p.in, extended ? 1 : 0};
-    if ((s = adapter::launch_shrink_tc(ctx, &job, 1, c.sorted, c.a.r, c.a.scale, c.st)) != FFSPLIT_OK) return s;
+    if ((s = adapter::launch_shrink_tc(ctx, &job, 1, 1, c.sorted, c.a.r, c.a.scale, c.st)) != FFSPLIT_OK) return s;
   } else {
     adapter::ShrinkArgs sh;
     std::memset(&sh, 0, sizeof(sh));
@@ -802,7 +802,7 @@ ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projecti
     adapter::Shrink jobs[2];
     if (dX || dA) jobs[n++] = {c.dY, c.B, c.tiles(c.L.D), c.p.out, extended ? 1 : 0};
     if (dB) jobs[n++] = {c.X, c.A, c.tiles(c.L.P), c.p.in, 0};
-    if ((s = adapter::launch_shrink_tc(ctx, jobs, n, c.sorted, c.a.r, c.a.scale, c.st)) != FFSPLIT_OK) return s;
+    if ((s = adapter::launch_shrink_tc(ctx, jobs, n, 2, c.sorted, c.a.r, c.a.scale, c.st)) != FFSPLIT_OK) return s;
   } else {
     adapter::ShrinkArgs sh;
     std::memset(&sh, 0, sizeof(sh));

@@ -42,7 +42,7 @@ ffsplit_status launch_sort(ffsplit_ctx* ctx, const int* index, const Sorted& s, 
 ffsplit_status launch_check(ffsplit_ctx* ctx, const void* F, long long each, const Sorted& s, cudaStream_t st);
 
 // P = scale_i V F_i for every tile: [tiles][128][pitch] bf16, zero rows behind the last token; and into the entries of the
-// extension, where the tokens have one.  Up to two at once.
+// extension, where the tokens have one.  Up to two at once; most_jobs: as many as calls of this kind may have.
 struct Shrink {
   tg::Matrix V;             // [T, K]
   Factor F;
@@ -50,7 +50,7 @@ struct Shrink {
   int K;
   int extends;
 };
-ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, const Sorted& s, int r, const float* scale, cudaStream_t st);
+ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, int most_jobs, const Sorted& s, int r, const float* scale, cudaStream_t st);
 
 // Y[t] = base[t] + P F_i: [T, N], pitch N.  rest: only the tokens that the extension leaves out.  late: base comes from the launches
 // behind the shrink; what else is read here is complete when they start to leave room for this kernel.

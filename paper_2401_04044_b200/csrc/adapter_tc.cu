@@ -329,6 +329,7 @@ struct ShrinkDev {
   CUtensorMap V, V_box, V_tile, F;
   __nv_bfloat16* P;
   int kb, f_mn;               // f_mn: the rank runs along memory
+  int ranges;                 // of K: no more than a cluster has CTAs
   int extends;
 };
 struct ShrinkParams {
@@ -349,7 +350,7 @@ constexpr int MAX_RANGES = 8;
 __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_constant__ ShrinkParams p) {
   extern __shared__ uint8_t raw[];
   const ShrinkDev& job = p.job[blockIdx.z];
-  const int ranges = gridDim.x, range = blockIdx.x;         // a cluster spans x
+  const int share = gridDim.x, range = blockIdx.x;          // a cluster spans x; behind the last range there is nothing to add up
   if (threadIdx.x == 0) {
     ptx::prefetch_tmap(&job.V_tile);
     ptx::prefetch_tmap(&job.F);
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int per = (job.kb + ranges - 1) / ranges, k0 = range * per, k1 = k0 + per < job.kb ? k0 + per : job.kb;
+  const int per = (job.kb + job.ranges - 1) / job.ranges, k0 = range * per, k1 = k0 + per < job.kb ? k0 + per : job.kb;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   float* part = reinterpret_cast<float*>(smem);
   const int part_pitch = p.cols + 4;
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
   const int pairs = p.cols / 2;
   __nv_bfloat16* P = job.P + static_cast<long long>(blockIdx.y) * TOKENS * p.pitch;
   const uint32_t part0 = ptx::smem_u32(part);
-  for (int e = range * TC_THREADS + threadIdx.x; e < TOKENS * pairs; e += ranges * TC_THREADS) {
+  for (int e = range * TC_THREADS + threadIdx.x; e < TOKENS * pairs; e += share * TC_THREADS) {
     const int row = e / pairs, c = (e - row * pairs) * 2;
     float x = 0.f, y = 0.f;
     if (row < tile.rows) {
@@ -472,7 +473,7 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
 #pragma unroll
       for (int k = 0; k < MAX_RANGES; ++k) {
         a[k] = b[k] = 0.f;
-        if (k < ranges) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(a[k]), "=f"(b[k]) : "r"(ptx::map_to_cta(part0 + (row * part_pitch + c) * 4, k)));
+        if (k < job.ranges) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(a[k]), "=f"(b[k]) : "r"(ptx::map_to_cta(part0 + (row * part_pitch + c) * 4, k)));
       }
 #pragma unroll
       for (int k = 0; k < MAX_RANGES; ++k) { x += a[k]; y += b[k]; }
@@ -869,13 +870,14 @@ ffsplit_status launch_check(ffsplit_ctx* ctx, const void* F, long long each, con
   return check_cuda(ctx, e, "adapter::check_kernel launch");
 }
 
-ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, const Sorted& s, int r, const float* scale, cudaStream_t st) {
+ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, int most_jobs, const Sorted& s, int r, const float* scale, cudaStream_t st) {
   ffsplit_status rc = set_up(ctx);
   if (rc != FFSPLIT_OK) return rc;
   ShrinkParams p;
   std::memset(&p, 0, sizeof(p));
   p.s = s; p.scale = scale; p.r = r; p.cols = round_up(r, 16); p.pitch = rank_pitch(r); p.stage = stage_bytes(r); p.status = ctx->status();
-  int kb = 1;
+  const long long tiles = tile_bound(s.T, s.n);
+  int share = 1;
   for (int i = 0; i < n; ++i) {
     ShrinkDev& d = p.job[i];
     if ((rc = encode_rows(ctx, jobs[i].V, TOKENS, &d.V, &d.V_box, &d.V_tile)) != FFSPLIT_OK) return rc;
@@ -884,14 +886,14 @@ ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, con
     d.P = jobs[i].P;
     d.extends = jobs[i].extends;
     d.kb = (jobs[i].K + BLOCK_K - 1) / BLOCK_K;
-    if (d.kb > kb) kb = d.kb;
+    // Ranges of K: two CTAs to an SM, four k-blocks each at least (the cluster's exchange takes about as long).  By what is the
+    // same whichever gradients are asked for (jobs a call may have, not those it has), so that they do not change each other's bits.
+    d.ranges = 1;
+    while (d.ranges < MAX_RANGES && d.ranges * tiles * most_jobs < ctx->num_sms && 8 * d.ranges <= d.kb) d.ranges *= 2;
+    if (d.ranges > share) share = d.ranges;
   }
-  // ranges of K: two CTAs to an SM, four k-blocks each at least (the cluster's exchange takes about as long)
-  const long long tiles = tile_bound(s.T, s.n);
-  int ranges = 1;
-  while (ranges < MAX_RANGES && ranges * tiles * n < ctx->num_sms && 8 * ranges <= kb) ranges *= 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ranges, static_cast<unsigned>(tiles), n);
+  cfg.gridDim = dim3(share, static_cast<unsigned>(tiles), n);
   cfg.blockDim = dim3(TC_THREADS);
   cfg.dynamicSmemBytes = smem_of(SHRINK_STAGES, r);
   cfg.stream = st;
@@ -899,7 +901,7 @@ ffsplit_status launch_shrink_tc(ffsplit_ctx* ctx, const Shrink* jobs, int n, con
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = ranges;
+  attr[1].val.clusterDim.x = share;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
