@@ -478,7 +478,9 @@ __global__ void __launch_bounds__(TC_THREADS) shrink_tc_kernel(const __grid_cons
 #pragma unroll
       for (int k = 0; k < MAX_RANGES; ++k) { x += a[k]; y += b[k]; }
     }
-    const uint32_t pair = bf16_pair(scale * x, scale * y);
+    // (zeros behind the rank, where an infinity in the row has met what the factor is filled up with: NaN, which the second
+    // product would carry into every column)
+    const uint32_t pair = bf16_pair(c < p.r ? scale * x : 0.f, c + 1 < p.r ? scale * y : 0.f);
     *reinterpret_cast<uint32_t*>(P + static_cast<long long>(row) * p.pitch + c) = pair;
     if (job.extends && row < tile.rows) {
       const int token = __ldcg(p.s.order + tile.first + row), slot = __ldcg(p.s.slot + token);
