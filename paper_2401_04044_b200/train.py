@@ -117,7 +117,7 @@ class Muon(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         for group in self.param_groups:
-            W, G, M, rates = [], [], [], []
+            W, G, M, updated = [], [], [], []
             for p in group["params"]:
                 if p.grad is None:
                     continue
@@ -127,12 +127,15 @@ class Muon(torch.optim.Optimizer):
                 W += _matrices(p)
                 G += _matrices(p.grad.contiguous())
                 M += _matrices(state["momentum"])
+                updated.append(p)
             if not W:
                 continue
             rates = [group["lr"] * 0.2 * math.sqrt(max(w.shape)) for w in W]
             tensors = MuonList(self.lib.device, G, W, M, rates, group["lr"] * group["weight_decay"])
             self.lib.ensure_workspace(self.lib.muon_workspace_size(tensors))
             self.lib.muon_step(tensors, group["momentum"], group["nesterov"], group["coefficients"], group["iterations"])
+            for p in updated:      # (the library writes by address: a graph that still holds a parameter must not go on with its new value)
+                torch.autograd.graph.increment_version(p)
         return loss
 
 
