@@ -86,8 +86,8 @@ def _matrices(t: torch.Tensor):
 class Muon(torch.optim.Optimizer):
     """Momentum, orthogonalised, as the update of matrices (ffsplit_muon_step): W <- (1 - lr weight_decay) W - lr 0.2
     sqrt(max(rows, cols)) X, where X is the orthogonal factor of the momentum and 0.2 sqrt(...) makes its elements as large as
-    0.2 in the mean.  Parameters are float32 or bfloat16 with two dimensions, or more (a matrix to each leading index);
-    momentum is float32.  All matrices of a group are one call on the current stream; a gradient that is not finite leaves its
+    0.2 in the mean.  Parameters are contiguous, float32 or bfloat16, with two dimensions, or more (a matrix to each leading
+    index); momentum is float32.  All matrices of a group are one call on the current stream; a gradient that is not finite leaves its
     matrix alone and is reported by lib.poll().  Workspace and streams: as for ffn()."""
 
     def __init__(self, lib: Context, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
@@ -98,9 +98,10 @@ class Muon(torch.optim.Optimizer):
 
     def add_param_group(self, param_group):
         super().add_param_group(param_group)
-        if any(p.dim() < 2 or p.dtype not in (torch.float32, torch.bfloat16) for p in self.param_groups[-1]["params"]):
+        fits = lambda p: p.dim() >= 2 and p.dtype in (torch.float32, torch.bfloat16) and p.numel() > 0 and p.is_contiguous()  # noqa: E731
+        if not all(fits(p) for p in self.param_groups[-1]["params"]):
             self.param_groups.pop()
-            raise FFSplitError(2, "Muon", "parameters are float32 or bfloat16 matrices, or stacks of them")
+            raise FFSplitError(2, "Muon", "parameters are contiguous float32 or bfloat16 matrices, or stacks of them, and not empty")
 
     def load_state_dict(self, state_dict):
         super().load_state_dict(state_dict)
@@ -116,25 +117,25 @@ class Muon(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        steps = []      # all of them are looked at before one is taken
         for group in self.param_groups:
-            W, G, M, updated = [], [], [], []
-            for p in group["params"]:
-                if p.grad is None:
-                    continue
-                state = self.state[p]
-                if "momentum" not in state:
-                    state["momentum"] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
-                W += _matrices(p)
-                G += _matrices(p.grad.contiguous())
-                M += _matrices(state["momentum"])
-                updated.append(p)
-            if not W:
+            params = [p for p in group["params"] if p.grad is not None]
+            if not params:
                 continue
+            for p in params:
+                if "momentum" not in self.state[p]:
+                    self.state[p]["momentum"] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+            each = lambda tensors: [m for t in tensors for m in _matrices(t)]  # noqa: E731
+            W = each(params)
             rates = [group["lr"] * 0.2 * math.sqrt(max(w.shape)) for w in W]
-            tensors = MuonList(self.lib.device, G, W, M, rates, group["lr"] * group["weight_decay"])
-            self.lib.ensure_workspace(self.lib.muon_workspace_size(tensors))
+            tensors = MuonList(self.lib.device, each(p.grad.contiguous() for p in params), W, each(self.state[p]["momentum"] for p in params),
+                               rates, group["lr"] * group["weight_decay"])
+            steps.append((group, params, tensors))
+        if steps:
+            self.lib.ensure_workspace(max(self.lib.muon_workspace_size(tensors) for _, _, tensors in steps))
+        for group, params, tensors in steps:
             self.lib.muon_step(tensors, group["momentum"], group["nesterov"], group["coefficients"], group["iterations"])
-            for p in updated:      # (the library writes by address: a graph that still holds a parameter must not go on with its new value)
+            for p in params:      # (the library writes by address: a graph that still holds a parameter must not go on with its new value)
                 torch.autograd.graph.increment_version(p)
         return loss
 

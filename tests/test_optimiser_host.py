@@ -42,3 +42,40 @@ def test_a_graph_from_before_a_step_is_refused():
             kept.backward()
     (other * other).sum().backward()      # (no gradient until now: left as it was)
     assert len(lib.lists) == 2 and [t.count for t in lib.lists] == [1, 3]
+
+
+def test_parameters_that_cannot_be_stepped_are_refused_when_they_are_added():
+    from paper_2401_04044_b200 import FFSplitError
+    from paper_2401_04044_b200.train import Muon
+    bad = [torch.randn(6, 4).t().requires_grad_(), torch.randn(2, 5, 3).transpose(1, 2).requires_grad_(), torch.randn(0, 4).requires_grad_(),
+           torch.randn(3, 0, 4).requires_grad_()]
+    opt = Muon(Library(), [parameter(4, 6)])
+    for p in bad:
+        with pytest.raises(FFSplitError):
+            Muon(Library(), [p])
+        with pytest.raises(FFSplitError):
+            opt.add_param_group({"params": [p]})
+    assert len(opt.param_groups) == 1
+
+
+def test_no_group_is_updated_where_a_later_one_cannot_be():
+    from paper_2401_04044_b200.train import Muon
+    lib, groups = Library(), [[parameter(4, 6)], [parameter(5, 7), parameter(2, 3, 4)], [parameter(9, 2)]]
+    opt = Muon(lib, [{"params": g} for g in groups])
+    for p in sum(groups, []):
+        p.grad = torch.ones_like(p)
+    opt.step()
+    assert [t.count for t in lib.lists] == [1, 3, 1]
+    for i, broken in ((1, torch.randn(7, 5).t()), (1, torch.randn(5, 7, dtype=torch.float64)), (2, torch.randn(2, 9).t())):
+        p = groups[i][0]
+        whole, p.grad = p.data, None
+        p.data = broken
+        p.grad = torch.ones(broken.shape, dtype=broken.dtype)
+        with pytest.raises(RuntimeError):
+            opt.step()
+        assert len(lib.lists) == 3
+        p.grad = None
+        p.data = whole
+        p.grad = torch.ones_like(p)
+    opt.step()
+    assert len(lib.lists) == 6
