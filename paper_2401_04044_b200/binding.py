@@ -222,6 +222,9 @@ class MuonList:
         rates = [list(v) if isinstance(v, (list, tuple)) else [v] * n for v in (step, decay)]
         if any(len(v) != n for v in (self.weights, self.momenta, self.out, self.out_momenta, *rates)):
             raise FFSplitError(2, "muon_list", "lists must be of the same length")
+        written = [v.data_ptr() for v in self.out + self.out_momenta if v is not None]
+        if len(set(written)) < len(written):
+            raise FFSplitError(1, "muon_list", "two matrices of one call write to the same memory")
         self.count = n
         self.array = (MuonTensor * max(1, n))()
         for e, g, w, m, o, mo, s, d in zip(self.array, self.grads, self.weights, self.momenta, self.out, self.out_momenta, *rates):

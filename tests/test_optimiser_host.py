@@ -79,3 +79,27 @@ def test_no_group_is_updated_where_a_later_one_cannot_be():
         p.grad = torch.ones_like(p)
     opt.step()
     assert len(lib.lists) == 6
+
+
+def test_a_matrix_that_is_named_twice_is_refused():
+    """Two updates of one matrix in one call would run at the same time."""
+    import warnings
+    from paper_2401_04044_b200 import FFSplitError, MuonList
+    from paper_2401_04044_b200.train import Muon
+    g, w, m = (torch.randn(4, 6) for _ in range(3))
+    other = [torch.randn(4, 6) for _ in range(4)]
+    for kw in (dict(grads=[g, g], weights=[w, w]), dict(grads=[g, g], weights=[w, other[0]], momenta=[m, m]),
+               dict(grads=[g, g], out=[w, w]), dict(grads=[g, g], weights=[w, other[0]], momenta=[m, other[1]], out=[other[2], other[3]], out_momenta=[m, other[3]])):
+        with pytest.raises(FFSplitError) as e:
+            MuonList(-1, **kw)
+        assert e.value.code == 1
+    # what is only read may be named again
+    assert MuonList(-1, [g, g], [w, w], [m, m], out=other[:2], out_momenta=other[2:]).count == 2
+    lib, p = Library(), parameter(4, 6)
+    p.grad = torch.ones_like(p)
+    with warnings.catch_warnings():
+        warnings.simplefilter("ignore")      # (torch's own, which is to become an error)
+        opt = Muon(lib, [p, p])
+    with pytest.raises(FFSplitError):
+        opt.step()
+    assert not lib.lists
