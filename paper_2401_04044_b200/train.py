@@ -75,6 +75,8 @@ def clip_grad_norm_(lib: Context, parameters: Union[torch.Tensor, Iterable[torch
         norm = torch.empty(1, dtype=torch.float32, device=f"cuda:{lib.device}")
     lib.ensure_workspace(lib.grad_workspace_size(len(grads)))
     lib.clip_grads(GradList(lib.device, grads), max_norm, norm)
+    for g in grads:      # (written by address: see Muon.step)
+        torch.autograd.graph.increment_version(g)
     return norm
 
 

@@ -103,3 +103,24 @@ def test_a_matrix_that_is_named_twice_is_refused():
     with pytest.raises(FFSplitError):
         opt.step()
     assert not lib.lists
+
+
+def test_clipping_counts_as_a_change_of_the_gradients():
+    from paper_2401_04044_b200.train import clip_grad_norm_
+
+    class Clipping(Library):
+        grad_workspace_size = staticmethod(lambda count: 0)
+
+        def clip_grads(self, grads, max_norm, norm):
+            self.lists.append(grads)
+
+    lib, params, norm = Clipping(), [parameter(4, 6), parameter(3), parameter(2)], torch.zeros(1)
+    for p in params[:2]:
+        p.grad = torch.ones_like(p)
+    x = torch.ones(4, 6, requires_grad=True)
+    kept = (x * params[0].grad).sum()
+    before = [p.grad._version for p in params[:2]]
+    clip_grad_norm_(lib, params, 1.0, norm)
+    assert len(lib.lists) == 1 and all(p.grad._version > v for p, v in zip(params, before))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        kept.backward()
