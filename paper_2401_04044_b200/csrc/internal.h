@@ -274,8 +274,11 @@ ffsplit_status decode_layer_launch(ffsplit_ctx* ctx, const DecodeLayerPlan* plan
                                    cudaStream_t st);
 
 // Launch with programmatic stream serialisation: the kernel may be scheduled while the kernel before it in
-// the stream is still running.  Every kernel launched this way executes `griddepcontrol.wait` before its
-// first global-memory access (pdl_wait() below), so only its launch latency overlaps.
+// the stream is still running.  Every kernel launched this way executes `griddepcontrol.wait` (pdl_wait() below),
+// so its end is the end of all kernels before it.  Most do so before their first global-memory access, and only their
+// launch latency overlaps.  Some wait later (train_gemm.cu: `early`, `apart`; train.cu, adapter.cu, adapter_tc.cu: `apart`,
+// `late`): what they touch before is neither written nor, where they write, read by the kernel before, and was complete
+// when that one let them start: the kernels they are launched behind do so only after their own wait.
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
                               Args&&... args) {
