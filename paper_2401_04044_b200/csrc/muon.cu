@@ -544,6 +544,12 @@ int thin_parts(int rows, int cols) {      // (parts are whole chunks)
   const int chunks = (q + chunk - 1) / chunk, most = chunks < muon::THIN_PARTS ? chunks : muon::THIN_PARTS, per = (chunks + most - 1) / most;
   return (chunks + per - 1) / per;
 }
+// Whether products take both planes of their operands and sums leave tensor memory every few k-blocks: fp32 gradients, and matrices
+// with a side above 2^18.  Tensor cores cut what they add at the last place of the running sum; the square's diagonal is a sum of
+// terms of one sign, which loses n 2^-28 or so of n terms: with bf16 gradients 65 x 2^17 is 1.6e-3 off, 2^18 2.1e-3, 2^19 3.1e-3,
+// 2^20 5.6e-3, 2^22 2.2e-2, and 2^25 terms no longer move the sum at all.
+constexpr int LONG_SIDE = 1 << 18;
+bool is_precise(const ffsplit_muon_tensor& t) { return t.grad_dtype == FFSPLIT_F32 || t.rows > LONG_SIDE || t.cols > LONG_SIDE; }
 bool is_thin(int rows, int cols) { return (rows < cols ? rows : cols) <= muon::THIN; }
 size_t matrix_bytes(int rows, int cols, bool precise) {
   const int p = rows < cols ? rows : cols;
@@ -557,7 +563,7 @@ int run_length(const ffsplit_muon_tensor* t, int count, size_t* bytes) {
   size_t sum = 0;
   int n = 0;
   while (n < count && n < muon::MAX_TENSORS) {
-    const size_t more = matrix_bytes(t[n].rows, t[n].cols, t[n].grad_dtype == FFSPLIT_F32);
+    const size_t more = matrix_bytes(t[n].rows, t[n].cols, is_precise(t[n]));
     if (n > 0 && sum + more > kRunBytes) break;
     sum += more;
     ++n;
@@ -742,7 +748,7 @@ ffsplit_status run_thin(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int firs
     e.parts = thin_parts(s.rows, s.cols);
     tab.S[tab.n] = reinterpret_cast<double*>(at);
     tab.Q[tab.n] = tab.S[tab.n] + static_cast<size_t>(e.parts) * p * p;
-    at += matrix_bytes(s.rows, s.cols, s.grad_dtype == FFSPLIT_F32);
+    at += matrix_bytes(s.rows, s.cols, is_precise(s));
     if (p > most) most = p;
     if (e.parts > blocks) blocks = e.parts;
     ++tab.n;
@@ -805,7 +811,7 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
                                           : run_thin<muon::MAX_TENSORS>(ctx, t, first, n, beta, nesterov, list.k, list.iterations, at, st);
     if (s != FFSPLIT_OK) return s;
     for (int i = 0; i < n; ++i)
-      if (is_thin(t[i].rows, t[i].cols)) at += matrix_bytes(t[i].rows, t[i].cols, t[i].grad_dtype == FFSPLIT_F32);
+      if (is_thin(t[i].rows, t[i].cols)) at += matrix_bytes(t[i].rows, t[i].cols, is_precise(t[i]));
   }
   if (thin == n) return FFSPLIT_OK;
   // matrices of one shape lie one after the other, whatever their place in the list
@@ -826,9 +832,9 @@ ffsplit_status run_matrices(ffsplit_ctx* ctx, const ffsplit_muon_tensor* t, int 
     if (done[i] || is_thin(t[i].rows, t[i].cols)) continue;
     Group& g = groups[n_groups++];
     g.first = placed; g.count = 0; g.rows = t[i].rows; g.cols = t[i].cols;
-    g.precise = t[i].grad_dtype == FFSPLIT_F32;
+    g.precise = is_precise(t[i]);
     for (int j = i; j < n; ++j)
-      if (!done[j] && t[j].rows == g.rows && t[j].cols == g.cols && (t[j].grad_dtype == FFSPLIT_F32) == g.precise) {
+      if (!done[j] && t[j].rows == g.rows && t[j].cols == g.cols && is_precise(t[j]) == g.precise) {
         done[j] = true;
         order[placed++] = j;
         ++g.count;

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_muon import DT, TOL, draw, near, orthogonal64, orthogonalize
+from test_gpu_muon import DT, STANDARD, TOL, draw, near, orthogonal64, orthogonalize
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,45 @@ def test_a_report_names_the_matrix_by_its_place_in_the_list(ctx, broken):
         ctx.poll()
     assert e.value.code == 6
     ctx.poll()
+
+
+@pytest.mark.parametrize("gdt,odt", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("shape", [(24, 100), (200, 90), (90, 1500), (640, 1000), (640, 700)])
+def test_an_orthogonal_factor_of_momentum(ctx, shape, gdt, odt):
+    """Without weights, with momentum that moves on: out = X of U, in either type."""
+    from paper_2401_04044_b200 import MuonList
+    g, m = draw(*shape, DT[gdt], seed=3).cuda(), 4 * draw(*shape, torch.float32, seed=4).cuda()
+    out, moved = torch.empty(*shape, dtype=DT[odt], device="cuda"), torch.empty(*shape, device="cuda")
+    lst = MuonList(0, [g], None, [m], out=[out], out_momenta=[moved])
+    ctx.ensure_workspace(ctx.muon_workspace_size(lst))
+    ctx.muon_step(lst, 0.5)
+    ctx.poll()
+    m64 = 0.5 * m.double() + g.double()
+    near(moved, m64.cpu(), 2.0 ** -22)      # (two operations; near() asks for 8 times that of single elements)
+    near(out, orthogonal64((g.double() + 0.5 * m64).cpu().numpy()), TOL[gdt] + (2.0 ** -8 if odt == "bf16" else 0.0))
+
+
+@pytest.mark.parametrize("rows,cols", [(65, 1 << 18), (65, (1 << 18) + 8), ((1 << 20) + 1, 66), (65, 1 << 22), (520, 1 << 20)])
+def test_long_sums(ctx, rows, cols):
+    """The square's diagonal is a sum of as many terms of one sign as the longer side has, far more than a running sum in the tensor
+    cores can take."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    m = torch.randn(rows, cols, generator=g, device="cuda").bfloat16()
+    out = torch.empty_like(m)
+    lst = ctx.orthogonal_list([m], [out])
+    ctx.ensure_workspace(ctx.muon_workspace_size(lst))
+    ctx.orthogonalize(lst)
+    ctx.poll()
+    x, o = (m, out) if rows <= cols else (m.t(), out.t())
+    gram = torch.zeros(len(x), len(x), dtype=torch.float64, device="cuda")
+    for at in range(0, x.shape[1], 1 << 18):
+        piece = x[:, at:at + (1 << 18)].double()
+        gram += piece @ piece.t()
+    eye = torch.eye(len(x), dtype=torch.float64, device="cuda")
+    norm = gram.trace().sqrt() + 1e-7
+    s, Q = gram / norm ** 2, eye / norm
+    for a, b, c in STANDARD:
+        A = a * eye + b * s + c * (s @ s)
+        Q, s = Q @ A, A @ s @ A
+    for at in (0, x.shape[1] - 4096):
+        near(o[:, at:at + 4096], (Q @ x[:, at:at + 4096].double()).cpu(), TOL["bf16"])
