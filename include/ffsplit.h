@@ -464,9 +464,10 @@ ffsplit_status ffsplit_grad_clip(ffsplit_ctx* ctx, const ffsplit_grad_tensor* te
  * Arithmetic: sums in fp32 and more.  X is kept in 22 bits.  Where the gradient is bf16, the operands of the products are
  * fp16 (11 bits); what is rounded off an operand perturbs X by a factor close to 1, not by a term, so small singular values
  * do not drown in it: X is off by 5e-4 to 3e-3 of its norm.  Where the gradient is fp32, or a side is above 2^18, operands
- * carry 22 bits too: 1e-7 to 2e-6.  (A direction in which the matrix has less than 2^-22 of its norm is filled with what is rounded off X, times up to
- * 3.44^5: 1e-4 of the result for matrices of nearly lower rank.)  Matrices with a side of at most 64 are worked on through
- * their Gram matrix in fp64.  Momentum is fp32 whatever the type of the gradient.
+ * carry 22 bits too: 1e-7 to 5e-6 (plain fp32 products leave 1e-6 to 7e-6), for fp32 matrices with a side of 2^15 and more up
+ * to 1.2e-5.  (A direction in which the matrix has less than 2^-22 of its norm is filled with what is rounded off X, times up
+ * to 3.44^5: 1e-4 of the result for matrices of nearly lower rank.)  These figures are of the standard coefficients.  Matrices
+ * with a side of at most 64 are worked on through their Gram matrix in fp64.  Momentum is fp32 whatever the type of the gradient.
  * Same inputs give the same bits, whatever else is in the list. */
 
 typedef struct {

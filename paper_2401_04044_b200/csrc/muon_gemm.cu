@@ -16,8 +16,7 @@
 // of the result, with bf16 8e-2).  So X has a second plane for the next 11 bits.  a is added to the diagonal of P, so that the
 // tensor cores form a X + P X from the first plane, and the epilogue adds a times the second: 6e-4 to 2e-3, for 2 bytes read and
 // written per element.  precise: the tensor cores take the second planes of all operands (three products of planes, the small
-// ones first), and sums leave them every PROMOTE k-blocks, because their running sums are cut, not rounded (see
-// train_gemm.cu).
+// ones first), and sums leave them every few k-blocks, because their running sums are cut, not rounded (see train_gemm.cu).
 //
 // Every wait is bounded; on expiry the CTA records FFSPLIT_ERR_TIMEOUT, lets its copies and MMAs land and returns.
 #include <cstring>
@@ -49,11 +48,15 @@ template <bool PRECISE> constexpr int FIRST_EPI = PRECISE ? 4 : 2;
 constexpr int START_REGS = 168, ROLE_REGS = 56, EPI_REGS = 224;
 static_assert(ROLE_REGS * 128 + EPI_REGS * 256 <= START_REGS * 384, "a split above what the block starts with waits forever");
 template <bool PRECISE> constexpr int GEMM_THREADS = 32 * (EPI_WARPS<PRECISE> + FIRST_EPI<PRECISE>);
-constexpr int PROMOTE = 4;
+// Every PROMOTE k-blocks, and every one of P = a I + b S + c S S: S S is what a whole P is off by, three times what the other sums'
+// loss comes to (of S itself most is lost again between b S and 2 c S S).  512 x 4096 fp32: 5.4e-6, with four k-blocks there too
+// 1.1e-5; three 1024 x 2752: 725 us, 677.  All sums after one k-block: 4.7e-6 and 855 us.
+constexpr int PROMOTE = 4, PROMOTE_POLYNOMIAL = 1;
 
 struct DevProduct {
   CUtensorMap a, b, c;
   int M, N, kb, count;
+  int promote;                // precise: k-blocks of a part
   int a_mn, b_mn, symmetric;
   int tiles_m, tiles_n, tiles, panel_m;
   int unit0;
@@ -101,10 +104,10 @@ __device__ __forceinline__ Unit find_unit(const Params& p, int u) {
 }
 // precise: k-blocks of a unit are counted over three runs, (low, high), (high, low), (high, high).  End of the part of the
 // sum that begins at `begin`: both small runs are one part.
-__device__ __forceinline__ int part_end(int kb, int begin) {
-  const int small = 2 * kb;
+__device__ __forceinline__ int part_end(const DevProduct& d, int begin) {
+  const int small = 2 * d.kb;
   if (begin < small) return small;
-  return begin + PROMOTE < 3 * kb ? begin + PROMOTE : 3 * kb;
+  return begin + d.promote < 3 * d.kb ? begin + d.promote : 3 * d.kb;
 }
 
 __device__ __forceinline__ float2 half_pair(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
@@ -326,7 +329,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
         const uint32_t a_step = d.a_mn ? 2048 >> 4 : 32 >> 4, b_step = d.b_mn ? 2048 >> 4 : 32 >> 4;
         const int all = (PRECISE ? 3 : 1) * d.kb;
         for (int begin = 0; begin < all && ok; ++tl) {
-          const int end = PRECISE ? part_end(d.kb, begin) : all;
+          const int end = PRECISE ? part_end(d, begin) : all;
           const uint32_t acc = tl & 1, aph = (tl >> 1) & 1;
           ok = __shfl_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aph ^ 1, abort_flag) ? 1 : 0, 0) != 0;
           if (!ok) break;
@@ -403,7 +406,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS<PRECISE
         constexpr int BLOCKS = TILE_N / GROUPS<PRECISE> / 32;             // (the first half of them in narrow tiles)
         float sum[BLOCKS][32];
         for (int begin = 0;; ++tl) {
-          const int end = part_end(d.kb, begin);
+          const int end = part_end(d, begin);
           const bool last = end == 3 * d.kb;
           if (!ptx::mbar_wait(&tfull[tl & 1], (tl >> 1) & 1, abort_flag)) { live = false; break; }
           ptx::tc_fence_after();
@@ -848,6 +851,7 @@ ffsplit_status launch_products(ffsplit_ctx* ctx, bool precise, const Product* pr
     if (!g.target && (s = encode(ctx, g.c, BOX, BOX, planes, &d.c)) != FFSPLIT_OK) return s;
     d.M = g.M; d.N = g.N; d.count = g.c.count;
     d.kb = (g.K + BLOCK_K - 1) / BLOCK_K;
+    d.promote = g.a.p == g.b.p && g.d ? PROMOTE_POLYNOMIAL : PROMOTE;
     d.a_mn = g.a_mn; d.b_mn = g.b_mn; d.symmetric = g.symmetric;
     d.tiles_m = (g.M + TILE_M - 1) / TILE_M;
     d.tiles_n = (g.N + p.tile_n - 1) / p.tile_n;

@@ -94,3 +94,16 @@ def test_long_sums(ctx, rows, cols):
         Q, s = Q @ A, A @ s @ A
     for at in (0, x.shape[1] - 4096):
         near(o[:, at:at + 4096], (Q @ x[:, at:at + 4096].double()).cpu(), TOL["bf16"])
+
+
+@pytest.mark.parametrize("kind", ["gauss", "positive"])
+@pytest.mark.parametrize("rows,cols", [(65, 1024), (256, 1024), (512, 1024), (512, 4096), (4096, 512), (512, 1 << 15), (1024, 2752), (2048, 2048)])
+def test_singular_values_close_together_in_fp32(ctx, rows, cols, kind):
+    """1e-5 in fp32: S is summed in parts of 256 terms of one sign; a term loses half of 2^-24 of the running sum on average, which is
+    half of the part's on average: 256 x 2^-26 = 3.8e-6 of S.  That enters through b s^2 + 2 c s^4, 0.71 where all singular
+    values are near 1 and the result is 0.7: 3.8e-6, and as much again from the iterations before the last one.  Values that are
+    close together do not average this out.  (P's own sums: parts of 64 terms.)"""
+    g = torch.Generator().manual_seed(10)
+    m = torch.randn(rows, cols, generator=g) if kind == "gauss" else torch.rand(rows, cols, generator=g)
+    got, = orthogonalize(ctx, [m])
+    near(got, orthogonal64(m.double().numpy()), TOL["f32"])
