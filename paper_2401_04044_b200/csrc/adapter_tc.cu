@@ -692,10 +692,14 @@ struct GradientParams {
   int r, cols, wide;          // wide: r is a multiple of 8
   int apart;                  // the kernel before was launched behind all that is read here, and does not touch what is written: waited for at the end
   int stage;
+  uint32_t tmem;              // columns: 128, and as many again for the sum of the parts where there may be several
   int* status;
 };
 constexpr int GRADIENT_STAGES = 4;
 constexpr uint32_t GRADIENT_TMEM = 128;
+// An adapter's tokens are summed in parts of so many k-blocks (2^18 tokens), whose sum is rounded.  Tensor cores cut what they add
+// at the last place of the running sum, and where all terms have one sign 2^19 of them lose 3.5e-3 of it, 2^20 6e-3.
+constexpr int GRADIENT_PART = 4096, GRADIENT_EPI_WARPS = 4;
 
 __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_constant__ GradientParams p) {
   extern __shared__ uint8_t raw[];
@@ -707,10 +711,10 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
     ptx::prefetch_tmap(&job.V_tile);
     ptx::prefetch_tmap(&job.P);
   }
-  const Frame f = frame_open(raw, GRADIENT_STAGES * p.stage, GRADIENT_STAGES, GRADIENT_TMEM);
+  const Frame f = frame_open(raw, GRADIENT_STAGES * p.stage, GRADIENT_STAGES, p.tmem, GRADIENT_EPI_WARPS);
   if (!p.apart) pdl_wait();
   const int count = __ldcg(p.s.count + i), first = __ldcg(p.s.offset + i);
-  const int kb = (count + BLOCK_K - 1) / BLOCK_K;
+  const int kb = (count + BLOCK_K - 1) / BLOCK_K, parts = kb > GRADIENT_PART ? (kb + GRADIENT_PART - 1) / GRADIENT_PART : 1;
   if (warp == COPY_WARP) {
     const int tile0 = tiles_before(p.s, i);
     const uint32_t tx = A_BYTES + (p.cols > 64 ? 2 : 1) * BLOCK64_BYTES;
@@ -744,33 +748,63 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
   } else if (warp == MMA_WARP) {
     const uint32_t idesc = ptx::umma_idesc_bf16(TOKENS, p.cols) | 1u << 15 | 1u << 16;
     bool ok = true;
-    for (int k = 0; k < kb; ++k) {
-      const int s = k % GRADIENT_STAGES;
-      ok = ptx::mbar_wait_warp(&f.full[s], (k / GRADIENT_STAGES) & 1, f.abort_flag);
-      if (!ok) break;
-      ptx::tc_fence_after();
-      const uint32_t at = f.smem0 + s * p.stage;
-      if (ptx::elect_one()) {
-        issue(f.tmem, ptx::umma_desc_mn128(at, BLOCK64_BYTES), 2048 >> 4, ptx::umma_desc_mn128(at + A_BYTES, BLOCK64_BYTES), 2048 >> 4, idesc, BLOCK_K / 16, k == 0);
-        ptx::umma_commit(&f.empty[s]);
+    for (int part = 0; part < parts && ok; ++part) {
+      const int begin = part * GRADIENT_PART, end = begin + GRADIENT_PART < kb ? begin + GRADIENT_PART : kb;
+      if (part > 0) ok = ptx::mbar_wait_warp(f.drain + 1, (part - 1) & 1, f.abort_flag);      // (the part before has been read)
+      for (int k = begin; k < end && ok; ++k) {
+        const int s = k % GRADIENT_STAGES;
+        ok = ptx::mbar_wait_warp(&f.full[s], (k / GRADIENT_STAGES) & 1, f.abort_flag);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        const uint32_t at = f.smem0 + s * p.stage;
+        if (ptx::elect_one()) {
+          issue(f.tmem, ptx::umma_desc_mn128(at, BLOCK64_BYTES), 2048 >> 4, ptx::umma_desc_mn128(at + A_BYTES, BLOCK64_BYTES), 2048 >> 4, idesc, BLOCK_K / 16, k == begin);
+          ptx::umma_commit(&f.empty[s]);
+        }
+        __syncwarp();
       }
-      __syncwarp();
+      if (ok) {
+        if (ptx::elect_one()) ptx::umma_commit(f.done);
+        __syncwarp();
+      }
     }
-    if (ok) {
-      if (ptx::elect_one()) ptx::umma_commit(f.done);
-      __syncwarp();
-    } else {
-      mma_gave_up(f);
-    }
+    if (!ok) mma_gave_up(f);
   } else {
     const int col = c0 + warp * 32 + lane;
     const bool in = col < job.N;
-    if (ptx::mbar_wait(f.done, 0, f.abort_flag)) {
+    const uint32_t t_row = f.tmem + (static_cast<uint32_t>(warp * 32) << 16);
+    // columns c .. c + 15 of the part that is complete, and of those before it
+    const auto load_sum = [&](int part, int c, float* v) {
+      ptx::tmem_ld16(t_row + c, v);
+      ptx::tmem_ld_wait();
+      if (part > 0) {
+        float before[16];
+        ptx::tmem_ld16(t_row + GRADIENT_TMEM + c, before);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] += before[k];
+      }
+    };
+    bool ok = true;
+    for (int part = 0; part + 1 < parts && ok; ++part) {
+      ok = ptx::mbar_wait_warp(f.done, part & 1, f.abort_flag);
+      if (!ok) break;
       ptx::tc_fence_after();
       for (int c = 0; c < p.r; c += 16) {
         float v[16];
-        ptx::tmem_ld16(f.tmem + (static_cast<uint32_t>(warp * 32) << 16) + c, v);
-        ptx::tmem_ld_wait();
+        load_sum(part, c, v);
+        ptx::tmem_st16(t_row + GRADIENT_TMEM + c, v);
+      }
+      ptx::tmem_st_wait();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(f.drain + 1);
+    }
+    if (ok && ptx::mbar_wait(f.done, (parts - 1) & 1, f.abort_flag)) {
+      ptx::tc_fence_after();
+      for (int c = 0; c < p.r; c += 16) {
+        float v[16];
+        load_sum(parts - 1, c, v);
         if (kb == 0) {
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] = 0.f;
@@ -798,7 +832,7 @@ __global__ void __launch_bounds__(TC_THREADS) gradient_tc_kernel(const __grid_co
     }
     __syncwarp();
   }
-  frame_close(f, GRADIENT_TMEM, p.status);
+  frame_close(f, p.tmem, p.status);
   if (p.apart) pdl_wait();
 }
 
@@ -945,6 +979,7 @@ ffsplit_status launch_gradients_tc(ffsplit_ctx* ctx, const Gradient* jobs, int n
   GradientParams p;
   std::memset(&p, 0, sizeof(p));
   p.s = s; p.r = r; p.cols = round_up(r, 16); p.wide = r % 8 == 0; p.stage = stage_bytes(r); p.apart = apart ? 1 : 0; p.status = ctx->status();
+  p.tmem = s.T > static_cast<long long>(GRADIENT_PART) * BLOCK_K ? 2 * GRADIENT_TMEM : GRADIENT_TMEM;
   int blocks = 0;
   for (int i = 0; i < n; ++i) {
     GradientDev& d = p.job[i];

@@ -186,3 +186,26 @@ def test_beside_a_split_layer(ctx, act, dtype, T):
     # the layer's own output is what test_gpu_parity.py looks at; here it is the base, as it came
     L["base"] = alone.cpu()
     check({"Y": Y.cpu(), "dX": dX.cpu(), "dA": dA.cpu(), "dB": dB.cpu()}, L, dtype)
+
+
+@pytest.mark.parametrize("T,n,k,m,r", [((1 << 18) + 1, 1, 72, 64, 8), ((1 << 20) + 3, 1, 64, 72, 72), ((1 << 20) + 129, 3, 136, 64, 20), ((1 << 19) + 64, 2, 33, 130, 128)])
+def test_gradients_of_an_adapter_with_many_tokens(ctx, T, n, k, m, r):
+    """All terms have one sign: a running sum in the tensor cores, which cut what they add, would lose 6e-3 of 2^20 terms.  (The
+    tolerance is that of the other gradients: the parts' sums are in fp32.)"""
+    from paper_2401_04044_b200 import Projection
+    g = torch.Generator(device="cuda").manual_seed(T % 1000)
+    new = lambda s, *shape: ((torch.rand(*shape, generator=g, device="cuda") + 0.5) * s).bfloat16()  # noqa: E731
+    X, dY, A, B = new(1.0, T, k), new(1e-3, T, m), new(1.0 / k, n, k, r), new(1.0 / r, n, r, m)
+    index = torch.zeros(T, dtype=torch.int32, device="cuda")      # (nearly all of the first one's: not in one run where there are others)
+    index[5::1009] = n - 1
+    index[7::997] = -1
+    p, dA, dB = Projection(k, m, torch.bfloat16), torch.empty_like(A), torch.empty_like(B)
+    ctx.ensure_workspace(ctx.adapter_workspace_size(p, n, r, T))
+    ctx.adapter_backward(p, X, A, B, index, dY, dA=dA, dB=dB)
+    ctx.poll()
+    for i in range(n):
+        t = (index == i).nonzero().flatten()
+        x, d = X[t].double(), dY[t].double()
+        for got, ref in ((dA[i], x.t() @ (d @ B[i].double().t())), (dB[i], (x @ A[i].double()).t() @ d)):
+            err, big = float((got.double() - ref).norm()), float((got.double() - ref).abs().max())
+            assert err <= TOL["bf16"] * float(ref.norm()) and big <= 8 * TOL["bf16"] * float(ref.abs().max()), (i, err / float(ref.norm()))
