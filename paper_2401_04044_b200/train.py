@@ -204,6 +204,8 @@ def finetune(lib: Context, d: int, m: int, act: str = "swiglu", tokens: int = 51
     """Recovers a layer whose weights were rounded to eight levels: SGD, or orthogonalised momentum ("muon"; lr is then the step
     of its matrices, biases take SGD), on the mean squared distance between its outputs and those of the layer before
     rounding.  -> (losses, the layer's shape, its weights as a dict)"""
+    if optimizer not in ("sgd", "muon"):
+        raise ValueError(f"unknown optimizer {optimizer!r}: sgd or muon")
     gen = torch.Generator(device="cuda").manual_seed(seed)
     new = lambda scale, *s: (torch.randn(*s, generator=gen, device="cuda") * scale).to(dtype)  # noqa: E731
     gated = act == "swiglu"
@@ -292,14 +294,14 @@ def main(argv=None) -> None:
     ap.add_argument("--adapters", type=int, default=0, metavar="RANK")
     ap.add_argument("--lr", type=float, default=None, help="5 (sgd), 0.001 (muon), 0.02 (adapters)")
     a = ap.parse_args(argv)
+    lr = a.lr if a.lr is not None else 2e-2 if a.adapters else 5.0 if a.optimizer == "sgd" else 1e-3
     lib = Context(0)
     report = lambda i, l, n: print(f"step {i:3d}  loss {l:.5f}  gradient norm {n:.4f}")  # noqa: E731
     if a.adapters:
-        losses, _, _, factors = finetune_adapters(lib, a.d, a.m, a.act, a.adapters, a.tokens, a.steps, a.lr or 2e-2, report=report)
+        losses, _, _, factors = finetune_adapters(lib, a.d, a.m, a.act, a.adapters, a.tokens, a.steps, lr, report=report)
         print(f"loss {losses[0]:.5f} -> {losses[-1]:.5f}; two adapters of {sum(t[0].numel() for v in factors.values() for t in v)} elements each")
         return
-    losses, shape, W = finetune(lib, a.d, a.m, a.act, a.tokens, a.steps, a.lr or (5.0 if a.optimizer == "sgd" else 1e-3), optimizer=a.optimizer,
-                                report=report)
+    losses, shape, W = finetune(lib, a.d, a.m, a.act, a.tokens, a.steps, lr, optimizer=a.optimizer, report=report)
     # the tuned layer, split: a tenth of its neurons kept, the others left out
     T, m = 512, shape.m
     k = m // 10

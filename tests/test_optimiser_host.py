@@ -124,3 +124,22 @@ def test_clipping_counts_as_a_change_of_the_gradients():
     assert len(lib.lists) == 1 and all(p.grad._version > v for p, v in zip(params, before))
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         kept.backward()
+
+
+def test_an_unknown_optimiser_is_refused_and_a_rate_of_zero_is_taken(monkeypatch):
+    from paper_2401_04044_b200 import train
+    with pytest.raises(ValueError, match="adam"):
+        train.finetune(None, 8, 16, optimizer="adam")
+    rates = []
+
+    def record(lib, d, m, act, *rest, **kw):
+        rates.append(rest[-1])
+        raise InterruptedError
+
+    monkeypatch.setattr(train, "Context", lambda device: None)
+    monkeypatch.setattr(train, "finetune", record)
+    monkeypatch.setattr(train, "finetune_adapters", record)
+    for argv in (["--lr", "0"], ["--lr", "0", "--optimizer", "muon"], ["--lr", "0", "--adapters", "4"], ["--lr", "0.5"], [], ["--optimizer", "muon"], ["--adapters", "4"]):
+        with pytest.raises(InterruptedError):
+            train.main(argv)
+    assert rates == [0.0, 0.0, 0.0, 0.5, 5.0, 1e-3, 2e-2]
