@@ -14,6 +14,7 @@ pytestmark = pytest.mark.gpu
 def ctx():
     from paper_2401_04044_b200 import Context, build
     build.build()
+    torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < 100 << 30:
         pytest.skip("100 GB of device memory are needed")
     c = Context(0)
