@@ -107,3 +107,22 @@ def test_singular_values_close_together_in_fp32(ctx, rows, cols, kind):
     m = torch.randn(rows, cols, generator=g) if kind == "gauss" else torch.rand(rows, cols, generator=g)
     got, = orthogonalize(ctx, [m])
     near(got, orthogonal64(m.double().numpy()), TOL["f32"])
+
+
+def test_a_list_of_several_runs(ctx):
+    """More than the three gigabytes that are worked on at once, shapes in turn: every matrix has the bits that it has alone."""
+    g = torch.Generator(device="cuda").manual_seed(12)
+    shapes = [(3000, 9000), (9000, 3000), (40, 9000), (3000, 3100)] * 4
+    ms = [torch.randn(*s, generator=g, device="cuda").bfloat16() for s in shapes]
+    outs = [torch.empty_like(m) for m in ms]
+    lst = ctx.orthogonal_list(ms, outs)
+    each = sum(ctx.muon_workspace_size(ctx.orthogonal_list([m], [o])) - ctx.muon_workspace_size(ctx.orthogonal_list([], [])) for m, o in zip(ms, outs))
+    assert ctx.muon_workspace_size(lst) <= 3.1e9 < each
+    ctx.ensure_workspace(ctx.muon_workspace_size(lst))
+    ctx.orthogonalize(lst)
+    ctx.poll()
+    for m, o in zip(ms, outs):
+        alone = torch.empty_like(o)
+        ctx.orthogonalize(ctx.orthogonal_list([m], [alone]))
+        ctx.poll()
+        assert torch.equal(alone, o)
