@@ -463,9 +463,9 @@ ffsplit_status ffsplit_grad_clip(ffsplit_ctx* ctx, const ffsplit_grad_tensor* te
  *
  * Arithmetic: sums in fp32 and more.  X is kept in 22 bits.  Where the gradient is bf16, the operands of the products are
  * fp16 (11 bits); what is rounded off an operand perturbs X by a factor close to 1, not by a term, so small singular values
- * do not drown in it: X is off by 5e-4 to 3e-3 of its norm.  Where the gradient is fp32, or a side is above 2^18, operands
- * carry 22 bits too: 1e-7 to 5e-6 (plain fp32 products leave 1e-6 to 7e-6), for fp32 matrices with a side of 2^15 and more up
- * to 1.2e-5.  (A direction in which the matrix has less than 2^-22 of its norm is filled with what is rounded off X, times up
+ * do not drown in it: X is off by 5e-4 to 4e-3 of its norm (most where all singular values are alike).  Where the gradient
+ * is fp32, or a side is above 2^18, operands carry 22 bits too: 4e-7 to 6e-6 (plain fp32 products leave as much), for fp32
+ * matrices with a side of 2^15 and more up to 1.2e-5.  (A direction in which the matrix has less than 2^-22 of its norm is filled with what is rounded off X, times up
  * to 3.44^5: 1e-4 of the result for matrices of nearly lower rank.)  These figures are of the standard coefficients.  Matrices
  * with a side of at most 64 are worked on through their Gram matrix in fp64.  Momentum is fp32 whatever the type of the gradient.
  * Same inputs give the same bits, whatever else is in the list. */
@@ -481,7 +481,9 @@ typedef struct {
   float step, decay;          /* not looked at where weight is NULL */
 } ffsplit_muon_tensor;
 
-/* Workspace that the call below needs for this list (only shapes and types are looked at). */
+/* Workspace that the call below needs for this list (only shapes and types are looked at).  A matrix takes about 8 bytes an
+ * element, and 8 or 16 bytes an element of its square on the shorter side; a list is worked on in runs of up to 3 GB, and
+ * needs what its largest run does (one matrix at least).  Lists of single matrices need least. */
 ffsplit_status ffsplit_muon_workspace_size(const ffsplit_muon_tensor* tensors, int32_t count, size_t* bytes);
 
 /* One step for every matrix of the list (a host array, read before the call returns).  coefficients: host
@@ -520,7 +522,11 @@ ffsplit_status ffsplit_adapter_workspace_size(const ffsplit_projection* projecti
 
 /* Y dev [T, out] from X dev [T, in], T >= 1.  W dev [in, out] and bias dev [out] (may be NULL), or base dev [T, out] (may be
  * Y) with W and bias NULL, or none of them.  X A_i is summed in fp32 and, for FFSPLIT_BF16 and more than 64 tokens, rounded to
- * bf16 before it meets B_i (the tensor cores take both operands in one type).  An infinity or NaN in a token or in an
+ * bf16 before it meets B_i (the tensor cores take both operands in one type).  Where the adapters' part is a pass of its own
+ * (few tokens, outputs of less than 2^25 elements, tiles of 256 tokens of many adapters, factors that are not finite), X W +
+ * bias is rounded to bf16 before that part is added and the sum is rounded again: 2.3e-3 of the norm where one rounding leaves
+ * 1.7e-3.  bf16 sums over more than 2^18 features (in, or out for dX and D) lose up to 2^-27 of themselves a term where
+ * all terms have one sign; sums over tokens do not.  An infinity or NaN in a token or in an
  * adapter's factors reaches the rows (and gradients) of that token or adapter only.  Fastest where the tokens of an adapter
  * lie together.  Y may not overlap X, W or the factors.  Uses the workspace. */
 ffsplit_status ffsplit_adapter_forward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W,
@@ -535,7 +541,8 @@ typedef struct {
 } ffsplit_adapter_grads;
 
 /* dY dev [T, out].  W and base: as above, for dX (base dev [T, in], may be dX); neither is looked at where dX is not
- * wanted.  No gradient may overlap another or an input (but base).  Sums are taken in a fixed order: same inputs give the
+ * wanted.  No gradient may overlap another or an input (but base).  X A_i and dY B_i^T, and dY W^T before the adapters' part
+ * is added to it, are rounded as above.  Sums are taken in a fixed order: same inputs give the
  * same bits, whichever gradients are asked for. */
 ffsplit_status ffsplit_adapter_backward(ffsplit_ctx* ctx, const ffsplit_projection* projection, const void* W,
                                         const void* base, const ffsplit_adapters* adapters, const void* X, int64_t T,

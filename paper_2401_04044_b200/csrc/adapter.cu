@@ -522,7 +522,7 @@ bool on_tensor_cores(const ffsplit_projection& p, int n, long long T) {
 bool is_sorted(long long T) { return T > adapter::FEW; }
 
 // Ranges of K of the products on the CUDA cores: two blocks to an SM (as many as fit: a few more take twice as long), 64
-// elements each at least.
+// elements each at least.  (148 SMs: the size of the workspace goes by this, and is asked for without a context.)
 int tokens_per_block(const ffsplit_projection& p, int n, long long T) {
   if (T > adapter::FEW) return p.dtype == FFSPLIT_F32 ? adapter::MANY : adapter::SOME;      // (bf16: 65000 adapters and more)
   return n == 1 ? adapter::SOME : 1;

@@ -625,8 +625,8 @@ struct Group {
 };
 // Two iterations at once, where P2 P stays below 200 (see coefficients_hold()).  The second one's S is P S P (all of these are
 // polynomials in S), so X need not be formed between the two: X <- (P2 P) X with P2 = a I + b S2 + c S2 S2, S2 = (P S) P.
-// 3 p^2 q + 5 p^3 multiply-adds instead of 6 p^2 q + 2 p^3, and X is read and written once instead of twice; for two roundings
-// more, which leave up to 3e-3 of the result instead of 2e-3.  Small matrices would pay for one launch more (256 x 1024: 50 us
+// 3 p^2 q + 5 p^3 operations instead of 6 p^2 q + 2 p^3, and X is read and written once instead of twice; for two roundings
+// more, which leave up to 4e-3 of the result instead of 3e-3 (512 x 2000, all singular values alike: 3.8e-3).  Small matrices would pay for one launch more (256 x 1024: 50 us
 // for a pair either way).
 bool in_pairs(int rows, int cols, bool precise) {
   const int p = rows < cols ? rows : cols, q = rows < cols ? cols : rows;

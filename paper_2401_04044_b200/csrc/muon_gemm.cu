@@ -8,13 +8,13 @@
 // is staged K-major or MN-major (a bit of the instruction descriptor and the shape of the TMA box).
 //
 // S and S S are symmetric: only tiles on and above the diagonal are computed, the others are written by their mirror images
-// (of 3 p^2 q + 2 p^3 multiply-adds per iteration, p <= q, (p^2 q + p^3) / 2 go).
+// (of 4 p^2 q + 2 p^3 operations per iteration, p <= q, p^2 q + p^3 go).
 //
 // Operands are fp16 (11 bits; bf16 has 8 at the same rate).  Rounding S or P multiplies X by a matrix close to the identity,
 // which the iteration corrects or carries along as it is.  Rounding X would add noise in every direction, and directions
 // with small singular values would drown in what is rounded off the large ones (a momentum with a few strong directions: 1e-2
 // of the result, with bf16 8e-2).  So X has a second plane for the next 11 bits.  a is added to the diagonal of P, so that the
-// tensor cores form a X + P X from the first plane, and the epilogue adds a times the second: 6e-4 to 2e-3, for 2 bytes read and
+// tensor cores form a X + P X from the first plane, and the epilogue adds a times the second: 5e-4 to 4e-3, for 2 bytes read and
 // written per element.  precise: the tensor cores take the second planes of all operands (three products of planes, the small
 // ones first), and sums leave them every few k-blocks, because their running sums are cut, not rounded (see train_gemm.cu).
 //
